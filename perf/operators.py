@@ -221,7 +221,7 @@ def _layer(s, bases):
     R = max(ranks)
     cols = torch.tensor([h * R + c for h, r in enumerate(ranks) for c in range(r)], device="cuda")
     for x in range(0, n, 8192):          # a prompt arrives in chunks
-        part = [s[side][:, x:x + 8192].reshape(B, -1, H * R) for side in "KV"]
+        part = [s[side][:, x:x + 8192].reshape(B, -1, H * R).contiguous() for side in "KV"]
         lay.append_kv(*[p if len(cols) == H * R else p[:, :, cols] for p in part], preprojected=True)
     if case["ragged"]:
         lay.set_lens(_lens(case))
