@@ -252,6 +252,70 @@ ea_status eigen_attn_quant_lens(eigen_attn_t h, int32_t* qlens);
 ea_status eigen_attn_quant_layout(eigen_attn_t h, int32_t head, size_t* slab_offset, size_t* block_bytes,
                                   size_t* k_scale_offset, size_t* v_code_offset, size_t* v_scale_offset);
 
+/* Speculative decoding (the generation phase of Section 2 with several drafted tokens at a time): attention of T <= 64
+ * drafted tokens per sequence, arranged as a tree, over the cached rows and over each other.
+ * decode_tree projects the drafted keys and values (d_k, d_v: [B][T][H][d_head]) and writes them behind every sequence's
+ * own rows, at rows len_b .. len_b + T - 1, WITHOUT changing the length: the calls that follow see the cache as it was,
+ * and overwrite those rows.  Drafted token t attends all cached rows of its sequence and the drafted tokens s whose bit s
+ * is set in d_mask[b][t] (DEVICE uint64 [B][T]; bits from T on are ignored; a tree sets a token's own bit and its
+ * ancestors').  A token whose mask is empty attends the cached rows alone; with no cached row either its output is zero.
+ * A masked token takes no part, whatever its rows hold.  d_q, d_out: [B][T][H * group][d_head] with element strides
+ * (batch, token), query head hq = kv_head * group + i as in eigen_attn_decode_gqa, 1 <= group <= 16.  Lengths may be zero
+ * and may differ (eigen_attn_set_lens); a page table is followed; both dtypes; every rank and d_head.  An ALiBi bias counts
+ * positions: drafted token t sits at len_b + (number of other tokens in its mask); only with group 1.  Not with a rotary
+ * embedding (EA_ERR_UNSUPPORTED).  flags: EA_Q_PREPROJECTED (d_q: packed [B][T][group * sum rp_k], head h at group *
+ * offs_k[h], query head i of its group rp_k[h] further each), EA_KV_PREPROJECTED, EA_OUT_LOWRANK (packed like q with rp_v).
+ * The call can be captured into a CUDA graph; replays use the lengths of the capture and the mask's present contents.
+ *
+ * tree_bytes:   size of the scratch for max_tokens (1..64) drafted tokens and `group` query heads per K/V head.
+ * tree_attach:  hands the library that DEVICE buffer (256-byte aligned, owned by the caller); NULL detaches.  Calls of one
+ *               handle share it, as they share the workspace.
+ * tree_commit:  accepts one path per sequence after the drafted tokens were verified: h_paths HOST int32 [B][T], the first
+ *               h_counts[b] entries of row b strictly ascending token numbers (parents come before their children); the
+ *               rows of these tokens move to rows len_b, len_b + 1, ..., and the sequence's length grows by h_counts[b]
+ *               (0 = nothing accepted).  T: the tokens of the decode_tree call.  The arrays may be reused when the call
+ *               returns.  Lengths that come to differ are uploaded as by eigen_attn_set_lens; not during stream capture
+ *               (EA_ERR_UNSUPPORTED). */
+ea_status eigen_attn_tree_bytes(eigen_attn_t h, int32_t max_tokens, int32_t group, size_t* bytes);
+ea_status eigen_attn_tree_attach(eigen_attn_t h, int32_t max_tokens, int32_t group, void* d_buf, size_t bytes);
+ea_status eigen_attn_decode_tree(eigen_attn_t h, const void* d_q, int64_t stride_b_q, int64_t stride_t_q, int32_t group,
+                                 const void* d_k, const void* d_v, int64_t stride_b_kv, int64_t stride_t_kv, int32_t T,
+                                 const uint64_t* d_mask, void* d_out, int64_t stride_b_out, int64_t stride_t_out,
+                                 uint32_t flags, void* cuda_stream);
+ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const int32_t* h_counts, int32_t T, void* cuda_stream);
+
+/* Decode over a selection of blocks (long contexts: the generation phase is limited by the bytes of K' and V', Section 2).
+ * The rows of a sequence are cut into blocks of block_rows; for every complete block the library keeps the minimum and
+ * the maximum of each channel of its keys.  For a query the score of a block is an upper bound on the scores of its rows,
+ *     ( sum_c max(q'_c lo_c, q'_c hi_c) ) / sqrt(d_head)  [ - slope * (len_b - 1 - last row of the block) with ALiBi ],
+ * the largest over the query heads of the group, worked out in 64 bits.  A sequence of more than n_blocks blocks (the last
+ * one possibly incomplete) attends its first `sink` and newest `recent` blocks and, of the others, the n_blocks - sink -
+ * recent with the highest score (equal scores: the lower block); a shorter one attends everything.  Cached rows are taken
+ * to be finite.
+ *
+ * sparse_bytes:  size of the caller's buffer (bounds and the call's scratch) for blocks of 16, 32, 64 or 128 rows.
+ * sparse_attach: hands over that DEVICE buffer (256-byte aligned, owned by the caller); no block has bounds yet.  NULL
+ *                detaches.  Synchronises `cuda_stream`.
+ * sparse_sync:   bounds of every complete block that has none yet; asynchronous.  Call it after rows were added:
+ *                decode_sparse refuses (EA_ERR_INVALID_ARG) while a block it would have to score has no bounds.
+ * sparse_lens:   rows covered by bounds per sequence: HOST [batch].  Shortening a sequence (set_len, set_lens) forgets the
+ *                bounds of the blocks it no longer fills; changing the page table forgets all.
+ * sparse_layout: where head `head`'s bounds live: byte offset of its slab [B][seq_blocks][2][rp_k] in the cache dtype
+ *                (minima, then maxima); with a page table the slab is indexed by the physical row / block_rows.
+ * decode_sparse: one query per sequence and query head as in eigen_attn_decode_gqa (group 1 = eigen_attn_decode); both
+ *                dtypes, every rank and d_head, unequal lengths, page table (sequences of at most n_max rows), ALiBi with
+ *                group 1; not with a rotary embedding (EA_ERR_UNSUPPORTED).  d_index: DEVICE int32 [B][H][n_blocks] that
+ *                receives the blocks attended, ascending, -1 behind the last; or NULL.  flags: EA_Q_PREPROJECTED,
+ *                EA_OUT_LOWRANK (packed as in eigen_attn_decode_tree). */
+ea_status eigen_attn_sparse_bytes(eigen_attn_t h, int32_t block_rows, size_t* bytes);
+ea_status eigen_attn_sparse_attach(eigen_attn_t h, int32_t block_rows, void* d_buf, size_t bytes, void* cuda_stream);
+ea_status eigen_attn_sparse_sync(eigen_attn_t h, void* cuda_stream);
+ea_status eigen_attn_sparse_lens(eigen_attn_t h, int32_t* lens);
+ea_status eigen_attn_sparse_layout(eigen_attn_t h, int32_t head, size_t* slab_offset, int32_t* seq_blocks);
+ea_status eigen_attn_decode_sparse(eigen_attn_t h, const void* d_q, int64_t stride_b_q, int32_t group, int32_t n_blocks,
+                                   int32_t sink, int32_t recent, void* d_out, int64_t stride_b_out, int32_t* d_index,
+                                   uint32_t flags, void* cuda_stream);
+
 /* Current number of cached rows; set_len truncates or rewinds (0 <= len <= n_max), e.g. to re-run
  * a step at a fixed context length.  Rows beyond the previous length hold whatever was last written. */
 ea_status eigen_attn_get_len(eigen_attn_t h, int32_t* len);

@@ -83,6 +83,16 @@ SYMBOLS = {
     "eigen_attn_quant_len": (_i32, [_vp, ctypes.POINTER(_i32)]),
     "eigen_attn_quant_lens": (_i32, [_vp, ctypes.POINTER(_i32)]),
     "eigen_attn_quant_layout": (_i32, [_vp, _i32] + [ctypes.POINTER(_sz)] * 5),
+    "eigen_attn_tree_bytes": (_i32, [_vp, _i32, _i32, ctypes.POINTER(_sz)]),
+    "eigen_attn_tree_attach": (_i32, [_vp, _i32, _i32, _vp, _sz]),
+    "eigen_attn_decode_tree": (_i32, [_vp, _vp, _i64, _i64, _i32, _vp, _vp, _i64, _i64, _i32, _vp, _vp, _i64, _i64, _u32, _vp]),
+    "eigen_attn_tree_commit": (_i32, [_vp, ctypes.POINTER(_i32), ctypes.POINTER(_i32), _i32, _vp]),
+    "eigen_attn_sparse_bytes": (_i32, [_vp, _i32, ctypes.POINTER(_sz)]),
+    "eigen_attn_sparse_attach": (_i32, [_vp, _i32, _vp, _sz, _vp]),
+    "eigen_attn_sparse_sync": (_i32, [_vp, _vp]),
+    "eigen_attn_sparse_lens": (_i32, [_vp, ctypes.POINTER(_i32)]),
+    "eigen_attn_sparse_layout": (_i32, [_vp, _i32, ctypes.POINTER(_sz), ctypes.POINTER(_i32)]),
+    "eigen_attn_decode_sparse": (_i32, [_vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _u32, _vp]),
     "eigen_attn_launch_count": (_i32, [_vp, ctypes.POINTER(ctypes.c_uint64)]),
     "eigen_attn_set_decode_events": (_i32, [_vp, _vp, _vp]),
     "eigen_attn_version": (_i32, []),
@@ -455,6 +465,148 @@ class EigenAttnLayer:
         self._check(lib.eigen_attn_decode_gqa(self.handle, q.data_ptr(), q.stride(0), int(group), out.data_ptr(),
                                               out.stride(0), _stream_ptr(stream)), "eigen_attn_decode_gqa")
         return out
+
+    # -- a tree of drafted tokens per sequence
+    def tree_attach(self, max_tokens: int, group: int = 1) -> torch.Tensor:
+        """Allocates the scratch for trees of up to `max_tokens` drafted tokens (kept on the layer) and attaches it."""
+        n = _sz(0)
+        self._check(lib.eigen_attn_tree_bytes(self.handle, int(max_tokens), int(group), ctypes.byref(n)), "eigen_attn_tree_bytes")
+        self.tree_buf = device_alloc(n.value, self.device)
+        self._check(lib.eigen_attn_tree_attach(self.handle, int(max_tokens), int(group), self.tree_buf.data_ptr(), n.value),
+                    "eigen_attn_tree_attach")
+        return self.tree_buf
+
+    def tree_detach(self) -> None:
+        self._check(lib.eigen_attn_tree_attach(self.handle, 0, 0, None, 0), "eigen_attn_tree_attach")
+        self.tree_buf = None
+
+    def _mq_tok(self, x: torch.Tensor, T: int, heads: int):
+        """Checks a [B][T][heads][d_head] tensor and returns (ptr, stride_b, stride_t)."""
+        assert x.is_cuda and x.dtype == self.torch_dtype and x.shape == (self.B, T, heads, self.d_head)
+        assert x.stride(3) == 1 and x.stride(2) == self.d_head
+        return x.data_ptr(), x.stride(0), x.stride(1)
+
+    def decode_tree(self, q, k, v, mask: torch.Tensor, group: int = 1, out: Optional[torch.Tensor] = None,
+                    q_preprojected: bool = False, kv_preprojected: bool = False, out_lowrank: bool = False,
+                    stream=None) -> torch.Tensor:
+        """eigen_attn_decode_tree: q [B][T][H * group][d_head], k, v [B][T][H][d_head], mask int64 [B][T] (bit s: token t
+        attends drafted token s).  The drafted rows land behind each sequence's own; the lengths stay."""
+        B, T = mask.shape
+        assert mask.is_cuda and mask.dtype == torch.int64 and mask.is_contiguous() and B == self.B
+        flags = 0
+        if q_preprojected:
+            flags |= EA_Q_PREPROJECTED
+            pq, sbq, stq = self._packed(q, T, group * self.offs_k[-1]), 0, 0
+        else:
+            pq, sbq, stq = self._mq_tok(q, T, self.H * group)
+        if kv_preprojected:
+            flags |= EA_KV_PREPROJECTED
+            pk, pv, sbk, stk = self._packed(k, T, self.offs_k[-1]), self._packed(v, T, self.offs_v[-1]), 0, 0
+        else:
+            pk, sbk, stk = self._mq_tok(k, T, self.H)
+            pv, sbv, stv = self._mq_tok(v, T, self.H)
+            if (sbk, stk) != (sbv, stv):
+                k, v = k.contiguous(), v.contiguous()
+                pk, sbk, stk = self._mq_tok(k, T, self.H)
+                pv = v.data_ptr()
+        if out_lowrank:
+            flags |= EA_OUT_LOWRANK
+            if out is None:
+                out = self._new_out(self.B, T, group * self.offs_v[-1])
+            po, sbo, sto = self._packed(out, T, group * self.offs_v[-1]), 0, 0
+        else:
+            if out is None:
+                out = self._new_out(self.B, T, self.H * group, self.d_head)
+            po, sbo, sto = self._mq_tok(out, T, self.H * group)
+        with torch.cuda.device(self.device):
+            self._check(lib.eigen_attn_decode_tree(self.handle, pq, sbq, stq, int(group), pk, pv, sbk, stk, T, mask.data_ptr(),
+                                                   po, sbo, sto, flags, _stream_ptr(stream)), "eigen_attn_decode_tree")
+        return out
+
+    def tree_commit(self, paths, T: int, stream=None) -> None:
+        """eigen_attn_tree_commit: paths[b] = accepted tokens of sequence b, ascending (empty: none); T as in decode_tree."""
+        assert len(paths) == self.B
+        arr = (ctypes.c_int32 * (self.B * T))()
+        counts = (ctypes.c_int32 * self.B)()
+        for b, path in enumerate(paths):
+            assert len(path) <= T
+            counts[b] = len(path)
+            arr[b * T:b * T + len(path)] = [int(x) for x in path]
+        with torch.cuda.device(self.device):
+            self._check(lib.eigen_attn_tree_commit(self.handle, arr, counts, int(T), _stream_ptr(stream)), "eigen_attn_tree_commit")
+
+    # -- decode over a selection of blocks
+    def sparse_attach(self, block_rows: int, stream=None) -> torch.Tensor:
+        """Allocates the buffer for block bounds (kept on the layer) and attaches it."""
+        n = _sz(0)
+        self._check(lib.eigen_attn_sparse_bytes(self.handle, int(block_rows), ctypes.byref(n)), "eigen_attn_sparse_bytes")
+        self.sparse_buf = device_alloc(n.value, self.device)
+        self.sparse_block = int(block_rows)
+        with torch.cuda.device(self.device):
+            self._check(lib.eigen_attn_sparse_attach(self.handle, int(block_rows), self.sparse_buf.data_ptr(), n.value,
+                                                     _stream_ptr(stream)), "eigen_attn_sparse_attach")
+        return self.sparse_buf
+
+    def sparse_detach(self, stream=None) -> None:
+        self._check(lib.eigen_attn_sparse_attach(self.handle, 0, None, 0, _stream_ptr(stream)), "eigen_attn_sparse_attach")
+        self.sparse_buf = None
+
+    def sparse_sync(self, stream=None) -> None:
+        with torch.cuda.device(self.device):
+            self._check(lib.eigen_attn_sparse_sync(self.handle, _stream_ptr(stream)), "eigen_attn_sparse_sync")
+
+    def sparse_lens(self):
+        arr = (ctypes.c_int32 * self.B)()
+        self._check(lib.eigen_attn_sparse_lens(self.handle, arr), "eigen_attn_sparse_lens")
+        return list(arr)
+
+    def sparse_bounds(self, head: Optional[int] = None) -> torch.Tensor:
+        """View of head `head`'s bounds [B][blocks][2][rp_k] (minima, maxima); of all heads, [H][B][blocks][2][rp_k], with
+        None (heads of one rank)."""
+        def layout(h):
+            off, blocks = _sz(0), ctypes.c_int32(0)
+            self._check(lib.eigen_attn_sparse_layout(self.handle, h, ctypes.byref(off), ctypes.byref(blocks)),
+                        "eigen_attn_sparse_layout")
+            return off.value, blocks.value
+        flat = self.sparse_buf.view(self.torch_dtype)
+        es = flat.element_size()
+        off, blocks = layout(0 if head is None else int(head))
+        rp = self.cache_layout(0 if head is None else int(head))[2]
+        one = flat.as_strided((self.B, blocks, 2, rp), (blocks * 2 * rp, 2 * rp, rp, 1), flat.storage_offset() + off // es)
+        if head is not None or self.H == 1:
+            return one if head is not None else one[None]
+        assert all(self.cache_layout(h)[2] == rp for h in range(self.H))
+        step = (layout(1)[0] - off) // es
+        return flat.as_strided((self.H,) + tuple(one.shape), (step,) + tuple(one.stride()), one.storage_offset())
+
+    def decode_sparse(self, q: torch.Tensor, n_blocks: int, group: int = 1, sink: int = 1, recent: int = 1,
+                      out: Optional[torch.Tensor] = None, q_preprojected: bool = False, out_lowrank: bool = False,
+                      return_index: bool = False, stream=None):
+        """eigen_attn_decode_sparse: q [B][1][H * group][d_head] over the n_blocks blocks with the highest score bound (the
+        first `sink` and the newest `recent` among them).  With return_index also the blocks, int32 [B][H][n_blocks]."""
+        flags = 0
+        if q_preprojected:
+            flags |= EA_Q_PREPROJECTED
+            pq, sbq = self._packed(q, 1, group * self.offs_k[-1]), group * self.offs_k[-1]
+        else:
+            pq, sbq, _ = self._mq_tok(q, 1, self.H * group)
+        if out_lowrank:
+            flags |= EA_OUT_LOWRANK
+            if out is None:
+                out = self._new_out(self.B, 1, group * self.offs_v[-1])
+            po, sbo = self._packed(out, 1, group * self.offs_v[-1]), group * self.offs_v[-1]
+        else:
+            if out is None:
+                out = self._new_out(self.B, 1, self.H * group, self.d_head)
+            po, sbo, _ = self._mq_tok(out, 1, self.H * group)
+        index = None
+        if return_index:
+            index = device_alloc(4 * self.B * self.H * int(n_blocks), self.device).view(torch.int32).view(self.B, self.H, int(n_blocks))
+        with torch.cuda.device(self.device):
+            self._check(lib.eigen_attn_decode_sparse(self.handle, pq, sbq, int(group), int(n_blocks), int(sink), int(recent), po,
+                                                     sbo, index.data_ptr() if index is not None else None, flags,
+                                                     _stream_ptr(stream)), "eigen_attn_decode_sparse")
+        return (out, index) if return_index else out
 
     def set_rope(self, base: float, interleaved: bool = False, stream=None) -> None:
         """Rotary position embedding for decode (Section 4.3); base 0 switches it off."""

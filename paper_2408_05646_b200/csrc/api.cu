@@ -227,6 +227,14 @@ bool encode_input_maps(const void* const ptrs[3], int H, int d_head, int T, int 
   return true;
 }
 
+// The caller's buffer of eigen_attn_sparse_attach: slab offsets per head, the bounds of every block, and the scratch of a
+// decode_sparse call.
+struct SparseLayout {
+  std::vector<int64_t> slab;   // [H]
+  int seq_blocks = 0;          // blocks of one sequence's slab
+  size_t off_q64 = 0, off_qp = 0, off_scores = 0, off_list = 0, off_part = 0, slots = 0, bytes = 0;
+};
+
 }  // namespace
 
 struct eigen_attn {
@@ -261,6 +269,16 @@ struct eigen_attn {
   std::vector<int32_t> qlens;   // [B]: rows of each sequence held as codes, kept (and uploaded) while lengths differ
   int q_max_stage_bytes = 0;
   std::vector<ea::QuantHead> qheads;
+  // scratch for trees of drafted tokens (eigen_attn_tree_attach)
+  char* tree_buf = nullptr;
+  int tree_rows = 0;      // tokens * group it was sized for
+  size_t tree_slots = 0;  // partials it holds
+  size_t tree_off_part = 0;
+  // block bounds of the cached keys (eigen_attn_sparse_attach)
+  char* sp_buf = nullptr;
+  int sp_shift = 0;       // log2 of the rows of a block
+  SparseLayout sp;
+  std::vector<int32_t> sp_len;   // [B]: rows of each sequence whose blocks have bounds (a multiple of the block)
   char err[256];
 };
 
@@ -313,6 +331,44 @@ ea_status check_quant_args(eigen_attn_t h, const char* who, int32_t bits, int32_
   return EA_OK;
 }
 
+constexpr int kMaxGroup = 16;
+constexpr size_t kMqSlots = 16384;       // partials that every scratch holds at least, so that few query rows can be split
+
+size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t* slots) {
+  const size_t units = static_cast<size_t>(h->desc.batch) * h->desc.n_heads;
+  const size_t off = align_up(units * rows * h->L.max_rp_k * sizeof(float));
+  const size_t n = units * rows > kMqSlots ? units * rows : kMqSlots;
+  if (off_part) *off_part = off;
+  if (slots) *slots = n;
+  return align_up(off + n * h->L.part_stride * sizeof(float));
+}
+
+void make_sparse_layout(const eigen_attn* h, int block_rows, SparseLayout* S) {
+  const int H = h->desc.n_heads;
+  const size_t B = h->desc.batch, units = B * H;
+  S->seq_blocks = (h->desc.n_max + block_rows - 1) / block_rows;
+  S->slab.resize(H);
+  size_t off = align_up(sizeof(int64_t) * H);
+  for (int i = 0; i < H; ++i) {
+    S->slab[i] = static_cast<int64_t>(off);
+    off = align_up(off + B * S->seq_blocks * 2 * h->L.heads[i].rp_k * h->L.es);
+  }
+  S->off_q64 = off;    off = align_up(off + units * kMaxGroup * h->L.max_rp_k * sizeof(double));
+  S->off_qp = off;     off = align_up(off + units * kMaxGroup * h->L.max_rp_k * sizeof(float));
+  S->off_scores = off; off = align_up(off + units * S->seq_blocks * sizeof(double));
+  S->off_list = off;   off = align_up(off + units * S->seq_blocks * sizeof(int32_t));
+  S->slots = units * kMaxGroup > kMqSlots ? units * kMaxGroup : kMqSlots;
+  S->off_part = off;   off = align_up(off + S->slots * h->L.part_stride * sizeof(float));
+  S->bytes = off;
+}
+
+// Rows past a sequence's new length are forgotten, and with them the bounds of the block they ended in.
+void clamp_sparse(eigen_attn* h, int b, int32_t len) {
+  if (!h->sp_buf) return;
+  const int32_t whole = len >> h->sp_shift << h->sp_shift;
+  if (h->sp_len[b] > whole) h->sp_len[b] = whole;
+}
+
 const HeadInfo* dev_heads(eigen_attn_t h) { return reinterpret_cast<const HeadInfo*>(h->ws + h->L.off_heads); }
 const float* dev_basis(eigen_attn_t h) { return reinterpret_cast<const float*>(h->ws + h->L.off_basis); }
 int* dev_status(eigen_attn_t h) { return reinterpret_cast<int*>(h->ws + h->L.off_status); }
@@ -340,6 +396,19 @@ const int32_t* dev_deficit(eigen_attn_t h) {
 }
 int* dev_counters(eigen_attn_t h) { return reinterpret_cast<int*>(h->ws + h->L.off_counters); }
 
+// T rows projected (or copied) behind every sequence's own; the caller has checked the room and advances the length.
+cudaError_t launch_append_rows(eigen_attn_t h, const void* d_k, const void* d_v, int32_t T, int64_t stride_b,
+                               int64_t stride_t, uint32_t flags, cudaStream_t s) {
+  ea::ProjectParams p{};
+  p.heads = dev_heads(h); p.basis = dev_basis(h); p.k = d_k; p.v = d_v; p.cache = h->cache;
+  p.stride_b = stride_b; p.stride_t = stride_t;
+  p.B = h->desc.batch; p.T = T; p.H = h->desc.n_heads; p.d_head = h->desc.d_head;
+  p.n_max = h->desc.n_max; p.row0 = h->len; p.deficit = dev_deficit(h); p.flags = flags;
+  p.lr_k_width = h->L.sum_rp_k; p.lr_v_width = h->L.sum_rp_v;
+  p.pages = dev_pages(h);
+  return ea::launch_project_append(p, h->desc.dtype, s, &h->launches);
+}
+
 ea_status do_append(eigen_attn_t h, const void* d_k, const void* d_v, int32_t T, int64_t stride_b,
                     int64_t stride_t, uint32_t flags, cudaStream_t s) {
   if (!d_k || !d_v) return fail(h, EA_ERR_INVALID_ARG, "append_kv: NULL k or v");
@@ -349,14 +418,7 @@ ea_status do_append(eigen_attn_t h, const void* d_k, const void* d_v, int32_t T,
   if (!room_for(h, T, &bad))
     return fail(h, EA_ERR_CAPACITY, "append_kv: T %d more rows exceed the capacity of sequence %d (%lld rows)", T, bad,
                 static_cast<long long>(capacity_of(h, bad)));
-  ea::ProjectParams p{};
-  p.heads = dev_heads(h); p.basis = dev_basis(h); p.k = d_k; p.v = d_v; p.cache = h->cache;
-  p.stride_b = stride_b; p.stride_t = stride_t;
-  p.B = h->desc.batch; p.T = T; p.H = h->desc.n_heads; p.d_head = h->desc.d_head;
-  p.n_max = h->desc.n_max; p.row0 = h->len; p.deficit = dev_deficit(h); p.flags = flags;
-  p.lr_k_width = h->L.sum_rp_k; p.lr_v_width = h->L.sum_rp_v;
-  p.pages = dev_pages(h);
-  const cudaError_t e = ea::launch_project_append(p, h->desc.dtype, s, &h->launches);
+  const cudaError_t e = launch_append_rows(h, d_k, d_v, T, stride_b, stride_t, flags, s);
   if (e != cudaSuccess) return cuda_fail(h, e, "append_kv launch");
   h->len += T;
   return EA_OK;
@@ -1025,6 +1087,7 @@ ea_status eigen_attn_set_len(eigen_attn_t h, int32_t len) {
       if (h->qlens[b] < h->qlen) h->qlen = h->qlens[b];
   h->len = len;
   h->max_deficit = 0;     // every sequence holds len rows again
+  for (int b = 0; b < h->desc.batch; ++b) clamp_sparse(h, b, len);
   if (h->q_group && h->qlen > len) h->qlen = len / h->q_group * h->q_group;   // rows past len are forgotten
   return EA_OK;
 }
@@ -1077,6 +1140,7 @@ ea_status eigen_attn_set_lens(eigen_attn_t h, const int32_t* lens, void* cuda_st
   h->deficit.swap(deficit);
   h->len = longest;
   h->max_deficit = widest;
+  for (int b = 0; b < B; ++b) clamp_sparse(h, b, lens[b]);
   return EA_OK;
 }
 
@@ -1088,6 +1152,7 @@ ea_status eigen_attn_set_page_table(eigen_attn_t h, const int32_t* h_table, int3
     int64_t longest = h->len;
     if (longest > h->desc.n_max) return fail(h, EA_ERR_CAPACITY, "set_page_table: len %d exceeds n_max %d", h->len, h->desc.n_max);
     h->paged = false;
+    for (int b = 0; b < B; ++b) clamp_sparse(h, b, 0);      // a sequence's rows are other ones now
     return EA_OK;
   }
   if (h->q_group) return fail(h, EA_ERR_UNSUPPORTED, "set_page_table: not available with a quantised cache");
@@ -1123,6 +1188,7 @@ ea_status eigen_attn_set_page_table(eigen_attn_t h, const int32_t* h_table, int3
   h->page_shift = 0;
   while ((1 << h->page_shift) < page_rows) ++h->page_shift;
   h->page_cap.swap(cap);
+  for (int b = 0; b < B; ++b) clamp_sparse(h, b, 0);        // a sequence's rows are other ones now
   return EA_OK;
 }
 
@@ -1185,6 +1251,7 @@ ea_status eigen_attn_set_alibi(eigen_attn_t h, const float* slopes, void* cuda_s
     const float sl = slopes ? slopes[i] : 0.f;
     if (!(sl >= 0.f) || !isfinite(sl)) return fail(h, EA_ERR_INVALID_ARG, "set_alibi: slope[%d] = %g", i, sl);
     h->L.heads[i].alibi_slope2 = static_cast<float>(static_cast<double>(sl) * 1.4426950408889634);
+    h->L.heads[i].alibi_slope = sl;
     any = any || sl != 0.f;
   }
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
@@ -1278,6 +1345,337 @@ ea_status eigen_attn_decode_gqa(eigen_attn_t h, const void* d_q, int64_t stride_
   if (h->ev_stop) cudaEventRecord(h->ev_stop, s);
   if (e != cudaSuccess) return cuda_fail(h, e, "decode_gqa launch");
   return EA_OK;
+}
+
+// ---- a tree of drafted tokens, and decode over a selection of blocks
+
+namespace {
+
+// What both calls ask of the layer and of the query heads.
+ea_status check_mq(eigen_attn_t h, const char* who, int32_t group) {
+  if (group < 1 || group > kMaxGroup) return fail(h, EA_ERR_SHAPE, "%s: group %d (1..%d)", who, group, kMaxGroup);
+  if (h->rope) return fail(h, EA_ERR_UNSUPPORTED, "%s: not available with a rotary embedding", who);
+  if (h->alibi && group > 1)
+    return fail(h, EA_ERR_UNSUPPORTED, "%s: an ALiBi bias is per K/V head: not available with group %d", who, group);
+  return EA_OK;
+}
+
+// The launches behind the query projection: attention over p's rows, then the merge of its pieces with the lift.
+// `slots`: partials the scratch holds.
+ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size_t slots, cudaStream_t s) {
+  const Layout& L = h->L;
+  p.heads = dev_heads(h); p.basis = dev_basis(h); p.cache = h->cache;
+  p.deficit = dev_deficit(h); p.pages = dev_pages(h);
+  p.B = h->desc.batch; p.H = h->desc.n_heads; p.d_head = h->desc.d_head;
+  p.n = h->len; p.n_max = h->desc.n_max;
+  p.rows = p.tokens * p.group;
+  p.q_stride = L.max_rp_k; p.part_stride = L.part_stride; p.lr_v_width = L.sum_rp_v;
+  // CTAs per run of eight query rows: waves of resident CTAs, a start-up worth a tile or two per CTA, and room for the
+  // partials
+  const int64_t ctas = static_cast<int64_t>(p.B) * p.H * ((p.rows + 7) / 8);
+  int64_t cap = static_cast<int64_t>(slots) / (static_cast<int64_t>(p.B) * p.H * p.rows);
+  if (cap > p.tiles) cap = p.tiles;
+  if (cap > 65535) cap = 65535;
+  if (cap < 1) cap = 1;
+  int64_t splits = 1;
+  if (h->opt_ctas > 0) {
+    splits = (h->opt_ctas + ctas - 1) / ctas;
+    if (splits > cap) splits = cap;
+  } else {
+    const int64_t wave = static_cast<int64_t>(h->sm_count) * 2;
+    int64_t best = INT64_MAX;
+    for (int64_t s2 = 1; s2 <= cap && s2 <= 256; ++s2) {
+      const int64_t cost = ((ctas * s2 + wave - 1) / wave) * ((p.tiles + s2 - 1) / s2 + 2);
+      if (cost < best) { best = cost; splits = s2; }
+    }
+  }
+  p.splits = static_cast<int32_t>(splits);
+  if (h->ev_start) cudaEventRecord(h->ev_start, s);
+  cudaError_t e = ea::launch_mq_simt(p, h->desc.dtype, s, &h->launches);
+  if (h->ev_stop) cudaEventRecord(h->ev_stop, s);
+  if (e == cudaSuccess) e = ea::launch_mq_combine(p, h->desc.dtype, s, &h->launches);
+  if (e != cudaSuccess) return cuda_fail(h, e, who);
+  return EA_OK;
+}
+
+ea_status launch_query(eigen_attn_t h, const char* who, const void* d_q, int64_t stride_b, int64_t stride_t, int group,
+                       int tokens, uint32_t flags, float* qp, double* q64, cudaStream_t s) {
+  ea::MqQueryParams q{};
+  q.heads = dev_heads(h); q.basis = dev_basis(h); q.q = d_q; q.q_stride_b = stride_b; q.q_stride_t = stride_t;
+  q.qp = qp; q.q64 = q64;
+  q.B = h->desc.batch; q.H = h->desc.n_heads; q.d_head = h->desc.d_head;
+  q.group = group; q.tokens = tokens; q.rows = tokens * group; q.q_stride = h->L.max_rp_k;
+  q.lr_k_width = h->L.sum_rp_k; q.scale = 1.0 / sqrt(static_cast<double>(h->desc.d_head)); q.flags = flags;
+  const cudaError_t e = ea::launch_mq_query(q, h->desc.dtype, s, &h->launches);
+  return e == cudaSuccess ? EA_OK : cuda_fail(h, e, who);
+}
+
+ea_status check_block(eigen_attn_t h, const char* who, int32_t block_rows) {
+  if (block_rows != 16 && block_rows != 32 && block_rows != 64 && block_rows != 128)
+    return fail(h, EA_ERR_SHAPE, "%s: blocks of %d rows (16, 32, 64 or 128)", who, block_rows);
+  return EA_OK;
+}
+
+}  // namespace
+
+ea_status eigen_attn_tree_bytes(eigen_attn_t h, int32_t max_tokens, int32_t group, size_t* bytes) {
+  if (!h || !bytes) return EA_ERR_INVALID_ARG;
+  if (max_tokens < 1 || max_tokens > ea::kTreeMaxTokens || group < 1 || group > kMaxGroup)
+    return fail(h, EA_ERR_SHAPE, "tree_bytes: %d tokens (1..%d), group %d (1..%d)", max_tokens, ea::kTreeMaxTokens, group, kMaxGroup);
+  *bytes = make_tree_layout(h, max_tokens * group, nullptr, nullptr);
+  return EA_OK;
+}
+
+ea_status eigen_attn_tree_attach(eigen_attn_t h, int32_t max_tokens, int32_t group, void* d_buf, size_t bytes) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!d_buf) {              // detach
+    h->tree_buf = nullptr; h->tree_rows = 0;
+    return EA_OK;
+  }
+  size_t need = 0;
+  const ea_status st = eigen_attn_tree_bytes(h, max_tokens, group, &need);
+  if (st != EA_OK) return st;
+  if (reinterpret_cast<uintptr_t>(d_buf) % kAlign) return fail(h, EA_ERR_INVALID_ARG, "tree_attach: buffer not 256-byte aligned");
+  if (bytes < need) return fail(h, EA_ERR_CAPACITY, "tree_attach: %zu bytes given, %zu needed", bytes, need);
+  h->tree_buf = static_cast<char*>(d_buf);
+  h->tree_rows = max_tokens * group;
+  make_tree_layout(h, h->tree_rows, &h->tree_off_part, &h->tree_slots);
+  return EA_OK;
+}
+
+ea_status eigen_attn_decode_tree(eigen_attn_t h, const void* d_q, int64_t stride_b_q, int64_t stride_t_q, int32_t group,
+                                 const void* d_k, const void* d_v, int64_t stride_b_kv, int64_t stride_t_kv, int32_t T,
+                                 const uint64_t* d_mask, void* d_out, int64_t stride_b_out, int64_t stride_t_out,
+                                 uint32_t flags, void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!h->tree_buf) return fail(h, EA_ERR_INVALID_ARG, "decode_tree: no scratch attached");
+  if (!d_q || !d_k || !d_v || !d_mask || !d_out) return fail(h, EA_ERR_INVALID_ARG, "decode_tree: NULL q, k, v, mask or out");
+  if (reinterpret_cast<uintptr_t>(d_mask) % sizeof(uint64_t)) return fail(h, EA_ERR_INVALID_ARG, "decode_tree: mask not 8-byte aligned");
+  if (flags & ~(EA_Q_PREPROJECTED | EA_KV_PREPROJECTED | EA_OUT_LOWRANK))
+    return fail(h, EA_ERR_INVALID_ARG, "decode_tree: unknown flag 0x%x", flags);
+  const ea_status st = check_mq(h, "decode_tree", group);
+  if (st != EA_OK) return st;
+  if (T < 1 || T > ea::kTreeMaxTokens) return fail(h, EA_ERR_SHAPE, "decode_tree: T = %d (1..%d)", T, ea::kTreeMaxTokens);
+  if (T * group > h->tree_rows)
+    return fail(h, EA_ERR_CAPACITY, "decode_tree: %d tokens x group %d exceed the attached scratch (%d query rows)", T, group, h->tree_rows);
+  int bad = 0;
+  if (!room_for(h, T, &bad))
+    return fail(h, EA_ERR_CAPACITY, "decode_tree: %d drafted rows exceed the capacity of sequence %d (%lld rows)", T, bad,
+                static_cast<long long>(capacity_of(h, bad)));
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  // the drafted rows, behind every sequence's own; the length stays where it is
+  const cudaError_t e = launch_append_rows(h, d_k, d_v, T, stride_b_kv, stride_t_kv, flags & EA_KV_PREPROJECTED, s);
+  if (e != cudaSuccess) return cuda_fail(h, e, "decode_tree append launch");
+  float* qp = reinterpret_cast<float*>(h->tree_buf);
+  const ea_status sq = launch_query(h, "decode_tree query launch", d_q, stride_b_q, stride_t_q, group, T,
+                                    flags & EA_Q_PREPROJECTED, qp, nullptr, s);
+  if (sq != EA_OK) return sq;
+  ea::MqDecodeParams p{};
+  p.qp = qp;
+  p.partials = reinterpret_cast<float*>(h->tree_buf + h->tree_off_part);
+  p.out = d_out; p.out_stride_b = stride_b_out; p.out_stride_t = stride_t_out;
+  p.mask = d_mask;
+  p.group = group; p.tokens = T; p.tail = T;
+  p.tiles = (h->len + T + 127) / 128;
+  p.flags = flags & EA_OUT_LOWRANK;
+  return launch_mq(h, "decode_tree launch", p, h->tree_slots, s);
+}
+
+ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const int32_t* h_counts, int32_t T, void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!h_paths || !h_counts) return fail(h, EA_ERR_INVALID_ARG, "tree_commit: NULL paths or counts");
+  if (T < 1 || T > ea::kTreeMaxTokens) return fail(h, EA_ERR_SHAPE, "tree_commit: T = %d (1..%d)", T, ea::kTreeMaxTokens);
+  const int B = h->desc.batch;
+  int bad = 0;
+  if (!room_for(h, T, &bad))
+    return fail(h, EA_ERR_CAPACITY, "tree_commit: %d drafted rows exceed the capacity of sequence %d", T, bad);
+  bool equal = true;
+  std::vector<int32_t> lens(B);
+  for (int b = 0; b < B; ++b) {
+    const int32_t c = h_counts[b];
+    if (c < 0 || c > T) return fail(h, EA_ERR_INVALID_ARG, "tree_commit: counts[%d] = %d outside [0, %d]", b, c, T);
+    for (int i = 0; i < c; ++i) {
+      const int32_t at = h_paths[static_cast<size_t>(b) * T + i];
+      if (at < 0 || at >= T || (i > 0 && at <= h_paths[static_cast<size_t>(b) * T + i - 1]))
+        return fail(h, EA_ERR_INVALID_ARG, "tree_commit: paths[%d][%d] = %d (strictly ascending, below %d)", b, i, at, T);
+    }
+    lens[b] = h->len - (h->max_deficit > 0 ? h->deficit[b] : 0) + c;
+    equal = equal && c == h_counts[0];
+  }
+  if (!equal && B > ea::kMaxRaggedBatch)
+    return fail(h, EA_ERR_UNSUPPORTED, "tree_commit: unequal counts with a batch of %d (at most %d)", B, ea::kMaxRaggedBatch);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing(s, &capture);
+  if (e != cudaSuccess) return cuda_fail(h, e, "tree_commit");
+  if (capture != cudaStreamCaptureStatusNone)
+    return fail(h, EA_ERR_UNSUPPORTED, "tree_commit: the lengths live on the host: not available during stream capture");
+  ea::TreeCommitParams p{};
+  p.heads = dev_heads(h); p.cache = h->cache; p.deficit = dev_deficit(h); p.pages = dev_pages(h);
+  p.B = B; p.H = h->desc.n_heads; p.n = h->len; p.n_max = h->desc.n_max; p.es = h->L.es;
+  for (int b0 = 0; b0 < B; b0 += ea::kCommitSeqs) {
+    const int nb = B - b0 < ea::kCommitSeqs ? B - b0 : ea::kCommitSeqs;
+    bool moves = false;
+    p.b0 = b0;
+    for (int i = 0; i < nb; ++i) {
+      p.count[i] = static_cast<uint8_t>(h_counts[b0 + i]);
+      for (int j = 0; j < h_counts[b0 + i]; ++j) {
+        const int32_t at = h_paths[static_cast<size_t>(b0 + i) * T + j];
+        p.path[i][j] = static_cast<uint8_t>(at);
+        moves = moves || at != j;
+      }
+    }
+    if (!moves) continue;                       // a chain: its rows are where they belong
+    e = ea::launch_tree_commit(p, nb, s, &h->launches);
+    if (e != cudaSuccess) return cuda_fail(h, e, "tree_commit launch");
+  }
+  if (equal) {                                  // the differences between the lengths stay as they are
+    h->len += h_counts[0];
+    return EA_OK;
+  }
+  return eigen_attn_set_lens(h, lens.data(), cuda_stream);
+}
+
+ea_status eigen_attn_sparse_bytes(eigen_attn_t h, int32_t block_rows, size_t* bytes) {
+  if (!h || !bytes) return EA_ERR_INVALID_ARG;
+  const ea_status st = check_block(h, "sparse_bytes", block_rows);
+  if (st != EA_OK) return st;
+  SparseLayout S;
+  make_sparse_layout(h, block_rows, &S);
+  *bytes = S.bytes;
+  return EA_OK;
+}
+
+ea_status eigen_attn_sparse_attach(eigen_attn_t h, int32_t block_rows, void* d_buf, size_t bytes, void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!d_buf) {              // detach
+    h->sp_buf = nullptr;
+    return EA_OK;
+  }
+  const ea_status st = check_block(h, "sparse_attach", block_rows);
+  if (st != EA_OK) return st;
+  if (reinterpret_cast<uintptr_t>(d_buf) % kAlign) return fail(h, EA_ERR_INVALID_ARG, "sparse_attach: buffer not 256-byte aligned");
+  SparseLayout S;
+  make_sparse_layout(h, block_rows, &S);
+  if (bytes < S.bytes) return fail(h, EA_ERR_CAPACITY, "sparse_attach: %zu bytes given, %zu needed", bytes, S.bytes);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e = cudaMemcpyAsync(d_buf, S.slab.data(), sizeof(int64_t) * S.slab.size(), cudaMemcpyHostToDevice, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e != cudaSuccess) return cuda_fail(h, e, "sparse_attach");
+  h->sp_buf = static_cast<char*>(d_buf);
+  h->sp_shift = 0;
+  while ((1 << h->sp_shift) < block_rows) ++h->sp_shift;
+  h->sp = S;
+  h->sp_len.assign(h->desc.batch, 0);
+  return EA_OK;
+}
+
+namespace {
+void fill_sparse_params(eigen_attn_t h, ea::SparseParams* p) {
+  *p = ea::SparseParams{};
+  p->heads = dev_heads(h); p->cache = h->cache;
+  p->bounds = h->sp_buf; p->slab = reinterpret_cast<const int64_t*>(h->sp_buf);
+  p->deficit = dev_deficit(h); p->pages = dev_pages(h);
+  p->B = h->desc.batch; p->H = h->desc.n_heads; p->n = h->len; p->n_max = h->desc.n_max;
+  p->block_shift = h->sp_shift; p->seq_blocks = h->sp.seq_blocks;
+  p->q_stride = h->L.max_rp_k; p->score_stride = h->sp.seq_blocks;
+}
+int32_t len_of(const eigen_attn* h, int b) { return h->len - (h->max_deficit > 0 ? h->deficit[b] : 0); }
+}  // namespace
+
+ea_status eigen_attn_sparse_sync(eigen_attn_t h, void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!h->sp_buf) return fail(h, EA_ERR_INVALID_ARG, "sparse_sync: no buffer attached");
+  const int B = h->desc.batch;
+  int lo = INT32_MAX, hi = 0;
+  for (int b = 0; b < B; ++b) {
+    const int done = h->sp_len[b] >> h->sp_shift, whole = len_of(h, b) >> h->sp_shift;
+    if (whole > done) {
+      if (done < lo) lo = done;
+      if (whole > hi) hi = whole;
+    }
+  }
+  if (hi <= lo) return EA_OK;
+  ea::SparseParams p;
+  fill_sparse_params(h, &p);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  constexpr int kStep = 1 << 18;              // the second grid dimension
+  for (int b0 = lo; b0 < hi; b0 += kStep) {
+    // bounds of a block that has them already are written again where lengths differ: the same values
+    p.block0 = b0; p.block1 = b0 + kStep < hi ? b0 + kStep : hi;
+    const cudaError_t e = ea::launch_block_bounds(p, h->desc.dtype, s, &h->launches);
+    if (e != cudaSuccess) return cuda_fail(h, e, "sparse_sync launch");
+  }
+  for (int b = 0; b < B; ++b) h->sp_len[b] = len_of(h, b) >> h->sp_shift << h->sp_shift;
+  return EA_OK;
+}
+
+ea_status eigen_attn_sparse_lens(eigen_attn_t h, int32_t* lens) {
+  if (!h || !lens) return EA_ERR_INVALID_ARG;
+  if (!h->sp_buf) return fail(h, EA_ERR_INVALID_ARG, "sparse_lens: no buffer attached");
+  for (int b = 0; b < h->desc.batch; ++b) lens[b] = h->sp_len[b];
+  return EA_OK;
+}
+
+ea_status eigen_attn_sparse_layout(eigen_attn_t h, int32_t head, size_t* slab_offset, int32_t* seq_blocks) {
+  if (!h || !slab_offset || !seq_blocks) return EA_ERR_INVALID_ARG;
+  if (!h->sp_buf) return fail(h, EA_ERR_INVALID_ARG, "sparse_layout: no buffer attached");
+  if (head < 0 || head >= h->desc.n_heads) return fail(h, EA_ERR_SHAPE, "sparse_layout: head %d", head);
+  *slab_offset = static_cast<size_t>(h->sp.slab[head]);
+  *seq_blocks = h->sp.seq_blocks;
+  return EA_OK;
+}
+
+ea_status eigen_attn_decode_sparse(eigen_attn_t h, const void* d_q, int64_t stride_b_q, int32_t group, int32_t n_blocks,
+                                   int32_t sink, int32_t recent, void* d_out, int64_t stride_b_out, int32_t* d_index,
+                                   uint32_t flags, void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!h->sp_buf) return fail(h, EA_ERR_INVALID_ARG, "decode_sparse: no buffer attached");
+  if (!d_q || !d_out) return fail(h, EA_ERR_INVALID_ARG, "decode_sparse: NULL q or out");
+  if (flags & ~(EA_Q_PREPROJECTED | EA_OUT_LOWRANK)) return fail(h, EA_ERR_INVALID_ARG, "decode_sparse: unknown flag 0x%x", flags);
+  const ea_status st = check_mq(h, "decode_sparse", group);
+  if (st != EA_OK) return st;
+  if (sink < 0 || recent < 1 || n_blocks < 1 || static_cast<int64_t>(sink) + recent > n_blocks)
+    return fail(h, EA_ERR_SHAPE, "decode_sparse: %d blocks hold the first %d and the newest %d (at least 1)", n_blocks, sink, recent);
+  const int B = h->desc.batch, G = 1 << h->sp_shift;
+  int max_blocks = 0;
+  for (int b = 0; b < B; ++b) {
+    const int32_t n_b = len_of(h, b);
+    if (n_b < 1) return fail(h, EA_ERR_SHAPE, "decode_sparse: sequence %d has no cached row", b);
+    const int have = (n_b + G - 1) >> h->sp_shift;
+    if (have > h->sp.seq_blocks)
+      return fail(h, EA_ERR_CAPACITY, "decode_sparse: sequence %d holds more than n_max rows", b);
+    if (have > max_blocks) max_blocks = have;
+    if (have > n_blocks && (h->sp_len[b] >> h->sp_shift) < have - recent)
+      return fail(h, EA_ERR_INVALID_ARG, "decode_sparse: sequence %d has bounds for %d of its %d rows: call sparse_sync first", b,
+                  h->sp_len[b], n_b);
+  }
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  float* qp = reinterpret_cast<float*>(h->sp_buf + h->sp.off_qp);
+  double* q64 = reinterpret_cast<double*>(h->sp_buf + h->sp.off_q64);
+  const ea_status sq = launch_query(h, "decode_sparse query launch", d_q, stride_b_q, 0, group, 1, flags & EA_Q_PREPROJECTED, qp, q64, s);
+  if (sq != EA_OK) return sq;
+  ea::SparseParams sp;
+  fill_sparse_params(h, &sp);
+  sp.q64 = q64; sp.group = group;
+  sp.scores = reinterpret_cast<double*>(h->sp_buf + h->sp.off_scores);
+  sp.list = reinterpret_cast<int32_t*>(h->sp_buf + h->sp.off_list);
+  sp.index = d_index; sp.index_len = n_blocks;
+  sp.list_len = n_blocks < max_blocks ? n_blocks : max_blocks;      // no unit's list is longer
+  sp.sink = sink; sp.recent = recent; sp.max_blocks = max_blocks;
+  cudaError_t e = cudaSuccess;
+  if (max_blocks > n_blocks) e = ea::launch_block_scores(sp, h->desc.dtype, h->L.max_rp_k, s, &h->launches);
+  if (e == cudaSuccess) e = ea::launch_block_select(sp, s, &h->launches);
+  if (e != cudaSuccess) return cuda_fail(h, e, "decode_sparse selection launch");
+  ea::MqDecodeParams p{};
+  p.qp = qp;
+  p.partials = reinterpret_cast<float*>(h->sp_buf + h->sp.off_part);
+  p.out = d_out; p.out_stride_b = stride_b_out;
+  p.list = sp.list; p.list_len = sp.list_len; p.block_shift = h->sp_shift;
+  p.group = group; p.tokens = 1; p.tail = 0;
+  p.tiles = static_cast<int32_t>(((static_cast<int64_t>(sp.list_len) << h->sp_shift) + 127) / 128);
+  p.flags = flags & EA_OUT_LOWRANK;
+  return launch_mq(h, "decode_sparse launch", p, h->sp.slots, s);
 }
 
 ea_status eigen_attn_set_rope(eigen_attn_t h, double base, int32_t interleaved, void* cuda_stream) {

@@ -23,6 +23,8 @@ struct HeadInfo {
   int32_t uvl16_off;  // float offset of the lift image of U^V: bf16 high then low part, each [d_head][rv16] canonical
   float alibi_slope2;  // ALiBi slope of the head times log2(e); 0 = no position bias
   int32_t ukl16_off;   // float offset of the lift image of U^K (as uvl16_off, [d_head][rk16] canonical, high then low)
+  float alibi_slope;   // the slope itself: block scores take it in 64 bits, where the rounded product above could tie
+  int32_t pad_;
 };
 
 // Paged cache: where logical row `row` of sequence `b` lives in a head's slab, viewed as one array of
@@ -275,7 +277,96 @@ struct QuantParams {
   uint32_t magic[4];        // float exponent patterns the decode kernel ORs nibbles into (set by its launcher)
 };
 
+// Several query rows per K/V head over the same rows of the cache.  The query rows of a unit (sequence b, K/V head h;
+// unit = h B + b) are numbered t * group + i: drafted token t (0 in a single-token call), query head i of the group.
+// The rows come either from the whole sequence with the drafted rows behind it (list == NULL: logical rows
+// [0, n_b + tail), row n_b + s seen by token t where bit s of mask[b][t] is set) or from a list of blocks.
+struct MqDecodeParams {
+  const HeadInfo* heads;
+  const float* basis;
+  const char* cache;
+  const float* qp;          // [unit][rows][q_stride]: Q' = Q U^K, times log2(e)/sqrt(d_head)
+  float* partials;          // [unit * rows + row][splits][part_stride]: m, l, pad, pad, o'[rp_v]
+  void* out;                // [B][tokens][H * group][d_head], or packed [B][tokens][group * sum rp_v]
+  int64_t out_stride_b, out_stride_t;
+  const int32_t* deficit;   // [B]: sequence b holds n - deficit[b] rows; NULL = all hold n
+  const uint64_t* mask;     // [B][tokens] (tail > 0)
+  const int32_t* list;      // [unit][list_len] blocks in ascending order, -1 behind the last; NULL = the whole sequence
+  int32_t list_len;
+  int32_t block_shift;      // log2 of the rows of a block (list only)
+  int32_t B, H, d_head;
+  int32_t n, n_max;
+  int32_t group, tokens, rows;   // rows = tokens * group
+  int32_t tail;             // drafted rows behind every sequence (0 or tokens)
+  int32_t q_stride, part_stride;
+  int32_t tiles;            // tiles of 128 rows of the longest unit
+  int32_t splits;           // CTAs per (unit, chunk of query rows)
+  int32_t lr_v_width;       // sum of rp_v: width of a packed output row of one query head
+  uint32_t flags;
+  PageMap pages;
+};
+
+struct MqQueryParams {       // Q' of every query row into the scratch, scaled into the base-2 domain
+  const HeadInfo* heads;
+  const float* basis;
+  const void* q;            // [B][tokens][H * group][d_head], or packed [B][tokens][group * sum rp_k]
+  int64_t q_stride_b, q_stride_t;
+  float* qp;                // [unit][rows][q_stride]
+  double* q64;              // [unit][rows][q_stride]: the same times 1/sqrt(d_head) in 64 bits (block scores), or NULL
+  int32_t B, H, d_head, group, tokens, rows, q_stride;
+  int32_t lr_k_width;
+  double scale;             // 1/sqrt(d_head)
+  uint32_t flags;
+};
+
+constexpr int kTreeMaxTokens = 64;
+constexpr int kCommitSeqs = 64;          // sequences whose paths travel in one launch's parameters
+struct TreeCommitParams {
+  const HeadInfo* heads;
+  char* cache;
+  const int32_t* deficit;
+  int32_t B, H, n, n_max, b0, es;
+  PageMap pages;
+  uint8_t count[kCommitSeqs];
+  uint8_t path[kCommitSeqs][kTreeMaxTokens];
+};
+
+struct SparseParams {
+  const HeadInfo* heads;
+  const char* cache;
+  char* bounds;             // per head [physical blocks][2][rp_k] in the cache dtype: minima, maxima
+  const int64_t* slab;      // [H] byte offsets of the heads in `bounds`
+  const double* q64;        // [unit][group][q_stride]
+  double* scores;           // [unit][score_stride]
+  int32_t* list;            // [unit][list_len]
+  int32_t* index;           // [B][H][list_len] for the caller, or NULL
+  const int32_t* deficit;
+  int32_t B, H, n, n_max;
+  int32_t block_shift;
+  int32_t seq_blocks;       // blocks of a sequence's slab = ceil(n_max / block rows)
+  int32_t block0, block1;   // bounds: blocks [block0, block1) of every sequence (complete ones only)
+  int32_t q_stride, score_stride, group;
+  int32_t list_len, index_len, sink, recent;   // index rows are padded with -1 to index_len
+  int32_t max_blocks;       // blocks of the longest sequence
+  PageMap pages;
+};
+#ifdef __CUDACC__
+// Where block `blk` of sequence b lives among a head's blocks: blocks never straddle pages (a page holds at least
+// 128 rows, a block at most 128, both powers of two).
+__device__ __forceinline__ int64_t physical_block(const SparseParams& p, int b, int blk) {
+  if (p.pages.table == nullptr) return static_cast<int64_t>(b) * p.seq_blocks + blk;
+  return physical_row(p.pages, b, p.n_max, blk << p.block_shift) >> p.block_shift;
+}
+#endif
+
 // Launchers (each returns the CUDA error of its launch); `launches` is incremented per kernel.
+cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_tree_commit(const TreeCommitParams& p, int sequences, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_block_bounds(const SparseParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_block_scores(const SparseParams& p, int dtype, int max_rp_k, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_block_select(const SparseParams& p, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_project_append(const ProjectParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_decode(const DecodeParams& p, int dtype, int grid, size_t smem_bytes,
                           cudaStream_t s, uint64_t* launches);
