@@ -1370,9 +1370,12 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size
   p.n = h->len; p.n_max = h->desc.n_max;
   p.rows = p.tokens * p.group;
   p.q_stride = L.max_rp_k; p.part_stride = L.part_stride; p.lr_v_width = L.sum_rp_v;
-  // CTAs per run of eight query rows: waves of resident CTAs, a start-up worth a tile or two per CTA, and room for the
+  // CTAs per run of query rows: waves of resident CTAs, a start-up worth a tile or two per CTA, and room for the
   // partials
-  const int64_t ctas = static_cast<int64_t>(p.B) * p.H * ((p.rows + 7) / 8);
+  const bool mma = h->desc.dtype == EA_BF16;
+  const int max_rp = L.max_rp_k > L.max_rp_v ? L.max_rp_k : L.max_rp_v;
+  const ea::MqShape shape = mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::MqShape{8, 2};
+  const int64_t ctas = static_cast<int64_t>(p.B) * p.H * ((p.rows + shape.queries - 1) / shape.queries);
   int64_t cap = static_cast<int64_t>(slots) / (static_cast<int64_t>(p.B) * p.H * p.rows);
   if (cap > p.tiles) cap = p.tiles;
   if (cap > 65535) cap = 65535;
@@ -1382,7 +1385,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size
     splits = (h->opt_ctas + ctas - 1) / ctas;
     if (splits > cap) splits = cap;
   } else {
-    const int64_t wave = static_cast<int64_t>(h->sm_count) * 2;
+    const int64_t wave = static_cast<int64_t>(h->sm_count) * shape.ctas_per_sm;
     int64_t best = INT64_MAX;
     for (int64_t s2 = 1; s2 <= cap && s2 <= 256; ++s2) {
       const int64_t cost = ((ctas * s2 + wave - 1) / wave) * ((p.tiles + s2 - 1) / s2 + 2);
@@ -1391,7 +1394,13 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size
   }
   p.splits = static_cast<int32_t>(splits);
   if (h->ev_start) cudaEventRecord(h->ev_start, s);
-  cudaError_t e = ea::launch_mq_simt(p, h->desc.dtype, s, &h->launches);
+  int min_rp = max_rp;
+  for (const HeadInfo& hi : L.heads) {
+    if (hi.rp_k < min_rp) min_rp = hi.rp_k;
+    if (hi.rp_v < min_rp) min_rp = hi.rp_v;
+  }
+  cudaError_t e = mma ? ea::launch_mq_mma(p, max_rp, min_rp, s, &h->launches)
+                      : ea::launch_mq_simt(p, h->desc.dtype, s, &h->launches);
   if (h->ev_stop) cudaEventRecord(h->ev_stop, s);
   if (e == cudaSuccess) e = ea::launch_mq_combine(p, h->desc.dtype, s, &h->launches);
   if (e != cudaSuccess) return cuda_fail(h, e, who);

@@ -1,0 +1,497 @@
+// Attention of several query rows per K/V head over one sequence's rows (a tree of drafted tokens, or one token over a
+// list of blocks) with warp-level tensor-core products, for 16-bit layers.
+//
+// A warp takes 32 cached rows of every tile of 128 and 8 or 16 query rows: S = Q' K'^T and O' += P V' with mma.sync
+// m16n8k16, the softmax in between on the accumulator fragments, which are at the same time the A fragments of the second
+// product.  The 16 rows of an A operand hold 8 queries twice: rows 0-7 the leading 16-bit part of Q' (or of P), rows 8-15
+// what it leaves.  A thread of the fragment layout owns rows g and g + 8, the two halves of one query, so adding them is
+// one addition in the same thread; Q' and P enter the products with 16 significant bits and the result carries no more
+// than the rounding of the output.  With at most 8 query rows the second half of the operand would be empty anyway.
+//
+// Rows travel by 16-byte asynchronous copies into a ring that belongs to the warps that read it (one warp, or two that
+// share the rows and split the queries): no block-wide barrier and no wait that could fail to end.  In shared memory a row
+// sits at an odd multiple of 16 bytes, so that the eight rows of an ldmatrix meet all banks once, whatever the rank.
+#include <cuda_bf16.h>
+
+#include "internal.h"
+#include "tc_common.cuh"
+
+namespace ea {
+namespace {
+
+using namespace tc;
+
+constexpr unsigned kFull = 0xffffffffu;
+constexpr float kRaise = 8.f;              // a running maximum is raised when a score exceeds it by this much
+constexpr int kGroups = 4;                 // key groups of a tile
+constexpr int kRows = 32;                  // rows of a key group
+
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(b0));
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, __shfl_xor_sync(kFull, v, 1));
+  return fmaxf(v, __shfl_xor_sync(kFull, v, 2));
+}
+// (x0, x1) as two pairs of 16-bit numbers: hi = the rounded values, lo = the rounded remainders
+__device__ __forceinline__ void split_pair(float x0, float x1, uint32_t& hi, uint32_t& lo) {
+  hi = pack_bf16(x0, x1);
+  lo = pack_bf16(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xffff0000u));
+}
+__device__ __forceinline__ uint64_t tree_mask(uint64_t m, int tokens) { return tokens < 64 ? m & ((1ull << tokens) - 1) : m; }
+__device__ __forceinline__ int tree_depth(uint64_t m, int t) { return __popcll(m & ~(1ull << t)); }
+
+// The 16-byte pieces of a row, and the distance of two rows in shared memory in such pieces.
+__host__ __device__ constexpr int odd_pieces(int pieces) { return pieces | 1; }
+
+// Shape of an instance: NC = 8-channel pieces of the widest row; MT = tiles of 8 queries per warp; WG = warps that share a
+// key group's rows.
+template <int NC, int MT, int WG>
+struct Shape {
+  static constexpr int kThreads = kGroups * WG * 32;
+  static constexpr int kQueries = 8 * MT * WG;
+  static constexpr int kSlot = kRows * 2 * odd_pieces(NC) * 16;          // one key group's rows of a tile
+  static constexpr int kCtas = WG == 1 && NC <= 10 ? 2 : 1;               // resident CTAs per SM
+  static constexpr bool kQReg = MT * NC * 2 <= 40;                        // Q' fragments in registers, else in shared memory
+  static constexpr int kQBytes = kQReg ? 0 : WG * MT * ((NC + 1) / 2) * 32 * 16;
+  static constexpr int kHead = 32 * 8 + 64 * 4;                           // masks of the queries, places of the drafted rows
+  static constexpr int kRoom = (kCtas == 2 ? 112 : 226) * 1024 - kHead - kQBytes - 64;
+  static constexpr int kStages = kRoom / (kGroups * kSlot) < 4 ? kRoom / (kGroups * kSlot) : 4;
+  static constexpr int kMerge = kGroups * kQueries * (2 + 8 * NC + 1) * 4;
+  static constexpr int kRing = kGroups * kSlot * kStages > kMerge ? kGroups * kSlot * kStages : kMerge;
+  static constexpr size_t kSmem = kHead + kQBytes + kRing + 64;           // (an ldmatrix may read past a row's last piece)
+  static_assert(kStages >= 2, "ring too shallow");
+};
+
+// Where the 32 rows of a key group come from: two runs of 16 neighbouring rows (a block can be 16 rows long).
+struct Source {
+  int64_t row[2];          // physical first row of each half
+  int valid[2];            // rows of each half that exist
+  int first[2];            // logical first row of each half (-1: nothing there)
+};
+
+template <int NC, int MT, int WG, bool FULL>
+__global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>::kCtas)
+    mq_mma_kernel(const MqDecodeParams p) {
+  using S = Shape<NC, MT, WG>;
+  constexpr int NKS = (NC + 1) / 2;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  uint64_t* q_mask = reinterpret_cast<uint64_t*>(smem);                   // [32]
+  float* draft_pos = reinterpret_cast<float*>(smem + 32 * 8);             // [64]
+  uint4* q_img = reinterpret_cast<uint4*>(smem + S::kHead);               // [WG][MT][NKS][32 lanes]
+  unsigned char* ring = smem + S::kHead + S::kQBytes;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+  const int kg = warp & 3, rg = warp >> 2;                                // key group, share of the queries
+  const int chunks = (p.rows + S::kQueries - 1) / S::kQueries;
+  const int unit = blockIdx.x / chunks, chunk = blockIdx.x - unit * chunks, split = blockIdx.y;
+  const int h = unit / p.B, b = unit - h * p.B;
+  const HeadInfo hd = p.heads[h];
+  const int nck = FULL ? NC : hd.rp_k >> 3, ncv = FULL ? NC : hd.rp_v >> 3;
+  const int kpitch = odd_pieces(nck) * 16, vpitch = odd_pieces(ncv) * 16;
+  const int row0 = chunk * S::kQueries;                                   // first query row of the CTA
+
+  const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
+  const int64_t end = p.list ? static_cast<int64_t>(p.list_len) << p.block_shift : static_cast<int64_t>(n_b) + p.tail;
+  const int nt = static_cast<int>((end + 127) >> 7);
+  const int per = (p.tiles + p.splits - 1) / p.splits;
+  const int t_lo = min(nt, split * per), t_hi = min(nt, t_lo + per);
+  const int32_t* list = p.list ? p.list + static_cast<int64_t>(unit) * p.list_len : nullptr;
+  const char* k_slab = p.cache + hd.k_off;
+  const char* v_slab = p.cache + hd.v_off;
+  const bool bias = hd.alibi_slope2 != 0.f;
+
+  // ---- rows: the copies of one key group, by its own warps.  What the address of a tile needs (the block's number, its
+  // page) is loaded one and two tiles ahead of its use.
+  const int64_t pos0 = static_cast<int64_t>(kg) * kRows;                  // of the key group inside a tile
+  int blk_next[2] = {-1, -1}, blk_now[2] = {-1, -1}, page_now[2] = {0, 0};
+  auto fetch_block = [&](int t, int (&blk)[2]) {                          // list entries of tile t
+    if (list == nullptr || t >= t_hi) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t at = ((static_cast<int64_t>(t) << 7) + pos0 + 16 * i) >> p.block_shift;
+      blk[i] = at < p.list_len ? __ldg(list + at) : -1;
+    }
+  };
+  auto logical = [&](int t, int i, int blk) -> int {                      // first logical row of a half
+    const int64_t at = (static_cast<int64_t>(t) << 7) + pos0 + 16 * i;
+    if (list == nullptr) return static_cast<int>(at);
+    return blk < 0 ? -1 : (blk << p.block_shift) + static_cast<int>(at & ((1 << p.block_shift) - 1));
+  };
+  const int row_end = n_b + p.tail;
+  auto fetch_page = [&](int t, const int (&blk)[2], int (&page)[2]) {
+    if (p.pages.table == nullptr || t >= t_hi) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = logical(t, i, blk[i]);
+      page[i] = r >= 0 && r < row_end ? __ldg(p.pages.table + static_cast<int64_t>(b) * p.pages.width + (r >> p.pages.shift)) : 0;
+    }
+  };
+  auto source = [&](int t, const int (&blk)[2], const int (&page)[2]) {
+    Source s;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = logical(t, i, blk[i]);
+      const bool there = r >= 0 && r < row_end;
+      s.first[i] = r;
+      s.valid[i] = there ? min(16, row_end - r) : 0;
+      s.row[i] = !there ? 0
+                 : p.pages.table == nullptr ? static_cast<int64_t>(b) * p.n_max + r
+                                            : (static_cast<int64_t>(page[i]) << p.pages.shift) + (r & ((1 << p.pages.shift) - 1));
+    }
+    return s;
+  };
+  const int cl = lane + 32 * rg;                                          // this thread among the copiers of the group
+  const uint32_t inv_k = 65536 / nck + 1, inv_v = 65536 / ncv + 1;        // i / nc = i inv >> 16 for i < 512
+  auto copy_rows = [&](unsigned char* dst, const char* slab, int nc, uint32_t inv, int pitch, const Source& s) {
+    const char* s0 = slab + s.row[0] * (nc * 16);
+    const char* s1 = slab + (s.row[1] - 16) * (nc * 16);
+#pragma unroll
+    for (int i0 = 0; i0 < kRows * NC; i0 += 32 * WG) {
+      const int i = i0 + cl;
+      if (i < kRows * nc) {
+        const int row = FULL ? i / NC : static_cast<int>(i * inv >> 16);
+        const bool late = row >= 16;
+        const bool there = (late ? row - 16 : row) < (late ? s.valid[1] : s.valid[0]);
+        cp_async16(dst + row * pitch + (i - row * nc) * 16, there ? (late ? s1 : s0) + static_cast<int64_t>(i) * 16 : slab, there ? 16u : 0u);
+      }
+    }
+  };
+  auto slot_of = [&](int it) { return ring + ((it % S::kStages) * kGroups + kg) * S::kSlot; };
+  int ahead[S::kStages - 1][2];                                           // logical first rows of the tiles under way
+  auto issue = [&](int t) {
+#pragma unroll
+    for (int i = 0; i + 1 < S::kStages - 1; ++i) { ahead[i][0] = ahead[i + 1][0]; ahead[i][1] = ahead[i + 1][1]; }
+    if (t < t_hi) {
+      const Source s = source(t, blk_now, page_now);
+      ahead[S::kStages - 2][0] = s.first[0]; ahead[S::kStages - 2][1] = s.first[1];
+      unsigned char* dst = slot_of(t - t_lo);
+      copy_rows(dst, k_slab, nck, inv_k, kpitch, s);
+      copy_rows(dst + kRows * kpitch, v_slab, ncv, inv_v, vpitch, s);
+    }
+    cp_async_commit();
+    blk_now[0] = blk_next[0]; blk_now[1] = blk_next[1];
+    fetch_page(t + 1, blk_now, page_now);
+    fetch_block(t + 2, blk_next);
+  };
+  fetch_block(t_lo, blk_now);
+  fetch_page(t_lo, blk_now, page_now);
+  fetch_block(t_lo + 1, blk_next);
+#pragma unroll
+  for (int i = 0; i < S::kStages - 1; ++i) issue(t_lo + i);
+
+  // ---- queries: fragments of Q' (leading parts in rows 0-7 of the operand, remainders in rows 8-15)
+  const uint64_t* masks = p.mask + static_cast<int64_t>(b) * p.tokens;
+  if (p.tail) {
+    if (tid < S::kQueries) {
+      const int r = row0 + tid;
+      q_mask[tid] = r < p.rows ? tree_mask(masks[r / p.group], p.tokens) : 0;
+    }
+    if (bias && tid < p.tokens) draft_pos[tid] = static_cast<float>(n_b + tree_depth(tree_mask(masks[tid], p.tokens), tid));
+  }
+  uint32_t qa[S::kQReg ? MT : 1][S::kQReg ? NKS : 1][4];
+  float q_pos[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = row0 + (rg * MT + mt) * 8 + gid;
+    const float* src = p.qp + (static_cast<int64_t>(unit) * p.rows + r) * p.q_stride;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      uint32_t f[4];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int c = 16 * ks + 8 * half + 2 * tig;
+        const bool in = r < p.rows && c < 8 * nck;
+        const float2 x = in ? *reinterpret_cast<const float2*>(src + c) : make_float2(0.f, 0.f);
+        split_pair(x.x, x.y, f[2 * half], f[2 * half + 1]);
+      }
+      if constexpr (S::kQReg) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qa[mt][ks][i] = f[i];
+      } else if (kg == 0) {
+        q_img[((rg * MT + mt) * NKS + ks) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
+      }
+    }
+    q_pos[mt] = static_cast<float>(n_b - 1);
+    if (p.tail && bias && r < p.rows) {
+      const int t = r / p.group;
+      q_pos[mt] = static_cast<float>(n_b + tree_depth(tree_mask(masks[t], p.tokens), t));
+    }
+  }
+  __syncthreads();
+
+  float o[MT][NC][4];
+  float m[MT], base[MT], l[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m[mt] = -INFINITY; base[mt] = 0.f; l[mt] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[mt][c][i] = 0.f;
+  }
+  auto group_sync = [&]() {
+    if constexpr (WG == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + kg), "n"(32 * WG) : "memory");
+  };
+  const uint32_t k_lane = static_cast<uint32_t>((lane & 7) * kpitch + (lane >> 3) * 16);
+  const uint32_t v_lane = static_cast<uint32_t>(kRows * kpitch + lane * vpitch);
+
+  for (int t = t_lo; t < t_hi; ++t) {
+    cp_async_wait<S::kStages - 2>();
+    group_sync();                      // the tile is there for every warp of the group, and the tile before it is read
+    const int first[2] = {ahead[0][0], ahead[0][1]};
+    issue(t + S::kStages - 1);
+    unsigned char* st = slot_of(t - t_lo);
+    const uint32_t k_addr = smem_u32(st) + k_lane, v_addr = smem_u32(st) + v_lane;
+
+    float s[MT][4][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[mt][j][i] = 0.f;
+#pragma unroll
+    for (int c4 = 0; c4 < NC; c4 += 4) {
+      if (FULL || c4 < nck) {
+        uint32_t kf[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ldsm4(kf[j], k_addr + j * 8 * kpitch + c4 * 16);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int ks = c4 / 2 + half;
+          if (ks < NKS) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              uint32_t a[4];
+              if constexpr (S::kQReg) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[i] = qa[mt][ks < NKS ? ks : 0][i];
+              } else {
+                const uint4 f = q_img[((rg * MT + mt) * NKS + ks) * 32 + lane];
+                a[0] = f.x; a[1] = f.y; a[2] = f.z; a[3] = f.w;
+              }
+              if (FULL ? 2 * ks + 1 < NC : 2 * ks + 1 < nck) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma16(s[mt][j], a, kf[j][2 * half], kf[j][2 * half + 1]);
+              } else if (FULL || 2 * ks < nck) {                          // a row's last piece: eight channels
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma8(s[mt][j], a[0], a[1], kf[j][2 * half]);
+              }
+            }
+          }
+        }
+      }
+    }
+    // ---- scores: the two halves of a query, the bias, the mask.  sc[mt][j][e]: row 8 j + 2 tig + e of the group
+    float sc[MT][4][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sc[mt][j][0] = s[mt][j][0] + s[mt][j][2];
+        sc[mt][j][1] = s[mt][j][1] + s[mt][j][3];
+      }
+    // the end of the sequence, drafted rows, a list entry that is not there (they come last, as the incomplete block does)
+    const bool special = bias || first[0] < 0 || first[1] < 0 || max(first[0], first[1]) + 16 > n_b;
+    unsigned odd_rows = 0;             // drafted rows whose values are not finite
+    if (special) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int kk = 8 * (j & 1) + 2 * tig + e;                       // inside its half
+          const int r = first[j >> 1] < 0 ? row_end : first[j >> 1] + kk;
+          const bool drafted = r >= n_b && r < row_end;
+          const float place = bias ? (drafted ? draft_pos[r - n_b] : static_cast<float>(r)) : 0.f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            bool open = r < n_b;
+            if (drafted) open = (q_mask[(rg * MT + mt) * 8 + gid] >> (r - n_b)) & 1;
+            if (bias) sc[mt][j][e] = fmaf(hd.alibi_slope2, place - q_pos[mt], sc[mt][j][e]);
+            if (!open) sc[mt][j][e] = -INFINITY;
+          }
+        }
+      if (p.tail && first[0] + kRows > n_b) {          // (the whole sequence: the two halves are neighbours)
+        const int r = first[0] + lane;
+        bool bad = false;
+        if (r >= n_b && r < row_end) {
+          const uint4* x = reinterpret_cast<const uint4*>(st + kRows * kpitch + lane * vpitch);
+          for (int c = 0; c < ncv; ++c) {
+            const uint4 w = x[c];
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              bad = bad || (u[i] & 0x7f80u) == 0x7f80u || (u[i] & 0x7f800000u) == 0x7f800000u;
+          }
+        }
+        odd_rows = __ballot_sync(kFull, bad);
+      }
+    }
+    // ---- online softmax on the fragments
+    bool raise = false;
+    float mx[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      mx[mt] = fmaxf(max3(sc[mt][0][0], sc[mt][0][1], sc[mt][1][0]), max3(sc[mt][1][1], sc[mt][2][0], sc[mt][2][1]));
+      mx[mt] = max3(mx[mt], sc[mt][3][0], sc[mt][3][1]);
+      raise = raise || mx[mt] > m[mt] + kRaise;
+    }
+    if (__any_sync(kFull, raise)) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const float top = fmaxf(m[mt], quad_max(mx[mt]));
+        base[mt] = top == -INFINITY ? 0.f : top;
+        const float f = ex2(m[mt] - base[mt]);                            // 0 before the first row
+        m[mt] = top;
+        l[mt] *= f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[mt][c][i] *= f;
+      }
+    }
+    uint32_t pa[MT][2][4];             // A fragments of P for the two steps of 16 rows: leading parts and remainders
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sc[mt][j][0] = ex2(sc[mt][j][0] - base[mt]);
+        sc[mt][j][1] = ex2(sc[mt][j][1] - base[mt]);
+        l[mt] += sc[mt][j][0] + sc[mt][j][1];
+        split_pair(sc[mt][j][0], sc[mt][j][1], pa[mt][j >> 1][(j & 1) * 2], pa[mt][j >> 1][(j & 1) * 2 + 1]);
+      }
+    if (odd_rows) {
+      // A product with a zero weight would still carry an infinity or NaN of a row that the query does not see: such rows
+      // are added one by one where their weight is not zero, and then cleared for the products.
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          for (int src = 0; src < 4; ++src) {
+            const int key = 8 * j + 2 * src + e;
+            if (!((odd_rows >> key) & 1)) continue;
+            const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(st + kRows * kpitch + key * vpitch);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              const float w = __shfl_sync(kFull, sc[mt][j][e], (lane & ~3) | src);
+              if (w != 0.f) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                  if (FULL || c < ncv) {
+                    o[mt][c][0] = fmaf(w, __bfloat162float(v[8 * c + 2 * tig]), o[mt][c][0]);
+                    o[mt][c][1] = fmaf(w, __bfloat162float(v[8 * c + 2 * tig + 1]), o[mt][c][1]);
+                  }
+              }
+            }
+          }
+      group_sync();
+      if ((odd_rows >> lane) & 1) {
+        uint4* x = reinterpret_cast<uint4*>(st + kRows * kpitch + lane * vpitch);
+        for (int c = 0; c < ncv; ++c) x[c] = make_uint4(0u, 0u, 0u, 0u);
+      }
+      group_sync();
+    }
+    // ---- O' += P V'
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (FULL || c < ncv) {
+        uint32_t vf[4];
+        ldsm4_t(vf, v_addr + c * 16);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          mma16(o[mt][c], pa[mt][0], vf[0], vf[1]);
+          mma16(o[mt][c], pa[mt][1], vf[2], vf[3]);
+        }
+      }
+  }
+  cp_async_wait<0>();
+  __syncthreads();
+
+  // ---- merge the key groups (the ring is idle): per query the maximum, then sums and O' scaled to it
+  constexpr int Q = S::kQueries, OS = 8 * NC + 1;
+  float* wm = reinterpret_cast<float*>(ring);                // [4][Q]
+  float* wl = wm + kGroups * Q;                              // [4][Q]
+  float* wo = wl + kGroups * Q;                              // [4][Q][OS]
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    l[mt] += __shfl_xor_sync(kFull, l[mt], 1);
+    l[mt] += __shfl_xor_sync(kFull, l[mt], 2);
+    const int q = kg * Q + (rg * MT + mt) * 8 + gid;
+    if (tig == 0) { wm[q] = m[mt]; wl[q] = l[mt]; }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (FULL || c < ncv) {
+        wo[q * OS + 8 * c + 2 * tig] = o[mt][c][0] + o[mt][c][2];
+        wo[q * OS + 8 * c + 2 * tig + 1] = o[mt][c][1] + o[mt][c][3];
+      }
+  }
+  __syncthreads();
+  const int rp_v = 8 * ncv;
+  const int nq = min(Q, p.rows - row0);
+  for (int i = tid; i < nq * (rp_v + 2); i += S::kThreads) {
+    const int q = i / (rp_v + 2), c = i - q * (rp_v + 2);
+    const float M = fmaxf(fmaxf(wm[q], wm[Q + q]), fmaxf(wm[2 * Q + q], wm[3 * Q + q]));
+    const float mb = M == -INFINITY ? 0.f : M;
+    float acc = 0.f;
+#pragma unroll
+    for (int w = 0; w < kGroups; ++w)
+      acc = fmaf(c < rp_v ? wo[(w * Q + q) * OS + c] : wl[w * Q + q], ex2(wm[w * Q + q] - mb), acc);
+    float* part = p.partials + ((static_cast<int64_t>(unit) * p.rows + row0 + q) * p.splits + split) * p.part_stride;
+    if (c < rp_v) part[4 + c] = acc;
+    else if (c == rp_v) part[1] = acc;
+    else part[0] = M;
+  }
+}
+
+template <int NC, int MT, int WG, bool FULL>
+cudaError_t launch_instance(const MqDecodeParams& p, cudaStream_t s) {
+  using S = Shape<NC, MT, WG>;
+  static size_t configured[kMaxDevices] = {};
+  const cudaError_t e = ensure_dynamic_smem(mq_mma_kernel<NC, MT, WG, FULL>, S::kSmem, configured);
+  if (e != cudaSuccess) return e;
+  const int chunks = (p.rows + S::kQueries - 1) / S::kQueries;
+  mq_mma_kernel<NC, MT, WG, FULL><<<dim3(p.B * p.H * chunks, p.splits), S::kThreads, S::kSmem, s>>>(p);
+  return cudaGetLastError();
+}
+template <int NC>
+cudaError_t launch_rank(const MqDecodeParams& p, bool full, cudaStream_t s) {
+  if (p.rows <= 8) return full ? launch_instance<NC, 1, 1, true>(p, s) : launch_instance<NC, 1, 1, false>(p, s);
+  if (p.rows <= 16) return full ? launch_instance<NC, 2, 1, true>(p, s) : launch_instance<NC, 2, 1, false>(p, s);
+  return full ? launch_instance<NC, 2, 2, true>(p, s) : launch_instance<NC, 2, 2, false>(p, s);
+}
+
+}  // namespace
+
+MqShape mq_mma_shape(int rows, int max_rp) {
+  if (rows <= 8) return {8, max_rp <= 80 ? 2 : 1};
+  if (rows <= 16) return {16, max_rp <= 80 ? 2 : 1};
+  return {32, 1};
+}
+
+cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, int min_rp, cudaStream_t s, uint64_t* launches) {
+  cudaError_t e;
+  if (max_rp <= 64) e = launch_rank<8>(p, min_rp == 64, s);
+  else if (max_rp <= 80) e = launch_rank<10>(p, min_rp == 80, s);
+  else e = launch_rank<16>(p, min_rp == 128, s);
+  ++*launches;
+  return e;
+}
+
+}  // namespace ea

@@ -362,6 +362,10 @@ __device__ __forceinline__ int64_t physical_block(const SparseParams& p, int b, 
 // Launchers (each returns the CUDA error of its launch); `launches` is incremented per kernel.
 cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+struct MqShape { int queries, ctas_per_sm; };   // query rows of a CTA, resident CTAs
+MqShape mq_mma_shape(int rows, int max_rp);
+// 16-bit layers; max_rp / min_rp: widest and narrowest padded rank over heads and K/V
+cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, int min_rp, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_tree_commit(const TreeCommitParams& p, int sequences, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_block_bounds(const SparseParams& p, int dtype, cudaStream_t s, uint64_t* launches);
