@@ -128,6 +128,15 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return stream.cuda_stream
 
 
+def _call_on(device: torch.device, stream: Optional[torch.cuda.Stream], fn, *args) -> int:
+    """fn(*args, stream pointer) with `device` current: its current stream, or the one given."""
+    index = device.index if device.index is not None else torch.cuda.current_device()
+    if torch.cuda.current_device() == index:
+        return fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream)
+    with torch.cuda.device(index):
+        return fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream)
+
+
 def _make_desc(batch, n_heads, d_head, n_max, dtype, r_k, r_v, U_k, U_v, max_prefill_tokens, flags):
     """Returns (desc, keepalive): ctypes arrays must outlive the call that reads them."""
     rk = (ctypes.c_int32 * n_heads)(*[int(r) for r in r_k])
@@ -518,22 +527,22 @@ class EigenAttnLayer:
             if out is None:
                 out = self._new_out(self.B, T, self.H * group, self.d_head)
             po, sbo, sto = self._mq_tok(out, T, self.H * group)
-        with torch.cuda.device(self.device):
-            self._check(lib.eigen_attn_decode_tree(self.handle, pq, sbq, stq, int(group), pk, pv, sbk, stk, T, mask.data_ptr(),
-                                                   po, sbo, sto, flags, _stream_ptr(stream)), "eigen_attn_decode_tree")
+        self._check(_call_on(self.device, stream, lib.eigen_attn_decode_tree, self.handle, pq, sbq, stq, group, pk, pv, sbk, stk, T,
+                             mask.data_ptr(), po, sbo, sto, flags), "eigen_attn_decode_tree")
         return out
 
     def tree_commit(self, paths, T: int, stream=None) -> None:
         """eigen_attn_tree_commit: paths[b] = accepted tokens of sequence b, ascending (empty: none); T as in decode_tree."""
         assert len(paths) == self.B
-        arr = (ctypes.c_int32 * (self.B * T))()
-        counts = (ctypes.c_int32 * self.B)()
-        for b, path in enumerate(paths):
+        flat, counts = [], []
+        for path in paths:
             assert len(path) <= T
-            counts[b] = len(path)
-            arr[b * T:b * T + len(path)] = [int(x) for x in path]
-        with torch.cuda.device(self.device):
-            self._check(lib.eigen_attn_tree_commit(self.handle, arr, counts, int(T), _stream_ptr(stream)), "eigen_attn_tree_commit")
+            counts.append(len(path))
+            flat += path
+            flat += [0] * (T - len(path))
+        arr = (ctypes.c_int32 * (self.B * T))(*flat)
+        self._check(_call_on(self.device, stream, lib.eigen_attn_tree_commit, self.handle, arr, (ctypes.c_int32 * self.B)(*counts), T),
+                    "eigen_attn_tree_commit")
 
     # -- decode over a selection of blocks
     def sparse_attach(self, block_rows: int, stream=None) -> torch.Tensor:
@@ -542,18 +551,32 @@ class EigenAttnLayer:
         self._check(lib.eigen_attn_sparse_bytes(self.handle, int(block_rows), ctypes.byref(n)), "eigen_attn_sparse_bytes")
         self.sparse_buf = device_alloc(n.value, self.device)
         self.sparse_block = int(block_rows)
-        with torch.cuda.device(self.device):
-            self._check(lib.eigen_attn_sparse_attach(self.handle, int(block_rows), self.sparse_buf.data_ptr(), n.value,
-                                                     _stream_ptr(stream)), "eigen_attn_sparse_attach")
+        self._check(_call_on(self.device, stream, lib.eigen_attn_sparse_attach, self.handle, int(block_rows),
+                             self.sparse_buf.data_ptr(), n.value), "eigen_attn_sparse_attach")
+        slabs = []
+        for h in range(self.H):
+            off, blocks = _sz(0), ctypes.c_int32(0)
+            self._check(lib.eigen_attn_sparse_layout(self.handle, h, ctypes.byref(off), ctypes.byref(blocks)), "eigen_attn_sparse_layout")
+            slabs.append((off.value, self.cache_layout(h)[2]))
+        flat = self.sparse_buf.view(self.torch_dtype)
+        es = flat.element_size()
+        self._bounds = []
+        for off, rp in slabs:
+            self._bounds.append(flat.as_strided((self.B, blocks.value, 2, rp), (blocks.value * 2 * rp, 2 * rp, rp, 1),
+                                                flat.storage_offset() + off // es))
+        self._all_bounds = None
+        if len({rp for _, rp in slabs}) == 1:
+            one = self._bounds[0]
+            step = (slabs[1][0] - slabs[0][0]) // es if self.H > 1 else 0
+            self._all_bounds = flat.as_strided((self.H,) + tuple(one.shape), (step,) + tuple(one.stride()), one.storage_offset())
         return self.sparse_buf
 
     def sparse_detach(self, stream=None) -> None:
         self._check(lib.eigen_attn_sparse_attach(self.handle, 0, None, 0, _stream_ptr(stream)), "eigen_attn_sparse_attach")
-        self.sparse_buf = None
+        self.sparse_buf = self._bounds = self._all_bounds = None
 
     def sparse_sync(self, stream=None) -> None:
-        with torch.cuda.device(self.device):
-            self._check(lib.eigen_attn_sparse_sync(self.handle, _stream_ptr(stream)), "eigen_attn_sparse_sync")
+        self._check(_call_on(self.device, stream, lib.eigen_attn_sparse_sync, self.handle), "eigen_attn_sparse_sync")
 
     def sparse_lens(self):
         arr = (ctypes.c_int32 * self.B)()
@@ -563,21 +586,9 @@ class EigenAttnLayer:
     def sparse_bounds(self, head: Optional[int] = None) -> torch.Tensor:
         """View of head `head`'s bounds [B][blocks][2][rp_k] (minima, maxima); of all heads, [H][B][blocks][2][rp_k], with
         None (heads of one rank)."""
-        def layout(h):
-            off, blocks = _sz(0), ctypes.c_int32(0)
-            self._check(lib.eigen_attn_sparse_layout(self.handle, h, ctypes.byref(off), ctypes.byref(blocks)),
-                        "eigen_attn_sparse_layout")
-            return off.value, blocks.value
-        flat = self.sparse_buf.view(self.torch_dtype)
-        es = flat.element_size()
-        off, blocks = layout(0 if head is None else int(head))
-        rp = self.cache_layout(0 if head is None else int(head))[2]
-        one = flat.as_strided((self.B, blocks, 2, rp), (blocks * 2 * rp, 2 * rp, rp, 1), flat.storage_offset() + off // es)
-        if head is not None or self.H == 1:
-            return one if head is not None else one[None]
-        assert all(self.cache_layout(h)[2] == rp for h in range(self.H))
-        step = (layout(1)[0] - off) // es
-        return flat.as_strided((self.H,) + tuple(one.shape), (step,) + tuple(one.stride()), one.storage_offset())
+        view = self._all_bounds if head is None else self._bounds[head]
+        assert view is not None, "heads of different ranks: ask for one head"
+        return view
 
     def decode_sparse(self, q: torch.Tensor, n_blocks: int, group: int = 1, sink: int = 1, recent: int = 1,
                       out: Optional[torch.Tensor] = None, q_preprojected: bool = False, out_lowrank: bool = False,
@@ -602,10 +613,8 @@ class EigenAttnLayer:
         index = None
         if return_index:
             index = device_alloc(4 * self.B * self.H * int(n_blocks), self.device).view(torch.int32).view(self.B, self.H, int(n_blocks))
-        with torch.cuda.device(self.device):
-            self._check(lib.eigen_attn_decode_sparse(self.handle, pq, sbq, int(group), int(n_blocks), int(sink), int(recent), po,
-                                                     sbo, index.data_ptr() if index is not None else None, flags,
-                                                     _stream_ptr(stream)), "eigen_attn_decode_sparse")
+        self._check(_call_on(self.device, stream, lib.eigen_attn_decode_sparse, self.handle, pq, sbq, group, n_blocks, sink, recent,
+                             po, sbo, None if index is None else index.data_ptr(), flags), "eigen_attn_decode_sparse")
         return (out, index) if return_index else out
 
     def set_rope(self, base: float, interleaved: bool = False, stream=None) -> None:

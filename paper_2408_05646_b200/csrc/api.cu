@@ -1370,29 +1370,42 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size
   p.n = h->len; p.n_max = h->desc.n_max;
   p.rows = p.tokens * p.group;
   p.q_stride = L.max_rp_k; p.part_stride = L.part_stride; p.lr_v_width = L.sum_rp_v;
-  // CTAs per run of query rows: waves of resident CTAs, a start-up worth a tile or two per CTA, and room for the
-  // partials
+  // Tiles of a piece: the CTAs run in waves of resident ones, each pays a start-up worth a tile or two; pieces are cut to
+  // one size, so a shorter sequence of the batch has fewer of them; the partials must have room.
   const bool mma = h->desc.dtype == EA_BF16;
   const int max_rp = L.max_rp_k > L.max_rp_v ? L.max_rp_k : L.max_rp_v;
   const ea::MqShape shape = mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::MqShape{8, 2};
-  const int64_t ctas = static_cast<int64_t>(p.B) * p.H * ((p.rows + shape.queries - 1) / shape.queries);
+  const int64_t chunks = static_cast<int64_t>(p.H) * ((p.rows + shape.queries - 1) / shape.queries);   // of one sequence
   int64_t cap = static_cast<int64_t>(slots) / (static_cast<int64_t>(p.B) * p.H * p.rows);
   if (cap > p.tiles) cap = p.tiles;
   if (cap > 65535) cap = 65535;
   if (cap < 1) cap = 1;
-  int64_t splits = 1;
+  int64_t per = p.tiles;
   if (h->opt_ctas > 0) {
-    splits = (h->opt_ctas + ctas - 1) / ctas;
+    int64_t splits = (h->opt_ctas + chunks * p.B - 1) / (chunks * p.B);
     if (splits > cap) splits = cap;
+    per = (p.tiles + splits - 1) / splits;
   } else {
     const int64_t wave = static_cast<int64_t>(h->sm_count) * shape.ctas_per_sm;
     int64_t best = INT64_MAX;
     for (int64_t s2 = 1; s2 <= cap && s2 <= 256; ++s2) {
-      const int64_t cost = ((ctas * s2 + wave - 1) / wave) * ((p.tiles + s2 - 1) / s2 + 2);
-      if (cost < best) { best = cost; splits = s2; }
+      const int64_t size = (p.tiles + s2 - 1) / s2;
+      if (s2 > 1 && (p.tiles + size - 1) / size < s2) continue;        // the same pieces as with fewer
+      int64_t pieces = 0;
+      if (h->max_deficit > 0 && p.list == nullptr) {
+        for (int b = 0; b < p.B; ++b) {
+          const int64_t t = (p.n - h->deficit[b] + p.tail + 127) / 128;
+          pieces += t > size ? (t + size - 1) / size : 1;
+        }
+      } else {
+        pieces = s2 * p.B;
+      }
+      const int64_t cost = ((pieces * chunks + wave - 1) / wave) * (size + 2);
+      if (cost < best) { best = cost; per = size; }
     }
   }
-  p.splits = static_cast<int32_t>(splits);
+  p.per = static_cast<int32_t>(per);
+  p.splits = static_cast<int32_t>((p.tiles + per - 1) / per);
   if (h->ev_start) cudaEventRecord(h->ev_start, s);
   int min_rp = max_rp;
   for (const HeadInfo& hi : L.heads) {
@@ -1402,7 +1415,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size
   cudaError_t e = mma ? ea::launch_mq_mma(p, max_rp, min_rp, s, &h->launches)
                       : ea::launch_mq_simt(p, h->desc.dtype, s, &h->launches);
   if (h->ev_stop) cudaEventRecord(h->ev_stop, s);
-  if (e == cudaSuccess) e = ea::launch_mq_combine(p, h->desc.dtype, s, &h->launches);
+  if (e == cudaSuccess) e = ea::launch_mq_combine(p, h->desc.dtype, L.max_rp_v, s, &h->launches);
   if (e != cudaSuccess) return cuda_fail(h, e, who);
   return EA_OK;
 }
@@ -1472,13 +1485,32 @@ ea_status eigen_attn_decode_tree(eigen_attn_t h, const void* d_q, int64_t stride
     return fail(h, EA_ERR_CAPACITY, "decode_tree: %d drafted rows exceed the capacity of sequence %d (%lld rows)", T, bad,
                 static_cast<long long>(capacity_of(h, bad)));
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  // the drafted rows, behind every sequence's own; the length stays where it is
-  const cudaError_t e = launch_append_rows(h, d_k, d_v, T, stride_b_kv, stride_t_kv, flags & EA_KV_PREPROJECTED, s);
-  if (e != cudaSuccess) return cuda_fail(h, e, "decode_tree append launch");
+  // the drafted rows, behind every sequence's own (the length stays where it is), and the queries
   float* qp = reinterpret_cast<float*>(h->tree_buf);
-  const ea_status sq = launch_query(h, "decode_tree query launch", d_q, stride_b_q, stride_t_q, group, T,
-                                    flags & EA_Q_PREPROJECTED, qp, nullptr, s);
-  if (sq != EA_OK) return sq;
+  cudaError_t e = cudaSuccess;
+  if (flags & EA_KV_PREPROJECTED) e = launch_append_rows(h, d_k, d_v, T, stride_b_kv, stride_t_kv, EA_KV_PREPROJECTED, s);
+  if (e == cudaSuccess && (flags & (EA_Q_PREPROJECTED | EA_KV_PREPROJECTED)) != (EA_Q_PREPROJECTED | EA_KV_PREPROJECTED)) {
+    ea::MqProjectParams pp{};
+    pp.heads = dev_heads(h); pp.basis = dev_basis(h); pp.cache = h->cache; pp.deficit = dev_deficit(h); pp.pages = dev_pages(h);
+    pp.q = d_q; pp.q_stride_b = stride_b_q; pp.q_stride_t = stride_t_q; pp.qp = qp;
+    pp.with_q = (flags & EA_Q_PREPROJECTED) ? 0 : 1;
+    bool aligned = pp.with_q ? reinterpret_cast<uintptr_t>(d_q) % 16 == 0 && stride_b_q * h->L.es % 16 == 0 && stride_t_q * h->L.es % 16 == 0 : true;
+    if (!(flags & EA_KV_PREPROJECTED)) {
+      pp.k = d_k; pp.v = d_v; pp.kv_stride_b = stride_b_kv; pp.kv_stride_t = stride_t_kv;
+      aligned = aligned && reinterpret_cast<uintptr_t>(d_k) % 16 == 0 && reinterpret_cast<uintptr_t>(d_v) % 16 == 0 &&
+                stride_b_kv * h->L.es % 16 == 0 && stride_t_kv * h->L.es % 16 == 0;
+    }
+    pp.aligned = aligned ? 1 : 0;
+    pp.B = h->desc.batch; pp.H = h->desc.n_heads; pp.d_head = h->desc.d_head; pp.group = group; pp.tokens = T;
+    pp.q_stride = h->L.max_rp_k; pp.n_max = h->desc.n_max; pp.row0 = h->len;
+    pp.q_scale = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(h->desc.d_head)));
+    e = ea::launch_mq_project(pp, h->desc.dtype, h->L.max_rp_k > h->L.max_rp_v ? h->L.max_rp_k : h->L.max_rp_v, s, &h->launches);
+  }
+  if (e != cudaSuccess) return cuda_fail(h, e, "decode_tree projection launch");
+  if (flags & EA_Q_PREPROJECTED) {
+    const ea_status sq = launch_query(h, "decode_tree query launch", d_q, 0, 0, group, T, EA_Q_PREPROJECTED, qp, nullptr, s);
+    if (sq != EA_OK) return sq;
+  }
   ea::MqDecodeParams p{};
   p.qp = qp;
   p.partials = reinterpret_cast<float*>(h->tree_buf + h->tree_off_part);

@@ -8,6 +8,7 @@
 #include <cuda_bf16.h>
 
 #include "internal.h"
+#include "tc_common.cuh"
 
 namespace ea {
 namespace {
@@ -61,51 +62,87 @@ __device__ __forceinline__ double tiny_double(uint32_t bits16) {
   return __hiloint2double(static_cast<int>(((bits16 & 0x8000u) << 16) | ((bits16 & 0x7fffu) << 13)), 0);
 }
 
-// Eight 16-bit channels (or four of 32 bits) of lo and hi against the same channels of the query.
-__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, double (&acc)[2], __nv_bfloat16) {
+// 16 bytes of lo and hi (eight 16-bit channels, or four of 32 bits) against the same channels of GQ queries: a channel
+// contributes q hi where q > 0 and q lo where q < 0.
+template <int GQ>
+__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, int q_stride, double (&acc)[GQ], __nv_bfloat16) {
+  const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t lb = i & 1 ? l[i >> 1] >> 16 : l[i >> 1] & 0xffffu, ub = i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xffffu;
+    const double dl = tiny_double(lb), du = tiny_double(ub);
+#pragma unroll
+    for (int g = 0; g < GQ; ++g) {
+      const double x = q[g * q_stride + i];
+      acc[g] = fma(x, x < 0 ? dl : du, acc[g]);
+    }
+  }
+}
+template <int GQ>
+__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, int q_stride, double (&acc)[GQ], float) {
   const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const double q0 = q[2 * i], q1 = q[2 * i + 1];
-    acc[0] = fma(q0, tiny_double((q0 < 0 ? l[i] : u[i]) & 0xffffu), acc[0]);
-    acc[1] = fma(q1, tiny_double((q1 < 0 ? l[i] : u[i]) >> 16), acc[1]);
-  }
-}
-__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, double (&acc)[2], float) {
-  const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
+    const double dl = __uint_as_float(l[i]), du = __uint_as_float(u[i]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) acc[i & 1] = fma(q[i], static_cast<double>(__uint_as_float(q[i] < 0 ? l[i] : u[i])), acc[i & 1]);
+    for (int g = 0; g < GQ; ++g) {
+      const double x = q[g * q_stride + i];
+      acc[g] = fma(x, x < 0 ? dl : du, acc[g]);
+    }
+  }
 }
 template <typename T> __device__ __forceinline__ double query_factor();
 template <> __device__ __forceinline__ double query_factor<__nv_bfloat16>() { return __hiloint2double((1023 + 896) << 20, 0); }   // 2^896
 template <> __device__ __forceinline__ double query_factor<float>() { return 1.0; }
 
-// One thread per block; the queries of the group sit in shared memory.
-template <typename T>
-__global__ void __launch_bounds__(128) block_scores_kernel(const SparseParams p) {
-  extern __shared__ double qs[];             // [group][rp_k]
-  const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B;
+// A CTA takes 128 blocks of a unit: their bounds come in by coalesced 16-byte copies (in shared memory a block's bounds sit
+// at an odd multiple of 16 bytes, so that 128 threads read one each without bank conflicts), then one thread scores one
+// block for the group's queries, GQ at a time.
+constexpr int kScoreBlocks = 128;
+template <typename T, int GQ>
+__global__ void __launch_bounds__(kScoreBlocks) block_scores_kernel(const SparseParams p) {
+  extern __shared__ __align__(16) unsigned char sm[];
+  __shared__ int64_t phys[kScoreBlocks];
+  const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B, tid = threadIdx.x;
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
   const int have = (n_b + (1 << p.block_shift) - 1) >> p.block_shift;
-  const int first = p.sink + blockIdx.y * 128, last = have - p.recent;
+  const int first = p.sink + blockIdx.y * kScoreBlocks, last = have - p.recent;
   if (have <= p.list_len || first >= last) return;           // nothing to choose
   const HeadInfo hd = p.heads[h];
-  for (int i = threadIdx.x; i < p.group * hd.rp_k; i += 128) {
-    const int g = i / hd.rp_k, c = i - g * hd.rp_k;
-    qs[i] = p.q64[(static_cast<int64_t>(unit) * p.group + g) * p.q_stride + c] * query_factor<T>();
-  }
-  __syncthreads();
-  const int blk = first + threadIdx.x;
-  if (blk >= last) return;
   constexpr int kPer = 16 / sizeof(T);       // channels of a 16-byte piece
-  const int nc = hd.rp_k / kPer;
-  const uint4* lo = reinterpret_cast<const uint4*>(p.bounds + p.slab[h]) + physical_block(p, b, blk) * 2 * nc;
+  const int nc = hd.rp_k / kPer, pitch = (2 * nc + 1) * 16;
+  const int groups = (p.group + GQ - 1) / GQ * GQ;
+  double* qs = reinterpret_cast<double*>(sm);                // [groups][rp_k]
+  unsigned char* bounds = sm + sizeof(double) * groups * hd.rp_k;
+  const int blk = first + tid;
+  phys[tid] = blk < last ? physical_block(p, b, blk) : -1;
+  __syncthreads();
+  const char* slab = p.bounds + p.slab[h];
+  const int per = 2 * nc;
+  for (int i = tid; i < kScoreBlocks * per; i += kScoreBlocks) {
+    const int j = i / per, c = i - j * per;
+    const int64_t at = phys[j];
+    if (at >= 0) tc::cp_async16(bounds + j * pitch + c * 16, slab + (at * per + c) * 16, 16);
+  }
+  tc::cp_async_commit();
+  for (int i = tid; i < groups * hd.rp_k; i += kScoreBlocks) {
+    const int g = i / hd.rp_k, c = i - g * hd.rp_k;
+    qs[i] = g < p.group ? p.q64[(static_cast<int64_t>(unit) * p.group + g) * p.q_stride + c] * query_factor<T>() : 0.0;
+  }
+  tc::cp_async_wait<0>();
+  __syncthreads();
+  if (blk >= last) return;
+  const uint4* lo = reinterpret_cast<const uint4*>(bounds + tid * pitch);
   double best = 0;
-  for (int g = 0; g < p.group; ++g) {
-    double acc[2] = {0, 0};
-    for (int c = 0; c < nc; ++c) add_bounds(__ldg(lo + c), __ldg(lo + nc + c), qs + g * hd.rp_k + c * kPer, acc, T());
-    const double s = acc[0] + acc[1];
-    best = g == 0 || s > best ? s : best;
+  for (int g0 = 0; g0 < p.group; g0 += GQ) {
+    double acc[GQ];
+#pragma unroll
+    for (int g = 0; g < GQ; ++g) acc[g] = 0;
+#pragma unroll 2
+    for (int c = 0; c < nc; ++c) add_bounds<GQ>(lo[c], lo[nc + c], qs + g0 * hd.rp_k + c * kPer, hd.rp_k, acc, T());
+#pragma unroll
+    for (int g = 0; g < GQ; ++g)
+      if (g0 + g < p.group && (g0 + g == 0 || acc[g] > best)) best = acc[g];
   }
   // the position bias of the block's last row, the one it takes least from
   if (hd.alibi_slope != 0.f)
@@ -228,13 +265,22 @@ cudaError_t launch_block_bounds(const SparseParams& p, int dtype, cudaStream_t s
   return cudaGetLastError();
 }
 
-cudaError_t launch_block_scores(const SparseParams& p, int dtype, int max_rp_k, cudaStream_t s, uint64_t* launches) {
-  const dim3 grid(p.B * p.H, (p.max_blocks + 127) / 128);
-  const size_t smem = sizeof(double) * p.group * max_rp_k;
-  if (dtype == 0) block_scores_kernel<__nv_bfloat16><<<grid, 128, smem, s>>>(p);
-  else block_scores_kernel<float><<<grid, 128, smem, s>>>(p);
-  ++*launches;
+template <typename T, int GQ>
+static cudaError_t launch_scores_t(const SparseParams& p, int max_rp_k, cudaStream_t s) {
+  const int groups = (p.group + GQ - 1) / GQ * GQ;
+  const size_t smem = sizeof(double) * groups * max_rp_k + static_cast<size_t>(kScoreBlocks) * (2 * max_rp_k * sizeof(T) + 16);
+  static size_t configured[kMaxDevices] = {};
+  const cudaError_t e = ensure_dynamic_smem(block_scores_kernel<T, GQ>, smem, configured);
+  if (e != cudaSuccess) return e;
+  const int middle = p.max_blocks - p.sink - p.recent;
+  block_scores_kernel<T, GQ><<<dim3(p.B * p.H, (middle + kScoreBlocks - 1) / kScoreBlocks), kScoreBlocks, smem, s>>>(p);
   return cudaGetLastError();
+}
+
+cudaError_t launch_block_scores(const SparseParams& p, int dtype, int max_rp_k, cudaStream_t s, uint64_t* launches) {
+  ++*launches;
+  if (p.group == 1) return dtype == 0 ? launch_scores_t<__nv_bfloat16, 1>(p, max_rp_k, s) : launch_scores_t<float, 1>(p, max_rp_k, s);
+  return dtype == 0 ? launch_scores_t<__nv_bfloat16, 4>(p, max_rp_k, s) : launch_scores_t<float, 4>(p, max_rp_k, s);
 }
 
 cudaError_t launch_block_select(const SparseParams& p, cudaStream_t s, uint64_t* launches) {

@@ -1,8 +1,8 @@
 // Several query rows per K/V head over one sequence's rows: the drafted tokens of a tree (each with its group of query
 // heads), or one token over a list of blocks.  This file holds the parts that are the same for every layer type:
-//   mq_query_kernel    Q' = Q U^K of every query row (and in 64 bits for the block scores)
+//   mq_project_*, mq_query64, mq_copy_query: Q' of every query row, K' and V' of drafted tokens
 //   mq_simt_kernel     attention on the CUDA cores, any dtype (single-precision layers run on it)
-//   mq_combine_kernel  merges the pieces of a query row and lifts o' through (U^V)^T
+//   mq_combine_*       merge the pieces of a query row and lift o' through (U^V)^T
 //   tree_commit_kernel moves the rows of an accepted path together
 #include <cuda_bf16.h>
 
@@ -29,56 +29,252 @@ __device__ __forceinline__ uint64_t tree_mask(uint64_t m, int tokens) { return t
 // How far behind the cached rows token t sits: the number of the other tokens it sees.
 __device__ __forceinline__ int tree_depth(uint64_t m, int t) { return __popcll(m & ~(1ull << t)); }
 
-// ---------------------------------------------------------------- Q'
+// ---------------------------------------------------------------- projections
 
-// One CTA per (unit, run of kQueryRows query rows): thread c owns column c of Q'.  With q64 the sums are taken in 64
-// bits (products of a 16-bit and a 32-bit number are exact there, so the order of the sum moves a block score by
-// 1e-16 of its terms, far below any two scores that are not equal).
-constexpr int kQueryRows = 8;
-template <typename T, typename Acc>
-__global__ void __launch_bounds__(128) mq_query_kernel(const MqQueryParams p) {
-  __shared__ float x[kQueryRows][128];
-  const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B;
-  const int r0 = blockIdx.y * kQueryRows, nr = min(kQueryRows, p.rows - r0);
-  const HeadInfo hd = p.heads[h];
-  const T* q = static_cast<const T*>(p.q);
-  const int c = threadIdx.x;
-  Acc acc[kQueryRows];
-  if (p.flags & 0x1u) {                      // EA_Q_PREPROJECTED: the rows are rank-r already
-    for (int r = 0; r < nr; ++r) {
-      const int t = (r0 + r) / p.group, i = (r0 + r) - t * p.group;
-      const T* src = q + (static_cast<int64_t>(b) * p.tokens + t) * p.group * p.lr_k_width +
-                     static_cast<int64_t>(p.group) * hd.lr_k_off + static_cast<int64_t>(i) * hd.rp_k;
-      acc[r] = c < hd.r_k ? static_cast<Acc>(to_f<T>(src[c])) : Acc(0);
-    }
-  } else {
-    for (int idx = threadIdx.x; idx < nr * p.d_head; idx += 128) {
-      const int r = idx / p.d_head, d = idx - r * p.d_head;
-      const int t = (r0 + r) / p.group, i = (r0 + r) - t * p.group;
-      x[r][d] = to_f<T>(q[b * p.q_stride_b + t * p.q_stride_t + (static_cast<int64_t>(h) * p.group + i) * p.d_head + d]);
-    }
-    __syncthreads();
+// Packed pairs of fp32: each half is the ordinary fused multiply-add.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ void ffma2(uint64_t& d, uint64_t a, uint64_t b) {
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b));
+}
+
+// Token rows of one head and kind (0: queries, 1: keys, 2: values) and where their rank-r form goes.
+struct Rows {
+  int kind, h, count;      // count: rows of this head and kind
+  int rp;
+  const float* U;          // [d_head][rp]
+};
+__device__ __forceinline__ Rows rows_of(const MqProjectParams& p, int kind, int h) {
+  Rows r;
+  const HeadInfo& hd = p.heads[h];
+  r.kind = kind; r.h = h;
+  r.count = p.B * p.tokens * (kind == 0 ? p.group : 1);
+  r.rp = kind == 2 ? hd.rp_v : hd.rp_k;
+  r.U = p.basis + (kind == 2 ? hd.uv_off : hd.uk_off);
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ const T* row_source(const MqProjectParams& p, const Rows& w, int row) {
+  if (w.kind == 0) {
+    const int bt = row / p.group, i = row - bt * p.group, b = bt / p.tokens, t = bt - b * p.tokens;
+    return static_cast<const T*>(p.q) + b * p.q_stride_b + t * p.q_stride_t + (static_cast<int64_t>(w.h) * p.group + i) * p.d_head;
+  }
+  const int b = row / p.tokens, t = row - b * p.tokens;
+  return static_cast<const T*>(w.kind == 1 ? p.k : p.v) + b * p.kv_stride_b + t * p.kv_stride_t + static_cast<int64_t>(w.h) * p.d_head;
+}
+// Columns c..c+N-1 of a projected row: scaled into the scratch (queries) or rounded into the cache.
+template <typename T, int N>
+__device__ __forceinline__ void store_row(const MqProjectParams& p, const Rows& w, int row, int c, const float (&x)[N]) {
+  if (w.kind == 0) {
+    const int bt = row / p.group, i = row - bt * p.group, b = bt / p.tokens, t = bt - b * p.tokens;
+    float* dst = p.qp + ((static_cast<int64_t>(w.h) * p.B + b) * p.tokens * p.group + t * p.group + i) * p.q_stride + c;
 #pragma unroll
-    for (int r = 0; r < kQueryRows; ++r) acc[r] = Acc(0);
-    if (c < hd.rp_k) {
-      const float* U = p.basis + hd.uk_off + c;
-#pragma unroll 8
-      for (int d = 0; d < p.d_head; ++d) {
-        const Acc u = static_cast<Acc>(__ldg(U + d * hd.rp_k));
+    for (int j = 0; j < N; j += 2) *reinterpret_cast<float2*>(dst + j) = make_float2(x[j] * p.q_scale, x[j + 1] * p.q_scale);
+    return;
+  }
+  const int b = row / p.tokens, t = row - b * p.tokens;
+  const HeadInfo& hd = p.heads[w.h];
+  const int64_t crow = physical_row(p.pages, b, p.n_max, p.row0 - (p.deficit ? __ldg(p.deficit + b) : 0) + t);
+  T* dst = reinterpret_cast<T*>(p.cache + (w.kind == 1 ? hd.k_off : hd.v_off)) + crow * w.rp + c;
 #pragma unroll
-        for (int r = 0; r < kQueryRows; ++r)
-          if (r < nr) acc[r] += static_cast<Acc>(x[r][d]) * u;
+  for (int j = 0; j < N; j += 2) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(dst + j) = tc::pack_bf16(x[j], x[j + 1]);
+    else *reinterpret_cast<float2*>(dst + j) = make_float2(x[j], x[j + 1]);
+  }
+}
+
+// Every output is one chain of fused multiply-adds over d_head in ascending order, as in the append kernel: a drafted row
+// that is accepted is bit for bit the row that appending its token would have stored.
+//
+// Many rows: a CTA takes 64 rows of one head and kind, a thread 8 rows x 4 columns (rows in packed pairs), both operands
+// in shared memory.  Per step of d: three 16-byte loads and 16 packed multiply-adds, so the arithmetic is what bounds it.
+constexpr int kPrRows = 64, kPrPitch = kPrRows + 4;
+template <typename T>
+__global__ void __launch_bounds__(256) mq_project_many_kernel(const __grid_constant__ MqProjectParams p) {
+  extern __shared__ __align__(16) float sm[];
+  const int tiles_q = (p.B * p.tokens * p.group + kPrRows - 1) / kPrRows, tiles_kv = (p.B * p.tokens + kPrRows - 1) / kPrRows;
+  const int nq = p.with_q ? tiles_q : 0;
+  int tile = blockIdx.x;
+  const int kind = tile < nq ? 0 : tile - nq < tiles_kv ? 1 : 2;
+  tile -= kind == 0 ? 0 : kind == 1 ? nq : nq + tiles_kv;
+  const Rows w = rows_of(p, kind, blockIdx.y);
+  float* xt = sm;                            // [d_head][68]: the rows, transposed
+  float* us = sm + p.d_head * kPrPitch;      // [d_head][rp]
+  const int tid = threadIdx.x, r0 = tile * kPrRows;
+  for (int i = tid; i < p.d_head * w.rp / 4; i += 256) tc::cp_async16(us + 4 * i, w.U + 4 * i, 16);
+  tc::cp_async_commit();
+  constexpr int kVec = 16 / sizeof(T);
+  const int pieces = p.d_head / kVec;
+  for (int i = tid; i < kPrRows * pieces; i += 256) {
+    const int r = i % kPrRows, d = i / kPrRows * kVec;
+    float x[kVec];
+    if (r0 + r < w.count) {
+      const T* src = row_source<T>(p, w, r0 + r) + d;
+      if (p.aligned) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(src));
+        const T* e = reinterpret_cast<const T*>(&v);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) x[j] = to_f<T>(e[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) x[j] = to_f<T>(src[j]);
       }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) x[j] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) xt[(d + j) * kPrPitch + r] = x[j];
+  }
+  tc::cp_async_wait<0>();
+  __syncthreads();
+  const int rg = tid & 7, cg = tid >> 3;     // 8 rows from 8 rg, 4 columns from 4 cg
+  if (4 * cg >= w.rp) return;
+  uint64_t acc[4][4];                        // [column][pair of rows]
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[c][r] = 0;
+  const float* xr = xt + 8 * rg;
+  const float* ur = us + 4 * cg;
+#pragma unroll 4
+  for (int d = 0; d < p.d_head; ++d) {
+    const ulonglong2 x0 = *reinterpret_cast<const ulonglong2*>(xr + d * kPrPitch);
+    const ulonglong2 x1 = *reinterpret_cast<const ulonglong2*>(xr + d * kPrPitch + 4);
+    const float4 u = *reinterpret_cast<const float4*>(ur + d * w.rp);
+    const uint64_t uu[4] = {pack2(u.x, u.x), pack2(u.y, u.y), pack2(u.z, u.z), pack2(u.w, u.w)};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      ffma2(acc[c][0], x0.x, uu[c]);
+      ffma2(acc[c][1], x0.y, uu[c]);
+      ffma2(acc[c][2], x1.x, uu[c]);
+      ffma2(acc[c][3], x1.y, uu[c]);
     }
   }
-  if (c >= hd.rp_k) return;
-  const int64_t row0 = static_cast<int64_t>(unit) * p.rows + r0;
 #pragma unroll
-  for (int r = 0; r < kQueryRows; ++r)
-    if (r < nr) {
-      p.qp[(row0 + r) * p.q_stride + c] = static_cast<float>(acc[r] * static_cast<Acc>(kLog2e * p.scale));
-      if (p.q64) p.q64[(row0 + r) * p.q_stride + c] = static_cast<double>(acc[r]) * p.scale;
+  for (int r = 0; r < 4; ++r) {
+    const float2 v[4] = {unpack2(acc[0][r]), unpack2(acc[1][r]), unpack2(acc[2][r]), unpack2(acc[3][r])};
+    const int row = r0 + 8 * rg + 2 * r;
+    const float even[4] = {v[0].x, v[1].x, v[2].x, v[3].x}, odd[4] = {v[0].y, v[1].y, v[2].y, v[3].y};
+    if (row < w.count) store_row<T, 4>(p, w, row, 4 * cg, even);
+    if (row + 1 < w.count) store_row<T, 4>(p, w, row + 1, 4 * cg, odd);
+  }
+}
+
+// Few rows (a batch of one, short trees): latency is all.  A CTA takes 8 rows x 32 columns, a thread one row and a pair of
+// columns; the rows and the 16 KB of the basis arrive together.
+constexpr int kPfRows = 8, kPfCols = 32;
+template <typename T>
+__global__ void __launch_bounds__(128) mq_project_few_kernel(const __grid_constant__ MqProjectParams p) {
+  __shared__ __align__(16) float us[128 * kPfCols];
+  __shared__ float xs[kPfRows][128 + 1];
+  const int tiles_q = (p.B * p.tokens * p.group + kPfRows - 1) / kPfRows, tiles_kv = (p.B * p.tokens + kPfRows - 1) / kPfRows;
+  const int nq = p.with_q ? tiles_q : 0;
+  int tile = blockIdx.x;
+  const int kind = tile < nq ? 0 : tile - nq < tiles_kv ? 1 : 2;
+  tile -= kind == 0 ? 0 : kind == 1 ? nq : nq + tiles_kv;
+  const Rows w = rows_of(p, kind, blockIdx.y);
+  const int c0 = blockIdx.z * kPfCols, r0 = tile * kPfRows, tid = threadIdx.x;
+  if (c0 >= w.rp) return;
+  const int nc = min(kPfCols, w.rp - c0);    // a multiple of 8
+  for (int i = tid; i < p.d_head * (kPfCols / 4); i += 128) {
+    const int d = i / (kPfCols / 4), c = i % (kPfCols / 4) * 4;
+    if (c < nc) tc::cp_async16(us + d * kPfCols + c, w.U + d * w.rp + c0 + c, 16);
+  }
+  tc::cp_async_commit();
+  const int nr = min(kPfRows, w.count - r0);
+  for (int i = tid; i < nr * p.d_head; i += 128) {
+    const int r = i / p.d_head, d = i - r * p.d_head;
+    xs[r][d] = to_f<T>(row_source<T>(p, w, r0 + r)[d]);
+  }
+  tc::cp_async_wait<0>();
+  __syncthreads();
+  const int r = tid >> 4, c = 2 * (tid & 15);
+  if (r >= nr || c >= nc) return;
+  uint64_t acc = 0;
+#pragma unroll 16
+  for (int d = 0; d < p.d_head; ++d)
+    ffma2(acc, pack2(xs[r][d], xs[r][d]), *reinterpret_cast<const uint64_t*>(us + d * kPfCols + c));
+  const float2 v = unpack2(acc);
+  const float x[2] = {v.x, v.y};
+  store_row<T, 2>(p, w, r0 + r, c0 + c, x);
+}
+
+// Queries that are rank-r already: into the scratch.
+template <typename T>
+__global__ void __launch_bounds__(128) mq_copy_query_kernel(const MqQueryParams p) {
+  const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B, row = blockIdx.y, c = threadIdx.x;
+  const HeadInfo hd = p.heads[h];
+  if (c >= hd.rp_k) return;
+  const int t = row / p.group, i = row - t * p.group;
+  const T* src = static_cast<const T*>(p.q) + (static_cast<int64_t>(b) * p.tokens + t) * p.group * p.lr_k_width +
+                 static_cast<int64_t>(p.group) * hd.lr_k_off + static_cast<int64_t>(i) * hd.rp_k;
+  const double x = c < hd.r_k ? static_cast<double>(to_f<T>(src[c])) : 0.0;
+  const int64_t at = (static_cast<int64_t>(unit) * p.rows + row) * p.q_stride + c;
+  p.qp[at] = static_cast<float>(x * (kLog2e * p.scale));
+  if (p.q64) p.q64[at] = x * p.scale;
+}
+
+// Q' of one token in 64 bits, for the block scores (and rounded once for the attention): products of a 16-bit and a 32-bit
+// number are exact there, so the order of the sum moves a score by 1e-16 of its terms, far below any two scores that are
+// not equal.  One CTA per unit: threads (column, share of d_head), four query heads of the group at a time; the shares are
+// added in a fixed order.
+constexpr int kQ64Threads = 256, kQ64Rows = 4;
+template <typename T>
+__global__ void __launch_bounds__(kQ64Threads) mq_query64_kernel(const MqQueryParams p) {
+  __shared__ double x[kQ64Rows][128];
+  __shared__ double part[kQ64Threads][kQ64Rows];
+  const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B, tid = threadIdx.x;
+  const HeadInfo hd = p.heads[h];
+  const T* q = static_cast<const T*>(p.q) + b * p.q_stride_b + static_cast<int64_t>(h) * p.group * p.d_head;
+  const int shares = kQ64Threads / hd.rp_k;                  // at least two
+  const int share = tid / hd.rp_k, c = tid - share * hd.rp_k;
+  const int each = (p.d_head + shares - 1) / shares, d0 = share * each, d1 = min(p.d_head, d0 + each);
+  const float* U = p.basis + hd.uk_off + c;
+  for (int g0 = 0; g0 < p.group; g0 += kQ64Rows) {
+    const int ng = min(kQ64Rows, p.group - g0);
+    for (int i = tid; i < ng * p.d_head; i += kQ64Threads) x[i / p.d_head][i % p.d_head] = to_f<T>(q[static_cast<int64_t>(g0) * p.d_head + i]);
+    __syncthreads();
+    double acc[kQ64Rows] = {0, 0, 0, 0};
+    if (share < shares) {
+      for (int d = d0; d < d1; d += 8) {
+        float u[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = d + j < d1 ? __ldg(U + (d + j) * hd.rp_k) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const double uu = u[j];
+          const int dd = min(d + j, p.d_head - 1);
+          if (ng == 1) {
+            acc[0] = fma(x[0][dd], uu, acc[0]);
+          } else {
+#pragma unroll
+            for (int g = 0; g < kQ64Rows; ++g) acc[g] = fma(x[g][dd], uu, acc[g]);
+          }
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < kQ64Rows; ++g) part[tid][g] = acc[g];
     }
+    __syncthreads();
+    for (int i = tid; i < ng * hd.rp_k; i += kQ64Threads) {
+      const int g = i / hd.rp_k, cc = i - g * hd.rp_k;
+      double s = 0;
+      for (int k = 0; k < shares; ++k) s += part[k * hd.rp_k + cc][g];
+      const int64_t at = (static_cast<int64_t>(unit) * p.rows + g0 + g) * p.q_stride + cc;
+      p.qp[at] = static_cast<float>(s * (kLog2e * p.scale));
+      p.q64[at] = s * p.scale;
+    }
+    __syncthreads();
+  }
 }
 
 // ---------------------------------------------------------------- attention on the CUDA cores
@@ -106,9 +302,9 @@ __global__ void __launch_bounds__(256) mq_simt_kernel(const MqDecodeParams p) {
 
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
   const int64_t end = p.list ? static_cast<int64_t>(p.list_len) << p.block_shift : static_cast<int64_t>(n_b) + p.tail;
-  const int per = (p.tiles + p.splits - 1) / p.splits;
-  const int64_t lo = min(end, static_cast<int64_t>(split) * per * 128);
-  const int64_t hi = min(end, lo + static_cast<int64_t>(per) * 128);
+  const int64_t lo = static_cast<int64_t>(split) * p.per * 128;
+  if (split > 0 && lo >= end) return;        // a shorter sequence: nothing left (its first piece always reports)
+  const int64_t hi = min(end, lo + static_cast<int64_t>(p.per) * 128);
   const uint64_t* masks = p.mask + static_cast<int64_t>(b) * p.tokens;
   const uint64_t seen = p.tail && live ? tree_mask(masks[t], p.tokens) : 0;
   const int pos = p.tail ? n_b + tree_depth(seen, t) : n_b - 1;        // position of the query
@@ -195,59 +391,142 @@ __global__ void __launch_bounds__(256) mq_simt_kernel(const MqDecodeParams p) {
 
 // ---------------------------------------------------------------- merge and lift
 
-// One CTA per run of RB query rows of a unit: a row of (U^V)^T is read once for the RB rows.
-template <typename T, int RB>
-__global__ void __launch_bounds__(128) mq_combine_kernel(const MqDecodeParams p) {
-  __shared__ float os[RB][128];
-  const int runs = (p.rows + RB - 1) / RB;
-  const int unit = blockIdx.x / runs, r0 = (blockIdx.x - unit * runs) * RB, tid = threadIdx.x;
-  const int h = unit / p.B, b = unit - h * p.B;
-  const HeadInfo hd = p.heads[h];
-  const int nr = min(RB, p.rows - r0);
-  for (int r = 0; r < nr; ++r) {
-    const float* part = p.partials + (static_cast<int64_t>(unit) * p.rows + r0 + r) * p.splits * p.part_stride;
-    float M = -INFINITY;
-    for (int s = 0; s < p.splits; ++s) M = fmaxf(M, part[s * p.part_stride]);
+// o' of one query row, column c, from its pieces (0 for a row that sees nothing).
+__device__ __forceinline__ float merged(const MqDecodeParams& p, int unit, int row, int pieces, int c) {
+  const float* part = p.partials + (static_cast<int64_t>(unit) * p.rows + row) * p.splits * p.part_stride;
+  float M = part[0], L = part[1], acc = part[4 + c];
+  if (pieces > 1) {
+    for (int s = 1; s < pieces; ++s) M = fmaxf(M, part[s * p.part_stride]);
     const float base = M == -INFINITY ? 0.f : M;
-    float L = 0.f, acc = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
+    L = 0.f; acc = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < pieces; ++s) {
       const float* x = part + s * p.part_stride;
       const float f = ex2(x[0] - base);      // 0 for a piece without rows
       L = fmaf(x[1], f, L);
-      if (tid < hd.rp_v) acc = fmaf(x[4 + tid], f, acc);
+      acc = fmaf(x[4 + c], f, acc);
     }
-    // a query row that sees nothing returns zeros
-    os[r][tid] = tid < hd.rp_v ? (L == 0.f ? 0.f : acc / L) : 0.f;
   }
+  return L == 0.f ? 0.f : acc / L;
+}
+__device__ __forceinline__ int pieces_of(const MqDecodeParams& p, int b) {
+  if (p.list != nullptr || p.deficit == nullptr) return p.splits;
+  const int tiles = (p.n - __ldg(p.deficit + b) + p.tail + 127) >> 7;
+  return max(1, (tiles + p.per - 1) / p.per);
+}
+
+// Packed rank-r output.
+template <typename T>
+__global__ void __launch_bounds__(128) mq_combine_lowrank_kernel(const MqDecodeParams p) {
+  const int unit = blockIdx.x / p.rows, row = blockIdx.x - unit * p.rows, c = threadIdx.x;
+  const int h = unit / p.B, b = unit - h * p.B;
+  const HeadInfo hd = p.heads[h];
+  if (c >= hd.rp_v) return;
+  const int t = row / p.group, i = row - t * p.group;
+  static_cast<T*>(p.out)[(static_cast<int64_t>(b) * p.tokens + t) * p.group * p.lr_v_width + static_cast<int64_t>(p.group) * hd.lr_v_off +
+                         static_cast<int64_t>(i) * hd.rp_v + c] = from_f<T>(merged(p, unit, row, pieces_of(p, b), c));
+}
+
+template <typename T>
+__device__ __forceinline__ T* out_row(const MqDecodeParams& p, int h, int b, int row) {
+  const int t = row / p.group, i = row - t * p.group;
+  return static_cast<T*>(p.out) + b * p.out_stride_b + t * p.out_stride_t + (static_cast<int64_t>(h) * p.group + i) * p.d_head;
+}
+
+// Few rows: one CTA per query row, thread = output column and half of the rank.
+template <typename T>
+__global__ void __launch_bounds__(256) mq_combine_few_kernel(const MqDecodeParams p) {
+  __shared__ float os[128], ys[128];
+  const int unit = blockIdx.x / p.rows, row = blockIdx.x - unit * p.rows, tid = threadIdx.x;
+  const int h = unit / p.B, b = unit - h * p.B;
+  const HeadInfo hd = p.heads[h];
+  const int d = tid & 127, half = tid >> 7;
+  const int cut = hd.rp_v >> 1, c0 = half ? cut : 0, nc = half ? hd.rp_v - cut : cut;
+  // the basis is on its way while the pieces are merged
+  constexpr int kAhead = 32;
+  const float* Ut = p.basis + hd.uvt_off + c0 * p.d_head + d;
+  float u[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) u[j] = j < nc && d < p.d_head ? __ldg(Ut + j * p.d_head) : 0.f;
+  if (tid < hd.rp_v) os[tid] = merged(p, unit, row, pieces_of(p, b), tid);
   __syncthreads();
-  T* out = static_cast<T*>(p.out);
-  if (p.flags & 0x2u) {                      // EA_OUT_LOWRANK
-    for (int r = 0; r < nr; ++r) {
-      const int t = (r0 + r) / p.group, i = (r0 + r) - t * p.group;
-      T* dst = out + (static_cast<int64_t>(b) * p.tokens + t) * p.group * p.lr_v_width +
-               static_cast<int64_t>(p.group) * hd.lr_v_off + static_cast<int64_t>(i) * hd.rp_v;
-      if (tid < hd.rp_v) dst[tid] = from_f<T>(os[r][tid]);
+  float y = 0.f;
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j)
+    if (j < nc) y = fmaf(os[c0 + j], u[j], y);
+  if (d < p.d_head)
+    for (int j = kAhead; j < nc; ++j) y = fmaf(os[c0 + j], __ldg(Ut + j * p.d_head), y);
+  if (half) ys[d] = y;
+  __syncthreads();
+  if (!half && d < p.d_head) out_row<T>(p, h, b, row)[d] = from_f<T>(y + ys[d]);
+}
+
+// Many rows: 64 query rows of one head (of one sequence after the other) against (U^V)^T in shared memory, a thread 8 rows
+// x 4 columns as in the projection.
+template <typename T>
+__global__ void __launch_bounds__(256) mq_combine_many_kernel(const __grid_constant__ MqDecodeParams p) {
+  extern __shared__ __align__(16) float sm[];
+  const int h = blockIdx.y, tid = threadIdx.x;
+  const HeadInfo hd = p.heads[h];
+  float* ot = sm;                            // [rp_v][68]
+  float* us = sm + hd.rp_v * kPrPitch;       // [rp_v][d_head]
+  const int r0 = blockIdx.x * kPrRows, total = p.B * p.rows;
+  const float* Ut = p.basis + hd.uvt_off;
+  for (int i = tid; i < hd.rp_v * p.d_head / 4; i += 256) tc::cp_async16(us + 4 * i, Ut + 4 * i, 16);
+  tc::cp_async_commit();
+  const int warp = tid >> 5, lane = tid & 31;
+  for (int r = warp; r < kPrRows; r += 8) {  // a warp per row, lanes along its columns
+    const int g = r0 + r, b = g / p.rows, row = g - b * p.rows;
+    const int pieces = g < total ? pieces_of(p, b) : 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = lane + 32 * j;
+      if (c < hd.rp_v) ot[c * kPrPitch + r] = g < total ? merged(p, h * p.B + b, row, pieces, c) : 0.f;
     }
-    return;
   }
-  if (tid >= p.d_head) return;
-  const float* Ut = p.basis + hd.uvt_off + tid;
-  float y[RB];
+  tc::cp_async_wait<0>();
+  __syncthreads();
+  const int rg = tid & 7, cg = tid >> 3;
+  if (4 * cg >= p.d_head) return;
+  uint64_t acc[4][4];
 #pragma unroll
-  for (int r = 0; r < RB; ++r) y[r] = 0.f;
-#pragma unroll 8
-  for (int c = 0; c < hd.rp_v; ++c) {
-    const float u = __ldg(Ut + c * p.d_head);
+  for (int c = 0; c < 4; ++c)
 #pragma unroll
-    for (int r = 0; r < RB; ++r)
-      if (r < nr) y[r] = fmaf(os[r][c], u, y[r]);
-  }
+    for (int r = 0; r < 4; ++r) acc[c][r] = 0;
+  const float* xr = ot + 8 * rg;
+  const float* ur = us + 4 * cg;
+#pragma unroll 4
+  for (int k = 0; k < hd.rp_v; ++k) {
+    const ulonglong2 x0 = *reinterpret_cast<const ulonglong2*>(xr + k * kPrPitch);
+    const ulonglong2 x1 = *reinterpret_cast<const ulonglong2*>(xr + k * kPrPitch + 4);
+    const float4 u = *reinterpret_cast<const float4*>(ur + k * p.d_head);
+    const uint64_t uu[4] = {pack2(u.x, u.x), pack2(u.y, u.y), pack2(u.z, u.z), pack2(u.w, u.w)};
 #pragma unroll
-  for (int r = 0; r < RB; ++r)
-    if (r < nr) {
-      const int t = (r0 + r) / p.group, i = (r0 + r) - t * p.group;
-      out[b * p.out_stride_b + t * p.out_stride_t + (static_cast<int64_t>(h) * p.group + i) * p.d_head + tid] = from_f<T>(y[r]);
+    for (int c = 0; c < 4; ++c) {
+      ffma2(acc[c][0], x0.x, uu[c]);
+      ffma2(acc[c][1], x0.y, uu[c]);
+      ffma2(acc[c][2], x1.x, uu[c]);
+      ffma2(acc[c][3], x1.y, uu[c]);
     }
+  }
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const int g = r0 + 8 * rg + r;
+    if (g >= total) return;
+    T* dst = out_row<T>(p, h, g / p.rows, g % p.rows) + 4 * cg;
+    float y[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float2 v = unpack2(acc[c][r >> 1]);
+      y[c] = r & 1 ? v.y : v.x;
+    }
+    if (sizeof(T) == 2 && reinterpret_cast<uintptr_t>(dst) % 8 == 0) {
+      *reinterpret_cast<uint2*>(dst) = make_uint2(tc::pack_bf16(y[0], y[1]), tc::pack_bf16(y[2], y[3]));
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) dst[c] = from_f<T>(y[c]);
+    }
+  }
 }
 
 // ---------------------------------------------------------------- acceptance of a path
@@ -292,13 +571,37 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const __grid_constant_
 }  // namespace
 
 cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, uint64_t* launches) {
-  const dim3 grid(p.B * p.H, (p.rows + kQueryRows - 1) / kQueryRows);
-  if (dtype == 0) {
-    if (p.q64) mq_query_kernel<__nv_bfloat16, double><<<grid, 128, 0, s>>>(p);
-    else mq_query_kernel<__nv_bfloat16, float><<<grid, 128, 0, s>>>(p);
+  if (p.flags & 0x1u) {                      // EA_Q_PREPROJECTED
+    const dim3 grid(p.B * p.H, p.rows);
+    if (dtype == 0) mq_copy_query_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(p);
+    else mq_copy_query_kernel<float><<<grid, 128, 0, s>>>(p);
   } else {
-    if (p.q64) mq_query_kernel<float, double><<<grid, 128, 0, s>>>(p);
-    else mq_query_kernel<float, float><<<grid, 128, 0, s>>>(p);
+    if (dtype == 0) mq_query64_kernel<__nv_bfloat16><<<p.B * p.H, kQ64Threads, 0, s>>>(p);
+    else mq_query64_kernel<float><<<p.B * p.H, kQ64Threads, 0, s>>>(p);
+  }
+  ++*launches;
+  return cudaGetLastError();
+}
+
+cudaError_t launch_mq_project(const MqProjectParams& p, int dtype, int max_rp, cudaStream_t s, uint64_t* launches) {
+  const int rows_kv = p.B * p.tokens, rows_q = rows_kv * p.group;
+  const bool with_kv = p.k != nullptr;
+  // whole tiles of 64 rows where the rows fill most of them and there are enough tiles for the chip
+  const bool many = rows_kv >= 48;
+  const int rows = many ? kPrRows : kPfRows;
+  const int tiles = (p.with_q ? (rows_q + rows - 1) / rows : 0) + (with_kv ? 2 * ((rows_kv + rows - 1) / rows) : 0);
+  if (many) {
+    const size_t smem = sizeof(float) * p.d_head * (kPrPitch + max_rp);
+    static size_t configured[2][kMaxDevices] = {};
+    cudaError_t e = dtype == 0 ? ensure_dynamic_smem(mq_project_many_kernel<__nv_bfloat16>, smem, configured[0])
+                               : ensure_dynamic_smem(mq_project_many_kernel<float>, smem, configured[1]);
+    if (e != cudaSuccess) return e;
+    if (dtype == 0) mq_project_many_kernel<__nv_bfloat16><<<dim3(tiles, p.H), 256, smem, s>>>(p);
+    else mq_project_many_kernel<float><<<dim3(tiles, p.H), 256, smem, s>>>(p);
+  } else {
+    const dim3 grid(tiles, p.H, (max_rp + kPfCols - 1) / kPfCols);
+    if (dtype == 0) mq_project_few_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(p);
+    else mq_project_few_kernel<float><<<grid, 128, 0, s>>>(p);
   }
   ++*launches;
   return cudaGetLastError();
@@ -314,20 +617,26 @@ cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, u
   return cudaGetLastError();
 }
 
-cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches) {
-  const int64_t units = static_cast<int64_t>(p.B) * p.H;
-  const bool many = units * p.rows >= 2048;                   // enough rows to fill the chip eight at a time
-  const int rb = many ? 8 : 1;
-  const unsigned grid = static_cast<unsigned>(units * ((p.rows + rb - 1) / rb));
-  if (dtype == 0) {
-    if (many) mq_combine_kernel<__nv_bfloat16, 8><<<grid, 128, 0, s>>>(p);
-    else mq_combine_kernel<__nv_bfloat16, 1><<<grid, 128, 0, s>>>(p);
+template <typename T>
+static cudaError_t launch_combine_t(const MqDecodeParams& p, int max_rp_v, cudaStream_t s) {
+  const int64_t units = static_cast<int64_t>(p.B) * p.H, rows = units * p.rows;
+  if (p.flags & 0x2u) {                      // EA_OUT_LOWRANK
+    mq_combine_lowrank_kernel<T><<<static_cast<unsigned>(rows), 128, 0, s>>>(p);
+  } else if (p.B * p.rows >= 64 && rows >= 2048) {
+    const size_t smem = sizeof(float) * max_rp_v * (kPrPitch + p.d_head);
+    static size_t configured[kMaxDevices] = {};
+    const cudaError_t e = ensure_dynamic_smem(mq_combine_many_kernel<T>, smem, configured);
+    if (e != cudaSuccess) return e;
+    mq_combine_many_kernel<T><<<dim3((p.B * p.rows + kPrRows - 1) / kPrRows, p.H), 256, smem, s>>>(p);
   } else {
-    if (many) mq_combine_kernel<float, 8><<<grid, 128, 0, s>>>(p);
-    else mq_combine_kernel<float, 1><<<grid, 128, 0, s>>>(p);
+    mq_combine_few_kernel<T><<<static_cast<unsigned>(rows), 256, 0, s>>>(p);
   }
-  ++*launches;
   return cudaGetLastError();
+}
+
+cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, int max_rp_v, cudaStream_t s, uint64_t* launches) {
+  ++*launches;
+  return dtype == 0 ? launch_combine_t<__nv_bfloat16>(p, max_rp_v, s) : launch_combine_t<float>(p, max_rp_v, s);
 }
 
 cudaError_t launch_tree_commit(const TreeCommitParams& p, int sequences, cudaStream_t s, uint64_t* launches) {

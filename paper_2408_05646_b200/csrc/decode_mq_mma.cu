@@ -109,8 +109,8 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
   const int64_t end = p.list ? static_cast<int64_t>(p.list_len) << p.block_shift : static_cast<int64_t>(n_b) + p.tail;
   const int nt = static_cast<int>((end + 127) >> 7);
-  const int per = (p.tiles + p.splits - 1) / p.splits;
-  const int t_lo = min(nt, split * per), t_hi = min(nt, t_lo + per);
+  const int t_lo = split * p.per, t_hi = min(nt, t_lo + p.per);
+  if (split > 0 && t_lo >= nt) return;       // a shorter sequence: nothing left (its first piece always reports)
   const int32_t* list = p.list ? p.list + static_cast<int64_t>(unit) * p.list_len : nullptr;
   const char* k_slab = p.cache + hd.k_off;
   const char* v_slab = p.cache + hd.v_off;

@@ -300,13 +300,31 @@ struct MqDecodeParams {
   int32_t tail;             // drafted rows behind every sequence (0 or tokens)
   int32_t q_stride, part_stride;
   int32_t tiles;            // tiles of 128 rows of the longest unit
-  int32_t splits;           // CTAs per (unit, chunk of query rows)
+  int32_t per;              // tiles of a piece
+  int32_t splits;           // pieces of the longest unit = ceil(tiles / per)
   int32_t lr_v_width;       // sum of rp_v: width of a packed output row of one query head
   uint32_t flags;
   PageMap pages;
 };
 
-struct MqQueryParams {       // Q' of every query row into the scratch, scaled into the base-2 domain
+struct MqProjectParams {     // drafted tokens: Q' into the scratch (scaled into the base-2 domain), K', V' rows into the cache
+  const HeadInfo* heads;
+  const float* basis;
+  const void* q;            // [B][tokens][H * group][d_head]
+  const void* k;            // [B][tokens][H][d_head]; NULL: queries only
+  const void* v;
+  int64_t q_stride_b, q_stride_t, kv_stride_b, kv_stride_t;
+  float* qp;                // [unit][tokens * group][q_stride]
+  char* cache;
+  const int32_t* deficit;
+  PageMap pages;
+  int32_t B, H, d_head, group, tokens, q_stride, n_max, row0;
+  int32_t with_q;           // 0: keys and values only
+  int32_t aligned;          // every row starts on a 16-byte boundary
+  float q_scale;            // log2(e)/sqrt(d_head)
+};
+
+struct MqQueryParams {       // Q' of every query row into the scratch: rank-space rows copied, or one token's in 64 bits
   const HeadInfo* heads;
   const float* basis;
   const void* q;            // [B][tokens][H * group][d_head], or packed [B][tokens][group * sum rp_k]
@@ -361,12 +379,13 @@ __device__ __forceinline__ int64_t physical_block(const SparseParams& p, int b, 
 
 // Launchers (each returns the CUDA error of its launch); `launches` is incremented per kernel.
 cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_mq_project(const MqProjectParams& p, int dtype, int max_rp, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 struct MqShape { int queries, ctas_per_sm; };   // query rows of a CTA, resident CTAs
 MqShape mq_mma_shape(int rows, int max_rp);
 // 16-bit layers; max_rp / min_rp: widest and narrowest padded rank over heads and K/V
 cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, int min_rp, cudaStream_t s, uint64_t* launches);
-cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, int max_rp_v, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_tree_commit(const TreeCommitParams& p, int sequences, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_block_bounds(const SparseParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_block_scores(const SparseParams& p, int dtype, int max_rp_k, cudaStream_t s, uint64_t* launches);
