@@ -5,6 +5,7 @@ streams.  There is no fallback: if the library is missing, importing this module
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import List, Optional, Sequence
@@ -122,6 +123,9 @@ def device_alloc(nbytes: int, device: torch.device) -> torch.Tensor:
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+_default_alloc = device_alloc
+
+
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     if stream is None:
         stream = torch.cuda.current_stream()
@@ -130,11 +134,13 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
 
 def _call_on(device: torch.device, stream: Optional[torch.cuda.Stream], fn, *args) -> int:
     """fn(*args, stream pointer) with `device` current: its current stream, or the one given."""
-    index = device.index if device.index is not None else torch.cuda.current_device()
-    if torch.cuda.current_device() == index:
-        return fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream)
+    current = torch.cuda.current_device()
+    index = current if device.index is None else device.index
+    ptr = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if current == index:
+        return fn(*args, ptr)
     with torch.cuda.device(index):
-        return fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream)
+        return fn(*args, ptr)
 
 
 def _make_desc(batch, n_heads, d_head, n_max, dtype, r_k, r_v, U_k, U_v, max_prefill_tokens, flags):
@@ -210,6 +216,8 @@ class EigenAttnLayer:
 
     # -- plumbing
     def _new_out(self, *shape) -> torch.Tensor:
+        if device_alloc is _default_alloc:
+            return torch.empty(shape, dtype=self.torch_dtype, device=self.device)
         es = 2 if self.torch_dtype == torch.bfloat16 else 4
         n = 1
         for d in shape:
@@ -534,14 +542,16 @@ class EigenAttnLayer:
     def tree_commit(self, paths, T: int, stream=None) -> None:
         """eigen_attn_tree_commit: paths[b] = accepted tokens of sequence b, ascending (empty: none); T as in decode_tree."""
         assert len(paths) == self.B
-        flat, counts = [], []
+        counts = array.array("i", map(len, paths))
+        assert max(counts) <= T
+        flat = array.array("i", bytes(4 * self.B * T))
+        at = 0
         for path in paths:
-            assert len(path) <= T
-            counts.append(len(path))
-            flat += path
-            flat += [0] * (T - len(path))
-        arr = (ctypes.c_int32 * (self.B * T))(*flat)
-        self._check(_call_on(self.device, stream, lib.eigen_attn_tree_commit, self.handle, arr, (ctypes.c_int32 * self.B)(*counts), T),
+            if path:
+                flat[at:at + len(path)] = array.array("i", path)
+            at += T
+        self._check(_call_on(self.device, stream, lib.eigen_attn_tree_commit, self.handle,
+                             (ctypes.c_int32 * len(flat)).from_buffer(flat), (ctypes.c_int32 * self.B).from_buffer(counts), T),
                     "eigen_attn_tree_commit")
 
     # -- decode over a selection of blocks
@@ -612,7 +622,11 @@ class EigenAttnLayer:
             po, sbo, _ = self._mq_tok(out, 1, self.H * group)
         index = None
         if return_index:
-            index = device_alloc(4 * self.B * self.H * int(n_blocks), self.device).view(torch.int32).view(self.B, self.H, int(n_blocks))
+            shape = (self.B, self.H, max(1, int(n_blocks)))          # (the call refuses less than one block)
+            if device_alloc is _default_alloc:
+                index = torch.empty(shape, dtype=torch.int32, device=self.device)
+            else:
+                index = device_alloc(4 * shape[0] * shape[1] * shape[2], self.device).view(torch.int32).view(shape)
         self._check(_call_on(self.device, stream, lib.eigen_attn_decode_sparse, self.handle, pq, sbq, group, n_blocks, sink, recent,
                              po, sbo, None if index is None else index.data_ptr(), flags), "eigen_attn_decode_sparse")
         return (out, index) if return_index else out

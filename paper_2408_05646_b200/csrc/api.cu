@@ -1362,7 +1362,8 @@ ea_status check_mq(eigen_attn_t h, const char* who, int32_t group) {
 
 // The launches behind the query projection: attention over p's rows, then the merge of its pieces with the lift.
 // `slots`: partials the scratch holds.
-ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size_t slots, cudaStream_t s) {
+// `end`: rows (places of the list) of the longest unit.
+ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int64_t end, size_t slots, cudaStream_t s) {
   const Layout& L = h->L;
   p.heads = dev_heads(h); p.basis = dev_basis(h); p.cache = h->cache;
   p.deficit = dev_deficit(h); p.pages = dev_pages(h);
@@ -1374,7 +1375,10 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size
   // one size, so a shorter sequence of the batch has fewer of them; the partials must have room.
   const bool mma = h->desc.dtype == EA_BF16;
   const int max_rp = L.max_rp_k > L.max_rp_v ? L.max_rp_k : L.max_rp_v;
-  const ea::MqShape shape = mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::MqShape{8, 2};
+  const ea::MqShape shape = mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::kMqSimtShape;
+  const int tile = 1 << shape.tile_shift;
+  p.tile_shift = shape.tile_shift;
+  p.tiles = static_cast<int32_t>((end + tile - 1) >> shape.tile_shift);
   const int64_t chunks = static_cast<int64_t>(p.H) * ((p.rows + shape.queries - 1) / shape.queries);   // of one sequence
   int64_t cap = static_cast<int64_t>(slots) / (static_cast<int64_t>(p.B) * p.H * p.rows);
   if (cap > p.tiles) cap = p.tiles;
@@ -1394,7 +1398,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size
       int64_t pieces = 0;
       if (h->max_deficit > 0 && p.list == nullptr) {
         for (int b = 0; b < p.B; ++b) {
-          const int64_t t = (p.n - h->deficit[b] + p.tail + 127) / 128;
+          const int64_t t = (p.n - h->deficit[b] + p.tail + tile - 1) >> shape.tile_shift;
           pieces += t > size ? (t + size - 1) / size : 1;
         }
       } else {
@@ -1407,12 +1411,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, size
   p.per = static_cast<int32_t>(per);
   p.splits = static_cast<int32_t>((p.tiles + per - 1) / per);
   if (h->ev_start) cudaEventRecord(h->ev_start, s);
-  int min_rp = max_rp;
-  for (const HeadInfo& hi : L.heads) {
-    if (hi.rp_k < min_rp) min_rp = hi.rp_k;
-    if (hi.rp_v < min_rp) min_rp = hi.rp_v;
-  }
-  cudaError_t e = mma ? ea::launch_mq_mma(p, max_rp, min_rp, s, &h->launches)
+  cudaError_t e = mma ? ea::launch_mq_mma(p, max_rp, s, &h->launches)
                       : ea::launch_mq_simt(p, h->desc.dtype, s, &h->launches);
   if (h->ev_stop) cudaEventRecord(h->ev_stop, s);
   if (e == cudaSuccess) e = ea::launch_mq_combine(p, h->desc.dtype, L.max_rp_v, s, &h->launches);
@@ -1517,9 +1516,8 @@ ea_status eigen_attn_decode_tree(eigen_attn_t h, const void* d_q, int64_t stride
   p.out = d_out; p.out_stride_b = stride_b_out; p.out_stride_t = stride_t_out;
   p.mask = d_mask;
   p.group = group; p.tokens = T; p.tail = T;
-  p.tiles = (h->len + T + 127) / 128;
   p.flags = flags & EA_OUT_LOWRANK;
-  return launch_mq(h, "decode_tree launch", p, h->tree_slots, s);
+  return launch_mq(h, "decode_tree launch", p, static_cast<int64_t>(h->len) + T, h->tree_slots, s);
 }
 
 ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const int32_t* h_counts, int32_t T, void* cuda_stream) {
@@ -1714,9 +1712,8 @@ ea_status eigen_attn_decode_sparse(eigen_attn_t h, const void* d_q, int64_t stri
   p.out = d_out; p.out_stride_b = stride_b_out;
   p.list = sp.list; p.list_len = sp.list_len; p.block_shift = h->sp_shift;
   p.group = group; p.tokens = 1; p.tail = 0;
-  p.tiles = static_cast<int32_t>(((static_cast<int64_t>(sp.list_len) << h->sp_shift) + 127) / 128);
   p.flags = flags & EA_OUT_LOWRANK;
-  return launch_mq(h, "decode_sparse launch", p, h->sp.slots, s);
+  return launch_mq(h, "decode_sparse launch", p, static_cast<int64_t>(sp.list_len) << h->sp_shift, h->sp.slots, s);
 }
 
 ea_status eigen_attn_set_rope(eigen_attn_t h, double base, int32_t interleaved, void* cuda_stream) {

@@ -56,40 +56,36 @@ __global__ void __launch_bounds__(256) block_bounds_kernel(const SparseParams p)
   dst[nc] = hi;
 }
 
-// A 16-bit number as a double, times 2^-896: its exponent and mantissa bits moved into place (zero and subnormal numbers
-// come out right too).  The factor is taken out of the query.
-__device__ __forceinline__ double tiny_double(uint32_t bits16) {
-  return __hiloint2double(static_cast<int>(((bits16 & 0x8000u) << 16) | ((bits16 & 0x7fffu) << 13)), 0);
-}
+// The two 16-bit numbers of a word as doubles, times 2^-896: exponent and mantissa bits moved into place (zeros and
+// subnormal numbers come out right too).  The factor is taken out of the query.
+__device__ __forceinline__ double tiny_high(uint32_t w) { return __hiloint2double((static_cast<int>(w) >> 3) & 0x8fffe000, 0); }
+__device__ __forceinline__ double tiny_low(uint32_t w) { return __hiloint2double((static_cast<int>(w << 16) >> 3) & 0x8fffffff, 0); }
 
 // 16 bytes of lo and hi (eight 16-bit channels, or four of 32 bits) against the same channels of GQ queries: a channel
-// contributes q hi where q > 0 and q lo where q < 0.
+// contributes q hi where q > 0 and q lo where q < 0.  Even and odd channels have sums of their own.
+__device__ __forceinline__ bool negative(double x) { return __double2hiint(x) < 0; }
 template <int GQ>
-__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, int q_stride, double (&acc)[GQ], __nv_bfloat16) {
+__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, int q_stride, double (&acc)[2 * GQ], __nv_bfloat16) {
   const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t lb = i & 1 ? l[i >> 1] >> 16 : l[i >> 1] & 0xffffu, ub = i & 1 ? u[i >> 1] >> 16 : u[i >> 1] & 0xffffu;
-    const double dl = tiny_double(lb), du = tiny_double(ub);
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
-      const double x = q[g * q_stride + i];
-      acc[g] = fma(x, x < 0 ? dl : du, acc[g]);
+      const double2 x = *reinterpret_cast<const double2*>(q + g * q_stride + 2 * i);
+      acc[2 * g] = fma(x.x, tiny_low(negative(x.x) ? l[i] : u[i]), acc[2 * g]);
+      acc[2 * g + 1] = fma(x.y, tiny_high(negative(x.y) ? l[i] : u[i]), acc[2 * g + 1]);
     }
-  }
 }
 template <int GQ>
-__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, int q_stride, double (&acc)[GQ], float) {
+__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, int q_stride, double (&acc)[2 * GQ], float) {
   const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const double dl = __uint_as_float(l[i]), du = __uint_as_float(u[i]);
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
       const double x = q[g * q_stride + i];
-      acc[g] = fma(x, x < 0 ? dl : du, acc[g]);
+      acc[2 * g + (i & 1)] = fma(x, static_cast<double>(__uint_as_float(negative(x) ? l[i] : u[i])), acc[2 * g + (i & 1)]);
     }
-  }
 }
 template <typename T> __device__ __forceinline__ double query_factor();
 template <> __device__ __forceinline__ double query_factor<__nv_bfloat16>() { return __hiloint2double((1023 + 896) << 20, 0); }   // 2^896
@@ -135,14 +131,16 @@ __global__ void __launch_bounds__(kScoreBlocks) block_scores_kernel(const Sparse
   const uint4* lo = reinterpret_cast<const uint4*>(bounds + tid * pitch);
   double best = 0;
   for (int g0 = 0; g0 < p.group; g0 += GQ) {
-    double acc[GQ];
+    double acc[2 * GQ];                      // even and odd channels
 #pragma unroll
-    for (int g = 0; g < GQ; ++g) acc[g] = 0;
+    for (int g = 0; g < 2 * GQ; ++g) acc[g] = 0;
 #pragma unroll 2
     for (int c = 0; c < nc; ++c) add_bounds<GQ>(lo[c], lo[nc + c], qs + g0 * hd.rp_k + c * kPer, hd.rp_k, acc, T());
 #pragma unroll
-    for (int g = 0; g < GQ; ++g)
-      if (g0 + g < p.group && (g0 + g == 0 || acc[g] > best)) best = acc[g];
+    for (int g = 0; g < GQ; ++g) {
+      const double s = acc[2 * g] + acc[2 * g + 1];
+      if (g0 + g < p.group && (g0 + g == 0 || s > best)) best = s;
+    }
   }
   // the position bias of the block's last row, the one it takes least from
   if (hd.alibi_slope != 0.f)
@@ -156,13 +154,16 @@ __device__ __forceinline__ uint64_t order_key(double x) {
   return b >> 63 ? ~b : b | (1ull << 63);
 }
 
-// One CTA per unit: the k-th highest key by counting digits of 11 bits from the top, then one ordered pass that writes
-// the chosen blocks in ascending order (sorted lists read the cache front to back, and equal scores go to the lower block).
-constexpr int kSelThreads = 256, kDigit = 11, kBins = 1 << kDigit;
+// One CTA per unit: the k-th highest key by counting digits of 11 bits, then one ordered pass that writes the chosen
+// blocks in ascending order (sorted lists read the cache front to back, and equal scores go to the lower block).  Keys are
+// taken relative to the lowest one and digits start at the highest bit of the range: scores share their leading bits, and
+// counting those would send every key to one counter.
+constexpr int kSelThreads = 256, kDigit = 11, kBins = 1 << kDigit, kKeep = 4;
 __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseParams p) {
   __shared__ int hist[kBins];
   __shared__ int warp_sum[8], warp_sum2[8];
   __shared__ int s_digit, s_above, s_count;
+  __shared__ uint64_t s_low[kSelThreads / 32], s_high[kSelThreads / 32];
   const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
@@ -185,17 +186,57 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseP
   if (want == 0) return;
   const double* scores = p.scores + static_cast<int64_t>(unit) * p.score_stride;
 
+  // the first kKeep keys of a thread stay in its registers, the rest (long sequences of short blocks) are read again
+  uint64_t keep[kKeep];
+#pragma unroll
+  for (int j = 0; j < kKeep; ++j) {
+    const int i = first + j * kSelThreads + tid;
+    keep[j] = i < last ? order_key(scores[i]) : 0;
+  }
+  auto key = [&](int j) { return order_key(scores[first + j * kSelThreads + tid]); };
+  const int mine_n = (last - first - tid + kSelThreads - 1) / kSelThreads;        // keys of this thread
+  uint64_t lowest = ~0ull, highest = 0;
+  auto extend = [&](uint64_t k) {
+    lowest = k < lowest ? k : lowest;
+    highest = k > highest ? k : highest;
+  };
+#pragma unroll
+  for (int j = 0; j < kKeep; ++j)
+    if (j < mine_n) extend(keep[j]);
+  for (int j = kKeep; j < mine_n; ++j) extend(key(j));
+#pragma unroll
+  for (int d = 16; d; d >>= 1) {
+    const uint64_t a = __shfl_xor_sync(kFull, lowest, d), c = __shfl_xor_sync(kFull, highest, d);
+    lowest = a < lowest ? a : lowest;
+    highest = c > highest ? c : highest;
+  }
+  if (lane == 0) { s_low[warp] = lowest; s_high[warp] = highest; }
+  for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSelThreads / 32; ++w) {
+    lowest = s_low[w] < lowest ? s_low[w] : lowest;
+    highest = s_high[w] > highest ? s_high[w] : highest;
+  }
   uint64_t prefix = 0;       // the digits found so far; keys above it (compared on their top bits) are chosen
-  int shift = 64, need = want;
+  int shift = 64 - __clzll(static_cast<long long>((highest - lowest) | 1)), need = want;   // no key has a bit from here on
+  bool again = false;
   while (shift > 0) {
     const int bits = shift >= kDigit ? kDigit : shift;
     const int next = shift - bits;
-    for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = first + tid; i < last; i += kSelThreads) {
-      const uint64_t k = order_key(scores[i]);
-      if (shift == 64 || (k >> shift) == prefix) atomicAdd(&hist[(k >> next) & ((1 << bits) - 1)], 1);
+    if (again) {
+      for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+      __syncthreads();
     }
+    again = true;
+    auto count = [&](uint64_t absolute) {
+      const uint64_t k = absolute - lowest;
+      if (shift >= 64 || (k >> shift) == prefix) atomicAdd(&hist[(k >> next) & ((1 << bits) - 1)], 1);
+    };
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j)
+      if (j < mine_n) count(keep[j]);
+    for (int j = kKeep; j < mine_n; ++j) count(key(j));
     __syncthreads();
     // counts from the highest digit down: thread i holds the bins 2047 - 8i .. 2040 - 8i
     int mine[8], sum = 0;
@@ -221,7 +262,7 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseP
       above += mine[j];
     }
     __syncthreads();
-    prefix = (shift == 64 ? 0 : prefix << bits) | static_cast<uint64_t>(s_digit);
+    prefix = prefix << bits | static_cast<uint64_t>(s_digit);
     need -= s_above;
     shift = next;
     if (s_count == need) break;              // every key of this digit is chosen
@@ -229,10 +270,8 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseP
   }
   // keys with (key >> shift) above the prefix are in; of those equal to it the first `need`
   int done = 0, ties = 0;
-  for (int i0 = first; i0 < last; i0 += kSelThreads) {
-    __syncthreads();
-    const int i = i0 + tid;
-    const uint64_t k = i < last ? order_key(scores[i]) >> shift : 0;
+  auto emit = [&](int i, uint64_t absolute) {
+    const uint64_t k = (absolute - lowest) >> shift;
     const bool eq = i < last && k == prefix, gt = i < last && k > prefix;
     const unsigned beq = __ballot_sync(kFull, eq), bgt = __ballot_sync(kFull, gt);
     if (lane == 0) { warp_sum[warp] = __popc(beq); warp_sum2[warp] = __popc(bgt); }
@@ -250,7 +289,14 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseP
     if (gt || (eq && my_e < need)) put(p.sink + done + g0 + __popc(bgt & below) + taken_e, i);
     done += g_all + min(ties + e_all, need) - min(ties, need);
     ties += e_all;
-  }
+    __syncthreads();
+  };
+  __syncthreads();
+  const int rounds = (last - first + kSelThreads - 1) / kSelThreads;
+#pragma unroll
+  for (int j = 0; j < kKeep; ++j)
+    if (j < rounds) emit(first + j * kSelThreads + tid, keep[j]);
+  for (int j = kKeep; j < rounds; ++j) emit(first + j * kSelThreads + tid, j < mine_n ? key(j) : 0);
 }
 
 }  // namespace

@@ -70,35 +70,84 @@ __device__ __forceinline__ const T* row_source(const MqProjectParams& p, const R
   const int b = row / p.tokens, t = row - b * p.tokens;
   return static_cast<const T*>(w.kind == 1 ? p.k : p.v) + b * p.kv_stride_b + t * p.kv_stride_t + static_cast<int64_t>(w.h) * p.d_head;
 }
-// Columns c..c+N-1 of a projected row: scaled into the scratch (queries) or rounded into the cache.
-template <typename T, int N>
-__device__ __forceinline__ void store_row(const MqProjectParams& p, const Rows& w, int row, int c, const float (&x)[N]) {
+// Where a projected row goes (its first column): the scratch for queries, the cache for keys and values.
+template <typename T>
+__device__ __forceinline__ char* row_target(const MqProjectParams& p, const Rows& w, int row) {
   if (w.kind == 0) {
     const int bt = row / p.group, i = row - bt * p.group, b = bt / p.tokens, t = bt - b * p.tokens;
-    float* dst = p.qp + ((static_cast<int64_t>(w.h) * p.B + b) * p.tokens * p.group + t * p.group + i) * p.q_stride + c;
-#pragma unroll
-    for (int j = 0; j < N; j += 2) *reinterpret_cast<float2*>(dst + j) = make_float2(x[j] * p.q_scale, x[j + 1] * p.q_scale);
-    return;
+    return reinterpret_cast<char*>(p.qp + ((static_cast<int64_t>(w.h) * p.B + b) * p.tokens * p.group + t * p.group + i) * p.q_stride);
   }
   const int b = row / p.tokens, t = row - b * p.tokens;
   const HeadInfo& hd = p.heads[w.h];
   const int64_t crow = physical_row(p.pages, b, p.n_max, p.row0 - (p.deficit ? __ldg(p.deficit + b) : 0) + t);
-  T* dst = reinterpret_cast<T*>(p.cache + (w.kind == 1 ? hd.k_off : hd.v_off)) + crow * w.rp + c;
+  return p.cache + (w.kind == 1 ? hd.k_off : hd.v_off) + crow * w.rp * static_cast<int64_t>(sizeof(T));
+}
+// Columns c..c+N-1: scaled into the scratch, or rounded into the cache.
+template <typename T, int N>
+__device__ __forceinline__ void store_row(const MqProjectParams& p, const Rows& w, char* row, int c, const float (&x)[N]) {
+  if (w.kind == 0 || sizeof(T) == 4) {
+    const float f = w.kind == 0 ? p.q_scale : 1.f;
+    float* dst = reinterpret_cast<float*>(row) + c;
 #pragma unroll
-  for (int j = 0; j < N; j += 2) {
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(dst + j) = tc::pack_bf16(x[j], x[j + 1]);
-    else *reinterpret_cast<float2*>(dst + j) = make_float2(x[j], x[j + 1]);
+    for (int j = 0; j < N; j += 2) *reinterpret_cast<float2*>(dst + j) = make_float2(x[j] * f, x[j + 1] * f);
+  } else {
+    uint32_t* dst = reinterpret_cast<uint32_t*>(row) + c / 2;
+#pragma unroll
+    for (int j = 0; j < N; j += 2) dst[j / 2] = tc::pack_bf16(x[j], x[j + 1]);
   }
 }
 
 // Every output is one chain of fused multiply-adds over d_head in ascending order, as in the append kernel: a drafted row
 // that is accepted is bit for bit the row that appending its token would have stored.
 //
-// Many rows: a CTA takes 64 rows of one head and kind, a thread 8 rows x 4 columns (rows in packed pairs), both operands
-// in shared memory.  Per step of d: three 16-byte loads and 16 packed multiply-adds, so the arithmetic is what bounds it.
-constexpr int kPrRows = 64, kPrPitch = kPrRows + 4;
+// Many rows: 64 rows of one head and kind against its basis, both in shared memory.  A lane has two rows, a warp a quarter
+// of the columns: the columns' numbers are the same for all lanes, so a 16-byte load feeds eight multiply-adds of every
+// lane, and what bounds the loop is the fp32 pipe.  (Register tiles of 8 x 4 and 8 x 8 with both operands spread over the
+// lanes were bound by their shared-memory reads, packed multiply-adds by the moves that duplicate an operand.)
+constexpr int kPrRows = 64, kPrPitch = kPrRows, kPrThreads = 128, kPrPad = 64;
+
+// acc[r][c]: row 2 lane + r, column c0 + c.  a: [k][64], b: [k][width] with kPrPad floats to spare behind it (the last
+// columns of the last warp can lie past the width; they are not stored).
+template <int C>
+struct RegTile {
+  float acc[2][C];
+  int lane, c0;
+  __device__ __forceinline__ RegTile(int tid) : lane(tid & 31), c0((tid >> 5) * C) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[0][c] = acc[1][c] = 0.f;
+  }
+  __device__ __forceinline__ void multiply(const float* a, const float* b, int k_count, int width) {
+    const float* ar = a + 2 * lane;
+    const float* br = b + c0;
+    if (c0 >= width) return;
+#pragma unroll 4
+    for (int k = 0; k < k_count; ++k) {
+      const float2 x = *reinterpret_cast<const float2*>(ar + k * kPrPitch);
+#pragma unroll
+      for (int c = 0; c < C; c += 4) {
+        const float4 u = *reinterpret_cast<const float4*>(br + c);
+        acc[0][c] = fmaf(x.x, u.x, acc[0][c]);         acc[1][c] = fmaf(x.y, u.x, acc[1][c]);
+        acc[0][c + 1] = fmaf(x.x, u.y, acc[0][c + 1]); acc[1][c + 1] = fmaf(x.y, u.y, acc[1][c + 1]);
+        acc[0][c + 2] = fmaf(x.x, u.z, acc[0][c + 2]); acc[1][c + 2] = fmaf(x.y, u.z, acc[1][c + 2]);
+        acc[0][c + 3] = fmaf(x.x, u.w, acc[0][c + 3]); acc[1][c + 3] = fmaf(x.y, u.w, acc[1][c + 3]);
+      }
+      br += width;
+    }
+  }
+};
+// Four values of a row at a time, as T or (wide) as fp32.
 template <typename T>
-__global__ void __launch_bounds__(256) mq_project_many_kernel(const __grid_constant__ MqProjectParams p) {
+__device__ __forceinline__ void put4(T* dst, float a, float b, float c, float d, bool whole) {
+  if (whole) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(tc::pack_bf16(a, b), tc::pack_bf16(c, d));
+    else *reinterpret_cast<float4*>(dst) = make_float4(a, b, c, d);
+  } else {
+    dst[0] = from_f<T>(a); dst[1] = from_f<T>(b); dst[2] = from_f<T>(c); dst[3] = from_f<T>(d);
+  }
+}
+
+template <typename T, int C>
+__global__ void __launch_bounds__(kPrThreads) mq_project_many_kernel(const __grid_constant__ MqProjectParams p) {
   extern __shared__ __align__(16) float sm[];
   const int tiles_q = (p.B * p.tokens * p.group + kPrRows - 1) / kPrRows, tiles_kv = (p.B * p.tokens + kPrRows - 1) / kPrRows;
   const int nq = p.with_q ? tiles_q : 0;
@@ -106,66 +155,51 @@ __global__ void __launch_bounds__(256) mq_project_many_kernel(const __grid_const
   const int kind = tile < nq ? 0 : tile - nq < tiles_kv ? 1 : 2;
   tile -= kind == 0 ? 0 : kind == 1 ? nq : nq + tiles_kv;
   const Rows w = rows_of(p, kind, blockIdx.y);
-  float* xt = sm;                            // [d_head][68]: the rows, transposed
+  float* xt = sm;                            // [d_head][64]: the rows, transposed
   float* us = sm + p.d_head * kPrPitch;      // [d_head][rp]
   const int tid = threadIdx.x, r0 = tile * kPrRows;
-  for (int i = tid; i < p.d_head * w.rp / 4; i += 256) tc::cp_async16(us + 4 * i, w.U + 4 * i, 16);
+  __shared__ char* target[kPrRows];
+  for (int i = tid; i < p.d_head * w.rp / 4; i += kPrThreads) tc::cp_async16(us + 4 * i, w.U + 4 * i, 16);
   tc::cp_async_commit();
-  constexpr int kVec = 16 / sizeof(T);
-  const int pieces = p.d_head / kVec;
-  for (int i = tid; i < kPrRows * pieces; i += 256) {
-    const int r = i % kPrRows, d = i / kPrRows * kVec;
-    float x[kVec];
-    if (r0 + r < w.count) {
-      const T* src = row_source<T>(p, w, r0 + r) + d;
-      if (p.aligned) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(src));
+  {
+    constexpr int kVec = 16 / sizeof(T);
+    const int r = tid & (kPrRows - 1);       // two threads share a row
+    const T* src = r0 + r < w.count ? row_source<T>(p, w, r0 + r) : nullptr;
+    if (tid >= kPrRows) target[r] = src ? row_target<T>(p, w, r0 + r) : nullptr;
+#pragma unroll 4
+    for (int d = (tid / kPrRows) * kVec; d < p.d_head; d += 2 * kVec) {
+      float x[kVec];
+      if (src == nullptr) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) x[j] = 0.f;
+      } else if (p.aligned) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(src + d));
         const T* e = reinterpret_cast<const T*>(&v);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) x[j] = to_f<T>(e[j]);
       } else {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) x[j] = to_f<T>(src[j]);
+        for (int j = 0; j < kVec; ++j) x[j] = to_f<T>(src[d + j]);
       }
-    } else {
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) x[j] = 0.f;
+      for (int j = 0; j < kVec; ++j) xt[(d + j) * kPrPitch + r] = x[j];
     }
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) xt[(d + j) * kPrPitch + r] = x[j];
   }
   tc::cp_async_wait<0>();
   __syncthreads();
-  const int rg = tid & 7, cg = tid >> 3;     // 8 rows from 8 rg, 4 columns from 4 cg
-  if (4 * cg >= w.rp) return;
-  uint64_t acc[4][4];                        // [column][pair of rows]
+  RegTile<C> t(tid);
+  t.multiply(xt, us, p.d_head, w.rp);
+  const float f = w.kind == 0 ? p.q_scale : 1.f;
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
+  for (int i = 0; i < 2; ++i) {
+    char* row = target[2 * t.lane + i];
+    if (row == nullptr) continue;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[c][r] = 0;
-  const float* xr = xt + 8 * rg;
-  const float* ur = us + 4 * cg;
-#pragma unroll 4
-  for (int d = 0; d < p.d_head; ++d) {
-    const ulonglong2 x0 = *reinterpret_cast<const ulonglong2*>(xr + d * kPrPitch);
-    const ulonglong2 x1 = *reinterpret_cast<const ulonglong2*>(xr + d * kPrPitch + 4);
-    const float4 u = *reinterpret_cast<const float4*>(ur + d * w.rp);
-    const uint64_t uu[4] = {pack2(u.x, u.x), pack2(u.y, u.y), pack2(u.z, u.z), pack2(u.w, u.w)};
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      ffma2(acc[c][0], x0.x, uu[c]);
-      ffma2(acc[c][1], x0.y, uu[c]);
-      ffma2(acc[c][2], x1.x, uu[c]);
-      ffma2(acc[c][3], x1.y, uu[c]);
+    for (int c = 0; c < C; c += 4) {
+      if (t.c0 + c >= w.rp) break;           // (whole pieces: the rank is a multiple of 8)
+      if (w.kind == 0) put4(reinterpret_cast<float*>(row) + t.c0 + c, t.acc[i][c] * f, t.acc[i][c + 1] * f, t.acc[i][c + 2] * f, t.acc[i][c + 3] * f, true);
+      else put4(reinterpret_cast<T*>(row) + t.c0 + c, t.acc[i][c], t.acc[i][c + 1], t.acc[i][c + 2], t.acc[i][c + 3], true);
     }
-  }
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const float2 v[4] = {unpack2(acc[0][r]), unpack2(acc[1][r]), unpack2(acc[2][r]), unpack2(acc[3][r])};
-    const int row = r0 + 8 * rg + 2 * r;
-    const float even[4] = {v[0].x, v[1].x, v[2].x, v[3].x}, odd[4] = {v[0].y, v[1].y, v[2].y, v[3].y};
-    if (row < w.count) store_row<T, 4>(p, w, row, 4 * cg, even);
-    if (row + 1 < w.count) store_row<T, 4>(p, w, row + 1, 4 * cg, odd);
   }
 }
 
@@ -205,7 +239,7 @@ __global__ void __launch_bounds__(128) mq_project_few_kernel(const __grid_consta
     ffma2(acc, pack2(xs[r][d], xs[r][d]), *reinterpret_cast<const uint64_t*>(us + d * kPfCols + c));
   const float2 v = unpack2(acc);
   const float x[2] = {v.x, v.y};
-  store_row<T, 2>(p, w, r0 + r, c0 + c, x);
+  store_row<T, 2>(p, w, row_target<T>(p, w, r0 + r), c0 + c, x);
 }
 
 // Queries that are rank-r already: into the scratch.
@@ -302,9 +336,9 @@ __global__ void __launch_bounds__(256) mq_simt_kernel(const MqDecodeParams p) {
 
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
   const int64_t end = p.list ? static_cast<int64_t>(p.list_len) << p.block_shift : static_cast<int64_t>(n_b) + p.tail;
-  const int64_t lo = static_cast<int64_t>(split) * p.per * 128;
+  const int64_t lo = (static_cast<int64_t>(split) * p.per) << p.tile_shift;
   if (split > 0 && lo >= end) return;        // a shorter sequence: nothing left (its first piece always reports)
-  const int64_t hi = min(end, lo + static_cast<int64_t>(p.per) * 128);
+  const int64_t hi = min(end, lo + (static_cast<int64_t>(p.per) << p.tile_shift));
   const uint64_t* masks = p.mask + static_cast<int64_t>(b) * p.tokens;
   const uint64_t seen = p.tail && live ? tree_mask(masks[t], p.tokens) : 0;
   const int pos = p.tail ? n_b + tree_depth(seen, t) : n_b - 1;        // position of the query
@@ -411,7 +445,7 @@ __device__ __forceinline__ float merged(const MqDecodeParams& p, int unit, int r
 }
 __device__ __forceinline__ int pieces_of(const MqDecodeParams& p, int b) {
   if (p.list != nullptr || p.deficit == nullptr) return p.splits;
-  const int tiles = (p.n - __ldg(p.deficit + b) + p.tail + 127) >> 7;
+  const int tiles = (p.n - __ldg(p.deficit + b) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
   return max(1, (tiles + p.per - 1) / p.per);
 }
 
@@ -461,71 +495,59 @@ __global__ void __launch_bounds__(256) mq_combine_few_kernel(const MqDecodeParam
   if (!half && d < p.d_head) out_row<T>(p, h, b, row)[d] = from_f<T>(y + ys[d]);
 }
 
-// Many rows: 64 query rows of one head (of one sequence after the other) against (U^V)^T in shared memory, a thread 8 rows
-// x 4 columns as in the projection.
-template <typename T>
-__global__ void __launch_bounds__(256) mq_combine_many_kernel(const __grid_constant__ MqDecodeParams p) {
+// Many rows: 64 query rows of one head (of one sequence after the other) against (U^V)^T in shared memory, in the register
+// tiles of the projection.  Two threads merge a row, half of its columns each.
+template <typename T, int C>
+__global__ void __launch_bounds__(kPrThreads) mq_combine_many_kernel(const __grid_constant__ MqDecodeParams p) {
   extern __shared__ __align__(16) float sm[];
   const int h = blockIdx.y, tid = threadIdx.x;
   const HeadInfo hd = p.heads[h];
-  float* ot = sm;                            // [rp_v][68]
+  float* ot = sm;                            // [rp_v][64]: o', transposed
   float* us = sm + hd.rp_v * kPrPitch;       // [rp_v][d_head]
-  const int r0 = blockIdx.x * kPrRows, total = p.B * p.rows;
+  __shared__ T* target[kPrRows];
+  const int total = p.B * p.rows;
   const float* Ut = p.basis + hd.uvt_off;
-  for (int i = tid; i < hd.rp_v * p.d_head / 4; i += 256) tc::cp_async16(us + 4 * i, Ut + 4 * i, 16);
+  for (int i = tid; i < hd.rp_v * p.d_head / 4; i += kPrThreads) tc::cp_async16(us + 4 * i, Ut + 4 * i, 16);
   tc::cp_async_commit();
-  const int warp = tid >> 5, lane = tid & 31;
-  for (int r = warp; r < kPrRows; r += 8) {  // a warp per row, lanes along its columns
-    const int g = r0 + r, b = g / p.rows, row = g - b * p.rows;
-    const int pieces = g < total ? pieces_of(p, b) : 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = lane + 32 * j;
-      if (c < hd.rp_v) ot[c * kPrPitch + r] = g < total ? merged(p, h * p.B + b, row, pieces, c) : 0.f;
+  {
+    const int r = tid & (kPrRows - 1), g = blockIdx.x * kPrRows + r;
+    const bool there = g < total;
+    const int b = there ? g / p.rows : 0;
+    const int pieces = there ? pieces_of(p, b) : 0;
+    if (tid < kPrRows) target[r] = there ? out_row<T>(p, h, b, g - b * p.rows) : nullptr;
+    const float* part = p.partials + (static_cast<int64_t>(h) * total + (there ? g : 0)) * p.splits * p.part_stride;
+    float M = -INFINITY, L = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < pieces; ++s) M = fmaxf(M, part[s * p.part_stride]);
+    const float base = M == -INFINITY ? 0.f : M;
+#pragma unroll 4
+    for (int s = 0; s < pieces; ++s) L = fmaf(part[s * p.part_stride + 1], ex2(part[s * p.part_stride] - base), L);
+    const float inv = L == 0.f ? 0.f : 1.f / L;              // (a row that sees nothing: its sums are zeros)
+    const int half = hd.rp_v / 2, c_lo = (tid / kPrRows) * half;
+    for (int c = c_lo; c < c_lo + half; c += 4) {            // half is a multiple of 4
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int s = 0; s < pieces; ++s) {
+        const float* x = part + s * p.part_stride;
+        const float f = ex2(x[0] - base) * inv;
+        const float4 v = *reinterpret_cast<const float4*>(x + 4 + c);
+        o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+      }
+      ot[c * kPrPitch + r] = o.x; ot[(c + 1) * kPrPitch + r] = o.y; ot[(c + 2) * kPrPitch + r] = o.z; ot[(c + 3) * kPrPitch + r] = o.w;
     }
   }
   tc::cp_async_wait<0>();
   __syncthreads();
-  const int rg = tid & 7, cg = tid >> 3;
-  if (4 * cg >= p.d_head) return;
-  uint64_t acc[4][4];
+  RegTile<C> t(tid);
+  t.multiply(ot, us, hd.rp_v, p.d_head);
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
+  for (int i = 0; i < 2; ++i) {
+    T* dst = target[2 * t.lane + i];
+    if (dst == nullptr) continue;
+    const bool whole = reinterpret_cast<uintptr_t>(dst) % (4 * sizeof(T)) == 0;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[c][r] = 0;
-  const float* xr = ot + 8 * rg;
-  const float* ur = us + 4 * cg;
-#pragma unroll 4
-  for (int k = 0; k < hd.rp_v; ++k) {
-    const ulonglong2 x0 = *reinterpret_cast<const ulonglong2*>(xr + k * kPrPitch);
-    const ulonglong2 x1 = *reinterpret_cast<const ulonglong2*>(xr + k * kPrPitch + 4);
-    const float4 u = *reinterpret_cast<const float4*>(ur + k * p.d_head);
-    const uint64_t uu[4] = {pack2(u.x, u.x), pack2(u.y, u.y), pack2(u.z, u.z), pack2(u.w, u.w)};
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      ffma2(acc[c][0], x0.x, uu[c]);
-      ffma2(acc[c][1], x0.y, uu[c]);
-      ffma2(acc[c][2], x1.x, uu[c]);
-      ffma2(acc[c][3], x1.y, uu[c]);
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    const int g = r0 + 8 * rg + r;
-    if (g >= total) return;
-    T* dst = out_row<T>(p, h, g / p.rows, g % p.rows) + 4 * cg;
-    float y[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const float2 v = unpack2(acc[c][r >> 1]);
-      y[c] = r & 1 ? v.y : v.x;
-    }
-    if (sizeof(T) == 2 && reinterpret_cast<uintptr_t>(dst) % 8 == 0) {
-      *reinterpret_cast<uint2*>(dst) = make_uint2(tc::pack_bf16(y[0], y[1]), tc::pack_bf16(y[2], y[3]));
-    } else {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) dst[c] = from_f<T>(y[c]);
-    }
+    for (int c = 0; c < C; c += 4)
+      if (t.c0 + c < p.d_head) put4(dst + t.c0 + c, t.acc[i][c], t.acc[i][c + 1], t.acc[i][c + 2], t.acc[i][c + 3], whole);
   }
 }
 
@@ -583,28 +605,40 @@ cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, u
   return cudaGetLastError();
 }
 
-cudaError_t launch_mq_project(const MqProjectParams& p, int dtype, int max_rp, cudaStream_t s, uint64_t* launches) {
+template <typename T, int C>
+static cudaError_t launch_project_many(const MqProjectParams& p, int tiles, int max_rp, cudaStream_t s) {
+  const size_t smem = sizeof(float) * (p.d_head * (kPrPitch + max_rp) + kPrPad);
+  static size_t configured[kMaxDevices] = {};
+  const cudaError_t e = ensure_dynamic_smem(mq_project_many_kernel<T, C>, smem, configured);
+  if (e != cudaSuccess) return e;
+  mq_project_many_kernel<T, C><<<dim3(tiles, p.H), kPrThreads, smem, s>>>(p);
+  return cudaGetLastError();
+}
+template <typename T>
+static cudaError_t launch_project_t(const MqProjectParams& p, int max_rp, cudaStream_t s) {
   const int rows_kv = p.B * p.tokens, rows_q = rows_kv * p.group;
-  const bool with_kv = p.k != nullptr;
-  // whole tiles of 64 rows where the rows fill most of them and there are enough tiles for the chip
+  // whole tiles of 64 rows where the rows fill most of one
   const bool many = rows_kv >= 48;
   const int rows = many ? kPrRows : kPfRows;
-  const int tiles = (p.with_q ? (rows_q + rows - 1) / rows : 0) + (with_kv ? 2 * ((rows_kv + rows - 1) / rows) : 0);
-  if (many) {
-    const size_t smem = sizeof(float) * p.d_head * (kPrPitch + max_rp);
-    static size_t configured[2][kMaxDevices] = {};
-    cudaError_t e = dtype == 0 ? ensure_dynamic_smem(mq_project_many_kernel<__nv_bfloat16>, smem, configured[0])
-                               : ensure_dynamic_smem(mq_project_many_kernel<float>, smem, configured[1]);
-    if (e != cudaSuccess) return e;
-    if (dtype == 0) mq_project_many_kernel<__nv_bfloat16><<<dim3(tiles, p.H), 256, smem, s>>>(p);
-    else mq_project_many_kernel<float><<<dim3(tiles, p.H), 256, smem, s>>>(p);
-  } else {
-    const dim3 grid(tiles, p.H, (max_rp + kPfCols - 1) / kPfCols);
-    if (dtype == 0) mq_project_few_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(p);
-    else mq_project_few_kernel<float><<<grid, 128, 0, s>>>(p);
+  const int tiles = (p.with_q ? (rows_q + rows - 1) / rows : 0) + (p.k != nullptr ? 2 * ((rows_kv + rows - 1) / rows) : 0);
+  if (!many) {
+    mq_project_few_kernel<T><<<dim3(tiles, p.H, (max_rp + kPfCols - 1) / kPfCols), 128, 0, s>>>(p);
+    return cudaGetLastError();
   }
+  switch ((max_rp + 15) / 16) {              // columns of a warp: a quarter of the widest rank, in fours
+    case 1: case 2: return launch_project_many<T, 8>(p, tiles, max_rp, s);
+    case 3: return launch_project_many<T, 12>(p, tiles, max_rp, s);
+    case 4: return launch_project_many<T, 16>(p, tiles, max_rp, s);
+    case 5: return launch_project_many<T, 20>(p, tiles, max_rp, s);
+    case 6: return launch_project_many<T, 24>(p, tiles, max_rp, s);
+    case 7: return launch_project_many<T, 28>(p, tiles, max_rp, s);
+    default: return launch_project_many<T, 32>(p, tiles, max_rp, s);
+  }
+}
+
+cudaError_t launch_mq_project(const MqProjectParams& p, int dtype, int max_rp, cudaStream_t s, uint64_t* launches) {
   ++*launches;
-  return cudaGetLastError();
+  return dtype == 0 ? launch_project_t<__nv_bfloat16>(p, max_rp, s) : launch_project_t<float>(p, max_rp, s);
 }
 
 cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches) {
@@ -617,17 +651,22 @@ cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, u
   return cudaGetLastError();
 }
 
+template <typename T, int C>
+static cudaError_t launch_combine_many(const MqDecodeParams& p, int max_rp_v, cudaStream_t s) {
+  const size_t smem = sizeof(float) * (max_rp_v * (kPrPitch + p.d_head) + kPrPad);
+  static size_t configured[kMaxDevices] = {};
+  const cudaError_t e = ensure_dynamic_smem(mq_combine_many_kernel<T, C>, smem, configured);
+  if (e != cudaSuccess) return e;
+  mq_combine_many_kernel<T, C><<<dim3((p.B * p.rows + kPrRows - 1) / kPrRows, p.H), kPrThreads, smem, s>>>(p);
+  return cudaGetLastError();
+}
 template <typename T>
 static cudaError_t launch_combine_t(const MqDecodeParams& p, int max_rp_v, cudaStream_t s) {
   const int64_t units = static_cast<int64_t>(p.B) * p.H, rows = units * p.rows;
   if (p.flags & 0x2u) {                      // EA_OUT_LOWRANK
     mq_combine_lowrank_kernel<T><<<static_cast<unsigned>(rows), 128, 0, s>>>(p);
   } else if (p.B * p.rows >= 64 && rows >= 2048) {
-    const size_t smem = sizeof(float) * max_rp_v * (kPrPitch + p.d_head);
-    static size_t configured[kMaxDevices] = {};
-    const cudaError_t e = ensure_dynamic_smem(mq_combine_many_kernel<T>, smem, configured);
-    if (e != cudaSuccess) return e;
-    mq_combine_many_kernel<T><<<dim3((p.B * p.rows + kPrRows - 1) / kPrRows, p.H), 256, smem, s>>>(p);
+    return p.d_head <= 64 ? launch_combine_many<T, 16>(p, max_rp_v, s) : launch_combine_many<T, 32>(p, max_rp_v, s);
   } else {
     mq_combine_few_kernel<T><<<static_cast<unsigned>(rows), 256, 0, s>>>(p);
   }

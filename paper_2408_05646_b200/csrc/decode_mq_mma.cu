@@ -1,7 +1,7 @@
 // Attention of several query rows per K/V head over one sequence's rows (a tree of drafted tokens, or one token over a
 // list of blocks) with warp-level tensor-core products, for 16-bit layers.
 //
-// A warp takes 32 cached rows of every tile of 128 and 8 or 16 query rows: S = Q' K'^T and O' += P V' with mma.sync
+// A warp takes 32 cached rows of every tile of 128 (16 of 64 for wide ranks) and 8 or 16 query rows: S = Q' K'^T and O' += P V' with mma.sync
 // m16n8k16, the softmax in between on the accumulator fragments, which are at the same time the A fragments of the second
 // product.  The 16 rows of an A operand hold 8 queries twice: rows 0-7 the leading 16-bit part of Q' (or of P), rows 8-15
 // what it leaves.  A thread of the fragment layout owns rows g and g + 8, the two halves of one query, so adding them is
@@ -11,6 +11,9 @@
 // Rows travel by 16-byte asynchronous copies into a ring that belongs to the warps that read it (one warp, or two that
 // share the rows and split the queries): no block-wide barrier and no wait that could fail to end.  In shared memory a row
 // sits at an odd multiple of 16 bytes, so that the eight rows of an ldmatrix meet all banks once, whatever the rank.
+// Heads narrower than the instance keep zeros in the rest of their rows: the products run over the instance's width
+// without a branch (with guards per piece of a row, which cut the code into short blocks that cannot overlap, a layer of
+// mixed ranks took 152 us where it now takes the time of its bytes).
 #include <cuda_bf16.h>
 
 #include "internal.h"
@@ -24,25 +27,31 @@ using namespace tc;
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kRaise = 8.f;              // a running maximum is raised when a score exceeds it by this much
 constexpr int kGroups = 4;                 // key groups of a tile
-constexpr int kRows = 32;                  // rows of a key group
 
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-  asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(b0));
-}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void ldsm2(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm2_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr) : "memory");
+}
 __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void cp_async16_to(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async16_fill(uint32_t dst, const void* src, uint32_t bytes) {   // 0 bytes: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ float quad_max(float v) {
   v = fmaxf(v, __shfl_xor_sync(kFull, v, 1));
@@ -59,37 +68,41 @@ __device__ __forceinline__ int tree_depth(uint64_t m, int t) { return __popcll(m
 // The 16-byte pieces of a row, and the distance of two rows in shared memory in such pieces.
 __host__ __device__ constexpr int odd_pieces(int pieces) { return pieces | 1; }
 
-// Shape of an instance: NC = 8-channel pieces of the widest row; MT = tiles of 8 queries per warp; WG = warps that share a
-// key group's rows.
+// Shape of an instance: NC = 8-channel pieces of a row (even); MT = tiles of 8 queries per warp; WG = warps that share a
+// key group's rows.  Wide rows come 16 at a time, so that two CTAs with two or three stages each still fit an SM.
 template <int NC, int MT, int WG>
 struct Shape {
+  static constexpr int kRows = NC > 12 ? 16 : 32;                         // rows of a key group
+  static constexpr int kHalves = kRows / 16, kJ = kRows / 8;
+  static constexpr int kTile = kGroups * kRows, kTileShift = kTile == 64 ? 6 : 7;
   static constexpr int kThreads = kGroups * WG * 32;
   static constexpr int kQueries = 8 * MT * WG;
-  static constexpr int kSlot = kRows * 2 * odd_pieces(NC) * 16;          // one key group's rows of a tile
-  static constexpr int kCtas = WG == 1 && NC <= 10 ? 2 : 1;               // resident CTAs per SM
+  static constexpr int kPitch = odd_pieces(NC) * 16;
+  static constexpr int kSlot = kRows * 2 * kPitch;                        // one key group's rows of a tile
+  static constexpr int kCtas = WG == 1 ? 2 : 1;                           // resident CTAs per SM
   static constexpr bool kQReg = MT * NC * 2 <= 40;                        // Q' fragments in registers, else in shared memory
-  static constexpr int kQBytes = kQReg ? 0 : WG * MT * ((NC + 1) / 2) * 32 * 16;
+  static constexpr int kQBytes = kQReg ? 0 : WG * MT * (NC / 2) * 32 * 16;
   static constexpr int kHead = 32 * 8 + 64 * 4;                           // masks of the queries, places of the drafted rows
-  static constexpr int kRoom = (kCtas == 2 ? 112 : 226) * 1024 - kHead - kQBytes - 64;
+  static constexpr int kRoom = (kCtas == 2 ? 113 : 226) * 1024 - kHead - kQBytes;
   static constexpr int kStages = kRoom / (kGroups * kSlot) < 4 ? kRoom / (kGroups * kSlot) : 4;
   static constexpr int kMerge = kGroups * kQueries * (2 + 8 * NC + 1) * 4;
   static constexpr int kRing = kGroups * kSlot * kStages > kMerge ? kGroups * kSlot * kStages : kMerge;
-  static constexpr size_t kSmem = kHead + kQBytes + kRing + 64;           // (an ldmatrix may read past a row's last piece)
-  static_assert(kStages >= 2, "ring too shallow");
+  static constexpr size_t kSmem = kHead + kQBytes + kRing;
+  static_assert(NC % 2 == 0 && kStages >= 2, "instance does not fit");
 };
 
-// Where the 32 rows of a key group come from: two runs of 16 neighbouring rows (a block can be 16 rows long).
+// Where the rows of a key group come from: runs of 16 neighbouring rows (a block can be 16 rows long).
 struct Source {
   int64_t row[2];          // physical first row of each half
   int valid[2];            // rows of each half that exist
   int first[2];            // logical first row of each half (-1: nothing there)
 };
 
-template <int NC, int MT, int WG, bool FULL>
+template <int NC, int MT, int WG>
 __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>::kCtas)
     mq_mma_kernel(const MqDecodeParams p) {
   using S = Shape<NC, MT, WG>;
-  constexpr int NKS = (NC + 1) / 2;
+  constexpr int NKS = NC / 2, kRows = S::kRows, HV = S::kHalves, NJ = S::kJ;
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* q_mask = reinterpret_cast<uint64_t*>(smem);                   // [32]
   float* draft_pos = reinterpret_cast<float*>(smem + 32 * 8);             // [64]
@@ -102,13 +115,13 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
   const int unit = blockIdx.x / chunks, chunk = blockIdx.x - unit * chunks, split = blockIdx.y;
   const int h = unit / p.B, b = unit - h * p.B;
   const HeadInfo hd = p.heads[h];
-  const int nck = FULL ? NC : hd.rp_k >> 3, ncv = FULL ? NC : hd.rp_v >> 3;
-  const int kpitch = odd_pieces(nck) * 16, vpitch = odd_pieces(ncv) * 16;
+  const int nck = hd.rp_k >> 3, ncv = hd.rp_v >> 3;                       // pieces of this head's rows
+  constexpr int kpitch = S::kPitch, vpitch = S::kPitch;
   const int row0 = chunk * S::kQueries;                                   // first query row of the CTA
 
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
   const int64_t end = p.list ? static_cast<int64_t>(p.list_len) << p.block_shift : static_cast<int64_t>(n_b) + p.tail;
-  const int nt = static_cast<int>((end + 127) >> 7);
+  const int nt = static_cast<int>((end + S::kTile - 1) >> S::kTileShift);
   const int t_lo = split * p.per, t_hi = min(nt, t_lo + p.per);
   if (split > 0 && t_lo >= nt) return;       // a shorter sequence: nothing left (its first piece always reports)
   const int32_t* list = p.list ? p.list + static_cast<int64_t>(unit) * p.list_len : nullptr;
@@ -119,17 +132,17 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
   // ---- rows: the copies of one key group, by its own warps.  What the address of a tile needs (the block's number, its
   // page) is loaded one and two tiles ahead of its use.
   const int64_t pos0 = static_cast<int64_t>(kg) * kRows;                  // of the key group inside a tile
-  int blk_next[2] = {-1, -1}, blk_now[2] = {-1, -1}, page_now[2] = {0, 0};
+  int blk_next[2] = {-1, -1}, blk_now[2] = {-1, -1}, page_now[2] = {0, 0};   // per half
   auto fetch_block = [&](int t, int (&blk)[2]) {                          // list entries of tile t
     if (list == nullptr || t >= t_hi) return;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t at = ((static_cast<int64_t>(t) << 7) + pos0 + 16 * i) >> p.block_shift;
+    for (int i = 0; i < HV; ++i) {
+      const int64_t at = ((static_cast<int64_t>(t) << S::kTileShift) + pos0 + 16 * i) >> p.block_shift;
       blk[i] = at < p.list_len ? __ldg(list + at) : -1;
     }
   };
   auto logical = [&](int t, int i, int blk) -> int {                      // first logical row of a half
-    const int64_t at = (static_cast<int64_t>(t) << 7) + pos0 + 16 * i;
+    const int64_t at = (static_cast<int64_t>(t) << S::kTileShift) + pos0 + 16 * i;
     if (list == nullptr) return static_cast<int>(at);
     return blk < 0 ? -1 : (blk << p.block_shift) + static_cast<int>(at & ((1 << p.block_shift) - 1));
   };
@@ -137,15 +150,16 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
   auto fetch_page = [&](int t, const int (&blk)[2], int (&page)[2]) {
     if (p.pages.table == nullptr || t >= t_hi) return;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < HV; ++i) {
       const int r = logical(t, i, blk[i]);
       page[i] = r >= 0 && r < row_end ? __ldg(p.pages.table + static_cast<int64_t>(b) * p.pages.width + (r >> p.pages.shift)) : 0;
     }
   };
   auto source = [&](int t, const int (&blk)[2], const int (&page)[2]) {
     Source s;
+    s.row[1] = 0; s.valid[1] = 0; s.first[1] = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < HV; ++i) {
       const int r = logical(t, i, blk[i]);
       const bool there = r >= 0 && r < row_end;
       s.first[i] = r;
@@ -157,18 +171,38 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
     return s;
   };
   const int cl = lane + 32 * rg;                                          // this thread among the copiers of the group
-  const uint32_t inv_k = 65536 / nck + 1, inv_v = 65536 / ncv + 1;        // i / nc = i inv >> 16 for i < 512
-  auto copy_rows = [&](unsigned char* dst, const char* slab, int nc, uint32_t inv, int pitch, const Source& s) {
-    const char* s0 = slab + s.row[0] * (nc * 16);
-    const char* s1 = slab + (s.row[1] - 16) * (nc * 16);
+  constexpr int kStep = 32 * WG;
+  // Piece i = cl, cl + kStep, ... of the rows, row after row: its row and place are stepped, not divided out (with a
+  // division and the row's checks for every piece the copies were most of the kernel's instructions).
+  struct Walk { int row, c, d_row, d_c; };
+  auto walk = [&](int nc) { return Walk{cl / nc, cl % nc, kStep / nc, kStep % nc}; };
+  const Walk wk = walk(nck), wv = walk(ncv);
+  auto copy_rows = [&](unsigned char* dst, const char* slab, int nc, const Walk& w0, const Source& s) {
+    const char* src = slab + s.row[0] * (nc * 16) + cl * 16;
+    Walk w = w0;
+    uint32_t to = smem_u32(dst) + w.row * kpitch + w.c * 16;
+    const uint32_t step = w.d_row * kpitch + w.d_c * 16, wrap = kpitch - nc * 16;
+    const int total = kRows * nc;
+    if (s.valid[0] == 16 && (HV == 1 || (s.valid[1] == 16 && s.row[1] == s.row[0] + 16))) {    // whole, and neighbours
 #pragma unroll
-    for (int i0 = 0; i0 < kRows * NC; i0 += 32 * WG) {
-      const int i = i0 + cl;
-      if (i < kRows * nc) {
-        const int row = FULL ? i / NC : static_cast<int>(i * inv >> 16);
-        const bool late = row >= 16;
-        const bool there = (late ? row - 16 : row) < (late ? s.valid[1] : s.valid[0]);
-        cp_async16(dst + row * pitch + (i - row * nc) * 16, there ? (late ? s1 : s0) + static_cast<int64_t>(i) * 16 : slab, there ? 16u : 0u);
+      for (int i0 = 0; i0 < kRows * NC; i0 += kStep) {
+        if (i0 + cl < total) cp_async16_to(to, src + i0 * 16);
+        to += step;
+        w.c += w.d_c;
+        if (w.c >= nc) { w.c -= nc; to += wrap; }
+      }
+    } else {
+      const int64_t skip = HV == 2 ? (s.row[1] - s.row[0] - 16) * (nc * 16) : 0;
+#pragma unroll 1
+      for (int i = cl; i < total; i += kStep) {
+        const bool late = HV == 2 && w.row >= 16;
+        const bool there = late ? w.row - 16 < s.valid[1] : w.row < s.valid[0];
+        cp_async16_fill(to, there ? src + (late ? skip : 0) : slab, there ? 16u : 0u);
+        src += kStep * 16;
+        to += step;
+        w.row += w.d_row;
+        w.c += w.d_c;
+        if (w.c >= nc) { w.c -= nc; ++w.row; to += wrap; }
       }
     }
   };
@@ -181,14 +215,19 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
       const Source s = source(t, blk_now, page_now);
       ahead[S::kStages - 2][0] = s.first[0]; ahead[S::kStages - 2][1] = s.first[1];
       unsigned char* dst = slot_of(t - t_lo);
-      copy_rows(dst, k_slab, nck, inv_k, kpitch, s);
-      copy_rows(dst + kRows * kpitch, v_slab, ncv, inv_v, vpitch, s);
+      copy_rows(dst, k_slab, nck, wk, s);
+      copy_rows(dst + kRows * kpitch, v_slab, ncv, wv, s);
     }
     cp_async_commit();
     blk_now[0] = blk_next[0]; blk_now[1] = blk_next[1];
     fetch_page(t + 1, blk_now, page_now);
     fetch_block(t + 2, blk_next);
   };
+  if (nck < NC || ncv < NC)            // the rest of a narrow head's rows: zeros that no copy touches
+    for (int i = tid; i < kGroups * S::kStages * kRows * 2; i += S::kThreads) {
+      uint4* row = reinterpret_cast<uint4*>(ring + i * kpitch);
+      for (int c = (i / kRows) & 1 ? ncv : nck; c < NC; ++c) row[c] = make_uint4(0u, 0u, 0u, 0u);
+    }
   fetch_block(t_lo, blk_now);
   fetch_page(t_lo, blk_now, page_now);
   fetch_block(t_lo + 1, blk_next);
@@ -250,7 +289,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + kg), "n"(32 * WG) : "memory");
   };
   const uint32_t k_lane = static_cast<uint32_t>((lane & 7) * kpitch + (lane >> 3) * 16);
-  const uint32_t v_lane = static_cast<uint32_t>(kRows * kpitch + lane * vpitch);
+  const uint32_t v_lane = static_cast<uint32_t>(kRows * kpitch + (lane & (kRows - 1)) * vpitch);
 
   for (int t = t_lo; t < t_hi; ++t) {
     cp_async_wait<S::kStages - 2>();
@@ -260,60 +299,56 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
     unsigned char* st = slot_of(t - t_lo);
     const uint32_t k_addr = smem_u32(st) + k_lane, v_addr = smem_u32(st) + v_lane;
 
-    float s[MT][4][4];
+    float s[MT][NJ][4];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[mt][j][i] = 0.f;
 #pragma unroll
     for (int c4 = 0; c4 < NC; c4 += 4) {
-      if (FULL || c4 < nck) {
-        uint32_t kf[4][4];
+      uint32_t kf[NJ][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) ldsm4(kf[j], k_addr + j * 8 * kpitch + c4 * 16);
+      for (int j = 0; j < NJ; ++j) {
+        if (c4 + 2 < NC) ldsm4(kf[j], k_addr + j * 8 * kpitch + c4 * 16);
+        else ldsm2(kf[j], k_addr + j * 8 * kpitch + c4 * 16);
+      }
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int ks = c4 / 2 + half;
-          if (ks < NKS) {
+      for (int half = 0; half < 2; ++half) {
+        const int ks = c4 / 2 + half;
+        if (ks < NKS) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              uint32_t a[4];
-              if constexpr (S::kQReg) {
+          for (int mt = 0; mt < MT; ++mt) {
+            uint32_t a[4];
+            if constexpr (S::kQReg) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) a[i] = qa[mt][ks < NKS ? ks : 0][i];
-              } else {
-                const uint4 f = q_img[((rg * MT + mt) * NKS + ks) * 32 + lane];
-                a[0] = f.x; a[1] = f.y; a[2] = f.z; a[3] = f.w;
-              }
-              if (FULL ? 2 * ks + 1 < NC : 2 * ks + 1 < nck) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) mma16(s[mt][j], a, kf[j][2 * half], kf[j][2 * half + 1]);
-              } else if (FULL || 2 * ks < nck) {                          // a row's last piece: eight channels
-#pragma unroll
-                for (int j = 0; j < 4; ++j) mma8(s[mt][j], a[0], a[1], kf[j][2 * half]);
-              }
+              for (int i = 0; i < 4; ++i) a[i] = qa[mt][ks < NKS ? ks : 0][i];
+            } else {
+              const uint4 f = q_img[((rg * MT + mt) * NKS + ks) * 32 + lane];
+              a[0] = f.x; a[1] = f.y; a[2] = f.z; a[3] = f.w;
             }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) mma16(s[mt][j], a, kf[j][2 * half], kf[j][2 * half + 1]);
           }
         }
       }
     }
     // ---- scores: the two halves of a query, the bias, the mask.  sc[mt][j][e]: row 8 j + 2 tig + e of the group
-    float sc[MT][4][2];
+    float sc[MT][NJ][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < NJ; ++j) {
         sc[mt][j][0] = s[mt][j][0] + s[mt][j][2];
         sc[mt][j][1] = s[mt][j][1] + s[mt][j][3];
       }
     // the end of the sequence, drafted rows, a list entry that is not there (they come last, as the incomplete block does)
-    const bool special = bias || first[0] < 0 || first[1] < 0 || max(first[0], first[1]) + 16 > n_b;
+    const bool special = bias || first[0] < 0 || (HV == 2 && first[1] < 0) || (HV == 2 ? max(first[0], first[1]) : first[0]) + 16 > n_b;
     unsigned odd_rows = 0;             // drafted rows whose values are not finite
     if (special) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int kk = 8 * (j & 1) + 2 * tig + e;                       // inside its half
@@ -331,7 +366,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
       if (p.tail && first[0] + kRows > n_b) {          // (the whole sequence: the two halves are neighbours)
         const int r = first[0] + lane;
         bool bad = false;
-        if (r >= n_b && r < row_end) {
+        if (lane < kRows && r >= n_b && r < row_end) {
           const uint4* x = reinterpret_cast<const uint4*>(st + kRows * kpitch + lane * vpitch);
           for (int c = 0; c < ncv; ++c) {
             const uint4 w = x[c];
@@ -349,8 +384,9 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
     float mx[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      mx[mt] = fmaxf(max3(sc[mt][0][0], sc[mt][0][1], sc[mt][1][0]), max3(sc[mt][1][1], sc[mt][2][0], sc[mt][2][1]));
-      mx[mt] = max3(mx[mt], sc[mt][3][0], sc[mt][3][1]);
+      mx[mt] = fmaxf(max3(sc[mt][0][0], sc[mt][0][1], sc[mt][1][0]), sc[mt][1][1]);
+#pragma unroll
+      for (int j = 2; j < NJ; ++j) mx[mt] = max3(mx[mt], sc[mt][j][0], sc[mt][j][1]);
       raise = raise || mx[mt] > m[mt] + kRaise;
     }
     if (__any_sync(kFull, raise)) {
@@ -367,11 +403,11 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
           for (int i = 0; i < 4; ++i) o[mt][c][i] *= f;
       }
     }
-    uint32_t pa[MT][2][4];             // A fragments of P for the two steps of 16 rows: leading parts and remainders
+    uint32_t pa[MT][HV][4];            // A fragments of P for the steps of 16 rows: leading parts and remainders
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < NJ; ++j) {
         sc[mt][j][0] = ex2(sc[mt][j][0] - base[mt]);
         sc[mt][j][1] = ex2(sc[mt][j][1] - base[mt]);
         l[mt] += sc[mt][j][0] + sc[mt][j][1];
@@ -381,7 +417,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
       // A product with a zero weight would still carry an infinity or NaN of a row that the query does not see: such rows
       // are added one by one where their weight is not zero, and then cleared for the products.
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
           for (int src = 0; src < 4; ++src) {
@@ -393,11 +429,10 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
               const float w = __shfl_sync(kFull, sc[mt][j][e], (lane & ~3) | src);
               if (w != 0.f) {
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-                  if (FULL || c < ncv) {
-                    o[mt][c][0] = fmaf(w, __bfloat162float(v[8 * c + 2 * tig]), o[mt][c][0]);
-                    o[mt][c][1] = fmaf(w, __bfloat162float(v[8 * c + 2 * tig + 1]), o[mt][c][1]);
-                  }
+                for (int c = 0; c < NC; ++c) {
+                  o[mt][c][0] = fmaf(w, __bfloat162float(v[8 * c + 2 * tig]), o[mt][c][0]);
+                  o[mt][c][1] = fmaf(w, __bfloat162float(v[8 * c + 2 * tig + 1]), o[mt][c][1]);
+                }
               }
             }
           }
@@ -410,16 +445,16 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
     }
     // ---- O' += P V'
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-      if (FULL || c < ncv) {
-        uint32_t vf[4];
-        ldsm4_t(vf, v_addr + c * 16);
+    for (int c = 0; c < NC; ++c) {
+      uint32_t vf[4];
+      if (HV == 2) ldsm4_t(vf, v_addr + c * 16);
+      else ldsm2_t(vf, v_addr + c * 16);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          mma16(o[mt][c], pa[mt][0], vf[0], vf[1]);
-          mma16(o[mt][c], pa[mt][1], vf[2], vf[3]);
-        }
+      for (int mt = 0; mt < MT; ++mt) {
+        mma16(o[mt][c], pa[mt][0], vf[0], vf[1]);
+        if (HV == 2) mma16(o[mt][c], pa[mt][HV - 1], vf[2], vf[3]);
       }
+    }
   }
   cp_async_wait<0>();
   __syncthreads();
@@ -437,7 +472,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
     if (tig == 0) { wm[q] = m[mt]; wl[q] = l[mt]; }
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      if (FULL || c < ncv) {
+      if (c < ncv) {
         wo[q * OS + 8 * c + 2 * tig] = o[mt][c][0] + o[mt][c][2];
         wo[q * OS + 8 * c + 2 * tig + 1] = o[mt][c][1] + o[mt][c][3];
       }
@@ -460,38 +495,40 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
   }
 }
 
-template <int NC, int MT, int WG, bool FULL>
+template <int NC, int MT, int WG>
 cudaError_t launch_instance(const MqDecodeParams& p, cudaStream_t s) {
   using S = Shape<NC, MT, WG>;
   static size_t configured[kMaxDevices] = {};
-  const cudaError_t e = ensure_dynamic_smem(mq_mma_kernel<NC, MT, WG, FULL>, S::kSmem, configured);
+  const cudaError_t e = ensure_dynamic_smem(mq_mma_kernel<NC, MT, WG>, S::kSmem, configured);
   if (e != cudaSuccess) return e;
   const int chunks = (p.rows + S::kQueries - 1) / S::kQueries;
-  mq_mma_kernel<NC, MT, WG, FULL><<<dim3(p.B * p.H * chunks, p.splits), S::kThreads, S::kSmem, s>>>(p);
+  mq_mma_kernel<NC, MT, WG><<<dim3(p.B * p.H * chunks, p.splits), S::kThreads, S::kSmem, s>>>(p);
   return cudaGetLastError();
 }
 template <int NC>
-cudaError_t launch_rank(const MqDecodeParams& p, bool full, cudaStream_t s) {
-  if (p.rows <= 8) return full ? launch_instance<NC, 1, 1, true>(p, s) : launch_instance<NC, 1, 1, false>(p, s);
-  if (p.rows <= 16) return full ? launch_instance<NC, 2, 1, true>(p, s) : launch_instance<NC, 2, 1, false>(p, s);
-  return full ? launch_instance<NC, 2, 2, true>(p, s) : launch_instance<NC, 2, 2, false>(p, s);
+cudaError_t launch_rank(const MqDecodeParams& p, cudaStream_t s) {
+  if (p.rows <= 8) return launch_instance<NC, 1, 1>(p, s);
+  if (p.rows <= 16) return launch_instance<NC, 2, 1>(p, s);
+  return launch_instance<NC, 2, 2>(p, s);
 }
 
 }  // namespace
 
 MqShape mq_mma_shape(int rows, int max_rp) {
-  if (rows <= 8) return {8, max_rp <= 80 ? 2 : 1};
-  if (rows <= 16) return {16, max_rp <= 80 ? 2 : 1};
-  return {32, 1};
+  const int shift = max_rp > 96 ? 6 : 7;
+  if (rows <= 8) return {8, 2, shift};
+  if (rows <= 16) return {16, 2, shift};
+  return {32, 1, shift};
 }
 
-cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, int min_rp, cudaStream_t s, uint64_t* launches) {
-  cudaError_t e;
-  if (max_rp <= 64) e = launch_rank<8>(p, min_rp == 64, s);
-  else if (max_rp <= 80) e = launch_rank<10>(p, min_rp == 80, s);
-  else e = launch_rank<16>(p, min_rp == 128, s);
+cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, cudaStream_t s, uint64_t* launches) {
   ++*launches;
-  return e;
+  if (max_rp <= 48) return launch_rank<6>(p, s);
+  if (max_rp <= 64) return launch_rank<8>(p, s);
+  if (max_rp <= 80) return launch_rank<10>(p, s);
+  if (max_rp <= 96) return launch_rank<12>(p, s);
+  if (max_rp <= 112) return launch_rank<14>(p, s);
+  return launch_rank<16>(p, s);
 }
 
 }  // namespace ea

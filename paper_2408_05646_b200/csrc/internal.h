@@ -299,7 +299,8 @@ struct MqDecodeParams {
   int32_t group, tokens, rows;   // rows = tokens * group
   int32_t tail;             // drafted rows behind every sequence (0 or tokens)
   int32_t q_stride, part_stride;
-  int32_t tiles;            // tiles of 128 rows of the longest unit
+  int32_t tile_shift;       // log2 of the rows of a tile
+  int32_t tiles;            // tiles of the longest unit
   int32_t per;              // tiles of a piece
   int32_t splits;           // pieces of the longest unit = ceil(tiles / per)
   int32_t lr_v_width;       // sum of rp_v: width of a packed output row of one query head
@@ -381,10 +382,11 @@ __device__ __forceinline__ int64_t physical_block(const SparseParams& p, int b, 
 cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_project(const MqProjectParams& p, int dtype, int max_rp, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, uint64_t* launches);
-struct MqShape { int queries, ctas_per_sm; };   // query rows of a CTA, resident CTAs
+struct MqShape { int queries, ctas_per_sm, tile_shift; };   // query rows of a CTA, resident CTAs, log2 of a tile's rows
+constexpr MqShape kMqSimtShape = {8, 2, 5};
 MqShape mq_mma_shape(int rows, int max_rp);
-// 16-bit layers; max_rp / min_rp: widest and narrowest padded rank over heads and K/V
-cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, int min_rp, cudaStream_t s, uint64_t* launches);
+// 16-bit layers; max_rp: widest padded rank over heads and K/V
+cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, int max_rp_v, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_tree_commit(const TreeCommitParams& p, int sequences, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_block_bounds(const SparseParams& p, int dtype, cudaStream_t s, uint64_t* launches);
