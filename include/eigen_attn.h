@@ -396,6 +396,9 @@ typedef enum {
   EA_OPT_GQA_IMPL = 9,        /* eigen_attn_decode_gqa without a rotary embedding: 0 = automatic (warp-level mma.sync
                                  products where every padded key rank is a multiple of 16 and d_head <= 128, else the
                                  tcgen05 kernel), 1 = always the tcgen05 kernel                              */
+  EA_OPT_TREE_IMPL = 10,      /* eigen_attn_decode_tree of a 16-bit layer: 0 = automatic (tcgen05 products from 17 query
+                                 rows per K/V head on, unless an ALiBi bias is set or pages do not divide n_max; warp-level
+                                 products otherwise), 1 = always the warp-level products                     */
   EA_OPT_TEST_WAIT_GIVES_UP = 7 /* failure-path test hook.  1 arms it for the NEXT eigen_attn_decode /
                                  _decode_step / _decode_static launch only: one warp of one CTA treats its
                                  first wait for a tile as having exceeded the bound.  The launch then ends the

@@ -259,6 +259,7 @@ struct eigen_attn {
   int64_t opt_min_copy = -1;  // EA_OPT_DECODE_MIN_COPY_BYTES; < 0 = the built-in default
   int64_t opt_give_up = 0;   // EA_OPT_TEST_WAIT_GIVES_UP: armed for the next split-KV decode launch
   int64_t opt_gqa_impl = 0;  // EA_OPT_GQA_IMPL
+  int64_t opt_tree_impl = 0; // EA_OPT_TREE_IMPL
   uint64_t launches = 0;
   cudaEvent_t ev_start = nullptr, ev_stop = nullptr;
   // quantised copy of the cache (Section 5.3), attached by the caller
@@ -1375,7 +1376,13 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
   // one size, so a shorter sequence of the batch has fewer of them; the partials must have room.
   const bool mma = h->desc.dtype == EA_BF16;
   const int max_rp = L.max_rp_k > L.max_rp_v ? L.max_rp_k : L.max_rp_v;
-  const ea::MqShape shape = mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::kMqSimtShape;
+  // Trees with more than 16 query rows: tcgen05 products, where the layer's slabs have tensor maps (pages then have to lie
+  // inside one sequence's slab) and no bias goes onto the scores.
+  p.tmaps = h->ws + L.off_tmaps;
+  p.status = dev_status(h);
+  const bool tc = mma && p.tail > 0 && p.rows > 16 && h->tmaps_ok && !h->alibi && h->opt_tree_impl != 1 &&
+                  (!h->paged || h->desc.n_max % (1 << h->page_shift) == 0);
+  const ea::MqShape shape = tc ? ea::kMqTcShape : mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::kMqSimtShape;
   const int tile = 1 << shape.tile_shift;
   p.tile_shift = shape.tile_shift;
   p.tiles = static_cast<int32_t>((end + tile - 1) >> shape.tile_shift);
@@ -1411,8 +1418,9 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
   p.per = static_cast<int32_t>(per);
   p.splits = static_cast<int32_t>((p.tiles + per - 1) / per);
   if (h->ev_start) cudaEventRecord(h->ev_start, s);
-  cudaError_t e = mma ? ea::launch_mq_mma(p, max_rp, s, &h->launches)
-                      : ea::launch_mq_simt(p, h->desc.dtype, s, &h->launches);
+  cudaError_t e = tc    ? ea::launch_mq_tc(p, L.max_rp_k, L.max_rp_v, s, &h->launches)
+                  : mma ? ea::launch_mq_mma(p, max_rp, s, &h->launches)
+                        : ea::launch_mq_simt(p, h->desc.dtype, s, &h->launches);
   if (h->ev_stop) cudaEventRecord(h->ev_stop, s);
   if (e == cudaSuccess) e = ea::launch_mq_combine(p, h->desc.dtype, L.max_rp_v, s, &h->launches);
   if (e != cudaSuccess) return cuda_fail(h, e, who);
@@ -1988,6 +1996,10 @@ ea_status eigen_attn_set_option(eigen_attn_t h, int32_t option, int64_t value) {
     case EA_OPT_GQA_IMPL:
       if (value < 0 || value > 1) return fail(h, EA_ERR_INVALID_ARG, "GQA_IMPL %lld", static_cast<long long>(value));
       h->opt_gqa_impl = value;
+      return EA_OK;
+    case EA_OPT_TREE_IMPL:
+      if (value < 0 || value > 1) return fail(h, EA_ERR_INVALID_ARG, "TREE_IMPL %lld", static_cast<long long>(value));
+      h->opt_tree_impl = value;
       return EA_OK;
     case EA_OPT_TEST_WAIT_GIVES_UP:
       if (value < 0 || value > 1) return fail(h, EA_ERR_INVALID_ARG, "TEST_WAIT_GIVES_UP %lld", static_cast<long long>(value));

@@ -1,0 +1,425 @@
+// Attention of many query rows per K/V head (a large tree of drafted tokens, or a smaller one times its group of query
+// heads) over one sequence's rows on the fifth-generation tensor cores: tcgen05 products, accumulators in TMEM.
+//
+// With more than 16 query rows a tile of cached rows carries more arithmetic than warp-level products deliver while it
+// streams; a tcgen05 product has 128 rows of queries.  One CTA per SM owns 128 query rows of a unit and a piece of its
+// rows, in tiles of 128:
+//   * one thread streams K' and V' tiles by TMA (64 x 64 boxes of the cache slabs' tensor maps, 128-byte swizzle) into a
+//     ring; boxes without a row of the sequence, and columns past the rank, arrive as zeros;
+//   * one thread issues S(t) = Q' K'^T, another O' += P V'.  Q' and P are A operands in TMEM, each as two 16-bit parts
+//     (leading part and remainder, 16 significant bits together), so every product is issued twice over; the result
+//     carries no more than the rounding of the output.  S has two buffers; P(t) takes the place of S(t): its leading part
+//     the first 64 columns, the remainder the other 64;
+//   * eight softmax warps, two threads per query row (64 rows of the tile each), as in the prompt kernel: a lazy reference
+//     that moves only when a score exceeds it by 8, agreed through one reducing barrier that also orders the loads of S
+//     before the stores of P.
+// The tiles that hold drafted rows are masked per query; there the softmax warps also clear rows behind the sequence's end
+// and the non-finite values of drafted rows in the V' tile (a product with a zero weight would still carry them): the
+// latter are added at the end to the query rows that do see them.
+// TMEM (512 columns): S[2] (128 each), O' (128), Q' (64 + 64).  Every wait is bounded.
+#include <cuda_bf16.h>
+
+#include "internal.h"
+#include "tc_common.cuh"
+
+namespace ea {
+namespace {
+
+using namespace tc;
+
+constexpr int kKeys = 128;                    // cached rows of a tile
+constexpr int kAtom = kKeys * 128;            // one swizzled atom column of a tile: 128 rows x 64 elements
+constexpr int kBox = 64 * 128;                // bytes of one TMA box
+constexpr int kSWarp = 8, kPvWarp = 9, kLoadWarp = 10;
+constexpr int kTcThreads = 12 * 32;           // 8 softmax warps, two issuers, the loader, one spare warp
+constexpr int kMaxStages = 6;
+
+struct __align__(16) TcHeader {
+  unsigned long long kv_full[kMaxStages], kv_empty[kMaxStages];
+  unsigned long long q_full;
+  unsigned long long s_full[2], p_full[2], o_done[2];       // per S buffer
+  unsigned long long odd;                     // drafted tokens with a value that is not finite
+  uint32_t tmem_base;
+  int abort_flag;
+  float exch[2][kTile];                       // [half][row]: row maxima (main loop), row sums (epilogue)
+};
+constexpr int kHeaderBytes = 2048;
+static_assert(sizeof(TcHeader) <= kHeaderBytes, "header outgrew its area");
+
+__device__ __forceinline__ bool softmax_barrier_or(bool pred) {    // the 256 softmax threads
+  uint32_t out;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 q, %1, 0;\n\t"
+      "bar.red.or.pred p, 1, 256, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(out)
+      : "r"(pred ? 1u : 0u)
+      : "memory");
+  return out != 0;
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void split_pair(float x0, float x1, uint32_t& hi, uint32_t& lo) {
+  hi = pack_bf16(x0, x1);
+  lo = pack_bf16(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xffff0000u));
+}
+__device__ __forceinline__ bool finite16(uint32_t bits16) { return (bits16 & 0x7f80u) != 0x7f80u; }
+
+template <int KS>
+__device__ __forceinline__ void issue_s(uint32_t d, uint32_t q, uint64_t dk, uint32_t idesc) {
+#pragma unroll
+  for (int part = 0; part < 2; ++part)
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+      mma_ts(d, q + 64 * part + 8 * s, dk + (s >> 2) * (kAtom >> 4) + (s & 3) * 2, idesc, part > 0 || s > 0);
+}
+
+__global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_constant__ MqDecodeParams p, int stages, int stage_bytes) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  TcHeader* hdr = reinterpret_cast<TcHeader*>(smem);
+  unsigned char* ring = smem + kHeaderBytes;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int chunks = (p.rows + kTile - 1) / kTile;
+  const int unit = blockIdx.x / chunks, chunk = blockIdx.x - unit * chunks, split = blockIdx.y;
+  const int h = unit / p.B, b = unit - h * p.B;
+  const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
+  const int row_end = n_b + p.tail;
+  const int all = (row_end + kKeys - 1) / kKeys;
+  const int t_lo = split * p.per, t_hi = min(all, t_lo + p.per), nt = t_hi - t_lo;
+  if (nt <= 0) return;                        // a shorter sequence: nothing left (there is always a drafted row for the first piece)
+  const HeadInfo hd = p.heads[h];
+  const int rpk16 = (hd.rp_k + 15) & ~15, rpv16 = (hd.rp_v + 15) & ~15;
+  const int k_atoms = (rpk16 + 63) >> 6, v_atoms = (rpv16 + 63) >> 6, k_bytes = k_atoms * kAtom;
+  const int row0 = chunk * kTile, live = min(kTile, p.rows - row0);
+
+  if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
+  if (tid == 0) {
+    for (int s = 0; s < kMaxStages; ++s) {
+      mbar_init(&hdr->kv_full[s], 1);
+      mbar_init(&hdr->kv_empty[s], 1);
+    }
+    mbar_init(&hdr->q_full, 256);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&hdr->s_full[i], 1);
+      mbar_init(&hdr->p_full[i], 256);
+      mbar_init(&hdr->o_done[i], 1);
+    }
+    hdr->odd = 0;
+    hdr->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = hdr->tmem_base;
+  volatile int* abort_flag = &hdr->abort_flag;
+
+  if (warp == kLoadWarp) {
+    if (lane == 0) {
+      const unsigned char* maps = static_cast<const unsigned char*>(p.tmaps) + static_cast<size_t>(h) * 256;
+      tensormap_acquire(maps);
+      tensormap_acquire(maps + 128);
+      bool ok = true;
+      int issued = 0;
+      for (int i = 0; i < nt; ++i) {
+        const int st = i % stages;
+        if (i >= stages) {
+          ok = mbar_wait(&hdr->kv_empty[st], ((i / stages) - 1) & 1u, p.status) && !*abort_flag;
+          if (!ok) break;
+        }
+        unsigned char* k_tile = ring + st * stage_bytes;
+        unsigned char* v_tile = k_tile + k_bytes;
+        mbar_arrive_expect_tx(&hdr->kv_full[st], static_cast<uint32_t>((k_atoms + v_atoms) * kAtom));
+        for (int box = 0; box < 2; ++box) {
+          const int r = (t_lo + i) * kKeys + 64 * box;
+          int y = 0, z = p.B;                 // no row of the sequence here: outside the map, zeros
+          if (r < row_end) {
+            y = r; z = b;
+            if (p.pages.table != nullptr) {   // (pages lie inside one slab of the pool)
+              const int64_t at = physical_row(p.pages, b, p.n_max, r);
+              z = static_cast<int>(at / p.n_max);
+              y = static_cast<int>(at - static_cast<int64_t>(z) * p.n_max);
+            }
+          }
+          for (int a = 0; a < k_atoms; ++a) tma_load_3d(k_tile + a * kAtom + box * kBox, maps, a * 64, y, z, &hdr->kv_full[st]);
+          for (int a = 0; a < v_atoms; ++a) tma_load_3d(v_tile + a * kAtom + box * kBox, maps + 128, a * 64, y, z, &hdr->kv_full[st]);
+        }
+        ++issued;
+      }
+      if (!ok) *abort_flag = 1;
+      // copies in flight must land before the CTA leaves; normally their consumers have waited for them
+      for (int s = 0; s < stages; ++s) {
+        int last = -1;
+        for (int i = s; i < issued; i += stages) last = i;
+        if (last >= 0) mbar_wait(&hdr->kv_full[s], (last / stages) & 1u, p.status);
+      }
+    }
+  } else if (warp == kSWarp) {
+    if (lane == 0) {
+      const uint32_t idesc = instr_desc(kKeys, false);
+      const uint64_t dk0 = smem_desc_sw128(smem_u32(ring), 16, 1024);
+      bool ok = mbar_wait(&hdr->q_full, 0, p.status);
+      for (int i = 0; i < nt && ok; ++i) {
+        const int st = i % stages, buf = i & 1;
+        ok = mbar_wait(&hdr->kv_full[st], (i / stages) & 1u, p.status);
+        if (ok && i >= 2) ok = mbar_wait(&hdr->o_done[buf], ((i - 2) >> 1) & 1u, p.status);    // P(i - 2) has been read
+        ok = ok && !*abort_flag;
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t dk = dk0 + static_cast<uint64_t>(st) * (stage_bytes >> 4);
+        const uint32_t d = tmem + buf * 128, q = tmem + 384;
+        switch (rpk16 >> 4) {
+          case 1: issue_s<1>(d, q, dk, idesc); break;
+          case 2: issue_s<2>(d, q, dk, idesc); break;
+          case 3: issue_s<3>(d, q, dk, idesc); break;
+          case 4: issue_s<4>(d, q, dk, idesc); break;
+          case 5: issue_s<5>(d, q, dk, idesc); break;
+          case 6: issue_s<6>(d, q, dk, idesc); break;
+          case 7: issue_s<7>(d, q, dk, idesc); break;
+          default: issue_s<8>(d, q, dk, idesc); break;
+        }
+        mma_commit(&hdr->s_full[buf]);
+      }
+      if (!ok) *abort_flag = 1;
+    }
+  } else if (warp == kPvWarp) {
+    if (lane == 0) {
+      const uint32_t idesc = instr_desc(rpv16, true);
+      const uint64_t dv0 = smem_desc_sw128(smem_u32(ring + k_bytes), kAtom, 1024);
+      bool ok = true;
+      for (int i = 0; i < nt && ok; ++i) {
+        const int st = i % stages, buf = i & 1;
+        ok = mbar_wait(&hdr->p_full[buf], (i >> 1) & 1u, p.status) && mbar_wait(&hdr->kv_full[st], (i / stages) & 1u, p.status) &&
+             !*abort_flag;
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t dv = dv0 + static_cast<uint64_t>(st) * (stage_bytes >> 4);
+        const uint32_t pa = tmem + buf * 128;
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int s = 0; s < kKeys / 16; ++s)
+            mma_ts(tmem + 256, pa + 64 * part + 8 * s, dv + s * (2048 >> 4), idesc, i > 0 || part > 0 || s > 0);
+        mma_commit(&hdr->o_done[buf]);
+        mma_commit(&hdr->kv_empty[st]);
+      }
+      // the last commits' arrivals must have landed before the CTA may leave
+      if (ok) ok = mbar_wait(&hdr->kv_empty[(nt - 1) % stages], ((nt - 1) / stages) & 1u, p.status);
+      if (!ok) *abort_flag = 1;
+    }
+  } else if (warp < 8) {
+    // ------------------------------------------------------------------ softmax: two threads per query row
+    const int hf = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tO = tmem + lane_base + 256;
+    const int my_row = row0 + row;
+    const uint64_t* masks = p.mask + static_cast<int64_t>(b) * p.tokens;
+    uint64_t seen = 0;
+    {
+      // Q' into TMEM: half hf takes every other step of 16 channels
+      const float* src = p.qp + (static_cast<int64_t>(unit) * p.rows + my_row) * p.q_stride;
+      for (int c0 = 16 * hf; c0 < rpk16; c0 += 32) {
+        uint32_t hi[8], lo[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const int c = c0 + 2 * j;
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (row < live && c < hd.rp_k) x = __ldg(reinterpret_cast<const float4*>(src + c));
+          split_pair(x.x, x.y, hi[j], lo[j]);
+          split_pair(x.z, x.w, hi[j + 1], lo[j + 1]);
+        }
+        tmem_st8(tmem + lane_base + 384 + (c0 >> 1), hi);
+        tmem_st8(tmem + lane_base + 448 + (c0 >> 1), lo);
+      }
+      if (row < live) {
+        seen = __ldg(masks + my_row / p.group);
+        if (p.tokens < 64) seen &= (1ull << p.tokens) - 1;
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(&hdr->q_full);
+    }
+    const int o_split = ((rpv16 >> 4) + 1) / 2 * 16;         // columns of O' each half looks after
+    const int o_lo = hf ? o_split : 0, o_hi = hf ? rpv16 : o_split;
+    float m_run = -INFINITY, base = 0.f, l_run = 0.f;
+    bool ok = true;
+    // Named barriers have no time limit: every decision to leave the loop is taken through one of them.
+    for (int i = 0; i < nt; ++i) {
+      const int buf = i & 1, key0 = (t_lo + i) * kKeys + 64 * hf;
+      const uint32_t tS = tmem + lane_base + buf * 128;
+      const bool waited = mbar_wait(&hdr->s_full[buf], (i >> 1) & 1u, p.status);
+      const bool special = (t_lo + i + 1) * kKeys > n_b;
+      uint32_t r[64];
+      float cand = -INFINITY;
+      if (waited) {
+        tc_fence_after();
+        tmem_ld64(tS + 64 * hf, r);
+        tmem_wait_ld();
+        if (special) {
+          uint64_t open = key0 >= n_b ? 0 : n_b - key0 >= 64 ? ~0ull : (1ull << (n_b - key0)) - 1;
+          const int s0 = key0 - n_b;
+          if (s0 >= 0) open |= s0 < 64 ? seen >> s0 : 0;
+          else if (s0 > -64) open |= seen << -s0;
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (!((open >> c) & 1)) r[c] = 0xff800000u;      // -inf
+        }
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 64; c += 4) {
+          mx0 = max3(mx0, __uint_as_float(r[c]), __uint_as_float(r[c + 1]));
+          mx1 = max3(mx1, __uint_as_float(r[c + 2]), __uint_as_float(r[c + 3]));
+        }
+        cand = fmaxf(mx0, mx1);
+      }
+      float alpha = 1.f;
+      if (softmax_barrier_or(!waited || cand > m_run + 8.f || *abort_flag != 0)) {
+        hdr->exch[hf][row] = cand;
+        if (softmax_barrier_or(!waited || *abort_flag != 0)) {        // a wait gave up somewhere: all 256 leave here
+          ok = false;
+          break;
+        }
+        const float top = fmaxf(cand, hdr->exch[hf ^ 1][row]);         // both halves take the same decision
+        if (top > m_run + 8.f) {
+          alpha = ex2(m_run - top);
+          m_run = base = top;
+        }
+        l_run *= alpha;
+        if (i > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {          // rescale this half's columns of the row of O'
+          const bool got = mbar_wait(&hdr->o_done[buf ^ 1], ((i - 1) >> 1) & 1u, p.status);
+          if (__all_sync(0xffffffffu, got)) {
+            tc_fence_after();
+#pragma unroll 1
+            for (int c0 = o_lo; c0 < o_hi; c0 += 16) {
+              uint32_t o[16];
+              tmem_ld16(tO + c0, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+              tmem_st16(tO + c0, o);
+            }
+          } else {
+            *abort_flag = 1;                                 // seen by every softmax thread at the next barrier
+          }
+        }
+      }
+      if (special) {
+        // the V' tile: rows behind the end cleared, values of drafted rows that are not finite cleared and noted
+        const int st = i % stages;
+        const bool landed = mbar_wait(&hdr->kv_full[st], (i / stages) & 1u, p.status);         // (over already: S(i) has read the tile)
+        const int r_log = (t_lo + i) * kKeys + row;
+        if (landed && r_log >= n_b) {
+          unsigned char* v_tile = ring + st * stage_bytes + k_bytes;
+          bool odd = false;
+          for (int c = hf; c < 8 * v_atoms; c += 2) {
+            uint4* at = reinterpret_cast<uint4*>(v_tile + (c >> 3) * kAtom + sw128_off(row, c & 7));
+            uint4 v = *at;
+            uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+            bool touched = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (r_log >= row_end) { touched = touched || w[j] != 0; w[j] = 0; continue; }
+              if (!finite16(w[j])) { w[j] &= 0xffff0000u; touched = odd = true; }
+              if (!finite16(w[j] >> 16)) { w[j] &= 0x0000ffffu; touched = odd = true; }
+            }
+            if (touched) *at = v;
+          }
+          if (odd) atomicOr(&hdr->odd, 1ull << (r_log - n_b));
+        }
+        fence_async_smem();
+      }
+      // exponentials against the reference, their sum, P as two 16-bit parts over S
+      float sum0 = 0.f, sum1 = 0.f;
+      const float neg = -base;
+#pragma unroll
+      for (int q4 = 0; q4 < 2; ++q4) {
+        uint32_t hi[16], lo[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int c = 32 * q4 + 2 * j;
+          float y0, y1;
+          fma2(y0, y1, __uint_as_float(r[c]), __uint_as_float(r[c + 1]), 1.f, neg);
+          const float e0 = ex2(y0), e1 = ex2(y1);
+          add2(sum0, sum1, e0, e1);
+          split_pair(e0, e1, hi[j], lo[j]);
+        }
+        tmem_st16(tS + 32 * hf + 16 * q4, hi);
+        tmem_st16(tS + 64 + 32 * hf + 16 * q4, lo);
+      }
+      l_run += sum0 + sum1;
+      tmem_wait_st();
+      tc_fence_before();
+      mbar_arrive(&hdr->p_full[buf]);
+    }
+    if (ok) {
+      ok = mbar_wait(&hdr->o_done[(nt - 1) & 1], ((nt - 1) >> 1) & 1u, p.status);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+    }
+    if (!ok) *abort_flag = 1;
+    hdr->exch[hf][row] = l_run;                              // the two halves' sums share the reference
+    softmax_barrier_or(false);
+    const bool fine = *abort_flag == 0;
+    const uint64_t odd = hdr->odd & seen;
+    float* part = p.partials + ((static_cast<int64_t>(unit) * p.rows + my_row) * p.splits + split) * p.part_stride;
+    if (hf == 0 && row < live) {
+      part[0] = fine ? m_run : -INFINITY;
+      part[1] = fine ? l_run + hdr->exch[1][row] : 0.f;
+    }
+    for (int c0 = o_lo; c0 < o_hi; c0 += 16) {
+      uint32_t o[16];
+      tmem_ld16(tO + c0, o);
+      tmem_wait_ld();
+      if (row >= live) continue;
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) {
+        if (c0 + j >= hd.rp_v) break;
+        float4 v = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3]));
+        if (!fine) v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint64_t left = odd; left; left &= left - 1) {  // (rare) values that are not finite, of rows this query sees
+          const int64_t at = physical_row(p.pages, b, p.n_max, n_b + __ffsll(static_cast<long long>(left)) - 1);
+          const uint2 w = *reinterpret_cast<const uint2*>(p.cache + hd.v_off + (at * hd.rp_v + c0 + j) * 2);
+          if (!finite16(w.x)) v.x += __uint_as_float(w.x << 16);
+          if (!finite16(w.x >> 16)) v.y += __uint_as_float(w.x & 0xffff0000u);
+          if (!finite16(w.y)) v.z += __uint_as_float(w.y << 16);
+          if (!finite16(w.y >> 16)) v.w += __uint_as_float(w.y & 0xffff0000u);
+        }
+        *reinterpret_cast<float4*>(part + 4 + c0 + j) = v;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace
+
+// Stages of the ring for a layer's widest ranks, and the shared memory with them (0: does not fit).
+int mq_tc_stages(int max_rp_k, int max_rp_v, int* stage_bytes, size_t* smem) {
+  const int atoms = ((max_rp_k + 63) >> 6) + ((max_rp_v + 63) >> 6);
+  *stage_bytes = atoms * kAtom;
+  int stages = static_cast<int>((227 * 1024 - kHeaderBytes) / *stage_bytes);
+  if (stages > kMaxStages) stages = kMaxStages;
+  *smem = kHeaderBytes + static_cast<size_t>(stages) * *stage_bytes;
+  return stages;
+}
+
+cudaError_t launch_mq_tc(const MqDecodeParams& p, int max_rp_k, int max_rp_v, cudaStream_t s, uint64_t* launches) {
+  int stage_bytes = 0;
+  size_t smem = 0;
+  const int stages = mq_tc_stages(max_rp_k, max_rp_v, &stage_bytes, &smem);
+  static size_t configured[kMaxDevices] = {};
+  const cudaError_t e = ensure_dynamic_smem(mq_tc_kernel, smem, configured);
+  if (e != cudaSuccess) return e;
+  const int chunks = (p.rows + kTile - 1) / kTile;
+  mq_tc_kernel<<<dim3(p.B * p.H * chunks, p.splits), kTcThreads, smem, s>>>(p, stages, stage_bytes);
+  ++*launches;
+  return cudaGetLastError();
+}
+
+}  // namespace ea

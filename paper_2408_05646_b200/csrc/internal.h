@@ -306,6 +306,8 @@ struct MqDecodeParams {
   int32_t lr_v_width;       // sum of rp_v: width of a packed output row of one query head
   uint32_t flags;
   PageMap pages;
+  const void* tmaps;        // CUtensorMap[2 * H]: K' and V' slab of every head (tcgen05 kernel)
+  int* status;              // (tcgen05 kernel: its waits are bounded)
 };
 
 struct MqProjectParams {     // drafted tokens: Q' into the scratch (scaled into the base-2 domain), K', V' rows into the cache
@@ -387,6 +389,9 @@ constexpr MqShape kMqSimtShape = {8, 2, 5};
 MqShape mq_mma_shape(int rows, int max_rp);
 // 16-bit layers; max_rp: widest padded rank over heads and K/V
 cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, cudaStream_t s, uint64_t* launches);
+// tcgen05 products (tail only: a tree of drafted tokens): 128 query rows per CTA, one CTA per SM
+constexpr MqShape kMqTcShape = {128, 1, 7};
+cudaError_t launch_mq_tc(const MqDecodeParams& p, int max_rp_k, int max_rp_v, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, int max_rp_v, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_tree_commit(const TreeCommitParams& p, int sequences, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_block_bounds(const SparseParams& p, int dtype, cudaStream_t s, uint64_t* launches);

@@ -72,7 +72,7 @@ class Case:
         self.page_rows, self.table = page_rows, None
         if page_rows:
             perm = np.random.default_rng(seed).permutation(batch * n_max // page_rows)
-            per = n_max // page_rows
+            per = len(perm) // batch
             self.table = [[int(x) for x in perm[b * per:(b + 1) * per]] for b in range(batch)]
             lay.set_page_table(self.table, page_rows)
         if slopes is not None:

@@ -47,16 +47,23 @@ SHAPES = [
     (BF16, 1, 2, 3, 40, [40, 17], [24, 40], [65], 7, "any", 0),                  # d_head that is no multiple of 16
     (BF16, 3, 2, 1, 128, [80, 64], [64, 80], [500, 256, 130], 31, "tree", 128),  # pages of 128 rows, shuffled
     (BF16, 2, 1, 8, 128, [112], [96], [900, 3], 3, "any", 256),
+    (BF16, 2, 1, 2, 128, [80], [80], [6000, 5000], 20, "tree", 0),               # many tiles for one unit
+    (BF16, 1, 2, 3, 128, [64, 48], [64, 40], [1500], 60, "any", 0),              # 180 query rows, narrow heads
+    (BF16, 2, 1, 1, 128, [80], [80], [200, 100], 40, "tree", 256),               # pages that do not divide n_max (384 rows)
     (FP32, 1, 4, 1, 64, [32] * 4, [32] * 4, [512], 5, "tree", 0),
     (FP32, 2, 2, 2, 80, [33, 80], [80, 12], [100, 0], 17, "any", 0),
     (FP32, 2, 2, 1, 128, [128, 64], [128, 32], [260, 131], 64, "tree", 128),
 ]
 
 
+@pytest.mark.parametrize("impl", [0, 1])               # 0: tcgen05 products from 17 query rows on, 1: warp-level products
 @pytest.mark.parametrize("dtype,batch,H,group,d,rk,rv,lens,T,kind,page", SHAPES)
-def test_tree_matches_the_definition(B, dtype, batch, H, group, d, rk, rv, lens, T, kind, page):
-    n_max = -(-(max(lens) + T + 5) // 256) * 256
+def test_tree_matches_the_definition(B, dtype, batch, H, group, d, rk, rv, lens, T, kind, page, impl):
+    if impl == 1 and (dtype == FP32 or T * group <= 16):
+        pytest.skip("one kernel serves this case")
+    n_max = 384 if (page, T) == (256, 40) else -(-(max(lens) + T + 5) // 256) * 256
     c = Case(B, dtype, batch, H, group, d, rk, rv, lens, n_max, seed=11, page_rows=page)
+    c.lay.set_option(B.EA_OPT_TREE_IMPL, impl)
     q, k, v = drafted(c, T, 31)
     masks, _ = trees(batch, T, 7, kind)
     c.lay.tree_attach(T, group)
