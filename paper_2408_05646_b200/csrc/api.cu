@@ -1397,21 +1397,27 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
     if (splits > cap) splits = cap;
     per = (p.tiles + splits - 1) / splits;
   } else {
+    // Equal sequences: waves of equal pieces.  Unequal ones: the CTAs take what comes next, so the end is at most the
+    // average load plus one piece.
     const int64_t wave = static_cast<int64_t>(h->sm_count) * shape.ctas_per_sm;
-    int64_t best = INT64_MAX;
+    const bool ragged = h->max_deficit > 0 && p.list == nullptr;
+    constexpr int64_t kStart = 2;             // tiles' worth of a CTA's start and end
+    int64_t best = INT64_MAX, last = 0;
     for (int64_t s2 = 1; s2 <= cap && s2 <= 256; ++s2) {
       const int64_t size = (p.tiles + s2 - 1) / s2;
-      if (s2 > 1 && (p.tiles + size - 1) / size < s2) continue;        // the same pieces as with fewer
-      int64_t pieces = 0;
-      if (h->max_deficit > 0 && p.list == nullptr) {
+      if (size == last) continue;
+      last = size;
+      int64_t cost = 0;
+      if (ragged) {
+        int64_t load = 0;
         for (int b = 0; b < p.B; ++b) {
           const int64_t t = (p.n - h->deficit[b] + p.tail + tile - 1) >> shape.tile_shift;
-          pieces += t > size ? (t + size - 1) / size : 1;
+          load += t + kStart * (t > size ? (t + size - 1) / size : 1);
         }
+        cost = load * chunks / wave + size + kStart;
       } else {
-        pieces = s2 * p.B;
+        cost = ((s2 * p.B * chunks + wave - 1) / wave) * (size + kStart);
       }
-      const int64_t cost = ((pieces * chunks + wave - 1) / wave) * (size + 2);
       if (cost < best) { best = cost; per = size; }
     }
   }

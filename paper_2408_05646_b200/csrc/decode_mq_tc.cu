@@ -4,19 +4,21 @@
 // With more than 16 query rows a tile of cached rows carries more arithmetic than warp-level products deliver while it
 // streams; a tcgen05 product has 128 rows of queries.  One CTA per SM owns 128 query rows of a unit and a piece of its
 // rows, in tiles of 128:
-//   * one thread streams K' and V' tiles by TMA (64 x 64 boxes of the cache slabs' tensor maps, 128-byte swizzle) into a
-//     ring; boxes without a row of the sequence, and columns past the rank, arrive as zeros;
-//   * one thread issues S(t) = Q' K'^T, another O' += P V'.  Q' and P are A operands in TMEM, each as two 16-bit parts
-//     (leading part and remainder, 16 significant bits together), so every product is issued twice over; the result
-//     carries no more than the rounding of the output.  S has two buffers; P(t) takes the place of S(t): its leading part
-//     the first 64 columns, the remainder the other 64;
-//   * eight softmax warps, two threads per query row (64 rows of the tile each), as in the prompt kernel: a lazy reference
-//     that moves only when a score exceeds it by 8, agreed through one reducing barrier that also orders the loads of S
-//     before the stores of P.
+//   * two threads stream K' and V' tiles by TMA (64 x 64 boxes of the cache slabs' tensor maps, 128-byte swizzle), each
+//     into a ring of its own: a K' stage is free again when S(t) has read it, two products before the V' stage of the same
+//     tile (with one ring for both the issuer of S waited 1400 cycles a tile for the copies).  Boxes without a row of the sequence, and columns past the rank, arrive as zeros;
+//   * one thread issues S(t) = Q' K'^T, another O' += P V'.  Q' (in shared memory) and P (in TMEM) enter as two 16-bit
+//     parts each (leading part and remainder, 16 significant bits together), so every product is issued twice over; the
+//     result carries no more than the rounding of the output.  P(t) takes the place of S(t): its leading part the first 64
+//     columns, the remainder the other 64.  S has three buffers: S(t), its softmax, P(t) V' and S(t + 3) into the same
+//     columns are a chain of some 5900 cycles, of which two tiles at a time left the products idle a third of the time;
+//   * sixteen softmax warps, four threads per query row (32 rows of the tile each): a lazy reference that moves only when a
+//     score exceeds it by 8, agreed through one reducing barrier that also orders the loads of S before the stores of P.
+//     (Eight warps were the bound: 2600 cycles a tile against 2300 of the products.)
 // The tiles that hold drafted rows are masked per query; there the softmax warps also clear rows behind the sequence's end
 // and the non-finite values of drafted rows in the V' tile (a product with a zero weight would still carry them): the
 // latter are added at the end to the query rows that do see them.
-// TMEM (512 columns): S[2] (128 each), O' (128), Q' (64 + 64).  Every wait is bounded.
+// TMEM (512 columns): S[3] (128 each), O' (128).  Every wait is bounded.
 #include <cuda_bf16.h>
 
 #include "internal.h"
@@ -30,31 +32,34 @@ using namespace tc;
 constexpr int kKeys = 128;                    // cached rows of a tile
 constexpr int kAtom = kKeys * 128;            // one swizzled atom column of a tile: 128 rows x 64 elements
 constexpr int kBox = 64 * 128;                // bytes of one TMA box
-constexpr int kSWarp = 8, kPvWarp = 9, kLoadWarp = 10;
-constexpr int kTcThreads = 12 * 32;           // 8 softmax warps, two issuers, the loader, one spare warp
+constexpr int kParts = 4, kPart = kKeys / kParts;            // threads per query row, rows of a tile each looks after
+constexpr int kSoftmax = kParts * kTile;      // softmax threads
+constexpr int kSWarp = kSoftmax / 32, kPvWarp = kSWarp + 1, kLoadWarp = kSWarp + 2;   // ... and the last: K' tiles, V' tiles
+constexpr int kTcThreads = kSoftmax + 128;
 constexpr int kMaxStages = 6;
+constexpr int kBufs = 3;                      // S buffers
 
 struct __align__(16) TcHeader {
-  unsigned long long kv_full[kMaxStages], kv_empty[kMaxStages];
+  unsigned long long k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
   unsigned long long q_full;
-  unsigned long long s_full[2], p_full[2], o_done[2];       // per S buffer
+  unsigned long long s_full[kBufs], p_full[kBufs], o_done[kBufs];       // per S buffer
   unsigned long long odd;                     // drafted tokens with a value that is not finite
   uint32_t tmem_base;
   int abort_flag;
-  float exch[2][kTile];                       // [half][row]: row maxima (main loop), row sums (epilogue)
+  float exch[kParts][kTile];                  // row maxima (main loop), row sums (epilogue)
 };
-constexpr int kHeaderBytes = 2048;
+constexpr int kHeaderBytes = 3072;
 static_assert(sizeof(TcHeader) <= kHeaderBytes, "header outgrew its area");
 
-__device__ __forceinline__ bool softmax_barrier_or(bool pred) {    // the 256 softmax threads
+__device__ __forceinline__ bool softmax_barrier_or(bool pred) {    // the softmax threads
   uint32_t out;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.u32 q, %1, 0;\n\t"
-      "bar.red.or.pred p, 1, 256, q;\n\t"
+      "bar.red.or.pred p, 1, %2, q;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(out)
-      : "r"(pred ? 1u : 0u)
+      : "r"(pred ? 1u : 0u), "n"(kSoftmax)
       : "memory");
   return out != 0;
 }
@@ -70,18 +75,22 @@ __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t& hi, uin
 __device__ __forceinline__ bool finite16(uint32_t bits16) { return (bits16 & 0x7f80u) != 0x7f80u; }
 
 template <int KS>
-__device__ __forceinline__ void issue_s(uint32_t d, uint32_t q, uint64_t dk, uint32_t idesc) {
+__device__ __forceinline__ void issue_s(uint32_t d, uint64_t dq, uint64_t q_part, uint64_t dk, uint32_t idesc) {
 #pragma unroll
   for (int part = 0; part < 2; ++part)
 #pragma unroll
     for (int s = 0; s < KS; ++s)
-      mma_ts(d, q + 64 * part + 8 * s, dk + (s >> 2) * (kAtom >> 4) + (s & 3) * 2, idesc, part > 0 || s > 0);
+      mma_ss(d, dq + part * q_part + 16 * s, dk + (s >> 2) * (kAtom >> 4) + (s & 3) * 2, idesc, part > 0 || s > 0);
 }
 
-__global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_constant__ MqDecodeParams p, int stages, int stage_bytes) {
+struct Ring { int q_bytes, k_stages, k_stage, v_stages, v_stage; };      // shared memory behind the header
+
+__global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_constant__ MqDecodeParams p, Ring rings) {
   extern __shared__ __align__(1024) unsigned char smem[];
   TcHeader* hdr = reinterpret_cast<TcHeader*>(smem);
-  unsigned char* ring = smem + kHeaderBytes;
+  unsigned char* q_tile = smem + kHeaderBytes;               // Q': leading parts, remainders; then K' stages, V' stages
+  unsigned char* ring = q_tile + rings.q_bytes;
+  unsigned char* v_ring = ring + rings.k_stages * rings.k_stage;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int chunks = (p.rows + kTile - 1) / kTile;
   const int unit = blockIdx.x / chunks, chunk = blockIdx.x - unit * chunks, split = blockIdx.y;
@@ -93,19 +102,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
   if (nt <= 0) return;                        // a shorter sequence: nothing left (there is always a drafted row for the first piece)
   const HeadInfo hd = p.heads[h];
   const int rpk16 = (hd.rp_k + 15) & ~15, rpv16 = (hd.rp_v + 15) & ~15;
-  const int k_atoms = (rpk16 + 63) >> 6, v_atoms = (rpv16 + 63) >> 6, k_bytes = k_atoms * kAtom;
+  const int k_atoms = (rpk16 + 63) >> 6, v_atoms = (rpv16 + 63) >> 6;
   const int row0 = chunk * kTile, live = min(kTile, p.rows - row0);
 
   if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
   if (tid == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
-      mbar_init(&hdr->kv_full[s], 1);
-      mbar_init(&hdr->kv_empty[s], 1);
+      mbar_init(&hdr->k_full[s], 1);
+      mbar_init(&hdr->k_empty[s], 1);
+      mbar_init(&hdr->v_full[s], 1);
+      mbar_init(&hdr->v_empty[s], 1);
     }
-    mbar_init(&hdr->q_full, 256);
-    for (int i = 0; i < 2; ++i) {
+    mbar_init(&hdr->q_full, kSoftmax);
+    for (int i = 0; i < kBufs; ++i) {
       mbar_init(&hdr->s_full[i], 1);
-      mbar_init(&hdr->p_full[i], 256);
+      mbar_init(&hdr->p_full[i], kSoftmax);
       mbar_init(&hdr->o_done[i], 1);
     }
     hdr->odd = 0;
@@ -118,111 +129,131 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
   const uint32_t tmem = hdr->tmem_base;
   volatile int* abort_flag = &hdr->abort_flag;
 
-  if (warp == kLoadWarp) {
+  if (warp >= kLoadWarp) {
     if (lane == 0) {
-      const unsigned char* maps = static_cast<const unsigned char*>(p.tmaps) + static_cast<size_t>(h) * 256;
-      tensormap_acquire(maps);
-      tensormap_acquire(maps + 128);
+      const bool v_side = warp > kLoadWarp;
+      const unsigned char* map = static_cast<const unsigned char*>(p.tmaps) + static_cast<size_t>(h) * 256 + (v_side ? 128 : 0);
+      tensormap_acquire(map);
+      unsigned char* tiles = v_side ? v_ring : ring;
+      unsigned long long* full = v_side ? hdr->v_full : hdr->k_full;
+      unsigned long long* empty = v_side ? hdr->v_empty : hdr->k_empty;
+      const int atoms = v_side ? v_atoms : k_atoms;
+      const int stage = v_side ? rings.v_stage : rings.k_stage, stages = v_side ? rings.v_stages : rings.k_stages;
+      const bool paged = p.pages.table != nullptr;
+      const int slab_pages = paged ? p.n_max >> p.pages.shift : 1;        // (pages lie inside one slab of the pool)
+      const int32_t* table = p.pages.table + static_cast<int64_t>(b) * p.pages.width;
+      int page[2] = {0, 0};
+      auto fetch = [&](int i) {               // a tile's pages, one tile ahead of their use
+        for (int box = 0; paged && i < nt && box < 2; ++box) {
+          const int r = (t_lo + i) * kKeys + 64 * box;
+          if (r < row_end) page[box] = __ldg(table + (r >> p.pages.shift));
+        }
+      };
+      fetch(0);
       bool ok = true;
       int issued = 0;
       for (int i = 0; i < nt; ++i) {
         const int st = i % stages;
-        if (i >= stages) {
-          ok = mbar_wait(&hdr->kv_empty[st], ((i / stages) - 1) & 1u, p.status) && !*abort_flag;
-          if (!ok) break;
-        }
-        unsigned char* k_tile = ring + st * stage_bytes;
-        unsigned char* v_tile = k_tile + k_bytes;
-        mbar_arrive_expect_tx(&hdr->kv_full[st], static_cast<uint32_t>((k_atoms + v_atoms) * kAtom));
+        if (i >= stages) ok = mbar_wait(&empty[st], ((i / stages) - 1) & 1u, p.status) && !*abort_flag;
+        if (!ok) break;
+        mbar_arrive_expect_tx(&full[st], static_cast<uint32_t>(atoms * kAtom));
+#pragma unroll
         for (int box = 0; box < 2; ++box) {
           const int r = (t_lo + i) * kKeys + 64 * box;
           int y = 0, z = p.B;                 // no row of the sequence here: outside the map, zeros
           if (r < row_end) {
             y = r; z = b;
-            if (p.pages.table != nullptr) {   // (pages lie inside one slab of the pool)
-              const int64_t at = physical_row(p.pages, b, p.n_max, r);
-              z = static_cast<int>(at / p.n_max);
-              y = static_cast<int>(at - static_cast<int64_t>(z) * p.n_max);
+            if (paged) {
+              z = page[box] / slab_pages;
+              y = ((page[box] - z * slab_pages) << p.pages.shift) + (r & ((1 << p.pages.shift) - 1));
             }
           }
-          for (int a = 0; a < k_atoms; ++a) tma_load_3d(k_tile + a * kAtom + box * kBox, maps, a * 64, y, z, &hdr->kv_full[st]);
-          for (int a = 0; a < v_atoms; ++a) tma_load_3d(v_tile + a * kAtom + box * kBox, maps + 128, a * 64, y, z, &hdr->kv_full[st]);
+          for (int a = 0; a < atoms; ++a) tma_load_3d(tiles + st * stage + a * kAtom + box * kBox, map, a * 64, y, z, &full[st]);
         }
         ++issued;
+        fetch(i + 1);
       }
       if (!ok) *abort_flag = 1;
       // copies in flight must land before the CTA leaves; normally their consumers have waited for them
       for (int s = 0; s < stages; ++s) {
         int last = -1;
         for (int i = s; i < issued; i += stages) last = i;
-        if (last >= 0) mbar_wait(&hdr->kv_full[s], (last / stages) & 1u, p.status);
+        if (last >= 0) mbar_wait(&full[s], (last / stages) & 1u, p.status);
       }
     }
   } else if (warp == kSWarp) {
     if (lane == 0) {
       const uint32_t idesc = instr_desc(kKeys, false);
       const uint64_t dk0 = smem_desc_sw128(smem_u32(ring), 16, 1024);
+      const uint64_t dq = smem_desc(smem_u32(q_tile), 128, (rpk16 >> 3) << 7);      // canonical tiles of 128 rows
+      const uint64_t q_part = static_cast<uint64_t>(kTile * rpk16 * 2 >> 4);
+      const int stages = rings.k_stages;
       bool ok = mbar_wait(&hdr->q_full, 0, p.status);
       for (int i = 0; i < nt && ok; ++i) {
-        const int st = i % stages, buf = i & 1;
-        ok = mbar_wait(&hdr->kv_full[st], (i / stages) & 1u, p.status);
-        if (ok && i >= 2) ok = mbar_wait(&hdr->o_done[buf], ((i - 2) >> 1) & 1u, p.status);    // P(i - 2) has been read
+        const int st = i % stages, buf = i % kBufs;
+        ok = mbar_wait(&hdr->k_full[st], (i / stages) & 1u, p.status);
+        if (ok && i >= kBufs) ok = mbar_wait(&hdr->o_done[buf], (i / kBufs - 1) & 1u, p.status);    // P(i - 3) has been read
         ok = ok && !*abort_flag;
         if (!ok) break;
         tc_fence_after();
-        const uint64_t dk = dk0 + static_cast<uint64_t>(st) * (stage_bytes >> 4);
-        const uint32_t d = tmem + buf * 128, q = tmem + 384;
+        const uint64_t dk = dk0 + static_cast<uint64_t>(st) * (rings.k_stage >> 4);
+        const uint32_t d = tmem + buf * 128;
         switch (rpk16 >> 4) {
-          case 1: issue_s<1>(d, q, dk, idesc); break;
-          case 2: issue_s<2>(d, q, dk, idesc); break;
-          case 3: issue_s<3>(d, q, dk, idesc); break;
-          case 4: issue_s<4>(d, q, dk, idesc); break;
-          case 5: issue_s<5>(d, q, dk, idesc); break;
-          case 6: issue_s<6>(d, q, dk, idesc); break;
-          case 7: issue_s<7>(d, q, dk, idesc); break;
-          default: issue_s<8>(d, q, dk, idesc); break;
+          case 1: issue_s<1>(d, dq, q_part, dk, idesc); break;
+          case 2: issue_s<2>(d, dq, q_part, dk, idesc); break;
+          case 3: issue_s<3>(d, dq, q_part, dk, idesc); break;
+          case 4: issue_s<4>(d, dq, q_part, dk, idesc); break;
+          case 5: issue_s<5>(d, dq, q_part, dk, idesc); break;
+          case 6: issue_s<6>(d, dq, q_part, dk, idesc); break;
+          case 7: issue_s<7>(d, dq, q_part, dk, idesc); break;
+          default: issue_s<8>(d, dq, q_part, dk, idesc); break;
         }
         mma_commit(&hdr->s_full[buf]);
+        mma_commit(&hdr->k_empty[st]);
       }
+      // the last commits' arrivals must have landed before the CTA may leave
+      if (ok) ok = mbar_wait(&hdr->k_empty[(nt - 1) % stages], ((nt - 1) / stages) & 1u, p.status);
       if (!ok) *abort_flag = 1;
     }
   } else if (warp == kPvWarp) {
     if (lane == 0) {
       const uint32_t idesc = instr_desc(rpv16, true);
-      const uint64_t dv0 = smem_desc_sw128(smem_u32(ring + k_bytes), kAtom, 1024);
+      const uint64_t dv0 = smem_desc_sw128(smem_u32(v_ring), kAtom, 1024);
+      const int stages = rings.v_stages;
       bool ok = true;
       for (int i = 0; i < nt && ok; ++i) {
-        const int st = i % stages, buf = i & 1;
-        ok = mbar_wait(&hdr->p_full[buf], (i >> 1) & 1u, p.status) && mbar_wait(&hdr->kv_full[st], (i / stages) & 1u, p.status) &&
+        const int st = i % stages, buf = i % kBufs;
+        ok = mbar_wait(&hdr->p_full[buf], (i / kBufs) & 1u, p.status) && mbar_wait(&hdr->v_full[st], (i / stages) & 1u, p.status) &&
              !*abort_flag;
         if (!ok) break;
         tc_fence_after();
-        const uint64_t dv = dv0 + static_cast<uint64_t>(st) * (stage_bytes >> 4);
+        const uint64_t dv = dv0 + static_cast<uint64_t>(st) * (rings.v_stage >> 4);
         const uint32_t pa = tmem + buf * 128;
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
           for (int s = 0; s < kKeys / 16; ++s)
-            mma_ts(tmem + 256, pa + 64 * part + 8 * s, dv + s * (2048 >> 4), idesc, i > 0 || part > 0 || s > 0);
+            mma_ts(tmem + kBufs * 128, pa + 64 * part + 8 * s, dv + s * (2048 >> 4), idesc, i > 0 || part > 0 || s > 0);
         mma_commit(&hdr->o_done[buf]);
-        mma_commit(&hdr->kv_empty[st]);
+        mma_commit(&hdr->v_empty[st]);
       }
-      // the last commits' arrivals must have landed before the CTA may leave
-      if (ok) ok = mbar_wait(&hdr->kv_empty[(nt - 1) % stages], ((nt - 1) / stages) & 1u, p.status);
+      if (ok) ok = mbar_wait(&hdr->v_empty[(nt - 1) % stages], ((nt - 1) / stages) & 1u, p.status);
       if (!ok) *abort_flag = 1;
     }
-  } else if (warp < 8) {
-    // ------------------------------------------------------------------ softmax: two threads per query row
-    const int hf = warp >> 2, row = (warp & 3) * 32 + lane;
+  } else {
+    // ------------------------------------------------------------------ softmax: four threads per query row
+    const int part_id = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t tO = tmem + lane_base + 256;
+    const uint32_t tO = tmem + lane_base + kBufs * 128;
     const int my_row = row0 + row;
     const uint64_t* masks = p.mask + static_cast<int64_t>(b) * p.tokens;
     uint64_t seen = 0;
     {
-      // Q' into TMEM: half hf takes every other step of 16 channels
+      // Q' as canonical tiles, a step of 16 channels at a time
       const float* src = p.qp + (static_cast<int64_t>(unit) * p.rows + my_row) * p.q_stride;
-      for (int c0 = 16 * hf; c0 < rpk16; c0 += 32) {
+      const int group = (rpk16 >> 3) << 7;
+#pragma unroll 1
+      for (int c0 = 16 * part_id; c0 < rpk16; c0 += 16 * kParts) {
         uint32_t hi[8], lo[8];
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
@@ -232,45 +263,47 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
           split_pair(x.x, x.y, hi[j], lo[j]);
           split_pair(x.z, x.w, hi[j + 1], lo[j + 1]);
         }
-        tmem_st8(tmem + lane_base + 384 + (c0 >> 1), hi);
-        tmem_st8(tmem + lane_base + 448 + (c0 >> 1), lo);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          unsigned char* at = q_tile + chunk_off(row, (c0 >> 3) + half, group);
+          *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * half], hi[4 * half + 1], hi[4 * half + 2], hi[4 * half + 3]);
+          *reinterpret_cast<uint4*>(at + kTile * rpk16 * 2) = make_uint4(lo[4 * half], lo[4 * half + 1], lo[4 * half + 2], lo[4 * half + 3]);
+        }
       }
       if (row < live) {
         seen = __ldg(masks + my_row / p.group);
         if (p.tokens < 64) seen &= (1ull << p.tokens) - 1;
       }
-      tmem_wait_st();
-      tc_fence_before();
+      fence_async_smem();
       mbar_arrive(&hdr->q_full);
     }
-    const int o_split = ((rpv16 >> 4) + 1) / 2 * 16;         // columns of O' each half looks after
-    const int o_lo = hf ? o_split : 0, o_hi = hf ? rpv16 : o_split;
     float m_run = -INFINITY, base = 0.f, l_run = 0.f;
     bool ok = true;
     // Named barriers have no time limit: every decision to leave the loop is taken through one of them.
     for (int i = 0; i < nt; ++i) {
-      const int buf = i & 1, key0 = (t_lo + i) * kKeys + 64 * hf;
+      const int buf = i % kBufs, key0 = (t_lo + i) * kKeys + kPart * part_id;
       const uint32_t tS = tmem + lane_base + buf * 128;
-      const bool waited = mbar_wait(&hdr->s_full[buf], (i >> 1) & 1u, p.status);
+      const bool waited = mbar_wait(&hdr->s_full[buf], (i / kBufs) & 1u, p.status);
       const bool special = (t_lo + i + 1) * kKeys > n_b;
-      uint32_t r[64];
+      uint32_t r[kPart];
       float cand = -INFINITY;
       if (waited) {
         tc_fence_after();
-        tmem_ld64(tS + 64 * hf, r);
+        tmem_ld16(tS + kPart * part_id, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
+        tmem_ld16(tS + kPart * part_id + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
         tmem_wait_ld();
         if (special) {
-          uint64_t open = key0 >= n_b ? 0 : n_b - key0 >= 64 ? ~0ull : (1ull << (n_b - key0)) - 1;
-          const int s0 = key0 - n_b;
-          if (s0 >= 0) open |= s0 < 64 ? seen >> s0 : 0;
-          else if (s0 > -64) open |= seen << -s0;
+          const int s0 = key0 - n_b;                         // drafted token of the first row; cached rows lie below 0
+          uint32_t open = s0 >= 0 ? 0u : s0 <= -kPart ? ~0u : (1u << -s0) - 1;
+          if (s0 >= 0) open |= s0 < 64 ? static_cast<uint32_t>(seen >> s0) : 0u;
+          else if (s0 > -kPart) open |= static_cast<uint32_t>(seen << -s0);
 #pragma unroll
-          for (int c = 0; c < 64; ++c)
+          for (int c = 0; c < kPart; ++c)
             if (!((open >> c) & 1)) r[c] = 0xff800000u;      // -inf
         }
         float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < 64; c += 4) {
+        for (int c = 0; c < kPart; c += 4) {
           mx0 = max3(mx0, __uint_as_float(r[c]), __uint_as_float(r[c + 1]));
           mx1 = max3(mx1, __uint_as_float(r[c + 2]), __uint_as_float(r[c + 3]));
         }
@@ -278,23 +311,23 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       }
       float alpha = 1.f;
       if (softmax_barrier_or(!waited || cand > m_run + 8.f || *abort_flag != 0)) {
-        hdr->exch[hf][row] = cand;
-        if (softmax_barrier_or(!waited || *abort_flag != 0)) {        // a wait gave up somewhere: all 256 leave here
+        hdr->exch[part_id][row] = cand;
+        if (softmax_barrier_or(!waited || *abort_flag != 0)) {        // a wait gave up somewhere: all of them leave here
           ok = false;
           break;
         }
-        const float top = fmaxf(cand, hdr->exch[hf ^ 1][row]);         // both halves take the same decision
+        const float top = fmaxf(fmaxf(hdr->exch[0][row], hdr->exch[1][row]), fmaxf(hdr->exch[2][row], hdr->exch[3][row]));   // the same for all four
         if (top > m_run + 8.f) {
           alpha = ex2(m_run - top);
           m_run = base = top;
         }
         l_run *= alpha;
-        if (i > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {          // rescale this half's columns of the row of O'
-          const bool got = mbar_wait(&hdr->o_done[buf ^ 1], ((i - 1) >> 1) & 1u, p.status);
+        if (i > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {          // rescale this thread's columns of the row of O'
+          const bool got = mbar_wait(&hdr->o_done[(i - 1) % kBufs], ((i - 1) / kBufs) & 1u, p.status);
           if (__all_sync(0xffffffffu, got)) {
             tc_fence_after();
 #pragma unroll 1
-            for (int c0 = o_lo; c0 < o_hi; c0 += 16) {
+            for (int c0 = 16 * part_id; c0 < rpv16; c0 += 16 * kParts) {
               uint32_t o[16];
               tmem_ld16(tO + c0, o);
               tmem_wait_ld();
@@ -309,13 +342,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       }
       if (special) {
         // the V' tile: rows behind the end cleared, values of drafted rows that are not finite cleared and noted
-        const int st = i % stages;
-        const bool landed = mbar_wait(&hdr->kv_full[st], (i / stages) & 1u, p.status);         // (over already: S(i) has read the tile)
+        const int st = i % rings.v_stages;
+        const bool landed = mbar_wait(&hdr->v_full[st], (i / rings.v_stages) & 1u, p.status);
         const int r_log = (t_lo + i) * kKeys + row;
         if (landed && r_log >= n_b) {
-          unsigned char* v_tile = ring + st * stage_bytes + k_bytes;
+          unsigned char* v_tile = v_ring + st * rings.v_stage;
           bool odd = false;
-          for (int c = hf; c < 8 * v_atoms; c += 2) {
+#pragma unroll 1
+          for (int c = part_id; c < 8 * v_atoms; c += kParts) {
             uint4* at = reinterpret_cast<uint4*>(v_tile + (c >> 3) * kAtom + sw128_off(row, c & 7));
             uint4 v = *at;
             uint32_t* w = reinterpret_cast<uint32_t*>(&v);
@@ -336,19 +370,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       float sum0 = 0.f, sum1 = 0.f;
       const float neg = -base;
 #pragma unroll
-      for (int q4 = 0; q4 < 2; ++q4) {
-        uint32_t hi[16], lo[16];
+      for (int j0 = 0; j0 < kPart / 2; j0 += 8) {
+        uint32_t hi[8], lo[8];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int c = 32 * q4 + 2 * j;
+        for (int j = 0; j < 8; ++j) {
           float y0, y1;
-          fma2(y0, y1, __uint_as_float(r[c]), __uint_as_float(r[c + 1]), 1.f, neg);
+          fma2(y0, y1, __uint_as_float(r[2 * (j0 + j)]), __uint_as_float(r[2 * (j0 + j) + 1]), 1.f, neg);
           const float e0 = ex2(y0), e1 = ex2(y1);
           add2(sum0, sum1, e0, e1);
           split_pair(e0, e1, hi[j], lo[j]);
         }
-        tmem_st16(tS + 32 * hf + 16 * q4, hi);
-        tmem_st16(tS + 64 + 32 * hf + 16 * q4, lo);
+        tmem_st8(tS + kPart / 2 * part_id + j0, hi);
+        tmem_st8(tS + 64 + kPart / 2 * part_id + j0, lo);
       }
       l_run += sum0 + sum1;
       tmem_wait_st();
@@ -356,21 +389,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       mbar_arrive(&hdr->p_full[buf]);
     }
     if (ok) {
-      ok = mbar_wait(&hdr->o_done[(nt - 1) & 1], ((nt - 1) >> 1) & 1u, p.status);
+      ok = mbar_wait(&hdr->o_done[(nt - 1) % kBufs], ((nt - 1) / kBufs) & 1u, p.status);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
     }
     if (!ok) *abort_flag = 1;
-    hdr->exch[hf][row] = l_run;                              // the two halves' sums share the reference
+    hdr->exch[part_id][row] = l_run;                         // the four sums share the reference
     softmax_barrier_or(false);
     const bool fine = *abort_flag == 0;
     const uint64_t odd = hdr->odd & seen;
     float* part = p.partials + ((static_cast<int64_t>(unit) * p.rows + my_row) * p.splits + split) * p.part_stride;
-    if (hf == 0 && row < live) {
+    if (part_id == 0 && row < live) {
       part[0] = fine ? m_run : -INFINITY;
-      part[1] = fine ? l_run + hdr->exch[1][row] : 0.f;
+      part[1] = fine ? (hdr->exch[0][row] + hdr->exch[1][row]) + (hdr->exch[2][row] + hdr->exch[3][row]) : 0.f;
     }
-    for (int c0 = o_lo; c0 < o_hi; c0 += 16) {
+#pragma unroll 1
+    for (int c0 = 16 * part_id; c0 < rpv16; c0 += 16 * kParts) {
       uint32_t o[16];
       tmem_ld16(tO + c0, o);
       tmem_wait_ld();
@@ -399,25 +433,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
 
 }  // namespace
 
-// Stages of the ring for a layer's widest ranks, and the shared memory with them (0: does not fit).
-int mq_tc_stages(int max_rp_k, int max_rp_v, int* stage_bytes, size_t* smem) {
-  const int atoms = ((max_rp_k + 63) >> 6) + ((max_rp_v + 63) >> 6);
-  *stage_bytes = atoms * kAtom;
-  int stages = static_cast<int>((227 * 1024 - kHeaderBytes) / *stage_bytes);
-  if (stages > kMaxStages) stages = kMaxStages;
-  *smem = kHeaderBytes + static_cast<size_t>(stages) * *stage_bytes;
-  return stages;
-}
-
 cudaError_t launch_mq_tc(const MqDecodeParams& p, int max_rp_k, int max_rp_v, cudaStream_t s, uint64_t* launches) {
-  int stage_bytes = 0;
-  size_t smem = 0;
-  const int stages = mq_tc_stages(max_rp_k, max_rp_v, &stage_bytes, &smem);
+  // three K' stages and two V' stages always fit (Q' 64 KB and 16 KB atoms at full rank); narrower ranks have more
+  Ring r{2 * kTile * ((max_rp_k + 15) & ~15) * 2, 3, ((max_rp_k + 63) >> 6) * kAtom, 2, ((max_rp_v + 63) >> 6) * kAtom};
+  const int room = 227 * 1024 - kHeaderBytes - r.q_bytes;
+  for (bool more = true; more;) {
+    more = false;
+    if (r.v_stages < r.k_stages && r.k_stages * r.k_stage + (r.v_stages + 1) * r.v_stage <= room) { ++r.v_stages; more = true; }
+    else if (r.k_stages < kMaxStages && (r.k_stages + 1) * r.k_stage + r.v_stages * r.v_stage <= room) { ++r.k_stages; more = true; }
+  }
+  const size_t smem = kHeaderBytes + r.q_bytes + static_cast<size_t>(r.k_stages) * r.k_stage + static_cast<size_t>(r.v_stages) * r.v_stage;
   static size_t configured[kMaxDevices] = {};
   const cudaError_t e = ensure_dynamic_smem(mq_tc_kernel, smem, configured);
   if (e != cudaSuccess) return e;
   const int chunks = (p.rows + kTile - 1) / kTile;
-  mq_tc_kernel<<<dim3(p.B * p.H * chunks, p.splits), kTcThreads, smem, s>>>(p, stages, stage_bytes);
+  mq_tc_kernel<<<dim3(p.B * p.H * chunks, p.splits), kTcThreads, smem, s>>>(p, r);
   ++*launches;
   return cudaGetLastError();
 }
