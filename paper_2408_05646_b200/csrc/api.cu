@@ -333,7 +333,7 @@ ea_status check_quant_args(eigen_attn_t h, const char* who, int32_t bits, int32_
 }
 
 constexpr int kMaxGroup = 16;
-constexpr size_t kMqSlots = 16384;       // partials that every scratch holds at least, so that few query rows can be split
+constexpr size_t kMqSlots = 65536;       // partials that every scratch holds at least, so that query rows can be split
 
 size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t* slots) {
   const size_t units = static_cast<size_t>(h->desc.batch) * h->desc.n_heads;
@@ -1401,7 +1401,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
     // average load plus one piece.
     const int64_t wave = static_cast<int64_t>(h->sm_count) * shape.ctas_per_sm;
     const bool ragged = h->max_deficit > 0 && p.list == nullptr;
-    constexpr int64_t kStart = 2;             // tiles' worth of a CTA's start and end
+    const int64_t kStart = tc ? 5 : 2;        // tiles' worth of a CTA's start and end (measured: 5 to 6 with tcgen05)
     int64_t best = INT64_MAX, last = 0;
     for (int64_t s2 = 1; s2 <= cap && s2 <= 256; ++s2) {
       const int64_t size = (p.tiles + s2 - 1) / s2;

@@ -105,6 +105,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
   const int k_atoms = (rpk16 + 63) >> 6, v_atoms = (rpv16 + 63) >> 6;
   const int row0 = chunk * kTile, live = min(kTile, p.rows - row0);
 
+  // The softmax threads' share of Q' (steps of 16 channels part_id and part_id + 4) is on its way while the block sets up.
+  float4 q_pre[2][4];
+  if (warp < kSWarp) {
+    const int r = row0 + (warp & 3) * 32 + lane;
+    const float* src = p.qp + (static_cast<int64_t>(unit) * p.rows + r) * p.q_stride;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = 16 * ((warp >> 2) + kParts * k) + 4 * j;
+        q_pre[k][j] = r < p.rows && c < hd.rp_k ? __ldg(reinterpret_cast<const float4*>(src + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+  }
   if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
   if (tid == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
@@ -250,24 +263,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
     uint64_t seen = 0;
     {
       // Q' as canonical tiles, a step of 16 channels at a time
-      const float* src = p.qp + (static_cast<int64_t>(unit) * p.rows + my_row) * p.q_stride;
       const int group = (rpk16 >> 3) << 7;
-#pragma unroll 1
-      for (int c0 = 16 * part_id; c0 < rpk16; c0 += 16 * kParts) {
-        uint32_t hi[8], lo[8];
 #pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-          const int c = c0 + 2 * j;
-          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (row < live && c < hd.rp_k) x = __ldg(reinterpret_cast<const float4*>(src + c));
-          split_pair(x.x, x.y, hi[j], lo[j]);
-          split_pair(x.z, x.w, hi[j + 1], lo[j + 1]);
-        }
+      for (int k = 0; k < 2; ++k) {
+        const int c0 = 16 * (part_id + kParts * k);
+        if (c0 >= rpk16) break;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
+          const float4 x = q_pre[k][2 * half], y = q_pre[k][2 * half + 1];
+          uint4 hi, lo;
+          split_pair(x.x, x.y, hi.x, lo.x);
+          split_pair(x.z, x.w, hi.y, lo.y);
+          split_pair(y.x, y.y, hi.z, lo.z);
+          split_pair(y.z, y.w, hi.w, lo.w);
           unsigned char* at = q_tile + chunk_off(row, (c0 >> 3) + half, group);
-          *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * half], hi[4 * half + 1], hi[4 * half + 2], hi[4 * half + 3]);
-          *reinterpret_cast<uint4*>(at + kTile * rpk16 * 2) = make_uint4(lo[4 * half], lo[4 * half + 1], lo[4 * half + 2], lo[4 * half + 3]);
+          *reinterpret_cast<uint4*>(at) = hi;
+          *reinterpret_cast<uint4*>(at + kTile * rpk16 * 2) = lo;
         }
       }
       if (row < live) {
@@ -403,12 +414,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       part[0] = fine ? m_run : -INFINITY;
       part[1] = fine ? (hdr->exch[0][row] + hdr->exch[1][row]) + (hdr->exch[2][row] + hdr->exch[3][row]) : 0.f;
     }
-#pragma unroll 1
-    for (int c0 = 16 * part_id; c0 < rpv16; c0 += 16 * kParts) {
-      uint32_t o[16];
-      tmem_ld16(tO + c0, o);
-      tmem_wait_ld();
-      if (row >= live) continue;
+    uint32_t o_all[2][16];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (16 * (part_id + kParts * k) < rpv16) tmem_ld16(tO + 16 * (part_id + kParts * k), o_all[k]);
+    tmem_wait_ld();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int c0 = 16 * (part_id + kParts * k);
+      const uint32_t (&o)[16] = o_all[k];
+      if (row >= live || c0 >= hd.rp_v) break;
 #pragma unroll
       for (int j = 0; j < 16; j += 4) {
         if (c0 + j >= hd.rp_v) break;
