@@ -44,12 +44,18 @@ __global__ void __launch_bounds__(256) block_bounds_kernel(const SparseParams p)
   if (blk >= p.block1 || blk >= (n_b >> p.block_shift)) return;     // complete blocks only
   const int64_t row0 = physical_row(p.pages, b, p.n_max, blk << p.block_shift);
   const uint4* src = reinterpret_cast<const uint4*>(p.cache + hd.k_off) + row0 * nc + c;
-  uint4 lo = __ldg(src), hi = lo;
-#pragma unroll 8
-  for (int r = 1; r < G; ++r) {
-    const uint4 x = __ldg(src + static_cast<int64_t>(r) * nc);
-    lo.x = Vec<T>::mn(lo.x, x.x); lo.y = Vec<T>::mn(lo.y, x.y); lo.z = Vec<T>::mn(lo.z, x.z); lo.w = Vec<T>::mn(lo.w, x.w);
-    hi.x = Vec<T>::mx(hi.x, x.x); hi.y = Vec<T>::mx(hi.y, x.y); hi.z = Vec<T>::mx(hi.z, x.z); hi.w = Vec<T>::mx(hi.w, x.w);
+  uint4 lo, hi;
+  constexpr int kAhead = 16;                 // loads of a thread under way together (the shortest block)
+  for (int r0 = 0; r0 < G; r0 += kAhead) {
+    uint4 x[kAhead];
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) x[r] = __ldg(src + static_cast<int64_t>(r0 + r) * nc);
+    if (r0 == 0) lo = hi = x[0];
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      lo.x = Vec<T>::mn(lo.x, x[r].x); lo.y = Vec<T>::mn(lo.y, x[r].y); lo.z = Vec<T>::mn(lo.z, x[r].z); lo.w = Vec<T>::mn(lo.w, x[r].w);
+      hi.x = Vec<T>::mx(hi.x, x[r].x); hi.y = Vec<T>::mx(hi.y, x[r].y); hi.z = Vec<T>::mx(hi.z, x[r].z); hi.w = Vec<T>::mx(hi.w, x[r].w);
+    }
   }
   uint4* dst = reinterpret_cast<uint4*>(p.bounds + p.slab[h]) + physical_block(p, b, blk) * 2 * nc + c;
   dst[0] = lo;
@@ -61,91 +67,111 @@ __global__ void __launch_bounds__(256) block_bounds_kernel(const SparseParams p)
 __device__ __forceinline__ double tiny_high(uint32_t w) { return __hiloint2double((static_cast<int>(w) >> 3) & 0x8fffe000, 0); }
 __device__ __forceinline__ double tiny_low(uint32_t w) { return __hiloint2double((static_cast<int>(w << 16) >> 3) & 0x8fffffff, 0); }
 
-// 16 bytes of lo and hi (eight 16-bit channels, or four of 32 bits) against the same channels of GQ queries: a channel
-// contributes q hi where q > 0 and q lo where q < 0.  Even and odd channels have sums of their own.
-__device__ __forceinline__ bool negative(double x) { return __double2hiint(x) < 0; }
-template <int GQ>
-__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, int q_stride, double (&acc)[2 * GQ], __nv_bfloat16) {
-  const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
+// 16 bytes of lo and hi (eight 16-bit channels, or four of 32 bits) against the same channels of a query: a channel
+// contributes q hi where q > 0 and q lo where q < 0.  `neg` has ones in the place of the channels whose q is negative.
+// Even and odd channels have sums of their own.
+__device__ __forceinline__ uint32_t pick(uint32_t neg, uint32_t lo, uint32_t hi) { return (lo & neg) | (hi & ~neg); }
+__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const uint4& neg, const double* q, double (&acc)[2], __nv_bfloat16) {
+  const uint32_t w[4] = {pick(neg.x, lo.x, hi.x), pick(neg.y, lo.y, hi.y), pick(neg.z, lo.z, hi.z), pick(neg.w, lo.w, hi.w)};
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int g = 0; g < GQ; ++g) {
-      const double2 x = *reinterpret_cast<const double2*>(q + g * q_stride + 2 * i);
-      acc[2 * g] = fma(x.x, tiny_low(negative(x.x) ? l[i] : u[i]), acc[2 * g]);
-      acc[2 * g + 1] = fma(x.y, tiny_high(negative(x.y) ? l[i] : u[i]), acc[2 * g + 1]);
-    }
+  for (int i = 0; i < 4; ++i) {
+    const double2 x = *reinterpret_cast<const double2*>(q + 2 * i);
+    acc[0] = fma(x.x, tiny_low(w[i]), acc[0]);
+    acc[1] = fma(x.y, tiny_high(w[i]), acc[1]);
+  }
 }
-template <int GQ>
-__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const double* q, int q_stride, double (&acc)[2 * GQ], float) {
-  const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
+__device__ __forceinline__ void add_bounds(const uint4& lo, const uint4& hi, const uint4& neg, const double* q, double (&acc)[2], float) {
+  const uint32_t w[4] = {pick(neg.x, lo.x, hi.x), pick(neg.y, lo.y, hi.y), pick(neg.z, lo.z, hi.z), pick(neg.w, lo.w, hi.w)};
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int g = 0; g < GQ; ++g) {
-      const double x = q[g * q_stride + i];
-      acc[2 * g + (i & 1)] = fma(x, static_cast<double>(__uint_as_float(negative(x) ? l[i] : u[i])), acc[2 * g + (i & 1)]);
-    }
+  for (int i = 0; i < 4; i += 2) {
+    const double2 x = *reinterpret_cast<const double2*>(q + i);
+    acc[0] = fma(x.x, static_cast<double>(__uint_as_float(w[i])), acc[0]);
+    acc[1] = fma(x.y, static_cast<double>(__uint_as_float(w[i + 1])), acc[1]);
+  }
 }
 template <typename T> __device__ __forceinline__ double query_factor();
 template <> __device__ __forceinline__ double query_factor<__nv_bfloat16>() { return __hiloint2double((1023 + 896) << 20, 0); }   // 2^896
 template <> __device__ __forceinline__ double query_factor<float>() { return 1.0; }
 
-// A CTA takes 128 blocks of a unit: their bounds come in by coalesced 16-byte copies (in shared memory a block's bounds sit
-// at an odd multiple of 16 bytes, so that 128 threads read one each without bank conflicts), then one thread scores one
-// block for the group's queries, GQ at a time.
-constexpr int kScoreBlocks = 128;
-template <typename T, int GQ>
-__global__ void __launch_bounds__(kScoreBlocks) block_scores_kernel(const SparseParams p) {
+// A CTA takes a run of blocks of a unit, 64 at a time: the bounds of the next 64 come in by coalesced 16-byte copies while
+// two threads score a block, half of its channels each (in shared memory a block's bounds sit at an odd multiple of 16 bytes,
+// so that the threads' reads meet all banks).
+constexpr int kScoreBlocks = 64, kScoreThreads = 2 * kScoreBlocks;
+template <typename T>
+__global__ void __launch_bounds__(kScoreThreads) block_scores_kernel(const SparseParams p, int max_steps) {
   extern __shared__ __align__(16) unsigned char sm[];
-  __shared__ int64_t phys[kScoreBlocks];
   const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B, tid = threadIdx.x;
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
   const int have = (n_b + (1 << p.block_shift) - 1) >> p.block_shift;
-  const int first = p.sink + blockIdx.y * kScoreBlocks, last = have - p.recent;
+  const int first = p.sink + blockIdx.y * kScoreBlocks * max_steps, last = min(have - p.recent, first + kScoreBlocks * max_steps);
   if (have <= p.list_len || first >= last) return;           // nothing to choose
-  const HeadInfo hd = p.heads[h];
+  const HeadInfo& hd = p.heads[h];
+  const int rp_k = hd.rp_k;
   constexpr int kPer = 16 / sizeof(T);       // channels of a 16-byte piece
-  const int nc = hd.rp_k / kPer, pitch = (2 * nc + 1) * 16;
-  const int groups = (p.group + GQ - 1) / GQ * GQ;
-  double* qs = reinterpret_cast<double*>(sm);                // [groups][rp_k]
-  unsigned char* bounds = sm + sizeof(double) * groups * hd.rp_k;
-  const int blk = first + tid;
-  phys[tid] = blk < last ? physical_block(p, b, blk) : -1;
-  __syncthreads();
+  const int nc = rp_k / kPer, per = 2 * nc, pitch = (per + 1) * 16;
+  double* qs = reinterpret_cast<double*>(sm);                // [group][rp_k]
+  T* neg = reinterpret_cast<T*>(qs + p.group * rp_k);        // [group][rp_k]: all ones where q is negative
+  unsigned char* ring = reinterpret_cast<unsigned char*>(neg + p.group * rp_k);    // [2][64][pitch]
   const char* slab = p.bounds + p.slab[h];
-  const int per = 2 * nc;
-  for (int i = tid; i < kScoreBlocks * per; i += kScoreBlocks) {
-    const int j = i / per, c = i - j * per;
-    const int64_t at = phys[j];
-    if (at >= 0) tc::cp_async16(bounds + j * pitch + c * 16, slab + (at * per + c) * 16, 16);
-  }
-  tc::cp_async_commit();
-  for (int i = tid; i < groups * hd.rp_k; i += kScoreBlocks) {
-    const int g = i / hd.rp_k, c = i - g * hd.rp_k;
-    qs[i] = g < p.group ? p.q64[(static_cast<int64_t>(unit) * p.group + g) * p.q_stride + c] * query_factor<T>() : 0.0;
-  }
-  tc::cp_async_wait<0>();
-  __syncthreads();
-  if (blk >= last) return;
-  const uint4* lo = reinterpret_cast<const uint4*>(bounds + tid * pitch);
-  double best = 0;
-  for (int g0 = 0; g0 < p.group; g0 += GQ) {
-    double acc[2 * GQ];                      // even and odd channels
-#pragma unroll
-    for (int g = 0; g < 2 * GQ; ++g) acc[g] = 0;
-#pragma unroll 2
-    for (int c = 0; c < nc; ++c) add_bounds<GQ>(lo[c], lo[nc + c], qs + g0 * hd.rp_k + c * kPer, hd.rp_k, acc, T());
-#pragma unroll
-    for (int g = 0; g < GQ; ++g) {
-      const double s = acc[2 * g] + acc[2 * g + 1];
-      if (g0 + g < p.group && (g0 + g == 0 || s > best)) best = s;
+  const int steps = (last - first + kScoreBlocks - 1) / kScoreBlocks;
+  // piece c of block j, stepped through in place of a division per piece
+  const int j_first = tid / per, c_first = tid % per, j_step = kScoreThreads / per, c_step = kScoreThreads % per;
+  const bool paged = p.pages.table != nullptr;
+  auto load = [&](int step) {
+    const int blk0 = first + step * kScoreBlocks, count = min(kScoreBlocks, last - blk0);
+    unsigned char* dst = ring + (step & 1) * kScoreBlocks * pitch + j_first * pitch + c_first * 16;
+    const char* src = slab + (static_cast<int64_t>(b) * p.seq_blocks + blk0) * per * 16 + tid * 16;
+    int j = j_first, c = c_first;
+    while (j < count) {
+      tc::cp_async16(dst, paged ? slab + (physical_block(p, b, blk0 + j) * per + c) * 16 : src, 16);
+      src += kScoreThreads * 16;
+      dst += j_step * pitch + c_step * 16;
+      j += j_step;
+      c += c_step;
+      if (c >= per) { c -= per; ++j; dst += pitch - per * 16; }
     }
+    tc::cp_async_commit();
+  };
+  load(0);
+  for (int i = tid; i < p.group * rp_k; i += kScoreThreads) {
+    const int g = i / rp_k, c = i - g * rp_k;
+    const double x = p.q64[(static_cast<int64_t>(unit) * p.group + g) * p.q_stride + c];
+    qs[i] = x * query_factor<T>();
+    if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(neg)[i] = x < 0 ? 0xffffu : 0u;
+    else reinterpret_cast<uint32_t*>(neg)[i] = x < 0 ? 0xffffffffu : 0u;
   }
-  // the position bias of the block's last row, the one it takes least from
-  if (hd.alibi_slope != 0.f)
-    best -= static_cast<double>(hd.alibi_slope) * (n_b - 1 - (((blk + 1) << p.block_shift) - 1));
-  p.scores[static_cast<int64_t>(unit) * p.score_stride + blk] = best;
+  const int mine = tid >> 1, half = tid & 1;
+  const int c_lo = half ? nc / 2 : 0, c_hi = half ? nc : nc / 2;
+  for (int step = 0; step < steps; ++step) {
+    if (step + 1 < steps) {
+      load(step + 1);
+      tc::cp_async_wait<1>();
+    } else {
+      tc::cp_async_wait<0>();
+    }
+    __syncthreads();
+    const int blk = first + step * kScoreBlocks + mine;
+    const uint4* lo = reinterpret_cast<const uint4*>(ring + ((step & 1) * kScoreBlocks + mine) * pitch);
+    double best = 0;
+    for (int g = 0; g < p.group; ++g) {
+      double acc[2] = {0, 0};                // even and odd channels
+      if (blk < last) {
+        const double* q = qs + g * rp_k;
+        const uint4* n4 = reinterpret_cast<const uint4*>(neg + g * rp_k);
+#pragma unroll 5
+        for (int c = c_lo; c < c_hi; ++c) add_bounds(lo[c], lo[nc + c], n4[c], q + c * kPer, acc, T());
+      }
+      const double part = acc[0] + acc[1];
+      const double other = __shfl_xor_sync(kFull, part, 1);
+      const double s = half ? other + part : part + other;                   // the same for both threads
+      if (g == 0 || s > best) best = s;
+    }
+    // the position bias of the block's last row, the one it takes least from
+    if (hd.alibi_slope != 0.f)
+      best -= static_cast<double>(hd.alibi_slope) * (n_b - 1 - (((blk + 1) << p.block_shift) - 1));
+    if (!half && blk < last) p.scores[static_cast<int64_t>(unit) * p.score_stride + blk] = best;
+    __syncthreads();
+  }
 }
 
 // Doubles as integers in the same order (a zero of either sign is one number).
@@ -158,10 +184,10 @@ __device__ __forceinline__ uint64_t order_key(double x) {
 // blocks in ascending order (sorted lists read the cache front to back, and equal scores go to the lower block).  Keys are
 // taken relative to the lowest one and digits start at the highest bit of the range: scores share their leading bits, and
 // counting those would send every key to one counter.
-constexpr int kSelThreads = 256, kDigit = 11, kBins = 1 << kDigit, kKeep = 4;
+constexpr int kSelThreads = 256, kDigit = 11, kBins = 1 << kDigit, kKeep = 4, kSegment = kSelThreads * kKeep;
 __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseParams p) {
   __shared__ int hist[kBins];
-  __shared__ int warp_sum[8], warp_sum2[8];
+  __shared__ int warp_sum[kSelThreads / 32];
   __shared__ int s_digit, s_above, s_count;
   __shared__ uint64_t s_low[kSelThreads / 32], s_high[kSelThreads / 32];
   const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B;
@@ -186,24 +212,36 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseP
   if (want == 0) return;
   const double* scores = p.scores + static_cast<int64_t>(unit) * p.score_stride;
 
-  // the first kKeep keys of a thread stay in its registers, the rest (long sequences of short blocks) are read again
+  // Segments of 1024 keys, four neighbours per thread; those of the first segment stay in registers, later ones (long
+  // sequences of short blocks) are read again.
+  const int count = last - first, segments = (count + kSegment - 1) / kSegment;
   uint64_t keep[kKeep];
+  auto read = [&](int segment, uint64_t (&k)[kKeep]) {
 #pragma unroll
-  for (int j = 0; j < kKeep; ++j) {
-    const int i = first + j * kSelThreads + tid;
-    keep[j] = i < last ? order_key(scores[i]) : 0;
-  }
-  auto key = [&](int j) { return order_key(scores[first + j * kSelThreads + tid]); };
-  const int mine_n = (last - first - tid + kSelThreads - 1) / kSelThreads;        // keys of this thread
+    for (int j = 0; j < kKeep; ++j) {
+      const int i = segment * kSegment + tid * kKeep + j;
+      k[j] = i < count ? order_key(scores[first + i]) : 0;
+    }
+  };
+  // f(key) for every key of this thread
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j)
+      if (tid * kKeep + j < count) f(keep[j]);
+    for (int s = 1; s < segments; ++s) {
+      uint64_t k[kKeep];
+      read(s, k);
+#pragma unroll
+      for (int j = 0; j < kKeep; ++j)
+        if (s * kSegment + tid * kKeep + j < count) f(k[j]);
+    }
+  };
+  read(0, keep);
   uint64_t lowest = ~0ull, highest = 0;
-  auto extend = [&](uint64_t k) {
+  each([&](uint64_t k) {
     lowest = k < lowest ? k : lowest;
     highest = k > highest ? k : highest;
-  };
-#pragma unroll
-  for (int j = 0; j < kKeep; ++j)
-    if (j < mine_n) extend(keep[j]);
-  for (int j = kKeep; j < mine_n; ++j) extend(key(j));
+  });
 #pragma unroll
   for (int d = 16; d; d >>= 1) {
     const uint64_t a = __shfl_xor_sync(kFull, lowest, d), c = __shfl_xor_sync(kFull, highest, d);
@@ -229,14 +267,10 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseP
       __syncthreads();
     }
     again = true;
-    auto count = [&](uint64_t absolute) {
+    each([&](uint64_t absolute) {
       const uint64_t k = absolute - lowest;
       if (shift >= 64 || (k >> shift) == prefix) atomicAdd(&hist[(k >> next) & ((1 << bits) - 1)], 1);
-    };
-#pragma unroll
-    for (int j = 0; j < kKeep; ++j)
-      if (j < mine_n) count(keep[j]);
-    for (int j = kKeep; j < mine_n; ++j) count(key(j));
+    });
     __syncthreads();
     // counts from the highest digit down: thread i holds the bins 2047 - 8i .. 2040 - 8i
     int mine[8], sum = 0;
@@ -270,33 +304,50 @@ __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseP
   }
   // keys with (key >> shift) above the prefix are in; of those equal to it the first `need`
   int done = 0, ties = 0;
-  auto emit = [&](int i, uint64_t absolute) {
-    const uint64_t k = (absolute - lowest) >> shift;
-    const bool eq = i < last && k == prefix, gt = i < last && k > prefix;
-    const unsigned beq = __ballot_sync(kFull, eq), bgt = __ballot_sync(kFull, gt);
-    if (lane == 0) { warp_sum[warp] = __popc(beq); warp_sum2[warp] = __popc(bgt); }
-    __syncthreads();
-    int e0 = ties, g0 = 0, e_all = 0, g_all = 0;
+  for (int seg = 0; seg < segments; ++seg) {
+    uint64_t k[kKeep];
+    if (seg == 0) {
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      if (w < warp) { e0 += warp_sum[w]; g0 += warp_sum2[w]; }
-      e_all += warp_sum[w];
-      g_all += warp_sum2[w];
+      for (int j = 0; j < kKeep; ++j) k[j] = keep[j];
+    } else {
+      read(seg, k);
     }
-    const unsigned below = (1u << lane) - 1;
-    const int my_e = e0 + __popc(beq & below);               // ties before this block, in the whole range
-    const int taken_e = min(my_e, need) - min(ties, need);   // of them chosen, within this round
-    if (gt || (eq && my_e < need)) put(p.sink + done + g0 + __popc(bgt & below) + taken_e, i);
-    done += g_all + min(ties + e_all, need) - min(ties, need);
-    ties += e_all;
-    __syncthreads();
-  };
-  __syncthreads();
-  const int rounds = (last - first + kSelThreads - 1) / kSelThreads;
+    int eq = 0, gt = 0;                      // of this thread
+    bool is_eq[kKeep], is_gt[kKeep];
 #pragma unroll
-  for (int j = 0; j < kKeep; ++j)
-    if (j < rounds) emit(first + j * kSelThreads + tid, keep[j]);
-  for (int j = kKeep; j < rounds; ++j) emit(first + j * kSelThreads + tid, j < mine_n ? key(j) : 0);
+    for (int j = 0; j < kKeep; ++j) {
+      const bool there = seg * kSegment + tid * kKeep + j < count;
+      const uint64_t d = (k[j] - lowest) >> shift;
+      is_eq[j] = there && d == prefix;
+      is_gt[j] = there && d > prefix;
+      eq += is_eq[j];
+      gt += is_gt[j];
+    }
+    int scan = eq << 16 | gt;                // both counts of a segment fit 16 bits
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(kFull, scan, d);
+      if (lane >= d) scan += y;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sum[warp] = scan;
+    __syncthreads();
+    int before = scan - (eq << 16 | gt), total = 0;
+#pragma unroll
+    for (int w = 0; w < kSelThreads / 32; ++w) {
+      if (w < warp) before += warp_sum[w];
+      total += warp_sum[w];
+    }
+    int e = ties + (before >> 16);           // ties before the thread's first key, in the whole range
+    int at = p.sink + done + (before & 0xffff) + min(e, need) - min(ties, need);
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j) {
+      if (is_gt[j] || (is_eq[j] && e < need)) put(at++, first + seg * kSegment + tid * kKeep + j);
+      e += is_eq[j];
+    }
+    done += (total & 0xffff) + min(ties + (total >> 16), need) - min(ties, need);
+    ties += total >> 16;
+  }
 }
 
 }  // namespace
@@ -311,22 +362,25 @@ cudaError_t launch_block_bounds(const SparseParams& p, int dtype, cudaStream_t s
   return cudaGetLastError();
 }
 
-template <typename T, int GQ>
+template <typename T>
 static cudaError_t launch_scores_t(const SparseParams& p, int max_rp_k, cudaStream_t s) {
-  const int groups = (p.group + GQ - 1) / GQ * GQ;
-  const size_t smem = sizeof(double) * groups * max_rp_k + static_cast<size_t>(kScoreBlocks) * (2 * max_rp_k * sizeof(T) + 16);
+  const size_t smem = (sizeof(double) + sizeof(T)) * p.group * max_rp_k +
+                      2 * static_cast<size_t>(kScoreBlocks) * (2 * max_rp_k * sizeof(T) + 16);
   static size_t configured[kMaxDevices] = {};
-  const cudaError_t e = ensure_dynamic_smem(block_scores_kernel<T, GQ>, smem, configured);
+  const cudaError_t e = ensure_dynamic_smem(block_scores_kernel<T>, smem, configured);
   if (e != cudaSuccess) return e;
-  const int middle = p.max_blocks - p.sink - p.recent;
-  block_scores_kernel<T, GQ><<<dim3(p.B * p.H, (middle + kScoreBlocks - 1) / kScoreBlocks), kScoreBlocks, smem, s>>>(p);
+  // runs of up to eight steps, as long as there are CTAs for five on every SM
+  const int64_t chunks = (p.max_blocks - p.sink - p.recent + kScoreBlocks - 1) / kScoreBlocks, units = static_cast<int64_t>(p.B) * p.H;
+  int64_t steps = units * chunks / (5 * 148);
+  steps = steps < 1 ? 1 : steps > 8 ? 8 : steps;
+  block_scores_kernel<T><<<dim3(static_cast<unsigned>(units), static_cast<unsigned>((chunks + steps - 1) / steps)), kScoreThreads, smem, s>>>(
+      p, static_cast<int>(steps));
   return cudaGetLastError();
 }
 
 cudaError_t launch_block_scores(const SparseParams& p, int dtype, int max_rp_k, cudaStream_t s, uint64_t* launches) {
   ++*launches;
-  if (p.group == 1) return dtype == 0 ? launch_scores_t<__nv_bfloat16, 1>(p, max_rp_k, s) : launch_scores_t<float, 1>(p, max_rp_k, s);
-  return dtype == 0 ? launch_scores_t<__nv_bfloat16, 4>(p, max_rp_k, s) : launch_scores_t<float, 4>(p, max_rp_k, s);
+  return dtype == 0 ? launch_scores_t<__nv_bfloat16>(p, max_rp_k, s) : launch_scores_t<float>(p, max_rp_k, s);
 }
 
 cudaError_t launch_block_select(const SparseParams& p, cudaStream_t s, uint64_t* launches) {

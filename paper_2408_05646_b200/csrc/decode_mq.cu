@@ -259,55 +259,54 @@ __global__ void __launch_bounds__(128) mq_copy_query_kernel(const MqQueryParams 
 
 // Q' of one token in 64 bits, for the block scores (and rounded once for the attention): products of a 16-bit and a 32-bit
 // number are exact there, so the order of the sum moves a score by 1e-16 of its terms, far below any two scores that are
-// not equal.  One CTA per unit: threads (column, share of d_head), four query heads of the group at a time; the shares are
+// not equal.  One CTA per four rows (sequences and query heads) of a head: threads (column, share of d_head); the shares are
 // added in a fixed order.
-constexpr int kQ64Threads = 256, kQ64Rows = 4;
+constexpr int kQ64Threads = 512, kQ64Rows = 4, kQ64Ahead = 16;
 template <typename T>
 __global__ void __launch_bounds__(kQ64Threads) mq_query64_kernel(const MqQueryParams p) {
   __shared__ double x[kQ64Rows][128];
   __shared__ double part[kQ64Threads][kQ64Rows];
-  const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B, tid = threadIdx.x;
-  const HeadInfo hd = p.heads[h];
-  const T* q = static_cast<const T*>(p.q) + b * p.q_stride_b + static_cast<int64_t>(h) * p.group * p.d_head;
-  const int shares = kQ64Threads / hd.rp_k;                  // at least two
-  const int share = tid / hd.rp_k, c = tid - share * hd.rp_k;
+  const int h = blockIdx.x, tid = threadIdx.x;
+  const int rp_k = p.heads[h].rp_k;
+  const float* U = p.basis + p.heads[h].uk_off;
+  // rows of a head: query head g of sequence b is row b * group + g; this CTA's four
+  const int r0 = blockIdx.y * kQ64Rows, nr = min(kQ64Rows, p.B * p.group - r0);
+  const int shares = kQ64Threads / rp_k;                     // at least four
+  const int share = tid / rp_k, c = tid - share * rp_k;
   const int each = (p.d_head + shares - 1) / shares, d0 = share * each, d1 = min(p.d_head, d0 + each);
-  const float* U = p.basis + hd.uk_off + c;
-  for (int g0 = 0; g0 < p.group; g0 += kQ64Rows) {
-    const int ng = min(kQ64Rows, p.group - g0);
-    for (int i = tid; i < ng * p.d_head; i += kQ64Threads) x[i / p.d_head][i % p.d_head] = to_f<T>(q[static_cast<int64_t>(g0) * p.d_head + i]);
-    __syncthreads();
-    double acc[kQ64Rows] = {0, 0, 0, 0};
-    if (share < shares) {
-      for (int d = d0; d < d1; d += 8) {
-        float u[8];
+  float u[kQ64Ahead];                        // on their way while the queries arrive
 #pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = d + j < d1 ? __ldg(U + (d + j) * hd.rp_k) : 0.f;
+  for (int j = 0; j < kQ64Ahead; ++j) u[j] = share < shares && d0 + j < d1 ? __ldg(U + (d0 + j) * rp_k + c) : 0.f;
+  for (int i = tid; i < kQ64Rows * p.d_head; i += kQ64Threads) {
+    const int r = i / p.d_head, d = i - r * p.d_head, b = (r0 + r) / p.group, g = (r0 + r) - b * p.group;
+    x[r][d] = r < nr ? static_cast<double>(to_f<T>(static_cast<const T*>(p.q)[b * p.q_stride_b + (static_cast<int64_t>(h) * p.group + g) * p.d_head + d])) : 0.0;
+  }
+  __syncthreads();
+  double acc[kQ64Rows] = {0, 0, 0, 0};
+  if (share < shares) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const double uu = u[j];
-          const int dd = min(d + j, p.d_head - 1);
-          if (ng == 1) {
-            acc[0] = fma(x[0][dd], uu, acc[0]);
-          } else {
+    for (int j = 0; j < kQ64Ahead; ++j)
+      if (d0 + j < d1) {
+        const double uu = u[j];
 #pragma unroll
-            for (int g = 0; g < kQ64Rows; ++g) acc[g] = fma(x[g][dd], uu, acc[g]);
-          }
-        }
+        for (int r = 0; r < kQ64Rows; ++r) acc[r] = fma(x[r][d0 + j], uu, acc[r]);
       }
+    for (int d = d0 + kQ64Ahead; d < d1; ++d) {
+      const double uu = __ldg(U + d * rp_k + c);
 #pragma unroll
-      for (int g = 0; g < kQ64Rows; ++g) part[tid][g] = acc[g];
+      for (int r = 0; r < kQ64Rows; ++r) acc[r] = fma(x[r][d], uu, acc[r]);
     }
-    __syncthreads();
-    for (int i = tid; i < ng * hd.rp_k; i += kQ64Threads) {
-      const int g = i / hd.rp_k, cc = i - g * hd.rp_k;
-      double s = 0;
-      for (int k = 0; k < shares; ++k) s += part[k * hd.rp_k + cc][g];
-      const int64_t at = (static_cast<int64_t>(unit) * p.rows + g0 + g) * p.q_stride + cc;
-      p.qp[at] = static_cast<float>(s * (kLog2e * p.scale));
-      p.q64[at] = s * p.scale;
-    }
-    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kQ64Rows; ++r) part[tid][r] = acc[r];
+  }
+  __syncthreads();
+  for (int i = tid; i < nr * rp_k; i += kQ64Threads) {
+    const int r = i / rp_k, cc = i - r * rp_k, b = (r0 + r) / p.group, g = (r0 + r) - b * p.group;
+    double s = 0;
+    for (int k = 0; k < shares; ++k) s += part[k * rp_k + cc][r];
+    const int64_t at = ((static_cast<int64_t>(h) * p.B + b) * p.group + g) * p.q_stride + cc;
+    p.qp[at] = static_cast<float>(s * (kLog2e * p.scale));
+    p.q64[at] = s * p.scale;
   }
 }
 
@@ -598,8 +597,9 @@ cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, u
     if (dtype == 0) mq_copy_query_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(p);
     else mq_copy_query_kernel<float><<<grid, 128, 0, s>>>(p);
   } else {
-    if (dtype == 0) mq_query64_kernel<__nv_bfloat16><<<p.B * p.H, kQ64Threads, 0, s>>>(p);
-    else mq_query64_kernel<float><<<p.B * p.H, kQ64Threads, 0, s>>>(p);
+    const dim3 grid(p.H, (p.B * p.group + kQ64Rows - 1) / kQ64Rows);
+    if (dtype == 0) mq_query64_kernel<__nv_bfloat16><<<grid, kQ64Threads, 0, s>>>(p);
+    else mq_query64_kernel<float><<<grid, kQ64Threads, 0, s>>>(p);
   }
   ++*launches;
   return cudaGetLastError();
