@@ -335,10 +335,15 @@ ea_status check_quant_args(eigen_attn_t h, const char* who, int32_t bits, int32_
 constexpr int kMaxGroup = 16;
 constexpr size_t kMqSlots = 65536;       // partials that every scratch holds at least, so that query rows can be split
 
+constexpr int kMqTcCtas = 296;           // largest grid of the tcgen05 tree kernel (its partials are slots of items + CTAs)
+int slot_rows_of(int rows) { return rows < ea::kMqTcRows ? rows : ea::kMqTcRows; }
+
 size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t* slots) {
   const size_t units = static_cast<size_t>(h->desc.batch) * h->desc.n_heads;
   const size_t off = align_up(units * rows * h->L.max_rp_k * sizeof(float));
-  const size_t n = units * rows > kMqSlots ? units * rows : kMqSlots;
+  size_t n = units * rows > kMqSlots ? units * rows : kMqSlots;
+  const size_t items = units * ((rows + ea::kMqTcRows - 1) / ea::kMqTcRows);
+  if ((items + kMqTcCtas) * slot_rows_of(rows) > n) n = (items + kMqTcCtas) * slot_rows_of(rows);
   if (off_part) *off_part = off;
   if (slots) *slots = n;
   return align_up(off + n * h->L.part_stride * sizeof(float));
@@ -1372,57 +1377,72 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
   p.n = h->len; p.n_max = h->desc.n_max;
   p.rows = p.tokens * p.group;
   p.q_stride = L.max_rp_k; p.part_stride = L.part_stride; p.lr_v_width = L.sum_rp_v;
-  // Tiles of a piece: the CTAs run in waves of resident ones, each pays a start-up worth a tile or two; pieces are cut to
-  // one size, so a shorter sequence of the batch has fewer of them; the partials must have room.
   const bool mma = h->desc.dtype == EA_BF16;
   const int max_rp = L.max_rp_k > L.max_rp_v ? L.max_rp_k : L.max_rp_v;
   // Trees with more than 16 query rows: tcgen05 products, where the layer's slabs have tensor maps (pages then have to lie
   // inside one sequence's slab) and no bias goes onto the scores.
-  p.tmaps = h->ws + L.off_tmaps;
-  p.status = dev_status(h);
   const bool tc = mma && p.tail > 0 && p.rows > 16 && h->tmaps_ok && !h->alibi && h->opt_tree_impl != 1 &&
                   (!h->paged || h->desc.n_max % (1 << h->page_shift) == 0);
-  const ea::MqShape shape = tc ? ea::kMqTcShape : mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::kMqSimtShape;
-  const int tile = 1 << shape.tile_shift;
-  p.tile_shift = shape.tile_shift;
-  p.tiles = static_cast<int32_t>((end + tile - 1) >> shape.tile_shift);
-  const int64_t chunks = static_cast<int64_t>(p.H) * ((p.rows + shape.queries - 1) / shape.queries);   // of one sequence
-  int64_t cap = static_cast<int64_t>(slots) / (static_cast<int64_t>(p.B) * p.H * p.rows);
-  if (cap > p.tiles) cap = p.tiles;
-  if (cap > 65535) cap = 65535;
-  if (cap < 1) cap = 1;
-  int64_t per = p.tiles;
-  if (h->opt_ctas > 0) {
-    int64_t splits = (h->opt_ctas + chunks * p.B - 1) / (chunks * p.B);
-    if (splits > cap) splits = cap;
-    per = (p.tiles + splits - 1) / splits;
-  } else {
-    // Equal sequences: waves of equal pieces.  Unequal ones: the CTAs take what comes next, so the end is at most the
-    // average load plus one piece.
-    const int64_t wave = static_cast<int64_t>(h->sm_count) * shape.ctas_per_sm;
-    const bool ragged = h->max_deficit > 0 && p.list == nullptr;
-    const int64_t kStart = tc ? 5 : 2;        // tiles' worth of a CTA's start and end (measured: 5 to 6 with tcgen05)
-    int64_t best = INT64_MAX, last = 0;
-    for (int64_t s2 = 1; s2 <= cap && s2 <= 256; ++s2) {
-      const int64_t size = (p.tiles + s2 - 1) / s2;
-      if (size == last) continue;
-      last = size;
-      int64_t cost = 0;
-      if (ragged) {
-        int64_t load = 0;
-        for (int b = 0; b < p.B; ++b) {
-          const int64_t t = (p.n - h->deficit[b] + p.tail + tile - 1) >> shape.tile_shift;
-          load += t + kStart * (t > size ? (t + size - 1) / size : 1);
-        }
-        cost = load * chunks / wave + size + kStart;
-      } else {
-        cost = ((s2 * p.B * chunks + wave - 1) / wave) * (size + kStart);
-      }
-      if (cost < best) { best = cost; per = size; }
+  const ea::MqShape shape = mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::kMqSimtShape;
+  p.tile_shift = tc ? 7 : shape.tile_shift;
+  const int tile = 1 << p.tile_shift;
+  p.tiles = static_cast<int32_t>((end + tile - 1) >> p.tile_shift);
+  if (tc) {
+    // one range of tiles per SM
+    p.tmaps = h->ws + L.off_tmaps;
+    p.status = dev_status(h);
+    p.head_tiles = static_cast<int64_t>(p.tiles) * p.B;
+    if (h->max_deficit > 0) {
+      p.head_tiles = 0;
+      for (int b = 0; b < p.B; ++b) p.head_tiles += (p.n - h->deficit[b] + p.tail + tile - 1) >> p.tile_shift;
     }
+    p.total_tiles = p.head_tiles * p.H * ((p.rows + ea::kMqTcRows - 1) / ea::kMqTcRows);
+    int64_t grid = h->opt_ctas > 0 ? h->opt_ctas : h->sm_count;
+    if (grid > kMqTcCtas) grid = kMqTcCtas;
+    if (grid > p.total_tiles) grid = p.total_tiles;
+    p.grid = static_cast<int32_t>(grid);
+    p.slot_rows = slot_rows_of(p.rows);
+  } else {
+    // Tiles of a piece: the CTAs run in waves of resident ones, each pays a start-up worth a tile or two; pieces are cut to
+    // one size, so a shorter sequence of the batch has fewer of them; the partials must have room.
+    const int64_t chunks = static_cast<int64_t>(p.H) * ((p.rows + shape.queries - 1) / shape.queries);   // of one sequence
+    int64_t cap = static_cast<int64_t>(slots) / (static_cast<int64_t>(p.B) * p.H * p.rows);
+    if (cap > p.tiles) cap = p.tiles;
+    if (cap > 65535) cap = 65535;
+    if (cap < 1) cap = 1;
+    int64_t per = p.tiles;
+    if (h->opt_ctas > 0) {
+      int64_t splits = (h->opt_ctas + chunks * p.B - 1) / (chunks * p.B);
+      if (splits > cap) splits = cap;
+      per = (p.tiles + splits - 1) / splits;
+    } else {
+      // Equal sequences: waves of equal pieces.  Unequal ones: the CTAs take what comes next, so the end is at most the
+      // average load plus one piece.
+      const int64_t wave = static_cast<int64_t>(h->sm_count) * shape.ctas_per_sm;
+      const bool ragged = h->max_deficit > 0 && p.list == nullptr;
+      constexpr int64_t kStart = 2;           // tiles' worth of a CTA's start and end
+      int64_t best = INT64_MAX, last = 0;
+      for (int64_t s2 = 1; s2 <= cap && s2 <= 256; ++s2) {
+        const int64_t size = (p.tiles + s2 - 1) / s2;
+        if (size == last) continue;
+        last = size;
+        int64_t cost = 0;
+        if (ragged) {
+          int64_t load = 0;
+          for (int b = 0; b < p.B; ++b) {
+            const int64_t t = (p.n - h->deficit[b] + p.tail + tile - 1) >> p.tile_shift;
+            load += t + kStart * (t > size ? (t + size - 1) / size : 1);
+          }
+          cost = load * chunks / wave + size + kStart;
+        } else {
+          cost = ((s2 * p.B * chunks + wave - 1) / wave) * (size + kStart);
+        }
+        if (cost < best) { best = cost; per = size; }
+      }
+    }
+    p.per = static_cast<int32_t>(per);
+    p.splits = static_cast<int32_t>((p.tiles + per - 1) / per);
   }
-  p.per = static_cast<int32_t>(per);
-  p.splits = static_cast<int32_t>((p.tiles + per - 1) / per);
   if (h->ev_start) cudaEventRecord(h->ev_start, s);
   cudaError_t e = tc    ? ea::launch_mq_tc(p, L.max_rp_k, L.max_rp_v, s, &h->launches)
                   : mma ? ea::launch_mq_mma(p, max_rp, s, &h->launches)

@@ -454,28 +454,55 @@ __global__ void __launch_bounds__(256) mq_simt_kernel(const MqDecodeParams p) {
 
 // ---------------------------------------------------------------- merge and lift
 
+// The pieces of a query row: `count` partials, `step` floats apart from `first` on.
+struct Pieces {
+  const float* first;
+  int64_t step;
+  int count;
+};
+// Equal pieces of an item: [unit * rows + row][splits].  Ranges over all items (grid > 0): the CTAs whose ranges meet the
+// item; `before` = tiles of the sequences in front of b (one run of query rows).
+__device__ __forceinline__ Pieces pieces_of(const MqDecodeParams& p, int unit, int row, int64_t before) {
+  const int h = unit / p.B, b = unit - h * p.B;
+  const int tiles = p.list != nullptr ? p.tiles
+                                      : (p.n - (p.deficit != nullptr ? __ldg(p.deficit + b) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
+  if (p.grid == 0)
+    return {p.partials + (static_cast<int64_t>(unit) * p.rows + row) * p.splits * p.part_stride, p.part_stride, max(1, (tiles + p.per - 1) / p.per)};
+  const int chunks = (p.rows + kMqTcRows - 1) / kMqTcRows, chunk = row / kMqTcRows;
+  const int64_t x = (h * p.head_tiles + before) * chunks + static_cast<int64_t>(chunk) * tiles;
+  const int c0 = static_cast<int>(((x + 1) * p.grid - 1) / p.total_tiles);             // the CTA that has tile x
+  const int c1 = static_cast<int>(((x + tiles) * p.grid - 1) / p.total_tiles);
+  const int64_t slot = static_cast<int64_t>(unit) * chunks + chunk + c0;
+  return {p.partials + (slot * p.slot_rows + (row - chunk * kMqTcRows)) * p.part_stride, static_cast<int64_t>(p.slot_rows) * p.part_stride,
+          c1 - c0 + 1};
+}
+// Tiles of the sequences in front of b, by a whole warp.
+__device__ __forceinline__ int64_t tiles_before(const MqDecodeParams& p, int b) {
+  if (p.grid == 0) return 0;
+  if (p.deficit == nullptr) return static_cast<int64_t>(b) * ((p.n + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift);
+  int64_t sum = 0;
+  for (int i = threadIdx.x & 31; i < b; i += 32) sum += (p.n - __ldg(p.deficit + i) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
+#pragma unroll
+  for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
+  return sum;
+}
 // o' of one query row, column c, from its pieces (0 for a row that sees nothing).
-__device__ __forceinline__ float merged(const MqDecodeParams& p, int unit, int row, int pieces, int c) {
-  const float* part = p.partials + (static_cast<int64_t>(unit) * p.rows + row) * p.splits * p.part_stride;
-  float M = part[0], L = part[1], acc = part[4 + c];
-  if (pieces > 1) {
-    for (int s = 1; s < pieces; ++s) M = fmaxf(M, part[s * p.part_stride]);
+__device__ __forceinline__ float merged(const Pieces& w, int c) {
+  float M = w.first[0], L = w.first[1], acc = w.first[4 + c];
+  if (w.count > 1) {
+#pragma unroll 4
+    for (int s = 1; s < w.count; ++s) M = fmaxf(M, w.first[s * w.step]);
     const float base = M == -INFINITY ? 0.f : M;
     L = 0.f; acc = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < pieces; ++s) {
-      const float* x = part + s * p.part_stride;
+    for (int s = 0; s < w.count; ++s) {
+      const float* x = w.first + s * w.step;
       const float f = ex2(x[0] - base);      // 0 for a piece without rows
       L = fmaf(x[1], f, L);
       acc = fmaf(x[4 + c], f, acc);
     }
   }
   return L == 0.f ? 0.f : acc / L;
-}
-__device__ __forceinline__ int pieces_of(const MqDecodeParams& p, int b) {
-  if (p.list != nullptr || p.deficit == nullptr) return p.splits;
-  const int tiles = (p.n - __ldg(p.deficit + b) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
-  return max(1, (tiles + p.per - 1) / p.per);
 }
 
 // Packed rank-r output.
@@ -484,10 +511,11 @@ __global__ void __launch_bounds__(128) mq_combine_lowrank_kernel(const MqDecodeP
   const int unit = blockIdx.x / p.rows, row = blockIdx.x - unit * p.rows, c = threadIdx.x;
   const int h = unit / p.B, b = unit - h * p.B;
   const HeadInfo hd = p.heads[h];
+  const Pieces w = pieces_of(p, unit, row, tiles_before(p, b));
   if (c >= hd.rp_v) return;
   const int t = row / p.group, i = row - t * p.group;
   static_cast<T*>(p.out)[(static_cast<int64_t>(b) * p.tokens + t) * p.group * p.lr_v_width + static_cast<int64_t>(p.group) * hd.lr_v_off +
-                         static_cast<int64_t>(i) * hd.rp_v + c] = from_f<T>(merged(p, unit, row, pieces_of(p, b), c));
+                         static_cast<int64_t>(i) * hd.rp_v + c] = from_f<T>(merged(w, c));
 }
 
 template <typename T>
@@ -511,7 +539,8 @@ __global__ void __launch_bounds__(256) mq_combine_few_kernel(const MqDecodeParam
   float u[kAhead];
 #pragma unroll
   for (int j = 0; j < kAhead; ++j) u[j] = j < nc && d < p.d_head ? __ldg(Ut + j * p.d_head) : 0.f;
-  if (tid < hd.rp_v) os[tid] = merged(p, unit, row, pieces_of(p, b), tid);
+  const Pieces w = pieces_of(p, unit, row, tiles_before(p, b));
+  if (tid < hd.rp_v) os[tid] = merged(w, tid);
   __syncthreads();
   float y = 0.f;
 #pragma unroll
@@ -543,22 +572,27 @@ __global__ void __launch_bounds__(kPrThreads) mq_combine_many_kernel(const __gri
     const int r = tid & (kCbRows - 1), g = blockIdx.x * kCbRows + r;
     const bool there = g < total;
     const int b = there ? g / p.rows : 0;
-    const int pieces = there ? pieces_of(p, b) : 0;
+    // tiles in front of the first sequence here, then of each of those up to this row's own
+    const int b0 = blockIdx.x * kCbRows / p.rows;
+    int64_t before = tiles_before(p, b0);
+    if (p.grid > 0)
+      for (int i = b0; i < b; ++i) before += (p.n - (p.deficit != nullptr ? __ldg(p.deficit + i) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
+    Pieces w{nullptr, 0, 0};
+    if (there) w = pieces_of(p, h * p.B + b, g - b * p.rows, before);
     if (tid < kCbRows) target[r] = there ? out_row<T>(p, h, b, g - b * p.rows) : nullptr;
-    const float* part = p.partials + (static_cast<int64_t>(h) * total + (there ? g : 0)) * p.splits * p.part_stride;
     float M = -INFINITY, L = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < pieces; ++s) M = fmaxf(M, part[s * p.part_stride]);
+    for (int s = 0; s < w.count; ++s) M = fmaxf(M, w.first[s * w.step]);
     const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll 4
-    for (int s = 0; s < pieces; ++s) L = fmaf(part[s * p.part_stride + 1], ex2(part[s * p.part_stride] - base), L);
+    for (int s = 0; s < w.count; ++s) L = fmaf(w.first[s * w.step + 1], ex2(w.first[s * w.step] - base), L);
     const float inv = L == 0.f ? 0.f : 1.f / L;              // (a row that sees nothing: its sums are zeros)
     const int half = hd.rp_v / 2, c_lo = (tid / kCbRows) * half;
     for (int c = c_lo; c < c_lo + half; c += 4) {            // half is a multiple of 4
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-      for (int s = 0; s < pieces; ++s) {
-        const float* x = part + s * p.part_stride;
+      for (int s = 0; s < w.count; ++s) {
+        const float* x = w.first + s * w.step;
         const float f = ex2(x[0] - base) * inv;
         const float4 v = *reinterpret_cast<const float4*>(x + 4 + c);
         o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);

@@ -306,8 +306,13 @@ struct MqDecodeParams {
   int32_t lr_v_width;       // sum of rp_v: width of a packed output row of one query head
   uint32_t flags;
   PageMap pages;
-  const void* tmaps;        // CUtensorMap[2 * H]: K' and V' slab of every head (tcgen05 kernel)
-  int* status;              // (tcgen05 kernel: its waits are bounded)
+  // tcgen05 kernel (grid > 0): the tiles of all items (unit, run of 128 query rows), laid end to end, in equal ranges.
+  // CTA c has tiles [c total / grid, (c + 1) total / grid); its piece of item u leaves the partials of u's rows in slot
+  // u + c, [slot_rows][part_stride] (unique along the staircase of pieces).
+  int32_t grid, slot_rows;
+  int64_t total_tiles, head_tiles;   // of all items; of all sequences for one head and run of query rows
+  const void* tmaps;        // CUtensorMap[2 * H]: K' and V' slab of every head
+  int* status;              // (its waits are bounded)
 };
 
 struct MqProjectParams {     // drafted tokens: Q' into the scratch (scaled into the base-2 domain), K', V' rows into the cache
@@ -390,7 +395,7 @@ MqShape mq_mma_shape(int rows, int max_rp);
 // 16-bit layers; max_rp: widest padded rank over heads and K/V
 cudaError_t launch_mq_mma(const MqDecodeParams& p, int max_rp, cudaStream_t s, uint64_t* launches);
 // tcgen05 products (tail only: a tree of drafted tokens): 128 query rows per CTA, one CTA per SM
-constexpr MqShape kMqTcShape = {128, 1, 7};
+constexpr int kMqTcRows = 128;       // query rows of an item
 cudaError_t launch_mq_tc(const MqDecodeParams& p, int max_rp_k, int max_rp_v, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, int max_rp_v, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_tree_commit(const TreeCommitParams& p, int sequences, cudaStream_t s, uint64_t* launches);
