@@ -486,22 +486,51 @@ __device__ __forceinline__ int64_t tiles_before(const MqDecodeParams& p, int b) 
   for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
   return sum;
 }
-// o' of one query row, column c, from its pieces (0 for a row that sees nothing).
-__device__ __forceinline__ float merged(const Pieces& w, int c) {
-  float M = w.first[0], L = w.first[1], acc = w.first[4 + c];
-  if (w.count > 1) {
-#pragma unroll 4
-    for (int s = 1; s < w.count; ++s) M = fmaxf(M, w.first[s * w.step]);
-    const float base = M == -INFINITY ? 0.f : M;
-    L = 0.f; acc = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < w.count; ++s) {
+// o' of one query row from its pieces (0 for a row that sees nothing), column c of this thread where `has`; by whole warps.
+// Few pieces: everything is read at once.  Many: the lanes read a piece's maximum and sum each, so that the chain of
+// dependent reads is two long.
+__device__ __forceinline__ float merged(const Pieces& w, int c, bool has) {
+  const int lane = threadIdx.x & 31;
+  constexpr int kFew = 4;
+  if (w.count <= kFew) {
+    float m[kFew], l[kFew], a[kFew], top = -INFINITY, sum = 0.f, o = 0.f;
+#pragma unroll
+    for (int s = 0; s < kFew; ++s) {
       const float* x = w.first + s * w.step;
-      const float f = ex2(x[0] - base);      // 0 for a piece without rows
-      L = fmaf(x[1], f, L);
-      acc = fmaf(x[4 + c], f, acc);
+      m[s] = s < w.count ? x[0] : -INFINITY;
+      l[s] = s < w.count ? x[1] : 0.f;
+      a[s] = s < w.count && has ? x[4 + c] : 0.f;
+    }
+#pragma unroll
+    for (int s = 0; s < kFew; ++s) top = fmaxf(top, m[s]);
+    if (top == -INFINITY) top = 0.f;
+#pragma unroll
+    for (int s = 0; s < kFew; ++s) {
+      const float f = ex2(m[s] - top);       // 0 for a piece without rows
+      sum = fmaf(l[s], f, sum);
+      o = fmaf(a[s], f, o);
+    }
+    return sum == 0.f ? 0.f : o / sum;
+  }
+  float M = -INFINITY;
+  for (int s = lane; s < w.count; s += 32) M = fmaxf(M, w.first[s * w.step]);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, d));
+  const float base = M == -INFINITY ? 0.f : M;
+  float L = 0.f, acc = 0.f;
+  for (int s0 = 0; s0 < w.count; s0 += 32) {
+    const int n = min(32, w.count - s0);
+    const float* x = w.first + s0 * w.step;
+    const float f = lane < n ? ex2(x[lane * w.step] - base) : 0.f;         // 0 for a piece without rows
+    L = lane < n ? fmaf(x[lane * w.step + 1], f, L) : L;
+#pragma unroll 8
+    for (int s = 0; s < n; ++s) {
+      const float fs = __shfl_sync(kFull, f, s);
+      if (has) acc = fmaf(x[s * w.step + 4 + c], fs, acc);
     }
   }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) L += __shfl_xor_sync(kFull, L, d);
   return L == 0.f ? 0.f : acc / L;
 }
 
@@ -512,10 +541,11 @@ __global__ void __launch_bounds__(128) mq_combine_lowrank_kernel(const MqDecodeP
   const int h = unit / p.B, b = unit - h * p.B;
   const HeadInfo hd = p.heads[h];
   const Pieces w = pieces_of(p, unit, row, tiles_before(p, b));
+  const float x = merged(w, c, c < hd.rp_v);
   if (c >= hd.rp_v) return;
   const int t = row / p.group, i = row - t * p.group;
   static_cast<T*>(p.out)[(static_cast<int64_t>(b) * p.tokens + t) * p.group * p.lr_v_width + static_cast<int64_t>(p.group) * hd.lr_v_off +
-                         static_cast<int64_t>(i) * hd.rp_v + c] = from_f<T>(merged(w, c));
+                         static_cast<int64_t>(i) * hd.rp_v + c] = from_f<T>(x);
 }
 
 template <typename T>
@@ -540,7 +570,10 @@ __global__ void __launch_bounds__(256) mq_combine_few_kernel(const MqDecodeParam
 #pragma unroll
   for (int j = 0; j < kAhead; ++j) u[j] = j < nc && d < p.d_head ? __ldg(Ut + j * p.d_head) : 0.f;
   const Pieces w = pieces_of(p, unit, row, tiles_before(p, b));
-  if (tid < hd.rp_v) os[tid] = merged(w, tid);
+  if (tid < 128) {
+    const float x = merged(w, tid, tid < hd.rp_v);
+    if (tid < hd.rp_v) os[tid] = x;
+  }
   __syncthreads();
   float y = 0.f;
 #pragma unroll

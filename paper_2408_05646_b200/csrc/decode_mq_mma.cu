@@ -79,11 +79,11 @@ struct Shape {
   static constexpr int kQueries = 8 * MT * WG;
   static constexpr int kPitch = odd_pieces(NC) * 16;
   static constexpr int kSlot = kRows * 2 * kPitch;                        // one key group's rows of a tile
-  static constexpr int kCtas = WG == 1 ? 2 : 1;                           // resident CTAs per SM
+  static constexpr int kCtas = WG == 2 ? 1 : NC <= 8 && MT == 1 ? 3 : 2;  // resident CTAs per SM
   static constexpr bool kQReg = MT * NC * 2 <= 40;                        // Q' fragments in registers, else in shared memory
   static constexpr int kQBytes = kQReg ? 0 : WG * MT * (NC / 2) * 32 * 16;
   static constexpr int kHead = 32 * 8 + 64 * 4;                           // masks of the queries, places of the drafted rows
-  static constexpr int kRoom = (kCtas == 2 ? 113 : 226) * 1024 - kHead - kQBytes;
+  static constexpr int kRoom = (kCtas == 3 ? 75 : kCtas == 2 ? 113 : 226) * 1024 - kHead - kQBytes;
   static constexpr int kStages = kRoom / (kGroups * kSlot) < 4 ? kRoom / (kGroups * kSlot) : 4;
   static constexpr int kMerge = kGroups * kQueries * (2 + 8 * NC + 1) * 4;
   static constexpr int kRing = kGroups * kSlot * kStages > kMerge ? kGroups * kSlot * kStages : kMerge;
@@ -344,8 +344,18 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
         sc[mt][j][1] = s[mt][j][1] + s[mt][j][3];
       }
     // the end of the sequence, drafted rows, a list entry that is not there (they come last, as the incomplete block does)
-    const bool special = bias || first[0] < 0 || (HV == 2 && first[1] < 0) || (HV == 2 ? max(first[0], first[1]) : first[0]) + 16 > n_b;
+    const bool special = first[0] < 0 || (HV == 2 && first[1] < 0) || (HV == 2 ? max(first[0], first[1]) : first[0]) + 16 > n_b;
     unsigned odd_rows = 0;             // drafted rows whose values are not finite
+    if (bias && !special) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float place = static_cast<float>(first[j >> 1] + 8 * (j & 1) + 2 * tig + e);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) sc[mt][j][e] = fmaf(hd.alibi_slope2, place - q_pos[mt], sc[mt][j][e]);
+        }
+    }
     if (special) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
@@ -516,7 +526,7 @@ cudaError_t launch_rank(const MqDecodeParams& p, cudaStream_t s) {
 
 MqShape mq_mma_shape(int rows, int max_rp) {
   const int shift = max_rp > 96 ? 6 : 7;
-  if (rows <= 8) return {8, 2, shift};
+  if (rows <= 8) return {8, max_rp <= 64 ? 3 : 2, shift};
   if (rows <= 16) return {16, 2, shift};
   return {32, 1, shift};
 }
