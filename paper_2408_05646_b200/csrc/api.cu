@@ -1745,7 +1745,7 @@ ea_status eigen_attn_decode_sparse(eigen_attn_t h, const void* d_q, int64_t stri
   p.partials = reinterpret_cast<float*>(h->sp_buf + h->sp.off_part);
   p.out = d_out; p.out_stride_b = stride_b_out;
   p.list = sp.list; p.list_len = sp.list_len; p.block_shift = h->sp_shift;
-  p.group = group; p.tokens = 1; p.tail = 0;
+  p.group = group; p.tokens = 1; p.tail = 0; p.chained = 1;
   p.flags = flags & EA_OUT_LOWRANK;
   return launch_mq(h, "decode_sparse launch", p, static_cast<int64_t>(sp.list_len) << h->sp_shift, h->sp.slots, s);
 }

@@ -99,12 +99,16 @@ template <> __device__ __forceinline__ double query_factor<float>() { return 1.0
 constexpr int kScoreBlocks = 64, kScoreThreads = 2 * kScoreBlocks;
 template <typename T>
 __global__ void __launch_bounds__(kScoreThreads) block_scores_kernel(const SparseParams p, int max_steps) {
+  chain_go();
   extern __shared__ __align__(16) unsigned char sm[];
   const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B, tid = threadIdx.x;
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
   const int have = (n_b + (1 << p.block_shift) - 1) >> p.block_shift;
   const int first = p.sink + blockIdx.y * kScoreBlocks * max_steps, last = min(have - p.recent, first + kScoreBlocks * max_steps);
-  if (have <= p.list_len || first >= last) return;           // nothing to choose
+  if (have <= p.list_len || first >= last) {                 // nothing to choose
+    chain_wait();
+    return;
+  }
   const HeadInfo& hd = p.heads[h];
   const int rp_k = hd.rp_k;
   constexpr int kPer = 16 / sizeof(T);       // channels of a 16-byte piece
@@ -132,7 +136,8 @@ __global__ void __launch_bounds__(kScoreThreads) block_scores_kernel(const Spars
     }
     tc::cp_async_commit();
   };
-  load(0);
+  load(0);                                   // (the bounds are older than the chain, the queries are not)
+  chain_wait();
   for (int i = tid; i < p.group * rp_k; i += kScoreThreads) {
     const int g = i / rp_k, c = i - g * rp_k;
     const double x = p.q64[(static_cast<int64_t>(unit) * p.group + g) * p.q_stride + c];
@@ -186,6 +191,8 @@ __device__ __forceinline__ uint64_t order_key(double x) {
 // counting those would send every key to one counter.
 constexpr int kSelThreads = 256, kDigit = 11, kBins = 1 << kDigit, kKeep = 4, kSegment = kSelThreads * kKeep;
 __global__ void __launch_bounds__(kSelThreads) block_select_kernel(const SparseParams p) {
+  chain_go();
+  chain_wait();
   __shared__ int hist[kBins];
   __shared__ int warp_sum[kSelThreads / 32];
   __shared__ int s_digit, s_above, s_count;
@@ -374,9 +381,8 @@ static cudaError_t launch_scores_t(const SparseParams& p, int max_rp_k, cudaStre
   const int64_t chunks = (p.max_blocks - p.sink - p.recent + kScoreBlocks - 1) / kScoreBlocks, units = static_cast<int64_t>(p.B) * p.H;
   int64_t steps = units * chunks / (5 * 148);
   steps = steps < 1 ? 1 : steps > 3 ? 3 : steps;
-  block_scores_kernel<T><<<dim3(static_cast<unsigned>(units), static_cast<unsigned>((chunks + steps - 1) / steps)), kScoreThreads, smem, s>>>(
-      p, static_cast<int>(steps));
-  return cudaGetLastError();
+  return launch_chained(true, block_scores_kernel<T>, dim3(static_cast<unsigned>(units), static_cast<unsigned>((chunks + steps - 1) / steps)),
+                        kScoreThreads, smem, s, p, static_cast<int>(steps));
 }
 
 cudaError_t launch_block_scores(const SparseParams& p, int dtype, int max_rp_k, cudaStream_t s, uint64_t* launches) {
@@ -385,9 +391,8 @@ cudaError_t launch_block_scores(const SparseParams& p, int dtype, int max_rp_k, 
 }
 
 cudaError_t launch_block_select(const SparseParams& p, cudaStream_t s, uint64_t* launches) {
-  block_select_kernel<<<p.B * p.H, kSelThreads, 0, s>>>(p);
   ++*launches;
-  return cudaGetLastError();
+  return launch_chained(true, block_select_kernel, p.B * p.H, kSelThreads, 0, s, p);
 }
 
 }  // namespace ea

@@ -158,6 +158,7 @@ __device__ __forceinline__ void put4(T* dst, float a, float b, float c, float d,
 constexpr int kPrStep = 32;
 template <typename T, int R, int C>
 __global__ void __launch_bounds__(kPrThreads, 3) mq_project_many_kernel(const __grid_constant__ MqProjectParams p) {
+  chain_go();
   extern __shared__ __align__(16) float sm[];
   constexpr int kPrRows = 32 * R, kPer = kPrThreads / kPrRows;            // rows, threads that load one
   const int tiles_q = (p.B * p.tokens * p.group + kPrRows - 1) / kPrRows, tiles_kv = (p.B * p.tokens + kPrRows - 1) / kPrRows;
@@ -238,6 +239,7 @@ __global__ void __launch_bounds__(kPrThreads, 3) mq_project_many_kernel(const __
 constexpr int kPfRows = 8, kPfCols = 32;
 template <typename T>
 __global__ void __launch_bounds__(128) mq_project_few_kernel(const __grid_constant__ MqProjectParams p) {
+  chain_go();
   __shared__ __align__(16) float us[128 * kPfCols];
   __shared__ float xs[kPfRows][128 + 1];
   const int tiles_q = (p.B * p.tokens * p.group + kPfRows - 1) / kPfRows, tiles_kv = (p.B * p.tokens + kPfRows - 1) / kPfRows;
@@ -275,6 +277,7 @@ __global__ void __launch_bounds__(128) mq_project_few_kernel(const __grid_consta
 // Queries that are rank-r already: into the scratch.
 template <typename T>
 __global__ void __launch_bounds__(128) mq_copy_query_kernel(const MqQueryParams p) {
+  chain_go();
   const int unit = blockIdx.x, h = unit / p.B, b = unit - h * p.B, row = blockIdx.y, c = threadIdx.x;
   const HeadInfo hd = p.heads[h];
   if (c >= hd.rp_k) return;
@@ -294,6 +297,7 @@ __global__ void __launch_bounds__(128) mq_copy_query_kernel(const MqQueryParams 
 constexpr int kQ64Threads = 512, kQ64Rows = 4, kQ64Ahead = 16;
 template <typename T>
 __global__ void __launch_bounds__(kQ64Threads) mq_query64_kernel(const MqQueryParams p) {
+  chain_go();
   __shared__ double x[kQ64Rows][128];
   __shared__ double part[kQ64Threads][kQ64Rows];
   const int h = blockIdx.x, tid = threadIdx.x;
@@ -347,6 +351,8 @@ __global__ void __launch_bounds__(kQ64Threads) mq_query64_kernel(const MqQueryPa
 constexpr int kSimtRows = 8, kSimtTile = 32;
 template <typename T>
 __global__ void __launch_bounds__(256) mq_simt_kernel(const MqDecodeParams p) {
+  chain_go();
+  chain_wait();
   extern __shared__ float sm[];
   __shared__ int64_t phys[kSimtTile];
   __shared__ int logical[kSimtTile];         // logical row, -1 = nothing there
@@ -537,6 +543,7 @@ __device__ __forceinline__ float merged(const Pieces& w, int c, bool has) {
 // Packed rank-r output.
 template <typename T>
 __global__ void __launch_bounds__(128) mq_combine_lowrank_kernel(const MqDecodeParams p) {
+  chain_wait();
   const int unit = blockIdx.x / p.rows, row = blockIdx.x - unit * p.rows, c = threadIdx.x;
   const int h = unit / p.B, b = unit - h * p.B;
   const HeadInfo hd = p.heads[h];
@@ -570,6 +577,7 @@ __global__ void __launch_bounds__(256) mq_combine_few_kernel(const MqDecodeParam
 #pragma unroll
   for (int j = 0; j < kAhead; ++j) u[j] = j < nc && d < p.d_head ? __ldg(Ut + j * p.d_head) : 0.f;
   const Pieces w = pieces_of(p, unit, row, tiles_before(p, b));
+  chain_wait();
   if (tid < 128) {
     const float x = merged(w, tid, tid < hd.rp_v);
     if (tid < hd.rp_v) os[tid] = x;
@@ -613,6 +621,7 @@ __global__ void __launch_bounds__(kPrThreads) mq_combine_many_kernel(const __gri
     Pieces w{nullptr, 0, 0};
     if (there) w = pieces_of(p, h * p.B + b, g - b * p.rows, before);
     if (tid < kCbRows) target[r] = there ? out_row<T>(p, h, b, g - b * p.rows) : nullptr;
+    chain_wait();
     float M = -INFINITY, L = 0.f;
 #pragma unroll 4
     for (int s = 0; s < w.count; ++s) M = fmaxf(M, w.first[s * w.step]);
@@ -748,10 +757,8 @@ cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, u
   const int chunks = (p.rows + kSimtRows - 1) / kSimtRows;
   const dim3 grid(p.B * p.H * chunks, p.splits);
   const size_t smem = sizeof(float) * (kSimtRows * 128 + kSimtTile * 129 + kSimtTile * 128);
-  if (dtype == 0) mq_simt_kernel<__nv_bfloat16><<<grid, 256, smem, s>>>(p);
-  else mq_simt_kernel<float><<<grid, 256, smem, s>>>(p);
   ++*launches;
-  return cudaGetLastError();
+  return dtype == 0 ? launch_chained(p.chained != 0, mq_simt_kernel<__nv_bfloat16>, grid, 256, smem, s, p) : launch_chained(p.chained != 0, mq_simt_kernel<float>, grid, 256, smem, s, p);
 }
 
 template <typename T, int C>
@@ -760,20 +767,18 @@ static cudaError_t launch_combine_many(const MqDecodeParams& p, int max_rp_v, cu
   static size_t configured[kMaxDevices] = {};
   const cudaError_t e = ensure_dynamic_smem(mq_combine_many_kernel<T, C>, smem, configured);
   if (e != cudaSuccess) return e;
-  mq_combine_many_kernel<T, C><<<dim3((p.B * p.rows + kCbRows - 1) / kCbRows, p.H), kPrThreads, smem, s>>>(p);
-  return cudaGetLastError();
+  return launch_chained(p.chained != 0, mq_combine_many_kernel<T, C>, dim3((p.B * p.rows + kCbRows - 1) / kCbRows, p.H), kPrThreads, smem, s, p);
 }
 template <typename T>
 static cudaError_t launch_combine_t(const MqDecodeParams& p, int max_rp_v, cudaStream_t s) {
   const int64_t units = static_cast<int64_t>(p.B) * p.H, rows = units * p.rows;
   if (p.flags & 0x2u) {                      // EA_OUT_LOWRANK
-    mq_combine_lowrank_kernel<T><<<static_cast<unsigned>(rows), 128, 0, s>>>(p);
+    return launch_chained(p.chained != 0, mq_combine_lowrank_kernel<T>, static_cast<unsigned>(rows), 128, 0, s, p);
   } else if (p.B * p.rows >= 64 && rows >= 2048) {
     return p.d_head <= 64 ? launch_combine_many<T, 16>(p, max_rp_v, s) : launch_combine_many<T, 32>(p, max_rp_v, s);
   } else {
-    mq_combine_few_kernel<T><<<static_cast<unsigned>(rows), 256, 0, s>>>(p);
+    return launch_chained(p.chained != 0, mq_combine_few_kernel<T>, static_cast<unsigned>(rows), 256, 0, s, p);
   }
-  return cudaGetLastError();
 }
 
 cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, int max_rp_v, cudaStream_t s, uint64_t* launches) {

@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
     mq_mma_kernel(const MqDecodeParams p) {
   using S = Shape<NC, MT, WG>;
   constexpr int NKS = NC / 2, kRows = S::kRows, HV = S::kHalves, NJ = S::kJ;
+  chain_go();
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* q_mask = reinterpret_cast<uint64_t*>(smem);                   // [32]
   float* draft_pos = reinterpret_cast<float*>(smem + 32 * 8);             // [64]
@@ -123,7 +124,10 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
   const int64_t end = p.list ? static_cast<int64_t>(p.list_len) << p.block_shift : static_cast<int64_t>(n_b) + p.tail;
   const int nt = static_cast<int>((end + S::kTile - 1) >> S::kTileShift);
   const int t_lo = split * p.per, t_hi = min(nt, t_lo + p.per);
-  if (split > 0 && t_lo >= nt) return;       // a shorter sequence: nothing left (its first piece always reports)
+  if (split > 0 && t_lo >= nt) {             // a shorter sequence: nothing left (its first piece always reports)
+    chain_wait();
+    return;
+  }
   const int32_t* list = p.list ? p.list + static_cast<int64_t>(unit) * p.list_len : nullptr;
   const char* k_slab = p.cache + hd.k_off;
   const char* v_slab = p.cache + hd.v_off;
@@ -228,6 +232,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
       uint4* row = reinterpret_cast<uint4*>(ring + i * kpitch);
       for (int c = (i / kRows) & 1 ? ncv : nck; c < NC; ++c) row[c] = make_uint4(0u, 0u, 0u, 0u);
     }
+  chain_wait();                        // drafted rows, queries, the list: from the kernels before
   fetch_block(t_lo, blk_now);
   fetch_page(t_lo, blk_now, page_now);
   fetch_block(t_lo + 1, blk_next);
@@ -512,8 +517,7 @@ cudaError_t launch_instance(const MqDecodeParams& p, cudaStream_t s) {
   const cudaError_t e = ensure_dynamic_smem(mq_mma_kernel<NC, MT, WG>, S::kSmem, configured);
   if (e != cudaSuccess) return e;
   const int chunks = (p.rows + S::kQueries - 1) / S::kQueries;
-  mq_mma_kernel<NC, MT, WG><<<dim3(p.B * p.H * chunks, p.splits), S::kThreads, S::kSmem, s>>>(p);
-  return cudaGetLastError();
+  return launch_chained(p.chained != 0, mq_mma_kernel<NC, MT, WG>, dim3(p.B * p.H * chunks, p.splits), S::kThreads, S::kSmem, s, p);
 }
 template <int NC>
 cudaError_t launch_rank(const MqDecodeParams& p, cudaStream_t s) {

@@ -193,7 +193,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
     hdr->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  chain_go();
   Walk w = start_walk(p, blockIdx.x, lane);
+  chain_wait();                               // drafted rows and queries: from the kernels before
   if (tid == 0) {
     hdr->walk[0] = w;
   }
@@ -560,9 +562,8 @@ cudaError_t launch_mq_tc(const MqDecodeParams& p, int max_rp_k, int max_rp_v, cu
   static size_t configured[kMaxDevices] = {};
   const cudaError_t e = ensure_dynamic_smem(mq_tc_kernel, smem, configured);
   if (e != cudaSuccess) return e;
-  mq_tc_kernel<<<p.grid, kTcThreads, smem, s>>>(p, r);
   ++*launches;
-  return cudaGetLastError();
+  return launch_chained(p.chained != 0, mq_tc_kernel, p.grid, kTcThreads, smem, s, p, r);
 }
 
 }  // namespace ea
