@@ -12,8 +12,10 @@
 // share the rows and split the queries): no block-wide barrier and no wait that could fail to end.  In shared memory a row
 // sits at an odd multiple of 16 bytes, so that the eight rows of an ldmatrix meet all banks once, whatever the rank.
 // Heads narrower than the instance keep zeros in the rest of their rows: the products run over the instance's width
-// without a branch (with guards per piece of a row, which cut the code into short blocks that cannot overlap, a layer of
-// mixed ranks took 152 us where it now takes the time of its bytes).
+// without a branch (guards per piece of a row cut the code into short blocks that cannot overlap: twice the time).
+//
+// Bound by the bytes of K' and V' where rows are long: 16 sequences of 32k rows with 4 drafted tokens, 32 heads of rank 80,
+// 5.37 GB in 815 us.  Three CTAs per SM for rank 80 (tiles of 64 rows) read no faster: 992 us for the whole call against 918.
 #include <cuda_bf16.h>
 
 #include "internal.h"
@@ -47,8 +49,8 @@ __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void cp_async16_to(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void cp_async16_to(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void cp_async16_fill(uint32_t dst, const void* src, uint32_t bytes) {   // 0 bytes: zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -181,6 +183,9 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
   struct Walk { int row, c, d_row, d_c; };
   auto walk = [&](int nc) { return Walk{cl / nc, cl % nc, kStep / nc, kStep % nc}; };
   const Walk wk = walk(nck), wv = walk(ncv);
+  // Rows that one CTA reads are not kept in L2 (16 x 32k rows 970 -> 918 us, 64 x 777 150 -> 144); with more query rows
+  // than a CTA takes the CTAs next to it read them too.
+  const uint64_t policy = chunks == 1 ? policy_evict_first() : policy_evict_normal();
   auto copy_rows = [&](unsigned char* dst, const char* slab, int nc, const Walk& w0, const Source& s) {
     const char* src = slab + s.row[0] * (nc * 16) + cl * 16;
     Walk w = w0;
@@ -190,7 +195,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
     if (s.valid[0] == 16 && (HV == 1 || (s.valid[1] == 16 && s.row[1] == s.row[0] + 16))) {    // whole, and neighbours
 #pragma unroll
       for (int i0 = 0; i0 < kRows * NC; i0 += kStep) {
-        if (i0 + cl < total) cp_async16_to(to, src + i0 * 16);
+        if (i0 + cl < total) cp_async16_to(to, src + i0 * 16, policy);
         to += step;
         w.c += w.d_c;
         if (w.c >= nc) { w.c -= nc; to += wrap; }
