@@ -265,7 +265,8 @@ ea_status eigen_attn_quant_layout(eigen_attn_t h, int32_t head, size_t* slab_off
  * positions: drafted token t sits at len_b + (number of other tokens in its mask); only with group 1.  Not with a rotary
  * embedding (EA_ERR_UNSUPPORTED).  flags: EA_Q_PREPROJECTED (d_q: packed [B][T][group * sum rp_k], head h at group *
  * offs_k[h], query head i of its group rp_k[h] further each), EA_KV_PREPROJECTED, EA_OUT_LOWRANK (packed like q with rp_v).
- * The call can be captured into a CUDA graph; replays use the lengths of the capture and the mask's present contents.
+ * The call can be captured into a CUDA graph; replays use the lengths of the capture (the drafted rows are written where
+ * they were then: do not replay once rows were added there) and the mask's present contents.
  *
  * tree_bytes:   size of the scratch for max_tokens (1..64) drafted tokens and `group` query heads per K/V head.
  * tree_attach:  hands the library that DEVICE buffer (256-byte aligned, owned by the caller); NULL detaches.  Calls of one
@@ -297,7 +298,9 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
  * sparse_attach: hands over that DEVICE buffer (256-byte aligned, owned by the caller); no block has bounds yet.  NULL
  *                detaches.  Synchronises `cuda_stream`.
  * sparse_sync:   bounds of every complete block that has none yet; asynchronous.  Call it after rows were added:
- *                decode_sparse refuses (EA_ERR_INVALID_ARG) while a block it would have to score has no bounds.
+ *                decode_sparse refuses (EA_ERR_INVALID_ARG) while a block it would have to score has no bounds.  Rows
+ *                that the caller rewrites in place, directly or by replaying a captured graph that adds rows, are not
+ *                noticed: call set_len or set_lens below them first, or attach again.
  * sparse_lens:   rows covered by bounds per sequence: HOST [batch].  Shortening a sequence (set_len, set_lens) forgets the
  *                bounds of the blocks it no longer fills; changing the page table forgets all.
  * sparse_layout: where head `head`'s bounds live: byte offset of its slab [B][seq_blocks][2][rp_k] in the cache dtype
@@ -354,7 +357,8 @@ ea_status eigen_attn_get_lens(eigen_attn_t h, int32_t* lens);
  * Available for eigen_attn_append_kv, _decode, _decode_step(_host), _decode_static, _set_len(s), and
  * eigen_attn_prefill (which then runs on the CUDA cores), and with a rotary embedding for all of these and for
  * eigen_attn_decode_gqa when page_rows divides n_max (a page then lies inside one sequence's slab, which the tiled
- * copies of the rotary decode kernel need); not (EA_ERR_UNSUPPORTED) with a quantised cache, nor
+ * copies of the rotary decode kernel need), for eigen_attn_decode_tree, _tree_commit, _sparse_sync and _decode_sparse; not
+ * (EA_ERR_UNSUPPORTED) with a quantised cache, nor
  * eigen_attn_decode_gqa without a rotary embedding.  batch * pages_per_seq entries must fit the table area of the workspace
  * (batch * batch * n_max / 128 entries, at most 4 Mi).  Uploaded on the stream (asynchronous; the array may be reused
  * when the call returns): later calls must run on that stream or be ordered after it. */

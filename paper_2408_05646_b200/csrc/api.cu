@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <new>
+#include <utility>
 #include <vector>
 
 #include <cuda.h>   // CUtensorMap and its enums only; the encoder is resolved at run time, libcuda is not linked
@@ -1563,7 +1564,12 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
   if (!room_for(h, T, &bad))
     return fail(h, EA_ERR_CAPACITY, "tree_commit: %d drafted rows exceed the capacity of sequence %d", T, bad);
   bool equal = true;
-  std::vector<int32_t> lens(B);
+  std::vector<int32_t> lens;
+  try {
+    lens.resize(B);
+  } catch (const std::bad_alloc&) {
+    return fail(h, EA_ERR_CAPACITY, "tree_commit: out of host memory");
+  }
   for (int b = 0; b < B; ++b) {
     const int32_t c = h_counts[b];
     if (c < 0 || c > T) return fail(h, EA_ERR_INVALID_ARG, "tree_commit: counts[%d] = %d outside [0, %d]", b, c, T);
@@ -1613,9 +1619,13 @@ ea_status eigen_attn_sparse_bytes(eigen_attn_t h, int32_t block_rows, size_t* by
   if (!h || !bytes) return EA_ERR_INVALID_ARG;
   const ea_status st = check_block(h, "sparse_bytes", block_rows);
   if (st != EA_OK) return st;
-  SparseLayout S;
-  make_sparse_layout(h, block_rows, &S);
-  *bytes = S.bytes;
+  try {
+    SparseLayout S;
+    make_sparse_layout(h, block_rows, &S);
+    *bytes = S.bytes;
+  } catch (const std::bad_alloc&) {
+    return fail(h, EA_ERR_CAPACITY, "sparse_bytes: out of host memory");
+  }
   return EA_OK;
 }
 
@@ -1629,7 +1639,13 @@ ea_status eigen_attn_sparse_attach(eigen_attn_t h, int32_t block_rows, void* d_b
   if (st != EA_OK) return st;
   if (reinterpret_cast<uintptr_t>(d_buf) % kAlign) return fail(h, EA_ERR_INVALID_ARG, "sparse_attach: buffer not 256-byte aligned");
   SparseLayout S;
-  make_sparse_layout(h, block_rows, &S);
+  std::vector<int32_t> lens;
+  try {
+    make_sparse_layout(h, block_rows, &S);
+    lens.assign(h->desc.batch, 0);
+  } catch (const std::bad_alloc&) {
+    return fail(h, EA_ERR_CAPACITY, "sparse_attach: out of host memory");
+  }
   if (bytes < S.bytes) return fail(h, EA_ERR_CAPACITY, "sparse_attach: %zu bytes given, %zu needed", bytes, S.bytes);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaMemcpyAsync(d_buf, S.slab.data(), sizeof(int64_t) * S.slab.size(), cudaMemcpyHostToDevice, s);
@@ -1638,8 +1654,8 @@ ea_status eigen_attn_sparse_attach(eigen_attn_t h, int32_t block_rows, void* d_b
   h->sp_buf = static_cast<char*>(d_buf);
   h->sp_shift = 0;
   while ((1 << h->sp_shift) < block_rows) ++h->sp_shift;
-  h->sp = S;
-  h->sp_len.assign(h->desc.batch, 0);
+  h->sp = std::move(S);
+  h->sp_len.swap(lens);
   return EA_OK;
 }
 

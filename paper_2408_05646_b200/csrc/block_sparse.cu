@@ -381,6 +381,7 @@ static cudaError_t launch_scores_t(const SparseParams& p, int max_rp_k, cudaStre
   const int64_t chunks = (p.max_blocks - p.sink - p.recent + kScoreBlocks - 1) / kScoreBlocks, units = static_cast<int64_t>(p.B) * p.H;
   int64_t steps = units * chunks / (5 * 148);
   steps = steps < 1 ? 1 : steps > 3 ? 3 : steps;
+  if (chunks > 65535 * steps) steps = (chunks + 65534) / 65535;              // (the second grid dimension)
   return launch_chained(true, block_scores_kernel<T>, dim3(static_cast<unsigned>(units), static_cast<unsigned>((chunks + steps - 1) / steps)),
                         kScoreThreads, smem, s, p, static_cast<int>(steps));
 }

@@ -300,11 +300,11 @@ __global__ void __launch_bounds__(kQ64Threads) mq_query64_kernel(const MqQueryPa
   chain_go();
   __shared__ double x[kQ64Rows][128];
   __shared__ double part[kQ64Threads][kQ64Rows];
-  const int h = blockIdx.x, tid = threadIdx.x;
+  const int h = blockIdx.y, tid = threadIdx.x;
   const int rp_k = p.heads[h].rp_k;
   const float* U = p.basis + p.heads[h].uk_off;
   // rows of a head: query head g of sequence b is row b * group + g; this CTA's four
-  const int r0 = blockIdx.y * kQ64Rows, nr = min(kQ64Rows, p.B * p.group - r0);
+  const int r0 = blockIdx.x * kQ64Rows, nr = min(kQ64Rows, p.B * p.group - r0);
   const int shares = kQ64Threads / rp_k;                     // at least four
   const int share = tid / rp_k, c = tid - share * rp_k;
   const int each = (p.d_head + shares - 1) / shares, d0 = share * each, d1 = min(p.d_head, d0 + each);
@@ -704,7 +704,7 @@ cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, u
     if (dtype == 0) mq_copy_query_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(p);
     else mq_copy_query_kernel<float><<<grid, 128, 0, s>>>(p);
   } else {
-    const dim3 grid(p.H, (p.B * p.group + kQ64Rows - 1) / kQ64Rows);
+    const dim3 grid((p.B * p.group + kQ64Rows - 1) / kQ64Rows, p.H);
     if (dtype == 0) mq_query64_kernel<__nv_bfloat16><<<grid, kQ64Threads, 0, s>>>(p);
     else mq_query64_kernel<float><<<grid, kQ64Threads, 0, s>>>(p);
   }

@@ -123,9 +123,10 @@ def check(got, want, slack, dtype, what):
     assert over[at] <= 0, f"{what}: {got[at]} for {want[at]} at {at}, {over[at]:.3e} over the bound (slack {slack[at]:.3e})"
 
 
-def tree_expected(c, q, masks, T, lowrank=False, rank_q=None):
+def tree_expected(c, q, masks, T, lowrank=False, rank_q=None, units=None):
     """(expected, slack) [batch][T][H * group][d] (lowrank: a list per head of [batch][T][group][r]) from the rows the cache
-    holds after the call.  rank_q: the queries as rank-r rows, a function (b, h, i) -> [T, r]."""
+    holds after the call.  rank_q: the queries as rank-r rows, a function (b, h, i) -> [T, r].  units: only these (b, h); the
+    rest stays zero."""
     want = np.zeros((c.batch, T, c.H * c.group, c.d))
     slack = np.zeros_like(want)
     low = [[np.zeros((c.batch, T, c.group, r)) for r in c.rv] for _ in range(2)]
@@ -133,6 +134,8 @@ def tree_expected(c, q, masks, T, lowrank=False, rank_q=None):
     for b in range(c.batch):
         n = c.lens[b]
         for h in range(c.H):
+            if units is not None and (b, h) not in units:
+                continue
             K, V = c.rows(b, h, n + T, "k"), c.rows(b, h, n + T, "v")
             slope = c.slopes[h] if c.slopes is not None else 0.0
             for i in range(c.group):
@@ -166,7 +169,8 @@ def sparse_expected(c, q, block, n_blocks, sink, recent):
             qp = x @ np.float64(c.U_k[h])
             blocks = ts.choose_blocks(qp, K, block, n_blocks, sink, recent, c.d, slope)
             index[b, h, :len(blocks)] = blocks
-            rows = [j for j in range(n) if j // block in set(blocks)]
+            chosen = set(blocks)
+            rows = [j for j in range(n) if j // block in chosen]
             for i in range(c.group):
                 s = K[rows] @ qp[i] / math.sqrt(c.d) - slope * ((n - 1) - np.asarray(rows, np.float64))
                 w = orc.softmax_rows(s[None])[0]

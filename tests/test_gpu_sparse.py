@@ -40,6 +40,9 @@ SHAPES = [
     (BF16, 2, 2, 5, 40, [40, 17], [24, 40], [900, 450], 64, 5, 1, 1, 0),
     (BF16, 2, 2, 1, 128, [80, 64], [64, 80], [1023, 512], 64, 5, 1, 1, 128),         # pages of 128 rows, shuffled
     (BF16, 1, 1, 2, 128, [80], [80], [5000], 16, 100, 4, 8, 256),                    # more blocks than a CTA's threads
+    (BF16, 2, 1, 1, 64, [32], [32], [40000, 17000], 16, 1500, 3, 2, 0),              # several segments of keys, many of them chosen
+    (BF16, 5, 30, 1, 16, [8] * 30, [16] * 30, [10240] * 5, 16, 40, 1, 1, 0),         # several steps of scores per CTA
+    (BF16, 64, 33, 1, 16, [16] * 33, [8] * 33, [96 - i for i in range(64)], 16, 4, 1, 1, 0),      # many query rows in the merge
     (FP32, 1, 4, 1, 64, [32] * 4, [32] * 4, [500], 16, 8, 1, 1, 0),
     (FP32, 2, 2, 2, 80, [33, 80], [80, 12], [640, 200], 32, 6, 1, 2, 128),
     (BF16, 1, 1, 1, 64, [32], [32], [40], 64, 50, 3, 4, 0),                          # a budget beyond the cache
@@ -97,6 +100,81 @@ def test_equal_scores_go_to_the_lower_block_and_zero_queries_choose_in_order(B):
     for q in (randn((1, 1, 2, 128), 69, BF16), torch.zeros((1, 1, 2, 128), dtype=BF16, device="cuda")):
         _, index = c.lay.decode_sparse(q, 6, return_index=True)
         assert index.tolist() == [[[0, 1, 2, 3, 4, 14]] * 2]
+
+
+def test_equal_scores_across_segments(B):
+    """One block's rows over and over, 2500 blocks of them, with a few others in between: those are chosen, and of the equal
+    ones the first, wherever in the list they lie."""
+    c = Case(B, BF16, 1, 1, 1, 64, [32], [32], [16], 40064, seed=68)
+    k, v = c.k[:, :, :, :], c.v[:, :, :, :]
+    c.lay.append_kv(k.repeat(1, 2499, 1, 1), v.repeat(1, 2499, 1, 1))
+    slab = c.lay.cache_rows(0, "k")
+    q = randn((1, 1, 1, 64), 70, BF16)
+    rank_q = np64(q)[0, 0, 0] @ np.float64(c.U_k[0])
+    big = torch.tensor(np.sign(rank_q) * 9.0, device="cuda").to(BF16)
+    high = [700, 1500, 2400]
+    for j in high:
+        slab[0, 16 * j + 5, :32] = big
+    c.lens = [40000]
+    c.lay.sparse_attach(16)
+    c.lay.sparse_sync()
+    for n_blocks in (6, 1200, 2300):
+        out, index = c.lay.decode_sparse(q, n_blocks, return_index=True)
+        middle = [j for j in range(1, 2499) if j not in high]
+        want = sorted([0, 2499] + high + middle[:n_blocks - 5])
+        assert index[0, 0].tolist() == want
+        e, slack, idx = sparse_expected(c, q, 16, n_blocks, 1, 1)
+        assert idx[0, 0].tolist() == want
+        check(out, e, slack, BF16, f"{n_blocks} blocks")
+
+
+def test_side_stream_and_two_layers_at_once(B):
+    """Two layers with buffers of their own on two streams: each call's launches depend on their own stream alone."""
+    cs = [Case(B, BF16, 2, 4, 2, 128, [80] * 4, [80] * 4, [6000, 3000], 6144, seed=s) for s in (105, 107)]
+    qs = [randn((2, 1, 8, 128), 109 + i, BF16, 2.0) for i in range(2)]
+    for c in cs:
+        c.lay.sparse_attach(32)
+        c.lay.sparse_sync()
+    want = [c.lay.decode_sparse(q, 12, group=2) for c, q in zip(cs, qs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.zeros_like(w) for _ in range(30)] for w in want]
+    for i in range(30):
+        for c, q, s, o in zip(cs, qs, streams, outs):
+            c.lay.decode_sparse(q, 12, group=2, out=o[i], stream=s)
+    torch.cuda.synchronize()
+    for w, o in zip(want, outs):
+        assert all(torch.equal(w, x) for x in o)
+
+
+def test_blocks_beyond_32_bit_offsets(B):
+    """A key slab of 2 GiB per sequence; a handful of blocks near the end of the second sequence score highest."""
+    n_max, d, n, block = 2 ** 23 + 128, 128, 2 ** 23 + 90, 128
+    U = np.eye(d, dtype=np.float32)
+    lay = B.EigenAttnLayer(2, 1, d, n_max, BF16, [U], [U])
+    for which in "kv":
+        lay.cache_rows(0, which).zero_()
+    lay.set_lens([1, n])
+    lay.sparse_attach(block)
+    far = [n // block - 3, n // block - 1000, 40000]
+    rows = randn((2, 3, d), 3, BF16)
+    rows[0, :, 0] = 32.0
+    for i, j in enumerate(far):
+        lay.cache_rows(0, "k")[1, block * j + 17 * i] = rows[0, i]
+        lay.cache_rows(0, "v")[1, block * j + 17 * i] = rows[1, i]
+    lay.sparse_sync()
+    q = randn((2, 1, 1, d), 5, BF16)
+    q[:, :, :, 0] = 32.0
+    out, index = lay.decode_sparse(q, 5, return_index=True)
+    last = (n + block - 1) // block - 1
+    assert index[:, 0].tolist() == [[0, -1, -1, -1, -1], sorted([0, last] + far)]
+    s = np64(rows[0]) @ np64(q[1, 0, 0]) / np.sqrt(d)
+    w = np.exp(s - s.max())
+    w /= w.sum()
+    e_s = (2.0 ** -16 + (2 * d + 4) * 2.0 ** -23) * (np.abs(np64(rows[0])) @ np.abs(np64(q[1, 0, 0]))).max() / np.sqrt(d)
+    assert s.min() > 60                                # the zero rows beside them: 640 times e^-60
+    e_w = 2.2 * e_s + 2.0 ** -15 + 1000 * 2.0 ** -24
+    check(out[1, 0, 0], w @ np64(rows[1]), (2 * e_w + (d + 2) * 2.0 ** -22) * (w @ np.abs(np64(rows[1]))), BF16, "far blocks")
 
 
 def test_a_budget_that_covers_everything_is_ordinary_decode(B):

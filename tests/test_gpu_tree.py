@@ -50,6 +50,8 @@ SHAPES = [
     (BF16, 2, 1, 2, 128, [80], [80], [6000, 5000], 20, "tree", 0),               # many tiles for one unit
     (BF16, 1, 2, 3, 128, [64, 48], [64, 40], [1500], 60, "any", 0),              # 180 query rows, narrow heads
     (BF16, 2, 1, 1, 128, [80], [80], [200, 100], 40, "tree", 256),               # pages that do not divide n_max (384 rows)
+    (BF16, 2, 1, 3, 128, [80], [80], [300, 0], 20, "any", 0),                    # empty masks beside no cached row, 60 query rows
+    (BF16, 40, 1, 4, 64, [32], [32], [37 * i % 290 for i in range(40)], 8, "tree", 0),     # more sequences than a warp has lanes
     (FP32, 1, 4, 1, 64, [32] * 4, [32] * 4, [512], 5, "tree", 0),
     (FP32, 2, 2, 2, 80, [33, 80], [80, 12], [100, 0], 17, "any", 0),
     (FP32, 2, 2, 1, 128, [128, 64], [128, 32], [260, 131], 64, "tree", 128),
@@ -79,6 +81,104 @@ def test_tree_matches_the_definition(B, dtype, batch, H, group, d, rk, rv, lens,
     c.lay.set_option(B.EA_OPT_DECODE_CTAS, 0)
     assert torch.equal(c.lay.decode_tree(q, k, v, mask_tensor(masks), group=group), out)      # the same again, bit for bit
     c.lay.poll_status()
+
+
+@pytest.mark.parametrize("dtype,batch,H,group,d,r,T,off", [
+    (BF16, 8, 25, 1, 64, 32, 64, 0),                   # 128 rows per CTA in the projection, 64 in the merge
+    (BF16, 8, 25, 1, 64, 32, 64, 1),                   # tensors that begin one element behind a 16-byte boundary
+    (BF16, 3, 14, 4, 128, 72, 24, 1),                  # 64 rows per CTA in the projection, d_head 128
+    (FP32, 8, 25, 1, 40, 24, 64, 1),
+    (FP32, 2, 2, 1, 64, 32, 3, 1),                     # few rows
+    (BF16, 2, 2, 1, 64, 32, 3, 1),
+])
+def test_many_rows_and_unaligned_tensors(B, dtype, batch, H, group, d, r, T, off):
+    """Every shape of the projection and the merge: stored rows are bit for bit those of append_kv, whatever the alignment."""
+    lens = [(29 * i) % 41 for i in range(batch)]
+    rk, rv = [r - 3 * (h % 4) for h in range(H)], [r - 5 * (h % 3) for h in range(H)]
+    a = Case(B, dtype, batch, H, group, d, rk, rv, lens, 128, seed=47)
+    ref = Case(B, dtype, batch, H, group, d, rk, rv, lens, 128, seed=47)
+    q, k, v = drafted(a, T, 141)
+    masks, _ = trees(batch, T, 17)
+    m = mask_tensor(masks)
+    a.lay.tree_attach(T, group)
+
+    def moved(x):                                      # the same numbers, `off` elements further
+        flat = torch.full((x.numel() + 8,), 3.0, dtype=dtype, device="cuda")
+        flat[off:off + x.numel()] = x.reshape(-1)
+        return flat, flat[off:off + x.numel()].view(x.shape)
+    flat, out = moved(torch.full_like(q, -7.0))
+    a.lay.decode_tree(moved(q)[1], moved(k)[1], moved(v)[1], m, group=group, out=out)
+    assert (flat[:off] == 3.0).all() and (flat[off + q.numel():] == 3.0).all()
+    units = {(b, h) for b in range(batch) for h in range(H) if (b * H + h) % (batch * H // 4) == 0 or (b, h) == (batch - 1, H - 1)}
+    want, slack = tree_expected(a, q, masks, T, units=units)
+    for b, h in units:
+        at = slice(h * group, (h + 1) * group)
+        check(out[b:b + 1, :, at], want[b:b + 1, :, at], slack[b:b + 1, :, at], dtype, f"unit {b, h}")
+    assert torch.isfinite(out).all()
+    ref.lay.append_kv(k, v)                            # the same rows by the ordinary way
+    a.lay.tree_commit([list(range(T))] * batch, T)
+    assert a.lay.lens() == ref.lay.lens()
+    for h in range(H):
+        for which in "kv":
+            x, y = a.lay.cache_rows(h, which), ref.lay.cache_rows(h, which)
+            for b in range(batch):
+                assert torch.equal(x[b, :lens[b] + T], y[b, :lens[b] + T]), (b, h, which)
+
+
+def test_commit_of_more_sequences_than_one_launch_takes(B):
+    batch, T = 150, 6
+    lens = [(7 * i) % 50 for i in range(batch)]
+    c = Case(B, BF16, batch, 1, 1, 16, [8], [16], lens, 64, seed=61)
+    q, k, v = drafted(c, T, 161)
+    masks, _ = trees(batch, T, 21)
+    c.lay.tree_attach(T)
+    c.lay.decode_tree(q, k, v, mask_tensor(masks))
+    g = np.random.default_rng(5)
+    paths = [sorted(int(x) for x in g.permutation(T)[:g.integers(0, T + 1)]) for _ in range(batch)]
+    slabs = {w: np64(c.lay.cache_rows(0, w)) for w in "kv"}
+    c.lay.tree_commit(paths, T)
+    assert c.lay.lens() == [n + len(p) for n, p in zip(lens, paths)]
+    for w in "kv":
+        got = np64(c.lay.cache_rows(0, w))
+        for b in range(batch):
+            want = slabs[w][b].copy()
+            want[lens[b]:lens[b] + len(paths[b])] = slabs[w][b][[lens[b] + s for s in paths[b]]]
+            assert np.array_equal(got[b], want), (b, w)
+
+
+@pytest.mark.parametrize("T", [4, 24])                 # warp-level products, tcgen05 products
+def test_rows_beyond_32_bit_offsets(B, T):
+    """A head's slab of 4 GiB: rows of the second sequence lie at byte offsets past 2^31 and 2^32.  All rows are zero but the
+    last 50, whose scores are some 60 above: the 8.4 million others together weigh e^-60 * 2^23 of them."""
+    n_max, d, n = 2 ** 23 + 256, 128, 2 ** 23 + 100
+    U = np.eye(d, dtype=np.float32)
+    lay = B.EigenAttnLayer(2, 1, d, n_max, BF16, [U], [U])
+    for which in "kv":
+        lay.cache_rows(0, which).zero_()
+    lay.set_lens([40, n])
+    rows = randn((2, 50, d), 3, BF16)
+    rows[0, :, 0] = 32.0                               # times the query's 32 / sqrt(128): a score of 90, the rest moves it by ~3
+    lay.cache_rows(0, "k")[1, n - 50:n] = rows[0]
+    lay.cache_rows(0, "v")[1, n - 50:n] = rows[1]
+    q, k, v = (randn((2, T, 1, d), 5 + i, BF16) for i in range(3))
+    q[:, :, :, 0] = 32.0
+    k[:, :, :, 0] = 32.0
+    masks, _ = trees(2, T, 1)
+    lay.tree_attach(T)
+    out = lay.decode_tree(q, k, v, mask_tensor(masks))
+    lay.poll_status()
+    assert torch.equal(lay.cache_rows(0, "k")[1, n:n + T], k[1, :, 0]) and torch.equal(lay.cache_rows(0, "v")[1, n:n + T], v[1, :, 0])
+    K, V = np.concatenate([np64(rows[0]), np64(k[1, :, 0])]), np.concatenate([np64(rows[1]), np64(v[1, :, 0])])
+    for t in range(T):
+        keep = [j for j in range(50 + T) if j < 50 or masks[1][t] >> (j - 50) & 1]
+        s = K[keep] @ np64(q[1, t, 0]) / np.sqrt(d)
+        assert s.min() > 60
+        w = np.exp(s - s.max())
+        w /= w.sum()
+        e_s = (2.0 ** -16 + (2 * d + 4) * 2.0 ** -23) * (np.abs(K[keep]) @ np.abs(np64(q[1, t, 0]))).max() / np.sqrt(d)
+        e_w = 2.2 * e_s + 2.0 ** -15 + 2 ** 23 * np.exp(-60.0) + 200 * 2.0 ** -24
+        slack = (2 * e_w + (d + 2) * 2.0 ** -22) * (w @ np.abs(V[keep]))
+        check(out[1, t, 0], w @ V[keep], slack, BF16, f"token {t}")
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
