@@ -1382,8 +1382,10 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
   const int max_rp = L.max_rp_k > L.max_rp_v ? L.max_rp_k : L.max_rp_v;
   // Trees with more than 16 query rows: tcgen05 products, where the layer's slabs have tensor maps (pages then have to lie
   // inside one sequence's slab) and no bias goes onto the scores.
-  const bool tc = mma && p.tail > 0 && p.rows > 16 && h->tmaps_ok && !h->alibi && h->opt_tree_impl != 1 &&
+  bool tc = mma && p.tail > 0 && p.rows > 16 && h->tmaps_ok && !h->alibi && h->opt_tree_impl != 1 &&
                   (!h->paged || h->desc.n_max % (1 << h->page_shift) == 0);
+  // (its tiles are counted in 32 bits)
+  tc = tc && ((end >> 7) + 1) * p.B * p.H * ((p.rows + ea::kMqTcRows - 1) / ea::kMqTcRows) < INT32_MAX;
   const ea::MqShape shape = mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::kMqSimtShape;
   p.tile_shift = tc ? 7 : shape.tile_shift;
   const int tile = 1 << p.tile_shift;
@@ -1402,6 +1404,8 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
     if (grid > kMqTcCtas) grid = kMqTcCtas;
     if (grid > p.total_tiles) grid = p.total_tiles;
     p.grid = static_cast<int32_t>(grid);
+    p.cta_tiles = static_cast<int32_t>(p.total_tiles / grid);
+    p.cta_extra = static_cast<int32_t>(p.total_tiles % grid);
     p.slot_rows = slot_rows_of(p.rows);
   } else {
     // Tiles of a piece: the CTAs run in waves of resident ones, each pays a start-up worth a tile or two; pieces are cut to

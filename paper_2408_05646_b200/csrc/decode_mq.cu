@@ -466,6 +466,11 @@ struct Pieces {
   int64_t step;
   int count;
 };
+// The CTA of the tcgen05 kernel that has tile x: the first cta_extra CTAs have a tile more.
+__device__ __forceinline__ int cta_of_tile(const MqDecodeParams& p, int x) {
+  const int cut = p.cta_extra * (p.cta_tiles + 1);
+  return x < cut ? x / (p.cta_tiles + 1) : p.cta_extra + (x - cut) / p.cta_tiles;
+}
 // Equal pieces of an item: [unit * rows + row][splits].  Ranges over all items (grid > 0): the CTAs whose ranges meet the
 // item; `before` = tiles of the sequences in front of b (one run of query rows).
 __device__ __forceinline__ Pieces pieces_of(const MqDecodeParams& p, int unit, int row, int64_t before) {
@@ -476,8 +481,7 @@ __device__ __forceinline__ Pieces pieces_of(const MqDecodeParams& p, int unit, i
     return {p.partials + (static_cast<int64_t>(unit) * p.rows + row) * p.splits * p.part_stride, p.part_stride, max(1, (tiles + p.per - 1) / p.per)};
   const int chunks = (p.rows + kMqTcRows - 1) / kMqTcRows, chunk = row / kMqTcRows;
   const int64_t x = (h * p.head_tiles + before) * chunks + static_cast<int64_t>(chunk) * tiles;
-  const int c0 = static_cast<int>(((x + 1) * p.grid - 1) / p.total_tiles);             // the CTA that has tile x
-  const int c1 = static_cast<int>(((x + tiles) * p.grid - 1) / p.total_tiles);
+  const int c0 = cta_of_tile(p, static_cast<int>(x)), c1 = cta_of_tile(p, static_cast<int>(x) + tiles - 1);
   const int64_t slot = static_cast<int64_t>(unit) * chunks + chunk + c0;
   return {p.partials + (slot * p.slot_rows + (row - chunk * kMqTcRows)) * p.part_stride, static_cast<int64_t>(p.slot_rows) * p.part_stride,
           c1 - c0 + 1};

@@ -35,12 +35,11 @@ using namespace tc;
 constexpr int kKeys = 128;                    // cached rows of a tile
 constexpr int kAtom = kKeys * 128;            // one swizzled atom column of a tile: 128 rows x 64 elements
 constexpr int kBox = 64 * 128;                // bytes of one TMA box
-constexpr int kParts = 4, kPart = kKeys / kParts;            // threads per query row, rows of a tile each looks after
-constexpr int kSoftmax = kParts * kTile;      // softmax threads
-constexpr int kSWarp = kSoftmax / 32, kPvWarp = kSWarp + 1, kLoadWarp = kSWarp + 2;   // ... and the last: K' tiles, V' tiles
+constexpr int kBufs = 3;                      // S buffers, each with a softmax group of its own: a thread per query row
+constexpr int kSoftmax = kBufs * kTile;       // softmax threads
+constexpr int kSWarp = kSoftmax / 32, kLoadWarp = kSWarp + 2;       // S, O'; K' tiles, V' tiles
 constexpr int kTcThreads = kSoftmax + 128;
 constexpr int kMaxStages = 6;
-constexpr int kBufs = 3;                      // S buffers
 
 // A walk over the items of a CTA's range: head, sequence, run of query rows, and the tiles of it that the CTA has.
 struct Walk {
@@ -48,7 +47,7 @@ struct Walk {
   int rp_k, rp_v;            // of the head
   int n_b, tiles;            // cached rows and tiles of the item
   int t, nt;                 // first tile and number of tiles of the piece
-  int64_t left;              // tiles of the CTA's range behind this piece
+  int left;                  // tiles of the CTA's range behind this piece
   __device__ __forceinline__ void sequence(const MqDecodeParams& p) {
     n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
     tiles = (n_b + p.tail + kKeys - 1) / kKeys;
@@ -58,7 +57,7 @@ struct Walk {
     rp_v = p.heads[h].rp_v;
   }
   __device__ __forceinline__ void piece() {
-    nt = static_cast<int>(left < tiles - t ? left : tiles - t);
+    nt = min(left, tiles - t);
     left -= nt;
   }
   __device__ __forceinline__ bool next(const MqDecodeParams& p) {
@@ -78,48 +77,49 @@ struct Walk {
   }
 };
 struct __align__(16) TcHeader {
+  // one arrival each
   unsigned long long k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
-  unsigned long long q_full;
-  unsigned long long s_full[kBufs], p_full[kBufs], o_done[kBufs];       // per S buffer
-  unsigned long long odd[2];                  // drafted tokens with a value that is not finite; pieces take turns
+  unsigned long long s_full[kBufs], o_done[kBufs];                      // per S buffer
+  unsigned long long ref_ready[kBufs][4];     // per S buffer and 32 query rows: the row references behind its tile
+  unsigned long long p_full[kBufs], o_free, q_full, sums_ready;         // arrivals of one group, of two
+  unsigned long long odd[3];                  // drafted tokens with a value that is not finite; pieces take turns
   uint32_t tmem_base;
   int abort_flag;
-  Walk walk[3];                               // the softmax warps' walk (they have no registers to spare for it): the piece
-  int more[3];                                //   before, which some still finish, this one and the next
-  float exch[kParts][kTile];                  // row maxima (main loop), row sums (epilogue)
+  float ref[kTile];                           // reference of every query row behind the newest tile
+  float sums[2][kBufs - 1][kTile];            // row sums of the other groups at a piece's end; pieces take turns
 };
+constexpr int kSingles = 4 * kMaxStages + 6 * kBufs;         // barriers with one arrival
 constexpr int kHeaderBytes = 3072;
 static_assert(sizeof(TcHeader) <= kHeaderBytes, "header outgrew its area");
 
-__device__ __forceinline__ bool softmax_barrier_or(bool pred) {    // the softmax threads
-  uint32_t out;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 q, %1, 0;\n\t"
-      "bar.red.or.pred p, 1, %2, q;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(out)
-      : "r"(pred ? 1u : 0u), "n"(kSoftmax)
-      : "memory");
-  return out != 0;
-}
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
-               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
-               : "memory");
-}
 __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t& hi, uint32_t& lo) {
   hi = pack_bf16(x0, x1);
   lo = pack_bf16(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xffff0000u));
 }
+// tcgen05.wait::ld that the registers of a load under way depend on
+__device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
 __device__ __forceinline__ bool finite16(uint32_t bits16) { return (bits16 & 0x7f80u) != 0x7f80u; }
 
+// One lane of the warp.  A warp that issues tcgen05 products stays together and lets this lane do it, so that descriptors live
+// in uniform registers: 42 and 66 cycles for a product of 80 and 128 columns (40 and 64 are the tensor core's own), where a
+// branch on the lane number, with a move into a uniform register per operand, takes 83 and 92.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
 template <int KS>
 __device__ __forceinline__ void issue_s(uint32_t d, uint64_t dq, uint64_t q_part, uint64_t dk, uint32_t idesc) {
 #pragma unroll
-  for (int part = 0; part < 2; ++part)
+  for (int s = 0; s < KS; ++s)
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+    for (int part = 0; part < 2; ++part)
       mma_ss(d, dq + part * q_part + 16 * s, dk + (s >> 2) * (kAtom >> 4) + (s & 3) * 2, idesc, part > 0 || s > 0);
 }
 
@@ -129,24 +129,24 @@ struct Ring { int q_bytes, k_stages, k_stage, v_stages, v_stage; };      // shar
 __device__ Walk start_walk(const MqDecodeParams& p, int c, int lane) {
   Walk w;
   w.chunks = (p.rows + kTile - 1) / kTile;
-  const int64_t x = c * p.total_tiles / p.grid, end = (c + 1) * p.total_tiles / p.grid;
-  const int64_t per_head = p.head_tiles * w.chunks;          // head_tiles: tiles of all sequences
-  w.h = static_cast<int>(x / per_head);
+  const int x = c * p.cta_tiles + min(c, p.cta_extra);
+  const int per_head = static_cast<int>(p.head_tiles) * w.chunks;      // head_tiles: tiles of all sequences
+  w.h = x / per_head;
   w.head(p);
-  int64_t rest = x - w.h * per_head;
+  int rest = x - w.h * per_head;
   w.b = 0;
   if (p.deficit == nullptr) {
     w.sequence(p);
-    const int64_t each = static_cast<int64_t>(w.tiles) * w.chunks;
-    w.b = static_cast<int>(rest / each);
+    const int each = w.tiles * w.chunks;
+    w.b = rest / each;
     rest -= w.b * each;
   } else {
     for (int b0 = 0; b0 < p.B; b0 += 32) {
       const int tiles = b0 + lane < p.B ? (p.n - __ldg(p.deficit + b0 + lane) + p.tail + kKeys - 1) / kKeys : 0;
-      int64_t scan = static_cast<int64_t>(tiles) * w.chunks;
+      int scan = tiles * w.chunks;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, scan, d);
+        const int y = __shfl_up_sync(0xffffffffu, scan, d);
         if (lane >= d) scan += y;
       }
       const unsigned past = __ballot_sync(0xffffffffu, rest < scan);      // sequences that end behind the place
@@ -160,9 +160,9 @@ __device__ Walk start_walk(const MqDecodeParams& p, int c, int lane) {
     }
     w.sequence(p);
   }
-  w.chunk = static_cast<int>(rest / w.tiles);
-  w.t = static_cast<int>(rest - static_cast<int64_t>(w.chunk) * w.tiles);
-  w.left = end - x;
+  w.chunk = rest / w.tiles;
+  w.t = rest - w.chunk * w.tiles;
+  w.left = p.cta_tiles + (c < p.cta_extra ? 1 : 0);
   w.piece();
   return w;
 }
@@ -176,29 +176,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
-  if (tid == 0) {
-    for (int s = 0; s < kMaxStages; ++s) {
-      mbar_init(&hdr->k_full[s], 1);
-      mbar_init(&hdr->k_empty[s], 1);
-      mbar_init(&hdr->v_full[s], 1);
-      mbar_init(&hdr->v_empty[s], 1);
-    }
-    mbar_init(&hdr->q_full, kSoftmax);
-    for (int i = 0; i < kBufs; ++i) {
-      mbar_init(&hdr->s_full[i], 1);
-      mbar_init(&hdr->p_full[i], kSoftmax);
-      mbar_init(&hdr->o_done[i], 1);
-    }
-    hdr->odd[0] = hdr->odd[1] = 0;
-    hdr->abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
+  if (tid < kSingles + kBufs + 3) mbar_init(&hdr->k_full[0] + tid, tid < kSingles ? 1 : tid <= kSingles + kBufs ? kTile : 2 * kTile);
+  else if (tid >= 64 && tid < 64 + 3) hdr->odd[tid - 64] = 0;
+  else if (tid == 67) hdr->abort_flag = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   chain_go();
   Walk w = start_walk(p, blockIdx.x, lane);
   chain_wait();                               // drafted rows and queries: from the kernels before
-  if (tid == 0) {
-    hdr->walk[0] = w;
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -257,288 +241,327 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       // copies in flight must land before the CTA leaves; normally their consumers have waited for them
       for (int s = 0; s < stages && s < g; ++s) mbar_wait(&full[s], ((g - 1 - s) / stages) & 1u, p.status);
     }
-  } else if (warp == kSWarp) {
-    if (lane == 0) {
+  } else if (warp >= kSWarp) {
+    const bool lead = elect_one();
+    auto wait = [&](unsigned long long* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status)) != 0; };
+    bool ok = true;
+    int g = 0, piece = 0;
+    if (warp == kSWarp) {
       const uint32_t idesc = instr_desc(kKeys, false);
       const uint64_t dk0 = smem_desc_sw128(smem_u32(ring), 16, 1024);
       const int stages = rings.k_stages;
-      bool ok = true;
-      int g = 0, piece = 0;
       do {
         const int rpk16 = (w.rp_k + 15) & ~15;
         const uint64_t dq = smem_desc(smem_u32(q_tile), 128, (rpk16 >> 3) << 7);    // canonical tiles of 128 rows
         const uint64_t q_part = static_cast<uint64_t>(kTile * rpk16 * 2 >> 4);
-        ok = mbar_wait(&hdr->q_full, piece & 1u, p.status);
+        ok = wait(&hdr->q_full, piece & 1u);
         for (int i = 0; i < w.nt && ok; ++i, ++g) {
           const int st = g % stages, buf = g % kBufs;
-          ok = mbar_wait(&hdr->k_full[st], (g / stages) & 1u, p.status);
-          if (ok && g >= kBufs) ok = mbar_wait(&hdr->o_done[buf], (g / kBufs - 1) & 1u, p.status);    // P(g - 3) has been read
-          ok = ok && !*abort_flag;
+          ok = wait(&hdr->k_full[st], (g / stages) & 1u);
+          if (ok && g >= kBufs) ok = wait(&hdr->o_done[buf], (g / kBufs - 1) & 1u);       // P(g - 3) has been read
+          ok = ok && __all_sync(0xffffffffu, !*abort_flag);
           if (!ok) break;
           tc_fence_after();
           const uint64_t dk = dk0 + static_cast<uint64_t>(st) * (rings.k_stage >> 4);
           const uint32_t d = tmem + buf * 128;
-          switch (rpk16 >> 4) {
-            case 1: issue_s<1>(d, dq, q_part, dk, idesc); break;
-            case 2: issue_s<2>(d, dq, q_part, dk, idesc); break;
-            case 3: issue_s<3>(d, dq, q_part, dk, idesc); break;
-            case 4: issue_s<4>(d, dq, q_part, dk, idesc); break;
-            case 5: issue_s<5>(d, dq, q_part, dk, idesc); break;
-            case 6: issue_s<6>(d, dq, q_part, dk, idesc); break;
-            case 7: issue_s<7>(d, dq, q_part, dk, idesc); break;
-            default: issue_s<8>(d, dq, q_part, dk, idesc); break;
+          if (lead) {
+            switch (rpk16 >> 4) {
+              case 1: issue_s<1>(d, dq, q_part, dk, idesc); break;
+              case 2: issue_s<2>(d, dq, q_part, dk, idesc); break;
+              case 3: issue_s<3>(d, dq, q_part, dk, idesc); break;
+              case 4: issue_s<4>(d, dq, q_part, dk, idesc); break;
+              case 5: issue_s<5>(d, dq, q_part, dk, idesc); break;
+              case 6: issue_s<6>(d, dq, q_part, dk, idesc); break;
+              case 7: issue_s<7>(d, dq, q_part, dk, idesc); break;
+              default: issue_s<8>(d, dq, q_part, dk, idesc); break;
+            }
+            mma_commit(&hdr->s_full[buf]);
+            mma_commit(&hdr->k_empty[st]);
           }
-          mma_commit(&hdr->s_full[buf]);
-          mma_commit(&hdr->k_empty[st]);
+          __syncwarp();
         }
         ++piece;
       } while (ok && w.next(p));
       // the last commits' arrivals must have landed before the CTA may leave
-      if (ok) ok = mbar_wait(&hdr->k_empty[(g - 1) % stages], ((g - 1) / stages) & 1u, p.status);
-      if (!ok) *abort_flag = 1;
-    }
-  } else if (warp == kPvWarp) {
-    if (lane == 0) {
+      if (ok) ok = wait(&hdr->k_empty[(g - 1) % stages], ((g - 1) / stages) & 1u);
+    } else {
       const uint64_t dv0 = smem_desc_sw128(smem_u32(v_ring), kAtom, 1024);
       const int stages = rings.v_stages;
-      bool ok = true;
-      int g = 0;
       do {
         const uint32_t idesc = instr_desc((w.rp_v + 15) & ~15, true);
+        if (piece > 0) ok = wait(&hdr->o_free, (piece - 1) & 1u);                         // the piece before has read O'
+        ++piece;
         for (int i = 0; i < w.nt && ok; ++i, ++g) {
           const int st = g % stages, buf = g % kBufs;
-          ok = mbar_wait(&hdr->p_full[buf], (g / kBufs) & 1u, p.status) && mbar_wait(&hdr->v_full[st], (g / stages) & 1u, p.status) &&
-               !*abort_flag;
+          ok = wait(&hdr->p_full[buf], (g / kBufs) & 1u) && wait(&hdr->v_full[st], (g / stages) & 1u) &&
+               __all_sync(0xffffffffu, !*abort_flag);
           if (!ok) break;
           tc_fence_after();
           const uint64_t dv = dv0 + static_cast<uint64_t>(st) * (rings.v_stage >> 4);
           const uint32_t pa = tmem + buf * 128;
-#pragma unroll
-          for (int part = 0; part < 2; ++part)
+          if (lead) {
 #pragma unroll
             for (int s = 0; s < kKeys / 16; ++s)
-              mma_ts(tmem + kBufs * 128, pa + 64 * part + 8 * s, dv + s * (2048 >> 4), idesc, i > 0 || part > 0 || s > 0);
-          mma_commit(&hdr->o_done[buf]);
-          mma_commit(&hdr->v_empty[st]);
+#pragma unroll
+              for (int part = 0; part < 2; ++part)
+                mma_ts(tmem + kBufs * 128, pa + 16 * s + 8 * part, dv + s * (2048 >> 4), idesc, i > 0 || part > 0 || s > 0);
+            mma_commit(&hdr->o_done[buf]);
+            mma_commit(&hdr->v_empty[st]);
+          }
+          __syncwarp();
         }
       } while (ok && w.next(p));
-      if (ok) ok = mbar_wait(&hdr->v_empty[(g - 1) % stages], ((g - 1) / stages) & 1u, p.status);
-      if (!ok) *abort_flag = 1;
+      if (ok) ok = wait(&hdr->v_empty[(g - 1) % stages], ((g - 1) / stages) & 1u);
     }
+    if (!ok) *abort_flag = 1;
   } else {
-    // ------------------------------------------------------------------ softmax: four threads per query row
-    const int part_id = warp >> 2, row = (warp & 3) * 32 + lane;
-    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t tO = tmem + lane_base + kBufs * 128;
-    bool ok = true;
-    // Q' of a piece as canonical tiles, a step of 16 channels at a time; returns the drafted tokens this thread's row sees
-    auto load_q = [&](const Walk& w) -> uint64_t {
+    // ------------------------------------------------------------------ softmax: a group per S buffer, a thread per query row
+    const int mine = warp >> 2, quad = warp & 3, row = quad * 32 + lane, prev = mine == 0 ? kBufs - 1 : mine - 1;
+    const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
+    const uint32_t tS = tmem + lane_base + mine * 128, tO = tmem + lane_base + kBufs * 128;
+    auto wait = [&](unsigned long long* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status)) != 0; };
+    // the drafted tokens that this thread's row sees
+    auto load_mask = [&](const Walk& w) -> uint64_t {
+      const int my_row = w.chunk * kTile + row;
+      const uint64_t seen = my_row < p.rows ? __ldg(p.mask + static_cast<int64_t>(w.b) * p.tokens + my_row / p.group) : 0;
+      return p.tokens < 64 ? seen & ((1ull << p.tokens) - 1) : seen;
+    };
+    // Q' of a piece as canonical tiles, 16 channels at a time, by two of the groups (slots 0 and 1); they announce it
+    auto load_q = [&](const Walk& w, int slot) {
       const int rp_k = w.rp_k, rpk16 = (rp_k + 15) & ~15, group = (rpk16 >> 3) << 7;
       const int my_row = w.chunk * kTile + row;
-      const bool there = my_row < p.rows;
       const float* src = p.qp + ((static_cast<int64_t>(w.h) * p.B + w.b) * p.rows + my_row) * p.q_stride;
-      uint64_t seen = there ? __ldg(p.mask + static_cast<int64_t>(w.b) * p.tokens + my_row / p.group) : 0;
-      float4 x[2][4];
+#pragma unroll 1
+      for (int c0 = 16 * slot; c0 < rpk16; c0 += 32) {
+        float4 x[4];
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+        for (int j = 0; j < 4; ++j)
+          x[j] = my_row < p.rows && c0 + 8 * (j >> 1) < rp_k ? __ldg(reinterpret_cast<const float4*>(src + c0) + j) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int c = 16 * (part_id + kParts * k) + 4 * j;
-          x[k][j] = there && c < rp_k ? __ldg(reinterpret_cast<const float4*>(src + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-      if (p.tokens < 64) seen &= (1ull << p.tokens) - 1;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int c0 = 16 * (part_id + kParts * k);
-        if (c0 < rpk16) {
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint4 hi, lo;
-            split_pair(x[k][2 * half].x, x[k][2 * half].y, hi.x, lo.x);
-            split_pair(x[k][2 * half].z, x[k][2 * half].w, hi.y, lo.y);
-            split_pair(x[k][2 * half + 1].x, x[k][2 * half + 1].y, hi.z, lo.z);
-            split_pair(x[k][2 * half + 1].z, x[k][2 * half + 1].w, hi.w, lo.w);
-            unsigned char* at = q_tile + chunk_off(row, (c0 >> 3) + half, group);
-            *reinterpret_cast<uint4*>(at) = hi;
-            *reinterpret_cast<uint4*>(at + kTile * rpk16 * 2) = lo;
-          }
+        for (int half = 0; half < 2; ++half) {
+          uint4 hi, lo;
+          split_pair(x[2 * half].x, x[2 * half].y, hi.x, lo.x);
+          split_pair(x[2 * half].z, x[2 * half].w, hi.y, lo.y);
+          split_pair(x[2 * half + 1].x, x[2 * half + 1].y, hi.z, lo.z);
+          split_pair(x[2 * half + 1].z, x[2 * half + 1].w, hi.w, lo.w);
+          unsigned char* at = q_tile + chunk_off(row, (c0 >> 3) + half, group);
+          *reinterpret_cast<uint4*>(at) = hi;
+          *reinterpret_cast<uint4*>(at + kTile * rpk16 * 2) = lo;
         }
       }
       fence_async_smem();
-      mbar_arrive(&hdr->q_full);
-      return seen;
     };
-    int g = 0, now = 0;                                      // now: this piece's place in hdr->walk
-    uint64_t seen = load_q(hdr->walk[0]);
-    for (int piece = 0; ok; ++piece) {
-      const Walk& w = hdr->walk[now];
-      const int ahead = now == 2 ? 0 : now + 1;
-      if (tid == 0) {                                        // the next piece, known behind the barriers of this one
-        Walk next = w;
-        hdr->more[ahead] = next.next(p) ? 1 : 0;
-        hdr->walk[ahead] = next;
-      }
-      const int nt = w.nt, first_special = max(0, w.n_b / kKeys - w.t);    // tiles with a row that is not a cached one
-      const int rpv16 = (w.rp_v + 15) & ~15;
-      float m_run = -INFINITY, base = 0.f, l_run = 0.f;
-      // Named barriers have no time limit: every decision to leave the loop is taken through one of them.
-      for (int i = 0; i < nt; ++i, ++g) {
-        const int buf = g % kBufs;
-        const uint32_t tS = tmem + lane_base + buf * 128;
-        const bool waited = mbar_wait(&hdr->s_full[buf], (g / kBufs) & 1u, p.status);
-        const bool special = i >= first_special;
-        uint32_t r[kPart];
-        float cand = -INFINITY;
-        if (waited) {
-          tc_fence_after();
-          tmem_ld16(tS + kPart * part_id, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
-          tmem_ld16(tS + kPart * part_id + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
-          tmem_wait_ld();
-          if (special) {
-            const int s0 = (w.t + i) * kKeys + kPart * part_id - w.n_b;        // drafted token of the first row; cached rows lie below 0
-            uint32_t open = s0 >= 0 ? 0u : s0 <= -kPart ? ~0u : (1u << -s0) - 1;
-            if (s0 >= 0) open |= s0 < 64 ? static_cast<uint32_t>(seen >> s0) : 0u;
-            else if (s0 > -kPart) open |= static_cast<uint32_t>(seen << -s0);
-#pragma unroll
-            for (int c = 0; c < kPart; ++c)
-              if (!((open >> c) & 1)) r[c] = 0xff800000u;    // -inf
-          }
-          float mx0 = -INFINITY, mx1 = -INFINITY;
-#pragma unroll
-          for (int c = 0; c < kPart; c += 4) {
-            mx0 = max3(mx0, __uint_as_float(r[c]), __uint_as_float(r[c + 1]));
-            mx1 = max3(mx1, __uint_as_float(r[c + 2]), __uint_as_float(r[c + 3]));
-          }
-          cand = fmaxf(mx0, mx1);
-        }
-        float alpha = 1.f;
-        if (softmax_barrier_or(!waited || cand > m_run + 8.f || *abort_flag != 0)) {
-          hdr->exch[part_id][row] = cand;
-          if (softmax_barrier_or(!waited || *abort_flag != 0)) {      // a wait gave up somewhere: all of them leave here
-            ok = false;
-            break;
-          }
-          const float top = fmaxf(fmaxf(hdr->exch[0][row], hdr->exch[1][row]), fmaxf(hdr->exch[2][row], hdr->exch[3][row]));
-          if (top > m_run + 8.f) {                           // the same decision in all four threads of the row
-            alpha = ex2(m_run - top);
-            m_run = base = top;
-          }
-          l_run *= alpha;
-          if (i > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {       // rescale this thread's columns of the row of O'
-            const bool got = mbar_wait(&hdr->o_done[(g - 1) % kBufs], ((g - 1) / kBufs) & 1u, p.status);
-            if (__all_sync(0xffffffffu, got)) {
-              tc_fence_after();
+    bool ok = true;
+    int g0 = 0;                                              // the CTA's tiles in front of this piece
+    uint64_t seen = load_mask(w);
+    if (mine < 2) {
+      load_q(w, mine);
+      mbar_arrive(&hdr->q_full);
+    }
+    for (int piece = 0;; ++piece) {
+      const int nt = w.nt, n_b = w.n_b, rp_v = w.rp_v, rpv16 = (rp_v + 15) & ~15;
+      const int live = min(kTile, p.rows - w.chunk * kTile);
+      const bool idle = quad * 32 >= live;                   // no query in these 32 rows
+      float m = -INFINITY, l = 0.f;                          // reference at this thread's newest tile, sum against it
+      for (int i = (mine + kBufs - g0 % kBufs) % kBufs; i < nt; i += kBufs) {
+        const int g = g0 + i;
+        ok = wait(&hdr->s_full[mine], (g / kBufs) & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        const int key0 = (w.t + i) * kKeys;                  // first row of the tile
+        const bool special = key0 + kKeys > n_b;
+        // the rows of columns 32 j .. 32 j + 31 that this query sees, one bit each
+        auto open = [&](int j) -> uint32_t {
+          const int s0 = key0 + 32 * j - n_b;                // drafted token of the first one; cached rows lie below 0
+          if (s0 >= 0) return s0 < 64 ? static_cast<uint32_t>(seen >> s0) : 0u;
+          return s0 <= -32 ? ~0u : ((1u << -s0) - 1) | static_cast<uint32_t>(seen << -s0);
+        };
+        float top = -INFINITY;
+        if (special && !idle) {                              // masked scores become -inf
 #pragma unroll 1
-              for (int c0 = 16 * part_id; c0 < rpv16; c0 += 16 * kParts) {
-                uint32_t o[16];
-                tmem_ld16(tO + c0, o);
-                tmem_wait_ld();
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t bits = open(j);
+            if (!__any_sync(0xffffffffu, bits != ~0u)) continue;
+            uint32_t r[32];
+            tmem_ld16(tS + 32 * j, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
+            tmem_ld16(tS + 32 * j + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
+            tmem_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
-                tmem_st16(tO + c0, o);
-              }
-            } else {
-              *abort_flag = 1;                               // seen by every softmax thread at the next barrier
-            }
+            for (int c = 0; c < 32; ++c)
+              if (!((bits >> c) & 1)) r[c] = 0xff800000u;
+            tmem_st16(tS + 32 * j, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
+            tmem_st16(tS + 32 * j + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
           }
+          tmem_wait_st();
+        }
+        if (!idle) {
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int j = 0; j < kKeys; j += 64) {
+            uint32_t r[64];
+            tmem_ld64(tS + j, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 64; c += 8)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(r[c + 2 * k]), __uint_as_float(r[c + 2 * k + 1]));
+          }
+          top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        }
+        // The reference of the row: from the tile before, raised here, handed on to the tile behind.
+        if (g > 0) ok = wait(&hdr->ref_ready[prev][quad], ((g - 1) / kBufs) & 1u);
+        if (!ok) break;
+        if (i == 0 && row == 0) hdr->odd[(piece + 1) % 3] = 0;                // (last read two pieces ago)
+        const float before = i > 0 ? hdr->ref[row] : -INFINITY;
+        const bool raise = top > before + 8.f;
+        const float now = raise ? top : before;
+        hdr->ref[row] = now;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&hdr->ref_ready[mine][quad]);
+        if (now != m) {
+          l *= ex2(m - now);                                 // (0 before the first row)
+          m = now;
+        }
+        if (i > 0 && __any_sync(0xffffffffu, raise)) {       // rescale O'
+          ok = wait(&hdr->o_done[prev], ((g - 1) / kBufs) & 1u);
+          if (!ok) break;
+          tc_fence_after();
+          const float alpha = raise ? ex2(before - now) : 1.f;
+#pragma unroll 1
+          for (int c0 = 0; c0 < rpv16; c0 += 16) {
+            uint32_t o[16];
+            tmem_ld16(tO + c0, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+            tmem_st16(tO + c0, o);
+          }
+        }
+        // Exponentials against the reference and their sum.  P takes S's place 16 rows at a time: the leading parts go into
+        // the first eight of their columns, the remainders into the other eight.
+        if (!idle) {
+          float sum0 = 0.f, sum1 = 0.f;
+          const float neg = m == -INFINITY ? 0.f : -m;
+          // Loops small enough to stay at hand: an instruction that has to be fetched costs some 25 cycles.  The next 16
+          // columns come in once these are in other registers.
+          uint32_t r[16], x[16];
+          tmem_ld16(tS, r);
+          tmem_wait_ld();
+#pragma unroll 1
+          for (int j = 0; j < kKeys; j += 16) {
+            float y[16];
+#pragma unroll
+            for (int c = 0; c < 16; c += 2) fma2(y[c], y[c + 1], __uint_as_float(r[c]), __uint_as_float(r[c + 1]), 1.f, neg);
+            if (j + 16 < kKeys) tmem_ld16(tS + j + 16, r);
+#pragma unroll
+            for (int c = 0; c < 16; c += 2) {
+              const float e0 = ex2(y[c]), e1 = ex2(y[c + 1]);
+              add2(sum0, sum1, e0, e1);
+              split_pair(e0, e1, x[c / 2], x[8 + c / 2]);
+            }
+            tmem_st16(tS + j, x);
+            tmem_wait_ld_of(r);
+          }
+          l += sum0 + sum1;
         }
         if (special) {
           // the V' tile: rows behind the end cleared, values of drafted rows that are not finite cleared and noted
-          const int st = g % rings.v_stages;
-          const bool landed = mbar_wait(&hdr->v_full[st], (g / rings.v_stages) & 1u, p.status);
-          const int r_log = (w.t + i) * kKeys + row, n_b = w.n_b, row_end = n_b + p.tail;
-          if (landed && r_log >= n_b) {
-            unsigned char* v_tile = v_ring + st * rings.v_stage;
+          // (A wait tells a phase from its neighbours only.  S(g) says that tile g - 3 has been used up; with two stages the
+          // one that this stage held before, g - 2, may still be on its way.)
+          const int st = g % rings.v_stages, held = g - rings.v_stages;
+          if (held >= 0 && rings.v_stages < kBufs) ok = wait(&hdr->o_done[held % kBufs], (held / kBufs) & 1u);
+          if (ok) ok = wait(&hdr->v_full[st], (g / rings.v_stages) & 1u);
+          if (!ok) break;
+          const int r_log = key0 + row, row_end = n_b + p.tail;
+          if (r_log >= n_b) {
+            unsigned char* v_row = v_ring + st * rings.v_stage;
             const int pieces16 = 8 * ((rpv16 + 63) >> 6);
-            bool odd = false;
+            auto piece_at = [&](int c) { return reinterpret_cast<uint4*>(v_row + (c >> 3) * kAtom + sw128_off(row, c & 7)); };
+            if (r_log >= row_end) {
 #pragma unroll 1
-            for (int c = part_id; c < pieces16; c += kParts) {
-              uint4* at = reinterpret_cast<uint4*>(v_tile + (c >> 3) * kAtom + sw128_off(row, c & 7));
-              uint4 v = *at;
-              uint32_t* u = reinterpret_cast<uint32_t*>(&v);
-              bool touched = false;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                if (r_log >= row_end) { touched = touched || u[j] != 0; u[j] = 0; continue; }
-                if (!finite16(u[j])) { u[j] &= 0xffff0000u; touched = odd = true; }
-                if (!finite16(u[j] >> 16)) { u[j] &= 0x0000ffffu; touched = odd = true; }
+              for (int c = 0; c < pieces16; ++c) *piece_at(c) = make_uint4(0u, 0u, 0u, 0u);
+            } else {
+              uint32_t odd = 0;                              // bits 15 and 31: an exponent of ones
+#pragma unroll 1
+              for (int c = 0; c < pieces16; ++c) {
+                const uint4 v = *piece_at(c);
+                odd |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) | ((v.z & 0x7f807f80u) + 0x00800080u) |
+                       ((v.w & 0x7f807f80u) + 0x00800080u);
               }
-              if (touched) *at = v;
+              if (odd & 0x80008000u) {
+#pragma unroll 1
+                for (int c = 0; c < 4 * pieces16; ++c) {
+                  uint32_t* at = reinterpret_cast<uint32_t*>(piece_at(c >> 2)) + (c & 3);
+                  uint32_t u = *at;
+                  if (!finite16(u)) u &= 0xffff0000u;
+                  if (!finite16(u >> 16)) u &= 0x0000ffffu;
+                  *at = u;
+                }
+                atomicOr(&hdr->odd[piece % 3], 1ull << (r_log - n_b));
+              }
             }
-            if (odd) atomicOr(&hdr->odd[piece & 1], 1ull << (r_log - n_b));
           }
           fence_async_smem();
         }
-        // exponentials against the reference, their sum, P as two 16-bit parts over S
-        float sum0 = 0.f, sum1 = 0.f;
-        const float neg = -base;
-#pragma unroll
-        for (int j0 = 0; j0 < kPart / 2; j0 += 8) {
-          uint32_t hi[8], lo[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float y0, y1;
-            fma2(y0, y1, __uint_as_float(r[2 * (j0 + j)]), __uint_as_float(r[2 * (j0 + j) + 1]), 1.f, neg);
-            const float e0 = ex2(y0), e1 = ex2(y1);
-            add2(sum0, sum1, e0, e1);
-            split_pair(e0, e1, hi[j], lo[j]);
-          }
-          tmem_st8(tS + kPart / 2 * part_id + j0, hi);
-          tmem_st8(tS + 64 + kPart / 2 * part_id + j0, lo);
-        }
-        l_run += sum0 + sum1;
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(&hdr->p_full[buf]);
+        mbar_arrive(&hdr->p_full[mine]);
       }
-      // ---- the next piece's Q' (this one's last S product has read its own), so that its products go on meanwhile
-      uint64_t seen_next = 0;
-      const bool more = ok && hdr->more[ahead] != 0;
-      if (more) seen_next = load_q(hdr->walk[ahead]);
-      // ---- the piece's partial
-      if (ok) {
-        const bool done = mbar_wait(&hdr->o_done[(g - 1) % kBufs], ((g - 1) / kBufs) & 1u, p.status);
-        if (!done) *abort_flag = 1;
+      if (!ok) break;
+      // ---- the piece's end.  The group of the last tile writes the partial; the other two load the next piece's Q' and go on.
+      // (They have handed over their sums and read the reference before they announce Q', and no product of the next piece
+      // comes before that: sums and references are not overwritten too early, and no barrier is two phases ahead of a waiter.)
+      const int last = g0 + nt - 1, last_buf = last % kBufs;
+      const uint32_t last_phase = (last / kBufs) & 1u;
+      g0 += nt;
+      Walk next = w;
+      const bool more = next.next(p);
+      if (mine != last_buf) {
+        const int slot = (mine - last_buf + 2) % kBufs;
+        ok = wait(&hdr->s_full[last_buf], last_phase);       // the last product that reads this piece's Q'
+        if (!ok) break;
+        if (more) load_q(next, slot);
+        ok = wait(&hdr->ref_ready[last_buf][quad], last_phase);
+        if (!ok) break;
+        const float top = hdr->ref[row];
+        hdr->sums[piece & 1][slot][row] = top == m ? l : l * ex2(m - top);
+        mbar_arrive(&hdr->sums_ready);
+        if (more) mbar_arrive(&hdr->q_full);
+      } else {
+        ok = wait(&hdr->sums_ready, piece & 1u) && wait(&hdr->o_done[last_buf], last_phase);
+        if (!ok) break;
         tc_fence_after();
-      }
-      hdr->exch[part_id][row] = l_run;                       // the four sums share the reference
-      const bool fine = !softmax_barrier_or(!ok || *abort_flag != 0);
-      ok = fine;
-      const uint64_t odd = hdr->odd[piece & 1] & seen;
-      if (tid == 0) hdr->odd[(piece + 1) & 1] = 0;           // (read by everyone before this barrier, next written behind another)
-      const int rp_v = w.rp_v, n_b = w.n_b, live = min(kTile, p.rows - w.chunk * kTile);
-      const int64_t item = (static_cast<int64_t>(w.h) * p.B + w.b) * w.chunks + w.chunk;
-      float* part = p.partials + ((item + blockIdx.x) * p.slot_rows + row) * p.part_stride;
-      if (part_id == 0 && row < live) {
-        part[0] = fine ? m_run : -INFINITY;
-        part[1] = fine ? (hdr->exch[0][row] + hdr->exch[1][row]) + (hdr->exch[2][row] + hdr->exch[3][row]) : 0.f;
-      }
-#pragma unroll 1
-      for (int c0 = 16 * part_id; c0 < rpv16; c0 += 16 * kParts) {
-        uint32_t o[16];
-        tmem_ld16(tO + c0, o);
-        tmem_wait_ld();
-        if (row >= live) continue;
-#pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-          if (c0 + j >= rp_v) break;
-          float4 v = make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]), __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3]));
-          if (!fine) v = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (uint64_t rest = odd; rest; rest &= rest - 1) {          // (rare) values that are not finite, of rows this query sees
-            const int64_t at = physical_row(p.pages, w.b, p.n_max, n_b + __ffsll(static_cast<long long>(rest)) - 1);
-            const uint2 u = *reinterpret_cast<const uint2*>(p.cache + p.heads[w.h].v_off + (at * rp_v + c0 + j) * 2);
-            if (!finite16(u.x)) v.x += __uint_as_float(u.x << 16);
-            if (!finite16(u.x >> 16)) v.y += __uint_as_float(u.x & 0xffff0000u);
-            if (!finite16(u.y)) v.z += __uint_as_float(u.y << 16);
-            if (!finite16(u.y >> 16)) v.w += __uint_as_float(u.y & 0xffff0000u);
-          }
-          *reinterpret_cast<float4*>(part + 4 + c0 + j) = v;
+        const uint64_t odd = hdr->odd[piece % 3] & seen;
+        const int64_t item = (static_cast<int64_t>(w.h) * p.B + w.b) * w.chunks + w.chunk;
+        float* part = p.partials + ((item + blockIdx.x) * p.slot_rows + row) * p.part_stride;
+        if (row < live) {
+          part[0] = m;
+          part[1] = l + (hdr->sums[piece & 1][0][row] + hdr->sums[piece & 1][1][row]);
         }
+#pragma unroll 1
+        for (int c0 = 0; c0 < rpv16; c0 += 16) {
+          uint32_t o[16];
+          tmem_ld16(tO + c0, o);
+          tmem_wait_ld();
+          if (row >= live) continue;
+#pragma unroll
+          for (int j = 0; j < 16; j += 4)
+            if (c0 + j < rp_v)
+              *reinterpret_cast<uint4*>(part + 4 + c0 + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+          for (uint64_t rest = odd; rest; rest &= rest - 1) {              // (rare) values that are not finite, of rows this query sees
+            const int64_t at = physical_row(p.pages, w.b, p.n_max, n_b + __ffsll(static_cast<long long>(rest)) - 1);
+            const uint16_t* v = reinterpret_cast<const uint16_t*>(p.cache + p.heads[w.h].v_off) + at * rp_v;
+#pragma unroll 1
+            for (int c = c0; c < min(c0 + 16, rp_v); ++c)
+              if (!finite16(v[c])) part[4 + c] += __uint_as_float(static_cast<uint32_t>(v[c]) << 16);
+          }
+        }
+        tc_fence_before();
+        mbar_arrive(&hdr->o_free);                           // the next piece's products may overwrite O'
       }
-      tc_fence_before();                                     // (the next piece's products overwrite O' once P is announced)
       if (!more) break;
-      seen = seen_next;
-      now = ahead;
+      w = next;
+      seen = load_mask(w);
     }
     if (!ok) *abort_flag = 1;
   }

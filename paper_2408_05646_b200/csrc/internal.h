@@ -308,9 +308,9 @@ struct MqDecodeParams {
   uint32_t flags;
   PageMap pages;
   // tcgen05 kernel (grid > 0): the tiles of all items (unit, run of 128 query rows), laid end to end, in equal ranges.
-  // CTA c has tiles [c total / grid, (c + 1) total / grid); its piece of item u leaves the partials of u's rows in slot
-  // u + c, [slot_rows][part_stride] (unique along the staircase of pieces).
-  int32_t grid, slot_rows;
+  // A CTA has cta_tiles of them, the first cta_extra CTAs one more; the piece of item u on CTA c leaves the partials of u's
+  // rows in slot u + c, [slot_rows][part_stride] (unique along the staircase of pieces).
+  int32_t grid, slot_rows, cta_tiles, cta_extra;
   int64_t total_tiles, head_tiles;   // of all items; of all sequences for one head and run of query rows
   const void* tmaps;        // CUtensorMap[2 * H]: K' and V' slab of every head
   int* status;              // (its waits are bounded)
