@@ -336,15 +336,15 @@ ea_status check_quant_args(eigen_attn_t h, const char* who, int32_t bits, int32_
 constexpr int kMaxGroup = 16;
 constexpr size_t kMqSlots = 65536;       // partials that every scratch holds at least, so that query rows can be split
 
+constexpr int kMqTcMinRows = 16;         // query rows that the warp-level products still serve
 constexpr int kMqTcCtas = 296;           // largest grid of the tcgen05 tree kernel (its partials are slots of items + CTAs)
-int slot_rows_of(int rows) { return rows < ea::kMqTcRows ? rows : ea::kMqTcRows; }
 
 size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t* slots) {
   const size_t units = static_cast<size_t>(h->desc.batch) * h->desc.n_heads;
   const size_t off = align_up(units * rows * h->L.max_rp_k * sizeof(float));
   size_t n = units * rows > kMqSlots ? units * rows : kMqSlots;
   const size_t items = units * ((rows + ea::kMqTcRows - 1) / ea::kMqTcRows);
-  if ((items + kMqTcCtas) * slot_rows_of(rows) > n) n = (items + kMqTcCtas) * slot_rows_of(rows);
+  if (rows > kMqTcMinRows && (items + kMqTcCtas) * ea::kMqTcRows > n) n = (items + kMqTcCtas) * ea::kMqTcRows;
   if (off_part) *off_part = off;
   if (slots) *slots = n;
   return align_up(off + n * h->L.part_stride * sizeof(float));
@@ -1382,7 +1382,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
   const int max_rp = L.max_rp_k > L.max_rp_v ? L.max_rp_k : L.max_rp_v;
   // Trees with more than 16 query rows: tcgen05 products, where the layer's slabs have tensor maps (pages then have to lie
   // inside one sequence's slab) and no bias goes onto the scores.
-  bool tc = mma && p.tail > 0 && p.rows > 16 && h->tmaps_ok && !h->alibi && h->opt_tree_impl != 1 &&
+  bool tc = mma && p.tail > 0 && p.rows > kMqTcMinRows && h->tmaps_ok && !h->alibi && h->opt_tree_impl != 1 &&
                   (!h->paged || h->desc.n_max % (1 << h->page_shift) == 0);
   // (its tiles are counted in 32 bits)
   tc = tc && ((end >> 7) + 1) * p.B * p.H * ((p.rows + ea::kMqTcRows - 1) / ea::kMqTcRows) < INT32_MAX;
@@ -1406,7 +1406,8 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
     p.grid = static_cast<int32_t>(grid);
     p.cta_tiles = static_cast<int32_t>(p.total_tiles / grid);
     p.cta_extra = static_cast<int32_t>(p.total_tiles % grid);
-    p.slot_rows = slot_rows_of(p.rows);
+    p.copies = p.rows <= 32 ? 4 : p.rows <= 64 ? 2 : 1;
+    p.slot_rows = ea::kMqTcRows;
   } else {
     // Tiles of a piece: the CTAs run in waves of resident ones, each pays a start-up worth a tile or two; pieces are cut to
     // one size, so a shorter sequence of the batch has fewer of them; the partials must have room.

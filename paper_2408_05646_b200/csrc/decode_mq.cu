@@ -460,11 +460,12 @@ __global__ void __launch_bounds__(256) mq_simt_kernel(const MqDecodeParams p) {
 
 // ---------------------------------------------------------------- merge and lift
 
-// The pieces of a query row: `count` partials, `step` floats apart from `first` on.
+// The pieces of a query row: `count` partials; 2^fold of them `step` floats apart from `first` on, then the same `stride` on.
 struct Pieces {
   const float* first;
-  int64_t step;
-  int count;
+  int64_t step, stride;
+  int count, fold;
+  __device__ __forceinline__ const float* at(int s) const { return first + (s >> fold) * stride + (s & ((1 << fold) - 1)) * step; }
 };
 // The CTA of the tcgen05 kernel that has tile x: the first cta_extra CTAs have a tile more.
 __device__ __forceinline__ int cta_of_tile(const MqDecodeParams& p, int x) {
@@ -478,13 +479,14 @@ __device__ __forceinline__ Pieces pieces_of(const MqDecodeParams& p, int unit, i
   const int tiles = p.list != nullptr ? p.tiles
                                       : (p.n - (p.deficit != nullptr ? __ldg(p.deficit + b) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
   if (p.grid == 0)
-    return {p.partials + (static_cast<int64_t>(unit) * p.rows + row) * p.splits * p.part_stride, p.part_stride, max(1, (tiles + p.per - 1) / p.per)};
+    return {p.partials + (static_cast<int64_t>(unit) * p.rows + row) * p.splits * p.part_stride, 0, p.part_stride, max(1, (tiles + p.per - 1) / p.per), 0};
   const int chunks = (p.rows + kMqTcRows - 1) / kMqTcRows, chunk = row / kMqTcRows;
   const int64_t x = (h * p.head_tiles + before) * chunks + static_cast<int64_t>(chunk) * tiles;
   const int c0 = cta_of_tile(p, static_cast<int>(x)), c1 = cta_of_tile(p, static_cast<int>(x) + tiles - 1);
   const int64_t slot = static_cast<int64_t>(unit) * chunks + chunk + c0;
-  return {p.partials + (slot * p.slot_rows + (row - chunk * kMqTcRows)) * p.part_stride, static_cast<int64_t>(p.slot_rows) * p.part_stride,
-          c1 - c0 + 1};
+  const int fold = p.copies >> 1;            // (1, 2 or 4 copies)
+  return {p.partials + (slot * p.slot_rows + (row - chunk * kMqTcRows)) * p.part_stride, static_cast<int64_t>(p.slot_rows >> fold) * p.part_stride,
+          static_cast<int64_t>(p.slot_rows) * p.part_stride, (c1 - c0 + 1) << fold, fold};
 }
 // Tiles of the sequences in front of b, by a whole warp.
 __device__ __forceinline__ int64_t tiles_before(const MqDecodeParams& p, int b) {
@@ -506,7 +508,7 @@ __device__ __forceinline__ float merged(const Pieces& w, int c, bool has) {
     float m[kFew], l[kFew], a[kFew], top = -INFINITY, sum = 0.f, o = 0.f;
 #pragma unroll
     for (int s = 0; s < kFew; ++s) {
-      const float* x = w.first + s * w.step;
+      const float* x = w.at(s);
       m[s] = s < w.count ? x[0] : -INFINITY;
       l[s] = s < w.count ? x[1] : 0.f;
       a[s] = s < w.count && has ? x[4 + c] : 0.f;
@@ -523,20 +525,20 @@ __device__ __forceinline__ float merged(const Pieces& w, int c, bool has) {
     return sum == 0.f ? 0.f : o / sum;
   }
   float M = -INFINITY;
-  for (int s = lane; s < w.count; s += 32) M = fmaxf(M, w.first[s * w.step]);
+  for (int s = lane; s < w.count; s += 32) M = fmaxf(M, w.at(s)[0]);
 #pragma unroll
   for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, d));
   const float base = M == -INFINITY ? 0.f : M;
   float L = 0.f, acc = 0.f;
   for (int s0 = 0; s0 < w.count; s0 += 32) {
     const int n = min(32, w.count - s0);
-    const float* x = w.first + s0 * w.step;
-    const float f = lane < n ? ex2(x[lane * w.step] - base) : 0.f;         // 0 for a piece without rows
-    L = lane < n ? fmaf(x[lane * w.step + 1], f, L) : L;
+    const float* x = w.at(s0 + lane);
+    const float f = lane < n ? ex2(x[0] - base) : 0.f;       // 0 for a piece without rows
+    L = lane < n ? fmaf(x[1], f, L) : L;
 #pragma unroll 8
     for (int s = 0; s < n; ++s) {
       const float fs = __shfl_sync(kFull, f, s);
-      if (has) acc = fmaf(x[s * w.step + 4 + c], fs, acc);
+      if (has) acc = fmaf(w.at(s0 + s)[4 + c], fs, acc);
     }
   }
 #pragma unroll
@@ -622,28 +624,40 @@ __global__ void __launch_bounds__(kPrThreads) mq_combine_many_kernel(const __gri
     int64_t before = tiles_before(p, b0);
     if (p.grid > 0)
       for (int i = b0; i < b; ++i) before += (p.n - (p.deficit != nullptr ? __ldg(p.deficit + i) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
-    Pieces w{nullptr, 0, 0};
+    Pieces w{nullptr, 0, 0, 0, 0};
     if (there) w = pieces_of(p, h * p.B + b, g - b * p.rows, before);
     if (tid < kCbRows) target[r] = there ? out_row<T>(p, h, b, g - b * p.rows) : nullptr;
     chain_wait();
     float M = -INFINITY, L = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < w.count; ++s) M = fmaxf(M, w.first[s * w.step]);
+    for (int s = 0; s < w.count; ++s) M = fmaxf(M, w.at(s)[0]);
     const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll 4
-    for (int s = 0; s < w.count; ++s) L = fmaf(w.first[s * w.step + 1], ex2(w.first[s * w.step] - base), L);
+    for (int s = 0; s < w.count; ++s) L = fmaf(w.at(s)[1], ex2(w.at(s)[0] - base), L);
     const float inv = L == 0.f ? 0.f : 1.f / L;              // (a row that sees nothing: its sums are zeros)
-    const int half = hd.rp_v / 2, c_lo = (tid / kCbRows) * half;
-    for (int c = c_lo; c < c_lo + half; c += 4) {            // half is a multiple of 4
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+    const int half = hd.rp_v / 2, c_lo = (tid / kCbRows) * half;         // half is a multiple of 4
+    constexpr int kPieces = 8;                               // 16-byte pieces of the row that are read together
+    for (int c0 = 0; c0 < half; c0 += 4 * kPieces) {
+      float4 o[kPieces];
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
       for (int s = 0; s < w.count; ++s) {
-        const float* x = w.first + s * w.step;
+        const float* x = w.at(s);
         const float f = ex2(x[0] - base) * inv;
-        const float4 v = *reinterpret_cast<const float4*>(x + 4 + c);
-        o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+          if (c0 + 4 * j >= half) continue;
+          const float4 v = *reinterpret_cast<const float4*>(x + 4 + c_lo + c0 + 4 * j);
+          o[j].x = fmaf(v.x, f, o[j].x); o[j].y = fmaf(v.y, f, o[j].y); o[j].z = fmaf(v.z, f, o[j].z); o[j].w = fmaf(v.w, f, o[j].w);
+        }
       }
-      ot[c * kCbRows + r] = o.x; ot[(c + 1) * kCbRows + r] = o.y; ot[(c + 2) * kCbRows + r] = o.z; ot[(c + 3) * kCbRows + r] = o.w;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        if (c0 + 4 * j >= half) continue;
+        float* at = ot + (c_lo + c0 + 4 * j) * kCbRows + r;
+        at[0] = o[j].x; at[kCbRows] = o[j].y; at[2 * kCbRows] = o[j].z; at[3 * kCbRows] = o[j].w;
+      }
     }
   }
   tc::cp_async_wait<0>();

@@ -84,7 +84,6 @@ struct __align__(16) TcHeader {
   unsigned long long p_full[kBufs], o_free, q_full, sums_ready;         // arrivals of one group, of two
   unsigned long long odd[3];                  // drafted tokens with a value that is not finite; pieces take turns
   uint32_t tmem_base;
-  int abort_flag;
   float ref[kTile];                           // reference of every query row behind the newest tile
   float sums[2][kBufs - 1][kTile];            // row sums of the other groups at a piece's end; pieces take turns
 };
@@ -178,7 +177,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
   if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
   if (tid < kSingles + kBufs + 3) mbar_init(&hdr->k_full[0] + tid, tid < kSingles ? 1 : tid <= kSingles + kBufs ? kTile : 2 * kTile);
   else if (tid >= 64 && tid < 64 + 3) hdr->odd[tid - 64] = 0;
-  else if (tid == 67) hdr->abort_flag = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   chain_go();
   Walk w = start_walk(p, blockIdx.x, lane);
@@ -187,7 +185,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = hdr->tmem_base;
-  volatile int* abort_flag = &hdr->abort_flag;
 
   // Every role counts the CTA's tiles through (g): ring stages, S buffers and the phases of their barriers go on over the
   // borders of the pieces.
@@ -218,7 +215,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
         fetch(0);
         for (int i = 0; i < w.nt; ++i, ++g) {
           const int st = g % stages;
-          if (g >= stages) ok = mbar_wait(&empty[st], (g / stages - 1) & 1u, p.status) && !*abort_flag;
+          if (g >= stages) ok = mbar_wait(&empty[st], (g / stages - 1) & 1u, p.status);
           if (!ok) break;
           mbar_arrive_expect_tx(&full[st], static_cast<uint32_t>(atoms * kAtom));
 #pragma unroll
@@ -237,7 +234,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
           fetch(i + 1);
         }
       } while (ok && w.next(p));
-      if (!ok) *abort_flag = 1;
       // copies in flight must land before the CTA leaves; normally their consumers have waited for them
       for (int s = 0; s < stages && s < g; ++s) mbar_wait(&full[s], ((g - 1 - s) / stages) & 1u, p.status);
     }
@@ -259,7 +255,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
           const int st = g % stages, buf = g % kBufs;
           ok = wait(&hdr->k_full[st], (g / stages) & 1u);
           if (ok && g >= kBufs) ok = wait(&hdr->o_done[buf], (g / kBufs - 1) & 1u);       // P(g - 3) has been read
-          ok = ok && __all_sync(0xffffffffu, !*abort_flag);
           if (!ok) break;
           tc_fence_after();
           const uint64_t dk = dk0 + static_cast<uint64_t>(st) * (rings.k_stage >> 4);
@@ -293,8 +288,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
         ++piece;
         for (int i = 0; i < w.nt && ok; ++i, ++g) {
           const int st = g % stages, buf = g % kBufs;
-          ok = wait(&hdr->p_full[buf], (g / kBufs) & 1u) && wait(&hdr->v_full[st], (g / stages) & 1u) &&
-               __all_sync(0xffffffffu, !*abort_flag);
+          ok = wait(&hdr->v_full[st], (g / stages) & 1u) && wait(&hdr->p_full[buf], (g / kBufs) & 1u);
           if (!ok) break;
           tc_fence_after();
           const uint64_t dv = dv0 + static_cast<uint64_t>(st) * (rings.v_stage >> 4);
@@ -313,23 +307,26 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       } while (ok && w.next(p));
       if (ok) ok = wait(&hdr->v_empty[(g - 1) % stages], ((g - 1) / stages) & 1u);
     }
-    if (!ok) *abort_flag = 1;
   } else {
     // ------------------------------------------------------------------ softmax: a group per S buffer, a thread per query row
     const int mine = warp >> 2, quad = warp & 3, row = quad * 32 + lane, prev = mine == 0 ? kBufs - 1 : mine - 1;
     const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
     const uint32_t tS = tmem + lane_base + mine * 128, tO = tmem + lane_base + kBufs * 128;
+    // At most 64 (32) query rows: the operand holds them two (four) times, and a copy looks after a half (quarter) of every
+    // tile's rows, with a reference, a sum and a partial of its own.
+    const int span = kKeys / p.copies, copy = row / span, c_lo = copy * span, c_hi = c_lo + span;       // (span: rows of a copy too)
+    const int q_row = p.copies > 1 ? row - copy * span : row;
     auto wait = [&](unsigned long long* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status)) != 0; };
     // the drafted tokens that this thread's row sees
     auto load_mask = [&](const Walk& w) -> uint64_t {
-      const int my_row = w.chunk * kTile + row;
+      const int my_row = w.chunk * kTile + q_row;
       const uint64_t seen = my_row < p.rows ? __ldg(p.mask + static_cast<int64_t>(w.b) * p.tokens + my_row / p.group) : 0;
       return p.tokens < 64 ? seen & ((1ull << p.tokens) - 1) : seen;
     };
     // Q' of a piece as canonical tiles, 16 channels at a time, by two of the groups (slots 0 and 1); they announce it
     auto load_q = [&](const Walk& w, int slot) {
       const int rp_k = w.rp_k, rpk16 = (rp_k + 15) & ~15, group = (rpk16 >> 3) << 7;
-      const int my_row = w.chunk * kTile + row;
+      const int my_row = w.chunk * kTile + q_row;
       const float* src = p.qp + ((static_cast<int64_t>(w.h) * p.B + w.b) * p.rows + my_row) * p.q_stride;
 #pragma unroll 1
       for (int c0 = 16 * slot; c0 < rpk16; c0 += 32) {
@@ -361,7 +358,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
     for (int piece = 0;; ++piece) {
       const int nt = w.nt, n_b = w.n_b, rp_v = w.rp_v, rpv16 = (rp_v + 15) & ~15;
       const int live = min(kTile, p.rows - w.chunk * kTile);
-      const bool idle = quad * 32 >= live;                   // no query in these 32 rows
+      const bool idle = (q_row & ~31) >= live;               // no query in these 32 rows
       float m = -INFINITY, l = 0.f;                          // reference at this thread's newest tile, sum against it
       for (int i = (mine + kBufs - g0 % kBufs) % kBufs; i < nt; i += kBufs) {
         const int g = g0 + i;
@@ -370,39 +367,40 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
         tc_fence_after();
         const int key0 = (w.t + i) * kKeys;                  // first row of the tile
         const bool special = key0 + kKeys > n_b;
-        // the rows of columns 32 j .. 32 j + 31 that this query sees, one bit each
+        // the rows of columns j .. j + 31 that this query sees, one bit each
         auto open = [&](int j) -> uint32_t {
-          const int s0 = key0 + 32 * j - n_b;                // drafted token of the first one; cached rows lie below 0
+          const int s0 = key0 + j - n_b;                    // drafted token of the first one; cached rows lie below 0
           if (s0 >= 0) return s0 < 64 ? static_cast<uint32_t>(seen >> s0) : 0u;
           return s0 <= -32 ? ~0u : ((1u << -s0) - 1) | static_cast<uint32_t>(seen << -s0);
         };
         float top = -INFINITY;
         if (special && !idle) {                              // masked scores become -inf
 #pragma unroll 1
-          for (int j = 0; j < 4; ++j) {
+          for (int j = c_lo; j < c_hi; j += 32) {
             const uint32_t bits = open(j);
             if (!__any_sync(0xffffffffu, bits != ~0u)) continue;
             uint32_t r[32];
-            tmem_ld16(tS + 32 * j, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
-            tmem_ld16(tS + 32 * j + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
+            tmem_ld16(tS + j, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
+            tmem_ld16(tS + j + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
             tmem_wait_ld();
 #pragma unroll
             for (int c = 0; c < 32; ++c)
               if (!((bits >> c) & 1)) r[c] = 0xff800000u;
-            tmem_st16(tS + 32 * j, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
-            tmem_st16(tS + 32 * j + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
+            tmem_st16(tS + j, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
+            tmem_st16(tS + j + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
           }
           tmem_wait_st();
         }
         if (!idle) {
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
-          for (int j = 0; j < kKeys; j += 64) {
-            uint32_t r[64];
-            tmem_ld64(tS + j, r);
+          for (int j = c_lo; j < c_hi; j += 32) {
+            uint32_t r[32];
+            tmem_ld16(tS + j, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
+            tmem_ld16(tS + j + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
             tmem_wait_ld();
 #pragma unroll
-            for (int c = 0; c < 64; c += 8)
+            for (int c = 0; c < 32; c += 8)
 #pragma unroll
               for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(r[c + 2 * k]), __uint_as_float(r[c + 2 * k + 1]));
           }
@@ -445,14 +443,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
           // Loops small enough to stay at hand: an instruction that has to be fetched costs some 25 cycles.  The next 16
           // columns come in once these are in other registers.
           uint32_t r[16], x[16];
-          tmem_ld16(tS, r);
+          tmem_ld16(tS + c_lo, r);
           tmem_wait_ld();
 #pragma unroll 1
-          for (int j = 0; j < kKeys; j += 16) {
+          for (int j = c_lo; j < c_hi; j += 16) {
             float y[16];
 #pragma unroll
             for (int c = 0; c < 16; c += 2) fma2(y[c], y[c + 1], __uint_as_float(r[c]), __uint_as_float(r[c + 1]), 1.f, neg);
-            if (j + 16 < kKeys) tmem_ld16(tS + j + 16, r);
+            if (j + 16 < c_hi) tmem_ld16(tS + j + 16, r);
 #pragma unroll
             for (int c = 0; c < 16; c += 2) {
               const float e0 = ex2(y[c]), e1 = ex2(y[c + 1]);
@@ -463,6 +461,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
             tmem_wait_ld_of(r);
           }
           l += sum0 + sum1;
+          if (p.copies > 1) {                                // the other copies' rows of the tile
+#pragma unroll
+            for (int c = 0; c < 16; ++c) x[c] = 0u;
+#pragma unroll 1
+            for (int j = 0; j < kKeys; j += 16)
+              if (j < c_lo || j >= c_hi) tmem_st16(tS + j, x);
+          }
         }
         if (special) {
           // the V' tile: rows behind the end cleared, values of drafted rows that are not finite cleared and noted
@@ -534,7 +539,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
         const uint64_t odd = hdr->odd[piece % 3] & seen;
         const int64_t item = (static_cast<int64_t>(w.h) * p.B + w.b) * w.chunks + w.chunk;
         float* part = p.partials + ((item + blockIdx.x) * p.slot_rows + row) * p.part_stride;
-        if (row < live) {
+        if (q_row < live) {
           part[0] = m;
           part[1] = l + (hdr->sums[piece & 1][0][row] + hdr->sums[piece & 1][1][row]);
         }
@@ -543,13 +548,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
           uint32_t o[16];
           tmem_ld16(tO + c0, o);
           tmem_wait_ld();
-          if (row >= live) continue;
+          if (q_row >= live) continue;
 #pragma unroll
           for (int j = 0; j < 16; j += 4)
             if (c0 + j < rp_v)
               *reinterpret_cast<uint4*>(part + 4 + c0 + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
           for (uint64_t rest = odd; rest; rest &= rest - 1) {              // (rare) values that are not finite, of rows this query sees
-            const int64_t at = physical_row(p.pages, w.b, p.n_max, n_b + __ffsll(static_cast<long long>(rest)) - 1);
+            const int r_log = n_b + __ffsll(static_cast<long long>(rest)) - 1, column = r_log & (kKeys - 1);
+            if (column < c_lo || column >= c_hi) continue;               // another copy's
+            const int64_t at = physical_row(p.pages, w.b, p.n_max, r_log);
             const uint16_t* v = reinterpret_cast<const uint16_t*>(p.cache + p.heads[w.h].v_off) + at * rp_v;
 #pragma unroll 1
             for (int c = c0; c < min(c0 + 16, rp_v); ++c)
@@ -563,7 +570,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       w = next;
       seen = load_mask(w);
     }
-    if (!ok) *abort_flag = 1;
   }
   tc_fence_before();
   __syncthreads();
