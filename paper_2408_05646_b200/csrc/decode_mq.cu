@@ -118,27 +118,37 @@ struct RegTile {
 #pragma unroll
       for (int c = 0; c < C; ++c) acc[r][c] = 0.f;
   }
-  __device__ __forceinline__ void multiply(const float* a, const float* b, int k_count, int width) {
+  __device__ __forceinline__ void multiply(const float* a, const float* b, int k_count, int width, int a_pitch) {
     const float* ar = a + R * lane;
     const float* br = b + c0;
     if (c0 >= width) return;
-#pragma unroll 4
-    for (int k = 0; k < k_count; ++k) {
-      float x[R];
-      if constexpr (R == 4) *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(ar + k * 32 * R);
-      else *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(ar + k * 32 * R);
+    // the operands of step k + 1 are on their way while those of step k are multiplied
+    float x[2][R];
+    float4 u[2][C / 4];
+    auto fetch = [&](int k, float (&xx)[R], float4 (&uu)[C / 4]) {
+      if constexpr (R == 4) *reinterpret_cast<float4*>(xx) = *reinterpret_cast<const float4*>(ar + k * a_pitch);
+      else *reinterpret_cast<float2*>(xx) = *reinterpret_cast<const float2*>(ar + k * a_pitch);
 #pragma unroll
-      for (int c = 0; c < C; c += 4) {
-        const float4 u = *reinterpret_cast<const float4*>(br + c);
+      for (int c = 0; c < C / 4; ++c) uu[c] = *reinterpret_cast<const float4*>(br + k * width + 4 * c);
+    };
+    auto fma_step = [&](const float (&xx)[R], const float4 (&uu)[C / 4]) {
+#pragma unroll
+      for (int c = 0; c < C; c += 4)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          acc[r][c] = fmaf(x[r], u.x, acc[r][c]);
-          acc[r][c + 1] = fmaf(x[r], u.y, acc[r][c + 1]);
-          acc[r][c + 2] = fmaf(x[r], u.z, acc[r][c + 2]);
-          acc[r][c + 3] = fmaf(x[r], u.w, acc[r][c + 3]);
+          acc[r][c] = fmaf(xx[r], uu[c / 4].x, acc[r][c]);
+          acc[r][c + 1] = fmaf(xx[r], uu[c / 4].y, acc[r][c + 1]);
+          acc[r][c + 2] = fmaf(xx[r], uu[c / 4].z, acc[r][c + 2]);
+          acc[r][c + 3] = fmaf(xx[r], uu[c / 4].w, acc[r][c + 3]);
         }
-      }
-      br += width;
+    };
+    fetch(0, x[0], u[0]);
+#pragma unroll 1
+    for (int k = 0; k < k_count; k += 2) {                   // k_count is even
+      fetch(k + 1, x[1], u[1]);
+      fma_step(x[0], u[0]);
+      if (k + 2 < k_count) fetch(k + 2, x[0], u[0]);
+      fma_step(x[1], u[1]);
     }
   }
 };
@@ -150,6 +160,83 @@ __device__ __forceinline__ void put4(T* dst, float a, float b, float c, float d,
     else *reinterpret_cast<float4*>(dst) = make_float4(a, b, c, d);
   } else {
     dst[0] = from_f<T>(a); dst[1] = from_f<T>(b); dst[2] = from_f<T>(c); dst[3] = from_f<T>(d);
+  }
+}
+
+// Warp-level products for 16-bit layers.  A 32-bit factor enters as two 16-bit parts (the rounded number and its rounded
+// remainder, together off by 2^-18 of it).
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void split_pair(float x0, float x1, uint32_t& hi, uint32_t& lo) {
+  hi = tc::pack_bf16(x0, x1);
+  lo = tc::pack_bf16(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xffff0000u));
+}
+// An image of a basis (leading parts, then remainders; blocks of 8 x 8 numbers, eight columns of the product by eight of its
+// inner dimension) into shared memory.  Word `lane` of a block is the lane's half of a B fragment.
+__device__ __forceinline__ void copy_image(const float* image, int words, uint32_t* to, int tid, int threads) {
+  for (int i = tid; i < words / 4; i += threads) tc::cp_async16(to + 4 * i, image + 4 * i, 16);
+  tc::cp_async_commit();
+}
+
+// Q' of 32 R token rows of a 16-bit layer: the rows are A fragments straight from global memory, exact; the basis is split.
+// (K' and V' rows keep their chains of 32-bit multiply-adds; a third to two thirds of all rows are queries.)
+template <int R>
+__device__ __forceinline__ void project_queries(const MqProjectParams& p, const Rows& w, int tile, uint32_t* image) {
+  constexpr int MT = R / 2;                  // runs of 16 rows per warp
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+  const int steps = p.d_head >> 4, tiles = w.rp >> 3, part = ((w.rp + 15) & ~15) * p.d_head / 2;      // words of one image
+  copy_image(p.basis + p.heads[w.h].ukt16_off, 2 * part, image, tid, kPrThreads);
+  uint32_t a[MT][8][4];
+  char* to[MT][2];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {            // rows gid and gid + 8
+      const int row = tile * 32 * R + (warp * MT + mt) * 16 + gid + 8 * i;
+      const bool there = row < w.count;
+      const __nv_bfloat16* src = there ? row_source<__nv_bfloat16>(p, w, row) : nullptr;
+      to[mt][i] = there ? row_target<__nv_bfloat16>(p, w, row) : nullptr;
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int c = 16 * s + 8 * j + 2 * tig;
+          uint32_t x = 0;
+          if (there && c < p.d_head) {
+            if (p.aligned) {
+              x = __ldg(reinterpret_cast<const uint32_t*>(src + c));
+            } else {
+              const uint16_t* e = reinterpret_cast<const uint16_t*>(src + c);
+              x = static_cast<uint32_t>(e[0]) | static_cast<uint32_t>(e[1]) << 16;
+            }
+          }
+          a[mt][s][2 * j + i] = x;
+        }
+    }
+  tc::cp_async_wait<0>();
+  __syncthreads();
+  for (int nt = 0; nt < tiles; ++nt) {
+    float acc[MT][2][4] = {};                // leading parts and remainders apart: twice as many chains
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      if (s >= steps) break;
+      const uint32_t* b = image + (nt * 2 * steps + 2 * s) * 32 + lane;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        mma16(acc[mt][0], a[mt][s], b[0], b[32]);
+        mma16(acc[mt][1], a[mt][s], b[part], b[part + 32]);
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (to[mt][i] != nullptr)
+          *reinterpret_cast<float2*>(reinterpret_cast<float*>(to[mt][i]) + 8 * nt + 2 * tig) =
+              make_float2((acc[mt][0][2 * i] + acc[mt][1][2 * i]) * p.q_scale, (acc[mt][0][2 * i + 1] + acc[mt][1][2 * i + 1]) * p.q_scale);
   }
 }
 
@@ -167,6 +254,12 @@ __global__ void __launch_bounds__(kPrThreads, 3) mq_project_many_kernel(const __
   const int kind = tile < nq ? 0 : tile - nq < tiles_kv ? 1 : 2;
   tile -= kind == 0 ? 0 : kind == 1 ? nq : nq + tiles_kv;
   const Rows w = rows_of(p, kind, blockIdx.y);
+  if constexpr (sizeof(T) == 2) {
+    if (kind == 0 && p.d_head % 16 == 0) {
+      project_queries<R>(p, w, tile, reinterpret_cast<uint32_t*>(sm));
+      return;
+    }
+  }
   const int tid = threadIdx.x, mine = tid % kPrRows, part = tid / kPrRows, row = tile * kPrRows + mine;
   float* xt = sm;                            // [2][32][rows]: a step of the rows, transposed
   float* us = sm + 2 * kPrStep * kPrRows;    // [2][32][rp], kPrPad to spare
@@ -217,7 +310,7 @@ __global__ void __launch_bounds__(kPrThreads, 3) mq_project_many_kernel(const __
       basis(d0 + kPrStep, buf ^ 1);
       fetch(d0 + kPrStep);
     }
-    t.multiply(xt + buf * kPrStep * kPrRows, us + buf * kPrStep * w.rp, min(kPrStep, p.d_head - d0), w.rp);
+    t.multiply(xt + buf * kPrStep * kPrRows, us + buf * kPrStep * w.rp, min(kPrStep, p.d_head - d0), w.rp, kPrRows);
     if (more) put(buf ^ 1);
   }
   const float f = w.kind == 0 ? p.q_scale : 1.f;
@@ -600,70 +693,74 @@ __global__ void __launch_bounds__(256) mq_combine_few_kernel(const MqDecodeParam
   if (!half && d < p.d_head) out_row<T>(p, h, b, row)[d] = from_f<T>(y + ys[d]);
 }
 
-constexpr int kCbRows = 64;
-// Many rows: 64 query rows of one head (of one sequence after the other) against (U^V)^T in shared memory, in the register
-// tiles of the projection.  Two threads merge a row, half of its columns each.
+// Many rows: 64 query rows of one head (of one sequence after the other) against (U^V)^T.
+constexpr int kCbRows = 64, kCbPitch = kCbRows + 4;
+// o' of the CTA's rows, transposed: [rp_v][kCbPitch].  Two threads merge a row, half of its columns each.
+template <typename T>
+__device__ __forceinline__ void merge_rows(const MqDecodeParams& p, const HeadInfo& hd, int h, int tid, float* ot, T** target) {
+  const int total = p.B * p.rows;
+  const int r = tid & (kCbRows - 1), g = blockIdx.x * kCbRows + r;
+  const bool there = g < total;
+  const int b = there ? g / p.rows : 0;
+  // tiles in front of the first sequence here, then of each of those up to this row's own
+  const int b0 = blockIdx.x * kCbRows / p.rows;
+  int64_t before = tiles_before(p, b0);
+  if (p.grid > 0)
+    for (int i = b0; i < b; ++i) before += (p.n - (p.deficit != nullptr ? __ldg(p.deficit + i) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
+  Pieces w{nullptr, 0, 0, 0, 0};
+  if (there) w = pieces_of(p, h * p.B + b, g - b * p.rows, before);
+  if (tid < kCbRows) target[r] = there ? out_row<T>(p, h, b, g - b * p.rows) : nullptr;
+  chain_wait();
+  float M = -INFINITY, L = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < w.count; ++s) M = fmaxf(M, w.at(s)[0]);
+  const float base = M == -INFINITY ? 0.f : M;
+#pragma unroll 4
+  for (int s = 0; s < w.count; ++s) L = fmaf(w.at(s)[1], ex2(w.at(s)[0] - base), L);
+  const float inv = L == 0.f ? 0.f : 1.f / L;                // (a row that sees nothing: its sums are zeros)
+  const int half = hd.rp_v / 2, c_lo = (tid / kCbRows) * half;           // half is a multiple of 4
+  constexpr int kPieces = 8;                                 // 16-byte pieces of the row that are read together
+  for (int c0 = 0; c0 < half; c0 += 4 * kPieces) {
+    float4 o[kPieces];
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int s = 0; s < w.count; ++s) {
+      const float* x = w.at(s);
+      const float f = ex2(x[0] - base) * inv;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        if (c0 + 4 * j >= half) continue;
+        const float4 v = *reinterpret_cast<const float4*>(x + 4 + c_lo + c0 + 4 * j);
+        o[j].x = fmaf(v.x, f, o[j].x); o[j].y = fmaf(v.y, f, o[j].y); o[j].z = fmaf(v.z, f, o[j].z); o[j].w = fmaf(v.w, f, o[j].w);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      if (c0 + 4 * j >= half) continue;
+      float* at = ot + (c_lo + c0 + 4 * j) * kCbPitch + r;
+      at[0] = o[j].x; at[kCbPitch] = o[j].y; at[2 * kCbPitch] = o[j].z; at[3 * kCbPitch] = o[j].w;
+    }
+  }
+}
+
+// fp32 layers, and head widths that are no multiple of 16: the register tiles of the projection.
 template <typename T, int C>
 __global__ void __launch_bounds__(kPrThreads) mq_combine_many_kernel(const __grid_constant__ MqDecodeParams p) {
   extern __shared__ __align__(16) float sm[];
   const int h = blockIdx.y, tid = threadIdx.x;
   const HeadInfo hd = p.heads[h];
-  float* ot = sm;                            // [rp_v][64]: o', transposed
-  float* us = sm + hd.rp_v * kCbRows;       // [rp_v][d_head]
+  float* ot = sm;
+  float* us = sm + hd.rp_v * kCbPitch;      // [rp_v][d_head]
   __shared__ T* target[kCbRows];
-  const int total = p.B * p.rows;
   const float* Ut = p.basis + hd.uvt_off;
   for (int i = tid; i < hd.rp_v * p.d_head / 4; i += kPrThreads) tc::cp_async16(us + 4 * i, Ut + 4 * i, 16);
   tc::cp_async_commit();
-  {
-    const int r = tid & (kCbRows - 1), g = blockIdx.x * kCbRows + r;
-    const bool there = g < total;
-    const int b = there ? g / p.rows : 0;
-    // tiles in front of the first sequence here, then of each of those up to this row's own
-    const int b0 = blockIdx.x * kCbRows / p.rows;
-    int64_t before = tiles_before(p, b0);
-    if (p.grid > 0)
-      for (int i = b0; i < b; ++i) before += (p.n - (p.deficit != nullptr ? __ldg(p.deficit + i) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
-    Pieces w{nullptr, 0, 0, 0, 0};
-    if (there) w = pieces_of(p, h * p.B + b, g - b * p.rows, before);
-    if (tid < kCbRows) target[r] = there ? out_row<T>(p, h, b, g - b * p.rows) : nullptr;
-    chain_wait();
-    float M = -INFINITY, L = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < w.count; ++s) M = fmaxf(M, w.at(s)[0]);
-    const float base = M == -INFINITY ? 0.f : M;
-#pragma unroll 4
-    for (int s = 0; s < w.count; ++s) L = fmaf(w.at(s)[1], ex2(w.at(s)[0] - base), L);
-    const float inv = L == 0.f ? 0.f : 1.f / L;              // (a row that sees nothing: its sums are zeros)
-    const int half = hd.rp_v / 2, c_lo = (tid / kCbRows) * half;         // half is a multiple of 4
-    constexpr int kPieces = 8;                               // 16-byte pieces of the row that are read together
-    for (int c0 = 0; c0 < half; c0 += 4 * kPieces) {
-      float4 o[kPieces];
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-      for (int s = 0; s < w.count; ++s) {
-        const float* x = w.at(s);
-        const float f = ex2(x[0] - base) * inv;
-#pragma unroll
-        for (int j = 0; j < kPieces; ++j) {
-          if (c0 + 4 * j >= half) continue;
-          const float4 v = *reinterpret_cast<const float4*>(x + 4 + c_lo + c0 + 4 * j);
-          o[j].x = fmaf(v.x, f, o[j].x); o[j].y = fmaf(v.y, f, o[j].y); o[j].z = fmaf(v.z, f, o[j].z); o[j].w = fmaf(v.w, f, o[j].w);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) {
-        if (c0 + 4 * j >= half) continue;
-        float* at = ot + (c_lo + c0 + 4 * j) * kCbRows + r;
-        at[0] = o[j].x; at[kCbRows] = o[j].y; at[2 * kCbRows] = o[j].z; at[3 * kCbRows] = o[j].w;
-      }
-    }
-  }
+  merge_rows<T>(p, hd, h, tid, ot, target);
   tc::cp_async_wait<0>();
   __syncthreads();
   RegTile<2, C> t(tid);
-  t.multiply(ot, us, hd.rp_v, p.d_head);
+  t.multiply(ot, us, hd.rp_v, p.d_head, kCbPitch);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     T* dst = target[2 * t.lane + i];
@@ -672,6 +769,59 @@ __global__ void __launch_bounds__(kPrThreads) mq_combine_many_kernel(const __gri
 #pragma unroll
     for (int c = 0; c < C; c += 4)
       if (t.c0 + c < p.d_head) put4(dst + t.c0 + c, t.acc[i][c], t.acc[i][c + 1], t.acc[i][c + 2], t.acc[i][c + 3], whole);
+  }
+}
+
+// 16-bit layers: a warp lifts 16 rows with warp-level products, both factors in two parts (three products: what is left out,
+// remainder times remainder, is 2^-18 of the terms).  NT: runs of 8 output columns.
+template <int NT>
+__global__ void __launch_bounds__(kPrThreads) mq_combine_mma_kernel(const __grid_constant__ MqDecodeParams p) {
+  extern __shared__ __align__(16) float sm[];
+  const int h = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+  const HeadInfo hd = p.heads[h];
+  const int steps = (hd.rp_v + 15) >> 4, tiles = p.d_head >> 3, part = 16 * steps * p.d_head / 2;     // words of one image
+  uint32_t* image = reinterpret_cast<uint32_t*>(sm);
+  float* ot = sm + 2 * part;                                 // [16 steps][kCbPitch]
+  __shared__ __nv_bfloat16* target[kCbRows];
+  copy_image(p.basis + hd.uvl16_off, 2 * part, image, tid, kPrThreads);
+  for (int i = hd.rp_v * kCbPitch + tid; i < 16 * steps * kCbPitch; i += kPrThreads) ot[i] = 0.f;
+  merge_rows<__nv_bfloat16>(p, hd, h, tid, ot, target);
+  tc::cp_async_wait<0>();
+  __syncthreads();
+  float acc[NT][4] = {};
+  for (int s = 0; s < steps; ++s) {
+    const float* x = ot + (16 * s + 2 * tig) * kCbPitch + 16 * warp + gid;
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {            // rows gid, gid + 8 of columns 2 tig, 2 tig + 1, then of the eight columns behind
+      const float* y = x + (i >> 1) * 8 * kCbPitch + (i & 1) * 8;
+      split_pair(y[0], y[kCbPitch], hi[i], lo[i]);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (nt >= tiles) break;
+      const uint32_t* b = image + (nt * 2 * steps + 2 * s) * 32 + lane;
+      mma16(acc[nt], hi, b[0], b[32]);
+      mma16(acc[nt], lo, b[0], b[32]);
+      mma16(acc[nt], hi, b[part], b[part + 32]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    __nv_bfloat16* dst = target[16 * warp + gid + 8 * i];
+    if (dst == nullptr) continue;
+    dst += 2 * tig;
+    const bool whole = reinterpret_cast<uintptr_t>(dst) % 4 == 0;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (nt >= tiles) break;
+      if (whole) {
+        *reinterpret_cast<uint32_t*>(dst + 8 * nt) = tc::pack_bf16(acc[nt][2 * i], acc[nt][2 * i + 1]);
+      } else {
+        dst[8 * nt] = __float2bfloat16_rn(acc[nt][2 * i]);
+        dst[8 * nt + 1] = __float2bfloat16_rn(acc[nt][2 * i + 1]);
+      }
+    }
   }
 }
 
@@ -732,7 +882,9 @@ cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, u
 
 template <typename T, int R, int C>
 static cudaError_t launch_project_many(const MqProjectParams& p, int tiles, int max_rp, cudaStream_t s) {
-  const size_t smem = sizeof(float) * (2 * kPrStep * (32 * R + max_rp) + kPrPad);
+  size_t smem = sizeof(float) * (2 * kPrStep * (32 * R + max_rp) + kPrPad);
+  const size_t image = static_cast<size_t>((max_rp + 15) & ~15) * p.d_head * 4;
+  if (sizeof(T) == 2 && p.with_q && image > smem) smem = image;
   static size_t configured[kMaxDevices] = {};
   const cudaError_t e = ensure_dynamic_smem(mq_project_many_kernel<T, R, C>, smem, configured);
   if (e != cudaSuccess) return e;
@@ -779,13 +931,11 @@ cudaError_t launch_mq_simt(const MqDecodeParams& p, int dtype, cudaStream_t s, u
   return dtype == 0 ? launch_chained(p.chained != 0, mq_simt_kernel<__nv_bfloat16>, grid, 256, smem, s, p) : launch_chained(p.chained != 0, mq_simt_kernel<float>, grid, 256, smem, s, p);
 }
 
-template <typename T, int C>
-static cudaError_t launch_combine_many(const MqDecodeParams& p, int max_rp_v, cudaStream_t s) {
-  const size_t smem = sizeof(float) * (max_rp_v * (kCbRows + p.d_head) + kPrPad);
-  static size_t configured[kMaxDevices] = {};
-  const cudaError_t e = ensure_dynamic_smem(mq_combine_many_kernel<T, C>, smem, configured);
+template <typename Kernel>
+static cudaError_t launch_combine_many(const MqDecodeParams& p, Kernel kernel, size_t smem, size_t (&configured)[kMaxDevices], cudaStream_t s) {
+  const cudaError_t e = ensure_dynamic_smem(kernel, smem, configured);
   if (e != cudaSuccess) return e;
-  return launch_chained(p.chained != 0, mq_combine_many_kernel<T, C>, dim3((p.B * p.rows + kCbRows - 1) / kCbRows, p.H), kPrThreads, smem, s, p);
+  return launch_chained(p.chained != 0, kernel, dim3((p.B * p.rows + kCbRows - 1) / kCbRows, p.H), kPrThreads, smem, s, p);
 }
 template <typename T>
 static cudaError_t launch_combine_t(const MqDecodeParams& p, int max_rp_v, cudaStream_t s) {
@@ -793,7 +943,15 @@ static cudaError_t launch_combine_t(const MqDecodeParams& p, int max_rp_v, cudaS
   if (p.flags & 0x2u) {                      // EA_OUT_LOWRANK
     return launch_chained(p.chained != 0, mq_combine_lowrank_kernel<T>, static_cast<unsigned>(rows), 128, 0, s, p);
   } else if (p.B * p.rows >= 64 && rows >= 2048) {
-    return p.d_head <= 64 ? launch_combine_many<T, 16>(p, max_rp_v, s) : launch_combine_many<T, 32>(p, max_rp_v, s);
+    static size_t configured[4][kMaxDevices] = {};
+    if (sizeof(T) == 2 && p.d_head % 16 == 0) {
+      const size_t smem = static_cast<size_t>((max_rp_v + 15) & ~15) * (p.d_head + kCbPitch) * sizeof(float);
+      return p.d_head <= 64 ? launch_combine_many(p, mq_combine_mma_kernel<8>, smem, configured[0], s)
+                            : launch_combine_many(p, mq_combine_mma_kernel<16>, smem, configured[1], s);
+    }
+    const size_t smem = sizeof(float) * (max_rp_v * (kCbPitch + p.d_head) + kPrPad);
+    return p.d_head <= 64 ? launch_combine_many(p, mq_combine_many_kernel<T, 16>, smem, configured[2], s)
+                          : launch_combine_many(p, mq_combine_many_kernel<T, 32>, smem, configured[3], s);
   } else {
     return launch_chained(p.chained != 0, mq_combine_few_kernel<T>, static_cast<unsigned>(rows), 256, 0, s, p);
   }
