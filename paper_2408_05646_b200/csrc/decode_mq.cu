@@ -100,55 +100,42 @@ __device__ __forceinline__ void store_row(const MqProjectParams& p, const Rows& 
 // Every output is one chain of fused multiply-adds over d_head in ascending order, as in the append kernel: a drafted row
 // that is accepted is bit for bit the row that appending its token would have stored.
 //
-// Many rows: a CTA takes 32 R rows of one head and kind against its basis.  A lane has R rows, a warp a quarter of the
-// columns: the columns' numbers are the same for all lanes, so a 16-byte load from shared memory feeds 4 R multiply-adds of
-// every lane.  With R = 4 the fp32 pipe is the bound, with R = 2 the loads are (a load that all lanes share still takes two
-// turns).  Register tiles of 8 x 4 and 8 x 8 with both operands spread over the lanes were bound by their loads too.
-constexpr int kPrThreads = 128, kPrPad = 64;
+// Many rows: a CTA takes 64 rows of one head and kind against its basis.  A lane has two rows, a warp a quarter of the
+// columns: the columns' numbers are the same for all lanes, so a 16-byte load from shared memory feeds eight multiply-adds of
+// every lane (and still takes two turns: the loads are the bound).  Four rows per lane halve the loads but leave three CTAs
+// per SM instead of five, and a CTA's first loads, past an L2 that the last pass over a long cache has emptied, are a third
+// of its time: 504 tokens of 32 heads 37 us against 36.  Tiles of 8 x 4 and 8 x 8 with both operands spread over the lanes
+// were bound by their loads too.
+constexpr int kPrThreads = 128, kPrRows = 64, kPrPad = 64;
 
-// acc[r][c]: row R lane + r, column c0 + c.  a: [k][32 R], b: [k][width] with kPrPad floats to spare behind it (the last
+// acc[r][c]: row 2 lane + r, column c0 + c.  a: [k][a_pitch], b: [k][width] with kPrPad floats to spare behind it (the last
 // columns of the last warp can lie past the width; they are not stored).
-template <int R, int C>
+template <int C>
 struct RegTile {
-  float acc[R][C];
+  float acc[2][C];
   int lane, c0;
   __device__ __forceinline__ RegTile(int tid) : lane(tid & 31), c0((tid >> 5) * C) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int c = 0; c < C; ++c) acc[r][c] = 0.f;
   }
   __device__ __forceinline__ void multiply(const float* a, const float* b, int k_count, int width, int a_pitch) {
-    const float* ar = a + R * lane;
+    const float* ar = a + 2 * lane;
     const float* br = b + c0;
     if (c0 >= width) return;
-    // the operands of step k + 1 are on their way while those of step k are multiplied
-    float x[2][R];
-    float4 u[2][C / 4];
-    auto fetch = [&](int k, float (&xx)[R], float4 (&uu)[C / 4]) {
-      if constexpr (R == 4) *reinterpret_cast<float4*>(xx) = *reinterpret_cast<const float4*>(ar + k * a_pitch);
-      else *reinterpret_cast<float2*>(xx) = *reinterpret_cast<const float2*>(ar + k * a_pitch);
+#pragma unroll 4
+    for (int k = 0; k < k_count; ++k) {
+      const float2 x = *reinterpret_cast<const float2*>(ar + k * a_pitch);
 #pragma unroll
-      for (int c = 0; c < C / 4; ++c) uu[c] = *reinterpret_cast<const float4*>(br + k * width + 4 * c);
-    };
-    auto fma_step = [&](const float (&xx)[R], const float4 (&uu)[C / 4]) {
-#pragma unroll
-      for (int c = 0; c < C; c += 4)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          acc[r][c] = fmaf(xx[r], uu[c / 4].x, acc[r][c]);
-          acc[r][c + 1] = fmaf(xx[r], uu[c / 4].y, acc[r][c + 1]);
-          acc[r][c + 2] = fmaf(xx[r], uu[c / 4].z, acc[r][c + 2]);
-          acc[r][c + 3] = fmaf(xx[r], uu[c / 4].w, acc[r][c + 3]);
-        }
-    };
-    fetch(0, x[0], u[0]);
-#pragma unroll 1
-    for (int k = 0; k < k_count; k += 2) {                   // k_count is even
-      fetch(k + 1, x[1], u[1]);
-      fma_step(x[0], u[0]);
-      if (k + 2 < k_count) fetch(k + 2, x[0], u[0]);
-      fma_step(x[1], u[1]);
+      for (int c = 0; c < C; c += 4) {
+        const float4 u = *reinterpret_cast<const float4*>(br + c);
+        acc[0][c] = fmaf(x.x, u.x, acc[0][c]); acc[0][c + 1] = fmaf(x.x, u.y, acc[0][c + 1]);
+        acc[0][c + 2] = fmaf(x.x, u.z, acc[0][c + 2]); acc[0][c + 3] = fmaf(x.x, u.w, acc[0][c + 3]);
+        acc[1][c] = fmaf(x.y, u.x, acc[1][c]); acc[1][c + 1] = fmaf(x.y, u.y, acc[1][c + 1]);
+        acc[1][c + 2] = fmaf(x.y, u.z, acc[1][c + 2]); acc[1][c + 3] = fmaf(x.y, u.w, acc[1][c + 3]);
+      }
+      br += width;
     }
   }
 };
@@ -181,73 +168,61 @@ __device__ __forceinline__ void copy_image(const float* image, int words, uint32
   tc::cp_async_commit();
 }
 
-// Q' of 32 R token rows of a 16-bit layer: the rows are A fragments straight from global memory, exact; the basis is split.
-// (K' and V' rows keep their chains of 32-bit multiply-adds; a third to two thirds of all rows are queries.)
-template <int R>
+// Q' of 64 token rows of a 16-bit layer: a warp's 16 rows are A fragments straight from global memory, exact; the basis is
+// split.  (K' and V' rows keep their chains of 32-bit multiply-adds.)
 __device__ __forceinline__ void project_queries(const MqProjectParams& p, const Rows& w, int tile, uint32_t* image) {
-  constexpr int MT = R / 2;                  // runs of 16 rows per warp
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+  uint32_t a[8][4] = {};
+  char* to[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {              // rows gid and gid + 8
+    const int row = tile * kPrRows + warp * 16 + gid + 8 * i;
+    to[i] = nullptr;
+    if (row >= w.count) continue;
+    const __nv_bfloat16* src = row_source<__nv_bfloat16>(p, w, row);
+    to[i] = row_target<__nv_bfloat16>(p, w, row);
+    if (p.aligned) {
+      const uint32_t* x = reinterpret_cast<const uint32_t*>(src) + tig;
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (8 * k < p.d_head) a[k >> 1][2 * (k & 1) + i] = __ldg(x + 4 * k);
+    } else {
+      const uint16_t* x = reinterpret_cast<const uint16_t*>(src) + 2 * tig;
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (8 * k < p.d_head) a[k >> 1][2 * (k & 1) + i] = static_cast<uint32_t>(x[8 * k]) | static_cast<uint32_t>(x[8 * k + 1]) << 16;
+    }
+  }
   const int steps = p.d_head >> 4, tiles = w.rp >> 3, part = ((w.rp + 15) & ~15) * p.d_head / 2;      // words of one image
   copy_image(p.basis + p.heads[w.h].ukt16_off, 2 * part, image, tid, kPrThreads);
-  uint32_t a[MT][8][4];
-  char* to[MT][2];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {            // rows gid and gid + 8
-      const int row = tile * 32 * R + (warp * MT + mt) * 16 + gid + 8 * i;
-      const bool there = row < w.count;
-      const __nv_bfloat16* src = there ? row_source<__nv_bfloat16>(p, w, row) : nullptr;
-      to[mt][i] = there ? row_target<__nv_bfloat16>(p, w, row) : nullptr;
-#pragma unroll
-      for (int s = 0; s < 8; ++s)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int c = 16 * s + 8 * j + 2 * tig;
-          uint32_t x = 0;
-          if (there && c < p.d_head) {
-            if (p.aligned) {
-              x = __ldg(reinterpret_cast<const uint32_t*>(src + c));
-            } else {
-              const uint16_t* e = reinterpret_cast<const uint16_t*>(src + c);
-              x = static_cast<uint32_t>(e[0]) | static_cast<uint32_t>(e[1]) << 16;
-            }
-          }
-          a[mt][s][2 * j + i] = x;
-        }
-    }
   tc::cp_async_wait<0>();
   __syncthreads();
+#pragma unroll 2
   for (int nt = 0; nt < tiles; ++nt) {
-    float acc[MT][2][4] = {};                // leading parts and remainders apart: twice as many chains
+    float acc[2][4] = {};                    // leading parts and remainders apart: twice as many chains
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       if (s >= steps) break;
       const uint32_t* b = image + (nt * 2 * steps + 2 * s) * 32 + lane;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        mma16(acc[mt][0], a[mt][s], b[0], b[32]);
-        mma16(acc[mt][1], a[mt][s], b[part], b[part + 32]);
-      }
+      mma16(acc[0], a[s], b[0], b[32]);
+      mma16(acc[1], a[s], b[part], b[part + 32]);
     }
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (to[mt][i] != nullptr)
-          *reinterpret_cast<float2*>(reinterpret_cast<float*>(to[mt][i]) + 8 * nt + 2 * tig) =
-              make_float2((acc[mt][0][2 * i] + acc[mt][1][2 * i]) * p.q_scale, (acc[mt][0][2 * i + 1] + acc[mt][1][2 * i + 1]) * p.q_scale);
+    for (int i = 0; i < 2; ++i)
+      if (to[i] != nullptr)
+        *reinterpret_cast<float2*>(reinterpret_cast<float*>(to[i]) + 8 * nt + 2 * tig) =
+            make_float2((acc[0][2 * i] + acc[1][2 * i]) * p.q_scale, (acc[0][2 * i + 1] + acc[1][2 * i + 1]) * p.q_scale);
   }
 }
 
-// 128 rows (64 where there would be too few CTAs), d_head in steps of 32: while a step is multiplied, the next one's rows are
-// on their way into registers and its part of the basis into shared memory.
+// d_head in steps of 32: while a step is multiplied, the next one's rows are on their way into registers and its part of the
+// basis into shared memory.
 constexpr int kPrStep = 32;
-template <typename T, int R, int C>
-__global__ void __launch_bounds__(kPrThreads, 3) mq_project_many_kernel(const __grid_constant__ MqProjectParams p) {
+template <typename T, int C>
+__global__ void __launch_bounds__(kPrThreads, C <= 20 ? 5 : 4) mq_project_many_kernel(const __grid_constant__ MqProjectParams p) {
   chain_go();
   extern __shared__ __align__(16) float sm[];
-  constexpr int kPrRows = 32 * R, kPer = kPrThreads / kPrRows;            // rows, threads that load one
+  constexpr int kPer = kPrThreads / kPrRows;                 // threads that load a row
   const int tiles_q = (p.B * p.tokens * p.group + kPrRows - 1) / kPrRows, tiles_kv = (p.B * p.tokens + kPrRows - 1) / kPrRows;
   const int nq = p.with_q ? tiles_q : 0;
   int tile = blockIdx.x;
@@ -256,7 +231,7 @@ __global__ void __launch_bounds__(kPrThreads, 3) mq_project_many_kernel(const __
   const Rows w = rows_of(p, kind, blockIdx.y);
   if constexpr (sizeof(T) == 2) {
     if (kind == 0 && p.d_head % 16 == 0) {
-      project_queries<R>(p, w, tile, reinterpret_cast<uint32_t*>(sm));
+      project_queries(p, w, tile, reinterpret_cast<uint32_t*>(sm));
       return;
     }
   }
@@ -301,7 +276,7 @@ __global__ void __launch_bounds__(kPrThreads, 3) mq_project_many_kernel(const __
   fetch(0);
   if (part == 0) target[mine] = src ? row_target<T>(p, w, row) : nullptr;
   put(0);
-  RegTile<R, C> t(tid);
+  RegTile<C> t(tid);
   for (int d0 = 0, buf = 0; d0 < p.d_head; d0 += kPrStep, buf ^= 1) {
     tc::cp_async_wait<0>();
     __syncthreads();                         // step d0 is there, the other buffers are free
@@ -315,8 +290,8 @@ __global__ void __launch_bounds__(kPrThreads, 3) mq_project_many_kernel(const __
   }
   const float f = w.kind == 0 ? p.q_scale : 1.f;
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    char* at = target[R * t.lane + i];
+  for (int i = 0; i < 2; ++i) {
+    char* at = target[2 * t.lane + i];
     if (at == nullptr) continue;
 #pragma unroll
     for (int c = 0; c < C; c += 4) {
@@ -712,10 +687,10 @@ __device__ __forceinline__ void merge_rows(const MqDecodeParams& p, const HeadIn
   if (tid < kCbRows) target[r] = there ? out_row<T>(p, h, b, g - b * p.rows) : nullptr;
   chain_wait();
   float M = -INFINITY, L = 0.f;
-#pragma unroll 4
+#pragma unroll 2
   for (int s = 0; s < w.count; ++s) M = fmaxf(M, w.at(s)[0]);
   const float base = M == -INFINITY ? 0.f : M;
-#pragma unroll 4
+#pragma unroll 2
   for (int s = 0; s < w.count; ++s) L = fmaf(w.at(s)[1], ex2(w.at(s)[0] - base), L);
   const float inv = L == 0.f ? 0.f : 1.f / L;                // (a row that sees nothing: its sums are zeros)
   const int half = hd.rp_v / 2, c_lo = (tid / kCbRows) * half;           // half is a multiple of 4
@@ -724,7 +699,7 @@ __device__ __forceinline__ void merge_rows(const MqDecodeParams& p, const HeadIn
     float4 o[kPieces];
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
+#pragma unroll 1
     for (int s = 0; s < w.count; ++s) {
       const float* x = w.at(s);
       const float f = ex2(x[0] - base) * inv;
@@ -759,7 +734,7 @@ __global__ void __launch_bounds__(kPrThreads) mq_combine_many_kernel(const __gri
   merge_rows<T>(p, hd, h, tid, ot, target);
   tc::cp_async_wait<0>();
   __syncthreads();
-  RegTile<2, C> t(tid);
+  RegTile<C> t(tid);
   t.multiply(ot, us, hd.rp_v, p.d_head, kCbPitch);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -880,28 +855,16 @@ cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, u
   return cudaGetLastError();
 }
 
-template <typename T, int R, int C>
+template <typename T, int C>
 static cudaError_t launch_project_many(const MqProjectParams& p, int tiles, int max_rp, cudaStream_t s) {
-  size_t smem = sizeof(float) * (2 * kPrStep * (32 * R + max_rp) + kPrPad);
+  size_t smem = sizeof(float) * (2 * kPrStep * (kPrRows + max_rp) + kPrPad);
   const size_t image = static_cast<size_t>((max_rp + 15) & ~15) * p.d_head * 4;
   if (sizeof(T) == 2 && p.with_q && image > smem) smem = image;
   static size_t configured[kMaxDevices] = {};
-  const cudaError_t e = ensure_dynamic_smem(mq_project_many_kernel<T, R, C>, smem, configured);
+  const cudaError_t e = ensure_dynamic_smem(mq_project_many_kernel<T, C>, smem, configured);
   if (e != cudaSuccess) return e;
-  mq_project_many_kernel<T, R, C><<<dim3(tiles, p.H), kPrThreads, smem, s>>>(p);
+  mq_project_many_kernel<T, C><<<dim3(tiles, p.H), kPrThreads, smem, s>>>(p);
   return cudaGetLastError();
-}
-template <typename T, int R>
-static cudaError_t launch_project_ranks(const MqProjectParams& p, int tiles, int max_rp, cudaStream_t s) {
-  switch ((max_rp + 15) / 16) {              // columns of a warp: a quarter of the widest rank, in fours
-    case 1: case 2: return launch_project_many<T, R, 8>(p, tiles, max_rp, s);
-    case 3: return launch_project_many<T, R, 12>(p, tiles, max_rp, s);
-    case 4: return launch_project_many<T, R, 16>(p, tiles, max_rp, s);
-    case 5: return launch_project_many<T, R, 20>(p, tiles, max_rp, s);
-    case 6: return launch_project_many<T, R, 24>(p, tiles, max_rp, s);
-    case 7: return launch_project_many<T, R, 28>(p, tiles, max_rp, s);
-    default: return launch_project_many<T, R, 32>(p, tiles, max_rp, s);
-  }
 }
 template <typename T>
 static cudaError_t launch_project_t(const MqProjectParams& p, int max_rp, cudaStream_t s) {
@@ -913,9 +876,16 @@ static cudaError_t launch_project_t(const MqProjectParams& p, int max_rp, cudaSt
     mq_project_few_kernel<T><<<dim3(tiles(kPfRows), p.H, (max_rp + kPfCols - 1) / kPfCols), 128, 0, s>>>(p);
     return cudaGetLastError();
   }
-  // two CTAs of 128 rows for every SM: 504 tokens of 32 heads 36 us against 41 with 64 rows, 256 tokens (192 CTAs) 26 against 22
-  if (static_cast<int64_t>(tiles(128)) * p.H >= 2 * 148) return launch_project_ranks<T, 4>(p, tiles(128), max_rp, s);
-  return launch_project_ranks<T, 2>(p, tiles(64), max_rp, s);
+  const int n = tiles(kPrRows);
+  switch ((max_rp + 15) / 16) {              // columns of a warp: a quarter of the widest rank, in fours
+    case 1: case 2: return launch_project_many<T, 8>(p, n, max_rp, s);
+    case 3: return launch_project_many<T, 12>(p, n, max_rp, s);
+    case 4: return launch_project_many<T, 16>(p, n, max_rp, s);
+    case 5: return launch_project_many<T, 20>(p, n, max_rp, s);
+    case 6: return launch_project_many<T, 24>(p, n, max_rp, s);
+    case 7: return launch_project_many<T, 28>(p, n, max_rp, s);
+    default: return launch_project_many<T, 32>(p, n, max_rp, s);
+  }
 }
 
 cudaError_t launch_mq_project(const MqProjectParams& p, int dtype, int max_rp, cudaStream_t s, uint64_t* launches) {

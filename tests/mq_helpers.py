@@ -4,13 +4,15 @@ values with a bound on what the kernels' arithmetic may add, and the drafted tre
 The bound (`expected`): the kernels round the stored rows (the expected value starts from the rows as the cache holds them,
 so that costs nothing here) and the output, by at most half a step (2^-8 of the value in bf16, 2^-24 in fp32).  In between
 everything is single precision or a pair of 16-bit numbers with 16 significant bits between them:
-  * Q' is off by 2^-16 of its entries' size and a sum of d_head products by d_head 2^-24 of the sum of their magnitudes,
+  * Q' is off by 2^-16 of its entries' size (a pair of 16-bit numbers holds a 32-bit one to 2^-18: once the basis, once Q'
+    itself) and a sum of d_head products by d_head 2^-24 of the sum of their magnitudes,
     a score's sum of r products by r 2^-24, its bias by 2^-22: together a score is off by at most
         e_s = (2^-16 + (d_head + r + 4) 2^-23) A + 2^-22 |bias|,   A = sum_c (sum_d |q_d U_dc|) |k'_c| / sqrt(d_head);
   * a weight is off by e^{2 e_s} - 1 (numerator and the maximum that is taken out), 2^-16 for its 16-bit pair, 2^-21 for
     the exponential, and the sum over n rows by n 2^-24: e_w = 2.2 max e_s + 2^-15 + (n + 64) 2^-24, once for the
     numerator and once for the sum of the weights;
-  * the lift adds (r + 2) 2^-24 of the sum of its products' magnitudes."""
+  * the lift adds (r + 2) 2^-24 of the sum of its products' magnitudes; with both factors as such pairs, and the product of
+    their remainders left out, 3 * 2^-18 more, which is taken as 2^-16."""
 import math
 
 import numpy as np
@@ -111,7 +113,8 @@ class Case:
         if lowrank:
             return o
         U = np.abs(np.float64(self.U_v[h]))
-        return U @ o + (self.rv[h] + 2) * 2.0 ** -24 * (U @ np.abs(w @ V))
+        pairs = 2.0 ** -16 if self.dtype == BF16 else 0.0
+        return U @ o + ((self.rv[h] + 2) * 2.0 ** -24 + pairs) * (U @ np.abs(w @ V))
 
 
 def check(got, want, slack, dtype, what):
