@@ -5,23 +5,33 @@
 // streams; a tcgen05 product has 128 rows of queries.  An item is a run of 128 query rows of a unit with all its cached
 // rows, in tiles of 128.  The tiles of all items, laid end to end, are cut into one equal range per CTA, one CTA per SM:
 // sequences of any lengths keep every SM busy to the end (with one CTA per piece of an item the last wave and the CTAs'
-// starts, five tiles' worth each, cost a third).  A piece of an item that a CTA works through leaves a partial; the loaders
-// and the issuer of S run on into the next piece while the softmax warps finish the last one.  Roles:
+// starts, five tiles' worth each, cost a third).  A piece of an item that a CTA works through leaves a partial.  Roles:
 //   * two threads stream K' and V' tiles by TMA (64 x 64 boxes of the cache slabs' tensor maps, 128-byte swizzle), each
 //     into a ring of its own: a K' stage is free again when S(t) has read it, two products before the V' stage of the same
-//     tile (with one ring for both the issuer of S waited 1400 cycles a tile for the copies).  Boxes without a row of the sequence, and columns past the rank, arrive as zeros;
-//   * one thread issues S(t) = Q' K'^T, another O' += P V'.  Q' (in shared memory) and P (in TMEM) enter as two 16-bit
+//     tile.  Boxes without a row of the sequence, and columns past the rank, arrive as zeros;
+//   * one warp issues S(t) = Q' K'^T, another O' += P V'.  Q' (in shared memory) and P (in TMEM) enter as two 16-bit
 //     parts each (leading part and remainder, 16 significant bits together), so every product is issued twice over; the
-//     result carries no more than the rounding of the output.  P(t) takes the place of S(t): its leading part the first 64
-//     columns, the remainder the other 64.  S has three buffers: S(t), its softmax, P(t) V' and S(t + 3) into the same
-//     columns are a chain of some 5900 cycles, of which two tiles at a time left the products idle a third of the time;
-//   * sixteen softmax warps, four threads per query row (32 rows of the tile each): a lazy reference that moves only when a
-//     score exceeds it by 8, agreed through one reducing barrier that also orders the loads of S before the stores of P.
-//     (Eight warps were the bound: 2600 cycles a tile against 2300 of the products.)
+//     result carries no more than the rounding of the output.  P(t) takes the place of S(t), 16 rows at a time, so that no
+//     thread overwrites what another still reads;
+//   * three softmax groups of four warps, one per S buffer, a thread per query row: S(t), its softmax, P(t) V' and S(t + 3)
+//     into the same columns are a chain of some 6000 cycles, of which three run at a time.  What the groups share is the
+//     reference of a row, a lazy one that moves only when a score exceeds it by 8: it is handed from tile to tile once a
+//     tile's maximum is known, before its exponentials.  At the end of a piece the group of its last tile writes the
+//     partial, the other two load the next piece's Q' and go on.
+// At most 64 (32) query rows: Q' is in the operand two (four) times, each copy takes a half (quarter) of every tile's rows
+// and leaves a partial of its own; the products cost the same, a softmax thread has half (a quarter) of the work.
+//
+// Bound by the chain of a buffer and, where three overlap, by the products: 1330 cycles a tile of rank 80 by the tensor
+// core's own rate, 1900 to 2050 measured.  16 sequences of 256 to 8192 rows, 8 heads, 128 query rows: 71 us (189 MB: 30 us of
+// copy rate); 8 x 4160 rows, 32 heads, 63 query rows: 90 us.  Before: sixteen softmax warps on one tile with a block-wide
+// maximum, 2700 cycles (88 and 119 us).  Not better: P and V' in halves with barriers of their own (2750 cycles: the issuing
+// warps share their schedulers with the softmax, and every instruction of theirs is fetched anew); boxes of 16 columns for
+// the last part of K', which leave room for more stages; L2 prefetches two tiles ahead.
 // The tiles that hold drafted rows are masked per query; there the softmax warps also clear rows behind the sequence's end
 // and the non-finite values of drafted rows in the V' tile (a product with a zero weight would still carry them): the
 // latter are added at the end to the query rows that do see them.
-// TMEM (512 columns): S[3] (128 each), O' (128).  Every wait is bounded.
+// TMEM (512 columns): S[3] (128 each), O' (128).  Every wait is bounded; one that runs out ends every other one of the
+// launch through the status word.
 #include <cuda_bf16.h>
 
 #include "internal.h"
