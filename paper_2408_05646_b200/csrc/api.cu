@@ -1448,6 +1448,9 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
     }
     p.per = static_cast<int32_t>(per);
     p.splits = static_cast<int32_t>((p.tiles + per - 1) / per);
+    // A tree's launches are chained while the attention's CTAs leave room for the next kernel's (4 heads, 512 rows: 20.4 ->
+    // 16.4 us a call; 352 CTAs for one sequence of 32 heads: 30 -> 36).
+    if (p.tail > 0) p.chained = chunks * p.B * p.splits <= h->sm_count / 2;
   }
   if (h->ev_start) cudaEventRecord(h->ev_start, s);
   cudaError_t e = tc    ? ea::launch_mq_tc(p, L.max_rp_k, L.max_rp_v, s, &h->launches)

@@ -393,8 +393,8 @@ __device__ __forceinline__ int64_t physical_block(const SparseParams& p, int b, 
 // Each kernel of such a chain lets the next one start (chain_go) and waits for the one before it to be complete and visible
 // (chain_wait) in every CTA, before it reads or writes anything that the chain passes on: a grid that ended without waiting
 // would let its successor overtake its predecessor.  Used where a call is many short kernels (block-sparse decode: 16 x 32k
-// rows 185 -> 173 us, one sequence of 131k rows 41 -> 33 us); the three kernels of a tree are slower chained (29 -> 35 us
-// for a batch of one, 153 -> 166 us for the grouped batch), so they are not.
+// rows 185 -> 173 us, one sequence of 131k rows 41 -> 33 us); the three kernels of a tree
+// gain while their grids are small and lose where the waiting CTAs take the place of others (grouped batch 128 -> 131 us).
 __device__ __forceinline__ void chain_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename... Params, typename... Args>
