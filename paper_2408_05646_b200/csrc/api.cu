@@ -337,6 +337,7 @@ constexpr int kMaxGroup = 16;
 constexpr size_t kMqSlots = 65536;       // partials that every scratch holds at least, so that query rows can be split
 
 constexpr int kMqTcMinRows = 16;         // query rows that the warp-level products still serve
+constexpr int kMqCtas = 592;             // largest grid of the warp-level kernel in ranges (partials: slots of items + CTAs)
 constexpr int kMqTcCtas = 296;           // largest grid of the tcgen05 tree kernel (its partials are slots of items + CTAs)
 
 size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t* slots) {
@@ -345,6 +346,8 @@ size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t*
   size_t n = units * rows > kMqSlots ? units * rows : kMqSlots;
   const size_t items = units * ((rows + ea::kMqTcRows - 1) / ea::kMqTcRows);
   if (rows > kMqTcMinRows && (items + kMqTcCtas) * ea::kMqTcRows > n) n = (items + kMqTcCtas) * ea::kMqTcRows;
+  const size_t small = rows < 32 ? rows : 32, ranges = (units * ((rows + 31) / 32) + kMqCtas) * small;
+  if (ranges > n) n = ranges;
   if (off_part) *off_part = off;
   if (slots) *slots = n;
   return align_up(off + n * h->L.part_stride * sizeof(float));
@@ -364,7 +367,7 @@ void make_sparse_layout(const eigen_attn* h, int block_rows, SparseLayout* S) {
   S->off_qp = off;     off = align_up(off + units * kMaxGroup * h->L.max_rp_k * sizeof(float));
   S->off_scores = off; off = align_up(off + units * S->seq_blocks * sizeof(double));
   S->off_list = off;   off = align_up(off + units * S->seq_blocks * sizeof(int32_t));
-  S->slots = units * kMaxGroup > kMqSlots ? units * kMaxGroup : kMqSlots;
+  S->slots = (units + kMqCtas) * kMaxGroup > kMqSlots ? (units + kMqCtas) * kMaxGroup : kMqSlots;
   S->off_part = off;   off = align_up(off + S->slots * h->L.part_stride * sizeof(float));
   S->bytes = off;
 }
@@ -1383,23 +1386,26 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
   // Trees with more than 16 query rows: tcgen05 products, where the layer's slabs have tensor maps (pages then have to lie
   // inside one sequence's slab) and no bias goes onto the scores.
   bool tc = mma && p.tail > 0 && p.rows > kMqTcMinRows && h->tmaps_ok && !h->alibi && h->opt_tree_impl != 1 &&
-                  (!h->paged || h->desc.n_max % (1 << h->page_shift) == 0);
+            (!h->paged || h->desc.n_max % (1 << h->page_shift) == 0);
   // (its tiles are counted in 32 bits)
   tc = tc && ((end >> 7) + 1) * p.B * p.H * ((p.rows + ea::kMqTcRows - 1) / ea::kMqTcRows) < INT32_MAX;
   const ea::MqShape shape = mma ? ea::mq_mma_shape(p.rows, max_rp) : ea::kMqSimtShape;
   p.tile_shift = tc ? 7 : shape.tile_shift;
   const int tile = 1 << p.tile_shift;
   p.tiles = static_cast<int32_t>((end + tile - 1) >> p.tile_shift);
+  // The tiles of all items, for ranges of them.
+  p.item_rows = tc ? ea::kMqTcRows : shape.queries;
+  const int64_t runs = (p.rows + p.item_rows - 1) / p.item_rows, items = runs * p.B * p.H;
+  p.head_tiles = static_cast<int64_t>(p.tiles) * p.B;
+  if (p.list == nullptr && h->max_deficit > 0) {
+    p.head_tiles = 0;
+    for (int b = 0; b < p.B; ++b) p.head_tiles += (p.n - h->deficit[b] + p.tail + tile - 1) >> p.tile_shift;
+  }
+  p.total_tiles = p.head_tiles * p.H * runs;
   if (tc) {
     // one range of tiles per SM
     p.tmaps = h->ws + L.off_tmaps;
     p.status = dev_status(h);
-    p.head_tiles = static_cast<int64_t>(p.tiles) * p.B;
-    if (h->max_deficit > 0) {
-      p.head_tiles = 0;
-      for (int b = 0; b < p.B; ++b) p.head_tiles += (p.n - h->deficit[b] + p.tail + tile - 1) >> p.tile_shift;
-    }
-    p.total_tiles = p.head_tiles * p.H * ((p.rows + ea::kMqTcRows - 1) / ea::kMqTcRows);
     int64_t grid = h->opt_ctas > 0 ? h->opt_ctas : h->sm_count;
     if (grid > kMqTcCtas) grid = kMqTcCtas;
     if (grid > p.total_tiles) grid = p.total_tiles;
@@ -1407,7 +1413,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
     p.cta_tiles = static_cast<int32_t>(p.total_tiles / grid);
     p.cta_extra = static_cast<int32_t>(p.total_tiles % grid);
     p.copies = p.rows <= 32 ? 4 : p.rows <= 64 ? 2 : 1;
-    p.slot_rows = ea::kMqTcRows;
+    p.slot_rows = p.item_rows = ea::kMqTcRows;
   } else {
     // Tiles of a piece: the CTAs run in waves of resident ones, each pays a start-up worth a tile or two; pieces are cut to
     // one size, so a shorter sequence of the batch has fewer of them; the partials must have room.
@@ -1416,7 +1422,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
     if (cap > p.tiles) cap = p.tiles;
     if (cap > 65535) cap = 65535;
     if (cap < 1) cap = 1;
-    int64_t per = p.tiles;
+    int64_t per = p.tiles, least = INT64_MAX;    // tiles of a piece, and what the call then takes in tiles
     if (h->opt_ctas > 0) {
       int64_t splits = (h->opt_ctas + chunks * p.B - 1) / (chunks * p.B);
       if (splits > cap) splits = cap;
@@ -1427,7 +1433,7 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
       const int64_t wave = static_cast<int64_t>(h->sm_count) * shape.ctas_per_sm;
       const bool ragged = h->max_deficit > 0 && p.list == nullptr;
       constexpr int64_t kStart = 2;           // tiles' worth of a CTA's start and end
-      int64_t best = INT64_MAX, last = 0;
+      int64_t last = 0;
       for (int64_t s2 = 1; s2 <= cap && s2 <= 256; ++s2) {
         const int64_t size = (p.tiles + s2 - 1) / s2;
         if (size == last) continue;
@@ -1443,14 +1449,30 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
         } else {
           cost = ((s2 * p.B * chunks + wave - 1) / wave) * (size + kStart);
         }
-        if (cost < best) { best = cost; per = size; }
+        if (cost < least) { least = cost; per = size; }
       }
     }
     p.per = static_cast<int32_t>(per);
+    if (mma && p.total_tiles < INT32_MAX) {
+      // Or one range of tiles for every resident CTA, with a start for every item that it meets: no last wave (16 x 32k rows
+      // 960 -> 943 us, lists of unequal sequences 66 -> 63, 64 x 777 rows 140 -> 138).  Short calls keep one piece per CTA.
+      const int64_t wave = static_cast<int64_t>(h->sm_count) * shape.ctas_per_sm;
+      int64_t grid = h->opt_ctas > 0 ? h->opt_ctas : wave;
+      if (grid > kMqCtas) grid = kMqCtas;
+      if (grid > p.total_tiles) grid = p.total_tiles;
+      const double cost = static_cast<double>(p.total_tiles) / wave + 2. * (static_cast<double>(items) / wave + 1.);
+      if (h->opt_ctas > 0 || cost < static_cast<double>(least)) {
+        p.grid = static_cast<int32_t>(grid);
+        p.cta_tiles = static_cast<int32_t>(p.total_tiles / grid);
+        p.cta_extra = static_cast<int32_t>(p.total_tiles % grid);
+        p.copies = 1;
+        p.slot_rows = runs == 1 ? p.rows : p.item_rows;
+      }
+    }
     p.splits = static_cast<int32_t>((p.tiles + per - 1) / per);
     // A tree's launches are chained while the attention's CTAs leave room for the next kernel's (4 heads, 512 rows: 20.4 ->
     // 16.4 us a call; 352 CTAs for one sequence of 32 heads: 30 -> 36).
-    if (p.tail > 0) p.chained = chunks * p.B * p.splits <= h->sm_count / 2;
+    if (p.tail > 0) p.chained = (p.grid > 0 ? p.grid : chunks * p.B * p.splits) <= h->sm_count / 2;
   }
   if (h->ev_start) cudaEventRecord(h->ev_start, s);
   cudaError_t e = tc    ? ea::launch_mq_tc(p, L.max_rp_k, L.max_rp_v, s, &h->launches)

@@ -535,7 +535,7 @@ struct Pieces {
   int count, fold;
   __device__ __forceinline__ const float* at(int s) const { return first + (s >> fold) * stride + (s & ((1 << fold) - 1)) * step; }
 };
-// The CTA of the tcgen05 kernel that has tile x: the first cta_extra CTAs have a tile more.
+// The CTA whose range has tile x: the first cta_extra CTAs have a tile more.
 __device__ __forceinline__ int cta_of_tile(const MqDecodeParams& p, int x) {
   const int cut = p.cta_extra * (p.cta_tiles + 1);
   return x < cut ? x / (p.cta_tiles + 1) : p.cta_extra + (x - cut) / p.cta_tiles;
@@ -548,17 +548,18 @@ __device__ __forceinline__ Pieces pieces_of(const MqDecodeParams& p, int unit, i
                                       : (p.n - (p.deficit != nullptr ? __ldg(p.deficit + b) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
   if (p.grid == 0)
     return {p.partials + (static_cast<int64_t>(unit) * p.rows + row) * p.splits * p.part_stride, 0, p.part_stride, max(1, (tiles + p.per - 1) / p.per), 0};
-  const int chunks = (p.rows + kMqTcRows - 1) / kMqTcRows, chunk = row / kMqTcRows;
+  const int chunks = (p.rows + p.item_rows - 1) / p.item_rows, chunk = row / p.item_rows;
   const int64_t x = (h * p.head_tiles + before) * chunks + static_cast<int64_t>(chunk) * tiles;
   const int c0 = cta_of_tile(p, static_cast<int>(x)), c1 = cta_of_tile(p, static_cast<int>(x) + tiles - 1);
   const int64_t slot = static_cast<int64_t>(unit) * chunks + chunk + c0;
   const int fold = p.copies >> 1;            // (1, 2 or 4 copies)
-  return {p.partials + (slot * p.slot_rows + (row - chunk * kMqTcRows)) * p.part_stride, static_cast<int64_t>(p.slot_rows >> fold) * p.part_stride,
+  return {p.partials + (slot * p.slot_rows + (row - chunk * p.item_rows)) * p.part_stride, static_cast<int64_t>(p.slot_rows >> fold) * p.part_stride,
           static_cast<int64_t>(p.slot_rows) * p.part_stride, (c1 - c0 + 1) << fold, fold};
 }
 // Tiles of the sequences in front of b, by a whole warp.
 __device__ __forceinline__ int64_t tiles_before(const MqDecodeParams& p, int b) {
   if (p.grid == 0) return 0;
+  if (p.list != nullptr) return static_cast<int64_t>(b) * p.tiles;
   if (p.deficit == nullptr) return static_cast<int64_t>(b) * ((p.n + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift);
   int64_t sum = 0;
   for (int i = threadIdx.x & 31; i < b; i += 32) sum += (p.n - __ldg(p.deficit + i) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
@@ -681,7 +682,7 @@ __device__ __forceinline__ void merge_rows(const MqDecodeParams& p, const HeadIn
   const int b0 = blockIdx.x * kCbRows / p.rows;
   int64_t before = tiles_before(p, b0);
   if (p.grid > 0)
-    for (int i = b0; i < b; ++i) before += (p.n - (p.deficit != nullptr ? __ldg(p.deficit + i) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
+    for (int i = b0; i < b; ++i) before += p.list != nullptr ? p.tiles : (p.n - (p.deficit != nullptr ? __ldg(p.deficit + i) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
   Pieces w{nullptr, 0, 0, 0, 0};
   if (there) w = pieces_of(p, h * p.B + b, g - b * p.rows, before);
   if (tid < kCbRows) target[r] = there ? out_row<T>(p, h, b, g - b * p.rows) : nullptr;

@@ -14,8 +14,8 @@
 // Heads narrower than the instance keep zeros in the rest of their rows: the products run over the instance's width
 // without a branch (guards per piece of a row cut the code into short blocks that cannot overlap: twice the time).
 //
-// Bound by the bytes of K' and V' where rows are long: 16 sequences of 32k rows with 4 drafted tokens, 32 heads of rank 80,
-// 5.37 GB in 815 us.  Three CTAs per SM for rank 80 (tiles of 64 rows) read no faster: 992 us for the whole call against 918.
+// Bound by the bytes of K' and V' where rows are long: 16 sequences of 32k rows with 16 drafted tokens, 32 heads of rank 80,
+// 5.37 GB in 847 us.  Three CTAs per SM for rank 80 (tiles of 64 rows) read no faster: 992 us for the whole call against 918.
 #include <cuda_bf16.h>
 
 #include "internal.h"
@@ -93,6 +93,50 @@ struct Shape {
   static_assert(NC % 2 == 0 && kStages >= 2, "instance does not fit");
 };
 
+// What a CTA works on: a piece of one item (unit, run of query rows), or, in ranges, one piece after the other.
+struct Item {
+  int h, b, chunk, t;        // first tile of the piece
+  int tiles;                 // of the item
+};
+__device__ __forceinline__ int item_tiles(const MqDecodeParams& p, int b) {
+  if (p.list != nullptr) return p.tiles;
+  return (p.n - (p.deficit != nullptr ? __ldg(p.deficit + b) : 0) + p.tail + (1 << p.tile_shift) - 1) >> p.tile_shift;
+}
+// The item that tile x of all of them belongs to.  By whole warps (sequences of unequal lengths are searched 32 at a time).
+__device__ __forceinline__ Item item_of(const MqDecodeParams& p, int x, int chunks, int lane) {
+  Item w;
+  const int per_head = static_cast<int>(p.head_tiles) * chunks;
+  w.h = x / per_head;
+  int rest = x - w.h * per_head;
+  w.b = 0;
+  if (p.deficit == nullptr || p.list != nullptr) {
+    w.tiles = p.tiles;
+    w.b = rest / (p.tiles * chunks);
+    rest -= w.b * p.tiles * chunks;
+  } else {
+    for (int b0 = 0; b0 < p.B; b0 += 32) {
+      int scan = b0 + lane < p.B ? item_tiles(p, b0 + lane) * chunks : 0;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(kFull, scan, d);
+        if (lane >= d) scan += y;
+      }
+      const unsigned past = __ballot_sync(kFull, rest < scan);            // sequences that end behind the place
+      if (past) {
+        const int k = __ffs(past) - 1;
+        if (k > 0) rest -= __shfl_sync(kFull, scan, k - 1);
+        w.b = b0 + k;
+        break;
+      }
+      rest -= __shfl_sync(kFull, scan, 31);
+    }
+    w.tiles = item_tiles(p, w.b);
+  }
+  w.chunk = rest / w.tiles;
+  w.t = rest - w.chunk * w.tiles;
+  return w;
+}
+
 // Where the rows of a key group come from: runs of 16 neighbouring rows (a block can be 16 rows long).
 struct Source {
   int64_t row[2];          // physical first row of each half
@@ -115,21 +159,29 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
   const int kg = warp & 3, rg = warp >> 2;                                // key group, share of the queries
   const int chunks = (p.rows + S::kQueries - 1) / S::kQueries;
-  const int unit = blockIdx.x / chunks, chunk = blockIdx.x - unit * chunks, split = blockIdx.y;
-  const int h = unit / p.B, b = unit - h * p.B;
+  Item item;
+  int left = 0;                                                           // tiles of the CTA's range from here on
+  if (p.grid > 0) {
+    const int c = blockIdx.x;
+    item = item_of(p, c * p.cta_tiles + min(c, p.cta_extra), chunks, lane);
+    left = p.cta_tiles + (c < p.cta_extra ? 1 : 0);
+  } else {
+    const int unit = blockIdx.x / chunks;
+    item.h = unit / p.B; item.b = unit - item.h * p.B; item.chunk = blockIdx.x - unit * chunks;
+    item.t = blockIdx.y * p.per;
+    item.tiles = item_tiles(p, item.b);
+  }
+  chain_wait();                        // drafted rows, queries, the list: from the kernels before
+  if (p.grid == 0 && item.t > 0 && item.t >= item.tiles) return;          // a shorter sequence: nothing left (its first piece always reports)
+  for (;;) {
+  const int h = item.h, b = item.b, unit = h * p.B + b, chunk = item.chunk;
   const HeadInfo hd = p.heads[h];
   const int nck = hd.rp_k >> 3, ncv = hd.rp_v >> 3;                       // pieces of this head's rows
   constexpr int kpitch = S::kPitch, vpitch = S::kPitch;
   const int row0 = chunk * S::kQueries;                                   // first query row of the CTA
 
   const int n_b = p.deficit != nullptr ? p.n - __ldg(p.deficit + b) : p.n;
-  const int64_t end = p.list ? static_cast<int64_t>(p.list_len) << p.block_shift : static_cast<int64_t>(n_b) + p.tail;
-  const int nt = static_cast<int>((end + S::kTile - 1) >> S::kTileShift);
-  const int t_lo = split * p.per, t_hi = min(nt, t_lo + p.per);
-  if (split > 0 && t_lo >= nt) {             // a shorter sequence: nothing left (its first piece always reports)
-    chain_wait();
-    return;
-  }
+  const int t_lo = item.t, t_hi = min(item.tiles, t_lo + (p.grid > 0 ? left : p.per));
   const int32_t* list = p.list ? p.list + static_cast<int64_t>(unit) * p.list_len : nullptr;
   const char* k_slab = p.cache + hd.k_off;
   const char* v_slab = p.cache + hd.v_off;
@@ -237,7 +289,6 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
       uint4* row = reinterpret_cast<uint4*>(ring + i * kpitch);
       for (int c = (i / kRows) & 1 ? ncv : nck; c < NC; ++c) row[c] = make_uint4(0u, 0u, 0u, 0u);
     }
-  chain_wait();                        // drafted rows, queries, the list: from the kernels before
   fetch_block(t_lo, blk_now);
   fetch_page(t_lo, blk_now, page_now);
   fetch_block(t_lo + 1, blk_next);
@@ -508,10 +559,24 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
 #pragma unroll
     for (int w = 0; w < kGroups; ++w)
       acc = fmaf(c < rp_v ? wo[(w * Q + q) * OS + c] : wl[w * Q + q], ex2(wm[w * Q + q] - mb), acc);
-    float* part = p.partials + ((static_cast<int64_t>(unit) * p.rows + row0 + q) * p.splits + split) * p.part_stride;
+    float* part = p.partials + (p.grid > 0 ? (static_cast<int64_t>(unit) * chunks + chunk + blockIdx.x) * p.slot_rows + q
+                                           : (static_cast<int64_t>(unit) * p.rows + row0 + q) * p.splits + blockIdx.y) * p.part_stride;
     if (c < rp_v) part[4 + c] = acc;
     else if (c == rp_v) part[1] = acc;
     else part[0] = M;
+  }
+  left -= t_hi - t_lo;
+  if (left <= 0) break;                // (one piece per CTA: left is 0)
+  item.t = 0;
+  if (++item.chunk == chunks) {
+    item.chunk = 0;
+    if (++item.b == p.B) {
+      item.b = 0;
+      ++item.h;
+    }
+    item.tiles = item_tiles(p, item.b);
+  }
+  __syncthreads();                     // the ring and the masks are the next piece's
   }
 }
 
@@ -522,7 +587,7 @@ cudaError_t launch_instance(const MqDecodeParams& p, cudaStream_t s) {
   const cudaError_t e = ensure_dynamic_smem(mq_mma_kernel<NC, MT, WG>, S::kSmem, configured);
   if (e != cudaSuccess) return e;
   const int chunks = (p.rows + S::kQueries - 1) / S::kQueries;
-  return launch_chained(p.chained != 0, mq_mma_kernel<NC, MT, WG>, dim3(p.B * p.H * chunks, p.splits), S::kThreads, S::kSmem, s, p);
+  return launch_chained(p.chained != 0, mq_mma_kernel<NC, MT, WG>, p.grid > 0 ? dim3(p.grid) : dim3(p.B * p.H * chunks, p.splits), S::kThreads, S::kSmem, s, p);
 }
 template <int NC>
 cudaError_t launch_rank(const MqDecodeParams& p, cudaStream_t s) {

@@ -307,12 +307,13 @@ struct MqDecodeParams {
   int32_t lr_v_width;       // sum of rp_v: width of a packed output row of one query head
   uint32_t flags;
   PageMap pages;
-  // tcgen05 kernel (grid > 0): the tiles of all items (unit, run of 128 query rows), laid end to end, in equal ranges.
+  // Ranges (grid > 0; the tcgen05 kernel always, the warp-level one where it pays): the tiles of all items (unit, run of
+  // item_rows query rows), laid end to end, in equal ranges.
   // A CTA has cta_tiles of them, the first cta_extra CTAs one more; the piece of item u on CTA c leaves the partials of u's
   // rows in slot u + c, [slot_rows][part_stride] (unique along the staircase of pieces).
   // `copies` (1, 2 or 4): how often the 128 rows of an item hold its query rows, each copy with a share of every tile's cached
   // rows; copy j of query row r has partial row r + j slot_rows / copies.
-  int32_t grid, slot_rows, cta_tiles, cta_extra, copies;
+  int32_t grid, slot_rows, cta_tiles, cta_extra, copies, item_rows;
   int64_t total_tiles, head_tiles;   // of all items; of all sequences for one head and run of query rows
   const void* tmaps;        // CUtensorMap[2 * H]: K' and V' slab of every head
   int* status;              // (its waits are bounded)
