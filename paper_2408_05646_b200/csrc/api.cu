@@ -1460,8 +1460,9 @@ ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int6
       int64_t grid = h->opt_ctas > 0 ? h->opt_ctas : wave;
       if (grid > kMqCtas) grid = kMqCtas;
       if (grid > p.total_tiles) grid = p.total_tiles;
-      const double cost = static_cast<double>(p.total_tiles) / wave + 2. * (static_cast<double>(items) / wave + 1.);
-      if (h->opt_ctas > 0 || cost < static_cast<double>(least)) {
+      const int64_t most = (p.total_tiles + grid - 1) / grid;               // tiles of a range, and the items that it can meet
+      const int64_t met = most > 1 ? (most - 2) * items / p.total_tiles + 2 : 1;
+      if (h->opt_ctas > 0 || most + 2 * met <= least) {
         p.grid = static_cast<int32_t>(grid);
         p.cta_tiles = static_cast<int32_t>(p.total_tiles / grid);
         p.cta_extra = static_cast<int32_t>(p.total_tiles % grid);
