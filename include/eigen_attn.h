@@ -261,7 +261,7 @@ ea_status eigen_attn_quant_layout(eigen_attn_t h, int32_t head, size_t* slab_off
  * ancestors').  A token whose mask is empty attends the cached rows alone; with no cached row either its output is zero.
  * A masked token takes no part, whatever its rows hold.  d_q, d_out: [B][T][H * group][d_head] with element strides
  * (batch, token), query head hq = kv_head * group + i as in eigen_attn_decode_gqa, 1 <= group <= 16.  Lengths may be zero
- * and may differ (eigen_attn_set_lens); a page table is followed; both dtypes; every rank and d_head.  An ALiBi bias counts
+ * and may differ (eigen_attn_set_lens), up to 2^31 - 513 rows; a page table is followed; both dtypes; every rank and d_head.  An ALiBi bias counts
  * positions: drafted token t sits at len_b + (number of other tokens in its mask); only with group 1.  Not with a rotary
  * embedding (EA_ERR_UNSUPPORTED).  flags: EA_Q_PREPROJECTED (d_q: packed [B][T][group * sum rp_k], head h at group *
  * offs_k[h], query head i of its group rp_k[h] further each), EA_KV_PREPROJECTED, EA_OUT_LOWRANK (packed like q with rp_v).

@@ -334,6 +334,7 @@ ea_status check_quant_args(eigen_attn_t h, const char* who, int32_t bits, int32_
 }
 
 constexpr int kMaxGroup = 16;
+constexpr int kMqMaxLen = INT32_MAX - 512;     // rows of a tree's or a block list's sequence: tiles are rounded up in 32 bits
 constexpr size_t kMqSlots = 65536;       // partials that every scratch holds at least, so that query rows can be split
 
 constexpr int kMqTcMinRows = 16;         // query rows that the warp-level products still serve
@@ -1367,6 +1368,7 @@ ea_status check_mq(eigen_attn_t h, const char* who, int32_t group) {
   if (h->rope) return fail(h, EA_ERR_UNSUPPORTED, "%s: not available with a rotary embedding", who);
   if (h->alibi && group > 1)
     return fail(h, EA_ERR_UNSUPPORTED, "%s: an ALiBi bias is per K/V head: not available with group %d", who, group);
+  if (h->len > kMqMaxLen) return fail(h, EA_ERR_UNSUPPORTED, "%s: %d rows (at most %d)", who, h->len, kMqMaxLen);
   return EA_OK;
 }
 
