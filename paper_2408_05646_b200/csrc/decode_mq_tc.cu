@@ -98,7 +98,7 @@ struct __align__(16) TcHeader {
   float sums[2][kBufs - 1][kTile];            // row sums of the other groups at a piece's end; pieces take turns
 };
 constexpr int kSingles = 4 * kMaxStages + 6 * kBufs;         // barriers with one arrival
-constexpr int kHeaderBytes = 3072;
+constexpr int kHeaderBytes = 3 * 1024;
 static_assert(sizeof(TcHeader) <= kHeaderBytes, "header outgrew its area");
 
 __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t& hi, uint32_t& lo) {
