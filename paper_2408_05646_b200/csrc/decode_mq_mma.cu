@@ -84,7 +84,7 @@ struct Shape {
   static constexpr int kCtas = WG == 2 ? 1 : NC <= 8 && MT == 1 ? 3 : 2;  // resident CTAs per SM
   static constexpr bool kQReg = MT * NC * 2 <= 40;                        // Q' fragments in registers, else in shared memory
   static constexpr int kQBytes = kQReg ? 0 : WG * MT * (NC / 2) * 32 * 16;
-  static constexpr int kHead = 32 * 8 + 64 * 4;                           // masks of the queries, places of the drafted rows
+  static constexpr int kHead = 32 * 8 + 64 * 4;                           // masks of the queries, positions of the drafted rows
   static constexpr int kRoom = (kCtas == 3 ? 75 : kCtas == 2 ? 113 : 226) * 1024 - kHead - kQBytes;
   static constexpr int kStages = kRoom / (kGroups * kSlot) < 4 ? kRoom / (kGroups * kSlot) : 4;
   static constexpr int kMerge = kGroups * kQueries * (2 + 8 * NC + 1) * 4;
@@ -302,9 +302,11 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
         const int r = row0 + tid;
         q_mask[tid] = r < p.rows ? tree_mask(masks[r / p.group], p.tokens) : 0;
       }
-      if (bias && tid < p.tokens) draft_pos[tid] = static_cast<float>(n_b + tree_depth(tree_mask(masks[tid], p.tokens), tid));
+      if (bias && tid < p.tokens) draft_pos[tid] = static_cast<float>(tree_depth(tree_mask(masks[tid], p.tokens), tid));
     }
     uint32_t qa[S::kQReg ? MT : 1][S::kQReg ? NKS : 1][4];
+    // Positions count from the first row behind the cached ones: they are small where a bias lets a row weigh anything, and
+    // exact in single precision there (counted from the front, neighbours past 2^24 rows would become one number).
     float q_pos[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -327,10 +329,10 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
           q_img[((rg * MT + mt) * NKS + ks) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
         }
       }
-      q_pos[mt] = static_cast<float>(n_b - 1);
+      q_pos[mt] = -1.f;
       if (p.tail && bias && r < p.rows) {
         const int t = r / p.group;
-        q_pos[mt] = static_cast<float>(n_b + tree_depth(tree_mask(masks[t], p.tokens), t));
+        q_pos[mt] = static_cast<float>(tree_depth(tree_mask(masks[t], p.tokens), t));
       }
     }
     __syncthreads();
@@ -412,7 +414,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float place = static_cast<float>(first[j >> 1] + 8 * (j & 1) + 2 * tig + e);
+            const float place = static_cast<float>(first[j >> 1] - n_b + 8 * (j & 1) + 2 * tig + e);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) sc[mt][j][e] = fmaf(hd.alibi_slope2, place - q_pos[mt], sc[mt][j][e]);
           }
@@ -425,7 +427,7 @@ __global__ void __launch_bounds__(Shape<NC, MT, WG>::kThreads, Shape<NC, MT, WG>
             const int kk = 8 * (j & 1) + 2 * tig + e;                       // inside its half
             const int r = first[j >> 1] < 0 ? row_end : first[j >> 1] + kk;
             const bool drafted = r >= n_b && r < row_end;
-            const float place = bias ? (drafted ? draft_pos[r - n_b] : static_cast<float>(r)) : 0.f;
+            const float place = bias ? (drafted ? draft_pos[r - n_b] : static_cast<float>(r - n_b)) : 0.f;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
               bool open = r < n_b;
