@@ -45,7 +45,7 @@ struct Layout {
   std::vector<HeadInfo> heads;
   size_t cache_bytes = 0;
   // workspace
-  size_t off_status = 0, off_heads = 0, off_basis = 0, off_partials = 0, off_counters = 0, off_staging = 0, off_qp = 0, off_tmaps = 0, off_rope = 0, off_deficit = 0, off_qlens = 0, off_pages = 0, off_krot = 0, off_tmaps_krot = 0;
+  size_t off_status = 0, off_zeros = 0, off_heads = 0, off_basis = 0, off_partials = 0, off_counters = 0, off_staging = 0, off_qp = 0, off_tmaps = 0, off_rope = 0, off_deficit = 0, off_qlens = 0, off_pages = 0, off_krot = 0, off_tmaps_krot = 0;
   bool rope_scratch = false;   // the workspace holds the rotated queries and lifted keys of a prompt (EA_ROPE_PROMPT_SCRATCH)
   size_t page_entries = 0;   // capacity of the page-table area, in entries
   size_t basis_floats = 0, staging_each = 0, workspace_bytes = 0;
@@ -110,6 +110,7 @@ void make_layout(const ea_desc* d, Layout* L) {
   L->part_stride = 4 + L->max_rp_v;
   size_t off = 0;
   L->off_status = off;   off = align_up(off + 64);
+  L->off_zeros = off;    off = align_up(off + ea::kZeroBytes);
   L->off_heads = off;    off = align_up(off + sizeof(HeadInfo) * H);
   L->off_basis = off;    off = align_up(off + basis * sizeof(float));
   L->off_partials = off;
@@ -778,13 +779,14 @@ ea_status eigen_attn_create(const ea_desc* desc, void* d_cache, size_t cache_byt
   h->ws = static_cast<char*>(d_workspace);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaMemsetAsync(h->ws + L.off_status, 0, 64, s);
+  if (e == cudaSuccess) e = cudaMemsetAsync(h->ws + L.off_zeros, 0, ea::kZeroBytes, s);
   if (e == cudaSuccess) e = cudaMemsetAsync(h->ws + L.off_counters, 0, static_cast<size_t>(desc->batch) * H * sizeof(int), s);
   if (e == cudaSuccess)
     e = cudaMemcpyAsync(h->ws + L.off_heads, L.heads.data(), sizeof(HeadInfo) * H, cudaMemcpyHostToDevice, s);
   if (e == cudaSuccess)
     e = cudaMemcpyAsync(h->ws + L.off_basis, basis.data(), basis.size() * sizeof(float), cudaMemcpyHostToDevice, s);
-  // Rows of the cache that no call has written yet must hold finite values: the tensor-core prefill loads
-  // whole 64-row tiles and multiplies the rows past the current length by zero weights.
+  // Rows that no call has written hold zeros.  (Every kernel clears or skips what lies behind a sequence's end, so that
+  // no result depends on it.)
   if (e == cudaSuccess) e = cudaMemsetAsync(h->cache, 0, L.cache_bytes, s);
   std::vector<CUtensorMap> tmaps;
   if (e == cudaSuccess && desc->dtype == EA_BF16 && dh % 16 == 0 &&
@@ -795,7 +797,7 @@ ea_status eigen_attn_create(const ea_desc* desc, void* d_cache, size_t cache_byt
     std::vector<CUtensorMap> kmaps;
     if (e == cudaSuccess && L.rope_scratch && encode_krot_maps(desc, h->ws + L.off_krot, &kmaps)) {
       e = cudaMemcpyAsync(h->ws + L.off_tmaps_krot, kmaps.data(), kmaps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice, s);
-      // rows the first prompt does not write are read by whole key tiles and must be finite
+      // rows the first prompt does not write are read by whole key tiles (their scores are not used)
       if (e == cudaSuccess) e = cudaMemsetAsync(h->ws + L.off_krot, 0, L.off_tmaps_krot - L.off_krot, s);
       h->krot_ok = true;
     }
@@ -1315,6 +1317,7 @@ ea_status eigen_attn_decode_gqa(eigen_attn_t h, const void* d_q, int64_t stride_
   p.partials = reinterpret_cast<float*>(h->ws + L.off_partials);
   p.status = dev_status(h);
   p.tmaps = h->ws + L.off_tmaps;
+  p.zeros = h->ws + L.off_zeros;
   p.deficit = dev_deficit(h);
   p.pages = dev_pages(h);
   p.part_stride = L.part_stride;

@@ -66,12 +66,31 @@ struct __align__(16) GqaSmemHeader {
   unsigned long long kv_full[kGqaMaxStages], kv_empty[kGqaMaxStages];
   unsigned long long s_done[2], p_ready[2], o_done[2];   // per S / P^T buffer
   unsigned long long q_ready;
+  unsigned long long tail_full;                          // copies of a last tile that is cleared behind the sequence's end
   uint32_t tmem_base;
   int abort_flag;
-  float red[2][kMaxGroup][4];                 // per query: the four warps' maxima / sums, alternating between tiles
+  alignas(16) float red[2][kMaxGroup][4];     // per query: the four warps' maxima / sums, alternating between tiles
 };
 static_assert(sizeof(GqaSmemHeader) <= kGqaHeader, "header outgrew its area");
 static_assert(offsetof(GqaSmemHeader, red) % 16 == 0, "the maxima are read as float4");
+
+// The last tile of a sequence can hold rows behind its end.  Their weights are zero, but what the cache holds there need
+// not be finite (rejected drafted tokens, a rewound sequence).  The tile's copies (k_atoms of K', if any, and v_atoms of V')
+// arrive on a barrier of their own, then zeros are copied over the V' rows from `first` on (the swizzle stays inside a row's
+// 128 bytes), and those copies announce the tile on `full`.  One thread.
+__device__ __forceinline__ void load_tail(void* landed, unsigned char* k_tile, int k_atoms, const void* map_k, unsigned char* v_tile,
+                                          int v_atoms, const void* map_v, int row0, int b, int first, void* full, const void* zeros,
+                                          int* status) {
+  mbar_arrive_expect_tx(landed, static_cast<uint32_t>((k_atoms + v_atoms) * kGqaAtom));
+  for (int a = 0; a < k_atoms; ++a)
+    for (int hh = 0; hh < 2; ++hh) tma_load_3d(k_tile + a * kGqaAtom + hh * (kGqaAtom / 2), map_k, a * 64, row0 + hh * 64, b, landed);
+  for (int a = 0; a < v_atoms; ++a)
+    for (int hh = 0; hh < 2; ++hh) tma_load_3d(v_tile + a * kGqaAtom + hh * (kGqaAtom / 2), map_v, a * 64, row0 + hh * 64, b, landed);
+  if (!mbar_wait(landed, 0, status)) return;
+  const uint32_t bytes = static_cast<uint32_t>(kTile - first) * 128;
+  mbar_arrive_expect_tx(full, v_atoms * bytes);
+  for (int a = 0; a < v_atoms; ++a) bulk_load(v_tile + a * kGqaAtom + first * 128, zeros, bytes, full, policy_evict_normal());
+}
 
 // Instruction descriptor with the A operand MN-major (bit 15) and B K-major: O'^T = V'^T P.
 __host__ __device__ constexpr uint32_t instr_desc_a_mn(int n) { return instr_desc(n, false) | (1u << 15); }
@@ -126,6 +145,7 @@ __global__ void __launch_bounds__(kGqaThreads, 1) decode_gqa_kernel(const GqaDec
       mbar_init(&hdr->o_done[i], 1);
     }
     mbar_init(&hdr->q_ready, kThreads);
+    mbar_init(&hdr->tail_full, 1);
     hdr->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -146,6 +166,7 @@ __global__ void __launch_bounds__(kGqaThreads, 1) decode_gqa_kernel(const GqaDec
 
   if (warp == 5) {
     // ------------------------------------------------------------------ TMA producer
+    const int tail_first = n_b - (t_hi - 1) * kTile;         // rows of the last tile
     if (lane == 0) {
       const unsigned char* maps = static_cast<const unsigned char*>(p.tmaps) + static_cast<size_t>(h) * 256;
       const void* map_k = maps;
@@ -156,7 +177,8 @@ __global__ void __launch_bounds__(kGqaThreads, 1) decode_gqa_kernel(const GqaDec
       bool ok = true;
       int stage = 0, issued = 0;
       uint32_t empty_parity = 1;
-      for (int i = 0; i < nt; ++i) {
+      const int whole = tail_first < kTile ? nt - 1 : nt;
+      for (int i = 0; i < whole; ++i) {
         if (i >= stages) {
           ok = mbar_wait(&hdr->kv_empty[stage], empty_parity, p.status) && !*abort_flag;
           if (!ok) { *abort_flag = 1; break; }
@@ -172,6 +194,17 @@ __global__ void __launch_bounds__(kGqaThreads, 1) decode_gqa_kernel(const GqaDec
             tma_load_3d(st + k_bytes + a * kGqaAtom + hh * (kGqaAtom / 2), map_v, a * 64, row0 + hh * 64, b, &hdr->kv_full[stage]);
         ++issued;
         if (++stage == stages) { stage = 0; empty_parity ^= 1u; }
+      }
+      if (whole < nt && ok) {
+        if (whole >= stages) ok = mbar_wait(&hdr->kv_empty[stage], empty_parity, p.status) && !*abort_flag;
+        if (ok) {
+          unsigned char* st = ring + stage * stage_bytes;
+          load_tail(&hdr->tail_full, st, ak, map_k, st + k_bytes, av, map_v, (t_hi - 1) * kTile, b, tail_first, &hdr->kv_full[stage],
+                    p.zeros, p.status);
+          ++issued;
+        } else {
+          *abort_flag = 1;
+        }
       }
       // if the CTA gives up, its copies in flight must land before it leaves
       if (!ok || *abort_flag) {
@@ -424,6 +457,7 @@ constexpr double kGrTwoPi = 6.283185307179586476925286766559;
 
 struct __align__(16) GrSmemHeader {
   unsigned long long k_full[2], x_full[2], kr_ready[2], s_done[2], p_ready[2], o_done[2], v_full[2], v_empty[2];
+  unsigned long long tail_full;               // V' copies of a last tile that is cleared behind the sequence's end
   uint32_t tmem_base;
   int abort_flag;
   alignas(16) float red[2][kMaxGroup][4];     // per query: the four softmax warps' maxima / sums, alternating between tiles
@@ -486,6 +520,7 @@ __global__ void __launch_bounds__(kGrThreads, 1) decode_gqa_rope_kernel(const Gq
       mbar_init(&hdr->v_full[i], 1);
       mbar_init(&hdr->v_empty[i], 1);
     }
+    mbar_init(&hdr->tail_full, 1);
     hdr->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -510,6 +545,7 @@ __global__ void __launch_bounds__(kGrThreads, 1) decode_gqa_rope_kernel(const Gq
   volatile int* abort_flag = &hdr->abort_flag;
   if (warp == kGrWorkers / 32 + 1) {
     // ------------------------------------------------------------------ TMA producer: K' runs a tile ahead of V'
+    const int tail_first = n_b - (t_hi - 1) * kTile;         // rows of the last tile
     if (lane == 0) {
       const unsigned char* maps = static_cast<const unsigned char*>(p.tmaps) + static_cast<size_t>(h) * 256;
       const void* map_k = maps;
@@ -540,9 +576,18 @@ __global__ void __launch_bounds__(kGrThreads, 1) decode_gqa_rope_kernel(const Gq
       int k_issued = 0, v_issued = 0;
       fetch_k(0);
       k_issued = 1;
-      for (int i = 0; i < nt && ok; ++i) {
+      const int whole = tail_first < kTile ? nt - 1 : nt;
+      for (int i = 0; i < whole && ok; ++i) {
         if (i + 1 < nt) { fetch_k(i + 1); if (ok) ++k_issued; }
         if (ok) { fetch_v(i); if (ok) ++v_issued; }
+      }
+      if (whole < nt && ok) {
+        if (whole >= 2) ok = mbar_wait(&hdr->v_empty[whole & 1], ((whole - 2) >> 1) & 1u, p.status) && !*abort_flag;
+        if (ok) {
+          load_tail(&hdr->tail_full, nullptr, 0, nullptr, Vr + (whole & 1) * v_bytes, av, map_v, (t_hi - 1) * kTile, b, tail_first,
+                    &hdr->v_full[whole & 1], p.zeros, p.status);
+          ++v_issued;
+        }
       }
       if (!ok || *abort_flag) {                              // the CTA gives up: its copies in flight must land first
         *abort_flag = 1;

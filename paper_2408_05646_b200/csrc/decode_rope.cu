@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) decode_rope_kernel(const Rope
   const void* map_k = static_cast<const unsigned char*>(p.tmaps) + static_cast<size_t>(h) * 256;
   // K' tile i into buffer i & 1: two boxes of 64 rows per atom column, in the layout the lift's A operand names (no
   // thread moves the tile); elements past the rank and rows past the capacity arrive as zeros, rows between the
-  // sequence's length and the capacity are finite (the cache starts as zeros) and meet zero weights
+  // sequence's length and the capacity give scores that are not used
   // With a page table the tile's rows are where the table says: a page holds whole tiles and lies inside one
   // sequence's slab, so the tile is still two boxes of the slab's tensor map and one contiguous run of V' rows.
   auto fetch_k = [&](int i) {

@@ -49,6 +49,7 @@ constexpr int kDecodeConsumerWarps = 8;
 constexpr int kDecodeThreads = (kDecodeConsumerWarps + 4) * 32;
 constexpr int kMaxHeads = 256;
 constexpr int kStatusTimeout = -6;
+constexpr int kZeroBytes = 16384;       // zeros in the workspace, the source of copies that clear rows behind a sequence's end
 constexpr int kMaxRaggedBatch = 1024;   // largest batch that may hold sequences of unequal lengths
 
 struct DecodeParams {
@@ -226,6 +227,7 @@ struct GqaDecodeParams {     // grouped-query decode (bf16 layers): `group` quer
   const float2* tile_step;  // [64]: cos, sin of -128 phi_i
   const float4* el_table;   // [32][128]: cos, cos, sin, sin of l phi for pairs 2k, 2k + 1 and row offset l
   int32_t interleaved;
+  const void* zeros;        // kZeroBytes of zeros (tcgen05 kernels)
   PageMap pages;            // paged cache (decode_gqa_mma_kernel): a tile of 128 rows lies inside one page
 };
 

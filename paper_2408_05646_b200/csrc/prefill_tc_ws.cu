@@ -7,7 +7,10 @@
 //   * one thread streams the K'/V' tiles of the unit from the rank-r cache into a ring of shared memory
 //     stages by TMA (tensor maps of the cache slabs, 64 x 64 boxes in the 128-byte swizzled layout the
 //     MMA descriptors name; each tile is fetched once for both query tiles).  Elements past the rank
-//     and rows past the capacity arrive as zeros;
+//     and rows past the capacity arrive as zeros.  The last key tile can hold rows behind the sequence's last token: their
+//     weights are zero, but what the cache holds there need not be finite (rejected drafted tokens, a rewound sequence).
+//     Its copies arrive on a barrier of their own, the loading warp clears those rows of V', and only then it announces
+//     the tile (an instantiation of its own, for calls with such a sequence: 4 x 4000 tokens 826 us, 816 without);
 //   * two threads feed the tensor pipe, one per query tile.  S is double-buffered in TMEM (2 x 64
 //     columns per query tile): S(j + 1) is computed while the softmax works on S(j).  Per key tile j the
 //     issuer waits for P(j), issues O' += P(j) V'(j), and once that product has read P(j) issues S(j + 2)
@@ -55,6 +58,7 @@ struct __align__(16) WsHeader {
   unsigned long long p_full[2][2];            // [query tile][buffer]: P written over S, O' rescaled if needed
   unsigned long long o_done[2][2];            // [query tile][buffer]: PV product of a key tile complete (P consumed)
   unsigned long long lift_done;
+  unsigned long long tail_full;               // copies of a last key tile with rows behind the sequence's end
   uint32_t tmem_base;
   int abort_flag;
   float exch[2][2][kTile];                    // [query tile][half][row]: row maxima (main loop), row sums (epilogue)
@@ -112,7 +116,8 @@ __device__ __forceinline__ void issue_s_steps(int ks, uint32_t d_tmem, uint64_t 
   }
 }
 
-template <bool ALIBI>
+// TAIL: a sequence of the call can end inside a key tile.
+template <bool ALIBI, bool TAIL>
 __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const PrefillParams p, int stages) {
   extern __shared__ __align__(1024) unsigned char smem[];
   WsHeader* hdr = reinterpret_cast<WsHeader*>(smem);
@@ -145,6 +150,7 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
     n_tiles[x] = tx < p.T ? (len0 + min(p.T, tx + kTile) + kKeys - 1) / kKeys : 0;
   }
   const int n_max_tiles = max(n_tiles[0], n_tiles[1]);
+  const bool ragged_tail = TAIL && n_max_tiles * kKeys > len0 + p.T;         // rows behind the last token in the last tile
   const int active_groups = (n_tiles[0] > 0) + (n_tiles[1] > 0);
   const int total_rows = p.B * p.T;
 
@@ -163,6 +169,7 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
       }
     }
     mbar_init(&hdr->lift_done, 1);
+    if (TAIL) mbar_init(&hdr->tail_full, 1);
     hdr->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -176,6 +183,7 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
   reg_dealloc<kRegsOther>();
   if (warp == kLoadWarp) {
     // ------------------------------------------------------------------ TMA producer
+    bool tail_issued = false;
     if (lane == 0) {
       const unsigned char* maps = static_cast<const unsigned char*>(p.tmaps) + static_cast<size_t>(h) * 256;
       const void* map_k = p.tmaps_k ? static_cast<const void*>(static_cast<const unsigned char*>(p.tmaps_k) + static_cast<size_t>(h) * 128)
@@ -193,10 +201,15 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
           if (!ok) { *abort_flag = 1; break; }
         }
         unsigned char* st = ring + stage * stage_bytes;
-        mbar_arrive_expect_tx(&hdr->kv_full[stage], static_cast<uint32_t>(stage_bytes));
-        for (int a = 0; a * 64 < rpk16; ++a) tma_load_3d(st + a * kAtomBytes, map_k, a * 64, j * kKeys, b, &hdr->kv_full[stage]);
+        unsigned long long* full = &hdr->kv_full[stage];
+        if constexpr (TAIL) {
+          tail_issued = ragged_tail && j == n_max_tiles - 1;
+          if (tail_issued) full = &hdr->tail_full;
+        }
+        mbar_arrive_expect_tx(full, static_cast<uint32_t>(stage_bytes));
+        for (int a = 0; a * 64 < rpk16; ++a) tma_load_3d(st + a * kAtomBytes, map_k, a * 64, j * kKeys, b, full);
         for (int a = 0; a * 64 < rpv16; ++a)
-          tma_load_3d(st + k_bytes + a * kAtomBytes, map_v, a * 64, j * kKeys, b, &hdr->kv_full[stage]);
+          tma_load_3d(st + k_bytes + a * kAtomBytes, map_v, a * 64, j * kKeys, b, full);
         ++issued;
         if (++stage == stages) { stage = 0; empty_parity ^= 1u; }
       }
@@ -206,7 +219,23 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
         for (int s = 0; s < stages; ++s) {
           int last = -1;                                     // newest tile whose copies went to stage s
           for (int jj = s; jj < issued; jj += stages) last = jj;
+          if (tail_issued && last == n_max_tiles - 1) continue;      // (waited for below)
           if (last >= 0) mbar_wait(&hdr->kv_full[s], (last / stages) & 1u, p.status);
+        }
+      }
+    }
+    if constexpr (TAIL) {
+      __syncwarp();
+      if (__shfl_sync(0xffffffffu, static_cast<int>(tail_issued), 0)) {
+        const int last = n_max_tiles - 1, first = len0 + p.T - last * kKeys;     // first row to clear
+        unsigned char* v_tile = ring + (last % stages) * stage_bytes + k_bytes;
+        if (__all_sync(0xffffffffu, mbar_wait(&hdr->tail_full, 0, p.status))) {
+          for (int a = 0; a * 64 < rpv16; ++a)               // the swizzle stays inside a row's 128 bytes
+            for (int i = first * 8 + lane; i < kKeys * 8; i += 32)
+              reinterpret_cast<uint4*>(v_tile + a * kAtomBytes)[i] = make_uint4(0u, 0u, 0u, 0u);
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&hdr->kv_full[last % stages]);
         }
       }
     }
@@ -549,13 +578,18 @@ int prefill_tc_ws_stages(int max_rp_k, int max_rp_v, int d_head, size_t* smem_by
 
 cudaError_t launch_prefill_tc_ws(const PrefillParams& p, int stages, size_t smem, bool alibi, cudaStream_t s,
                                  uint64_t* launches) {
-  static size_t configured[2][kMaxDevices] = {};
-  const cudaError_t ec = alibi ? ensure_dynamic_smem(prefill_tc_ws_kernel<true>, smem, configured[1])
-                               : ensure_dynamic_smem(prefill_tc_ws_kernel<false>, smem, configured[0]);
+  // (with unequal lengths some sequence ends inside a tile)
+  const bool tail = p.deficit != nullptr || (p.len0 + p.T) % kKeys != 0;
+  static size_t configured[4][kMaxDevices] = {};
+  auto run = [&](auto kernel, size_t (&done)[kMaxDevices]) -> cudaError_t {
+    const cudaError_t e = ensure_dynamic_smem(kernel, smem, done);
+    if (e != cudaSuccess) return e;
+    kernel<<<dim3(p.B * p.H, (p.T + 2 * kTile - 1) / (2 * kTile)), kWsThreads, smem, s>>>(p, stages);
+    return cudaSuccess;
+  };
+  const cudaError_t ec = alibi ? (tail ? run(prefill_tc_ws_kernel<true, true>, configured[3]) : run(prefill_tc_ws_kernel<true, false>, configured[2]))
+                               : (tail ? run(prefill_tc_ws_kernel<false, true>, configured[1]) : run(prefill_tc_ws_kernel<false, false>, configured[0]));
   if (ec != cudaSuccess) return ec;
-  dim3 grid(p.B * p.H, (p.T + 2 * kTile - 1) / (2 * kTile));
-  if (alibi) prefill_tc_ws_kernel<true><<<grid, kWsThreads, smem, s>>>(p, stages);
-  else prefill_tc_ws_kernel<false><<<grid, kWsThreads, smem, s>>>(p, stages);
   ++*launches;
   return cudaGetLastError();
 }

@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(kLiftThreads, 2) rope_lift_tc_kernel(const Pre
   unsigned char* Kt = Us + lift_kb(u_bytes);                 // K' tiles [2], 128-byte swizzle
 
   // rows this sequence holds after the call, up to the end of the 64-row key tile of its last row (the attention
-  // kernel reads whole key tiles; rows past the length meet masked scores and must only be finite)
+  // kernel reads whole key tiles; the scores of rows past the length are not used)
   const int len_b = p.len0 - (p.deficit != nullptr ? __ldg(p.deficit + b) : 0) + p.T;
   const int rows_b = min(min(p.krot_rows, p.n_max), (len_b + 63) & ~63);
   const int nt_b = (rows_b + kTile - 1) / kTile;
