@@ -500,114 +500,6 @@ class EigenAttnLayer:
 
     def _mq_tok(self, x: torch.Tensor, T: int, heads: int):
         """Checks a [B][T][heads][d_head] tensor and returns (ptr, stride_b, stride_t)."""
-        assert x.is_cuda and x.dtype is self.torch_dtype and x.shape == (self.B, T, heads, self.d_head)
-        stride_b, stride_t, stride_h, stride_d = x.stride()
-        assert stride_d == 1 and stride_h == self.d_head
-        return x.data_ptr(), stride_b, stride_t
-
-    def decode_tree(self, q, k, v, mask: torch.Tensor, group: int = 1, out: Optional[torch.Tensor] = None,
-                    q_preprojected: bool = False, kv_preprojected: bool = False, out_lowrank: bool = False,
-                    stream=None) -> torch.Tensor:
-        """eigen_attn_decode_tree: q [B][T][H * group][d_head], k, v [B][T][H][d_head], mask int64 [B][T] (bit s: token t
-        attends drafted token s).  The drafted rows land behind each sequence's own; the lengths stay."""
-        B, T = mask.shape
-        assert mask.is_cuda and mask.dtype == torch.int64 and mask.is_contiguous() and B == self.B
-        flags = 0
-        if q_preprojected:
-            flags |= EA_Q_PREPROJECTED
-            pq, sbq, stq = self._packed(q, T, group * self.offs_k[-1]), 0, 0
-        else:
-            pq, sbq, stq = self._mq_tok(q, T, self.H * group)
-        if kv_preprojected:
-            flags |= EA_KV_PREPROJECTED
-            pk, pv, sbk, stk = self._packed(k, T, self.offs_k[-1]), self._packed(v, T, self.offs_v[-1]), 0, 0
-        else:
-            pk, sbk, stk = self._mq_tok(k, T, self.H)
-            pv, sbv, stv = self._mq_tok(v, T, self.H)
-            assert (sbk, stk) == (sbv, stv), "k and v: the same strides"
-        if out_lowrank:
-            flags |= EA_OUT_LOWRANK
-            if out is None:
-                out = self._new_out(self.B, T, self.offs_v[-1])
-            assert out.is_contiguous()
-            po, sbo, sto = out.data_ptr(), T * self.offs_v[-1], self.offs_v[-1]
-        else:
-            if out is None:
-                out = self._new_out(self.B, T, self.H, self.d_head)
-            po, _, sbo, sto = self._tok(out, T)
-        self._check(lib.eigen_attn_prefill(self.handle, pq, pk, pv, T, sb, stt, po, sbo, sto, flags, _stream_ptr(stream)),
-                    "eigen_attn_prefill")
-        return out
-
-    @property
-    def len(self) -> int:
-        n = ctypes.c_int32(0)
-        self._check(lib.eigen_attn_get_len(self.handle, ctypes.byref(n)), "eigen_attn_get_len")
-        return n.value
-
-    def set_len(self, n: int) -> None:
-        self._check(lib.eigen_attn_set_len(self.handle, int(n)), "eigen_attn_set_len")
-
-    def set_lens(self, lens, stream=None) -> None:
-        """Per-sequence lengths of a batch whose sequences differ in length (host integers, one per sequence)."""
-        arr = (ctypes.c_int32 * self.B)(*[int(x) for x in lens])
-        self._check(lib.eigen_attn_set_lens(self.handle, arr, _stream_ptr(stream)), "eigen_attn_set_lens")
-
-    def lens(self):
-        arr = (ctypes.c_int32 * self.B)()
-        self._check(lib.eigen_attn_get_lens(self.handle, arr), "eigen_attn_get_lens")
-        return list(arr)
-
-    def set_page_table(self, table, page_rows: int = 128, stream=None) -> None:
-        """table: [batch][pages_per_seq] physical page of every logical page (-1 = not mapped); None = contiguous."""
-        if table is None:
-            self._check(lib.eigen_attn_set_page_table(self.handle, None, 0, 0, _stream_ptr(stream)), "eigen_attn_set_page_table")
-            return
-        width = len(table[0])
-        assert len(table) == self.B and all(len(r) == width for r in table)
-        arr = (ctypes.c_int32 * (self.B * width))(*[int(x) for r in table for x in r])
-        self._check(lib.eigen_attn_set_page_table(self.handle, arr, width, int(page_rows), _stream_ptr(stream)),
-                    "eigen_attn_set_page_table")
-
-    def poll_status(self, stream=None) -> None:
-        self._check(lib.eigen_attn_poll_status(self.handle, _stream_ptr(stream)), "eigen_attn_poll_status")
-
-    def set_alibi(self, slopes, stream=None) -> None:
-        """Per-head ALiBi slopes (host floats, one per head); None switches the bias off."""
-        if slopes is None:
-            arr = None
-        else:
-            assert len(slopes) == self.H
-            arr = (ctypes.c_float * self.H)(*[float(x) for x in slopes])
-        self._check(lib.eigen_attn_set_alibi(self.handle, arr, _stream_ptr(stream)), "eigen_attn_set_alibi")
-
-    def decode_gqa(self, q: torch.Tensor, group: int, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        """eigen_attn_decode_gqa: q [B][1][H * group][d_head]; the layer's heads are the K/V heads."""
-        assert q.shape == (self.B, 1, self.H * group, self.d_head) and q.dtype == self.torch_dtype
-        assert q.stride(3) == 1 and q.stride(2) == self.d_head
-        if out is None:
-            out = self._new_out(self.B, 1, self.H * group, self.d_head)
-        assert out.stride(3) == 1 and out.stride(2) == self.d_head
-        self._check(lib.eigen_attn_decode_gqa(self.handle, q.data_ptr(), q.stride(0), int(group), out.data_ptr(),
-                                              out.stride(0), _stream_ptr(stream)), "eigen_attn_decode_gqa")
-        return out
-
-    # -- a tree of drafted tokens per sequence
-    def tree_attach(self, max_tokens: int, group: int = 1) -> torch.Tensor:
-        """Allocates the scratch for trees of up to `max_tokens` drafted tokens (kept on the layer) and attaches it."""
-        n = _sz(0)
-        self._check(lib.eigen_attn_tree_bytes(self.handle, int(max_tokens), int(group), ctypes.byref(n)), "eigen_attn_tree_bytes")
-        self.tree_buf = device_alloc(n.value, self.device)
-        self._check(lib.eigen_attn_tree_attach(self.handle, int(max_tokens), int(group), self.tree_buf.data_ptr(), n.value),
-                    "eigen_attn_tree_attach")
-        return self.tree_buf
-
-    def tree_detach(self) -> None:
-        self._check(lib.eigen_attn_tree_attach(self.handle, 0, 0, None, 0), "eigen_attn_tree_attach")
-        self.tree_buf = None
-
-    def _mq_tok(self, x: torch.Tensor, T: int, heads: int):
-        """Checks a [B][T][heads][d_head] tensor and returns (ptr, stride_b, stride_t)."""
         assert x.is_cuda and x.dtype == self.torch_dtype and x.shape == (self.B, T, heads, self.d_head)
         assert x.stride(3) == 1 and x.stride(2) == self.d_head
         return x.data_ptr(), x.stride(0), x.stride(1)
