@@ -356,6 +356,12 @@ class EigenAttnLayer:
         assert x.is_cuda and x.is_contiguous() and x.dtype == self.torch_dtype and x.shape == (self.B, T, width)
         return x.data_ptr()
 
+    def _one_layout(self, k: torch.Tensor, v: torch.Tensor, stream):
+        """k and v in one layout for a call on `stream`: copies are made there, in front of the call, and their memory goes
+        back to that stream."""
+        with torch.cuda.stream(stream):
+            return k.contiguous(), v.contiguous()
+
     def decode_step(self, q, k, v, out: Optional[torch.Tensor] = None, q_preprojected: bool = False,
                     kv_preprojected: bool = False, out_lowrank: bool = False, stream=None) -> torch.Tensor:
         flags = 0
@@ -371,7 +377,7 @@ class EigenAttnLayer:
             pk, _, sbk, _ = self._tok(k, 1)
             pv, _, sbv, _ = self._tok(v, 1)
             if sbk != sbv:
-                k, v = k.contiguous(), v.contiguous()
+                k, v = self._one_layout(k, v, stream)
                 pk, _, sbk, _ = self._tok(k, 1)
                 pv, _, sbv, _ = self._tok(v, 1)
         if out_lowrank:
@@ -524,7 +530,7 @@ class EigenAttnLayer:
             pk, sbk, stk = self._mq_tok(k, T, self.H)
             pv, sbv, stv = self._mq_tok(v, T, self.H)
             if (sbk, stk) != (sbv, stv):
-                k, v = k.contiguous(), v.contiguous()
+                k, v = self._one_layout(k, v, stream)
                 pk, sbk, stk = self._mq_tok(k, T, self.H)
                 pv = v.data_ptr()
         if out_lowrank:
