@@ -176,7 +176,10 @@ def cache_bytes(batch, n_heads, d_head, n_max, dtype, r_k, r_v=None, max_prefill
 
 
 class EigenAttnLayer:
-    """One decoder layer's rank-r KV cache and the library calls on it (eigen_attn_t)."""
+    """One decoder layer's rank-r KV cache and the library calls on it (eigen_attn_t).
+
+    A call runs on `stream` (default: the current one).  Tensors handed to it must be ready on that stream; results that it
+    creates belong to it, as torch's own do: another stream that uses them waits for it, and record_stream tells the allocator."""
 
     def __init__(self, batch: int, n_heads: int, d_head: int, n_max: int, dtype: torch.dtype,
                  U_k: Sequence[np.ndarray], U_v: Sequence[np.ndarray], max_prefill_tokens: int = 0,
@@ -216,14 +219,19 @@ class EigenAttnLayer:
         self.offs_k, self.offs_v = list(offs_k), list(offs_v)
 
     # -- plumbing
-    def _new_out(self, *shape) -> torch.Tensor:
+    def _new_out(self, *shape, stream=None, dtype=None) -> torch.Tensor:
+        """A result of a call on `stream`, allocated there: memory that another stream's work may still use is not handed to
+        it, and the result's own memory goes back to that stream."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self._new_out(*shape, dtype=dtype)
+        dtype = dtype or self.torch_dtype
         if device_alloc is _default_alloc:
-            return torch.empty(shape, dtype=self.torch_dtype, device=self.device)
-        es = 2 if self.torch_dtype == torch.bfloat16 else 4
-        n = 1
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        n = dtype.itemsize
         for d in shape:
             n *= int(d)
-        return device_alloc(n * es, self.device).view(self.torch_dtype).view(*shape)
+        return device_alloc(n, self.device).view(dtype).view(*shape)
 
     def _check(self, st: int, where: str) -> None:
         if st != EA_OK:
@@ -277,12 +285,12 @@ class EigenAttnLayer:
         if out_lowrank:
             flags |= EA_OUT_LOWRANK
             if out is None:
-                out = self._new_out(self.B, 1, self.offs_v[-1])
+                out = self._new_out(self.B, 1, self.offs_v[-1], stream=stream)
             assert out.is_contiguous() and out.dtype == self.torch_dtype
             sbo = self.offs_v[-1]
         else:
             if out is None:
-                out = self._new_out(self.B, 1, self.H, self.d_head)
+                out = self._new_out(self.B, 1, self.H, self.d_head, stream=stream)
             _, _, sbo, _ = self._tok(out, 1)
         fn = _fn if _fn is not None else lib.eigen_attn_decode
         self._check(fn(self.handle, pq, sbq, out.data_ptr(), sbo, flags, _stream_ptr(stream)), _name)
@@ -297,7 +305,8 @@ class EigenAttnLayer:
     def quant_attach(self, bits: int, group: int, stream=None) -> torch.Tensor:
         """Allocates the quantised buffer (a torch byte tensor kept on the layer) and attaches it."""
         nbytes = self.quant_bytes(bits, group)
-        self.qcache = device_alloc(nbytes, self.device).zero_()
+        with torch.cuda.stream(stream):
+            self.qcache = device_alloc(nbytes, self.device).zero_()
         self.q_group = int(group)
         self._check(lib.eigen_attn_quant_attach(self.handle, int(bits), int(group), self.qcache.data_ptr(), nbytes,
                                                 _stream_ptr(stream)), "eigen_attn_quant_attach")
@@ -346,7 +355,7 @@ class EigenAttnLayer:
         GPU share that array and must be serialised."""
         pq, _, sbq, _ = self._tok(q, 1)
         if out is None:
-            out = self._new_out(self.B, 1, self.H, self.d_head)
+            out = self._new_out(self.B, 1, self.H, self.d_head, stream=stream)
         _, _, sbo, _ = self._tok(out, 1)
         self._check(lib.eigen_attn_decode_static(self.handle, pq, sbq, out.data_ptr(), sbo, 0,
                                                  _stream_ptr(stream)), "eigen_attn_decode_static")
@@ -383,11 +392,11 @@ class EigenAttnLayer:
         if out_lowrank:
             flags |= EA_OUT_LOWRANK
             if out is None:
-                out = self._new_out(self.B, 1, self.offs_v[-1])
+                out = self._new_out(self.B, 1, self.offs_v[-1], stream=stream)
             po, sbo = self._packed(out, 1, self.offs_v[-1]), self.offs_v[-1]
         else:
             if out is None:
-                out = self._new_out(self.B, 1, self.H, self.d_head)
+                out = self._new_out(self.B, 1, self.H, self.d_head, stream=stream)
             po, _, sbo, _ = self._tok(out, 1)
         self._check(lib.eigen_attn_decode_step(self.handle, pq, sbq, pk, pv, sbk, po, sbo, flags, _stream_ptr(stream)),
                     "eigen_attn_decode_step")
@@ -426,12 +435,12 @@ class EigenAttnLayer:
         if out_lowrank:
             flags |= EA_OUT_LOWRANK
             if out is None:
-                out = self._new_out(self.B, T, self.offs_v[-1])
+                out = self._new_out(self.B, T, self.offs_v[-1], stream=stream)
             assert out.is_contiguous()
             po, sbo, sto = out.data_ptr(), T * self.offs_v[-1], self.offs_v[-1]
         else:
             if out is None:
-                out = self._new_out(self.B, T, self.H, self.d_head)
+                out = self._new_out(self.B, T, self.H, self.d_head, stream=stream)
             po, _, sbo, sto = self._tok(out, T)
         self._check(lib.eigen_attn_prefill(self.handle, pq, pk, pv, T, sb, stt, po, sbo, sto, flags, _stream_ptr(stream)),
                     "eigen_attn_prefill")
@@ -484,7 +493,7 @@ class EigenAttnLayer:
         assert q.shape == (self.B, 1, self.H * group, self.d_head) and q.dtype == self.torch_dtype
         assert q.stride(3) == 1 and q.stride(2) == self.d_head
         if out is None:
-            out = self._new_out(self.B, 1, self.H * group, self.d_head)
+            out = self._new_out(self.B, 1, self.H * group, self.d_head, stream=stream)
         assert out.stride(3) == 1 and out.stride(2) == self.d_head
         self._check(lib.eigen_attn_decode_gqa(self.handle, q.data_ptr(), q.stride(0), int(group), out.data_ptr(),
                                               out.stride(0), _stream_ptr(stream)), "eigen_attn_decode_gqa")
@@ -536,11 +545,11 @@ class EigenAttnLayer:
         if out_lowrank:
             flags |= EA_OUT_LOWRANK
             if out is None:
-                out = self._new_out(self.B, T, group * self.offs_v[-1])
+                out = self._new_out(self.B, T, group * self.offs_v[-1], stream=stream)
             po, sbo, sto = self._packed(out, T, group * self.offs_v[-1]), 0, 0
         else:
             if out is None:
-                out = self._new_out(self.B, T, self.H * group, self.d_head)
+                out = self._new_out(self.B, T, self.H * group, self.d_head, stream=stream)
             po, sbo, sto = self._mq_tok(out, T, self.H * group)
         self._check(_call_on(self.device, stream, lib.eigen_attn_decode_tree, self.handle, pq, sbq, stq, group, pk, pv, sbk, stk, T,
                              mask.data_ptr(), po, sbo, sto, flags), "eigen_attn_decode_tree")
@@ -566,7 +575,8 @@ class EigenAttnLayer:
         """Allocates the buffer for block bounds (kept on the layer) and attaches it."""
         n = _sz(0)
         self._check(lib.eigen_attn_sparse_bytes(self.handle, int(block_rows), ctypes.byref(n)), "eigen_attn_sparse_bytes")
-        self.sparse_buf = device_alloc(n.value, self.device)
+        with torch.cuda.stream(stream):
+            self.sparse_buf = device_alloc(n.value, self.device)
         self.sparse_block = int(block_rows)
         self._check(_call_on(self.device, stream, lib.eigen_attn_sparse_attach, self.handle, int(block_rows),
                              self.sparse_buf.data_ptr(), n.value), "eigen_attn_sparse_attach")
@@ -621,19 +631,15 @@ class EigenAttnLayer:
         if out_lowrank:
             flags |= EA_OUT_LOWRANK
             if out is None:
-                out = self._new_out(self.B, 1, group * self.offs_v[-1])
+                out = self._new_out(self.B, 1, group * self.offs_v[-1], stream=stream)
             po, sbo = self._packed(out, 1, group * self.offs_v[-1]), group * self.offs_v[-1]
         else:
             if out is None:
-                out = self._new_out(self.B, 1, self.H * group, self.d_head)
+                out = self._new_out(self.B, 1, self.H * group, self.d_head, stream=stream)
             po, sbo, _ = self._mq_tok(out, 1, self.H * group)
         index = None
         if return_index:
-            shape = (self.B, self.H, max(1, int(n_blocks)))          # (the call refuses less than one block)
-            if device_alloc is _default_alloc:
-                index = torch.empty(shape, dtype=torch.int32, device=self.device)
-            else:
-                index = device_alloc(4 * shape[0] * shape[1] * shape[2], self.device).view(torch.int32).view(shape)
+            index = self._new_out(self.B, self.H, max(1, int(n_blocks)), stream=stream, dtype=torch.int32)   # (the call refuses less than one block)
         self._check(_call_on(self.device, stream, lib.eigen_attn_decode_sparse, self.handle, pq, sbq, group, n_blocks, sink, recent,
                              po, sbo, None if index is None else index.data_ptr(), flags), "eigen_attn_decode_sparse")
         return (out, index) if return_index else out

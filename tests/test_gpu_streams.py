@@ -66,3 +66,49 @@ def test_keys_and_values_of_different_strides(B, dtype, call, delayed):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     del trash
+
+
+def test_what_a_call_allocates_belongs_to_its_stream(B, monkeypatch):
+    """Every result (and buffer) that a call on another stream creates comes from that stream's memory: from the current
+    stream's it could still be in use there."""
+    guarded, seen = B.device_alloc, []
+
+    def alloc(nbytes, device):
+        seen.append(torch.cuda.current_stream())
+        return guarded(nbytes, device)
+    c = Case(B, BF16, 2, 2, 1, 64, [32, 48], [48, 32], [300, 300], 512, seed=9)
+    pre = B.EigenAttnLayer(2, 2, 64, 512, BF16, c.U_k, c.U_v, max_prefill_tokens=64)
+    lay = c.lay
+    lay.tree_attach(6, 2)
+    s = torch.cuda.Stream()
+    q1, q2, qt = randn((2, 1, 2, 64), 1, BF16), randn((2, 1, 4, 64), 2, BF16), randn((2, 6, 4, 64), 3, BF16)
+    k, v = randn((2, 6, 2, 64), 4, BF16), randn((2, 6, 2, 64), 5, BF16)
+    mask = mask_tensor(trees(2, 6, 1)[0])
+    torch.cuda.synchronize()
+    monkeypatch.setattr(B, "device_alloc", alloc)
+    calls = [
+        (1, lambda: lay.decode(q1, stream=s)), (1, lambda: lay.decode(q1, out_lowrank=True, stream=s)),
+        (1, lambda: lay.decode_static(q1, stream=s)), (1, lambda: lay.decode_step(q1, k[:, :1], v[:, :1], stream=s)),
+        (1, lambda: lay.decode_step(q1, k[:, :1], v[:, :1], out_lowrank=True, stream=s)),
+        (1, lambda: lay.decode_gqa(q2, 2, stream=s)),
+        (1, lambda: pre.prefill(k, k, v, stream=s)), (1, lambda: pre.prefill(k, k, v, out_lowrank=True, stream=s)),
+        (1, lambda: lay.decode_tree(qt, k, v, mask, group=2, stream=s)),
+        (1, lambda: lay.decode_tree(qt, k, v, mask, group=2, out_lowrank=True, stream=s)),
+        (1, lambda: lay.sparse_attach(32, stream=s)), (0, lambda: lay.sparse_sync(stream=s)),
+        (2, lambda: lay.decode_sparse(q2, 3, group=2, return_index=True, stream=s)),
+        (1, lambda: lay.decode_sparse(q2, 3, group=2, out_lowrank=True, stream=s)),
+        (1, lambda: lay.quant_attach(4, 32, stream=s)), (0, lambda: lay.quant_sync(stream=s)),
+        (1, lambda: lay.decode_quant(q1, stream=s)),
+    ]
+    current = torch.cuda.current_stream()
+    for i, (count, call) in enumerate(calls):
+        seen.clear()
+        keep = call()
+        assert len(seen) == count and all(x == s for x in seen), i
+        assert torch.cuda.current_stream() == current
+        torch.cuda.synchronize()
+        del keep
+    seen.clear()
+    lay.decode(q1)
+    assert seen == [current]
+    torch.cuda.synchronize()
