@@ -300,7 +300,8 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
  * sparse_sync:   bounds of every complete block that has none yet; asynchronous.  Call it after rows were added:
  *                decode_sparse refuses (EA_ERR_INVALID_ARG) while a block it would have to score has no bounds.  Rows
  *                that the caller rewrites in place, directly or by replaying a captured graph that adds rows, are not
- *                noticed: call set_len or set_lens below them first, or attach again.
+ *                noticed: call set_len or set_lens below them first, or attach again.  Not during stream capture while
+ *                there is a block to do (EA_ERR_UNSUPPORTED): its bounds would be taken for there before the graph has run.
  * sparse_lens:   rows covered by bounds per sequence: HOST [batch].  Shortening a sequence (set_len, set_lens) forgets the
  *                bounds of the blocks it no longer fills; changing the page table forgets all.
  * sparse_layout: where head `head`'s bounds live: byte offset of its slab [B][seq_blocks][2][rp_k] in the cache dtype

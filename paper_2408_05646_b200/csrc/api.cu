@@ -1375,6 +1375,14 @@ ea_status check_mq(eigen_attn_t h, const char* who, int32_t group) {
   return EA_OK;
 }
 
+// For calls whose effect the handle keeps on the host: a captured one would be taken for done before the graph has run.
+ea_status refuse_capture(eigen_attn_t h, const char* who, const char* why, cudaStream_t s) {
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  const cudaError_t e = cudaStreamIsCapturing(s, &capture);
+  if (e != cudaSuccess) return cuda_fail(h, e, who);
+  return capture == cudaStreamCaptureStatusNone ? EA_OK : fail(h, EA_ERR_UNSUPPORTED, "%s: %s: not available during stream capture", who, why);
+}
+
 // The launches behind the query projection: attention over p's rows, then the merge of its pieces with the lift.
 // `slots`: partials the scratch holds.
 // `end`: rows (places of the list) of the longest unit.
@@ -1620,11 +1628,9 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
   if (!equal && B > ea::kMaxRaggedBatch)
     return fail(h, EA_ERR_UNSUPPORTED, "tree_commit: unequal counts with a batch of %d (at most %d)", B, ea::kMaxRaggedBatch);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-  cudaError_t e = cudaStreamIsCapturing(s, &capture);
-  if (e != cudaSuccess) return cuda_fail(h, e, "tree_commit");
-  if (capture != cudaStreamCaptureStatusNone)
-    return fail(h, EA_ERR_UNSUPPORTED, "tree_commit: the lengths live on the host: not available during stream capture");
+  const ea_status captured = refuse_capture(h, "tree_commit", "the lengths live on the host", s);
+  if (captured != EA_OK) return captured;
+  cudaError_t e = cudaSuccess;
   ea::TreeCommitParams p{};
   p.heads = dev_heads(h); p.cache = h->cache; p.deficit = dev_deficit(h); p.pages = dev_pages(h);
   p.B = B; p.H = h->desc.n_heads; p.n = h->len; p.n_max = h->desc.n_max; p.es = h->L.es;
@@ -1721,9 +1727,11 @@ ea_status eigen_attn_sparse_sync(eigen_attn_t h, void* cuda_stream) {
     }
   }
   if (hi <= lo) return EA_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const ea_status captured = refuse_capture(h, "sparse_sync", "which blocks have bounds is kept on the host", s);
+  if (captured != EA_OK) return captured;
   ea::SparseParams p;
   fill_sparse_params(h, &p);
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   constexpr int kStep = 1 << 18;              // the second grid dimension
   for (int b0 = lo; b0 < hi; b0 += kStep) {
     // bounds of a block that has them already are written again where lengths differ: the same values
