@@ -296,7 +296,7 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
  *
  * sparse_bytes:  size of the caller's buffer (bounds and the call's scratch) for blocks of 16, 32, 64 or 128 rows.
  * sparse_attach: hands over that DEVICE buffer (256-byte aligned, owned by the caller); no block has bounds yet.  NULL
- *                detaches.  Synchronises `cuda_stream`.
+ *                detaches.  Synchronises `cuda_stream`; not during stream capture (EA_ERR_UNSUPPORTED).
  * sparse_sync:   bounds of every complete block that has none yet; asynchronous.  Call it after rows were added:
  *                decode_sparse refuses (EA_ERR_INVALID_ARG) while a block it would have to score has no bounds.  Rows
  *                that the caller rewrites in place, directly or by replaying a captured graph that adds rows, are not

@@ -306,11 +306,11 @@ class EigenAttnLayer:
         """Allocates the quantised buffer (a torch byte tensor kept on the layer) and attaches it."""
         nbytes = self.quant_bytes(bits, group)
         with torch.cuda.stream(stream):
-            self.qcache = device_alloc(nbytes, self.device).zero_()
-        self.q_group = int(group)
-        self._check(lib.eigen_attn_quant_attach(self.handle, int(bits), int(group), self.qcache.data_ptr(), nbytes,
-                                                _stream_ptr(stream)), "eigen_attn_quant_attach")
-        return self.qcache
+            buf = device_alloc(nbytes, self.device).zero_()
+        self._check(lib.eigen_attn_quant_attach(self.handle, int(bits), int(group), buf.data_ptr(), nbytes, _stream_ptr(stream)),
+                    "eigen_attn_quant_attach")
+        self.qcache, self.q_group = buf, int(group)        # (the layer keeps the one it had if the call refuses)
+        return buf
 
     def quant_detach(self, stream=None) -> None:
         """Detaches the quantised buffer (eigen_attn_quant_attach with NULL) and drops the tensor."""
@@ -504,10 +504,11 @@ class EigenAttnLayer:
         """Allocates the scratch for trees of up to `max_tokens` drafted tokens (kept on the layer) and attaches it."""
         n = _sz(0)
         self._check(lib.eigen_attn_tree_bytes(self.handle, int(max_tokens), int(group), ctypes.byref(n)), "eigen_attn_tree_bytes")
-        self.tree_buf = device_alloc(n.value, self.device)
-        self._check(lib.eigen_attn_tree_attach(self.handle, int(max_tokens), int(group), self.tree_buf.data_ptr(), n.value),
+        buf = device_alloc(n.value, self.device)           # (the layer keeps the one it had if the call refuses)
+        self._check(lib.eigen_attn_tree_attach(self.handle, int(max_tokens), int(group), buf.data_ptr(), n.value),
                     "eigen_attn_tree_attach")
-        return self.tree_buf
+        self.tree_buf = buf
+        return buf
 
     def tree_detach(self) -> None:
         self._check(lib.eigen_attn_tree_attach(self.handle, 0, 0, None, 0), "eigen_attn_tree_attach")
@@ -576,10 +577,10 @@ class EigenAttnLayer:
         n = _sz(0)
         self._check(lib.eigen_attn_sparse_bytes(self.handle, int(block_rows), ctypes.byref(n)), "eigen_attn_sparse_bytes")
         with torch.cuda.stream(stream):
-            self.sparse_buf = device_alloc(n.value, self.device)
-        self.sparse_block = int(block_rows)
-        self._check(_call_on(self.device, stream, lib.eigen_attn_sparse_attach, self.handle, int(block_rows),
-                             self.sparse_buf.data_ptr(), n.value), "eigen_attn_sparse_attach")
+            buf = device_alloc(n.value, self.device)       # (the layer keeps the one it had if the call refuses)
+        self._check(_call_on(self.device, stream, lib.eigen_attn_sparse_attach, self.handle, int(block_rows), buf.data_ptr(), n.value),
+                    "eigen_attn_sparse_attach")
+        self.sparse_buf, self.sparse_block = buf, int(block_rows)
         slabs = []
         for h in range(self.H):
             off, blocks = _sz(0), ctypes.c_int32(0)

@@ -1690,6 +1690,8 @@ ea_status eigen_attn_sparse_attach(eigen_attn_t h, int32_t block_rows, void* d_b
   }
   if (bytes < S.bytes) return fail(h, EA_ERR_CAPACITY, "sparse_attach: %zu bytes given, %zu needed", bytes, S.bytes);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const ea_status captured = refuse_capture(h, "sparse_attach", "it waits for the stream", s);
+  if (captured != EA_OK) return captured;
   cudaError_t e = cudaMemcpyAsync(d_buf, S.slab.data(), sizeof(int64_t) * S.slab.size(), cudaMemcpyHostToDevice, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e != cudaSuccess) return cuda_fail(h, e, "sparse_attach");

@@ -41,3 +41,24 @@ def test_bounds_are_not_taken_for_there_during_a_capture(B):
     g.replay()
     torch.cuda.synchronize()
     check(out, want, slack, BF16, "replayed")
+
+
+def test_a_refused_attach_leaves_the_buffer_that_was_there(B, monkeypatch):
+    """sparse_attach waits for the stream, which a capture does not allow: it refuses before it touches the capture, and the
+    layer keeps the buffer that the library still uses."""
+    c = Case(B, BF16, 1, 2, 1, 128, [80, 48], [80, 64], [900], 1024, seed=17)
+    lay = c.lay
+    buf = lay.sparse_attach(32)
+    lay.sparse_sync()
+    q = randn((1, 1, 2, 128), 19, BF16, 2.0)
+    want = lay.decode_sparse(q, 5)
+    spare = torch.empty(2 * buf.numel(), dtype=torch.uint8, device="cuda")
+    monkeypatch.setattr(B, "device_alloc", lambda n, device: spare[:n])    # (the guarded one fills what it hands out)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(B.EigenAttnError) as e:
+            lay.sparse_attach(64)
+        assert e.value.status == B.EA_ERR_UNSUPPORTED
+        q.mul_(1.0)
+    assert lay.sparse_buf is buf and lay.sparse_block == 32 and lay.sparse_lens() == [896]
+    assert torch.equal(lay.decode_sparse(q, 5), want)
