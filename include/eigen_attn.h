@@ -265,8 +265,10 @@ ea_status eigen_attn_quant_layout(eigen_attn_t h, int32_t head, size_t* slab_off
  * positions: drafted token t sits at len_b + (number of other tokens in its mask); only with group 1.  Not with a rotary
  * embedding (EA_ERR_UNSUPPORTED).  flags: EA_Q_PREPROJECTED (d_q: packed [B][T][group * sum rp_k], head h at group *
  * offs_k[h], query head i of its group rp_k[h] further each), EA_KV_PREPROJECTED, EA_OUT_LOWRANK (packed like q with rp_v).
- * The call can be captured into a CUDA graph; replays use the lengths of the capture (the drafted rows are written where
- * they were then: do not replay once rows were added there) and the mask's present contents.
+ * The call can be captured into a CUDA graph; replays use the lengths of the capture, equal or not (the drafted rows are
+ * written where they were then: do not replay once rows were added there), and the mask's present contents.  They use the
+ * page table as it is at replay, which has to map the rows that the capture's lengths name, and the scratch and the cache of
+ * the capture.
  *
  * tree_bytes:   size of the scratch for max_tokens (1..64) drafted tokens and `group` query heads per K/V head.
  * tree_attach:  hands the library that DEVICE buffer (256-byte aligned, owned by the caller); NULL detaches.  Calls of one
@@ -310,7 +312,8 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
  *                dtypes, every rank and d_head, unequal lengths, page table (sequences of at most n_max rows), ALiBi with
  *                group 1; not with a rotary embedding (EA_ERR_UNSUPPORTED).  d_index: DEVICE int32 [B][H][n_blocks] that
  *                receives the blocks attended, ascending, -1 behind the last; or NULL.  flags: EA_Q_PREPROJECTED,
- *                EA_OUT_LOWRANK (packed as in eigen_attn_decode_tree). */
+ *                EA_OUT_LOWRANK (packed as in eigen_attn_decode_tree).  The call can be captured into a CUDA graph; replays
+ *                use the lengths of the capture and the rows, bounds and page table (as in eigen_attn_decode_tree) of now. */
 ea_status eigen_attn_sparse_bytes(eigen_attn_t h, int32_t block_rows, size_t* bytes);
 ea_status eigen_attn_sparse_attach(eigen_attn_t h, int32_t block_rows, void* d_buf, size_t bytes, void* cuda_stream);
 ea_status eigen_attn_sparse_sync(eigen_attn_t h, void* cuda_stream);
@@ -339,7 +342,9 @@ ea_status eigen_attn_set_len(eigen_attn_t h, int32_t len);
  * the T new tokens of sequence b behind that sequence's own rows (token t at position lens[b] + t, attending over
  * the sequence's rows only; the projections then run on the CUDA cores).  The lengths are uploaded on the stream
  * (asynchronous; the array may be reused when the call returns), so the calls that follow must run on that
- * stream or be ordered after it. */
+ * stream or be ordered after it.  Replays of calls that were captured with unequal lengths read the uploaded lengths, with
+ * work cut for those of the capture: replay them with the capture's lengths only (eigen_attn_decode_tree and _decode_sparse
+ * keep their own). */
 ea_status eigen_attn_set_lens(eigen_attn_t h, const int32_t* lens, void* cuda_stream);
 ea_status eigen_attn_get_lens(eigen_attn_t h, int32_t* lens);
 

@@ -234,7 +234,7 @@ bool encode_input_maps(const void* const ptrs[3], int H, int d_head, int T, int 
 struct SparseLayout {
   std::vector<int64_t> slab;   // [H]
   int seq_blocks = 0;          // blocks of one sequence's slab
-  size_t off_q64 = 0, off_qp = 0, off_scores = 0, off_list = 0, off_part = 0, slots = 0, bytes = 0;
+  size_t off_q64 = 0, off_qp = 0, off_scores = 0, off_list = 0, off_part = 0, off_lens = 0, slots = 0, bytes = 0;
 };
 
 }  // namespace
@@ -276,7 +276,7 @@ struct eigen_attn {
   char* tree_buf = nullptr;
   int tree_rows = 0;      // tokens * group it was sized for
   size_t tree_slots = 0;  // partials it holds
-  size_t tree_off_part = 0;
+  size_t tree_off_part = 0, tree_off_lens = 0;
   // block bounds of the cached keys (eigen_attn_sparse_attach)
   char* sp_buf = nullptr;
   int sp_shift = 0;       // log2 of the rows of a block
@@ -342,7 +342,7 @@ constexpr int kMqTcMinRows = 16;         // query rows that the warp-level produ
 constexpr int kMqCtas = 592;             // largest grid of the warp-level kernel in ranges (partials: slots of items + CTAs)
 constexpr int kMqTcCtas = 296;           // largest grid of the tcgen05 tree kernel (its partials are slots of items + CTAs)
 
-size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t* slots) {
+size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t* slots, size_t* off_lens) {
   const size_t units = static_cast<size_t>(h->desc.batch) * h->desc.n_heads;
   const size_t off = align_up(units * rows * h->L.max_rp_k * sizeof(float));
   size_t n = units * rows > kMqSlots ? units * rows : kMqSlots;
@@ -352,7 +352,9 @@ size_t make_tree_layout(const eigen_attn* h, int rows, size_t* off_part, size_t*
   if (ranges > n) n = ranges;
   if (off_part) *off_part = off;
   if (slots) *slots = n;
-  return align_up(off + n * h->L.part_stride * sizeof(float));
+  const size_t lens = align_up(off + n * h->L.part_stride * sizeof(float));
+  if (off_lens) *off_lens = lens;
+  return align_up(lens + h->desc.batch * sizeof(int32_t));
 }
 
 void make_sparse_layout(const eigen_attn* h, int block_rows, SparseLayout* S) {
@@ -371,6 +373,7 @@ void make_sparse_layout(const eigen_attn* h, int block_rows, SparseLayout* S) {
   S->off_list = off;   off = align_up(off + units * S->seq_blocks * sizeof(int32_t));
   S->slots = (units + kMqCtas) * kMaxGroup > kMqSlots ? (units + kMqCtas) * kMaxGroup : kMqSlots;
   S->off_part = off;   off = align_up(off + S->slots * h->L.part_stride * sizeof(float));
+  S->off_lens = off;   off = align_up(off + B * sizeof(int32_t));
   S->bytes = off;
 }
 
@@ -409,13 +412,14 @@ const int32_t* dev_deficit(eigen_attn_t h) {
 int* dev_counters(eigen_attn_t h) { return reinterpret_cast<int*>(h->ws + h->L.off_counters); }
 
 // T rows projected (or copied) behind every sequence's own; the caller has checked the room and advances the length.
+// deficit: the device array of the differences between the lengths (NULL: equal lengths).
 cudaError_t launch_append_rows(eigen_attn_t h, const void* d_k, const void* d_v, int32_t T, int64_t stride_b,
-                               int64_t stride_t, uint32_t flags, cudaStream_t s) {
+                               int64_t stride_t, uint32_t flags, const int32_t* deficit, cudaStream_t s) {
   ea::ProjectParams p{};
   p.heads = dev_heads(h); p.basis = dev_basis(h); p.k = d_k; p.v = d_v; p.cache = h->cache;
   p.stride_b = stride_b; p.stride_t = stride_t;
   p.B = h->desc.batch; p.T = T; p.H = h->desc.n_heads; p.d_head = h->desc.d_head;
-  p.n_max = h->desc.n_max; p.row0 = h->len; p.deficit = dev_deficit(h); p.flags = flags;
+  p.n_max = h->desc.n_max; p.row0 = h->len; p.deficit = deficit; p.flags = flags;
   p.lr_k_width = h->L.sum_rp_k; p.lr_v_width = h->L.sum_rp_v;
   p.pages = dev_pages(h);
   return ea::launch_project_append(p, h->desc.dtype, s, &h->launches);
@@ -430,7 +434,7 @@ ea_status do_append(eigen_attn_t h, const void* d_k, const void* d_v, int32_t T,
   if (!room_for(h, T, &bad))
     return fail(h, EA_ERR_CAPACITY, "append_kv: T %d more rows exceed the capacity of sequence %d (%lld rows)", T, bad,
                 static_cast<long long>(capacity_of(h, bad)));
-  const cudaError_t e = launch_append_rows(h, d_k, d_v, T, stride_b, stride_t, flags, s);
+  const cudaError_t e = launch_append_rows(h, d_k, d_v, T, stride_b, stride_t, flags, dev_deficit(h), s);
   if (e != cudaSuccess) return cuda_fail(h, e, "append_kv launch");
   h->len += T;
   return EA_OK;
@@ -1383,13 +1387,35 @@ ea_status refuse_capture(eigen_attn_t h, const char* who, const char* why, cudaS
   return capture == cudaStreamCaptureStatusNone ? EA_OK : fail(h, EA_ERR_UNSUPPORTED, "%s: %s: not available during stream capture", who, why);
 }
 
+// The device array of the differences between the lengths for a call's kernels (NULL: equal lengths).  A call that is being
+// captured has its grids and tiles made for the lengths of now, and set_lens rewrites the handle's array: the call then gets
+// an array of its own in its scratch, written by a launch that carries the numbers.
+ea_status call_deficit(eigen_attn_t h, const char* who, char* scratch, cudaStream_t s, const int32_t** deficit) {
+  *deficit = dev_deficit(h);
+  if (*deficit == nullptr) return EA_OK;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing(s, &capture);
+  if (e == cudaSuccess && capture != cudaStreamCaptureStatusNone) {
+    int32_t* to = reinterpret_cast<int32_t*>(scratch);
+    for (int b0 = 0; b0 < h->desc.batch && e == cudaSuccess; b0 += ea::kLensPerLaunch) {
+      ea::LensParams p{};
+      p.to = to + b0;
+      p.count = h->desc.batch - b0 < ea::kLensPerLaunch ? h->desc.batch - b0 : ea::kLensPerLaunch;
+      memcpy(p.value, h->deficit.data() + b0, sizeof(int32_t) * p.count);
+      e = ea::launch_write_lens(p, s, &h->launches);
+    }
+    *deficit = to;
+  }
+  return e == cudaSuccess ? EA_OK : cuda_fail(h, e, who);
+}
+
 // The launches behind the query projection: attention over p's rows, then the merge of its pieces with the lift.
 // `slots`: partials the scratch holds.
-// `end`: rows (places of the list) of the longest unit.
+// `end`: rows (places of the list) of the longest unit.  p.deficit is the caller's.
 ea_status launch_mq(eigen_attn_t h, const char* who, ea::MqDecodeParams& p, int64_t end, size_t slots, cudaStream_t s) {
   const Layout& L = h->L;
   p.heads = dev_heads(h); p.basis = dev_basis(h); p.cache = h->cache;
-  p.deficit = dev_deficit(h); p.pages = dev_pages(h);
+  p.pages = dev_pages(h);
   p.B = h->desc.batch; p.H = h->desc.n_heads; p.d_head = h->desc.d_head;
   p.n = h->len; p.n_max = h->desc.n_max;
   p.rows = p.tokens * p.group;
@@ -1522,7 +1548,7 @@ ea_status eigen_attn_tree_bytes(eigen_attn_t h, int32_t max_tokens, int32_t grou
   if (!h || !bytes) return EA_ERR_INVALID_ARG;
   if (max_tokens < 1 || max_tokens > ea::kTreeMaxTokens || group < 1 || group > kMaxGroup)
     return fail(h, EA_ERR_SHAPE, "tree_bytes: %d tokens (1..%d), group %d (1..%d)", max_tokens, ea::kTreeMaxTokens, group, kMaxGroup);
-  *bytes = make_tree_layout(h, max_tokens * group, nullptr, nullptr);
+  *bytes = make_tree_layout(h, max_tokens * group, nullptr, nullptr, nullptr);
   return EA_OK;
 }
 
@@ -1539,7 +1565,7 @@ ea_status eigen_attn_tree_attach(eigen_attn_t h, int32_t max_tokens, int32_t gro
   if (bytes < need) return fail(h, EA_ERR_CAPACITY, "tree_attach: %zu bytes given, %zu needed", bytes, need);
   h->tree_buf = static_cast<char*>(d_buf);
   h->tree_rows = max_tokens * group;
-  make_tree_layout(h, h->tree_rows, &h->tree_off_part, &h->tree_slots);
+  make_tree_layout(h, h->tree_rows, &h->tree_off_part, &h->tree_slots, &h->tree_off_lens);
   return EA_OK;
 }
 
@@ -1565,11 +1591,14 @@ ea_status eigen_attn_decode_tree(eigen_attn_t h, const void* d_q, int64_t stride
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   // the drafted rows, behind every sequence's own (the length stays where it is), and the queries
   float* qp = reinterpret_cast<float*>(h->tree_buf);
+  const int32_t* deficit = nullptr;
+  const ea_status sl = call_deficit(h, "decode_tree lengths", h->tree_buf + h->tree_off_lens, s, &deficit);
+  if (sl != EA_OK) return sl;
   cudaError_t e = cudaSuccess;
-  if (flags & EA_KV_PREPROJECTED) e = launch_append_rows(h, d_k, d_v, T, stride_b_kv, stride_t_kv, EA_KV_PREPROJECTED, s);
+  if (flags & EA_KV_PREPROJECTED) e = launch_append_rows(h, d_k, d_v, T, stride_b_kv, stride_t_kv, EA_KV_PREPROJECTED, deficit, s);
   if (e == cudaSuccess && (flags & (EA_Q_PREPROJECTED | EA_KV_PREPROJECTED)) != (EA_Q_PREPROJECTED | EA_KV_PREPROJECTED)) {
     ea::MqProjectParams pp{};
-    pp.heads = dev_heads(h); pp.basis = dev_basis(h); pp.cache = h->cache; pp.deficit = dev_deficit(h); pp.pages = dev_pages(h);
+    pp.heads = dev_heads(h); pp.basis = dev_basis(h); pp.cache = h->cache; pp.deficit = deficit; pp.pages = dev_pages(h);
     pp.q = d_q; pp.q_stride_b = stride_b_q; pp.q_stride_t = stride_t_q; pp.qp = qp;
     pp.with_q = (flags & EA_Q_PREPROJECTED) ? 0 : 1;
     bool aligned = pp.with_q ? reinterpret_cast<uintptr_t>(d_q) % 16 == 0 && stride_b_q * h->L.es % 16 == 0 && stride_t_q * h->L.es % 16 == 0 : true;
@@ -1593,7 +1622,7 @@ ea_status eigen_attn_decode_tree(eigen_attn_t h, const void* d_q, int64_t stride
   p.qp = qp;
   p.partials = reinterpret_cast<float*>(h->tree_buf + h->tree_off_part);
   p.out = d_out; p.out_stride_b = stride_b_out; p.out_stride_t = stride_t_out;
-  p.mask = d_mask;
+  p.mask = d_mask; p.deficit = deficit;
   p.group = group; p.tokens = T; p.tail = T;
   p.flags = flags & EA_OUT_LOWRANK;
   return launch_mq(h, "decode_tree launch", p, static_cast<int64_t>(h->len) + T, h->tree_slots, s);
@@ -1788,11 +1817,14 @@ ea_status eigen_attn_decode_sparse(eigen_attn_t h, const void* d_q, int64_t stri
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   float* qp = reinterpret_cast<float*>(h->sp_buf + h->sp.off_qp);
   double* q64 = reinterpret_cast<double*>(h->sp_buf + h->sp.off_q64);
+  const int32_t* deficit = nullptr;
+  const ea_status sl = call_deficit(h, "decode_sparse lengths", h->sp_buf + h->sp.off_lens, s, &deficit);
+  if (sl != EA_OK) return sl;
   const ea_status sq = launch_query(h, "decode_sparse query launch", d_q, stride_b_q, 0, group, 1, flags & EA_Q_PREPROJECTED, qp, q64, s);
   if (sq != EA_OK) return sq;
   ea::SparseParams sp;
   fill_sparse_params(h, &sp);
-  sp.q64 = q64; sp.group = group;
+  sp.q64 = q64; sp.group = group; sp.deficit = deficit;
   sp.scores = reinterpret_cast<double*>(h->sp_buf + h->sp.off_scores);
   sp.list = reinterpret_cast<int32_t*>(h->sp_buf + h->sp.off_list);
   sp.index = d_index; sp.index_len = n_blocks;
@@ -1805,7 +1837,7 @@ ea_status eigen_attn_decode_sparse(eigen_attn_t h, const void* d_q, int64_t stri
   ea::MqDecodeParams p{};
   p.qp = qp;
   p.partials = reinterpret_cast<float*>(h->sp_buf + h->sp.off_part);
-  p.out = d_out; p.out_stride_b = stride_b_out;
+  p.out = d_out; p.out_stride_b = stride_b_out; p.deficit = deficit;
   p.list = sp.list; p.list_len = sp.list_len; p.block_shift = h->sp_shift;
   p.group = group; p.tokens = 1; p.tail = 0; p.chained = 1;
   p.flags = flags & EA_OUT_LOWRANK;

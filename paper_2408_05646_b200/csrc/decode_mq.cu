@@ -4,6 +4,7 @@
 //   mq_simt_kernel     attention on the CUDA cores, any dtype (single-precision layers run on it)
 //   mq_combine_*       merge the pieces of a query row and lift o' through (U^V)^T
 //   tree_commit_kernel moves the rows of an accepted path together
+//   write_lens_kernel  the lengths of a captured call
 #include <cuda_bf16.h>
 
 #include "internal.h"
@@ -840,7 +841,17 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const __grid_constant_
   }
 }
 
+__global__ void __launch_bounds__(128) write_lens_kernel(const __grid_constant__ LensParams p) {
+  for (int i = threadIdx.x; i < p.count; i += 128) p.to[i] = p.value[i];
+}
+
 }  // namespace
+
+cudaError_t launch_write_lens(const LensParams& p, cudaStream_t s, uint64_t* launches) {
+  write_lens_kernel<<<1, 128, 0, s>>>(p);
+  ++*launches;
+  return cudaGetLastError();
+}
 
 cudaError_t launch_mq_query(const MqQueryParams& p, int dtype, cudaStream_t s, uint64_t* launches) {
   if (p.flags & 0x1u) {                      // EA_Q_PREPROJECTED

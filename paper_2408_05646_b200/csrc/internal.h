@@ -363,6 +363,13 @@ struct TreeCommitParams {
   uint8_t path[kCommitSeqs][kTreeMaxTokens];
 };
 
+constexpr int kLensPerLaunch = 960;      // lengths that travel in one launch's parameters
+struct LensParams {          // copies the differences between the lengths into a call's scratch (see call_deficit in api.cu)
+  int32_t* to;
+  int32_t count;
+  int32_t value[kLensPerLaunch];
+};
+
 struct SparseParams {
   const HeadInfo* heads;
   const char* cache;
@@ -430,6 +437,7 @@ constexpr int kMqTcRows = 128;       // query rows of an item
 cudaError_t launch_mq_tc(const MqDecodeParams& p, int max_rp_k, int max_rp_v, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_mq_combine(const MqDecodeParams& p, int dtype, int max_rp_v, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_tree_commit(const TreeCommitParams& p, int sequences, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_write_lens(const LensParams& p, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_block_bounds(const SparseParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_block_scores(const SparseParams& p, int dtype, int max_rp_k, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_block_select(const SparseParams& p, cudaStream_t s, uint64_t* launches);
