@@ -1637,9 +1637,10 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
   if (!room_for(h, T, &bad))
     return fail(h, EA_ERR_CAPACITY, "tree_commit: %d drafted rows exceed the capacity of sequence %d", T, bad);
   bool equal = true;
-  std::vector<int32_t> lens;
+  std::vector<int32_t> before, after;           // lengths
   try {
-    lens.resize(B);
+    before.resize(B);
+    after.resize(B);
   } catch (const std::bad_alloc&) {
     return fail(h, EA_ERR_CAPACITY, "tree_commit: out of host memory");
   }
@@ -1651,7 +1652,8 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
       if (at < 0 || at >= T || (i > 0 && at <= h_paths[static_cast<size_t>(b) * T + i - 1]))
         return fail(h, EA_ERR_INVALID_ARG, "tree_commit: paths[%d][%d] = %d (strictly ascending, below %d)", b, i, at, T);
     }
-    lens[b] = h->len - (h->max_deficit > 0 ? h->deficit[b] : 0) + c;
+    before[b] = h->len - (h->max_deficit > 0 ? h->deficit[b] : 0);
+    after[b] = before[b] + c;
     equal = equal && c == h_counts[0];
   }
   if (!equal && B > ea::kMaxRaggedBatch)
@@ -1659,10 +1661,22 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const ea_status captured = refuse_capture(h, "tree_commit", "the lengths live on the host", s);
   if (captured != EA_OK) return captured;
-  cudaError_t e = cudaSuccess;
+  // Counts that differ: the new lengths are uploaded before a row moves, so that a call that fails there has changed nothing.
+  // Equal counts leave the differences between the lengths as they are.
+  auto set_lengths = [&](const std::vector<int32_t>& lens) -> ea_status {
+    try {
+      return eigen_attn_set_lens(h, lens.data(), cuda_stream);
+    } catch (const std::bad_alloc&) {
+      return fail(h, EA_ERR_CAPACITY, "tree_commit: out of host memory");
+    }
+  };
+  if (!equal) {
+    const ea_status st = set_lengths(after);
+    if (st != EA_OK) return st;
+  }
   ea::TreeCommitParams p{};
   p.heads = dev_heads(h); p.cache = h->cache; p.deficit = dev_deficit(h); p.pages = dev_pages(h);
-  p.B = B; p.H = h->desc.n_heads; p.n = h->len; p.n_max = h->desc.n_max; p.es = h->L.es;
+  p.B = B; p.H = h->desc.n_heads; p.n = h->len; p.n_max = h->desc.n_max; p.es = h->L.es; p.grown = equal ? 0 : 1;
   for (int b0 = 0; b0 < B; b0 += ea::kCommitSeqs) {
     const int nb = B - b0 < ea::kCommitSeqs ? B - b0 : ea::kCommitSeqs;
     bool moves = false;
@@ -1676,14 +1690,14 @@ ea_status eigen_attn_tree_commit(eigen_attn_t h, const int32_t* h_paths, const i
       }
     }
     if (!moves) continue;                       // a chain: its rows are where they belong
-    e = ea::launch_tree_commit(p, nb, s, &h->launches);
-    if (e != cudaSuccess) return cuda_fail(h, e, "tree_commit launch");
+    const cudaError_t e = ea::launch_tree_commit(p, nb, s, &h->launches);
+    if (e != cudaSuccess) {
+      if (!equal) set_lengths(before);
+      return cuda_fail(h, e, "tree_commit launch");
+    }
   }
-  if (equal) {                                  // the differences between the lengths stay as they are
-    h->len += h_counts[0];
-    return EA_OK;
-  }
-  return eigen_attn_set_lens(h, lens.data(), cuda_stream);
+  if (equal) h->len += h_counts[0];
+  return EA_OK;
 }
 
 ea_status eigen_attn_sparse_bytes(eigen_attn_t h, int32_t block_rows, size_t* bytes) {

@@ -812,7 +812,7 @@ __global__ void __launch_bounds__(256) tree_commit_kernel(const __grid_constant_
   const int count = p.count[bi];
   if (count == 0) return;
   const HeadInfo hd = p.heads[h];
-  const int n_b = p.deficit != nullptr ? p.n - p.deficit[b] : p.n;
+  const int n_b = (p.deficit != nullptr ? p.n - p.deficit[b] : p.n) - (p.grown ? count : 0);
   const int kc = hd.rp_k * p.es / 16, vc = hd.rp_v * p.es / 16, per = kc + vc;
   constexpr int kBatch = 4;
   for (int i0 = 0; i0 < count * per; i0 += 256 * kBatch) {

@@ -358,6 +358,7 @@ struct TreeCommitParams {
   char* cache;
   const int32_t* deficit;
   int32_t B, H, n, n_max, b0, es;
+  int32_t grown;            // the lengths count the accepted rows already
   PageMap pages;
   uint8_t count[kCommitSeqs];
   uint8_t path[kCommitSeqs][kTreeMaxTokens];
