@@ -267,8 +267,8 @@ ea_status eigen_attn_quant_layout(eigen_attn_t h, int32_t head, size_t* slab_off
  * offs_k[h], query head i of its group rp_k[h] further each), EA_KV_PREPROJECTED, EA_OUT_LOWRANK (packed like q with rp_v).
  * The call can be captured into a CUDA graph; replays use the lengths of the capture, equal or not (the drafted rows are
  * written where they were then: do not replay once rows were added there), and the mask's present contents.  They use the
- * page table as it is at replay, which has to map the rows that the capture's lengths name, and the scratch and the cache of
- * the capture.
+ * scratch of the capture and the page table's entries of now: between replays set_page_table may come with the same
+ * pages_per_seq and page_rows only, and has to map the rows that the capture's lengths name.
  *
  * tree_bytes:   size of the scratch for max_tokens (1..64) drafted tokens and `group` query heads per K/V head.
  * tree_attach:  hands the library that DEVICE buffer (256-byte aligned, owned by the caller); NULL detaches.  Calls of one

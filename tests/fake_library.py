@@ -67,7 +67,7 @@ class FakeLayer:
     def tree_attach(self, tokens, group=1):
         n = ctypes.c_size_t(0)
         self.check(self.lib.eigen_attn_tree_bytes(self.h, tokens, group, ctypes.byref(n)))
-        self.tree, at = aligned(n.value)
+        self.tree_buf, at = aligned(n.value)
         self.check(self.lib.eigen_attn_tree_attach(self.h, tokens, group, at, n.value))
         self.tree_at, self.tree_bytes = at, n.value
 
