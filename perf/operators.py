@@ -342,7 +342,7 @@ def _bounds_of(s):
         x = x.reshape(case["heads"], -1, 2, x.shape[-1])[:, at]
     x = x[:, :, :nb].permute(1, 2, 0, 3, 4)
     if case["ragged"]:
-        x = x * _complete(s)[:, :, None, None, None]
+        x = x.masked_fill(~_complete(s)[:, :, None, None, None], 0)          # (nothing has been written there)
     return {"lo": x[..., 0, :], "hi": x[..., 1, :]}
 
 
