@@ -103,8 +103,9 @@ __device__ __forceinline__ void store_row(const MqProjectParams& p, const Rows& 
 //
 // Many rows: a CTA takes 64 rows of one head and kind against its basis.  A lane has two rows, a warp a quarter of the
 // columns: the columns' numbers are the same for all lanes, so a 16-byte load from shared memory feeds eight multiply-adds of
-// every lane (and still takes two turns: the loads are the bound).  Four rows per lane halve the loads but leave three CTAs
-// per SM instead of five, and a CTA's first loads, past an L2 that the last pass over a long cache has emptied, are a third
+// every lane (and still takes two turns: the loads are the bound).  Five CTAs per SM hold the instance for rank 80 to 96
+// registers, 24 bytes of them spilled for 16-bit layers and 204 for fp32 ones (four CTAs: 136 and 140 at rank 128).  Four
+// rows per lane halve the loads but leave three CTAs per SM, and a CTA's first loads, past an L2 that the last pass over a long cache has emptied, are a third
 // of its time: 504 tokens of 32 heads 37 us against 36.  Tiles of 8 x 4 and 8 x 8 with both operands spread over the lanes
 // were bound by their loads too.
 constexpr int kPrThreads = 128, kPrRows = 64, kPrPad = 64;
@@ -417,6 +418,10 @@ __global__ void __launch_bounds__(kQ64Threads) mq_query64_kernel(const MqQueryPa
 
 // 8 warps, one query row each, over tiles of 32 cached rows staged in shared memory as fp32: lane = cached row for the
 // scores, lane = channel (up to four) for the weighted sum.  Sums and the softmax state are fp32.
+// This is the simple form, right for every layer; it suits few query rows over short contexts (4 heads, 512 rows, 5 tokens:
+// 28 us a call).  Every 8 query rows read all cached rows again, and a multiply-add of a score costs two loads from shared
+// memory: 4 x 8192 rows, 32 heads of rank 80, fp32: 16 tokens 1618 us and 64 tokens 6138 us, where the bytes are 105 us and
+// elementary torch operations take 1324 and 2058; 64 blocks of 64 rows of 4 x 32768: 1007 us, bytes 59.
 constexpr int kSimtRows = 8, kSimtTile = 32;
 template <typename T>
 __global__ void __launch_bounds__(256) mq_simt_kernel(const MqDecodeParams p) {

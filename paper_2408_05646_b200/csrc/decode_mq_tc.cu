@@ -260,10 +260,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
         const int rpk16 = (w.rp_k + 15) & ~15;
         const uint64_t dq = smem_desc(smem_u32(q_tile), 128, (rpk16 >> 3) << 7);    // canonical tiles of 128 rows
         const uint64_t q_part = static_cast<uint64_t>(kTile * rpk16 * 2 >> 4);
-        ok = wait(&hdr->q_full, piece & 1u);
+        ok = wait(&hdr->q_full, piece & 1u);   // (the piece behind is announced after products that this warp issues below)
         for (int i = 0; i < w.nt && ok; ++i, ++g) {
           const int st = g % stages, buf = g % kBufs;
-          ok = wait(&hdr->k_full[st], (g / stages) & 1u);
+          ok = wait(&hdr->k_full[st], (g / stages) & 1u);    // (a stage is refilled after k_empty, which this warp commits below)
           if (ok && g >= kBufs) ok = wait(&hdr->o_done[buf], (g / kBufs - 1) & 1u);       // P(g - 3) has been read
           if (!ok) break;
           tc_fence_after();
@@ -294,10 +294,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
       const int stages = rings.v_stages;
       do {
         const uint32_t idesc = instr_desc((w.rp_v + 15) & ~15, true);
-        if (piece > 0) ok = wait(&hdr->o_free, (piece - 1) & 1u);                         // the piece before has read O'
+        // the piece before has read O' (and the phase behind needs products that this warp issues below)
+        if (piece > 0) ok = wait(&hdr->o_free, (piece - 1) & 1u);
         ++piece;
         for (int i = 0; i < w.nt && ok; ++i, ++g) {
           const int st = g % stages, buf = g % kBufs;
+          // (both are filled again only after the commits below)
           ok = wait(&hdr->v_full[st], (g / stages) & 1u) && wait(&hdr->p_full[buf], (g / kBufs) & 1u);
           if (!ok) break;
           tc_fence_after();
@@ -543,6 +545,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) mq_tc_kernel(const __grid_const
         mbar_arrive(&hdr->sums_ready);
         if (more) mbar_arrive(&hdr->q_full);
       } else {
+        // (The next piece's sums cannot complete before this: either this group hands over some of them itself, or it has
+        // that piece's last tile, whose reference the others wait for before they hand over theirs.)
         ok = wait(&hdr->sums_ready, piece & 1u) && wait(&hdr->o_done[last_buf], last_phase);
         if (!ok) break;
         tc_fence_after();
