@@ -323,6 +323,57 @@ ea_status eigen_attn_decode_sparse(eigen_attn_t h, const void* d_q, int64_t stri
                                    int32_t sink, int32_t recent, void* d_out, int64_t stride_b_out, int32_t* d_index,
                                    uint32_t flags, void* cuda_stream);
 
+/* A learned bias of relative positions (a third kind beside ALiBi and the rotary embedding): the score of the query at
+ * position pos against row j of head i gets table[i][bucket(pos - j)] before the softmax.  Buckets of distances: with half =
+ * n_buckets / 2 (rounded down) and rest = n_buckets - half, distance d < half is bucket d; a larger one is bucket half + k, k
+ * the largest number below rest with (d / half)^rest >= (max_distance / half)^k, decided in whole numbers.  A bucket can be
+ * empty.  2 <= n_buckets <= 256, n_buckets / 2 < max_distance <= 32768.
+ *
+ * bias_bytes:  size of the caller's buffer (host arithmetic).
+ * bias_attach: hands the library that DEVICE buffer (256-byte aligned, owned by the caller); the table is zero until bias_set.
+ *              NULL detaches.  Synchronises `cuda_stream`; not during stream capture (EA_ERR_UNSUPPORTED).  Not together with
+ *              an ALiBi bias or a rotary embedding (EA_ERR_INVALID_ARG, here and in set_alibi and set_rope).
+ * bias_set:    d_table: DEVICE [n_heads][n_buckets] in the layer's dtype, finite numbers; asynchronous (calls on other streams
+ *              are ordered behind it by the caller), can be captured, the table may be changed once the launch has run.
+ * bias_starts: first distance of every bucket: HOST [n_buckets], not descending (an empty bucket starts where the next does).
+ * In effect for eigen_attn_append_kv's counterparts that attend: decode, decode_static, decode_step(_host) and prefill (unequal
+ * lengths, page tables), train_forward and train_backward.  decode_gqa, decode_quant, decode_tree and decode_sparse return
+ * EA_ERR_UNSUPPORTED while a bias is attached. */
+ea_status eigen_attn_bias_bytes(eigen_attn_t h, int32_t n_buckets, int32_t max_distance, size_t* bytes);
+ea_status eigen_attn_bias_attach(eigen_attn_t h, int32_t n_buckets, int32_t max_distance, void* d_buf, size_t bytes,
+                                 void* cuda_stream);
+ea_status eigen_attn_bias_set(eigen_attn_t h, const void* d_table, void* cuda_stream);
+ea_status eigen_attn_bias_starts(eigen_attn_t h, int32_t* starts);
+
+/* Training of a layer whose weights carry the bases (Eq. 8; the paper fine-tunes its models after the compression): causal
+ * attention over rank-space rows that keeps what its gradient needs, and the backward pass, which recomputes the
+ * probabilities.  Neither reads nor writes the cache; a layer that only trains may have n_max = 1.
+ *   S_ij = q'_i k'_j / sqrt(d_head) + bias(i - j)  (j <= i < length),  P = softmax(S),  o'_i = sum_j P_ij v'_j
+ *   delta_i = do'_i o'_i,  dS_ij = P_ij (do'_i v'_j - delta_i),  dq'_i = sum_j dS_ij k'_j / sqrt(d_head),
+ *   dk'_j = sum_i dS_ij q'_i / sqrt(d_head),  dv'_j = sum_i P_ij do'_i,  dtable[h][u] = sum of dS_ij with bucket(i - j) = u
+ * Rows are packed and contiguous in the layer's dtype: d_q, d_dq [B][T][group * sum rp_k] and d_out, d_dout
+ * [B][T][group * sum rp_v] as in eigen_attn_decode_tree, d_k, d_dk [B][T][sum rp_k], d_v, d_dv [B][T][sum rp_v]; what an
+ * input holds in a rank's padding columns is ignored, an output has zeros there.  group query heads (1..16) share a K/V head,
+ * whose gradients are summed over them in a fixed order.  Results do not depend on the order in which blocks run.
+ * d_lens: DEVICE int32 [B] or NULL (all T): sequence b has its first d_lens[b] tokens (taken into 0..T); rows behind are not
+ * read, and their outputs and gradients are zero.  The lengths are read by the launch, so a captured call follows them.
+ * A position bias (ALiBi or learned) is per K/V head: only with group 1 (EA_ERR_UNSUPPORTED).  Not with a rotary embedding.
+ *
+ * train_bytes:    size of the scratch for up to max_tokens (1..2^20) tokens and `group` query heads per K/V head.
+ * train_attach:   hands the library that DEVICE buffer (256-byte aligned, owned by the caller); NULL detaches.  It keeps the
+ *                 rows and statistics of the newest forward pass: a layer whose steps overlap needs one handle for each.
+ * train_forward:  out' and what the backward pass needs.
+ * train_backward: gradients of the newest forward pass; may be called again with another d_dout.  d_dtable: DEVICE
+ *                 [n_heads][n_buckets] in the layer's dtype, or NULL.  EA_ERR_INVALID_ARG without a forward pass, or when the
+ *                 position bias was set, attached or detached since (set a new table after the backward pass).
+ * Both calls can be captured; a replayed pair uses the scratch of the capture and the contents of now. */
+ea_status eigen_attn_train_bytes(eigen_attn_t h, int32_t max_tokens, int32_t group, size_t* bytes);
+ea_status eigen_attn_train_attach(eigen_attn_t h, int32_t max_tokens, int32_t group, void* d_buf, size_t bytes);
+ea_status eigen_attn_train_forward(eigen_attn_t h, const void* d_q, const void* d_k, const void* d_v, int32_t T, int32_t group,
+                                   const int32_t* d_lens, void* d_out, void* cuda_stream);
+ea_status eigen_attn_train_backward(eigen_attn_t h, const void* d_dout, void* d_dq, void* d_dk, void* d_dv, void* d_dtable,
+                                    void* cuda_stream);
+
 /* Current number of cached rows; set_len truncates or rewinds (0 <= len <= n_max), e.g. to re-run
  * a step at a fixed context length.  Rows beyond the previous length hold whatever was last written. */
 ea_status eigen_attn_get_len(eigen_attn_t h, int32_t* len);

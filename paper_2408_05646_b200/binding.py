@@ -95,6 +95,14 @@ SYMBOLS = {
     "eigen_attn_sparse_lens": (_i32, [_vp, ctypes.POINTER(_i32)]),
     "eigen_attn_sparse_layout": (_i32, [_vp, _i32, ctypes.POINTER(_sz), ctypes.POINTER(_i32)]),
     "eigen_attn_decode_sparse": (_i32, [_vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _u32, _vp]),
+    "eigen_attn_bias_bytes": (_i32, [_vp, _i32, _i32, ctypes.POINTER(_sz)]),
+    "eigen_attn_bias_attach": (_i32, [_vp, _i32, _i32, _vp, _sz, _vp]),
+    "eigen_attn_bias_set": (_i32, [_vp, _vp, _vp]),
+    "eigen_attn_bias_starts": (_i32, [_vp, ctypes.POINTER(_i32)]),
+    "eigen_attn_train_bytes": (_i32, [_vp, _i32, _i32, ctypes.POINTER(_sz)]),
+    "eigen_attn_train_attach": (_i32, [_vp, _i32, _i32, _vp, _sz]),
+    "eigen_attn_train_forward": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp]),
+    "eigen_attn_train_backward": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "eigen_attn_launch_count": (_i32, [_vp, ctypes.POINTER(ctypes.c_uint64)]),
     "eigen_attn_set_decode_events": (_i32, [_vp, _vp, _vp]),
     "eigen_attn_version": (_i32, []),
@@ -644,6 +652,87 @@ class EigenAttnLayer:
         self._check(_call_on(self.device, stream, lib.eigen_attn_decode_sparse, self.handle, pq, sbq, group, n_blocks, sink, recent,
                              po, sbo, None if index is None else index.data_ptr(), flags), "eigen_attn_decode_sparse")
         return (out, index) if return_index else out
+
+    # -- a learned bias of relative positions
+    def bias_attach(self, n_buckets: int, max_distance: int, stream=None) -> torch.Tensor:
+        """Allocates the buffer of a learned position bias (kept on the layer) and attaches it; the table is zero until set_bias."""
+        n = _sz(0)
+        self._check(lib.eigen_attn_bias_bytes(self.handle, int(n_buckets), int(max_distance), ctypes.byref(n)), "eigen_attn_bias_bytes")
+        with torch.cuda.stream(stream):
+            buf = device_alloc(n.value, self.device)       # (the layer keeps the one it had if the call refuses)
+        self._check(_call_on(self.device, stream, lib.eigen_attn_bias_attach, self.handle, int(n_buckets), int(max_distance),
+                             buf.data_ptr(), n.value), "eigen_attn_bias_attach")
+        self.bias_buf, self.bias_buckets = buf, int(n_buckets)
+        return buf
+
+    def bias_detach(self, stream=None) -> None:
+        self._check(lib.eigen_attn_bias_attach(self.handle, 0, 0, None, 0, _stream_ptr(stream)), "eigen_attn_bias_attach")
+        self.bias_buf, self.bias_buckets = None, 0
+
+    def set_bias(self, table: torch.Tensor, stream=None) -> None:
+        """eigen_attn_bias_set: table [H][n_buckets] in the layer's dtype, on its device."""
+        assert table.is_cuda and table.is_contiguous() and table.dtype == self.torch_dtype
+        assert table.shape == (self.H, getattr(self, "bias_buckets", 0))
+        self._check(_call_on(self.device, stream, lib.eigen_attn_bias_set, self.handle, table.data_ptr()), "eigen_attn_bias_set")
+
+    def bias_starts(self):
+        """First distance of every bucket."""
+        arr = (ctypes.c_int32 * max(1, getattr(self, "bias_buckets", 0)))()
+        self._check(lib.eigen_attn_bias_starts(self.handle, arr), "eigen_attn_bias_starts")
+        return list(arr)
+
+    # -- training: attention over rank-space rows with its backward pass
+    def train_attach(self, max_tokens: int, group: int = 1) -> torch.Tensor:
+        """Allocates the scratch of the training calls for up to `max_tokens` tokens (kept on the layer) and attaches it."""
+        n = _sz(0)
+        self._check(lib.eigen_attn_train_bytes(self.handle, int(max_tokens), int(group), ctypes.byref(n)), "eigen_attn_train_bytes")
+        buf = device_alloc(n.value, self.device)           # (the layer keeps the one it had if the call refuses)
+        self._check(lib.eigen_attn_train_attach(self.handle, int(max_tokens), int(group), buf.data_ptr(), n.value),
+                    "eigen_attn_train_attach")
+        self.train_buf, self._trained = buf, None
+        return buf
+
+    def train_detach(self) -> None:
+        self._check(lib.eigen_attn_train_attach(self.handle, 0, 0, None, 0), "eigen_attn_train_attach")
+        self.train_buf = self._trained = None
+
+    def train_forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: Optional[torch.Tensor] = None,
+                      group: int = 1, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """eigen_attn_train_forward: q [B][T][group * sum rp_k], k, v [B][T][sum rp_k], [B][T][sum rp_v], lens int32 [B] on the
+        device (None: all T).  The layer keeps what train_backward needs; the tensors may be changed afterwards."""
+        T = q.shape[1]
+        pq = self._packed(q, T, group * self.offs_k[-1])
+        pk, pv = self._packed(k, T, self.offs_k[-1]), self._packed(v, T, self.offs_v[-1])
+        if lens is not None:
+            assert lens.is_cuda and lens.dtype == torch.int32 and lens.is_contiguous() and lens.shape == (self.B,)
+        if out is None:
+            out = self._new_out(self.B, T, group * self.offs_v[-1], stream=stream)
+        po = self._packed(out, T, group * self.offs_v[-1])
+        self._check(_call_on(self.device, stream, lib.eigen_attn_train_forward, self.handle, pq, pk, pv, T, int(group),
+                             None if lens is None else lens.data_ptr(), po), "eigen_attn_train_forward")
+        self._trained = (T, int(group))
+        return out
+
+    def train_backward(self, d_out: torch.Tensor, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                       dv: Optional[torch.Tensor] = None, bias_grad: bool = False, stream=None):
+        """eigen_attn_train_backward: gradients (dq, dk, dv) of the newest train_forward, packed like its inputs; with
+        bias_grad also of the bias table, [H][n_buckets]."""
+        T, group = getattr(self, "_trained", None) or (d_out.shape[1], 1)     # (the call refuses without a forward pass)
+        pg = self._packed(d_out, T, group * self.offs_v[-1])
+        if dq is None:
+            dq = self._new_out(self.B, T, group * self.offs_k[-1], stream=stream)
+        if dk is None:
+            dk = self._new_out(self.B, T, self.offs_k[-1], stream=stream)
+        if dv is None:
+            dv = self._new_out(self.B, T, self.offs_v[-1], stream=stream)
+        table = None
+        if bias_grad:
+            table = self._new_out(self.H, max(1, getattr(self, "bias_buckets", 0)), stream=stream)   # (refused without a bias)
+        self._check(_call_on(self.device, stream, lib.eigen_attn_train_backward, self.handle, pg,
+                             self._packed(dq, T, group * self.offs_k[-1]), self._packed(dk, T, self.offs_k[-1]),
+                             self._packed(dv, T, self.offs_v[-1]), None if table is None else table.data_ptr()),
+                    "eigen_attn_train_backward")
+        return (dq, dk, dv, table) if bias_grad else (dq, dk, dv)
 
     def set_rope(self, base: float, interleaved: bool = False, stream=None) -> None:
         """Rotary position embedding for decode (Section 4.3); base 0 switches it off."""

@@ -237,6 +237,11 @@ struct SparseLayout {
   size_t off_q64 = 0, off_qp = 0, off_scores = 0, off_list = 0, off_part = 0, off_lens = 0, slots = 0, bytes = 0;
 };
 
+// The caller's buffer of eigen_attn_train_attach.
+struct TrainLayout {
+  size_t lens = 0, o = 0, lse = 0, delta = 0, q = 0, k = 0, v = 0, g = 0, q_exp = 0, k_exp = 0, v_exp = 0, g_exp = 0, bias = 0, bytes = 0;
+};
+
 }  // namespace
 
 struct eigen_attn {
@@ -282,6 +287,16 @@ struct eigen_attn {
   int sp_shift = 0;       // log2 of the rows of a block
   SparseLayout sp;
   std::vector<int32_t> sp_len;   // [B]: rows of each sequence whose blocks have bounds (a multiple of the block)
+  // learned bias of relative positions (eigen_attn_bias_attach): first distances of the buckets, bias of every distance
+  char* bias_buf = nullptr;
+  size_t bias_off = 0;
+  std::vector<int32_t> bias_starts;
+  // scratch of the training calls (eigen_attn_train_attach)
+  char* train_buf = nullptr;
+  int train_tokens = 0, train_group = 0;   // it was sized for
+  TrainLayout train;
+  int32_t train_T = 0, train_g = 0;        // the forward pass whose rows and statistics it holds (0 = none)
+  uint64_t position_writes = 0, train_writes = 0;   // changes of the position bias, as of now and of that pass
   char err[256];
 };
 
@@ -409,6 +424,9 @@ bool room_for(const eigen_attn* h, int64_t T, int* bad) {
 const int32_t* dev_deficit(eigen_attn_t h) {
   return h->max_deficit > 0 ? reinterpret_cast<const int32_t*>(h->ws + h->L.off_deficit) : nullptr;
 }
+// Learned bias of every distance (NULL: none attached); the last entry stands for all distances behind it.
+const float* dev_bias(const eigen_attn* h) { return h->bias_buf ? reinterpret_cast<const float*>(h->bias_buf + h->bias_off) : nullptr; }
+int bias_len(const eigen_attn* h) { return h->bias_buf ? h->bias_starts[h->bias_starts.size() - 2] + 1 : 0; }
 int* dev_counters(eigen_attn_t h) { return reinterpret_cast<int*>(h->ws + h->L.off_counters); }
 
 // T rows projected (or copied) behind every sequence's own; the caller has checked the room and advances the length.
@@ -543,6 +561,7 @@ ea_status plan_decode(eigen_attn_t h, const char* who, const void* d_q, int64_t 
   p.flags = flags;
   p.give_up_once = h->opt_give_up ? 1 : 0;
   p.pages = dev_pages(h);
+  p.bias = dev_bias(h); p.bias_len = bias_len(h);
   plan->grid = grid;
   plan->smem = static_cast<size_t>(fixed) + static_cast<size_t>(ring_bytes);
 
@@ -1070,10 +1089,11 @@ ea_status eigen_attn_prefill(eigen_attn_t h, const void* d_q, const void* d_k, c
   p.flags = flags & EA_OUT_LOWRANK; p.status = dev_status(h);
   p.tmaps = h->ws + L.off_tmaps;
   p.pages = dev_pages(h);
+  p.bias = dev_bias(h); p.bias_len = bias_len(h);
   if (h->ev_start) cudaEventRecord(h->ev_start, s);
   size_t ws_smem = 0;
   const int ws_stages = tc_attn && h->tmaps_ok ? ea::prefill_tc_ws_stages(L.max_rp_k, L.max_rp_v, h->desc.d_head, &ws_smem) : 0;
-  if (tc_attn && h->opt_prefill != 1 && h->opt_prefill != 3 && ws_stages >= 3)
+  if (tc_attn && h->opt_prefill != 1 && h->opt_prefill != 3 && ws_stages >= 3 && !p.bias)
     e = ea::launch_prefill_tc_ws(p, ws_stages, ws_smem, h->alibi, s, &h->launches);   // warp-specialised, 256 query rows per CTA
   else if (tc_attn && h->opt_prefill != 1)
     e = ea::launch_prefill_tc(p, L.max_rp_k, L.max_rp_v, s, &h->launches);  // single query tile per CTA (wide ranks)
@@ -1264,6 +1284,9 @@ ea_status eigen_attn_set_alibi(eigen_attn_t h, const float* slopes, void* cuda_s
   if (h->rope && slopes) return fail(h, EA_ERR_INVALID_ARG, "set_alibi: the layer has a rotary embedding");
   const int H = h->desc.n_heads;
   bool any = false;
+  for (int i = 0; i < H && slopes && h->bias_buf; ++i)
+    if (slopes[i] != 0.f) return fail(h, EA_ERR_INVALID_ARG, "set_alibi: the layer has a learned bias (eigen_attn_bias_attach)");
+  ++h->position_writes;
   for (int i = 0; i < H; ++i) {
     const float sl = slopes ? slopes[i] : 0.f;
     if (!(sl >= 0.f) || !isfinite(sl)) return fail(h, EA_ERR_INVALID_ARG, "set_alibi: slope[%d] = %g", i, sl);
@@ -1287,6 +1310,7 @@ ea_status eigen_attn_decode_gqa(eigen_attn_t h, const void* d_q, int64_t stride_
   if (h->desc.dtype != EA_BF16 || h->desc.d_head % 16 || !h->tmaps_ok)
     return fail(h, EA_ERR_UNSUPPORTED, "decode_gqa: needs a bf16 layer with d_head %% 16 == 0");
   if (h->alibi) return fail(h, EA_ERR_UNSUPPORTED, "decode_gqa: not available with an ALiBi bias set");
+  if (h->bias_buf) return fail(h, EA_ERR_UNSUPPORTED, "decode_gqa: not available with a learned bias attached");
   if (h->len - h->max_deficit < 1) return fail(h, EA_ERR_SHAPE, "decode_gqa: the cache is empty (for some sequence)");
   // Section 4.3 for a group.  On the tensor cores where the tiles fit (decode_gqa_rope_kernel: the keys of a tile are
   // lifted and turned once for the whole group); otherwise (wide ranks, a page table) every query head of the group
@@ -1373,6 +1397,7 @@ namespace {
 ea_status check_mq(eigen_attn_t h, const char* who, int32_t group) {
   if (group < 1 || group > kMaxGroup) return fail(h, EA_ERR_SHAPE, "%s: group %d (1..%d)", who, group, kMaxGroup);
   if (h->rope) return fail(h, EA_ERR_UNSUPPORTED, "%s: not available with a rotary embedding", who);
+  if (h->bias_buf) return fail(h, EA_ERR_UNSUPPORTED, "%s: not available with a learned bias attached", who);
   if (h->alibi && group > 1)
     return fail(h, EA_ERR_UNSUPPORTED, "%s: an ALiBi bias is per K/V head: not available with group %d", who, group);
   if (h->len > kMqMaxLen) return fail(h, EA_ERR_UNSUPPORTED, "%s: %d rows (at most %d)", who, h->len, kMqMaxLen);
@@ -1868,6 +1893,7 @@ ea_status eigen_attn_set_rope(eigen_attn_t h, double base, int32_t interleaved, 
   if (h->desc.dtype != EA_BF16 || h->desc.d_head % 16 || !h->tmaps_ok)
     return fail(h, EA_ERR_UNSUPPORTED, "set_rope: needs a bf16 layer with d_head %% 16 == 0 (and the driver's tensor-map encoder)");
   if (h->alibi) return fail(h, EA_ERR_INVALID_ARG, "set_rope: the layer has an ALiBi bias");
+  if (h->bias_buf) return fail(h, EA_ERR_INVALID_ARG, "set_rope: the layer has a learned bias (eigen_attn_bias_attach)");
   const int dh = h->desc.d_head;
   // the constants the kernels read: the inverse frequencies phi_i, e^{-i 128 phi_i} (one tile of cached rows back)
   // and e^{i l phi_i} for the 128 row offsets of a tile, worked out here in double precision
@@ -1894,6 +1920,257 @@ ea_status eigen_attn_set_rope(eigen_attn_t h, double base, int32_t interleaved, 
   if (e != cudaSuccess) return cuda_fail(h, e, "set_rope");
   h->rope = true;
   h->rope_interleaved = interleaved ? 1 : 0;
+  return EA_OK;
+}
+
+// ---- a learned bias of relative positions
+
+namespace {
+constexpr int kMaxBuckets = 256, kMaxDistance = 32768;
+
+// base^exponent as a sum of 32-bit words, times the words given
+void multiply_power(std::vector<uint32_t>* x, uint32_t base, int exponent) {
+  for (int i = 0; i < exponent; ++i) {
+    uint64_t carry = 0;
+    for (uint32_t& w : *x) {
+      carry += static_cast<uint64_t>(w) * base;
+      w = static_cast<uint32_t>(carry);
+      carry >>= 32;
+    }
+    if (carry) x->push_back(static_cast<uint32_t>(carry));
+  }
+}
+// (d / half)^rest >= (far / half)^k, in whole numbers: a bucket's border may fall on a distance exactly
+bool reaches(int d, int half, int far, int rest, int k) {
+  std::vector<uint32_t> a{1}, b{1};
+  multiply_power(&a, d, rest);
+  multiply_power(&a, half, k);
+  multiply_power(&b, far, k);
+  multiply_power(&b, half, rest);
+  if (a.size() != b.size()) return a.size() > b.size();
+  for (size_t i = a.size(); i-- > 0;)
+    if (a[i] != b[i]) return a[i] > b[i];
+  return true;
+}
+// First distance of every bucket, then INT32_MAX: one distance each below half = n_buckets / 2, then a geometric series
+// that would reach max_distance behind the last bucket.
+std::vector<int32_t> bucket_starts(int n_buckets, int max_distance) {
+  const int half = n_buckets / 2, rest = n_buckets - half;
+  std::vector<int32_t> starts;
+  starts.reserve(n_buckets + 1);
+  for (int i = 0; i < half; ++i) starts.push_back(i);
+  for (int k = 0; k < rest; ++k) {
+    int d = static_cast<int>(half * pow(static_cast<double>(max_distance) / half, static_cast<double>(k) / rest));
+    if (d < half) d = half;
+    while (d > half && reaches(d - 1, half, max_distance, rest, k)) --d;
+    while (!reaches(d, half, max_distance, rest, k)) ++d;
+    starts.push_back(d);
+  }
+  starts.push_back(INT32_MAX);
+  return starts;
+}
+ea_status plan_bias(eigen_attn_t h, const char* who, int32_t n_buckets, int32_t max_distance, std::vector<int32_t>* starts,
+                    size_t* off, size_t* bytes) {
+  if (n_buckets < 2 || n_buckets > kMaxBuckets || max_distance <= n_buckets / 2 || max_distance > kMaxDistance)
+    return fail(h, EA_ERR_SHAPE, "%s: %d buckets (2..%d), max_distance %d (more than half of that, at most %d)", who, n_buckets,
+                kMaxBuckets, max_distance, kMaxDistance);
+  try {
+    *starts = bucket_starts(n_buckets, max_distance);
+  } catch (const std::bad_alloc&) {
+    return fail(h, EA_ERR_CAPACITY, "%s: out of host memory", who);
+  }
+  *off = align_up(starts->size() * sizeof(int32_t));
+  *bytes = align_up(*off + static_cast<size_t>(h->desc.n_heads) * ((*starts)[n_buckets - 1] + 1) * sizeof(float));
+  return EA_OK;
+}
+}  // namespace
+
+ea_status eigen_attn_bias_bytes(eigen_attn_t h, int32_t n_buckets, int32_t max_distance, size_t* bytes) {
+  if (!h || !bytes) return EA_ERR_INVALID_ARG;
+  std::vector<int32_t> starts;
+  size_t off = 0;
+  return plan_bias(h, "bias_bytes", n_buckets, max_distance, &starts, &off, bytes);
+}
+
+ea_status eigen_attn_bias_attach(eigen_attn_t h, int32_t n_buckets, int32_t max_distance, void* d_buf, size_t bytes,
+                                 void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!d_buf) {              // detach
+    h->bias_buf = nullptr;
+    ++h->position_writes;
+    return EA_OK;
+  }
+  if (h->rope) return fail(h, EA_ERR_INVALID_ARG, "bias_attach: the layer has a rotary embedding");
+  if (h->alibi) return fail(h, EA_ERR_INVALID_ARG, "bias_attach: the layer has an ALiBi bias");
+  std::vector<int32_t> starts;
+  size_t off = 0, need = 0;
+  const ea_status st = plan_bias(h, "bias_attach", n_buckets, max_distance, &starts, &off, &need);
+  if (st != EA_OK) return st;
+  if (reinterpret_cast<uintptr_t>(d_buf) % kAlign) return fail(h, EA_ERR_INVALID_ARG, "bias_attach: buffer not 256-byte aligned");
+  if (bytes < need) return fail(h, EA_ERR_CAPACITY, "bias_attach: %zu bytes given, %zu needed", bytes, need);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const ea_status captured = refuse_capture(h, "bias_attach", "it waits for the stream", s);
+  if (captured != EA_OK) return captured;
+  cudaError_t e = cudaMemcpyAsync(d_buf, starts.data(), starts.size() * sizeof(int32_t), cudaMemcpyHostToDevice, s);
+  if (e == cudaSuccess) e = cudaMemsetAsync(static_cast<char*>(d_buf) + off, 0, need - off, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e != cudaSuccess) return cuda_fail(h, e, "bias_attach");
+  h->bias_buf = static_cast<char*>(d_buf);
+  h->bias_off = off;
+  h->bias_starts.swap(starts);
+  ++h->position_writes;
+  return EA_OK;
+}
+
+ea_status eigen_attn_bias_starts(eigen_attn_t h, int32_t* starts) {
+  if (!h || !starts) return EA_ERR_INVALID_ARG;
+  if (!h->bias_buf) return fail(h, EA_ERR_INVALID_ARG, "bias_starts: no bias attached");
+  memcpy(starts, h->bias_starts.data(), (h->bias_starts.size() - 1) * sizeof(int32_t));
+  return EA_OK;
+}
+
+ea_status eigen_attn_bias_set(eigen_attn_t h, const void* d_table, void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!h->bias_buf) return fail(h, EA_ERR_INVALID_ARG, "bias_set: no bias attached");
+  if (!d_table) return fail(h, EA_ERR_INVALID_ARG, "bias_set: NULL table");
+  ea::BiasParams p{};
+  p.table = d_table;
+  p.starts = reinterpret_cast<const int32_t*>(h->bias_buf);
+  p.bias = reinterpret_cast<float*>(h->bias_buf + h->bias_off);
+  p.H = h->desc.n_heads; p.buckets = static_cast<int32_t>(h->bias_starts.size()) - 1; p.bias_len = bias_len(h);
+  const cudaError_t e = ea::launch_bias_expand(p, h->desc.dtype, static_cast<cudaStream_t>(cuda_stream), &h->launches);
+  if (e != cudaSuccess) return cuda_fail(h, e, "bias_set launch");
+  ++h->position_writes;
+  return EA_OK;
+}
+
+// ---- training: attention over rank-space rows with its backward pass
+
+namespace {
+constexpr int kTrainMaxTokens = 1 << 20;
+
+void make_train_layout(const eigen_attn* h, int tokens, int group, TrainLayout* t) {
+  const size_t B = h->desc.batch, units = B * h->desc.n_heads, q_units = units * group;
+  const size_t tiles = (static_cast<size_t>(tokens) + ea::kTrainTile - 1) / ea::kTrainTile, pad = tiles * ea::kTrainTile;
+  const size_t rows = B * tokens;
+  size_t off = 0;
+  auto area = [&off](size_t bytes) { const size_t at = off; off = align_up(off + bytes); return at; };
+  t->lens = area(B * sizeof(int32_t));
+  t->o = area(q_units * tokens * h->L.max_rp_v * sizeof(float));
+  t->lse = area(q_units * pad * sizeof(float) * 2);
+  t->delta = area(q_units * pad * sizeof(float));
+  t->q = area(rows * group * h->L.sum_rp_k * sizeof(float));
+  t->k = area(rows * h->L.sum_rp_k * sizeof(float));
+  t->v = area(rows * h->L.sum_rp_v * sizeof(float));
+  t->bias = area(group == 1 ? units * ea::train_simt_tiles(tokens) * kMaxBuckets * sizeof(float) : 0);
+  t->bytes = off;
+}
+
+ea_status check_train(eigen_attn_t h, const char* who, int32_t group) {
+  if (h->rope) return fail(h, EA_ERR_UNSUPPORTED, "%s: not available with a rotary embedding", who);
+  if (group > 1 && (h->alibi || h->bias_buf))
+    return fail(h, EA_ERR_UNSUPPORTED, "%s: a position bias is per K/V head: not available with group %d", who, group);
+  return EA_OK;
+}
+
+void fill_train(eigen_attn_t h, int T, int group, ea::TrainParams* p) {
+  const TrainLayout& t = h->train;
+  char* buf = h->train_buf;
+  *p = ea::TrainParams{};
+  p->heads = dev_heads(h);
+  p->lens = reinterpret_cast<int32_t*>(buf + t.lens);
+  p->o = reinterpret_cast<float*>(buf + t.o);
+  p->lse = reinterpret_cast<float*>(buf + t.lse);
+  p->delta = reinterpret_cast<float*>(buf + t.delta);
+  p->q_copy = reinterpret_cast<float*>(buf + t.q);
+  p->k_copy = reinterpret_cast<float*>(buf + t.k);
+  p->v_copy = reinterpret_cast<float*>(buf + t.v);
+  p->B = h->desc.batch; p->T = T; p->H = h->desc.n_heads; p->group = group;
+  p->tiles = (T + ea::kTrainTile - 1) / ea::kTrainTile;
+  p->pad = p->tiles * ea::kTrainTile;
+  p->o_stride = h->L.max_rp_v;
+  p->lr_k_width = h->L.sum_rp_k; p->lr_v_width = h->L.sum_rp_v;
+  p->max_rp_k = h->L.max_rp_k; p->max_rp_v = h->L.max_rp_v;
+  p->scale = static_cast<float>(1.0 / sqrt(static_cast<double>(h->desc.d_head)));
+  p->scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(h->desc.d_head)));
+  p->alibi = h->alibi ? 1 : 0;
+  if (h->bias_buf) {
+    p->bias = dev_bias(h); p->bias_len = bias_len(h);
+    p->starts = reinterpret_cast<const int32_t*>(h->bias_buf);
+    p->buckets = static_cast<int32_t>(h->bias_starts.size()) - 1;
+    p->bias_part = reinterpret_cast<float*>(buf + t.bias);
+    p->bias_parts = p->B * ea::train_simt_tiles(T);
+  }
+  p->status = dev_status(h);
+}
+}  // namespace
+
+ea_status eigen_attn_train_bytes(eigen_attn_t h, int32_t max_tokens, int32_t group, size_t* bytes) {
+  if (!h || !bytes) return EA_ERR_INVALID_ARG;
+  if (max_tokens < 1 || max_tokens > kTrainMaxTokens || group < 1 || group > kMaxGroup)
+    return fail(h, EA_ERR_SHAPE, "train_bytes: %d tokens (1..%d), group %d (1..%d)", max_tokens, kTrainMaxTokens, group, kMaxGroup);
+  TrainLayout t;
+  make_train_layout(h, max_tokens, group, &t);
+  *bytes = t.bytes;
+  return EA_OK;
+}
+
+ea_status eigen_attn_train_attach(eigen_attn_t h, int32_t max_tokens, int32_t group, void* d_buf, size_t bytes) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!d_buf) {              // detach
+    h->train_buf = nullptr; h->train_T = 0;
+    return EA_OK;
+  }
+  size_t need = 0;
+  const ea_status st = eigen_attn_train_bytes(h, max_tokens, group, &need);
+  if (st != EA_OK) return st;
+  if (reinterpret_cast<uintptr_t>(d_buf) % kAlign) return fail(h, EA_ERR_INVALID_ARG, "train_attach: buffer not 256-byte aligned");
+  if (bytes < need) return fail(h, EA_ERR_CAPACITY, "train_attach: %zu bytes given, %zu needed", bytes, need);
+  h->train_buf = static_cast<char*>(d_buf);
+  h->train_tokens = max_tokens; h->train_group = group; h->train_T = 0;
+  make_train_layout(h, max_tokens, group, &h->train);
+  return EA_OK;
+}
+
+ea_status eigen_attn_train_forward(eigen_attn_t h, const void* d_q, const void* d_k, const void* d_v, int32_t T, int32_t group,
+                                   const int32_t* d_lens, void* d_out, void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!h->train_buf) return fail(h, EA_ERR_INVALID_ARG, "train_forward: no scratch attached");
+  if (!d_q || !d_k || !d_v || !d_out) return fail(h, EA_ERR_INVALID_ARG, "train_forward: NULL q, k, v or out");
+  if (T < 1 || group < 1) return fail(h, EA_ERR_SHAPE, "train_forward: T = %d, group %d", T, group);
+  if (T > h->train_tokens || group > h->train_group)
+    return fail(h, EA_ERR_CAPACITY, "train_forward: %d tokens, group %d exceed the attached scratch (%d, %d)", T, group,
+                h->train_tokens, h->train_group);
+  const ea_status st = check_train(h, "train_forward", group);
+  if (st != EA_OK) return st;
+  ea::TrainParams p;
+  fill_train(h, T, group, &p);
+  p.q = d_q; p.k = d_k; p.v = d_v; p.out = d_out; p.lens_in = d_lens;
+  h->train_T = 0;
+  const cudaError_t e = ea::launch_train_simt_forward(p, h->desc.dtype, static_cast<cudaStream_t>(cuda_stream), &h->launches);
+  if (e != cudaSuccess) return cuda_fail(h, e, "train_forward launch");
+  h->train_T = T;
+  h->train_g = group;
+  h->train_writes = h->position_writes;
+  return EA_OK;
+}
+
+ea_status eigen_attn_train_backward(eigen_attn_t h, const void* d_dout, void* d_dq, void* d_dk, void* d_dv, void* d_dtable,
+                                    void* cuda_stream) {
+  if (!h) return EA_ERR_INVALID_ARG;
+  if (!h->train_buf || h->train_T == 0) return fail(h, EA_ERR_INVALID_ARG, "train_backward: no forward pass to go back through");
+  if (!d_dout || !d_dq || !d_dk || !d_dv) return fail(h, EA_ERR_INVALID_ARG, "train_backward: NULL gradient");
+  if (h->rope) return fail(h, EA_ERR_UNSUPPORTED, "train_backward: not available with a rotary embedding");
+  if (h->train_writes != h->position_writes)
+    return fail(h, EA_ERR_INVALID_ARG, "train_backward: the position bias was changed after the forward pass");
+  if (d_dtable && !h->bias_buf) return fail(h, EA_ERR_INVALID_ARG, "train_backward: gradient of a bias table, but no bias attached");
+  ea::TrainParams p;
+  fill_train(h, h->train_T, h->train_g, &p);
+  p.d_out = d_dout; p.dq = d_dq; p.dk = d_dk; p.dv = d_dv; p.dtable = d_dtable;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e = ea::launch_train_simt_backward(p, h->desc.dtype, s, &h->launches);
+  if (e == cudaSuccess && d_dtable) e = ea::launch_bias_reduce(p, h->desc.dtype, s, &h->launches);
+  if (e != cudaSuccess) return cuda_fail(h, e, "train_backward launch");
   return EA_OK;
 }
 
@@ -2040,6 +2317,7 @@ ea_status eigen_attn_decode_quant(eigen_attn_t h, const void* d_q, int64_t strid
   if (!d_q || !d_out) return fail(h, EA_ERR_INVALID_ARG, "decode_quant: NULL q or out");
   if (flags & ~(EA_Q_PREPROJECTED | EA_OUT_LOWRANK)) return fail(h, EA_ERR_INVALID_ARG, "decode_quant: unknown flag 0x%x", flags);
   if (h->rope) return fail(h, EA_ERR_UNSUPPORTED, "decode_quant: not available with a rotary embedding");
+  if (h->bias_buf) return fail(h, EA_ERR_UNSUPPORTED, "decode_quant: not available with a learned bias attached");
   if (h->len - h->max_deficit < 1) return fail(h, EA_ERR_SHAPE, "decode_quant: the cache is empty (for some sequence)");
   const Layout& L = h->L;
   ea::QuantParams p;

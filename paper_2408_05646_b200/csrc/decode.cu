@@ -261,8 +261,9 @@ __device__ __forceinline__ Piece locate(const DecodeParams& p, const int* pre, l
 
 // ---------------------------------------------------------------- one (CTA, unit) piece
 
-template <typename T, int NCH>
-__device__ __forceinline__ void run_segment(const DecodeParams& p, DecodeSmemFixed* fx,
+// BIAS: a learned bias of relative positions; `bias` is the head's, one number per distance.
+template <typename T, int NCH, bool BIAS>
+__device__ __forceinline__ void run_segment(const DecodeParams& p, DecodeSmemFixed* fx, const float* bias,
                                             unsigned char* ring, const HeadInfo& hd, int i0, int i1,
                                             Ring& ring_state, int warp, int lane, bool with_new_row, int n_b, int buf) {
   constexpr int EPC = Elem<T>::kPerChunk;
@@ -304,6 +305,8 @@ __device__ __forceinline__ void run_segment(const DecodeParams& p, DecodeSmemFix
   const float slope2 = hd.alibi_slope2;
   const int pos_q = n_b - 1 + (p.k_new != nullptr ? 1 : 0);
   auto process_row = [&](const unsigned char* kr, const unsigned char* vr, bool valid, int j_abs) {
+    float far = 0.f;
+    if (BIAS) far = __ldg(bias + min(pos_q - j_abs, p.bias_len - 1));
     float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
@@ -317,7 +320,8 @@ __device__ __forceinline__ void run_segment(const DecodeParams& p, DecodeSmemFix
     }
     float s = (a0 + a1) + (a2 + a3);
     s += __shfl_xor_sync(0xffffffffu, s, 1);
-    s = fmaf(slope2, static_cast<float>(j_abs - pos_q), s);
+    if (BIAS) s += far;
+    else s = fmaf(slope2, static_cast<float>(j_abs - pos_q), s);
     if (valid) {
       if (s > m) {                      // rare after the first rows: rescale the running state
         const float c = fast_exp2(m - s);
@@ -578,7 +582,7 @@ __device__ __forceinline__ void finish_piece(const DecodeParams& p, DecodeSmemFi
   consumer_sync();                    // o_acc, q' and the staging area are reused by the next piece
 }
 
-template <typename T>
+template <typename T, bool BIAS>
 __global__ void __launch_bounds__(kDecodeThreads, 1) decode_splitkv_kernel(const DecodeParams p) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   DecodeSmemFixed* fx = reinterpret_cast<DecodeSmemFixed*>(smem_raw);
@@ -759,15 +763,16 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) decode_splitkv_kernel(const
       const int mx = max(hd.rp_k, hd.rp_v);
       const int cls = (mx + 15) >> 4;               // a lane pair covers 16 columns per step
       constexpr int MUL = 8 / Elem<T>::kPerChunk;   // 16-byte chunks per 8 columns: 1 (bf16) or 2 (fp32)
+      const float* bias = BIAS ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
       switch (cls) {
-        case 1: run_segment<T, 1 * MUL>(p, fx, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
-        case 2: run_segment<T, 2 * MUL>(p, fx, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
-        case 3: run_segment<T, 3 * MUL>(p, fx, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
-        case 4: run_segment<T, 4 * MUL>(p, fx, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
-        case 5: run_segment<T, 5 * MUL>(p, fx, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
-        case 6: run_segment<T, 6 * MUL>(p, fx, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
-        case 7: run_segment<T, 7 * MUL>(p, fx, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
-        default: run_segment<T, 8 * MUL>(p, fx, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
+        case 1: run_segment<T, 1 * MUL, BIAS>(p, fx, bias, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
+        case 2: run_segment<T, 2 * MUL, BIAS>(p, fx, bias, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
+        case 3: run_segment<T, 3 * MUL, BIAS>(p, fx, bias, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
+        case 4: run_segment<T, 4 * MUL, BIAS>(p, fx, bias, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
+        case 5: run_segment<T, 5 * MUL, BIAS>(p, fx, bias, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
+        case 6: run_segment<T, 6 * MUL, BIAS>(p, fx, bias, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
+        case 7: run_segment<T, 7 * MUL, BIAS>(p, fx, bias, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
+        default: run_segment<T, 8 * MUL, BIAS>(p, fx, bias, ring, hd, i0, i1, rg, warp, lane, with_new_row, n_b, bufk); break;
       }
       mbar_arrive(&fx->proj_empty[bufk]);           // q' is in registers, the new row has been attended
       finish_piece<T>(p, fx, hd, pc, cta, grid, whole, tid);
@@ -856,19 +861,22 @@ size_t decode_fixed_smem_bytes() { return sizeof(DecodeSmemFixed); }
 
 cudaError_t decode_configure(int dtype) {
   const int max_smem = 227 * 1024;
-  if (dtype == 0)
-    return cudaFuncSetAttribute(decode_splitkv_kernel<__nv_bfloat16>,
-                                cudaFuncAttributeMaxDynamicSharedMemorySize, max_smem);
-  return cudaFuncSetAttribute(decode_splitkv_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              max_smem);
+  auto allow = [&](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, max_smem); };
+  const cudaError_t e = dtype == 0 ? allow(decode_splitkv_kernel<__nv_bfloat16, false>) : allow(decode_splitkv_kernel<float, false>);
+  if (e != cudaSuccess) return e;
+  return dtype == 0 ? allow(decode_splitkv_kernel<__nv_bfloat16, true>) : allow(decode_splitkv_kernel<float, true>);
 }
 
 cudaError_t launch_decode(const DecodeParams& p, int dtype, int grid, size_t smem_bytes, cudaStream_t s,
                           uint64_t* launches) {
-  if (dtype == 0)
-    decode_splitkv_kernel<__nv_bfloat16><<<grid, kDecodeThreads, smem_bytes, s>>>(p);
-  else
-    decode_splitkv_kernel<float><<<grid, kDecodeThreads, smem_bytes, s>>>(p);
+  auto run = [&](auto kernel) { kernel<<<grid, kDecodeThreads, smem_bytes, s>>>(p); };
+  if (dtype == 0) {
+    if (p.bias != nullptr) run(decode_splitkv_kernel<__nv_bfloat16, true>);
+    else run(decode_splitkv_kernel<__nv_bfloat16, false>);
+  } else {
+    if (p.bias != nullptr) run(decode_splitkv_kernel<float, true>);
+    else run(decode_splitkv_kernel<float, false>);
+  }
   ++*launches;
   return cudaGetLastError();
 }

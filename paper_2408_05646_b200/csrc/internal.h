@@ -84,6 +84,8 @@ struct DecodeParams {
   uint32_t flags;
   int32_t give_up_once;     // test hook: warp 0 of CTA 0 reports its first wait for a tile as run out
   PageMap pages;            // paged cache (tile_rows divides the page size, one tile per ring slot)
+  const float* bias;        // [H][bias_len]: learned bias of a distance times log2(e), the last entry for all behind; or NULL
+  int32_t bias_len;
 };
 
 struct CombineParams {
@@ -171,6 +173,8 @@ struct PrefillParams {
   const double* inv_freq;   // [d_head/2]: base^(-2i/d_head)
   int32_t rope_interleaved; // pairs (2i, 2i+1) instead of (i, i + d_head/2)
   const float4* el_table;   // [32][128]: cos, cos, sin, sin of l phi for pairs 2k, 2k + 1 and row offset l
+  const float* bias;        // learned bias of relative positions, as in DecodeParams
+  int32_t bias_len;
   void* krot;               // lifted, rotated keys [H][B][krot_rows][d_head] (16-bit), written by the preparing kernels
   int32_t krot_rows;
 };
@@ -491,6 +495,53 @@ size_t decode_quant_mma_smem_bytes(int max_stage_bytes, int max_rp, int group);
 cudaError_t launch_decode_quant_mma(const QuantParams& p, int max_rp, int min_rp, size_t smem, cudaStream_t s,
                                     uint64_t* launches);   // min_rp: narrowest padded rank over heads and K/V
 cudaError_t launch_quant_combine(const QuantParams& p, cudaStream_t s, uint64_t* launches);
+
+// Attention over rank-space rows with its backward pass (eigen_attn_train_*).  Query unit u = (h group + i) B + b: query head
+// i of K/V head h, sequence b; key unit h B + b.  Rows of T tokens are kept in `pad` = T rounded up to whole tiles of 128.
+constexpr int kTrainTile = 128;
+struct TrainParams {
+  const HeadInfo* heads;
+  const void *q, *k, *v;    // packed [B][T][group * sum rp_k], [B][T][sum rp_k], [B][T][sum rp_v]: the caller's
+  const void* d_out;        // packed [B][T][group * sum rp_v]
+  void *out, *dq, *dk, *dv; // packed like d_out, q, k, v
+  const int32_t* lens_in;   // [B] tokens of every sequence (the caller's), or NULL
+  int32_t* lens;            // [B] the same within [0, T], kept for the backward pass
+  float* o;                 // [query unit][T][rp_v of the widest head]: o' as computed
+  float* lse;               // [query unit][pad]: -log2 of the sum of 2^score, -inf where a row has none (tensor-core kernels);
+                            //   fp32 layers: maximum of the scores, and behind all of them the reciprocal of the sum
+  float* delta;             // [query unit][pad]: gradient of o' times o'
+  float *q_copy, *k_copy, *v_copy;   // fp32 layers: the rows of the call, packed like the caller's
+  // 16-bit layers: tiles of 128 rows in the order of the products' operands, fp16 numbers times a power of two per tile
+  char *q_tiles, *k_tiles, *v_tiles, *g_tiles;     // [unit][tiles][tile bytes]
+  int32_t *q_exp, *k_exp, *v_exp, *g_exp;          // [unit][tiles]: exponent of that power
+  int32_t tile_k, tile_v;   // bytes of a tile: 256 times the widest rank, padded to 16
+  int32_t o_stride;         // rp_v of the widest head
+  int32_t B, T, H, group, pad, tiles;
+  int32_t lr_k_width, lr_v_width;
+  float scale;              // 1/sqrt(d_head)
+  float scale_log2;
+  int32_t max_rp_k, max_rp_v;
+  const float* bias;        // [H][bias_len]: bias of a distance times log2(e), the last entry for all behind; or NULL
+  const int32_t* starts;    // [buckets + 1]: first distance of every bucket, then INT32_MAX
+  int32_t bias_len, buckets;
+  float* bias_part;         // [H][parts][buckets]: sums of dS of a part of the scores
+  int32_t bias_parts;
+  void* dtable;             // [H][buckets] gradient of the table, or NULL
+  int32_t alibi;
+  int* status;
+};
+cudaError_t launch_train_simt_forward(const TrainParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_train_simt_backward(const TrainParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+int train_simt_tiles(int T);              // query tiles of the fp32 kernels: parts of a unit's bias gradient
+cudaError_t launch_bias_reduce(const TrainParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+// table [H][buckets] in the layer's dtype -> bias of every distance [H][bias_len], times log2(e)
+struct BiasParams {
+  const void* table;
+  const int32_t* starts;
+  float* bias;
+  int32_t H, buckets, bias_len;
+};
+cudaError_t launch_bias_expand(const BiasParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 
 // Built-in scratch for eigen_attn_decode_static: device address and capacity (in floats) of the
 // library's own partials array on the current device (queried from the runtime on every call).

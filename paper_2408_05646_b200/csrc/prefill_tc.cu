@@ -70,6 +70,10 @@ __global__ void __launch_bounds__(kThreads) prefill_tc_kernel(const PrefillParam
 
   const int my_pos = len0 + t0 + tid;                      // last key this thread's query sees
   const float slope2 = hd.alibi_slope2;                      // ALiBi: slope * (key - query position), log2 domain
+  const float* bias = p.bias != nullptr ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;   // or a learned bias
+  auto position = [&](int key) {
+    return bias != nullptr ? __ldg(bias + min(max(my_pos - key, 0), p.bias_len - 1)) : slope2 * static_cast<float>(key - my_pos);
+  };
   const int n_keys = len0 + min(p.T, t0 + kTile);          // keys the block needs
   const int n_tiles = (n_keys + kTile - 1) / kTile;
   const uint32_t idesc_s = instr_desc(kTile, false);
@@ -107,7 +111,7 @@ __global__ void __launch_bounds__(kThreads) prefill_tc_kernel(const PrefillParam
       tmem_wait_ld();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float s = fmaf(__uint_as_float(r[i]), p.scale_log2, slope2 * static_cast<float>(key0 + c0 + i - my_pos));
+        float s = fmaf(__uint_as_float(r[i]), p.scale_log2, position(key0 + c0 + i));
         if (diag && key0 + c0 + i > my_pos) s = -INFINITY;
         row_max = fmaxf(row_max, s);
       }
@@ -123,7 +127,7 @@ __global__ void __launch_bounds__(kThreads) prefill_tc_kernel(const PrefillParam
       float pr[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float s = fmaf(__uint_as_float(r[i]), p.scale_log2, slope2 * static_cast<float>(key0 + c0 + i - my_pos)) - m_new;
+        float s = fmaf(__uint_as_float(r[i]), p.scale_log2, position(key0 + c0 + i)) - m_new;
         if (diag && key0 + c0 + i > my_pos) s = -INFINITY;
         pr[i] = ex2(s);
         row_sum += pr[i];
