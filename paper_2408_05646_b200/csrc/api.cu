@@ -2049,20 +2049,38 @@ ea_status eigen_attn_bias_set(eigen_attn_t h, const void* d_table, void* cuda_st
 namespace {
 constexpr int kTrainMaxTokens = 1 << 20;
 
+size_t train_tile_bytes(int rp) { return static_cast<size_t>(ea::kTrainTile) * ((rp + 15) & ~15) * 2; }
+// parts of a sequence's scores that leave a sum per bucket of their own
+int train_bias_parts(const eigen_attn* h, int T) {
+  return h->desc.dtype == EA_FP32 ? ea::train_simt_tiles(T) : (T + ea::kTrainTile - 1) / ea::kTrainTile;
+}
 void make_train_layout(const eigen_attn* h, int tokens, int group, TrainLayout* t) {
   const size_t B = h->desc.batch, units = B * h->desc.n_heads, q_units = units * group;
   const size_t tiles = (static_cast<size_t>(tokens) + ea::kTrainTile - 1) / ea::kTrainTile, pad = tiles * ea::kTrainTile;
   const size_t rows = B * tokens;
+  *t = TrainLayout{};
   size_t off = 0;
   auto area = [&off](size_t bytes) { const size_t at = off; off = align_up(off + bytes); return at; };
   t->lens = area(B * sizeof(int32_t));
   t->o = area(q_units * tokens * h->L.max_rp_v * sizeof(float));
-  t->lse = area(q_units * pad * sizeof(float) * 2);
+  t->lse = area(q_units * pad * sizeof(float) * (h->desc.dtype == EA_FP32 ? 2 : 1));
   t->delta = area(q_units * pad * sizeof(float));
-  t->q = area(rows * group * h->L.sum_rp_k * sizeof(float));
-  t->k = area(rows * h->L.sum_rp_k * sizeof(float));
-  t->v = area(rows * h->L.sum_rp_v * sizeof(float));
-  t->bias = area(group == 1 ? units * ea::train_simt_tiles(tokens) * kMaxBuckets * sizeof(float) : 0);
+  if (h->desc.dtype == EA_BF16) {
+    const size_t tile_k = train_tile_bytes(h->L.max_rp_k), tile_v = train_tile_bytes(h->L.max_rp_v);
+    t->q = area(q_units * tiles * tile_k);
+    t->k = area(units * tiles * tile_k);
+    t->v = area(units * tiles * tile_v);
+    t->g = area(q_units * tiles * tile_v);
+    t->q_exp = area(q_units * tiles * sizeof(int32_t));
+    t->k_exp = area(units * tiles * sizeof(int32_t));
+    t->v_exp = area(units * tiles * sizeof(int32_t));
+    t->g_exp = area(q_units * tiles * sizeof(int32_t));
+  } else {
+    t->q = area(rows * group * h->L.sum_rp_k * sizeof(float));
+    t->k = area(rows * h->L.sum_rp_k * sizeof(float));
+    t->v = area(rows * h->L.sum_rp_v * sizeof(float));
+  }
+  t->bias = area(group == 1 ? units * train_bias_parts(h, tokens) * kMaxBuckets * sizeof(float) : 0);
   t->bytes = off;
 }
 
@@ -2082,9 +2100,19 @@ void fill_train(eigen_attn_t h, int T, int group, ea::TrainParams* p) {
   p->o = reinterpret_cast<float*>(buf + t.o);
   p->lse = reinterpret_cast<float*>(buf + t.lse);
   p->delta = reinterpret_cast<float*>(buf + t.delta);
-  p->q_copy = reinterpret_cast<float*>(buf + t.q);
-  p->k_copy = reinterpret_cast<float*>(buf + t.k);
-  p->v_copy = reinterpret_cast<float*>(buf + t.v);
+  if (h->desc.dtype == EA_FP32) {
+    p->q_copy = reinterpret_cast<float*>(buf + t.q);
+    p->k_copy = reinterpret_cast<float*>(buf + t.k);
+    p->v_copy = reinterpret_cast<float*>(buf + t.v);
+  } else {
+    p->q_tiles = buf + t.q; p->k_tiles = buf + t.k; p->v_tiles = buf + t.v; p->g_tiles = buf + t.g;
+    p->q_exp = reinterpret_cast<int32_t*>(buf + t.q_exp);
+    p->k_exp = reinterpret_cast<int32_t*>(buf + t.k_exp);
+    p->v_exp = reinterpret_cast<int32_t*>(buf + t.v_exp);
+    p->g_exp = reinterpret_cast<int32_t*>(buf + t.g_exp);
+    p->tile_k = static_cast<int32_t>(train_tile_bytes(h->L.max_rp_k));
+    p->tile_v = static_cast<int32_t>(train_tile_bytes(h->L.max_rp_v));
+  }
   p->B = h->desc.batch; p->T = T; p->H = h->desc.n_heads; p->group = group;
   p->tiles = (T + ea::kTrainTile - 1) / ea::kTrainTile;
   p->pad = p->tiles * ea::kTrainTile;
@@ -2099,7 +2127,7 @@ void fill_train(eigen_attn_t h, int T, int group, ea::TrainParams* p) {
     p->starts = reinterpret_cast<const int32_t*>(h->bias_buf);
     p->buckets = static_cast<int32_t>(h->bias_starts.size()) - 1;
     p->bias_part = reinterpret_cast<float*>(buf + t.bias);
-    p->bias_parts = p->B * ea::train_simt_tiles(T);
+    p->bias_parts = p->B * train_bias_parts(h, T);
   }
   p->status = dev_status(h);
 }
@@ -2147,7 +2175,14 @@ ea_status eigen_attn_train_forward(eigen_attn_t h, const void* d_q, const void* 
   fill_train(h, T, group, &p);
   p.q = d_q; p.k = d_k; p.v = d_v; p.out = d_out; p.lens_in = d_lens;
   h->train_T = 0;
-  const cudaError_t e = ea::launch_train_simt_forward(p, h->desc.dtype, static_cast<cudaStream_t>(cuda_stream), &h->launches);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e;
+  if (h->desc.dtype == EA_FP32) {
+    e = ea::launch_train_simt_forward(p, s, &h->launches);
+  } else {
+    e = ea::launch_train_pack(p, false, s, &h->launches);
+    if (e == cudaSuccess) e = ea::launch_train_tc_forward(p, s, &h->launches);
+  }
   if (e != cudaSuccess) return cuda_fail(h, e, "train_forward launch");
   h->train_T = T;
   h->train_g = group;
@@ -2168,7 +2203,13 @@ ea_status eigen_attn_train_backward(eigen_attn_t h, const void* d_dout, void* d_
   fill_train(h, h->train_T, h->train_g, &p);
   p.d_out = d_dout; p.dq = d_dq; p.dk = d_dk; p.dv = d_dv; p.dtable = d_dtable;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  cudaError_t e = ea::launch_train_simt_backward(p, h->desc.dtype, s, &h->launches);
+  cudaError_t e;
+  if (h->desc.dtype == EA_FP32) {
+    e = ea::launch_train_simt_backward(p, s, &h->launches);
+  } else {
+    e = ea::launch_train_pack(p, true, s, &h->launches);
+    if (e == cudaSuccess) e = ea::launch_train_tc_backward(p, s, &h->launches);
+  }
   if (e == cudaSuccess && d_dtable) e = ea::launch_bias_reduce(p, h->desc.dtype, s, &h->launches);
   if (e != cudaSuccess) return cuda_fail(h, e, "train_backward launch");
   return EA_OK;

@@ -499,6 +499,7 @@ cudaError_t launch_quant_combine(const QuantParams& p, cudaStream_t s, uint64_t*
 // Attention over rank-space rows with its backward pass (eigen_attn_train_*).  Query unit u = (h group + i) B + b: query head
 // i of K/V head h, sequence b; key unit h B + b.  Rows of T tokens are kept in `pad` = T rounded up to whole tiles of 128.
 constexpr int kTrainTile = 128;
+constexpr int kTrainNoNumber = 120;       // exponent of a tile without a number other than zero (above every other)
 struct TrainParams {
   const HeadInfo* heads;
   const void *q, *k, *v;    // packed [B][T][group * sum rp_k], [B][T][sum rp_k], [B][T][sum rp_v]: the caller's
@@ -530,8 +531,11 @@ struct TrainParams {
   int32_t alibi;
   int* status;
 };
-cudaError_t launch_train_simt_forward(const TrainParams& p, int dtype, cudaStream_t s, uint64_t* launches);
-cudaError_t launch_train_simt_backward(const TrainParams& p, int dtype, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_train_simt_forward(const TrainParams& p, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_train_simt_backward(const TrainParams& p, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_train_pack(const TrainParams& p, bool gradient, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_train_tc_forward(const TrainParams& p, cudaStream_t s, uint64_t* launches);
+cudaError_t launch_train_tc_backward(const TrainParams& p, cudaStream_t s, uint64_t* launches);
 int train_simt_tiles(int T);              // query tiles of the fp32 kernels: parts of a unit's bias gradient
 cudaError_t launch_bias_reduce(const TrainParams& p, int dtype, cudaStream_t s, uint64_t* launches);
 // table [H][buckets] in the layer's dtype -> bias of every distance [H][bias_len], times log2(e)

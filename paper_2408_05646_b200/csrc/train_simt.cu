@@ -1,4 +1,4 @@
-// Causal attention over rank-space rows and its backward pass on the CUDA cores.
+// Causal attention over rank-space rows and its backward pass on the CUDA cores, for fp32 layers.
 //   S_ij = scale q'_i k'_j + b(i - j)  (j <= i < length),  P = softmax(S),  o'_i = sum_j P_ij v'_j
 //   delta_i = do'_i o'_i,  dS_ij = P_ij (do'_i v'_j - delta_i),
 //   dq'_i = scale sum_j dS_ij k'_j,  dk'_j = scale sum_i dS_ij q'_i,  dv'_j = sum_i P_ij do'_i,  db_u = sum dS_ij over the
@@ -8,8 +8,6 @@
 // of 64; a thread has 4 x 4 scores and 4 rows x 8 columns of the sums.  dq' and dk', dv' are two kernels, so that nothing is
 // added up by atomics.  A tile's products are summed apart and then added, which keeps the rounding errors of long sums down.
 // Bound by the loads from shared memory (two for eight multiply-adds in the score products): figures in the table of cases.
-#include <cuda_bf16.h>
-
 #include "internal.h"
 
 namespace ea {
@@ -19,13 +17,6 @@ constexpr int kRows = 64;
 constexpr int kThreads = 256;
 constexpr int kPitchP = kRows + 4;
 
-template <typename T> __device__ __forceinline__ float to_f(T v);
-template <> __device__ __forceinline__ float to_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <typename T> __device__ __forceinline__ T from_f(float v);
-template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -34,14 +25,13 @@ __device__ __forceinline__ float ex2(float x) {
 
 // rows x width numbers of packed rows into shared memory (pitch = width + 4), zeros behind `rows`; columns from `live` on are
 // the rank's padding: zeros, whatever the caller left there.  copy: the same numbers kept for the backward pass.
-template <typename T>
-__device__ __forceinline__ void load_rows(float* dst, const T* src, int64_t stride, int rows, int width, int live, int tid,
+__device__ __forceinline__ void load_rows(float* dst, const float* src, int64_t stride, int rows, int width, int live, int tid,
                                           float* copy = nullptr) {
   for (int idx = tid; idx < kRows * width; idx += kThreads) {
     const int r = idx / width, c = idx - r * width;
     float x = 0.f;
     if (r < rows) {
-      if (c < live) x = to_f<T>(src[r * stride + c]);
+      if (c < live) x = src[r * stride + c];
       if (copy != nullptr) copy[r * stride + c] = x;
     }
     dst[r * (width + 4) + c] = x;
@@ -139,7 +129,7 @@ __device__ __forceinline__ int64_t v_at(const TrainParams& p, const HeadInfo& hd
   return (static_cast<int64_t>(b) * p.T + t) * p.lr_v_width + hd.lr_v_off;
 }
 
-template <typename T, int NC>
+template <int NC>
 __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
   const Unit u = query_unit(p, blockIdx.x);
@@ -154,7 +144,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
   float* Vs = Ks + kRows * (rk + 4);
   float* Ps = Vs + kRows * (rv + 4);
   const int64_t q_stride = static_cast<int64_t>(p.group) * p.lr_k_width, o_stride = static_cast<int64_t>(p.group) * p.lr_v_width;
-  const T *q = static_cast<const T*>(p.q), *k = static_cast<const T*>(p.k), *v = static_cast<const T*>(p.v);
+  const float *q = static_cast<const float*>(p.q), *k = static_cast<const float*>(p.k), *v = static_cast<const float*>(p.v);
   load_rows(Qs, q + q_at(p, hd, u, i0), q_stride, max(0, min(kRows, n - i0)), rk, hd.r_k, tid, p.q_copy + q_at(p, hd, u, i0));
   if (u.i == 0) {                                            // one query head of the group keeps the keys and values
     load_rows(Ks, k + k_at(p, hd, u.b, i0), p.lr_k_width, max(0, min(kRows, n - i0)), rk, hd.r_k, tid, p.k_copy + k_at(p, hd, u.b, i0));
@@ -207,7 +197,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
     __syncthreads();
     product_nn<NC>(o, Ps, Vs, rv, ty, tx);
   }
-  T* out = static_cast<T*>(p.out);
+  float* out = static_cast<float*>(p.out);
   const int64_t stat = static_cast<int64_t>(blockIdx.x) * p.pad, all = static_cast<int64_t>(gridDim.x) * p.pad;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -223,7 +213,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
       const int col = tx + 16 * c;
       if (col >= rv) continue;
       const float x = row < n ? o[i][c] * inv : 0.f;
-      out[o_at(p, hd, u, row) + col] = from_f<T>(x);
+      out[o_at(p, hd, u, row) + col] = x;
       p.o[(static_cast<int64_t>(blockIdx.x) * p.T + row) * p.o_stride + col] = x;
     }
   }
@@ -236,7 +226,7 @@ __device__ __forceinline__ float probability(const TrainParams& p, const HeadInf
 }
 
 // dq' of a tile of query rows; also their delta, and this tile's share of the bias gradient.
-template <typename T, int NC>
+template <int NC>
 __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
   __shared__ float stats[3][kRows];                          // maximum, reciprocal sum, delta
@@ -253,7 +243,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainPara
   float* Ps = Vs + kRows * (rv + 4);
   const int64_t stat = static_cast<int64_t>(blockIdx.x) * p.pad, all = static_cast<int64_t>(gridDim.x) * p.pad;
   load_rows(Qs, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, rows, rk, hd.r_k, tid);
-  load_rows(Gs, static_cast<const T*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v, tid);
+  load_rows(Gs, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v, tid);
   __syncthreads();
   for (int r = tid >> 2; r < kRows; r += kThreads / 4) {     // four threads for a row of do' o'
     float sum = 0.f;
@@ -312,21 +302,21 @@ __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainPara
       }
     }
   }
-  T* out = static_cast<T*>(p.dq);
+  float* out = static_cast<float*>(p.dq);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = i0 + ty + 16 * i;
     if (row >= p.T) continue;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      if (tx + 16 * c < rk) out[q_at(p, hd, u, row) + tx + 16 * c] = from_f<T>(dq[i][c] * p.scale);
+      if (tx + 16 * c < rk) out[q_at(p, hd, u, row) + tx + 16 * c] = dq[i][c] * p.scale;
   }
   if (p.dtable != nullptr && tid < p.buckets)                // (group 1: a head's units are its sequences)
     p.bias_part[(static_cast<int64_t>(blockIdx.x) * gridDim.y + tile) * p.buckets + tid] = static_cast<float>(by_bucket);
 }
 
 // dk', dv' of a tile of keys: the query rows of every query head of the group.
-template <typename T, int NC>
+template <int NC>
 __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
   __shared__ float stats[3][kRows];
@@ -355,7 +345,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
       const int rows = min(kRows, n - i0);
       __syncthreads();
       load_rows(Qs, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, rows, rk, hd.r_k, tid);
-      load_rows(Gs, static_cast<const T*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v, tid);
+      load_rows(Gs, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v, tid);
       if (tid < kRows) {
         stats[0][tid] = tid < rows ? p.lse[stat + i0 + tid] : INFINITY;
         stats[1][tid] = tid < rows ? p.lse[all + stat + i0 + tid] : 0.f;
@@ -385,7 +375,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
       product_nn<NC>(dk, Ps, Qs, rk, ty, tx);
     }
   }
-  T *out_k = static_cast<T*>(p.dk), *out_v = static_cast<T*>(p.dv);
+  float *out_k = static_cast<float*>(p.dk), *out_v = static_cast<float*>(p.dv);
 #pragma unroll
   for (int a = 0; a < 4; ++a) {
     const int key = j0 + ty + 16 * a;
@@ -393,8 +383,8 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int col = tx + 16 * c;
-      if (col < rk) out_k[k_at(p, hd, b, key) + col] = from_f<T>(dk[a][c] * p.scale);
-      if (col < rv) out_v[v_at(p, hd, b, key) + col] = from_f<T>(dv[a][c]);
+      if (col < rk) out_k[k_at(p, hd, b, key) + col] = dk[a][c] * p.scale;
+      if (col < rv) out_v[v_at(p, hd, b, key) + col] = dv[a][c];
     }
   }
 }
@@ -403,24 +393,24 @@ size_t smem_bytes(const TrainParams& p, int key_tiles, int value_tiles) {
   return (static_cast<size_t>(kRows) * (key_tiles * (p.max_rp_k + 4) + value_tiles * (p.max_rp_v + 4)) + kRows * kPitchP) * sizeof(float);
 }
 
-template <typename T, int NC>
+template <int NC>
 cudaError_t forward_t(const TrainParams& p, cudaStream_t s) {
   static size_t done[kMaxDevices] = {};
   const size_t smem = smem_bytes(p, 2, 1);
-  const cudaError_t e = ensure_dynamic_smem(train_simt_forward_kernel<T, NC>, smem, done);
+  const cudaError_t e = ensure_dynamic_smem(train_simt_forward_kernel<NC>, smem, done);
   if (e != cudaSuccess) return e;
-  train_simt_forward_kernel<T, NC><<<dim3(p.H * p.group * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
+  train_simt_forward_kernel<NC><<<dim3(p.H * p.group * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
   return cudaGetLastError();
 }
-template <typename T, int NC>
+template <int NC>
 cudaError_t backward_t(const TrainParams& p, cudaStream_t s) {
   static size_t done_q[kMaxDevices] = {}, done_kv[kMaxDevices] = {};
   const size_t smem = smem_bytes(p, 2, 2);
-  cudaError_t e = ensure_dynamic_smem(train_simt_dq_kernel<T, NC>, smem, done_q);
-  if (e == cudaSuccess) e = ensure_dynamic_smem(train_simt_dkv_kernel<T, NC>, smem, done_kv);
+  cudaError_t e = ensure_dynamic_smem(train_simt_dq_kernel<NC>, smem, done_q);
+  if (e == cudaSuccess) e = ensure_dynamic_smem(train_simt_dkv_kernel<NC>, smem, done_kv);
   if (e != cudaSuccess) return e;
-  train_simt_dq_kernel<T, NC><<<dim3(p.H * p.group * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
-  train_simt_dkv_kernel<T, NC><<<dim3(p.H * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
+  train_simt_dq_kernel<NC><<<dim3(p.H * p.group * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
+  train_simt_dkv_kernel<NC><<<dim3(p.H * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
   return cudaGetLastError();
 }
 
@@ -430,17 +420,15 @@ int train_simt_tiles(int T) { return (T + kRows - 1) / kRows; }
 
 // Columns of a thread by the widest rank: 32, 64 or 128 columns over 16 threads (a rank of 40 in the widest instance would
 // spend three quarters of its multiply-adds on columns that are not there).
-cudaError_t launch_train_simt_forward(const TrainParams& p, int dtype, cudaStream_t s, uint64_t* launches) {
+cudaError_t launch_train_simt_forward(const TrainParams& p, cudaStream_t s, uint64_t* launches) {
   ++*launches;
   const int widest = p.max_rp_k > p.max_rp_v ? p.max_rp_k : p.max_rp_v;
-  if (dtype == 0) return widest <= 32 ? forward_t<__nv_bfloat16, 2>(p, s) : widest <= 64 ? forward_t<__nv_bfloat16, 4>(p, s) : forward_t<__nv_bfloat16, 8>(p, s);
-  return widest <= 32 ? forward_t<float, 2>(p, s) : widest <= 64 ? forward_t<float, 4>(p, s) : forward_t<float, 8>(p, s);
+  return widest <= 32 ? forward_t<2>(p, s) : widest <= 64 ? forward_t<4>(p, s) : forward_t<8>(p, s);
 }
-cudaError_t launch_train_simt_backward(const TrainParams& p, int dtype, cudaStream_t s, uint64_t* launches) {
+cudaError_t launch_train_simt_backward(const TrainParams& p, cudaStream_t s, uint64_t* launches) {
   *launches += 2;
   const int widest = p.max_rp_k > p.max_rp_v ? p.max_rp_k : p.max_rp_v;
-  if (dtype == 0) return widest <= 32 ? backward_t<__nv_bfloat16, 2>(p, s) : widest <= 64 ? backward_t<__nv_bfloat16, 4>(p, s) : backward_t<__nv_bfloat16, 8>(p, s);
-  return widest <= 32 ? backward_t<float, 2>(p, s) : widest <= 64 ? backward_t<float, 4>(p, s) : backward_t<float, 8>(p, s);
+  return widest <= 32 ? backward_t<2>(p, s) : widest <= 64 ? backward_t<4>(p, s) : backward_t<8>(p, s);
 }
 
 }  // namespace ea
