@@ -2052,7 +2052,7 @@ constexpr int kTrainMaxTokens = 1 << 20;
 size_t train_tile_bytes(int rp) { return static_cast<size_t>(ea::kTrainTile) * ((rp + 15) & ~15) * 2; }
 // parts of a sequence's scores that leave a sum per bucket of their own
 int train_bias_parts(const eigen_attn* h, int T) {
-  return h->desc.dtype == EA_FP32 ? ea::train_simt_tiles(T) : (T + ea::kTrainTile - 1) / ea::kTrainTile;
+  return h->desc.dtype == EA_FP32 ? ea::train_simt_tiles(T) : (T + ea::kTrainTile - 1) / ea::kTrainTile * ea::kTrainBiasParts;
 }
 void make_train_layout(const eigen_attn* h, int tokens, int group, TrainLayout* t) {
   const size_t B = h->desc.batch, units = B * h->desc.n_heads, q_units = units * group;
@@ -2122,6 +2122,7 @@ void fill_train(eigen_attn_t h, int T, int group, ea::TrainParams* p) {
   p->scale = static_cast<float>(1.0 / sqrt(static_cast<double>(h->desc.d_head)));
   p->scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(h->desc.d_head)));
   p->alibi = h->alibi ? 1 : 0;
+  p->sm_count = h->sm_count;
   if (h->bias_buf) {
     p->bias = dev_bias(h); p->bias_len = bias_len(h);
     p->starts = reinterpret_cast<const int32_t*>(h->bias_buf);
@@ -2171,6 +2172,9 @@ ea_status eigen_attn_train_forward(eigen_attn_t h, const void* d_q, const void* 
                 h->train_tokens, h->train_group);
   const ea_status st = check_train(h, "train_forward", group);
   if (st != EA_OK) return st;
+  const int64_t tiles = (static_cast<int64_t>(T) + ea::kTrainTile - 1) / ea::kTrainTile;
+  if (static_cast<int64_t>(h->desc.batch) * h->desc.n_heads * (group + 2) * tiles > INT32_MAX / 2)
+    return fail(h, EA_ERR_SHAPE, "train_forward: %d tokens of %d sequences: too many tiles", T, h->desc.batch);
   ea::TrainParams p;
   fill_train(h, T, group, &p);
   p.q = d_q; p.k = d_k; p.v = d_v; p.out = d_out; p.lens_in = d_lens;

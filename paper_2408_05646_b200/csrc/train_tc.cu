@@ -6,12 +6,18 @@
 // Scores are kept in the base-2 domain.  The forward pass leaves L_i = log2 sum_j 2^S_ij per row; the backward pass recomputes
 // P_ij = 2^(S_ij - L_i) from one product, without a maximum or a sum.
 //
-// A tile is 128 rows.  Every CTA is one thread that copies tiles (one bulk copy each, into a ring), one warp that issues the
-// products, and eight softmax warps; one CTA per SM, whose 512 TMEM columns it takes.  P and dS go back to TMEM in the place of
-// the scores they came from, as the A operand of the next product, and never touch shared memory.  The backward pass is two
-// kernels, one that owns a tile of keys (dk', dv': four products per pair of tiles) and one that owns a tile of queries (dq':
-// three, S and do' v' a second time): the alternative, dq' added up in memory by every tile of keys, moves 512 r bytes of
-// fp32 additions per pair of tiles through L2 and leaves sums whose order changes from run to run.
+// A tile is 128 rows.  A persistent CTA per SM (it takes the SM's 512 TMEM columns) works through items: a tile (or two) of one
+// axis, which it keeps in shared memory, against the tiles of the other axis, which stream through a ring in halves of 64 rows
+// with score buffers of their own: while the softmax works on one half, the products of the other run.  Roles:
+//   * a copying warp: one bulk copy per tile.  It alone reads the item list, lengths and exponents; what the others need to know
+//     of an item goes with the item's own tiles, of which there are two sets where they fit, so that an item starts with its
+//     tiles at hand (a CTA per item spent some 7000 clocks on its start and end: a fifth of the time at 4096 tokens);
+//   * issuing warps, two or three.  (With one, the products were late: it shares its scheduler with softmax warps, which leave
+//     it an instruction every 10 to 20 clocks.)  Products of one accumulator have one issuer, so that their order is fixed;
+//   * eight softmax warps.  P and dS go back to TMEM as the A operand of the next product and never touch shared memory.
+// The backward pass is two kernels, one that owns tiles of keys (dk', dv': four products per pair of tiles) and one that owns
+// tiles of queries (dq': three, S and do' v' a second time): the alternative, dq' added up in memory by every tile of keys,
+// moves 512 r bytes of fp32 additions per pair of tiles through L2 and leaves sums whose order changes from run to run.
 //
 // Tiles carry a power of two each (2^e).  What is accumulated over tiles needs one scale: the tile's deviation from the
 // smallest exponent of all goes into the factors that P and dS are formed with, where it costs nothing.
@@ -29,18 +35,41 @@ using namespace tc;
 
 constexpr int kNone = 0, kAlibi = 1, kTable = 2;             // position bias
 constexpr int kSoftmaxWarps = 8, kCopyWarp = 8, kIssueWarp = 9;
-constexpr int kTrThreads = 10 * 32;
+constexpr int kTrThreads = 12 * 32;       // softmax, copies, up to three issuing warps
+constexpr int kHalf = 64;                 // rows of the walked axis that share a score buffer
 constexpr int kMaxRing = 8;
 constexpr int kHeaderBytes = 1024;
+constexpr int kScaleBytes = 16;           // behind a stage's tiles: the scales of the pair of tiles, worked out by the copying warp
 constexpr int kForwardShift = 7;          // P of the forward pass times 2^7: its reference lags behind the maximum by up to 2^8
 constexpr int kBackwardShift = 14;        // P of the backward pass, at most 1, times 2^14: fp16 keeps all bits down to 2^-28
 
+// What a launch decides for all its CTAs.
+struct Plan {
+  int stages, sets;         // of the ring; sets of own tiles (1 or 2)
+  int items, per_unit;      // items of the launch, and of a unit
+  int units, chunk;         // units; as many as follow one another in the list with all their items (see item_of)
+  int aligned;              // outputs on 16-byte boundaries: bit 0, bit 1
+  int apart;                // dk', dv': P has TMEM columns of its own
+};
+
+// An item, as the copying warp passes it on.
+struct Item {
+  int unit, h, b, i;        // unit of the owned axis, its K/V head, sequence, query head of the group
+  int tile, n;              // first tile of the owned axis, tokens of the sequence
+  int rp_k, rp_v;
+  int tiles[2];             // tiles that it walks (forward: for either of its two tiles of queries); tiles[0] < 0: no more items
+  int small[4];             // smallest exponents of q', k', v', do'
+};
+
 struct __align__(16) TrHeader {
   unsigned long long full[kMaxRing], empty[kMaxRing];        // ring of tiles
-  unsigned long long own;                                    // the CTA's own tiles
-  unsigned long long s_full[2], p_full[2], g_full, g_read, done;
+  unsigned long long own_full[2], own_empty[2];              // the item's own tiles and its description
+  unsigned long long s_full[2][2], p_full[2][2];             // forward: [tile of queries][half]
+  unsigned long long g_full[2], g_read[2], s_read[2], p_used[2][2];
+  unsigned long long acc_full[2], acc_free[2];               // sums complete; read
+  unsigned long long drain[3];                               // an issuing warp's last products
   uint32_t tmem_base;
-  int smallest[4];                                           // smallest exponents of q', k', v', do'
+  Item item[2];
 };
 static_assert(sizeof(TrHeader) <= kHeaderBytes, "header outgrew its area");
 
@@ -49,8 +78,10 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
   return p != 0;
 }
+__device__ __noinline__ bool wait_long(unsigned long long* bar, uint32_t parity, int* status) { return mbar_wait(bar, parity, status); }
 __device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parity, int* status) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, status)) != 0;
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, wait_long(bar, parity, status)) != 0;
 }
 // 2^e; exponents that no pair of ordinary tiles has end at the ends of the range
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((min(max(e, -126), 127) + 127) << 23); }
@@ -76,14 +107,14 @@ __device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {
 }
 constexpr uint32_t kMnMajorB = 1u << 16;
 
-// A product over the rank: D[128][128] = A B^T, both tiles K-major; KS steps of 16 columns.
+// A product over the rank: D[128][64] = A B^T, both K-major, B the half of a tile; KS steps of 16 columns.
 template <int KS>
 __device__ __forceinline__ void issue_rank_steps(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
 #pragma unroll
   for (int s = 0; s < KS; ++s) mma_ss(d, a + 16 * s, b + 16 * s, idesc, s > 0);
 }
 __device__ __forceinline__ void issue_rank(int steps, uint32_t d, uint64_t a, uint64_t b) {
-  const uint32_t idesc = instr_desc_f16(kTile);
+  const uint32_t idesc = instr_desc_f16(kHalf);
   switch (steps) {
     case 1: issue_rank_steps<1>(d, a, b, idesc); break;
     case 2: issue_rank_steps<2>(d, a, b, idesc); break;
@@ -95,13 +126,45 @@ __device__ __forceinline__ void issue_rank(int steps, uint32_t d, uint64_t a, ui
     default: issue_rank_steps<8>(d, a, b, idesc); break;
   }
 }
-// A product over 128 rows: D[128][r16] (+)= A B with A (P or dS) in TMEM, its second half `half` columns behind the first,
-// and B a tile taken MN-major (`group`: bytes of 8 of its rows).
-__device__ __forceinline__ void issue_rows(uint32_t d, uint32_t a, uint32_t half, uint64_t b, int group, uint32_t idesc, bool add) {
+// A product over the 64 rows of a half: D[128][r16] (+)= A B with A (P or dS) in 32 columns of TMEM and B the half of a tile,
+// taken MN-major (`group`: bytes of 8 of its rows).
+__device__ __forceinline__ void issue_rows(uint32_t d, uint32_t a, uint64_t b, int group, uint32_t idesc, bool add) {
   const uint64_t step = static_cast<uint64_t>(group) >> 3;   // 16 rows = two groups, in units of 16 bytes
 #pragma unroll
-  for (int s = 0; s < kTile / 16; ++s) mma_ts(d, a + (s >> 2) * half + (s & 3) * 8, b + s * step, idesc, add || s > 0);
+  for (int s = 0; s < kHalf / 16; ++s) mma_ts(d, a + 8 * s, b + s * step, idesc, add || s > 0);
 }
+// second half of a tile, in a descriptor: 64 rows = 8 groups
+__device__ __forceinline__ uint64_t half_of(int half, int group) { return static_cast<uint64_t>(half) * (group >> 1); }
+// A place in the ring and the phase of its barriers.
+struct Place {
+  int stage = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int stages) {
+    if (++stage == stages) { stage = 0; phase ^= 1u; }
+  }
+};
+// Pairs of fp32 numbers in 64-bit registers.
+__device__ __forceinline__ unsigned long long both(float x) { return pack2(x, x); }
+__device__ __forceinline__ unsigned long long pair_at(const uint32_t (&r)[32], int k) {
+  return pack2(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
+}
+
+// Entry `index` of the list of items.  The items of `chunk` units follow one another, the longest (slot 0) first: those that run
+// at a time then stream tiles of a few units, which stay in L2 (all units at once are 168 MB for 4 x 4096 tokens of 32 heads),
+// and the longest of many units together leave short ones for the end.
+__device__ __forceinline__ void item_of(const Plan& plan, int index, int& unit, int& slot) {
+  const int per_chunk = plan.chunk * plan.per_unit, first = index / per_chunk * plan.chunk, rest = index % per_chunk;
+  const int width = min(plan.chunk, plan.units - first);
+  slot = rest / width;
+  unit = first + rest - slot * width;
+}
+// Items of a CTA: every gridDim.x-th, there and back, so that no CTA has the longer one every time.
+__device__ __forceinline__ int64_t list_index(int it) {
+  return static_cast<int64_t>(it) * gridDim.x + (it & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+}
+// Set of own tiles of a CTA's item and the phase of its barriers.
+__device__ __forceinline__ int set_of(const Plan& plan, int it) { return plan.sets == 2 ? it & 1 : 0; }
+__device__ __forceinline__ uint32_t set_phase(const Plan& plan, int it) { return (plan.sets == 2 ? it >> 1 : it) & 1u; }
 
 // One query row's (or key row's) numbers of the packed gradients: 8 columns from `c`, rounded to bf16, `live` columns exist.
 __device__ __forceinline__ void store8(__nv_bfloat16* dst, const float* x, bool aligned) {
@@ -147,273 +210,347 @@ __device__ __forceinline__ int smallest_of(const int32_t* e, int count, int lane
   return __reduce_min_sync(0xffffffffu, m);
 }
 
-// Bias of a tile of queries i0 .. against a tile of keys j0 ..: one number for all (`far`), unless some distance lies in front of the last entry.
+// Bias of a half tile of queries i0 .. against keys j0 ..: one number for all, unless some distance lies in front of the last entry.
 __device__ __forceinline__ bool near_tile(const TrainParams& p, int i0, int j0) { return i0 - j0 - (kTile - 1) < p.bias_len - 1; }
 
-// ---------------------------------------------------------------- forward
-
-// A CTA has two tiles of queries, each with four softmax warps (a thread per query row, all 128 keys of a tile), so that the
-// products of one run under the softmax of the other.  Per tile of keys: S, the row's maximum, 2^(S - reference) and their
-// sum, P in the place of S, o' += P v'.  The reference is a lazy one: it moves, and o' is rescaled, only when a score exceeds
-// it by 8.  TMEM: S of both tiles (128 columns each, P in the first 64 of them), o' of both.
-// Bound by the exponentials (16 a clock: 2048 clocks for two pairs of tiles; their products take 1280 at rank 80).
-template <int BIAS>
-__global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const TrainParams p, int stages, int aligned) {
-  extern __shared__ __align__(1024) unsigned char smem[];
-  TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int unit = blockIdx.x, hq = unit / p.B, b = unit - hq * p.B, h = hq / p.group, ih = hq - h * p.group;
-  const int key_unit = h * p.B + b;
-  const HeadInfo hd = p.heads[h];
-  const int pair = gridDim.y - 1 - blockIdx.y;               // long rows first
-  const int n = __ldg(p.lens + b);
-  const int rk16 = (hd.rp_k + 15) & ~15, rv16 = (hd.rp_v + 15) & ~15;
-  const int q_bytes = kTile * rk16 * 2, v_bytes = kTile * rv16 * 2, stage_bytes = q_bytes + v_bytes;
-  unsigned char* own = smem + kHeaderBytes;
-  unsigned char* ring = own + 2 * q_bytes;
-  int nt[2];                                                 // tiles of keys that a tile of queries sees
-  for (int x = 0; x < 2; ++x) nt[x] = (2 * pair + x) * kTile < n ? 2 * pair + x + 1 : 0;
-  const int most = max(nt[0], nt[1]);
-
+// Barriers, TMEM and the layout that all three kernels share; returns the TMEM base.
+__device__ __forceinline__ uint32_t set_up(TrHeader* hdr, int warp, int tid, int empty, int own_empty, int p_full, int acc_full, int acc_free) {
   if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
   if (tid == 0) {
     for (int s = 0; s < kMaxRing; ++s) {
       mbar_init(&hdr->full[s], 1);
-      mbar_init(&hdr->empty[s], 1);
+      mbar_init(&hdr->empty[s], empty);
     }
-    mbar_init(&hdr->own, 1);
     for (int x = 0; x < 2; ++x) {
-      mbar_init(&hdr->s_full[x], 1);
-      mbar_init(&hdr->p_full[x], 4);
+      mbar_init(&hdr->own_full[x], 1);
+      mbar_init(&hdr->own_empty[x], own_empty);
+      for (int y = 0; y < 2; ++y) {
+        mbar_init(&hdr->s_full[x][y], 1);
+        mbar_init(&hdr->p_full[x][y], p_full);
+        mbar_init(&hdr->p_used[x][y], 1);
+      }
+      mbar_init(&hdr->g_full[x], 1);
+      mbar_init(&hdr->g_read[x], kSoftmaxWarps / 2);
+      mbar_init(&hdr->s_read[x], kSoftmaxWarps / 2);
+      mbar_init(&hdr->acc_full[x], acc_full);
+      mbar_init(&hdr->acc_free[x], acc_free);
     }
-    mbar_init(&hdr->done, 1);
+    for (int x = 0; x < 3; ++x) mbar_init(&hdr->drain[x], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == kIssueWarp) {
-    const int m = smallest_of(p.v_exp + static_cast<int64_t>(key_unit) * p.tiles, p.tiles, lane);
-    if (lane == 0) hdr->smallest[2] = m;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = hdr->tmem_base;
+  return __shfl_sync(0xffffffffu, hdr->tmem_base, 0);
+}
+// The end of an issuing warp: nothing of it is under way when the CTA leaves.
+__device__ __forceinline__ void drain(TrHeader* hdr, int which, bool lead, int* status) {
+  if (lead) mma_commit(&hdr->drain[which]);
+  __syncwarp();
+  wait_all(&hdr->drain[which], 0, status);
+}
+// The end of a copying warp that gave up: copies in flight must land before the CTA leaves.  (Otherwise their consumers have
+// waited for all of them.)
+__device__ __forceinline__ void drain_copies(TrHeader* hdr, const Plan& plan, int items, int issued, int* status) {
+  for (int s = 0; s < plan.sets && s < items; ++s)
+    mbar_wait(&hdr->own_full[s], set_phase(plan, items - 1 - ((items - 1 - s) % plan.sets)), status);
+  for (int s = 0; s < plan.stages && s < issued; ++s) mbar_wait(&hdr->full[s], ((issued - 1 - s) / plan.stages) & 1u, status);
+}
+
+// ---------------------------------------------------------------- forward
+
+// An item is two tiles of queries, each with four softmax warps (a thread per query row) and an issuing warp.  Per half tile of
+// keys: S, the row's maximum, 2^(S - reference) and their sum, P in the place of S, o' += P v'.  The reference is a lazy one:
+// it moves, and o' is rescaled, only when a score exceeds it by 8.  TMEM: two halves of S for both tiles (64 columns each, P in
+// the first 32 of them), o' of both.
+// Bound by the exponentials (16 a clock: 2048 clocks for two pairs of tiles; their products take 1630 at rank 80).
+template <int BIAS>
+__global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const TrainParams p, const Plan plan) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  unsigned char* own = smem + kHeaderBytes;                  // sets of two tiles of q'
+  unsigned char* ring = own + plan.sets * 2 * p.tile_k;
+  const int stage_bytes = p.tile_k + p.tile_v + kScaleBytes; // (tiles of narrower heads fill a part)
+  const uint32_t tmem = set_up(hdr, warp, tid, 2, 2 + kSoftmaxWarps, 4, 1, 4);
 
   if (warp == kCopyWarp) {
-    if (lane == 0 && most > 0) {
-      const uint64_t keep = policy_evict_normal();
-      const char* q = p.q_tiles + (static_cast<int64_t>(unit) * p.tiles + 2 * pair) * p.tile_k;
-      mbar_arrive_expect_tx(&hdr->own, (nt[1] > 0 ? 2 : 1) * q_bytes);
-      bulk_load(own, q, q_bytes, &hdr->own, keep);
-      if (nt[1] > 0) bulk_load(own + q_bytes, q + p.tile_k, q_bytes, &hdr->own, keep);
-      const char* k = p.k_tiles + static_cast<int64_t>(key_unit) * p.tiles * p.tile_k;
-      const char* v = p.v_tiles + static_cast<int64_t>(key_unit) * p.tiles * p.tile_v;
-      int issued = 0;
-      for (int j = 0; j < most; ++j, ++issued) {
-        const int st = j % stages;
-        if (j >= stages && !mbar_wait(&hdr->empty[st], (j / stages - 1) & 1u, p.status)) break;
-        mbar_arrive_expect_tx(&hdr->full[st], stage_bytes);
-        bulk_load(ring + st * stage_bytes, k + static_cast<int64_t>(j) * p.tile_k, q_bytes, &hdr->full[st], keep);
-        bulk_load(ring + st * stage_bytes + q_bytes, v + static_cast<int64_t>(j) * p.tile_v, v_bytes, &hdr->full[st], keep);
-      }
-      // copies in flight must land before the CTA leaves; normally their consumers have waited for them
-      mbar_wait(&hdr->own, 0, p.status);
-      for (int s = 0; s < stages && s < issued; ++s) mbar_wait(&hdr->full[s], ((issued - 1 - s) / stages) & 1u, p.status);
-    }
-  } else if (warp == kIssueWarp) {
-    if (most > 0) {
-      const bool lead = elect_one();
-      const uint32_t idesc_o = instr_desc_f16(rv16) | kMnMajorB;
-      const uint64_t dq = smem_desc(smem_u32(own), 128, rk16 << 4);
-      const uint64_t dk = smem_desc(smem_u32(ring), 128, rk16 << 4);
-      const uint64_t dv = smem_desc(smem_u32(ring) + q_bytes, rv16 << 4, 128);
-      const uint64_t stage = stage_bytes >> 4;
-      auto score = [&](int x, int st) {                      // S of tile x against the keys of a stage
-        if (lead) {
-          issue_rank(rk16 >> 4, tmem + x * kTile, dq + x * (q_bytes >> 4), dk + st * stage);
-          mma_commit(&hdr->s_full[x]);
+    const uint64_t keep = policy_evict_normal();
+    bool ok = true;
+    Place at;
+    int issued = 0, it = 0;
+    for (;; ++it) {
+      const int set = set_of(plan, it);
+      if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
+      if (!ok) break;
+      Item* item = &hdr->item[set];
+      const int64_t index = list_index(it);
+      if (index >= plan.items) {
+        if (lane == 0) {
+          item->tiles[0] = -1;
+          mbar_arrive(&hdr->own_full[set]);
         }
-        __syncwarp();
-      };
-      bool ok = wait_all(&hdr->own, 0, p.status) && wait_all(&hdr->full[0], 0, p.status);
-      if (ok) {
-        tc_fence_after();
-        for (int x = 0; x < 2; ++x)
-          if (nt[x] > 0) score(x, 0);
+        break;
       }
-      for (int j = 0; j < most && ok; ++j) {
-        const int st = j % stages, next = (j + 1) % stages;
-        bool ready = false;
-        for (int x = 0; x < 2 && ok; ++x) {
-          if (j >= nt[x]) continue;
-          ok = wait_all(&hdr->p_full[x], j & 1u, p.status);
+      int unit, slot;
+      item_of(plan, static_cast<int>(index), unit, slot);
+      const int hq = unit / p.B, b = unit - hq * p.B, h = hq / p.group, key_unit = h * p.B + b;
+      const int tile = 2 * (plan.per_unit - 1 - slot);
+      const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
+      const int q_bytes = kTile * ((rp_k + 15) & ~15) * 2, v_bytes = kTile * ((rp_v + 15) & ~15) * 2;
+      const int nt0 = tile * kTile < n ? tile + 1 : 0, nt1 = (tile + 1) * kTile < n ? tile + 2 : 0, most = max(nt0, nt1);
+      const int32_t *k_exp = p.k_exp + static_cast<int64_t>(key_unit) * p.tiles, *v_exp = p.v_exp + static_cast<int64_t>(key_unit) * p.tiles;
+      const int g_v = smallest_of(v_exp, p.tiles, lane);
+      const int64_t q_at = static_cast<int64_t>(unit) * p.tiles + tile;
+      const int q_e0 = __ldg(p.q_exp + q_at), q_e1 = nt1 > 0 ? __ldg(p.q_exp + q_at + 1) : 0;
+      if (lane == 0) {
+        item->unit = unit; item->h = h; item->b = b; item->i = hq - h * p.group;
+        item->tile = tile; item->n = n; item->rp_k = rp_k; item->rp_v = rp_v;
+        item->tiles[0] = nt0; item->tiles[1] = nt1;
+        item->small[2] = g_v;
+        unsigned char* to = own + set * 2 * p.tile_k;
+        const char* q = p.q_tiles + q_at * p.tile_k;
+        if (most > 0) {
+          mbar_arrive_expect_tx(&hdr->own_full[set], (nt1 > 0 ? 2 : 1) * q_bytes);
+          bulk_load(to, q, q_bytes, &hdr->own_full[set], keep);
+          if (nt1 > 0) bulk_load(to + p.tile_k, q + p.tile_k, q_bytes, &hdr->own_full[set], keep);
+        } else {
+          mbar_arrive(&hdr->own_full[set]);
+        }
+        const char* k = p.k_tiles + static_cast<int64_t>(key_unit) * p.tiles * p.tile_k;
+        const char* v = p.v_tiles + static_cast<int64_t>(key_unit) * p.tiles * p.tile_v;
+        for (int j = 0; j < most; ++j, ++issued, at.next(plan.stages)) {
+          // the tile's deviation from the largest v'; at 2^-60 of it P is zero in fp16, and the sum of the row still exact
+          const int k_e = __ldg(k_exp + j), f = max(g_v - __ldg(v_exp + j), -60);
+          unsigned long long* full = &hdr->full[at.stage];
+          if (issued >= plan.stages && !(ok = mbar_wait(&hdr->empty[at.stage], at.phase ^ 1u, p.status))) break;
+          unsigned char* st = ring + at.stage * stage_bytes;
+          *reinterpret_cast<float4*>(st + p.tile_k + p.tile_v) =
+              make_float4(p.scale_log2 * pow2(-q_e0 - k_e), p.scale_log2 * pow2(-q_e1 - k_e), static_cast<float>(f), pow2(-f));
+          mbar_arrive_expect_tx(full, q_bytes + v_bytes);
+          bulk_load(st, k + static_cast<int64_t>(j) * p.tile_k, q_bytes, full, keep);
+          bulk_load(st + p.tile_k, v + static_cast<int64_t>(j) * p.tile_v, v_bytes, full, keep);
+        }
+      }
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) { ++it; break; }
+    }
+    if (!ok && lane == 0) drain_copies(hdr, plan, it, issued, p.status);
+  } else if (warp >= kIssueWarp && warp < kIssueWarp + 2) {
+    const int x = warp - kIssueWarp;                         // the products of one tile of queries
+    const bool lead = elect_one();
+    const uint64_t stage = stage_bytes >> 4;
+    const uint32_t tS = tmem + x * kTile, tO = tmem + 256 + x * kTile;
+    bool ok = true;
+    int done = 0, sums = 0;                                  // tiles and items behind this warp
+    Place at, next;                                          // of P v' and of S
+    for (int it = 0; ok; ++it) {
+      const int set = set_of(plan, it);
+      ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
+      if (!ok || hdr->item[set].tiles[0] < 0) break;
+      const int nt = hdr->item[set].tiles[x], most = max(hdr->item[set].tiles[0], hdr->item[set].tiles[1]);
+      const int rk16 = (hdr->item[set].rp_k + 15) & ~15, rv16 = (hdr->item[set].rp_v + 15) & ~15;
+      const uint32_t idesc_o = instr_desc_f16(rv16) | kMnMajorB;
+      const uint64_t dq = smem_desc(smem_u32(own) + (set * 2 + x) * p.tile_k, 128, rk16 << 4);
+      const uint64_t dk = smem_desc(smem_u32(ring), 128, rk16 << 4), dv = smem_desc(smem_u32(ring) + p.tile_k, rv16 << 4, 128);
+      if (nt > 0 && sums > 0) ok = wait_all(&hdr->acc_free[x], (sums - 1) & 1u, p.status);
+      for (int j = 0; nt > 0 && j < 2 * nt + 2 && ok; ++j) { // S of half j, two halves ahead of P
+        const int half = j & 1;
+        if (j >= 2) {
+          ok = wait_all(&hdr->p_full[x][half], (done + ((j - 2) >> 1)) & 1u, p.status);
           if (!ok) break;
           tc_fence_after();
-          if (lead) issue_rows(tmem + 256 + x * kTile, tmem + x * kTile, 32, dv + st * stage, rv16 << 4, idesc_o, j > 0);
-          __syncwarp();
-          if (j + 1 < nt[x]) {
-            if (!ready) ok = wait_all(&hdr->full[next], ((j + 1) / stages) & 1u, p.status);
-            ready = true;
-            if (!ok) break;
-            tc_fence_after();
-            score(x, next);
-          } else if (x == (nt[1] > 0 ? 1 : 0)) {             // (the longer tile ends last)
-            if (lead) mma_commit(&hdr->done);
-            __syncwarp();
+          if (lead) {
+            issue_rows(tO, tS + half * kHalf, dv + stage * at.stage + half_of(half, rv16 << 4), rv16 << 4, idesc_o, j > 2);
+            mma_commit(&hdr->p_used[x][half]);
+            if (half) mma_commit(&hdr->empty[at.stage]);
           }
+          __syncwarp();
+          if (half) at.next(plan.stages);
         }
-        if (ok && lead) mma_commit(&hdr->empty[st]);
-        __syncwarp();
+        if (j < 2 * nt) {                                    // (in P's place: behind the product that takes it)
+          if (!half) ok = wait_all(&hdr->full[next.stage], next.phase, p.status);
+          if (!ok) break;
+          tc_fence_after();
+          if (lead) {
+            issue_rank(rk16 >> 4, tS + half * kHalf, dq, dk + stage * next.stage + half_of(half, rk16 << 4));
+            mma_commit(&hdr->s_full[x][half]);
+          }
+          __syncwarp();
+          if (half) next.next(plan.stages);
+        }
       }
-      if (!ok && lead) mma_commit(&hdr->done);               // (the softmax leaves by the status word)
-      wait_all(&hdr->done, 0, p.status);                     // nothing is under way when the CTA leaves
-      if (ok) wait_all(&hdr->empty[(most - 1) % stages], ((most - 1) / stages) & 1u, p.status);
+      if (ok && lead) {
+        if (nt > 0) mma_commit(&hdr->acc_full[x]);
+        mma_commit(&hdr->own_empty[set]);
+      }
+      __syncwarp();
+      done += nt;
+      sums += nt > 0;
+      for (int j = nt; j < most && ok; ++j) {                // tiles that only the other tile of queries sees
+        ok = wait_all(&hdr->full[at.stage], at.phase, p.status);
+        if (ok && lead) mbar_arrive(&hdr->empty[at.stage]);
+        at.next(plan.stages);
+        next.next(plan.stages);
+      }
     }
-  } else {
-    const int x = warp >> 2, row = (warp & 3) * 32 + lane, tile = 2 * pair + x, i0 = tile * kTile, i = i0 + row;
+    drain(hdr, x, lead, p.status);
+  } else if (warp < kSoftmaxWarps) {
+    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + lanes + x * kTile, tO = tmem + lanes + 256 + x * kTile;
-    const int64_t tiles_at = static_cast<int64_t>(key_unit) * p.tiles;
-    const int g_v = hdr->smallest[2];
-    const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
-    const float slope2 = BIAS == kAlibi ? hd.alibi_slope2 : 0.f;
-    float m = -INFINITY, l = 0.f;
     bool ok = true;
-    const int q_e = nt[x] > 0 ? __ldg(p.q_exp + static_cast<int64_t>(unit) * p.tiles + tile) : 0;
-    for (int j = 0; j < nt[x]; ++j) {
-      const int j0 = j * kTile;
-      float c = p.scale_log2 * pow2(-q_e - __ldg(p.k_exp + tiles_at + j));
-      const float f = pow2(g_v - __ldg(p.v_exp + tiles_at + j));
-      const bool diag = j0 == i0, near = BIAS == kTable && near_tile(p, i0, j0);
-      float base = BIAS == kTable && !near ? __ldg(table + p.bias_len - 1) : BIAS == kAlibi ? slope2 * static_cast<float>(j0 - i) : 0.f;
-      ok = wait_all(&hdr->s_full[x], j & 1u, p.status);
+    int done = 0, sums = 0;
+    Place at;
+    for (int it = 0; ok; ++it) {
+      const int set = set_of(plan, it);
+      ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
       if (!ok) break;
-      tc_fence_after();
-      // S of a tile with masked keys or distances of their own goes back scaled, biased and masked
-      if (diag || near) {
+      const Item item = hdr->item[set];
+      if (item.tiles[0] < 0) break;
+      const int nt = x ? item.tiles[1] : item.tiles[0], most = max(item.tiles[0], item.tiles[1]);
+      const int tile = item.tile + x, i0 = tile * kTile, i = i0 + row, n = item.n, rv16 = (item.rp_v + 15) & ~15, g_v = item.small[2];
+      const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(item.h) * p.bias_len : nullptr;
+      const float far_bias = BIAS == kTable ? __ldg(table + p.bias_len - 1) : 0.f;
+      const float slope2 = BIAS == kAlibi ? __ldg(&p.heads[item.h].alibi_slope2) : 0.f;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < 2 * nt; ++j) {
+        const int half = j & 1, j0 = j * kHalf;
+        const bool diag = j >= 2 * nt - 2, near = BIAS == kTable && near_tile(p, i0, j0);
+        float base = BIAS == kTable && !near ? far_bias : BIAS == kAlibi ? slope2 * static_cast<float>(j0 - i) : 0.f;
+        const uint32_t tSh = tS + half * kHalf;
+        ok = (half || wait_all(&hdr->full[at.stage], at.phase, p.status)) && wait_all(&hdr->s_full[x][half], (done + (j >> 1)) & 1u, p.status);
+        if (!ok) break;
+        tc_fence_after();
+        const float4 scales = *reinterpret_cast<const float4*>(ring + at.stage * stage_bytes + p.tile_k + p.tile_v);
+        float c = x ? scales.y : scales.x;
+        // S of a tile with masked keys or distances of their own goes back scaled, biased and masked
+        if (diag || near) {
 #pragma unroll 1
-        for (int k = 0; k < kTile; k += 32) {
-          uint32_t r[32];
-          tmem_ld32(tS + k, r);
-          tmem_wait_ld_of(r);
+          for (int k = 0; k < kHalf; k += 32) {
+            uint32_t r[32];
+            tmem_ld32(tSh + k, r);
+            tmem_wait_ld_of(r);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            float y = __uint_as_float(r[e]) * c;
-            if (near) y += __ldg(table + min(max(i - j0 - k - e, 0), p.bias_len - 1));
-            if (BIAS == kAlibi) y += base + slope2 * static_cast<float>(k + e);
-            if (diag && k + e > row) y = -INFINITY;
-            r[e] = __float_as_uint(y);
+            for (int e = 0; e < 32; ++e) {
+              float y = __uint_as_float(r[e]) * c;
+              if (near) y += __ldg(table + min(max(i - j0 - k - e, 0), p.bias_len - 1));
+              if (BIAS == kAlibi) y += base + slope2 * static_cast<float>(k + e);
+              if (diag && half * kHalf + k + e > row) y = -INFINITY;
+              r[e] = __float_as_uint(y);
+            }
+            tmem_st16(tSh + k, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
+            tmem_st16(tSh + k + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
           }
-          tmem_st16(tS + k, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
-          tmem_st16(tS + k + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
+          tmem_wait_st();
+          c = 1.f;
+          base = 0.f;
         }
-        tmem_wait_st();
-        c = 1.f;
-        base = 0.f;
-      }
-      const bool slanted = BIAS == kAlibi && !diag;          // the bias grows along the keys
-      float top = -INFINITY;
-      {
+        const bool slanted = BIAS == kAlibi && !diag;        // the bias grows along the keys
+        uint32_t r[2][32];
+        tmem_ld32(tSh, r[0]);
+        tmem_ld32(tSh + 32, r[1]);
+        tmem_wait_ld_of(r[0]);
+        tmem_wait_ld_of(r[1]);
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-        for (int k = 0; k < kTile; k += 32) {
-          uint32_t r[32];
-          tmem_ld32(tS + k, r);
-          tmem_wait_ld_of(r);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
           if (slanted) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(fmaf(__uint_as_float(r[e]), c, slope2 * static_cast<float>(k + e)));
+            for (int e = 0; e < 32; ++e) r[k][e] = __float_as_uint(fmaf(__uint_as_float(r[k][e]), c, slope2 * static_cast<float>(32 * k + e)));
           }
 #pragma unroll
           for (int e = 0; e < 32; e += 8)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) mx[w] = max3(mx[w], __uint_as_float(r[e + 2 * w]), __uint_as_float(r[e + 2 * w + 1]));
+            for (int w = 0; w < 4; ++w) mx[w] = max3(mx[w], __uint_as_float(r[k][e + 2 * w]), __uint_as_float(r[k][e + 2 * w + 1]));
         }
-        top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        top = (slanted ? top : top * c) + base;              // (the scale is positive)
+        if (slanted) c = 1.f;
+        const float top = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), c, base);         // (the scale is positive)
+        const bool raise = top > m + 8.f;
+        const float now = raise ? top : m;
+        if (__any_sync(0xffffffffu, raise)) {
+          const float alpha = raise ? ex2(m - now) : 1.f;    // (0 at the first keys)
+          l *= alpha;
+          if (j > 0) {                                       // the half before has been added to o'
+            ok = wait_all(&hdr->p_used[x][half ^ 1], (done + ((j - 1) >> 1)) & 1u, p.status);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int k = 0; k < rv16; k += 16) {
+              uint32_t o[16];
+              tmem_ld16(tO + k, o);
+              tmem_wait_ld_of(o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+              tmem_st16(tO + k, o);
+            }
+          }
+          m = now;
+        }
+        const float add = m == -INFINITY ? 0.f : base - m + kForwardShift + scales.z;
+        float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            float y0, y1;
+            fma2(y0, y1, __uint_as_float(r[k][e]), __uint_as_float(r[k][e + 1]), c, add);
+            y0 = ex2(y0);
+            y1 = ex2(y1);
+            add2(sum0, sum1, y0, y1);
+            w[e / 2] = pack_f16(y0, y1);
+          }
+          tmem_st16(tSh + 16 * k, w);
+        }
+        l = fmaf(sum0 + sum1, scales.w, l);
+        tmem_wait_st();
+        tc_fence_before();
+        arrive_warp(&hdr->p_full[x][half], lane);
+        if (half) at.next(plan.stages);
       }
-      const bool raise = top > m + 8.f;
-      const float now = raise ? top : m;
-      if (__any_sync(0xffffffffu, raise)) {
-        const float alpha = raise ? ex2(m - now) : 1.f;      // (0 at the first tile)
-        l *= alpha;
-        if (j > 0) {                                         // (S(j) came behind the product that last added to o')
+      if (!ok) break;
+      for (int j = nt; j < most; ++j) at.next(plan.stages);
+      done += nt;
+      if (nt > 0) ok = wait_all(&hdr->acc_full[x], sums & 1u, p.status);
+      if (!ok) break;
+      tc_fence_after();
+      if (tile < p.tiles) {
+        const bool live = nt > 0 && i < n, there = i < p.T;
+        const float inv = live ? 1.f / l : 0.f, back = pow2(-g_v);
+        p.lse[static_cast<int64_t>(item.unit) * p.pad + i] = live ? kForwardShift - m - log2f(l) : -INFINITY;
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (static_cast<int64_t>(item.b) * p.T + i) * (static_cast<int64_t>(p.group) * p.lr_v_width) +
+                             p.group * __ldg(&p.heads[item.h].lr_v_off) + item.i * item.rp_v;
+        float* o32 = p.o + (static_cast<int64_t>(item.unit) * p.T + i) * p.o_stride;
+        if (nt == 0) {
+          if (there) zero_row(0, rv16, item.rp_v, out, plan.aligned & 1);
+        } else {
 #pragma unroll 1
           for (int k = 0; k < rv16; k += 16) {
             uint32_t o[16];
             tmem_ld16(tO + k, o);
             tmem_wait_ld_of(o);
+            float y[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-            tmem_st16(tO + k, o);
-          }
-        }
-        m = now;
-      }
-      const float add = m == -INFINITY ? 0.f : base - m + kForwardShift;
-      float sum0 = 0.f, sum1 = 0.f;
-      uint32_t r[32];
-      tmem_ld32(tS, r);
-      tmem_wait_ld_of(r);
-#pragma unroll 1
-      for (int k = 0; k < kTile; k += 32) {
-        float y[32];
+            for (int e = 0; e < 16; ++e) y[e] = live ? __uint_as_float(o[e]) * inv * back : 0.f;
+            if (there) {
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          if (slanted) {
-            y[e] = fmaf(__uint_as_float(r[e]), c, fmaf(slope2, static_cast<float>(k + e), add));
-            y[e + 1] = fmaf(__uint_as_float(r[e + 1]), c, fmaf(slope2, static_cast<float>(k + e + 1), add));
-          } else {
-            fma2(y[e], y[e + 1], __uint_as_float(r[e]), __uint_as_float(r[e + 1]), c, add);
-          }
-        }
-        if (k + 32 < kTile) tmem_ld32(tS + k + 32, r);
-        uint32_t w[16];
-#pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          float e0 = ex2(y[e]), e1 = ex2(y[e + 1]);
-          add2(sum0, sum1, e0, e1);
-          if (f != 1.f) { e0 *= f; e1 *= f; }
-          w[e / 2] = pack_f16(e0, e1);
-        }
-        tmem_wait_ld_of(r);                                      // (the columns behind are read before P reaches them)
-        tmem_st16(tS + k / 2, w);
-      }
-      l += sum0 + sum1;
-      tmem_wait_st();
-      tc_fence_before();
-      arrive_warp(&hdr->p_full[x], lane);
-    }
-    if (most > 0 && ok) ok = wait_all(&hdr->done, 0, p.status);
-    tc_fence_after();
-    if (ok && tile < p.tiles) {
-      const bool live = nt[x] > 0 && i < n;
-      const float inv = live ? 1.f / l : 0.f, back = pow2(-g_v);
-      p.lse[static_cast<int64_t>(unit) * p.pad + i] = live ? kForwardShift - m - log2f(l) : -INFINITY;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) +
-                           (static_cast<int64_t>(b) * p.T + i) * (static_cast<int64_t>(p.group) * p.lr_v_width) + p.group * hd.lr_v_off + ih * hd.rp_v;
-      float* o32 = p.o + (static_cast<int64_t>(unit) * p.T + i) * p.o_stride;
-      if (nt[x] == 0) {
-        if (i < p.T) zero_row(0, rv16, hd.rp_v, out, aligned);
-      } else {
-#pragma unroll 1
-        for (int k = 0; k < rv16; k += 16) {
-          uint32_t o[16];
-          tmem_ld16(tO + k, o);
-          tmem_wait_ld_of(o);
-          float y[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) y[e] = live ? __uint_as_float(o[e]) * inv * back : 0.f;
-          if (i < p.T) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              if (k + 8 * half >= hd.rp_v) continue;
-              store8(out + k + 8 * half, y + 8 * half, aligned);
-              *reinterpret_cast<float4*>(o32 + k + 8 * half) = make_float4(y[8 * half], y[8 * half + 1], y[8 * half + 2], y[8 * half + 3]);
-              *reinterpret_cast<float4*>(o32 + k + 8 * half + 4) = make_float4(y[8 * half + 4], y[8 * half + 5], y[8 * half + 6], y[8 * half + 7]);
+              for (int part = 0; part < 2; ++part) {
+                if (k + 8 * part >= item.rp_v) continue;
+                store8(out + k + 8 * part, y + 8 * part, plan.aligned & 1);
+                *reinterpret_cast<float4*>(o32 + k + 8 * part) = make_float4(y[8 * part], y[8 * part + 1], y[8 * part + 2], y[8 * part + 3]);
+                *reinterpret_cast<float4*>(o32 + k + 8 * part + 4) = make_float4(y[8 * part + 4], y[8 * part + 5], y[8 * part + 6], y[8 * part + 7]);
+              }
             }
           }
         }
       }
+      if (nt > 0) {
+        tc_fence_before();
+        arrive_warp(&hdr->acc_free[x], lane);
+        ++sums;
+      }
+      arrive_warp(&hdr->own_empty[set], lane);
     }
   }
   tc_fence_before();
@@ -423,253 +560,331 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const Trai
 
 // ---------------------------------------------------------------- dk', dv'
 
-// A CTA owns a tile of keys and walks the tiles of queries that see it, of every query head of the group.  Per pair of tiles:
+// An item is a tile of keys; it walks the tiles of queries that see it, of every query head of the group.  Per half:
 //   S^T = k' q'^T,  P^T = 2^(S^T - L);   dv' += P^T do';   G^T = v' do'^T,  dS^T = P^T (G^T - delta);   dk' += dS^T q'
-// A thread has a key row (one TMEM lane) and half of the tile's queries; L and delta lie along its columns and come with the
-// tile's ring stage.  While the softmax forms dS^T, the products run dv' and the next S^T; while it forms P^T, dk' and the next
-// G^T.  TMEM: S^T, G^T (P^T and dS^T in their place, a half in each half's first 32 columns), dv', dk'.
-// Bound by the two phases' chains: 1024 clocks of exponentials and some 500 of arithmetic a pair, 1280 of products at rank 80.
+// Each half has four softmax warps of its own; a thread has a key row (one TMEM lane).  L and delta lie along its columns and
+// come with the tile's ring stage.  One issuing warp has S^T, one dv', one G^T and dk'.
+// TMEM: S^T and G^T of both halves (dS^T in G^T's place), dv', dk'.  P^T has columns of its own where the ranks leave 64 of
+// them (their sum at most 192, each in steps of 32): the next S^T then starts when this one has been read.  Otherwise it takes
+// S^T's place.
 template <int BIAS>
-__global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainParams p, int stages, int aligned) {
+__global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainParams p, const Plan plan) {
   extern __shared__ __align__(1024) unsigned char smem[];
   TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int key_unit = blockIdx.x, h = key_unit / p.B, b = key_unit - h * p.B;
-  const HeadInfo hd = p.heads[h];
-  const int tile = blockIdx.y, j0 = tile * kTile;            // the first keys have the most queries
-  const int n = __ldg(p.lens + b);
-  const int rk16 = (hd.rp_k + 15) & ~15, rv16 = (hd.rp_v + 15) & ~15;
-  const int k_bytes = kTile * rk16 * 2, v_bytes = kTile * rv16 * 2, stage_bytes = k_bytes + v_bytes + 1024;
-  unsigned char* own = smem + kHeaderBytes;
-  unsigned char* ring = own + k_bytes + v_bytes;
-  const int per_head = (n + kTile - 1) / kTile - tile;       // tiles of queries of one head
-  const int total = per_head > 0 ? per_head * p.group : 0;
-
-  if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
-  if (tid == 0) {
-    for (int s = 0; s < kMaxRing; ++s) {
-      mbar_init(&hdr->full[s], 1);
-      mbar_init(&hdr->empty[s], 1);
-    }
-    mbar_init(&hdr->own, 1);
-    mbar_init(&hdr->s_full[0], 1);
-    mbar_init(&hdr->g_full, 1);
-    for (int x = 0; x < 2; ++x) mbar_init(&hdr->p_full[x], kSoftmaxWarps);      // P^T, dS^T
-    mbar_init(&hdr->done, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == kIssueWarp) {
-    const int v = smallest_of(p.v_exp + static_cast<int64_t>(key_unit) * p.tiles, p.tiles, lane);
-    int q = kTrainNoNumber, g = kTrainNoNumber;
-    for (int i = 0; i < p.group; ++i) {
-      const int64_t at = (static_cast<int64_t>(h * p.group + i) * p.B + b) * p.tiles;
-      q = smallest_of(p.q_exp + at, p.tiles, lane, q);
-      g = smallest_of(p.g_exp + at, p.tiles, lane, g);
-    }
-    if (lane == 0) {
-      hdr->smallest[0] = q;
-      hdr->smallest[2] = v;
-      hdr->smallest[3] = g;
-    }
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = hdr->tmem_base;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  unsigned char* own = smem + kHeaderBytes;                  // sets of a tile of k' and one of v'
+  unsigned char* ring = own + plan.sets * (p.tile_k + p.tile_v);
+  const int rows_at = p.tile_k + p.tile_v, stage_bytes = rows_at + 1024 + kScaleBytes;      // q', do', then L and delta
+  const bool apart = plan.apart != 0;
+  // TMEM columns of S^T, G^T, dv', dk', and of P^T
+  constexpr uint32_t cS = 0, cG = 128;
+  const uint32_t cP = apart ? 256 : cS, p_step = apart ? 32 : kHalf, cV = apart ? 320 : 256;
+  const uint32_t cK = cV + (apart ? (((p.max_rp_v + 15) & ~15) + 31) & ~31 : 128);
+  const uint32_t tmem = set_up(hdr, warp, tid, 2, 3 + kSoftmaxWarps, kSoftmaxWarps / 2, 2, kSoftmaxWarps);
 
   if (warp == kCopyWarp) {
-    if (lane == 0 && total > 0) {
-      const uint64_t keep = policy_evict_normal();
-      mbar_arrive_expect_tx(&hdr->own, k_bytes + v_bytes);
-      bulk_load(own, p.k_tiles + (static_cast<int64_t>(key_unit) * p.tiles + tile) * p.tile_k, k_bytes, &hdr->own, keep);
-      bulk_load(own + k_bytes, p.v_tiles + (static_cast<int64_t>(key_unit) * p.tiles + tile) * p.tile_v, v_bytes, &hdr->own, keep);
-      int g = 0;
-      bool ok = true;
-      for (int i = 0; i < p.group && ok; ++i) {
-        const int64_t unit = static_cast<int64_t>(h * p.group + i) * p.B + b;
-        for (int t = 0; t < per_head; ++t, ++g) {
-          const int st = g % stages;
-          if (g >= stages && !(ok = mbar_wait(&hdr->empty[st], (g / stages - 1) & 1u, p.status))) break;
-          unsigned char* to = ring + st * stage_bytes;
-          unsigned long long* full = &hdr->full[st];
-          const int64_t at = unit * p.tiles + tile + t;
-          mbar_arrive_expect_tx(full, stage_bytes);
-          bulk_load(to, p.q_tiles + at * p.tile_k, k_bytes, full, keep);
-          bulk_load(to + k_bytes, p.g_tiles + at * p.tile_v, v_bytes, full, keep);
-          bulk_load(to + k_bytes + v_bytes, p.lse + unit * p.pad + (tile + t) * kTile, 512, full, keep);
-          bulk_load(to + k_bytes + v_bytes + 512, p.delta + unit * p.pad + (tile + t) * kTile, 512, full, keep);
-        }
-      }
-      mbar_wait(&hdr->own, 0, p.status);
-      for (int s = 0; s < stages && s < g; ++s) mbar_wait(&hdr->full[s], ((g - 1 - s) / stages) & 1u, p.status);
-    }
-  } else if (warp == kIssueWarp) {
-    if (total > 0) {
-      const bool lead = elect_one();
-      const uint32_t idesc_k = instr_desc_f16(rk16) | kMnMajorB, idesc_v = instr_desc_f16(rv16) | kMnMajorB;
-      const uint64_t dk = smem_desc(smem_u32(own), 128, rk16 << 4), dv = smem_desc(smem_u32(own) + k_bytes, 128, rv16 << 4);
-      const uint64_t q_rank = smem_desc(smem_u32(ring), 128, rk16 << 4), g_rank = smem_desc(smem_u32(ring) + k_bytes, 128, rv16 << 4);
-      const uint64_t q_rows = smem_desc(smem_u32(ring), rk16 << 4, 128), g_rows = smem_desc(smem_u32(ring) + k_bytes, rv16 << 4, 128);
-      const uint64_t stage = stage_bytes >> 4;
-      const uint32_t tS = tmem, tG = tmem + 128, tV = tmem + 256, tK = tmem + 384;
-      bool ok = wait_all(&hdr->own, 0, p.status) && wait_all(&hdr->full[0], 0, p.status);
-      if (ok) {
-        tc_fence_after();
-        if (lead) {
-          issue_rank(rk16 >> 4, tS, dk, q_rank);
-          mma_commit(&hdr->s_full[0]);
-          issue_rank(rv16 >> 4, tG, dv, g_rank);
-          mma_commit(&hdr->g_full);
-        }
-        __syncwarp();
-      }
-      for (int g = 0; g < total && ok; ++g) {
-        const uint64_t at = static_cast<uint64_t>(g % stages) * stage, next = static_cast<uint64_t>((g + 1) % stages) * stage;
-        const bool more = g + 1 < total;
-        ok = wait_all(&hdr->p_full[0], g & 1u, p.status);
-        if (ok && more) ok = wait_all(&hdr->full[(g + 1) % stages], ((g + 1) / stages) & 1u, p.status);
-        if (!ok) break;
-        tc_fence_after();
-        if (lead) {
-          issue_rows(tV, tS, 64, g_rows + at, rv16 << 4, idesc_v, g > 0);
-          if (more) {
-            issue_rank(rk16 >> 4, tS, dk, q_rank + next);
-            mma_commit(&hdr->s_full[0]);
-          }
-        }
-        __syncwarp();
-        ok = wait_all(&hdr->p_full[1], g & 1u, p.status);
-        if (!ok) break;
-        tc_fence_after();
-        if (lead) {
-          issue_rows(tK, tG, 64, q_rows + at, rk16 << 4, idesc_k, g > 0);
-          mma_commit(&hdr->empty[g % stages]);
-          if (more) {
-            issue_rank(rv16 >> 4, tG, dv, g_rank + next);
-            mma_commit(&hdr->g_full);
-          }
-        }
-        __syncwarp();
-      }
-      if (lead) mma_commit(&hdr->done);
-      __syncwarp();
-      wait_all(&hdr->done, 0, p.status);
-    }
-  } else {
-    const int hf = warp >> 2, row = (warp & 3) * 32 + lane, key = j0 + row;
-    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t tS = tmem + lanes + hf * 64, tG = tmem + lanes + 128 + hf * 64;
-    const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
-    const float slope2 = BIAS == kAlibi ? hd.alibi_slope2 : 0.f;
-    const int g_q = hdr->smallest[0], g_v = hdr->smallest[2], g_g = hdr->smallest[3];
-    const int k_e = __ldg(p.k_exp + static_cast<int64_t>(key_unit) * p.tiles + tile), v_e = __ldg(p.v_exp + static_cast<int64_t>(key_unit) * p.tiles + tile);
+    const uint64_t keep = policy_evict_normal();
     bool ok = true;
-    int64_t exps = (static_cast<int64_t>(h * p.group) * p.B + b) * p.tiles + tile;
-    int t = 0;
-    for (int g = 0; g < total; ++g) {
-      const int st = g % stages, i0 = j0 + t * kTile;
-      const int q_e = __ldg(p.q_exp + exps + t), g_e = __ldg(p.g_exp + exps + t);
-      // P^T = 2^(S c + add - L), times 2^14 and the tile's share of do''s scale;  dS^T = P^T (G^T a - delta d), at most 2^15:
-      // |do' v'| and |delta| are below r 2^(16 - e - e'), e and e' the smallest exponents of do' and v'
-      const float c = p.scale_log2 * pow2(-q_e - k_e);
-      const int lift = kBackwardShift + g_g - g_e;
-      const int d_e = -9 + g_g + g_v + g_q - q_e - lift;
-      const float d = pow2(d_e), a = pow2(d_e - g_e - v_e);
-      const bool near = BIAS == kTable && near_tile(p, i0, j0);
-      float add = static_cast<float>(max(lift, -2000));
-      if (BIAS == kTable && !near) add += __ldg(table + p.bias_len - 1);
-      if (BIAS == kAlibi) add += slope2 * static_cast<float>(key - i0 - hf * 64);
-      if (++t == per_head) { t = 0; exps += static_cast<int64_t>(p.B) * p.tiles; }
-      ok = wait_all(&hdr->full[st], (g / stages) & 1u, p.status) && wait_all(&hdr->s_full[0], g & 1u, p.status);
+    Place at;
+    int issued = 0, it = 0;
+    for (;; ++it) {
+      const int set = set_of(plan, it);
+      if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
       if (!ok) break;
-      tc_fence_after();
-      const float* lse = reinterpret_cast<const float*>(ring + st * stage_bytes + k_bytes + v_bytes) + hf * 64;
-      const float* delta = lse + 128;
-      const bool diag = i0 == j0;
-      float e[64];
-#pragma unroll
-      for (int k = 0; k < 64; k += 32) {
-        uint32_t r[32];
-        tmem_ld32(tS + k, r);
-        tmem_wait_ld_of(r);
-#pragma unroll
-        for (int x = 0; x < 32; x += 4) {
-          const float4 ls = *reinterpret_cast<const float4*>(lse + k + x);
-          const float l4[4] = {ls.x, ls.y, ls.z, ls.w};
-#pragma unroll
-          for (int y = 0; y < 4; y += 2) {
-            float a0 = add, a1 = add;
-            if (BIAS == kAlibi) { a0 = fmaf(-slope2, static_cast<float>(k + x + y), add); a1 = fmaf(-slope2, static_cast<float>(k + x + y + 1), add); }
-            a0 += l4[y];
-            a1 += l4[y + 1];
-            e[k + x + y] = fmaf(__uint_as_float(r[x + y]), c, a0);
-            e[k + x + y + 1] = fmaf(__uint_as_float(r[x + y + 1]), c, a1);
+      Item* item = &hdr->item[set];
+      const int64_t index = list_index(it);
+      if (index >= plan.items) {
+        if (lane == 0) {
+          item->tiles[0] = -1;
+          mbar_arrive(&hdr->own_full[set]);
+        }
+        break;
+      }
+      int unit, tile;                                        // (the first keys have the most queries)
+      item_of(plan, static_cast<int>(index), unit, tile);
+      const int h = unit / p.B, b = unit - h * p.B;
+      const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
+      const int k_bytes = kTile * ((rp_k + 15) & ~15) * 2, v_bytes = kTile * ((rp_v + 15) & ~15) * 2;
+      const int per_head = max((n + kTile - 1) / kTile - tile, 0);                          // tiles of queries of one head
+      const int64_t own_at = static_cast<int64_t>(unit) * p.tiles + tile;
+      const int k_e = __ldg(p.k_exp + own_at), v_e = __ldg(p.v_exp + own_at);
+      const int g_v = smallest_of(p.v_exp + static_cast<int64_t>(unit) * p.tiles, p.tiles, lane);
+      int g_q = kTrainNoNumber, g_g = kTrainNoNumber;
+      for (int i = 0; i < p.group; ++i) {
+        const int64_t at_q = (static_cast<int64_t>(h * p.group + i) * p.B + b) * p.tiles;
+        g_q = smallest_of(p.q_exp + at_q, p.tiles, lane, g_q);
+        g_g = smallest_of(p.g_exp + at_q, p.tiles, lane, g_g);
+      }
+      if (lane == 0) {
+        item->unit = unit; item->h = h; item->b = b; item->i = 0;
+        item->tile = tile; item->n = n; item->rp_k = rp_k; item->rp_v = rp_v;
+        item->tiles[0] = per_head * p.group; item->tiles[1] = per_head;
+        item->small[0] = g_q; item->small[2] = g_v; item->small[3] = g_g;
+        unsigned char* to = own + set * (p.tile_k + p.tile_v);
+        if (per_head > 0) {
+          mbar_arrive_expect_tx(&hdr->own_full[set], k_bytes + v_bytes);
+          bulk_load(to, p.k_tiles + own_at * p.tile_k, k_bytes, &hdr->own_full[set], keep);
+          bulk_load(to + p.tile_k, p.v_tiles + own_at * p.tile_v, v_bytes, &hdr->own_full[set], keep);
+        } else {
+          mbar_arrive(&hdr->own_full[set]);
+        }
+        for (int i = 0; i < p.group && ok; ++i) {
+          const int64_t q_unit = static_cast<int64_t>(h * p.group + i) * p.B + b;
+          for (int t = 0; t < per_head; ++t, ++issued, at.next(plan.stages)) {
+            // P^T = 2^(S c + lift - L), times 2^14 and the tile's share of do''s scale;  dS^T = P^T (G^T a - delta d), at most
+            // 2^15: |do' v'| and |delta| are below r 2^(16 - e - e'), e and e' the smallest exponents of do' and v'
+            const int64_t from = q_unit * p.tiles + tile + t;
+            const int q_e = __ldg(p.q_exp + from), g_e = __ldg(p.g_exp + from);
+            const int lift = kBackwardShift + g_g - g_e, d_e = -9 + g_g + g_v + g_q - q_e - lift;
+            unsigned long long* full = &hdr->full[at.stage];
+            if (issued >= plan.stages && !(ok = mbar_wait(&hdr->empty[at.stage], at.phase ^ 1u, p.status))) break;
+            unsigned char* st = ring + at.stage * stage_bytes;
+            *reinterpret_cast<float4*>(st + rows_at + 1024) =
+                make_float4(p.scale_log2 * pow2(-q_e - k_e), static_cast<float>(lift), -pow2(d_e), pow2(d_e - g_e - v_e));
+            mbar_arrive_expect_tx(full, k_bytes + v_bytes + 1024);
+            bulk_load(st, p.q_tiles + from * p.tile_k, k_bytes, full, keep);
+            bulk_load(st + p.tile_k, p.g_tiles + from * p.tile_v, v_bytes, full, keep);
+            bulk_load(st + rows_at, p.lse + q_unit * p.pad + (tile + t) * kTile, 512, full, keep);
+            bulk_load(st + rows_at + 512, p.delta + q_unit * p.pad + (tile + t) * kTile, 512, full, keep);
           }
         }
       }
-      if (near) {
-#pragma unroll
-        for (int k = 0; k < 64; ++k) e[k] += __ldg(table + min(max(i0 + hf * 64 + k - key, 0), p.bias_len - 1));
-      }
-#pragma unroll
-      for (int k = 0; k < 64; ++k) e[k] = ex2(e[k]);
-      if (diag) {
-#pragma unroll
-        for (int k = 0; k < 64; ++k)
-          if (hf * 64 + k < row) e[k] = 0.f;
-      }
-#pragma unroll
-      for (int k = 0; k < 64; k += 32) {
-        uint32_t w[16];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) w[x] = pack_f16(e[k + 2 * x], e[k + 2 * x + 1]);
-        tmem_st16(tS + k / 2, w);
-      }
-      tmem_wait_st();
-      tc_fence_before();
-      arrive_warp(&hdr->p_full[0], lane);
-      ok = wait_all(&hdr->g_full, g & 1u, p.status);
-      if (!ok) break;
-      tc_fence_after();
-#pragma unroll
-      for (int k = 0; k < 64; k += 32) {
-        uint32_t r[32], w[16];
-        tmem_ld32(tG + k, r);
-        tmem_wait_ld_of(r);
-#pragma unroll
-        for (int x = 0; x < 32; x += 4) {
-          const float4 dl = *reinterpret_cast<const float4*>(delta + k + x);
-          const float d4[4] = {dl.x, dl.y, dl.z, dl.w};
-#pragma unroll
-          for (int y = 0; y < 4; y += 2) {
-            const float x0 = e[k + x + y] * fmaf(__uint_as_float(r[x + y]), a, -d * d4[y]);
-            const float x1 = e[k + x + y + 1] * fmaf(__uint_as_float(r[x + y + 1]), a, -d * d4[y + 1]);
-            w[(x + y) / 2] = pack_f16(x0, x1);
-          }
-        }
-        tmem_st16(tG + k / 2, w);
-      }
-      tmem_wait_st();
-      tc_fence_before();
-      arrive_warp(&hdr->p_full[1], lane);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) { ++it; break; }
     }
-    if (total > 0 && ok) ok = wait_all(&hdr->done, 0, p.status);
-    tc_fence_after();
-    if (ok) {
-      const bool in_range = key < p.T, live = key < n;
-      const int k_split = ((rk16 >> 4) + 1) / 2 * 16, v_split = ((rv16 >> 4) + 1) / 2 * 16;
-      const int k_lo = hf ? k_split : 0, k_hi = hf ? rk16 : k_split, v_lo = hf ? v_split : 0, v_hi = hf ? rv16 : v_split;
-      __nv_bfloat16* to_k = static_cast<__nv_bfloat16*>(p.dk) + (static_cast<int64_t>(b) * p.T + key) * p.lr_k_width + hd.lr_k_off;
-      __nv_bfloat16* to_v = static_cast<__nv_bfloat16*>(p.dv) + (static_cast<int64_t>(b) * p.T + key) * p.lr_v_width + hd.lr_v_off;
-      if (total == 0) {
-        if (in_range) {
-          zero_row(k_lo, k_hi, hd.rp_k, to_k, aligned & 1);
-          zero_row(v_lo, v_hi, hd.rp_v, to_v, aligned & 2);
+    if (!ok && lane == 0) drain_copies(hdr, plan, it, issued, p.status);
+  } else if (warp >= kIssueWarp) {
+    const int role = warp - kIssueWarp;                      // S^T; dv'; G^T and dk'
+    const bool lead = elect_one();
+    const uint64_t stage = stage_bytes >> 4;
+    bool ok = true;
+    int done = 0, sums = 0;                                  // tiles and items behind this warp
+    Place at, next;
+    for (int it = 0; ok; ++it) {
+      const int set = set_of(plan, it);
+      ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
+      if (!ok || hdr->item[set].tiles[0] < 0) break;
+      const int total = hdr->item[set].tiles[0];
+      const int rk16 = (hdr->item[set].rp_k + 15) & ~15, rv16 = (hdr->item[set].rp_v + 15) & ~15;
+      const uint32_t own_at = smem_u32(own) + set * (p.tile_k + p.tile_v), ring_at = smem_u32(ring);
+      if (role == 0) {
+        const uint64_t dk = smem_desc(own_at, 128, rk16 << 4), q_rank = smem_desc(ring_at, 128, rk16 << 4);
+        for (int g = 0; g < 2 * total && ok; ++g) {
+          const int half = g & 1, behind = done + (g >> 1);  // tiles before this one
+          if (!half) ok = wait_all(&hdr->full[at.stage], at.phase, p.status);
+          // the buffer is free when its S^T has been read, or the P^T in its place taken in
+          if (ok && behind > 0) ok = wait_all(apart ? &hdr->s_read[half] : &hdr->p_used[0][half], (behind - 1) & 1u, p.status);
+          if (!ok) break;
+          tc_fence_after();
+          if (lead) {
+            issue_rank(rk16 >> 4, tmem + cS + half * kHalf, dk, q_rank + stage * at.stage + half_of(half, rk16 << 4));
+            mma_commit(&hdr->s_full[0][half]);
+          }
+          __syncwarp();
+          if (half) at.next(plan.stages);
         }
+      } else if (role == 1) {
+        const uint32_t idesc = instr_desc_f16(rv16) | kMnMajorB;
+        const uint64_t g_rows = smem_desc(ring_at + p.tile_k, rv16 << 4, 128);
+        if (total > 0 && sums > 0) ok = wait_all(&hdr->acc_free[0], (sums - 1) & 1u, p.status);
+        for (int g = 0; g < 2 * total && ok; ++g) {
+          const int half = g & 1;
+          if (!half) ok = wait_all(&hdr->full[at.stage], at.phase, p.status);
+          if (ok) ok = wait_all(&hdr->p_full[0][half], (done + (g >> 1)) & 1u, p.status);
+          if (!ok) break;
+          tc_fence_after();
+          if (lead) {
+            issue_rows(tmem + cV, tmem + cP + half * p_step, g_rows + stage * at.stage + half_of(half, rv16 << 4), rv16 << 4, idesc, g > 0);
+            mma_commit(&hdr->p_used[0][half]);
+            if (half) mma_commit(&hdr->empty[at.stage]);
+          }
+          __syncwarp();
+          if (half) at.next(plan.stages);
+        }
+        if (ok && lead && total > 0) mma_commit(&hdr->acc_full[0]);
+        __syncwarp();
       } else {
-        store_row(tmem + lanes + 384, k_lo, k_hi, hd.rp_k, p.scale * pow2(9 - g_g - g_v - g_q), to_k, in_range, live, aligned & 1);
-        store_row(tmem + lanes + 256, v_lo, v_hi, hd.rp_v, pow2(-kBackwardShift - g_g), to_v, in_range, live, aligned & 2);
+        const uint32_t idesc = instr_desc_f16(rk16) | kMnMajorB;
+        const uint64_t dv = smem_desc(own_at + p.tile_k, 128, rv16 << 4), g_rank = smem_desc(ring_at + p.tile_k, 128, rv16 << 4);
+        const uint64_t q_rows = smem_desc(ring_at, rk16 << 4, 128);
+        for (int g = 0; total > 0 && g < 2 * total + 2 && ok; ++g) {
+          const int half = g & 1;
+          if (g >= 2) {
+            if (g == 2 && sums > 0) ok = wait_all(&hdr->acc_free[0], (sums - 1) & 1u, p.status);
+            if (ok) ok = wait_all(&hdr->p_full[1][half], (done + ((g - 2) >> 1)) & 1u, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            if (lead) {
+              issue_rows(tmem + cK, tmem + cG + half * kHalf, q_rows + stage * at.stage + half_of(half, rk16 << 4), rk16 << 4, idesc, g > 2);
+              if (half) mma_commit(&hdr->empty[at.stage]);
+            }
+            __syncwarp();
+            if (half) at.next(plan.stages);
+          }
+          if (g < 2 * total) {                               // (in dS^T's place: behind the product that takes it)
+            if (!half) ok = wait_all(&hdr->full[next.stage], next.phase, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            if (lead) {
+              issue_rank(rv16 >> 4, tmem + cG + half * kHalf, dv, g_rank + stage * next.stage + half_of(half, rv16 << 4));
+              mma_commit(&hdr->g_full[half]);
+            }
+            __syncwarp();
+            if (half) next.next(plan.stages);
+          }
+        }
+        if (ok && lead && total > 0) mma_commit(&hdr->acc_full[0]);
+        __syncwarp();
       }
+      if (ok && lead) mma_commit(&hdr->own_empty[set]);
+      __syncwarp();
+      done += total;
+      sums += total > 0;
+    }
+    drain(hdr, role, lead, p.status);
+  } else {
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + lanes + cS + half * kHalf, tG = tmem + lanes + cG + half * kHalf, tP = tmem + lanes + cP + half * p_step;
+    bool ok = true;
+    int done = 0, sums = 0;
+    Place at;
+    for (int it = 0; ok; ++it) {
+      const int set = set_of(plan, it);
+      ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
+      if (!ok) break;
+      const int total = hdr->item[set].tiles[0], per_head = hdr->item[set].tiles[1], h = hdr->item[set].h;
+      if (total < 0) break;
+      const int j0 = hdr->item[set].tile * kTile, key = j0 + row;
+      const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
+      const float far_bias = BIAS == kTable ? __ldg(table + p.bias_len - 1) : 0.f;
+      const float slope2 = BIAS == kAlibi ? __ldg(&p.heads[h].alibi_slope2) : 0.f;
+      int t = 0;
+      for (int g = 0; g < total; ++g) {
+        const uint32_t phase = (done + g) & 1u;
+        const int i0 = j0 + t * kTile + half * kHalf;
+        const bool near = BIAS == kTable && near_tile(p, i0, j0), diag = t == 0;
+        if (++t == per_head) t = 0;
+        float add = BIAS == kAlibi ? slope2 * static_cast<float>(key - i0) : 0.f;
+        if (BIAS == kTable && !near) add = far_bias;
+        ok = wait_all(&hdr->full[at.stage], at.phase, p.status) && wait_all(&hdr->s_full[0][half], phase, p.status);
+        if (!ok) break;
+        tc_fence_after();
+        const float* lse = reinterpret_cast<const float*>(ring + at.stage * stage_bytes + rows_at) + half * kHalf;
+        const float4 scales = *reinterpret_cast<const float4*>(ring + at.stage * stage_bytes + rows_at + 1024);
+        float c = scales.x;
+        uint32_t r[2][32];
+        // S of a tile with masked queries or distances of their own goes back scaled, biased and masked
+        if (diag || near) {
+#pragma unroll 1
+          for (int k0 = 0; k0 < kHalf; k0 += 32) {
+            tmem_ld32(tS + k0, r[0]);
+            tmem_wait_ld_of(r[0]);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              float y = __uint_as_float(r[0][k]) * c;
+              if (near) y += __ldg(table + min(max(i0 + k0 + k - key, 0), p.bias_len - 1));
+              if (diag && half * kHalf + k0 + k < row) y = -INFINITY;
+              r[0][k] = __float_as_uint(y);
+            }
+            tmem_st16(tS + k0, *reinterpret_cast<uint32_t(*)[16]>(&r[0][0]));
+            tmem_st16(tS + k0 + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[0][16]));
+          }
+          tmem_wait_st();
+          c = 1.f;
+        }
+        tmem_ld32(tS, r[0]);
+        tmem_ld32(tS + 32, r[1]);
+        unsigned long long e[32];                            // pairs of queries
+        const unsigned long long add_2 = both(add + scales.y), c_2 = both(c);
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+          const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(lse + 2 * k);
+          if (BIAS == kAlibi) {
+            e[k] = add2p(l.x, fma2p(both(-slope2), pack2(2 * k, 2 * k + 1), add_2));
+            e[k + 1] = add2p(l.y, fma2p(both(-slope2), pack2(2 * k + 2, 2 * k + 3), add_2));
+          } else {
+            e[k] = add2p(l.x, add_2);
+            e[k + 1] = add2p(l.y, add_2);
+          }
+        }
+        tmem_wait_ld_of(r[0]);
+        tmem_wait_ld_of(r[1]);
+        tc_fence_before();
+        arrive_warp(&hdr->s_read[half], lane);
+        uint32_t w[2][16];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          float x, y;
+          unpack2(fma2p(pair_at(r[k >> 4], k & 15), c_2, e[k]), x, y);
+          x = ex2(x);
+          y = ex2(y);
+          w[k >> 4][k & 15] = pack_f16(x, y);
+          e[k] = pack2(x, y);
+        }
+        if (apart && done + g > 0) {                         // dv' has taken in the P^T of the tile before
+          ok = wait_all(&hdr->p_used[0][half], phase ^ 1u, p.status);
+          if (!ok) break;
+          tc_fence_after();
+        }
+        tmem_st16(tP, w[0]);
+        tmem_st16(tP + 16, w[1]);
+        tmem_wait_st();
+        tc_fence_before();
+        arrive_warp(&hdr->p_full[0][half], lane);
+        ok = wait_all(&hdr->g_full[half], phase, p.status);
+        if (!ok) break;
+        tc_fence_after();
+        tmem_ld32(tG, r[0]);
+        tmem_ld32(tG + 32, r[1]);
+        tmem_wait_ld_of(r[0]);
+        tmem_wait_ld_of(r[1]);
+        const unsigned long long d = both(scales.z), a = both(scales.w);
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+          const ulonglong2 dl = *reinterpret_cast<const ulonglong2*>(lse + 128 + 2 * k);
+          float x, y;
+          unpack2(mul2p(e[k], fma2p(pair_at(r[k >> 4], k & 15), a, mul2p(dl.x, d))), x, y);
+          w[k >> 4][k & 15] = pack_f16(x, y);
+          unpack2(mul2p(e[k + 1], fma2p(pair_at(r[k >> 4], (k & 15) + 1), a, mul2p(dl.y, d))), x, y);
+          w[k >> 4][(k & 15) + 1] = pack_f16(x, y);
+        }
+        tmem_st16(tG, w[0]);
+        tmem_st16(tG + 16, w[1]);
+        tmem_wait_st();
+        tc_fence_before();
+        arrive_warp(&hdr->p_full[1][half], lane);
+        at.next(plan.stages);
+      }
+      if (!ok) break;
+      done += total;
+      if (total > 0) ok = wait_all(&hdr->acc_full[0], sums & 1u, p.status);
+      if (!ok) break;
+      tc_fence_after();
+      {
+        // a half's warps have half of the columns of their rows
+        const Item item = hdr->item[set];
+        const bool there = key < p.T, live = key < item.n;
+        const int rk16 = (item.rp_k + 15) & ~15, rv16 = (item.rp_v + 15) & ~15;
+        const int k_split = ((rk16 >> 4) + 1) / 2 * 16, v_split = ((rv16 >> 4) + 1) / 2 * 16;
+        const int k_lo = half ? k_split : 0, k_hi = half ? rk16 : k_split, v_lo = half ? v_split : 0, v_hi = half ? rv16 : v_split;
+        const int64_t at_row = static_cast<int64_t>(item.b) * p.T + key;
+        __nv_bfloat16* to_k = static_cast<__nv_bfloat16*>(p.dk) + at_row * p.lr_k_width + __ldg(&p.heads[h].lr_k_off);
+        __nv_bfloat16* to_v = static_cast<__nv_bfloat16*>(p.dv) + at_row * p.lr_v_width + __ldg(&p.heads[h].lr_v_off);
+        if (total == 0) {
+          if (there) {
+            zero_row(k_lo, k_hi, item.rp_k, to_k, plan.aligned & 1);
+            zero_row(v_lo, v_hi, item.rp_v, to_v, plan.aligned & 2);
+          }
+        } else {
+          store_row(tmem + lanes + cK, k_lo, k_hi, item.rp_k, p.scale * pow2(9 - item.small[3] - item.small[2] - item.small[0]), to_k, there, live, plan.aligned & 1);
+          store_row(tmem + lanes + cV, v_lo, v_hi, item.rp_v, pow2(-kBackwardShift - item.small[3]), to_v, there, live, plan.aligned & 2);
+          tc_fence_before();
+          arrive_warp(&hdr->acc_free[0], lane);
+          ++sums;
+        }
+      }
+      arrive_warp(&hdr->own_empty[set], lane);
     }
   }
   tc_fence_before();
@@ -679,302 +894,337 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
 
 // ---------------------------------------------------------------- dq'
 
-// A CTA owns a tile of queries and walks the tiles of keys that it sees: S = q' k'^T, G = do' v'^T, dS = P (G - delta),
-// dq' += dS k'.  A thread has a query row and half of the tile's keys.  S has two buffers, so that the softmax finds the next
-// scores when it has done a tile; dS takes the place of S, and G is free again as soon as it has been read.
-// TMEM: S[2], G, dq'.  Bound by the softmax warps: 1024 clocks of exponentials and some 500 of arithmetic a pair.
+// An item is a tile of queries; it walks the tiles of keys that it sees: S = q' k'^T, G = do' v'^T, dS = P (G - delta),
+// dq' += dS k'.  Each half tile of keys has four softmax warps of its own; a thread has a query row.  dS takes the place of S,
+// which has two buffers for each half, so that the next S is there when dS is done; G is free again as soon as it has been read.
+// One issuing warp has S, one dq', one G.  TMEM: S (four buffers) and G of both halves, dq'.
 // The gradient of a learned bias is a sum over dS of equal distance: over diagonals.  Far tiles, whose distances share the last
 // bucket, are added up whole; in the others a sum moves one lane up with every column, so that it follows its diagonal, and
 // leaves the warp complete.  All of it in a fixed order, without atomics.
 template <int BIAS>
-__global__ void __launch_bounds__(kTrThreads, 1) train_dq_kernel(const TrainParams p, int stages, int aligned) {
+__global__ void __launch_bounds__(kTrThreads, 1) train_dq_kernel(const TrainParams p, const Plan plan) {
   extern __shared__ __align__(1024) unsigned char smem[];
   TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int unit = blockIdx.x, hq = unit / p.B, b = unit - hq * p.B, h = hq / p.group, ih = hq - h * p.group;
-  const int key_unit = h * p.B + b;
-  const HeadInfo hd = p.heads[h];
-  const int tile = gridDim.y - 1 - blockIdx.y, i0 = tile * kTile;
-  const int n = __ldg(p.lens + b);
-  const int rk16 = (hd.rp_k + 15) & ~15, rv16 = (hd.rp_v + 15) & ~15;
-  const int k_bytes = kTile * rk16 * 2, v_bytes = kTile * rv16 * 2, stage_bytes = k_bytes + v_bytes;
-  unsigned char* own = smem + kHeaderBytes;
-  unsigned char* ring = own + k_bytes + v_bytes;
-  float* diagonals = reinterpret_cast<float*>(ring + stages * stage_bytes);      // [softmax warps][96], then [warps][buckets]
-  const int nt = i0 < n ? tile + 1 : 0;
-
-  if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
-  if (tid == 0) {
-    for (int s = 0; s < kMaxRing; ++s) {
-      mbar_init(&hdr->full[s], 1);
-      mbar_init(&hdr->empty[s], 1);
-    }
-    mbar_init(&hdr->own, 1);
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(&hdr->s_full[x], 1);
-      mbar_init(&hdr->p_full[x], kSoftmaxWarps);             // dS in S's buffer
-    }
-    mbar_init(&hdr->g_full, 1);
-    mbar_init(&hdr->g_read, kSoftmaxWarps);
-    mbar_init(&hdr->done, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == kIssueWarp) {
-    const int k = smallest_of(p.k_exp + static_cast<int64_t>(key_unit) * p.tiles, p.tiles, lane);
-    const int v = smallest_of(p.v_exp + static_cast<int64_t>(key_unit) * p.tiles, p.tiles, lane);
-    if (lane == 0) {
-      hdr->smallest[1] = k;
-      hdr->smallest[2] = v;
-    }
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = hdr->tmem_base;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  unsigned char* own = smem + kHeaderBytes;                  // sets of a tile of q' and one of do'
+  unsigned char* ring = own + plan.sets * (p.tile_k + p.tile_v);
+  const int scales_at = p.tile_k + p.tile_v, stage_bytes = scales_at + kScaleBytes;
+  float* diagonals = reinterpret_cast<float*>(ring + plan.stages * stage_bytes);           // [softmax warps][96]
+  constexpr uint32_t cS = 0, cG = 256, cQ = 384;             // TMEM columns of S ([half][tile & 1]), G ([half]), dq'
+  const uint32_t tmem = set_up(hdr, warp, tid, 2, 3 + kSoftmaxWarps, kSoftmaxWarps / 2, 1, kSoftmaxWarps);
 
   if (warp == kCopyWarp) {
-    if (lane == 0 && nt > 0) {
-      const uint64_t keep = policy_evict_normal();
-      const int64_t at = static_cast<int64_t>(unit) * p.tiles + tile, keys = static_cast<int64_t>(key_unit) * p.tiles;
-      mbar_arrive_expect_tx(&hdr->own, k_bytes + v_bytes);
-      bulk_load(own, p.q_tiles + at * p.tile_k, k_bytes, &hdr->own, keep);
-      bulk_load(own + k_bytes, p.g_tiles + at * p.tile_v, v_bytes, &hdr->own, keep);
-      int issued = 0;
-      for (int j = 0; j < nt; ++j, ++issued) {
-        const int st = j % stages;
-        if (j >= stages && !mbar_wait(&hdr->empty[st], (j / stages - 1) & 1u, p.status)) break;
-        unsigned char* to = ring + st * stage_bytes;
-        mbar_arrive_expect_tx(&hdr->full[st], stage_bytes);
-        bulk_load(to, p.k_tiles + (keys + j) * p.tile_k, k_bytes, &hdr->full[st], keep);
-        bulk_load(to + k_bytes, p.v_tiles + (keys + j) * p.tile_v, v_bytes, &hdr->full[st], keep);
+    const uint64_t keep = policy_evict_normal();
+    bool ok = true;
+    Place at;
+    int issued = 0, it = 0;
+    for (;; ++it) {
+      const int set = set_of(plan, it);
+      if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
+      if (!ok) break;
+      Item* item = &hdr->item[set];
+      const int64_t index = list_index(it);
+      if (index >= plan.items) {
+        if (lane == 0) {
+          item->tiles[0] = -1;
+          mbar_arrive(&hdr->own_full[set]);
+        }
+        break;
       }
-      mbar_wait(&hdr->own, 0, p.status);
-      for (int s = 0; s < stages && s < issued; ++s) mbar_wait(&hdr->full[s], ((issued - 1 - s) / stages) & 1u, p.status);
+      int unit, slot;
+      item_of(plan, static_cast<int>(index), unit, slot);
+      const int tile = p.tiles - 1 - slot;
+      const int hq = unit / p.B, b = unit - hq * p.B, h = hq / p.group, key_unit = h * p.B + b;
+      const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
+      const int k_bytes = kTile * ((rp_k + 15) & ~15) * 2, v_bytes = kTile * ((rp_v + 15) & ~15) * 2;
+      const int nt = tile * kTile < n ? tile + 1 : 0;
+      const int64_t own_at = static_cast<int64_t>(unit) * p.tiles + tile, keys = static_cast<int64_t>(key_unit) * p.tiles;
+      const int q_e = __ldg(p.q_exp + own_at), g_e = __ldg(p.g_exp + own_at);
+      const int g_k = smallest_of(p.k_exp + keys, p.tiles, lane), g_v = smallest_of(p.v_exp + keys, p.tiles, lane);
+      if (lane == 0) {
+        item->unit = unit; item->h = h; item->b = b; item->i = hq - h * p.group;
+        item->tile = tile; item->n = n; item->rp_k = rp_k; item->rp_v = rp_v;
+        item->tiles[0] = nt;
+        item->small[1] = g_k; item->small[2] = g_v; item->small[3] = g_e;
+        unsigned char* to = own + set * (p.tile_k + p.tile_v);
+        if (nt > 0) {
+          mbar_arrive_expect_tx(&hdr->own_full[set], k_bytes + v_bytes);
+          bulk_load(to, p.q_tiles + own_at * p.tile_k, k_bytes, &hdr->own_full[set], keep);
+          bulk_load(to + p.tile_k, p.g_tiles + own_at * p.tile_v, v_bytes, &hdr->own_full[set], keep);
+        } else {
+          mbar_arrive(&hdr->own_full[set]);
+        }
+        for (int j = 0; j < nt; ++j, ++issued, at.next(plan.stages)) {
+          // P = 2^(S c - L);  dS = P (G a - delta d), at most 2^15 (as above), times the tile's share of the scale of k'
+          const int k_e = __ldg(p.k_exp + keys + j), v_e = __ldg(p.v_exp + keys + j), d_e = -9 + g_e + g_v + g_k - k_e;
+          unsigned long long* full = &hdr->full[at.stage];
+          if (issued >= plan.stages && !(ok = mbar_wait(&hdr->empty[at.stage], at.phase ^ 1u, p.status))) break;
+          unsigned char* st = ring + at.stage * stage_bytes;
+          *reinterpret_cast<float4*>(st + scales_at) =
+              make_float4(p.scale_log2 * pow2(-q_e - k_e), pow2(d_e), pow2(d_e - g_e - v_e), pow2(-d_e));
+          mbar_arrive_expect_tx(full, k_bytes + v_bytes);
+          bulk_load(st, p.k_tiles + (keys + j) * p.tile_k, k_bytes, full, keep);
+          bulk_load(st + p.tile_k, p.v_tiles + (keys + j) * p.tile_v, v_bytes, full, keep);
+        }
+      }
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) { ++it; break; }
     }
-  } else if (warp == kIssueWarp) {
-    if (nt > 0) {
-      const bool lead = elect_one();
+    if (!ok && lane == 0) drain_copies(hdr, plan, it, issued, p.status);
+  } else if (warp >= kIssueWarp) {
+    const int role = warp - kIssueWarp;                      // S; dq'; G
+    const bool lead = elect_one();
+    const uint64_t stage = stage_bytes >> 4;
+    bool ok = true;
+    int done = 0, sums = 0;                                  // tiles and items behind this warp
+    Place at;
+    for (int it = 0; ok; ++it) {
+      const int set = set_of(plan, it);
+      ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
+      if (!ok || hdr->item[set].tiles[0] < 0) break;
+      const int nt = hdr->item[set].tiles[0];
+      const int rk16 = (hdr->item[set].rp_k + 15) & ~15, rv16 = (hdr->item[set].rp_v + 15) & ~15;
+      const uint32_t own_at = smem_u32(own) + set * (p.tile_k + p.tile_v), ring_at = smem_u32(ring);
+      const uint64_t dq = smem_desc(own_at, 128, rk16 << 4), dg = smem_desc(own_at + p.tile_k, 128, rv16 << 4);
+      const uint64_t k_rank = smem_desc(ring_at, 128, rk16 << 4), v_rank = smem_desc(ring_at + p.tile_k, 128, rv16 << 4);
+      const uint64_t k_rows = smem_desc(ring_at, rk16 << 4, 128);
       const uint32_t idesc = instr_desc_f16(rk16) | kMnMajorB;
-      const uint64_t dq = smem_desc(smem_u32(own), 128, rk16 << 4), dg = smem_desc(smem_u32(own) + k_bytes, 128, rv16 << 4);
-      const uint64_t k_rank = smem_desc(smem_u32(ring), 128, rk16 << 4), v_rank = smem_desc(smem_u32(ring) + k_bytes, 128, rv16 << 4);
-      const uint64_t k_rows = smem_desc(smem_u32(ring), rk16 << 4, 128);
-      const uint64_t stage = stage_bytes >> 4;
-      const uint32_t tG = tmem + 256, tQ = tmem + 384;
-      bool ok = wait_all(&hdr->own, 0, p.status);
-      // S(j) into buffer j & 1 and, for the first tile, G(0)
-      auto score = [&](int j) {
-        ok = wait_all(&hdr->full[j % stages], (j / stages) & 1u, p.status);
-        if (!ok) return;
-        tc_fence_after();
-        if (lead) {
-          issue_rank(rk16 >> 4, tmem + (j & 1) * kTile, dq, k_rank + static_cast<uint64_t>(j % stages) * stage);
-          mma_commit(&hdr->s_full[j & 1]);
-        }
-        __syncwarp();
-      };
-      auto second = [&](int j) {
-        if (lead) {
-          issue_rank(rv16 >> 4, tG, dg, v_rank + static_cast<uint64_t>(j % stages) * stage);
-          mma_commit(&hdr->g_full);
-        }
-        __syncwarp();
-      };
-      if (ok) score(0);
-      if (ok) second(0);
-      if (ok && nt > 1) score(1);
-      for (int j = 0; j < nt && ok; ++j) {
-        if (j + 1 < nt) {                                    // G(j) has been read: G(j + 1)
-          ok = wait_all(&hdr->g_read, j & 1u, p.status);
+      if (role == 1 && nt > 0 && sums > 0) ok = wait_all(&hdr->acc_free[0], (sums - 1) & 1u, p.status);
+      for (int j = 0; j < 2 * nt && ok; ++j) {
+        const int half = j & 1, behind = done + (j >> 1), buf = behind & 1;                // tiles before this one; buffer of S
+        const uint32_t tS = tmem + cS + half * 128 + buf * kHalf;
+        if (!half) ok = wait_all(&hdr->full[at.stage], at.phase, p.status);
+        if (role == 0) {
+          if (ok && behind >= 2) ok = wait_all(&hdr->p_used[buf][half], ((behind - 2) >> 1) & 1u, p.status);     // dS taken in
           if (!ok) break;
           tc_fence_after();
-          second(j + 1);
-        }
-        ok = wait_all(&hdr->p_full[j & 1], (j >> 1) & 1u, p.status);
-        if (!ok) break;
-        tc_fence_after();
-        if (lead) {
-          issue_rows(tQ, tmem + (j & 1) * kTile, 64, k_rows + static_cast<uint64_t>(j % stages) * stage, rk16 << 4, idesc, j > 0);
-          mma_commit(&hdr->empty[j % stages]);
+          if (lead) {
+            issue_rank(rk16 >> 4, tS, dq, k_rank + stage * at.stage + half_of(half, rk16 << 4));
+            mma_commit(&hdr->s_full[buf][half]);
+          }
+        } else if (role == 1) {
+          if (ok) ok = wait_all(&hdr->p_full[buf][half], (behind >> 1) & 1u, p.status);
+          if (!ok) break;
+          tc_fence_after();
+          if (lead) {
+            issue_rows(tmem + cQ, tS, k_rows + stage * at.stage + half_of(half, rk16 << 4), rk16 << 4, idesc, j > 0);
+            mma_commit(&hdr->p_used[buf][half]);
+            if (half) mma_commit(&hdr->empty[at.stage]);
+          }
+        } else {
+          if (ok && behind > 0) ok = wait_all(&hdr->g_read[half], (behind - 1) & 1u, p.status);
+          if (!ok) break;
+          tc_fence_after();
+          if (lead) {
+            issue_rank(rv16 >> 4, tmem + cG + half * kHalf, dg, v_rank + stage * at.stage + half_of(half, rv16 << 4));
+            mma_commit(&hdr->g_full[half]);
+            if (half) mma_commit(&hdr->empty[at.stage]);
+          }
         }
         __syncwarp();
-        if (j + 2 < nt) score(j + 2);
+        if (half) at.next(plan.stages);
       }
-      if (lead) mma_commit(&hdr->done);
+      if (ok && lead) {
+        if (role == 1 && nt > 0) mma_commit(&hdr->acc_full[0]);
+        mma_commit(&hdr->own_empty[set]);
+      }
       __syncwarp();
-      wait_all(&hdr->done, 0, p.status);
+      done += nt;
+      sums += nt > 0;
     }
+    drain(hdr, role, lead, p.status);
   } else {
-    const int hf = warp >> 2, row = (warp & 3) * 32 + lane, i = i0 + row;
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t tG = tmem + lanes + 256 + hf * 64;
-    const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
-    const float slope2 = BIAS == kAlibi ? hd.alibi_slope2 : 0.f;
-    const int g_k = hdr->smallest[1], g_v = hdr->smallest[2];
-    const int64_t keys = static_cast<int64_t>(key_unit) * p.tiles;
-    const int64_t stat = static_cast<int64_t>(unit) * p.pad + i;
-    const float lse = nt > 0 ? __ldg(p.lse + stat) : 0.f, delta = nt > 0 ? __ldg(p.delta + stat) : 0.f;
-    const int q_e = nt > 0 ? __ldg(p.q_exp + static_cast<int64_t>(unit) * p.tiles + tile) : 0;
-    const int g_e = nt > 0 ? __ldg(p.g_exp + static_cast<int64_t>(unit) * p.tiles + tile) : 0;
-    const bool sums = BIAS == kTable && p.dtable != nullptr;
+    const uint32_t tG = tmem + lanes + cG + half * kHalf;
+    const bool want = BIAS == kTable && p.dtable != nullptr;
     float* my_diagonals = diagonals + warp * 96;
-    float far_sum = 0.f;                                     // dS of far tiles, this thread's
-    float by_bucket[8] = {};                                 // buckets lane, lane + 32, ...: this warp's
     bool ok = true;
-    for (int j = 0; j < nt; ++j) {
-      const int j0 = j * kTile;
-      const int k_e = __ldg(p.k_exp + keys + j), v_e = __ldg(p.v_exp + keys + j);
-      // dS at most 2^15 (see above), times the tile's share of the scale of k'
-      const float c = p.scale_log2 * pow2(-q_e - k_e);
-      const int d_e = -9 + g_e + g_v + g_k - k_e;
-      const float a = pow2(d_e - g_e - v_e), d = pow2(d_e) * delta;
-      const bool near = BIAS == kTable && near_tile(p, i0, j0), diag = j0 == i0;
-      float add = lse;
-      if (BIAS == kTable && !near) add += __ldg(table + p.bias_len - 1);
-      if (BIAS == kAlibi) add += slope2 * static_cast<float>(j0 + hf * 64 - i);
-      const uint32_t tS = tmem + lanes + (j & 1) * kTile + hf * 64;
-      ok = wait_all(&hdr->s_full[j & 1], (j >> 1) & 1u, p.status);
+    int done = 0, sums = 0;
+    Place at;
+    for (int it = 0; ok; ++it) {
+      const int set = set_of(plan, it);
+      ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
       if (!ok) break;
-      tc_fence_after();
-      float e[64];
+      const int nt = hdr->item[set].tiles[0], h = hdr->item[set].h, unit = hdr->item[set].unit, tile = hdr->item[set].tile;
+      if (nt < 0) break;
+      const int i0 = tile * kTile, i = i0 + row;
+      const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
+      const float far_bias = BIAS == kTable ? __ldg(table + p.bias_len - 1) : 0.f;
+      const float slope2 = BIAS == kAlibi ? __ldg(&p.heads[h].alibi_slope2) : 0.f;
+      const int64_t stat = static_cast<int64_t>(unit) * p.pad + i;
+      const float lse = nt > 0 ? __ldg(p.lse + stat) : 0.f, delta = nt > 0 ? __ldg(p.delta + stat) : 0.f;
+      float far_sum = 0.f;                                   // dS of far tiles, this thread's
+      float by_bucket[8] = {};                               // buckets lane, lane + 32, ...: this warp's
+      for (int j = 0; j < nt; ++j, at.next(plan.stages)) {
+        const int behind = done + j, buf = behind & 1, j0 = j * kTile + half * kHalf;
+        const bool near = BIAS == kTable && near_tile(p, i0, j0), diag = j == nt - 1;
+        const uint32_t tS = tmem + lanes + cS + half * 128 + buf * kHalf;
+        float add = lse;
+        if (BIAS == kTable && !near) add += far_bias;
+        if (BIAS == kAlibi) add += slope2 * static_cast<float>(j0 - i);
+        ok = wait_all(&hdr->full[at.stage], at.phase, p.status) && wait_all(&hdr->s_full[buf][half], (behind >> 1) & 1u, p.status);
+        if (!ok) break;
+        tc_fence_after();
+        const float4 scales = *reinterpret_cast<const float4*>(ring + at.stage * stage_bytes + scales_at);
+        float c = scales.x;
+        uint32_t r[2][32];
+        // S of a tile with masked keys or distances of their own goes back scaled, biased and masked
+        if (diag || near) {
+#pragma unroll 1
+          for (int k0 = 0; k0 < kHalf; k0 += 32) {
+            tmem_ld32(tS + k0, r[0]);
+            tmem_wait_ld_of(r[0]);
 #pragma unroll
-      for (int k = 0; k < 64; k += 32) {
-        uint32_t r[32];
-        tmem_ld32(tS + k, r);
-        tmem_wait_ld_of(r);
-#pragma unroll
-        for (int x = 0; x < 32; x += 2) {
-          if (BIAS == kAlibi) {
-            e[k + x] = fmaf(__uint_as_float(r[x]), c, fmaf(slope2, static_cast<float>(k + x), add));
-            e[k + x + 1] = fmaf(__uint_as_float(r[x + 1]), c, fmaf(slope2, static_cast<float>(k + x + 1), add));
-          } else {
-            fma2(e[k + x], e[k + x + 1], __uint_as_float(r[x]), __uint_as_float(r[x + 1]), c, add);
-          }
-        }
-      }
-      if (near) {
-#pragma unroll
-        for (int k = 0; k < 64; ++k) e[k] += __ldg(table + min(max(i - j0 - hf * 64 - k, 0), p.bias_len - 1));
-      }
-#pragma unroll
-      for (int k = 0; k < 64; ++k) e[k] = ex2(e[k]);
-      if (diag) {
-#pragma unroll
-        for (int k = 0; k < 64; ++k)
-          if (hf * 64 + k > row) e[k] = 0.f;
-      }
-      ok = wait_all(&hdr->g_full, j & 1u, p.status);
-      if (!ok) break;
-      tc_fence_after();
-#pragma unroll
-      for (int k = 0; k < 64; k += 32) {
-        uint32_t r[32];
-        tmem_ld32(tG + k, r);
-        tmem_wait_ld_of(r);
-#pragma unroll
-        for (int x = 0; x < 32; x += 2) {
-          float y0, y1;
-          fma2(y0, y1, __uint_as_float(r[x]), __uint_as_float(r[x + 1]), a, -d);
-          e[k + x] *= y0;
-          e[k + x + 1] *= y1;
-        }
-      }
-      tc_fence_before();
-      arrive_warp(&hdr->g_read, lane);
-#pragma unroll
-      for (int k = 0; k < 64; k += 32) {
-        uint32_t w[16];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) w[x] = pack_f16(e[k + 2 * x], e[k + 2 * x + 1]);
-        tmem_st16(tS + k / 2, w);
-      }
-      tmem_wait_st();
-      tc_fence_before();
-      arrive_warp(&hdr->p_full[j & 1], lane);
-      if (sums) {
-        const float back = pow2(-d_e);
-        if (!near) {
-          float s = 0.f;
-#pragma unroll
-          for (int k = 0; k < 64; ++k) s += e[k];
-          far_sum = fmaf(s, back, far_sum);
-        } else {
-          // slot 63 + (row in the warp) - column
-          float s = 0.f;
-#pragma unroll
-          for (int k = 0; k < 64; ++k) {
-            s = __shfl_up_sync(0xffffffffu, s, 1);
-            s = (lane == 0 ? 0.f : s) + e[k];
-            if (lane == 31) my_diagonals[94 - k] = s;
-          }
-          if (lane < 31) my_diagonals[lane] = s;
-          __syncwarp();
-          const int first = i0 + (warp & 3) * 32 - j0 - hf * 64 - 63;      // distance of slot 0
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int bucket = lane + 32 * u;
-            if (bucket < p.buckets) {
-              const int from = max(__ldg(p.starts + bucket) - first, 0);
-              const int next = __ldg(p.starts + bucket + 1), to = next > first + 95 ? 95 : next - first;
-              float sum = 0.f;
-              for (int x = from; x < to; ++x) sum += my_diagonals[x];
-              by_bucket[u] = fmaf(sum, back, by_bucket[u]);
+            for (int k = 0; k < 32; ++k) {
+              float y = __uint_as_float(r[0][k]) * c;
+              if (near) y += __ldg(table + min(max(i - j0 - k0 - k, 0), p.bias_len - 1));
+              if (diag && half * kHalf + k0 + k > row) y = -INFINITY;
+              r[0][k] = __float_as_uint(y);
             }
+            tmem_st16(tS + k0, *reinterpret_cast<uint32_t(*)[16]>(&r[0][0]));
+            tmem_st16(tS + k0 + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[0][16]));
           }
-          __syncwarp();
+          tmem_wait_st();
+          c = 1.f;
+        }
+        tmem_ld32(tS, r[0]);
+        tmem_ld32(tS + 32, r[1]);
+        tmem_wait_ld_of(r[0]);
+        tmem_wait_ld_of(r[1]);
+        unsigned long long e[32];                            // pairs of keys
+        const unsigned long long c_2 = both(c), add_2 = both(add);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          float x, y;
+          unpack2(fma2p(pair_at(r[k >> 4], k & 15), c_2, BIAS == kAlibi ? fma2p(both(slope2), pack2(2 * k, 2 * k + 1), add_2) : add_2), x, y);
+          e[k] = pack2(ex2(x), ex2(y));
+        }
+        ok = wait_all(&hdr->g_full[half], behind & 1u, p.status);
+        if (!ok) break;
+        tc_fence_after();
+        tmem_ld32(tG, r[0]);
+        tmem_ld32(tG + 32, r[1]);
+        tmem_wait_ld_of(r[0]);
+        tmem_wait_ld_of(r[1]);
+        tc_fence_before();
+        arrive_warp(&hdr->g_read[half], lane);
+        const unsigned long long a_2 = both(scales.z), d_2 = both(-scales.y * delta);
+        uint32_t w[2][16];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          e[k] = mul2p(e[k], fma2p(pair_at(r[k >> 4], k & 15), a_2, d_2));
+          float x, y;
+          unpack2(e[k], x, y);
+          w[k >> 4][k & 15] = pack_f16(x, y);
+        }
+        tmem_st16(tS, w[0]);
+        tmem_st16(tS + 16, w[1]);
+        tmem_wait_st();
+        tc_fence_before();
+        arrive_warp(&hdr->p_full[buf][half], lane);
+        if (want) {
+          const float back = scales.w;
+          if (!near) {
+            unsigned long long s = e[0];
+#pragma unroll
+            for (int k = 1; k < 32; ++k) s = add2p(s, e[k]);
+            float x, y;
+            unpack2(s, x, y);
+            far_sum = fmaf(x + y, back, far_sum);
+          } else {
+            // slot 63 + (row in the warp) - column
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < kHalf; ++k) {
+              float x, y;
+              unpack2(e[k / 2], x, y);
+              s = __shfl_up_sync(0xffffffffu, s, 1);
+              s = (lane == 0 ? 0.f : s) + (k & 1 ? y : x);
+              if (lane == 31) my_diagonals[94 - k] = s;
+            }
+            if (lane < 31) my_diagonals[lane] = s;
+            __syncwarp();
+            const int first = i0 + (warp & 3) * 32 - j0 - 63;                              // distance of slot 0
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const int bucket = lane + 32 * u;
+              if (bucket < p.buckets) {
+                const int from = max(__ldg(p.starts + bucket) - first, 0);
+                const int next = __ldg(p.starts + bucket + 1), to = next > first + 95 ? 95 : next - first;
+                float sum = 0.f;
+                for (int x = from; x < to; ++x) sum += my_diagonals[x];
+                by_bucket[u] = fmaf(sum, back, by_bucket[u]);
+              }
+            }
+            __syncwarp();
+          }
         }
       }
-    }
-    if (nt > 0 && ok) ok = wait_all(&hdr->done, 0, p.status);
-    tc_fence_after();
-    if (ok) {
-      const int split = ((rk16 >> 4) + 1) / 2 * 16, lo = hf ? split : 0, hi = hf ? rk16 : split;
-      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.dq) +
-                          (static_cast<int64_t>(b) * p.T + i) * (static_cast<int64_t>(p.group) * p.lr_k_width) + p.group * hd.lr_k_off + ih * hd.rp_k;
-      if (nt == 0) {
-        if (i < p.T) zero_row(lo, hi, hd.rp_k, to, aligned);
-      } else {
-        store_row(tmem + lanes + 384, lo, hi, hd.rp_k, p.scale * pow2(9 - g_e - g_v - g_k), to, i < p.T, i < n, aligned);
-      }
-    }
-    if (sums) {
+      if (!ok) break;
+      done += nt;
+      if (want) {
 #pragma unroll
-      for (int d = 16; d >= 1; d >>= 1) far_sum += __shfl_xor_sync(0xffffffffu, far_sum, d);
-      float* mine = diagonals + kSoftmaxWarps * 96 + warp * p.buckets;
+        for (int d = 16; d >= 1; d >>= 1) far_sum += __shfl_xor_sync(0xffffffffu, far_sum, d);
+        // (group 1: a head's units are its sequences)
+        float* part = p.bias_part + ((static_cast<int64_t>(unit) * p.tiles + tile) * kSoftmaxWarps + warp) * p.buckets;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int bucket = lane + 32 * u;
-        if (bucket < p.buckets) mine[bucket] = by_bucket[u] + (bucket == p.buckets - 1 ? far_sum : 0.f);
+        for (int u = 0; u < 8; ++u) {
+          const int bucket = lane + 32 * u;
+          if (bucket < p.buckets) part[bucket] = by_bucket[u] + (bucket == p.buckets - 1 ? far_sum : 0.f);
+        }
       }
+      if (nt > 0) ok = wait_all(&hdr->acc_full[0], sums & 1u, p.status);
+      if (!ok) break;
+      tc_fence_after();
+      {
+        const Item item = hdr->item[set];
+        const int rk16 = (item.rp_k + 15) & ~15, split = ((rk16 >> 4) + 1) / 2 * 16, lo = half ? split : 0, hi = half ? rk16 : split;
+        __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.dq) + (static_cast<int64_t>(item.b) * p.T + i) * (static_cast<int64_t>(p.group) * p.lr_k_width) +
+                            p.group * __ldg(&p.heads[h].lr_k_off) + item.i * item.rp_k;
+        if (nt == 0) {
+          if (i < p.T) zero_row(lo, hi, item.rp_k, to, plan.aligned & 1);
+        } else {
+          store_row(tmem + lanes + cQ, lo, hi, item.rp_k, p.scale * pow2(9 - item.small[3] - item.small[2] - item.small[1]), to, i < p.T, i < item.n, plan.aligned & 1);
+          tc_fence_before();
+          arrive_warp(&hdr->acc_free[0], lane);
+          ++sums;
+        }
+      }
+      arrive_warp(&hdr->own_empty[set], lane);
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (BIAS == kTable && p.dtable != nullptr && tid < p.buckets) {        // (group 1: a head's units are its sequences)
-    float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kSoftmaxWarps; ++w) sum += diagonals[kSoftmaxWarps * 96 + w * p.buckets + tid];
-    p.bias_part[(static_cast<int64_t>(unit) * p.tiles + tile) * p.buckets + tid] = sum;
-  }
   if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
-// Ring stages that fit beside the CTA's own tiles.
-int ring_stages(size_t fixed, size_t stage, size_t* smem) {
-  int stages = static_cast<int>((227 * 1024 - fixed) / stage);
-  if (stages > kMaxRing) stages = kMaxRing;
-  *smem = fixed + stages * stage;
+// Sets of own tiles and ring stages: two sets where three stages fit beside them, else one.
+Plan plan_of(const TrainParams& p, int units, int per_unit, size_t own, size_t stage, size_t behind, size_t* smem) {
+  Plan plan{};
+  const size_t room = 227 * 1024 - kHeaderBytes - behind;
+  plan.sets = 2 * own + 3 * stage <= room ? 2 : 1;
+  plan.stages = static_cast<int>((room - plan.sets * own) / stage);
+  if (plan.stages > kMaxRing) plan.stages = kMaxRing;
+  *smem = kHeaderBytes + behind + plan.sets * own + plan.stages * stage;
   if (*smem < 120 * 1024) *smem = 120 * 1024;                // one CTA per SM: it takes all of the SM's TMEM
-  return stages;
+  plan.units = units;
+  plan.per_unit = per_unit;
+  plan.items = units * per_unit;
+  const size_t walked = static_cast<size_t>(p.tiles) * (p.tile_k + p.tile_v);               // of a unit
+  const size_t chunk = (size_t(48) << 20) / walked;          // (some 50 of the 126 MB of L2)
+  plan.chunk = chunk < 1 ? 1 : chunk > static_cast<size_t>(units) ? units : static_cast<int>(chunk);
+  return plan;
 }
 template <typename Kernel>
-cudaError_t run(Kernel kernel, size_t (&done)[kMaxDevices], dim3 grid, size_t smem, const TrainParams& p, int stages, int aligned, cudaStream_t s) {
+cudaError_t run(Kernel kernel, size_t (&done)[kMaxDevices], const TrainParams& p, const Plan& plan, size_t smem, cudaStream_t s) {
   const cudaError_t e = ensure_dynamic_smem(kernel, smem, done);
   if (e != cudaSuccess) return e;
-  kernel<<<grid, kTrThreads, smem, s>>>(p, stages, aligned);
+  kernel<<<plan.items < p.sm_count ? plan.items : p.sm_count, kTrThreads, smem, s>>>(p, plan);
   return cudaGetLastError();
 }
 int bias_of(const TrainParams& p) { return p.bias != nullptr ? kTable : p.alibi ? kAlibi : kNone; }
-bool on16(const void* x) { return reinterpret_cast<uintptr_t>(x) % 16 == 0; }
+int on16(const void* x) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 ? 1 : 0; }
 
 }  // namespace
 
@@ -982,13 +1232,13 @@ cudaError_t launch_train_tc_forward(const TrainParams& p, cudaStream_t s, uint64
   static size_t done[3][kMaxDevices] = {};
   const size_t k = p.tile_k, v = p.tile_v;
   size_t smem = 0;
-  const int stages = ring_stages(kHeaderBytes + 2 * k, k + v, &smem), bias = bias_of(p);
-  const dim3 grid(p.H * p.group * p.B, (p.tiles + 1) / 2);
+  Plan plan = plan_of(p, p.H * p.group * p.B, (p.tiles + 1) / 2, 2 * k, k + v + kScaleBytes, 0, &smem);
+  plan.aligned = on16(p.out);
   ++*launches;
-  const int aligned = on16(p.out);
-  if (bias == kTable) return run(train_forward_kernel<kTable>, done[2], grid, smem, p, stages, aligned, s);
-  if (bias == kAlibi) return run(train_forward_kernel<kAlibi>, done[1], grid, smem, p, stages, aligned, s);
-  return run(train_forward_kernel<kNone>, done[0], grid, smem, p, stages, aligned, s);
+  const int bias = bias_of(p);
+  if (bias == kTable) return run(train_forward_kernel<kTable>, done[2], p, plan, smem, s);
+  if (bias == kAlibi) return run(train_forward_kernel<kAlibi>, done[1], p, plan, smem, s);
+  return run(train_forward_kernel<kNone>, done[0], p, plan, smem, s);
 }
 
 cudaError_t launch_train_tc_backward(const TrainParams& p, cudaStream_t s, uint64_t* launches) {
@@ -996,20 +1246,21 @@ cudaError_t launch_train_tc_backward(const TrainParams& p, cudaStream_t s, uint6
   const size_t k = p.tile_k, v = p.tile_v;
   const int bias = bias_of(p);
   size_t smem = 0;
-  int stages = ring_stages(kHeaderBytes + k + v, k + v + 1024, &smem);
-  const dim3 grid_kv(p.H * p.B, p.tiles), grid_q(p.H * p.group * p.B, p.tiles);
-  const int aligned = on16(p.dk) | on16(p.dv) << 1;
-  cudaError_t e = bias == kTable   ? run(train_dkv_kernel<kTable>, done_kv[2], grid_kv, smem, p, stages, aligned, s)
-                  : bias == kAlibi ? run(train_dkv_kernel<kAlibi>, done_kv[1], grid_kv, smem, p, stages, aligned, s)
-                                   : run(train_dkv_kernel<kNone>, done_kv[0], grid_kv, smem, p, stages, aligned, s);
+  Plan plan = plan_of(p, p.H * p.B, p.tiles, k + v, k + v + 1024 + kScaleBytes, 0, &smem);
+  plan.aligned = on16(p.dk) | on16(p.dv) << 1;
+  auto in_32 = [](int rp) { return (((rp + 15) & ~15) + 31) & ~31; };
+  plan.apart = in_32(p.max_rp_k) + in_32(p.max_rp_v) <= 192;
+  cudaError_t e = bias == kTable   ? run(train_dkv_kernel<kTable>, done_kv[2], p, plan, smem, s)
+                  : bias == kAlibi ? run(train_dkv_kernel<kAlibi>, done_kv[1], p, plan, smem, s)
+                                   : run(train_dkv_kernel<kNone>, done_kv[0], p, plan, smem, s);
   if (e != cudaSuccess) return e;
   ++*launches;
-  const size_t sums = p.dtable != nullptr ? kSoftmaxWarps * (96 + static_cast<size_t>(p.buckets)) * sizeof(float) : 0;
-  stages = ring_stages(kHeaderBytes + k + v + sums, k + v, &smem);
-  const bool q16 = on16(p.dq);
-  e = bias == kTable   ? run(train_dq_kernel<kTable>, done_q[2], grid_q, smem, p, stages, q16, s)
-      : bias == kAlibi ? run(train_dq_kernel<kAlibi>, done_q[1], grid_q, smem, p, stages, q16, s)
-                       : run(train_dq_kernel<kNone>, done_q[0], grid_q, smem, p, stages, q16, s);
+  const size_t diagonals = p.dtable != nullptr ? kSoftmaxWarps * 96 * sizeof(float) : 0;
+  plan = plan_of(p, p.H * p.group * p.B, p.tiles, k + v, k + v + kScaleBytes, diagonals, &smem);
+  plan.aligned = on16(p.dq);
+  e = bias == kTable   ? run(train_dq_kernel<kTable>, done_q[2], p, plan, smem, s)
+      : bias == kAlibi ? run(train_dq_kernel<kAlibi>, done_q[1], p, plan, smem, s)
+                       : run(train_dq_kernel<kNone>, done_q[0], p, plan, smem, s);
   ++*launches;
   return e;
 }
