@@ -37,6 +37,7 @@ __device__ __forceinline__ uint32_t take_max(uint32_t m, uint32_t w) {
 template <bool GRAD>
 __global__ void __launch_bounds__(kPackThreads) train_pack_kernel(const TrainParams p, int aligned) {
   __shared__ uint32_t tops[kPackThreads / 32];
+  chain_go();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int tile = blockIdx.x % p.tiles;
   int unit = blockIdx.x / p.tiles;

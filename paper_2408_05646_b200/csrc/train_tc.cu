@@ -71,7 +71,7 @@ struct __align__(16) TrHeader {
   uint32_t tmem_base;
   Item item[2];
 };
-static_assert(sizeof(TrHeader) <= kHeaderBytes, "header outgrew its area");
+static_assert(2 * sizeof(TrHeader) <= kHeaderBytes, "header outgrew its area");
 
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
@@ -159,8 +159,8 @@ __device__ __forceinline__ void item_of(const Plan& plan, int index, int& unit, 
   unit = first + rest - slot * width;
 }
 // Items of a CTA: every gridDim.x-th, there and back, so that no CTA has the longer one every time.
-__device__ __forceinline__ int64_t list_index(int it) {
-  return static_cast<int64_t>(it) * gridDim.x + (it & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+__device__ __forceinline__ int64_t list_index(int it, int cta) {
+  return static_cast<int64_t>(it) * gridDim.x + (it & 1 ? gridDim.x - 1 - cta : cta);
 }
 // Set of own tiles of a CTA's item and the phase of its barriers.
 __device__ __forceinline__ int set_of(const Plan& plan, int it) { return plan.sets == 2 ? it & 1 : 0; }
@@ -213,35 +213,43 @@ __device__ __forceinline__ int smallest_of(const int32_t* e, int count, int lane
 // Bias of a half tile of queries i0 .. against keys j0 ..: one number for all, unless some distance lies in front of the last entry.
 __device__ __forceinline__ bool near_tile(const TrainParams& p, int i0, int j0) { return i0 - j0 - (kTile - 1) < p.bias_len - 1; }
 
-// Barriers, TMEM and the layout that all three kernels share; returns the TMEM base.
-__device__ __forceinline__ uint32_t set_up(TrHeader* hdr, int warp, int tid, int empty, int own_empty, int p_full, int acc_full, int acc_free) {
-  if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
-  if (tid == 0) {
-    for (int s = 0; s < kMaxRing; ++s) {
-      mbar_init(&hdr->full[s], 1);
-      mbar_init(&hdr->empty[s], empty);
-    }
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(&hdr->own_full[x], 1);
-      mbar_init(&hdr->own_empty[x], own_empty);
-      for (int y = 0; y < 2; ++y) {
-        mbar_init(&hdr->s_full[x][y], 1);
-        mbar_init(&hdr->p_full[x][y], p_full);
-        mbar_init(&hdr->p_used[x][y], 1);
-      }
-      mbar_init(&hdr->g_full[x], 1);
-      mbar_init(&hdr->g_read[x], kSoftmaxWarps / 2);
-      mbar_init(&hdr->s_read[x], kSoftmaxWarps / 2);
-      mbar_init(&hdr->acc_full[x], acc_full);
-      mbar_init(&hdr->acc_free[x], acc_free);
-    }
-    for (int x = 0; x < 3; ++x) mbar_init(&hdr->drain[x], 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+// Barriers of a run through a list of items.
+__device__ __forceinline__ void set_up(TrHeader* hdr, int empty, int own_empty, int p_full, int acc_full, int acc_free) {
+  for (int s = 0; s < kMaxRing; ++s) {
+    mbar_init(&hdr->full[s], 1);
+    mbar_init(&hdr->empty[s], empty);
   }
+  for (int x = 0; x < 2; ++x) {
+    mbar_init(&hdr->own_full[x], 1);
+    mbar_init(&hdr->own_empty[x], own_empty);
+    for (int y = 0; y < 2; ++y) {
+      mbar_init(&hdr->s_full[x][y], 1);
+      mbar_init(&hdr->p_full[x][y], p_full);
+      mbar_init(&hdr->p_used[x][y], 1);
+    }
+    mbar_init(&hdr->g_full[x], 1);
+    mbar_init(&hdr->g_read[x], kSoftmaxWarps / 2);
+    mbar_init(&hdr->s_read[x], kSoftmaxWarps / 2);
+    mbar_init(&hdr->acc_full[x], acc_full);
+    mbar_init(&hdr->acc_free[x], acc_free);
+  }
+  for (int x = 0; x < 3; ++x) mbar_init(&hdr->drain[x], 1);
+}
+// All of a CTA's threads behind the set-up; returns the TMEM base.  What the launch before this one wrote is there afterwards.
+__device__ __forceinline__ uint32_t begin(TrHeader* hdr, int warp, int tid) {
+  if (warp == 0) tmem_alloc(&hdr->tmem_base, 512);
+  if (tid == 0) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  chain_go();
+  chain_wait();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   return __shfl_sync(0xffffffffu, hdr->tmem_base, 0);
+}
+__device__ __forceinline__ void end(uint32_t tmem, int warp) {
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, 512);
 }
 // The end of an issuing warp: nothing of it is under way when the CTA leaves.
 __device__ __forceinline__ void drain(TrHeader* hdr, int which, bool lead, int* status) {
@@ -265,14 +273,15 @@ __device__ __forceinline__ void drain_copies(TrHeader* hdr, const Plan& plan, in
 // the first 32 of them), o' of both.
 // Bound by the exponentials (16 a clock: 2048 clocks for two pairs of tiles; their products take 1630 at rank 80).
 template <int BIAS>
-__global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const TrainParams p, const Plan plan) {
+__global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __grid_constant__ TrainParams p, const __grid_constant__ Plan plan) {
   extern __shared__ __align__(1024) unsigned char smem[];
   TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   unsigned char* own = smem + kHeaderBytes;                  // sets of two tiles of q'
   unsigned char* ring = own + plan.sets * 2 * p.tile_k;
   const int stage_bytes = p.tile_k + p.tile_v + kScaleBytes; // (tiles of narrower heads fill a part)
-  const uint32_t tmem = set_up(hdr, warp, tid, 2, 2 + kSoftmaxWarps, 4, 1, 4);
+  if (tid == 0) set_up(hdr, 2, 2 + kSoftmaxWarps, 4, 1, 4);
+  const uint32_t tmem = begin(hdr, warp, tid);
 
   if (warp == kCopyWarp) {
     const uint64_t keep = policy_evict_normal();
@@ -284,7 +293,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const Trai
       if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
       if (!ok) break;
       Item* item = &hdr->item[set];
-      const int64_t index = list_index(it);
+      const int64_t index = list_index(it, blockIdx.x);
       if (index >= plan.items) {
         if (lane == 0) {
           item->tiles[0] = -1;
@@ -300,7 +309,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const Trai
       const int q_bytes = kTile * ((rp_k + 15) & ~15) * 2, v_bytes = kTile * ((rp_v + 15) & ~15) * 2;
       const int nt0 = tile * kTile < n ? tile + 1 : 0, nt1 = (tile + 1) * kTile < n ? tile + 2 : 0, most = max(nt0, nt1);
       const int32_t *k_exp = p.k_exp + static_cast<int64_t>(key_unit) * p.tiles, *v_exp = p.v_exp + static_cast<int64_t>(key_unit) * p.tiles;
-      const int g_v = smallest_of(v_exp, p.tiles, lane);
+      const int g_v = smallest_of(v_exp, most, lane);                                      // (of the tiles it walks)
       const int64_t q_at = static_cast<int64_t>(unit) * p.tiles + tile;
       const int q_e0 = __ldg(p.q_exp + q_at), q_e1 = nt1 > 0 ? __ldg(p.q_exp + q_at + 1) : 0;
       if (lane == 0) {
@@ -553,9 +562,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const Trai
       arrive_warp(&hdr->own_empty[set], lane);
     }
   }
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 0) tmem_dealloc(tmem, 512);
+  end(tmem, warp);
 }
 
 // ---------------------------------------------------------------- dk', dv'
@@ -568,11 +575,8 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const Trai
 // them (their sum at most 192, each in steps of 32): the next S^T then starts when this one has been read.  Otherwise it takes
 // S^T's place.
 template <int BIAS>
-__global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainParams p, const Plan plan) {
-  extern __shared__ __align__(1024) unsigned char smem[];
-  TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);
-  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  unsigned char* own = smem + kHeaderBytes;                  // sets of a tile of k' and one of v'
+__device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan, TrHeader* hdr, unsigned char* smem, uint32_t tmem, int warp, int lane, int cta) {
+  unsigned char* own = smem;                                 // sets of a tile of k' and one of v'
   unsigned char* ring = own + plan.sets * (p.tile_k + p.tile_v);
   const int rows_at = p.tile_k + p.tile_v, stage_bytes = rows_at + 1024 + kScaleBytes;      // q', do', then L and delta
   const bool apart = plan.apart != 0;
@@ -580,8 +584,6 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
   constexpr uint32_t cS = 0, cG = 128;
   const uint32_t cP = apart ? 256 : cS, p_step = apart ? 32 : kHalf, cV = apart ? 320 : 256;
   const uint32_t cK = cV + (apart ? (((p.max_rp_v + 15) & ~15) + 31) & ~31 : 128);
-  const uint32_t tmem = set_up(hdr, warp, tid, 2, 3 + kSoftmaxWarps, kSoftmaxWarps / 2, 2, kSoftmaxWarps);
-
   if (warp == kCopyWarp) {
     const uint64_t keep = policy_evict_normal();
     bool ok = true;
@@ -592,7 +594,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
       if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
       if (!ok) break;
       Item* item = &hdr->item[set];
-      const int64_t index = list_index(it);
+      const int64_t index = list_index(it, cta);
       if (index >= plan.items) {
         if (lane == 0) {
           item->tiles[0] = -1;
@@ -608,12 +610,12 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
       const int per_head = max((n + kTile - 1) / kTile - tile, 0);                          // tiles of queries of one head
       const int64_t own_at = static_cast<int64_t>(unit) * p.tiles + tile;
       const int k_e = __ldg(p.k_exp + own_at), v_e = __ldg(p.v_exp + own_at);
-      const int g_v = smallest_of(p.v_exp + static_cast<int64_t>(unit) * p.tiles, p.tiles, lane);
+      const int g_v = smallest_of(p.v_exp + static_cast<int64_t>(unit) * p.tiles, p.tiles, lane);   // (delta knows every key)
       int g_q = kTrainNoNumber, g_g = kTrainNoNumber;
       for (int i = 0; i < p.group; ++i) {
-        const int64_t at_q = (static_cast<int64_t>(h * p.group + i) * p.B + b) * p.tiles;
-        g_q = smallest_of(p.q_exp + at_q, p.tiles, lane, g_q);
-        g_g = smallest_of(p.g_exp + at_q, p.tiles, lane, g_g);
+        const int64_t at_q = (static_cast<int64_t>(h * p.group + i) * p.B + b) * p.tiles + tile;          // (of the tiles it walks)
+        g_q = smallest_of(p.q_exp + at_q, p.tiles - tile, lane, g_q);
+        g_g = smallest_of(p.g_exp + at_q, p.tiles - tile, lane, g_g);
       }
       if (lane == 0) {
         item->unit = unit; item->h = h; item->b = b; item->i = 0;
@@ -628,24 +630,38 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
         } else {
           mbar_arrive(&hdr->own_full[set]);
         }
-        for (int i = 0; i < p.group && ok; ++i) {
-          const int64_t q_unit = static_cast<int64_t>(h * p.group + i) * p.B + b;
-          for (int t = 0; t < per_head; ++t, ++issued, at.next(plan.stages)) {
-            // P^T = 2^(S c + lift - L), times 2^14 and the tile's share of do''s scale;  dS^T = P^T (G^T a - delta d), at most
-            // 2^15: |do' v'| and |delta| are below r 2^(16 - e - e'), e and e' the smallest exponents of do' and v'
-            const int64_t from = q_unit * p.tiles + tile + t;
-            const int q_e = __ldg(p.q_exp + from), g_e = __ldg(p.g_exp + from);
-            const int lift = kBackwardShift + g_g - g_e, d_e = -9 + g_g + g_v + g_q - q_e - lift;
-            unsigned long long* full = &hdr->full[at.stage];
-            if (issued >= plan.stages && !(ok = mbar_wait(&hdr->empty[at.stage], at.phase ^ 1u, p.status))) break;
-            unsigned char* st = ring + at.stage * stage_bytes;
-            *reinterpret_cast<float4*>(st + rows_at + 1024) =
-                make_float4(p.scale_log2 * pow2(-q_e - k_e), static_cast<float>(lift), -pow2(d_e), pow2(d_e - g_e - v_e));
-            mbar_arrive_expect_tx(full, k_bytes + v_bytes + 1024);
+      }
+      const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
+      const float far_bias = BIAS == kTable ? __ldg(table + p.bias_len - 1) : 0.f;
+      const float slope2 = BIAS == kAlibi ? __ldg(&p.heads[h].alibi_slope2) : 0.f;
+      for (int i = 0; i < p.group && ok; ++i) {
+        const int64_t q_unit = static_cast<int64_t>(h * p.group + i) * p.B + b;
+        for (int t = 0; t < per_head; ++t, ++issued, at.next(plan.stages)) {
+          // P^T = 2^(S c + lift - L), times 2^14 and the tile's share of do''s scale;  dS^T = P^T (G^T a - delta d), at most
+          // 2^15: |do' v'| and |delta| are below r 2^(16 - e - e'), e and e' the smallest exponents of do' and v'.  The rows'
+          // own numbers, lift - L and delta d, are worked out here, four a lane.
+          const int64_t from = q_unit * p.tiles + tile + t, row_at = q_unit * p.pad + (tile + t) * kTile + 4 * lane;
+          const int q_e = __ldg(p.q_exp + from), g_e = __ldg(p.g_exp + from);
+          float4 l = __ldg(reinterpret_cast<const float4*>(p.lse + row_at)), dl = __ldg(reinterpret_cast<const float4*>(p.delta + row_at));
+          const int lift = kBackwardShift + g_g - g_e, d_e = -9 + g_g + g_v + g_q - q_e - lift;
+          float add = static_cast<float>(lift);
+          if (BIAS == kTable && !near_tile(p, t * kTile, 0)) add += far_bias;
+          if (BIAS == kAlibi) add -= slope2 * static_cast<float>(t * kTile + 4 * lane);
+          l.x += add; l.y += add - slope2; l.z += add - 2.f * slope2; l.w += add - 3.f * slope2;
+          const float d = -pow2(d_e);
+          dl.x *= d; dl.y *= d; dl.z *= d; dl.w *= d;
+          unsigned long long* full = &hdr->full[at.stage];
+          if (issued >= plan.stages && !(ok = wait_all(&hdr->empty[at.stage], at.phase ^ 1u, p.status))) break;
+          unsigned char* st = ring + at.stage * stage_bytes;
+          *reinterpret_cast<float4*>(st + rows_at + 16 * lane) = l;
+          *reinterpret_cast<float4*>(st + rows_at + 512 + 16 * lane) = dl;
+          if (lane == 0)
+            *reinterpret_cast<float2*>(st + rows_at + 1024) = make_float2(p.scale_log2 * pow2(-q_e - k_e), pow2(d_e - g_e - v_e));
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive_expect_tx(full, k_bytes + v_bytes);
             bulk_load(st, p.q_tiles + from * p.tile_k, k_bytes, full, keep);
             bulk_load(st + p.tile_k, p.g_tiles + from * p.tile_v, v_bytes, full, keep);
-            bulk_load(st + rows_at, p.lse + q_unit * p.pad + (tile + t) * kTile, 512, full, keep);
-            bulk_load(st + rows_at + 512, p.delta + q_unit * p.pad + (tile + t) * kTile, 512, full, keep);
           }
         }
       }
@@ -757,21 +773,19 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
       if (total < 0) break;
       const int j0 = hdr->item[set].tile * kTile, key = j0 + row;
       const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
-      const float far_bias = BIAS == kTable ? __ldg(table + p.bias_len - 1) : 0.f;
       const float slope2 = BIAS == kAlibi ? __ldg(&p.heads[h].alibi_slope2) : 0.f;
       int t = 0;
       for (int g = 0; g < total; ++g) {
         const uint32_t phase = (done + g) & 1u;
-        const int i0 = j0 + t * kTile + half * kHalf;
-        const bool near = BIAS == kTable && near_tile(p, i0, j0), diag = t == 0;
+        const int far0 = t * kTile + half * kHalf - row;     // distance of the thread's first pair
+        // (near: by whole tiles, as the copying warp has it)
+        const bool near = BIAS == kTable && near_tile(p, t * kTile, 0), diag = t == 0;
         if (++t == per_head) t = 0;
-        float add = BIAS == kAlibi ? slope2 * static_cast<float>(key - i0) : 0.f;
-        if (BIAS == kTable && !near) add = far_bias;
         ok = wait_all(&hdr->full[at.stage], at.phase, p.status) && wait_all(&hdr->s_full[0][half], phase, p.status);
         if (!ok) break;
         tc_fence_after();
         const float* lse = reinterpret_cast<const float*>(ring + at.stage * stage_bytes + rows_at) + half * kHalf;
-        const float4 scales = *reinterpret_cast<const float4*>(ring + at.stage * stage_bytes + rows_at + 1024);
+        const float2 scales = *reinterpret_cast<const float2*>(ring + at.stage * stage_bytes + rows_at + 1024);
         float c = scales.x;
         uint32_t r[2][32];
         // S of a tile with masked queries or distances of their own goes back scaled, biased and masked
@@ -783,7 +797,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
 #pragma unroll
             for (int k = 0; k < 32; ++k) {
               float y = __uint_as_float(r[0][k]) * c;
-              if (near) y += __ldg(table + min(max(i0 + k0 + k - key, 0), p.bias_len - 1));
+              if (near) y += __ldg(table + min(max(far0 + k0 + k, 0), p.bias_len - 1));
               if (diag && half * kHalf + k0 + k < row) y = -INFINITY;
               r[0][k] = __float_as_uint(y);
             }
@@ -796,17 +810,12 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
         tmem_ld32(tS, r[0]);
         tmem_ld32(tS + 32, r[1]);
         unsigned long long e[32];                            // pairs of queries
-        const unsigned long long add_2 = both(add + scales.y), c_2 = both(c);
+        const unsigned long long c_2 = both(c), slant = both(slope2 * static_cast<float>(row));
 #pragma unroll
         for (int k = 0; k < 32; k += 2) {
           const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(lse + 2 * k);
-          if (BIAS == kAlibi) {
-            e[k] = add2p(l.x, fma2p(both(-slope2), pack2(2 * k, 2 * k + 1), add_2));
-            e[k + 1] = add2p(l.y, fma2p(both(-slope2), pack2(2 * k + 2, 2 * k + 3), add_2));
-          } else {
-            e[k] = add2p(l.x, add_2);
-            e[k + 1] = add2p(l.y, add_2);
-          }
+          e[k] = BIAS == kAlibi ? add2p(l.x, slant) : l.x;
+          e[k + 1] = BIAS == kAlibi ? add2p(l.y, slant) : l.y;
         }
         tmem_wait_ld_of(r[0]);
         tmem_wait_ld_of(r[1]);
@@ -839,14 +848,14 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
         tmem_ld32(tG + 32, r[1]);
         tmem_wait_ld_of(r[0]);
         tmem_wait_ld_of(r[1]);
-        const unsigned long long d = both(scales.z), a = both(scales.w);
+        const unsigned long long a = both(scales.y);
 #pragma unroll
         for (int k = 0; k < 32; k += 2) {
           const ulonglong2 dl = *reinterpret_cast<const ulonglong2*>(lse + 128 + 2 * k);
           float x, y;
-          unpack2(mul2p(e[k], fma2p(pair_at(r[k >> 4], k & 15), a, mul2p(dl.x, d))), x, y);
+          unpack2(mul2p(e[k], fma2p(pair_at(r[k >> 4], k & 15), a, dl.x)), x, y);
           w[k >> 4][k & 15] = pack_f16(x, y);
-          unpack2(mul2p(e[k + 1], fma2p(pair_at(r[k >> 4], (k & 15) + 1), a, mul2p(dl.y, d))), x, y);
+          unpack2(mul2p(e[k + 1], fma2p(pair_at(r[k >> 4], (k & 15) + 1), a, dl.y)), x, y);
           w[k >> 4][(k & 15) + 1] = pack_f16(x, y);
         }
         tmem_st16(tG, w[0]);
@@ -887,9 +896,6 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
       arrive_warp(&hdr->own_empty[set], lane);
     }
   }
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
 // ---------------------------------------------------------------- dq'
@@ -902,17 +908,12 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dkv_kernel(const TrainPar
 // bucket, are added up whole; in the others a sum moves one lane up with every column, so that it follows its diagonal, and
 // leaves the warp complete.  All of it in a fixed order, without atomics.
 template <int BIAS>
-__global__ void __launch_bounds__(kTrThreads, 1) train_dq_kernel(const TrainParams p, const Plan plan) {
-  extern __shared__ __align__(1024) unsigned char smem[];
-  TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);
-  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  unsigned char* own = smem + kHeaderBytes;                  // sets of a tile of q' and one of do'
+__device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan, TrHeader* hdr, unsigned char* smem, uint32_t tmem, int warp, int lane, int cta) {
+  unsigned char* own = smem;                                 // sets of a tile of q' and one of do'
   unsigned char* ring = own + plan.sets * (p.tile_k + p.tile_v);
   const int scales_at = p.tile_k + p.tile_v, stage_bytes = scales_at + kScaleBytes;
   float* diagonals = reinterpret_cast<float*>(ring + plan.stages * stage_bytes);           // [softmax warps][96]
   constexpr uint32_t cS = 0, cG = 256, cQ = 384;             // TMEM columns of S ([half][tile & 1]), G ([half]), dq'
-  const uint32_t tmem = set_up(hdr, warp, tid, 2, 3 + kSoftmaxWarps, kSoftmaxWarps / 2, 1, kSoftmaxWarps);
-
   if (warp == kCopyWarp) {
     const uint64_t keep = policy_evict_normal();
     bool ok = true;
@@ -923,7 +924,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dq_kernel(const TrainPara
       if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
       if (!ok) break;
       Item* item = &hdr->item[set];
-      const int64_t index = list_index(it);
+      const int64_t index = list_index(it, cta);
       if (index >= plan.items) {
         if (lane == 0) {
           item->tiles[0] = -1;
@@ -940,7 +941,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dq_kernel(const TrainPara
       const int nt = tile * kTile < n ? tile + 1 : 0;
       const int64_t own_at = static_cast<int64_t>(unit) * p.tiles + tile, keys = static_cast<int64_t>(key_unit) * p.tiles;
       const int q_e = __ldg(p.q_exp + own_at), g_e = __ldg(p.g_exp + own_at);
-      const int g_k = smallest_of(p.k_exp + keys, p.tiles, lane), g_v = smallest_of(p.v_exp + keys, p.tiles, lane);
+      const int g_k = smallest_of(p.k_exp + keys, nt, lane), g_v = smallest_of(p.v_exp + keys, nt, lane);         // (of the tiles it walks)
       if (lane == 0) {
         item->unit = unit; item->h = h; item->b = b; item->i = hq - h * p.group;
         item->tile = tile; item->n = n; item->rp_k = rp_k; item->rp_v = rp_v;
@@ -1194,9 +1195,31 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_dq_kernel(const TrainPara
       arrive_warp(&hdr->own_empty[set], lane);
     }
   }
+}
+
+// ---------------------------------------------------------------- both in one launch
+
+// A CTA has its share of the tiles of keys, then its share of the tiles of queries; the list of the latter begins at the CTA
+// behind the last one with a tile of keys more, so that a small call has all its items running at a time (a text of 129 tokens
+// through 32 heads: 64 and 64 items).
+template <int BIAS>
+__global__ void __launch_bounds__(kTrThreads, 1) train_backward_kernel(const __grid_constant__ TrainParams p, const __grid_constant__ Plan plan_kv, const __grid_constant__ Plan plan_q) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);         // one for each list
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  if (tid == 0) {
+    set_up(hdr, 2, 3 + kSoftmaxWarps, kSoftmaxWarps / 2, 2, kSoftmaxWarps);
+    set_up(hdr + 1, 2, 3 + kSoftmaxWarps, kSoftmaxWarps / 2, 1, kSoftmaxWarps);
+  }
+  const uint32_t tmem = begin(hdr, warp, tid);
+  const int cta = blockIdx.x, behind = cta - plan_kv.items % static_cast<int>(gridDim.x);
+  dkv_items<BIAS>(p, plan_kv, hdr, smem + kHeaderBytes, tmem, warp, lane, cta);
+  fence_async_smem();                                        // (copies follow on plain writes)
   tc_fence_before();
   __syncthreads();
-  if (warp == 0) tmem_dealloc(tmem, 512);
+  tc_fence_after();
+  dq_items<BIAS>(p, plan_q, hdr + 1, smem + kHeaderBytes, tmem, warp, lane, behind < 0 ? behind + gridDim.x : behind);
+  end(tmem, warp);
 }
 
 // Sets of own tiles and ring stages: two sets where three stages fit beside them, else one.
@@ -1216,53 +1239,55 @@ Plan plan_of(const TrainParams& p, int units, int per_unit, size_t own, size_t s
   plan.chunk = chunk < 1 ? 1 : chunk > static_cast<size_t>(units) ? units : static_cast<int>(chunk);
   return plan;
 }
-template <typename Kernel>
-cudaError_t run(Kernel kernel, size_t (&done)[kMaxDevices], const TrainParams& p, const Plan& plan, size_t smem, cudaStream_t s) {
-  const cudaError_t e = ensure_dynamic_smem(kernel, smem, done);
-  if (e != cudaSuccess) return e;
-  kernel<<<plan.items < p.sm_count ? plan.items : p.sm_count, kTrThreads, smem, s>>>(p, plan);
-  return cudaGetLastError();
-}
 int bias_of(const TrainParams& p) { return p.bias != nullptr ? kTable : p.alibi ? kAlibi : kNone; }
 int on16(const void* x) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 ? 1 : 0; }
 
 }  // namespace
 
+// (chained to the launch before it, which packs the tiles: its set-up runs beside that one's end)
 cudaError_t launch_train_tc_forward(const TrainParams& p, cudaStream_t s, uint64_t* launches) {
   static size_t done[3][kMaxDevices] = {};
   const size_t k = p.tile_k, v = p.tile_v;
   size_t smem = 0;
   Plan plan = plan_of(p, p.H * p.group * p.B, (p.tiles + 1) / 2, 2 * k, k + v + kScaleBytes, 0, &smem);
   plan.aligned = on16(p.out);
-  ++*launches;
+  const int grid = plan.items < p.sm_count ? plan.items : p.sm_count;
+  auto run = [&](auto kernel, size_t (&table)[kMaxDevices]) -> cudaError_t {
+    const cudaError_t e = ensure_dynamic_smem(kernel, smem, table);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    return launch_chained(true, kernel, dim3(grid), dim3(kTrThreads), smem, s, p, plan);
+  };
   const int bias = bias_of(p);
-  if (bias == kTable) return run(train_forward_kernel<kTable>, done[2], p, plan, smem, s);
-  if (bias == kAlibi) return run(train_forward_kernel<kAlibi>, done[1], p, plan, smem, s);
-  return run(train_forward_kernel<kNone>, done[0], p, plan, smem, s);
+  if (bias == kTable) return run(train_forward_kernel<kTable>, done[2]);
+  if (bias == kAlibi) return run(train_forward_kernel<kAlibi>, done[1]);
+  return run(train_forward_kernel<kNone>, done[0]);
 }
 
 cudaError_t launch_train_tc_backward(const TrainParams& p, cudaStream_t s, uint64_t* launches) {
-  static size_t done_kv[3][kMaxDevices] = {}, done_q[3][kMaxDevices] = {};
+  static size_t done[3][kMaxDevices] = {};
   const size_t k = p.tile_k, v = p.tile_v;
-  const int bias = bias_of(p);
-  size_t smem = 0;
-  Plan plan = plan_of(p, p.H * p.B, p.tiles, k + v, k + v + 1024 + kScaleBytes, 0, &smem);
-  plan.aligned = on16(p.dk) | on16(p.dv) << 1;
+  size_t smem = 0, smem_q = 0;
+  Plan plan_kv = plan_of(p, p.H * p.B, p.tiles, k + v, k + v + 1024 + kScaleBytes, 0, &smem);
+  plan_kv.aligned = on16(p.dk) | on16(p.dv) << 1;
   auto in_32 = [](int rp) { return (((rp + 15) & ~15) + 31) & ~31; };
-  plan.apart = in_32(p.max_rp_k) + in_32(p.max_rp_v) <= 192;
-  cudaError_t e = bias == kTable   ? run(train_dkv_kernel<kTable>, done_kv[2], p, plan, smem, s)
-                  : bias == kAlibi ? run(train_dkv_kernel<kAlibi>, done_kv[1], p, plan, smem, s)
-                                   : run(train_dkv_kernel<kNone>, done_kv[0], p, plan, smem, s);
-  if (e != cudaSuccess) return e;
-  ++*launches;
+  plan_kv.apart = in_32(p.max_rp_k) + in_32(p.max_rp_v) <= 192;
   const size_t diagonals = p.dtable != nullptr ? kSoftmaxWarps * 96 * sizeof(float) : 0;
-  plan = plan_of(p, p.H * p.group * p.B, p.tiles, k + v, k + v + kScaleBytes, diagonals, &smem);
-  plan.aligned = on16(p.dq);
-  e = bias == kTable   ? run(train_dq_kernel<kTable>, done_q[2], p, plan, smem, s)
-      : bias == kAlibi ? run(train_dq_kernel<kAlibi>, done_q[1], p, plan, smem, s)
-                       : run(train_dq_kernel<kNone>, done_q[0], p, plan, smem, s);
-  ++*launches;
-  return e;
+  Plan plan_q = plan_of(p, p.H * p.group * p.B, p.tiles, k + v, k + v + kScaleBytes, diagonals, &smem_q);
+  plan_q.aligned = on16(p.dq);
+  if (smem_q > smem) smem = smem_q;
+  const int64_t items = static_cast<int64_t>(plan_kv.items) + plan_q.items;
+  const int grid = items < p.sm_count ? static_cast<int>(items) : p.sm_count;
+  auto run = [&](auto kernel, size_t (&table)[kMaxDevices]) -> cudaError_t {
+    const cudaError_t e = ensure_dynamic_smem(kernel, smem, table);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    return launch_chained(true, kernel, dim3(grid), dim3(kTrThreads), smem, s, p, plan_kv, plan_q);
+  };
+  const int bias = bias_of(p);
+  if (bias == kTable) return run(train_backward_kernel<kTable>, done[2]);
+  if (bias == kAlibi) return run(train_backward_kernel<kAlibi>, done[1]);
+  return run(train_backward_kernel<kNone>, done[0]);
 }
 
 }  // namespace ea
