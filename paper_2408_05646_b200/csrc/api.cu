@@ -1926,7 +1926,7 @@ ea_status eigen_attn_set_rope(eigen_attn_t h, double base, int32_t interleaved, 
 // ---- a learned bias of relative positions
 
 namespace {
-constexpr int kMaxBuckets = 256, kMaxDistance = 32768;
+constexpr int kMaxDistance = 32768;
 
 // base^exponent as a sum of 32-bit words, times the words given
 void multiply_power(std::vector<uint32_t>* x, uint32_t base, int exponent) {
@@ -1971,9 +1971,9 @@ std::vector<int32_t> bucket_starts(int n_buckets, int max_distance) {
 }
 ea_status plan_bias(eigen_attn_t h, const char* who, int32_t n_buckets, int32_t max_distance, std::vector<int32_t>* starts,
                     size_t* off, size_t* bytes) {
-  if (n_buckets < 2 || n_buckets > kMaxBuckets || max_distance <= n_buckets / 2 || max_distance > kMaxDistance)
+  if (n_buckets < 2 || n_buckets > ea::kMaxBuckets || max_distance <= n_buckets / 2 || max_distance > kMaxDistance)
     return fail(h, EA_ERR_SHAPE, "%s: %d buckets (2..%d), max_distance %d (more than half of that, at most %d)", who, n_buckets,
-                kMaxBuckets, max_distance, kMaxDistance);
+                ea::kMaxBuckets, max_distance, kMaxDistance);
   try {
     *starts = bucket_starts(n_buckets, max_distance);
   } catch (const std::bad_alloc&) {
@@ -2080,7 +2080,7 @@ void make_train_layout(const eigen_attn* h, int tokens, int group, TrainLayout* 
     t->k = area(rows * h->L.sum_rp_k * sizeof(float));
     t->v = area(rows * h->L.sum_rp_v * sizeof(float));
   }
-  t->bias = area(group == 1 ? units * train_bias_parts(h, tokens) * kMaxBuckets * sizeof(float) : 0);
+  t->bias = area(group == 1 ? units * train_bias_parts(h, tokens) * ea::kMaxBuckets * sizeof(float) : 0);
   t->bytes = off;
 }
 

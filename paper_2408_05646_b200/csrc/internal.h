@@ -499,6 +499,7 @@ cudaError_t launch_quant_combine(const QuantParams& p, cudaStream_t s, uint64_t*
 // Attention over rank-space rows with its backward pass (eigen_attn_train_*).  Query unit u = (h group + i) B + b: query head
 // i of K/V head h, sequence b; key unit h B + b.  Rows of T tokens are kept in `pad` = T rounded up to whole tiles of 128.
 constexpr int kTrainTile = 128;
+constexpr int kMaxBuckets = 256;          // of a learned bias
 constexpr int kTrainBiasParts = 8;        // sums per bucket that a tile of queries leaves (tensor-core kernels: one per warp)
 constexpr int kTrainNoNumber = 120;       // exponent of a tile without a number other than zero (above every other)
 struct TrainParams {

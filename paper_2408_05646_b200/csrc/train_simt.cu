@@ -9,13 +9,16 @@
 // added up by atomics.  A tile's products are summed apart and then added, which keeps the rounding errors of long sums down.
 // Bound by the loads from shared memory (two for eight multiply-adds in the score products): figures in the table of cases.
 #include "internal.h"
+#include "tc_common.cuh"
 
 namespace ea {
 namespace {
 
-constexpr int kRows = 64;
+constexpr int kOwn = 32;                  // rows of a CTA's own tile
+constexpr int kWalk = 64;                 // rows of a tile of the walked axis
 constexpr int kThreads = 256;
-constexpr int kPitchP = kRows + 4;
+constexpr int kPitchP = kWalk + 4;
+constexpr int RI = kOwn / 16;             // own rows of a thread
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -23,37 +26,54 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// rows x width numbers of packed rows into shared memory (pitch = width + 4), zeros behind `rows`; columns from `live` on are
-// the rank's padding: zeros, whatever the caller left there.  copy: the same numbers kept for the backward pass.
-__device__ __forceinline__ void load_rows(float* dst, const float* src, int64_t stride, int rows, int width, int live, int tid,
-                                          float* copy = nullptr) {
-  for (int idx = tid; idx < kRows * width; idx += kThreads) {
-    const int r = idx / width, c = idx - r * width;
-    float x = 0.f;
-    if (r < rows) {
-      if (c < live) x = src[r * stride + c];
-      if (copy != nullptr) copy[r * stride + c] = x;
+// Packed rows on their way into shared memory (pitch = width + 4), zeros behind `rows`; columns from `live` on are the rank's
+// padding: zeros, whatever the caller left there.  wide: the rows lie on 16-byte boundaries.
+template <int COUNT>
+__device__ __forceinline__ void fetch_rows(float* dst, const float* src, int64_t stride, int rows, int width, int live, bool wide, int tid) {
+  const uint32_t to = tc::smem_u32(dst);
+  if (wide) {
+    const int quads = width >> 2;
+    for (int idx = tid; idx < COUNT * quads; idx += kThreads) {
+      const int r = idx / quads, c = 4 * (idx - r * quads);
+      const int bytes = r < rows ? 4 * min(max(live - c, 0), 4) : 0;
+      const float* from = bytes > 0 ? src + r * stride + c : src;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 4 * (r * (width + 4) + c)), "l"(from), "r"(bytes) : "memory");
     }
-    dst[r * (width + 4) + c] = x;
+  } else {
+    for (int idx = tid; idx < COUNT * width; idx += kThreads) {
+      const int r = idx / width, c = idx - r * width;
+      const int bytes = r < rows && c < live ? 4 : 0;
+      const float* from = bytes > 0 ? src + r * stride + c : src;
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * (r * (width + 4) + c)), "l"(from), "r"(bytes) : "memory");
+    }
   }
 }
+// The rows of this CTA's own tile, kept for the backward pass.
+__device__ __forceinline__ void keep_rows(float* dst, const float* src, int64_t stride, int rows, int width, int tid) {
+  const int quads = width >> 2;
+  for (int idx = tid; idx < rows * quads; idx += kThreads) {
+    const int r = idx / quads, c = 4 * (idx - r * quads);
+    *reinterpret_cast<float4*>(dst + r * stride + c) = *reinterpret_cast<const float4*>(src + r * (width + 4) + c);
+  }
+}
+__device__ __forceinline__ bool on16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }
 
 // s[i][j] = sum_c a[ty + 16 i][c] b[tx + 16 j][c]
-__device__ __forceinline__ void product_nt(float (&s)[4][4], const float* a, const float* b, int width, int ty, int tx) {
+__device__ __forceinline__ void product_nt(float (&s)[RI][4], const float* a, const float* b, int width, int ty, int tx) {
   const int pitch = width + 4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < RI; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 2
   for (int c = 0; c < width; c += 4) {
-    float4 x[4], y[4];
+    float4 x[RI], y[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * pitch + c);
+    for (int i = 0; i < RI; ++i) x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * pitch + c);
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(b + (tx + 16 * j) * pitch + c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < RI; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         s[i][j] = fmaf(x[i].x, y[j].x, s[i][j]);
@@ -64,40 +84,49 @@ __device__ __forceinline__ void product_nt(float (&s)[4][4], const float* a, con
   }
 }
 
-// sum[i][c] += sum_k w[ty + 16 i][k] x[k][tx + 16 c], k = 0 .. 63
+// Column pairs of a thread: 2 tx and 2 tx + 1 of every 32.
+__device__ __forceinline__ int column(int c, int tx) { return 32 * (c >> 1) + 2 * tx + (c & 1); }
+
+// sum[i][c] += sum_k w[ty + 16 i][k] x[k][column(c)], k = 0 .. 63
 template <int NC>
-__device__ __forceinline__ void product_nn(float (&sum)[4][NC], const float* w, const float* x, int width, int ty, int tx) {
+__device__ __forceinline__ void product_nn(float (&sum)[RI][NC], const float* w, const float* x, int width, int ty, int tx) {
   const int pitch = width + 4;
-  float part[4][NC];
+  float part[RI][NC];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < RI; ++i)
 #pragma unroll
     for (int c = 0; c < NC; ++c) part[i][c] = 0.f;
 #pragma unroll 2
-  for (int k = 0; k < kRows; k += 4) {
-    float4 a[4];
+  for (int k = 0; k < kWalk; k += 4) {
+    float4 a[RI];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(w + (ty + 16 * i) * kPitchP + k);
+    for (int i = 0; i < RI; ++i) a[i] = *reinterpret_cast<const float4*>(w + (ty + 16 * i) * kPitchP + k);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int col = min(tx + 16 * c, width - 1);           // (columns past the width repeat the last one and are not stored)
-      const float x0 = x[k * pitch + col], x1 = x[(k + 1) * pitch + col];
-      const float x2 = x[(k + 2) * pitch + col], x3 = x[(k + 3) * pitch + col];
+    for (int c = 0; c < NC; c += 2) {
+      const float* at = x + k * pitch + min(column(c, tx), width - 2);   // (columns past the width repeat the last ones and are not stored)
+      const float2 x0 = *reinterpret_cast<const float2*>(at), x1 = *reinterpret_cast<const float2*>(at + pitch);
+      const float2 x2 = *reinterpret_cast<const float2*>(at + 2 * pitch), x3 = *reinterpret_cast<const float2*>(at + 3 * pitch);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        part[i][c] = fmaf(a[i].w, x3, fmaf(a[i].z, x2, fmaf(a[i].y, x1, fmaf(a[i].x, x0, part[i][c]))));
+      for (int i = 0; i < RI; ++i) {
+        part[i][c] = fmaf(a[i].w, x3.x, fmaf(a[i].z, x2.x, fmaf(a[i].y, x1.x, fmaf(a[i].x, x0.x, part[i][c]))));
+        part[i][c + 1] = fmaf(a[i].w, x3.y, fmaf(a[i].z, x2.y, fmaf(a[i].y, x1.y, fmaf(a[i].x, x0.y, part[i][c + 1]))));
+      }
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < RI; ++i)
 #pragma unroll
     for (int c = 0; c < NC; ++c) sum[i][c] += part[i][c];
 }
 
-// Bias of a distance >= 0 in the base-2 domain: ALiBi's slope or the table's entry.
-__device__ __forceinline__ float bias_of(const TrainParams& p, const HeadInfo& hd, int h, int distance) {
-  if (p.bias != nullptr) return __ldg(p.bias + static_cast<int64_t>(h) * p.bias_len + min(max(distance, 0), p.bias_len - 1));
-  return -hd.alibi_slope2 * static_cast<float>(distance);
+// Bias in the base-2 domain (ALiBi's slope or the table's entry) of the kOwn + kWalk - 1 distances of a pair of tiles, from
+// `first` on; -infinity where the key comes after the query.
+__device__ __forceinline__ void fetch_bias(float* dst, const TrainParams& p, const HeadInfo& hd, int h, int first, int tid) {
+  const int x = first + tid;
+  if (tid < kOwn + kWalk)
+    dst[tid] = x < 0 ? -INFINITY
+               : p.bias != nullptr ? __ldg(p.bias + static_cast<int64_t>(h) * p.bias_len + min(x, p.bias_len - 1))
+                                   : -hd.alibi_slope2 * static_cast<float>(x);
 }
 // 2^(s scale + bias - m).  The maximum comes off inside the multiply-add: what is rounded is the difference, which is small
 // where the weight counts.
@@ -132,49 +161,67 @@ __device__ __forceinline__ int64_t v_at(const TrainParams& p, const HeadInfo& hd
 template <int NC>
 __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
+  __shared__ float bias_of[2][kOwn + kWalk];
   const Unit u = query_unit(p, blockIdx.x);
   const HeadInfo hd = p.heads[u.h];
-  const int tile = gridDim.y - 1 - blockIdx.y, i0 = tile * kRows;        // long rows first
+  const int tile = gridDim.y - 1 - blockIdx.y, i0 = tile * kOwn;         // long rows first
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  const int rk = hd.rp_k, rv = hd.rp_v, n = tokens_of(p, u.b);
+  const int rk = hd.rp_k, rv = hd.rp_v, n = tokens_of(p, u.b), rows = max(0, min(kOwn, n - i0)), end = rows > 0 ? i0 + rows : 0;
   if (blockIdx.x == 0 && blockIdx.y == 0)
     for (int b = tid; b < p.B; b += kThreads) p.lens[b] = tokens_of(p, b);
+  const int k_tile = kWalk * (rk + 4), v_tile = kWalk * (rv + 4);
   float* Qs = sm;
-  float* Ks = Qs + kRows * (rk + 4);
-  float* Vs = Ks + kRows * (rk + 4);
-  float* Ps = Vs + kRows * (rv + 4);
-  const int64_t q_stride = static_cast<int64_t>(p.group) * p.lr_k_width, o_stride = static_cast<int64_t>(p.group) * p.lr_v_width;
+  float* Ks = Qs + kOwn * (rk + 4);
+  float* Vs = Ks + 2 * k_tile;
+  float* Ps = Vs + 2 * v_tile;
+  const int64_t q_stride = static_cast<int64_t>(p.group) * p.lr_k_width;
   const float *q = static_cast<const float*>(p.q), *k = static_cast<const float*>(p.k), *v = static_cast<const float*>(p.v);
-  load_rows(Qs, q + q_at(p, hd, u, i0), q_stride, max(0, min(kRows, n - i0)), rk, hd.r_k, tid, p.q_copy + q_at(p, hd, u, i0));
-  if (u.i == 0) {                                            // one query head of the group keeps the keys and values
-    load_rows(Ks, k + k_at(p, hd, u.b, i0), p.lr_k_width, max(0, min(kRows, n - i0)), rk, hd.r_k, tid, p.k_copy + k_at(p, hd, u.b, i0));
-    load_rows(Vs, v + v_at(p, hd, u.b, i0), p.lr_v_width, max(0, min(kRows, n - i0)), rv, hd.r_v, tid, p.v_copy + v_at(p, hd, u.b, i0));
+  const bool wide_k = on16(k), wide_v = on16(v);
+  auto fetch = [&](int j0) {
+    const int buf = (j0 / kWalk) & 1;
+    fetch_rows<kWalk>(Ks + buf * k_tile, k + k_at(p, hd, u.b, j0), p.lr_k_width, n - j0, rk, hd.r_k, wide_k, tid);
+    fetch_rows<kWalk>(Vs + buf * v_tile, v + v_at(p, hd, u.b, j0), p.lr_v_width, n - j0, rv, hd.r_v, wide_v, tid);
+    fetch_bias(bias_of[buf], p, hd, u.h, i0 - j0 - (kWalk - 1), tid);
+  };
+  if (rows > 0) {
+    fetch_rows<kOwn>(Qs, q + q_at(p, hd, u, i0), q_stride, rows, rk, hd.r_k, on16(q), tid);
+    if (u.i == 0) {                                          // one query head of the group keeps the keys and values
+      fetch_rows<kOwn>(Ks + k_tile, k + k_at(p, hd, u.b, i0), p.lr_k_width, rows, rk, hd.r_k, wide_k, tid);
+      fetch_rows<kOwn>(Vs + v_tile, v + v_at(p, hd, u.b, i0), p.lr_v_width, rows, rv, hd.r_v, wide_v, tid);
+    }
+    fetch(0);
+    tc::cp_async_commit();
+    tc::cp_async_wait<0>();
+    __syncthreads();
+    keep_rows(p.q_copy + q_at(p, hd, u, i0), Qs, q_stride, rows, rk, tid);
+    if (u.i == 0) {
+      keep_rows(p.k_copy + k_at(p, hd, u.b, i0), Ks + k_tile, p.lr_k_width, rows, rk, tid);
+      keep_rows(p.v_copy + v_at(p, hd, u.b, i0), Vs + v_tile, p.lr_v_width, rows, rv, tid);
+    }
   }
-  float m[4], l[4], o[4][NC];
+  float m[RI], l[RI], o[RI][NC];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < RI; ++i) {
     m[i] = -INFINITY;
     l[i] = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) o[i][c] = 0.f;
   }
-  for (int j0 = 0; j0 <= i0 && i0 < n; j0 += kRows) {
-    __syncthreads();
-    load_rows(Ks, k + k_at(p, hd, u.b, j0), p.lr_k_width, min(kRows, n - j0), rk, hd.r_k, tid);
-    load_rows(Vs, v + v_at(p, hd, u.b, j0), p.lr_v_width, min(kRows, n - j0), rv, hd.r_v, tid);
-    __syncthreads();
-    float s[4][4];
-    product_nt(s, Qs, Ks, rk, ty, tx);
+  for (int j0 = 0; j0 < end; j0 += kWalk) {
+    const int buf = (j0 / kWalk) & 1;
+    tc::cp_async_wait<0>();
+    __syncthreads();                                         // this tile is there, the one before is done with
+    if (j0 + kWalk < end) fetch(j0 + kWalk);
+    tc::cp_async_commit();
+    float s[RI][4];
+    product_nt(s, Qs, Ks + buf * k_tile, rk, ty, tx);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = i0 + ty + 16 * i;
+    for (int i = 0; i < RI; ++i) {
       float top = m[i], bias[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int key = j0 + tx + 16 * j;
-        const bool open = row < n && key <= row;
-        bias[j] = open ? bias_of(p, hd, u.h, row - key) : -INFINITY;
-        if (open) top = fmaxf(top, fmaf(s[i][j], p.scale_log2, bias[j]));
+        bias[j] = bias_of[buf][ty + 16 * i - tx - 16 * j + kWalk - 1];
+        if (bias[j] != -INFINITY) top = fmaxf(top, fmaf(s[i][j], p.scale_log2, bias[j]));
         else s[i][j] = 0.f;
       }
 #pragma unroll
@@ -194,13 +241,13 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
 #pragma unroll
       for (int c = 0; c < NC; ++c) o[i][c] *= keep;
     }
-    __syncthreads();
-    product_nn<NC>(o, Ps, Vs, rv, ty, tx);
+    __syncwarp();                                            // (a warp reads the rows that it wrote)
+    product_nn<NC>(o, Ps, Vs + buf * v_tile, rv, ty, tx);
   }
   float* out = static_cast<float*>(p.out);
   const int64_t stat = static_cast<int64_t>(blockIdx.x) * p.pad, all = static_cast<int64_t>(gridDim.x) * p.pad;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < RI; ++i) {
     const int row = i0 + ty + 16 * i;
     if (row >= p.T) continue;
     const float inv = row < n ? 1.f / l[i] : 0.f;
@@ -210,7 +257,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int col = tx + 16 * c;
+      const int col = column(c, tx);
       if (col >= rv) continue;
       const float x = row < n ? o[i][c] * inv : 0.f;
       out[o_at(p, hd, u, row) + col] = x;
@@ -219,184 +266,222 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
   }
 }
 
-// P (or its transpose) of a score tile, from the statistics of its rows
-__device__ __forceinline__ float probability(const TrainParams& p, const HeadInfo& hd, int h, float s, int row, int key, int n,
-                                             float m, float inv) {
-  return row < n && key <= row ? weight(s, p.scale_log2, bias_of(p, hd, h, row - key), m) * inv : 0.f;
+// P of a score, from the statistics of its row
+__device__ __forceinline__ float probability(float s, float scale, float bias, float m, float inv) {
+  return bias != -INFINITY ? weight(s, scale, bias, m) * inv : 0.f;
 }
 
 // dq' of a tile of query rows; also their delta, and this tile's share of the bias gradient.
 template <int NC>
 __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
-  __shared__ float stats[3][kRows];                          // maximum, reciprocal sum, delta
-  __shared__ float diagonal[2 * kRows];
+  __shared__ float stats[3][kOwn];                           // maximum, reciprocal sum, delta
+  __shared__ float bias_of[2][kOwn + kWalk], diagonal[kOwn + kWalk];
+  __shared__ double by_bucket[kMaxBuckets];
   const Unit u = query_unit(p, blockIdx.x);
   const HeadInfo hd = p.heads[u.h];
-  const int tile = gridDim.y - 1 - blockIdx.y, i0 = tile * kRows;
+  const int tile = gridDim.y - 1 - blockIdx.y, i0 = tile * kOwn;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  const int rk = hd.rp_k, rv = hd.rp_v, n = __ldg(p.lens + u.b), rows = max(0, min(kRows, n - i0));
+  const int rk = hd.rp_k, rv = hd.rp_v, n = __ldg(p.lens + u.b), rows = max(0, min(kOwn, n - i0)), end = rows > 0 ? i0 + rows : 0;
+  const int k_tile = kWalk * (rk + 4), v_tile = kWalk * (rv + 4);
   float* Qs = sm;
-  float* Gs = Qs + kRows * (rk + 4);
-  float* Ks = Gs + kRows * (rv + 4);
-  float* Vs = Ks + kRows * (rk + 4);
-  float* Ps = Vs + kRows * (rv + 4);
+  float* Gs = Qs + kOwn * (rk + 4);
+  float* Ks = Gs + kOwn * (rv + 4);
+  float* Vs = Ks + 2 * k_tile;
+  float* Ps = Vs + 2 * v_tile;
   const int64_t stat = static_cast<int64_t>(blockIdx.x) * p.pad, all = static_cast<int64_t>(gridDim.x) * p.pad;
-  load_rows(Qs, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, rows, rk, hd.r_k, tid);
-  load_rows(Gs, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v, tid);
+  auto fetch = [&](int j0) {
+    const int buf = (j0 / kWalk) & 1;
+    fetch_rows<kWalk>(Ks + buf * k_tile, p.k_copy + k_at(p, hd, u.b, j0), p.lr_k_width, n - j0, rk, hd.r_k, true, tid);
+    fetch_rows<kWalk>(Vs + buf * v_tile, p.v_copy + v_at(p, hd, u.b, j0), p.lr_v_width, n - j0, rv, hd.r_v, true, tid);
+    fetch_bias(bias_of[buf], p, hd, u.h, i0 - j0 - (kWalk - 1), tid);
+  };
+  if (rows > 0) {
+    fetch_rows<kOwn>(Qs, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, rows, rk, hd.r_k, true, tid);
+    fetch_rows<kOwn>(Gs, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v,
+                     on16(p.d_out), tid);
+    fetch(0);
+    tc::cp_async_commit();
+    tc::cp_async_wait<0>();
+  }
+  if (p.dtable != nullptr && tid < p.buckets) by_bucket[tid] = 0;
   __syncthreads();
-  for (int r = tid >> 2; r < kRows; r += kThreads / 4) {     // four threads for a row of do' o'
+  {
+    const int r = tid >> 3;                                  // eight threads for a row of do' o'
     float sum = 0.f;
     if (r < rows) {
       const float* o = p.o + (static_cast<int64_t>(blockIdx.x) * p.T + i0 + r) * p.o_stride;
-      for (int c = tid & 3; c < hd.r_v; c += 4) sum = fmaf(Gs[r * (rv + 4) + c], o[c], sum);
+      for (int c = tid & 7; c < hd.r_v; c += 8) sum = fmaf(Gs[r * (rv + 4) + c], o[c], sum);
     }
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    if ((tid & 3) == 0) {
+    sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+    if ((tid & 7) == 0) {
       stats[0][r] = r < rows ? p.lse[stat + i0 + r] : INFINITY;
       stats[1][r] = r < rows ? p.lse[all + stat + i0 + r] : 0.f;
       stats[2][r] = sum;
       if (i0 + r < p.T) p.delta[stat + i0 + r] = sum;
     }
   }
-  float dq[4][NC];
+  float dq[RI][NC];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < RI; ++i)
 #pragma unroll
     for (int c = 0; c < NC; ++c) dq[i][c] = 0.f;
-  double by_bucket = 0;                                      // thread u < buckets: bucket u
-  for (int j0 = 0; j0 <= i0 && i0 < n; j0 += kRows) {
-    __syncthreads();
-    load_rows(Ks, p.k_copy + k_at(p, hd, u.b, j0), p.lr_k_width, min(kRows, n - j0), rk, hd.r_k, tid);
-    load_rows(Vs, p.v_copy + v_at(p, hd, u.b, j0), p.lr_v_width, min(kRows, n - j0), rv, hd.r_v, tid);
-    __syncthreads();
-    float s[4][4], g[4][4];
-    product_nt(s, Qs, Ks, rk, ty, tx);
-    product_nt(g, Gs, Vs, rv, ty, tx);
+  for (int j0 = 0; j0 < end; j0 += kWalk) {
+    const int buf = (j0 / kWalk) & 1;
+    tc::cp_async_wait<0>();
+    __syncthreads();                                         // this tile is there, the one before is done with
+    if (j0 + kWalk < end) fetch(j0 + kWalk);
+    tc::cp_async_commit();
+    float s[RI][4], g[RI][4];
+    product_nt(s, Qs, Ks + buf * k_tile, rk, ty, tx);
+    product_nt(g, Gs, Vs + buf * v_tile, rv, ty, tx);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RI; ++i) {
       const int r = ty + 16 * i;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float pr = probability(p, hd, u.h, s[i][j], i0 + r, j0 + tx + 16 * j, n, stats[0][r], stats[1][r]);
+        const float pr = probability(s[i][j], p.scale_log2, bias_of[buf][r - tx - 16 * j + kWalk - 1], stats[0][r], stats[1][r]);
         Ps[r * kPitchP + tx + 16 * j] = pr * (g[i][j] - stats[2][r]);
       }
     }
-    __syncthreads();
-    product_nn<NC>(dq, Ps, Ks, rk, ty, tx);
+    __syncwarp();                                            // (a warp reads the rows that it wrote)
+    product_nn<NC>(dq, Ps, Ks + buf * k_tile, rk, ty, tx);
     if (p.dtable != nullptr) {
-      // sums along the diagonals, i.e. over equal distances; then each bucket's distances, in their order
-      if (tid < 2 * kRows - 1) {
+      // sums along the diagonals, i.e. over equal distances; then each bucket's distances by a warp, in a fixed order
+      __syncthreads();
+      if (tid < kOwn + kWalk - 1) {
         float sum = 0.f;
-        const int d = tid - (kRows - 1);                     // row - column
-        for (int r = max(0, d); r < min(kRows, kRows + d); ++r) sum += Ps[r * kPitchP + r - d];
+        const int d = tid - (kWalk - 1);                     // row - column
+#pragma unroll 4
+        for (int r = max(0, d); r < min(kOwn, kWalk + d); ++r) sum += Ps[r * kPitchP + r - d];
         diagonal[tid] = sum;
       }
       __syncthreads();
-      if (tid < p.buckets) {
-        const int shift = i0 - j0 - (kRows - 1);             // distance of diagonal[0]
-        const int64_t from = static_cast<int64_t>(__ldg(p.starts + tid)) - shift, to = static_cast<int64_t>(__ldg(p.starts + tid + 1)) - shift;
-        for (int d = static_cast<int>(max(static_cast<long long>(from), 0ll)); d < min(static_cast<long long>(to), 2ll * kRows - 1); ++d)
-          by_bucket += diagonal[d];
+      const int shift = i0 - j0 - (kWalk - 1), lane = tid & 31;          // distance of diagonal[0]
+      for (int b = tid >> 5; b < p.buckets; b += kThreads / 32) {
+        const int first = __ldg(p.starts + b), behind = __ldg(p.starts + b + 1);
+        if (first > shift + kOwn + kWalk - 2 || behind <= shift) continue;
+        const int from = max(first - shift, 0), to = behind > shift + kOwn + kWalk - 1 ? kOwn + kWalk - 1 : behind - shift;
+        double sum = 0;
+        for (int d = from + lane; d < to; d += 32) sum += diagonal[d];
+#pragma unroll
+        for (int x = 16; x >= 1; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+        if (lane == 0) by_bucket[b] += sum;
       }
     }
   }
   float* out = static_cast<float*>(p.dq);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < RI; ++i) {
     const int row = i0 + ty + 16 * i;
     if (row >= p.T) continue;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
-      if (tx + 16 * c < rk) out[q_at(p, hd, u, row) + tx + 16 * c] = dq[i][c] * p.scale;
+      if (column(c, tx) < rk) out[q_at(p, hd, u, row) + column(c, tx)] = dq[i][c] * p.scale;
   }
+  __syncthreads();
   if (p.dtable != nullptr && tid < p.buckets)                // (group 1: a head's units are its sequences)
-    p.bias_part[(static_cast<int64_t>(blockIdx.x) * gridDim.y + tile) * p.buckets + tid] = static_cast<float>(by_bucket);
+    p.bias_part[(static_cast<int64_t>(blockIdx.x) * gridDim.y + tile) * p.buckets + tid] = static_cast<float>(by_bucket[tid]);
 }
 
 // dk', dv' of a tile of keys: the query rows of every query head of the group.
 template <int NC>
 __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
-  __shared__ float stats[3][kRows];
+  __shared__ float stats[2][3][kWalk], bias_of[2][kOwn + kWalk];
   const int h = blockIdx.x / p.B, b = blockIdx.x - h * p.B;
   const HeadInfo hd = p.heads[h];
-  const int j0 = blockIdx.y * kRows;                         // the first keys have the most queries
+  const int j0 = blockIdx.y * kOwn;                          // the first keys have the most queries
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  const int rk = hd.rp_k, rv = hd.rp_v, n = __ldg(p.lens + b);
+  const int rk = hd.rp_k, rv = hd.rp_v, n = __ldg(p.lens + b), rows = max(0, min(kOwn, n - j0));
+  const int k_tile = kWalk * (rk + 4), v_tile = kWalk * (rv + 4);
   float* Ks = sm;
-  float* Vs = Ks + kRows * (rk + 4);
-  float* Qs = Vs + kRows * (rv + 4);
-  float* Gs = Qs + kRows * (rk + 4);
-  float* Ps = Gs + kRows * (rv + 4);
-  load_rows(Ks, p.k_copy + k_at(p, hd, b, j0), p.lr_k_width, max(0, min(kRows, n - j0)), rk, hd.r_k, tid);
-  load_rows(Vs, p.v_copy + v_at(p, hd, b, j0), p.lr_v_width, max(0, min(kRows, n - j0)), rv, hd.r_v, tid);
-  float dk[4][NC], dv[4][NC];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) dk[i][c] = dv[i][c] = 0.f;
+  float* Vs = Ks + kOwn * (rk + 4);
+  float* Qs = Vs + kOwn * (rv + 4);
+  float* Gs = Qs + 2 * k_tile;
+  float* Ps = Gs + 2 * v_tile;
   const int64_t all = static_cast<int64_t>(p.H) * p.group * p.B * p.pad;
-  for (int i = 0; i < p.group; ++i) {
+  const int per_head = (n - j0 + kWalk - 1) / kWalk, total = rows > 0 ? p.group * per_head : 0;
+  const bool wide_g = on16(p.d_out);
+  auto fetch = [&](int t) {                                  // tile t of all the group's
+    const int buf = t & 1, i = t / per_head, i0 = j0 + (t - i * per_head) * kWalk;
     const Unit u = {h, i, b};
     const int64_t stat = (static_cast<int64_t>(h * p.group + i) * p.B + b) * p.pad;
-    for (int i0 = j0; i0 < n; i0 += kRows) {
-      const int rows = min(kRows, n - i0);
-      __syncthreads();
-      load_rows(Qs, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, rows, rk, hd.r_k, tid);
-      load_rows(Gs, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v, tid);
-      if (tid < kRows) {
-        stats[0][tid] = tid < rows ? p.lse[stat + i0 + tid] : INFINITY;
-        stats[1][tid] = tid < rows ? p.lse[all + stat + i0 + tid] : 0.f;
-        stats[2][tid] = tid < rows ? p.delta[stat + i0 + tid] : 0.f;
-      }
-      __syncthreads();
-      float s[4][4], g[4][4];
-      product_nt(s, Ks, Qs, rk, ty, tx);
-#pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int r = tx + 16 * c;
-          s[a][c] = probability(p, hd, h, s[a][c], i0 + r, j0 + ty + 16 * a, n, stats[0][r], stats[1][r]);
-          Ps[(ty + 16 * a) * kPitchP + r] = s[a][c];
-        }
-      product_nt(g, Vs, Gs, rv, ty, tx);
-      __syncthreads();
-      product_nn<NC>(dv, Ps, Gs, rv, ty, tx);
-      __syncthreads();
-#pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          Ps[(ty + 16 * a) * kPitchP + tx + 16 * c] = s[a][c] * (g[a][c] - stats[2][tx + 16 * c]);
-      __syncthreads();
-      product_nn<NC>(dk, Ps, Qs, rk, ty, tx);
+    fetch_rows<kWalk>(Qs + buf * k_tile, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, n - i0, rk, hd.r_k, true, tid);
+    fetch_rows<kWalk>(Gs + buf * v_tile, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, n - i0, rv,
+                      hd.r_v, wide_g, tid);
+    if (tid < kWalk) {
+      const bool there = i0 + tid < n;
+      stats[buf][0][tid] = there ? p.lse[stat + i0 + tid] : INFINITY;
+      stats[buf][1][tid] = there ? p.lse[all + stat + i0 + tid] : 0.f;
+      stats[buf][2][tid] = there ? p.delta[stat + i0 + tid] : 0.f;
     }
+    fetch_bias(bias_of[buf], p, hd, h, i0 - j0 - (kOwn - 1), tid);
+  };
+  float dk[RI][NC], dv[RI][NC];
+#pragma unroll
+  for (int i = 0; i < RI; ++i)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) dk[i][c] = dv[i][c] = 0.f;
+  if (total > 0) {
+    fetch_rows<kOwn>(Ks, p.k_copy + k_at(p, hd, b, j0), p.lr_k_width, rows, rk, hd.r_k, true, tid);
+    fetch_rows<kOwn>(Vs, p.v_copy + v_at(p, hd, b, j0), p.lr_v_width, rows, rv, hd.r_v, true, tid);
+    fetch(0);
+    tc::cp_async_commit();
+  }
+  for (int t = 0; t < total; ++t) {
+    const int buf = t & 1;
+    tc::cp_async_wait<0>();
+    __syncthreads();                                         // this tile is there, the one before is done with
+    if (t + 1 < total) fetch(t + 1);
+    tc::cp_async_commit();
+    float s[RI][4], g[RI][4];
+    product_nt(s, Ks, Qs + buf * k_tile, rk, ty, tx);
+#pragma unroll
+    for (int a = 0; a < RI; ++a)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int r = tx + 16 * c, key = ty + 16 * a;
+        s[a][c] = probability(s[a][c], p.scale_log2, bias_of[buf][r - key + kOwn - 1], stats[buf][0][r], stats[buf][1][r]);
+        Ps[key * kPitchP + r] = s[a][c];
+      }
+    product_nt(g, Vs, Gs + buf * v_tile, rv, ty, tx);
+    __syncwarp();                                            // (a warp reads the rows that it wrote)
+    product_nn<NC>(dv, Ps, Gs + buf * v_tile, rv, ty, tx);
+    __syncwarp();
+#pragma unroll
+    for (int a = 0; a < RI; ++a)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        Ps[(ty + 16 * a) * kPitchP + tx + 16 * c] = s[a][c] * (g[a][c] - stats[buf][2][tx + 16 * c]);
+    __syncwarp();
+    product_nn<NC>(dk, Ps, Qs + buf * k_tile, rk, ty, tx);
   }
   float *out_k = static_cast<float*>(p.dk), *out_v = static_cast<float*>(p.dv);
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
+  for (int a = 0; a < RI; ++a) {
     const int key = j0 + ty + 16 * a;
     if (key >= p.T) continue;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int col = tx + 16 * c;
+      const int col = column(c, tx);
       if (col < rk) out_k[k_at(p, hd, b, key) + col] = dk[a][c] * p.scale;
       if (col < rv) out_v[v_at(p, hd, b, key) + col] = dv[a][c];
     }
   }
 }
 
-size_t smem_bytes(const TrainParams& p, int key_tiles, int value_tiles) {
-  return (static_cast<size_t>(kRows) * (key_tiles * (p.max_rp_k + 4) + value_tiles * (p.max_rp_v + 4)) + kRows * kPitchP) * sizeof(float);
+size_t smem_bytes(const TrainParams& p, bool both) {
+  const size_t k = p.max_rp_k + 4, v = p.max_rp_v + 4;
+  return (kOwn * (k + (both ? v : 0)) + 2 * kWalk * (k + v) + kOwn * kPitchP) * sizeof(float);
 }
 
 template <int NC>
 cudaError_t forward_t(const TrainParams& p, cudaStream_t s) {
   static size_t done[kMaxDevices] = {};
-  const size_t smem = smem_bytes(p, 2, 1);
+  const size_t smem = smem_bytes(p, false);
   const cudaError_t e = ensure_dynamic_smem(train_simt_forward_kernel<NC>, smem, done);
   if (e != cudaSuccess) return e;
   train_simt_forward_kernel<NC><<<dim3(p.H * p.group * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
@@ -405,7 +490,7 @@ cudaError_t forward_t(const TrainParams& p, cudaStream_t s) {
 template <int NC>
 cudaError_t backward_t(const TrainParams& p, cudaStream_t s) {
   static size_t done_q[kMaxDevices] = {}, done_kv[kMaxDevices] = {};
-  const size_t smem = smem_bytes(p, 2, 2);
+  const size_t smem = smem_bytes(p, true);
   cudaError_t e = ensure_dynamic_smem(train_simt_dq_kernel<NC>, smem, done_q);
   if (e == cudaSuccess) e = ensure_dynamic_smem(train_simt_dkv_kernel<NC>, smem, done_kv);
   if (e != cudaSuccess) return e;
@@ -416,7 +501,7 @@ cudaError_t backward_t(const TrainParams& p, cudaStream_t s) {
 
 }  // namespace
 
-int train_simt_tiles(int T) { return (T + kRows - 1) / kRows; }
+int train_simt_tiles(int T) { return (T + kOwn - 1) / kOwn; }
 
 // Columns of a thread by the widest rank: 32, 64 or 128 columns over 16 threads (a rank of 40 in the widest instance would
 // spend three quarters of its multiply-adds on columns that are not there).
