@@ -4,10 +4,13 @@
 //   dq'_i = scale sum_j dS_ij k'_j,  dk'_j = scale sum_i dS_ij q'_i,  dv'_j = sum_i P_ij do'_i,  db_u = sum dS_ij over the
 //   distances of bucket u
 // P is recomputed from the row's maximum and the reciprocal of its sum, which the forward pass leaves: their logarithm, one
-// number, would cost the exponent's last bits.  A CTA has a tile of 64 query (or key) rows and walks the other axis in tiles
-// of 64; a thread has 4 x 4 scores and 4 rows x 8 columns of the sums.  dq' and dk', dv' are two kernels, so that nothing is
-// added up by atomics.  A tile's products are summed apart and then added, which keeps the rounding errors of long sums down.
-// Bound by the loads from shared memory (two for eight multiply-adds in the score products): figures in the table of cases.
+// number, would cost the exponent's last bits.  A CTA has a tile of 32 query (or key) rows and walks the other axis in tiles
+// of 64, fetched one ahead; a thread has 2 x 4 scores and 2 rows x 2 to 8 columns of the sums.  dq' and dk', dv' are two
+// kernels, so that nothing is added up by atomics.  A tile's products are summed apart and then added, which keeps the rounding
+// errors of long sums down.  Bound by the latency of the shared-memory reads in front of the multiply-adds (2 x 500 tokens,
+// 8 heads of rank 40: forward 49, dq' 60, dk' and dv' 57 us; own tiles of 64 rows, half as many CTAs, took 95, 128 and 136).
+// The loops are unrolled for registers, not for CTAs: with the compiler's own choice, 128 registers and two CTAs per SM, the
+// three took 188 us, with one CTA and its loads four steps ahead 159.
 #include "internal.h"
 #include "tc_common.cuh"
 
@@ -19,6 +22,7 @@ constexpr int kWalk = 64;                 // rows of a tile of the walked axis
 constexpr int kThreads = 256;
 constexpr int kPitchP = kWalk + 4;
 constexpr int RI = kOwn / 16;             // own rows of a thread
+template <int NC> constexpr int kPitch = 16 * NC + 4;        // of rows in shared memory, for NC columns a thread
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -26,9 +30,9 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// Packed rows on their way into shared memory (pitch = width + 4), zeros behind `rows`; columns from `live` on are the rank's
+// Packed rows on their way into shared memory, zeros behind `rows`; columns from `live` on are the rank's
 // padding: zeros, whatever the caller left there.  wide: the rows lie on 16-byte boundaries.
-template <int COUNT>
+template <int COUNT, int PITCH>
 __device__ __forceinline__ void fetch_rows(float* dst, const float* src, int64_t stride, int rows, int width, int live, bool wide, int tid) {
   const uint32_t to = tc::smem_u32(dst);
   if (wide) {
@@ -37,41 +41,42 @@ __device__ __forceinline__ void fetch_rows(float* dst, const float* src, int64_t
       const int r = idx / quads, c = 4 * (idx - r * quads);
       const int bytes = r < rows ? 4 * min(max(live - c, 0), 4) : 0;
       const float* from = bytes > 0 ? src + r * stride + c : src;
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 4 * (r * (width + 4) + c)), "l"(from), "r"(bytes) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 4 * (r * PITCH + c)), "l"(from), "r"(bytes) : "memory");
     }
   } else {
     for (int idx = tid; idx < COUNT * width; idx += kThreads) {
       const int r = idx / width, c = idx - r * width;
       const int bytes = r < rows && c < live ? 4 : 0;
       const float* from = bytes > 0 ? src + r * stride + c : src;
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * (r * (width + 4) + c)), "l"(from), "r"(bytes) : "memory");
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * (r * PITCH + c)), "l"(from), "r"(bytes) : "memory");
     }
   }
 }
 // The rows of this CTA's own tile, kept for the backward pass.
+template <int PITCH>
 __device__ __forceinline__ void keep_rows(float* dst, const float* src, int64_t stride, int rows, int width, int tid) {
   const int quads = width >> 2;
   for (int idx = tid; idx < rows * quads; idx += kThreads) {
     const int r = idx / quads, c = 4 * (idx - r * quads);
-    *reinterpret_cast<float4*>(dst + r * stride + c) = *reinterpret_cast<const float4*>(src + r * (width + 4) + c);
+    *reinterpret_cast<float4*>(dst + r * stride + c) = *reinterpret_cast<const float4*>(src + r * PITCH + c);
   }
 }
 __device__ __forceinline__ bool on16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }
 
 // s[i][j] = sum_c a[ty + 16 i][c] b[tx + 16 j][c]
+template <int PITCH>
 __device__ __forceinline__ void product_nt(float (&s)[RI][4], const float* a, const float* b, int width, int ty, int tx) {
-  const int pitch = width + 4;
 #pragma unroll
   for (int i = 0; i < RI; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-#pragma unroll 2
+#pragma unroll 4
   for (int c = 0; c < width; c += 4) {
     float4 x[RI], y[4];
 #pragma unroll
-    for (int i = 0; i < RI; ++i) x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * pitch + c);
+    for (int i = 0; i < RI; ++i) x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * PITCH + c);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(b + (tx + 16 * j) * pitch + c);
+    for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(b + (tx + 16 * j) * PITCH + c);
 #pragma unroll
     for (int i = 0; i < RI; ++i)
 #pragma unroll
@@ -88,24 +93,23 @@ __device__ __forceinline__ void product_nt(float (&s)[RI][4], const float* a, co
 __device__ __forceinline__ int column(int c, int tx) { return 32 * (c >> 1) + 2 * tx + (c & 1); }
 
 // sum[i][c] += sum_k w[ty + 16 i][k] x[k][column(c)], k = 0 .. 63
-template <int NC>
-__device__ __forceinline__ void product_nn(float (&sum)[RI][NC], const float* w, const float* x, int width, int ty, int tx) {
-  const int pitch = width + 4;
+template <int NC, int PITCH>
+__device__ __forceinline__ void product_nn(float (&sum)[RI][NC], const float* w, const float* x, int ty, int tx) {
   float part[RI][NC];
 #pragma unroll
   for (int i = 0; i < RI; ++i)
 #pragma unroll
     for (int c = 0; c < NC; ++c) part[i][c] = 0.f;
-#pragma unroll 2
+#pragma unroll 4
   for (int k = 0; k < kWalk; k += 4) {
     float4 a[RI];
 #pragma unroll
     for (int i = 0; i < RI; ++i) a[i] = *reinterpret_cast<const float4*>(w + (ty + 16 * i) * kPitchP + k);
 #pragma unroll
     for (int c = 0; c < NC; c += 2) {
-      const float* at = x + k * pitch + min(column(c, tx), width - 2);   // (columns past the width repeat the last ones and are not stored)
-      const float2 x0 = *reinterpret_cast<const float2*>(at), x1 = *reinterpret_cast<const float2*>(at + pitch);
-      const float2 x2 = *reinterpret_cast<const float2*>(at + 2 * pitch), x3 = *reinterpret_cast<const float2*>(at + 3 * pitch);
+      const float* at = x + k * PITCH + column(c, tx);         // (columns past the width hold anything and are not stored)
+      const float2 x0 = *reinterpret_cast<const float2*>(at), x1 = *reinterpret_cast<const float2*>(at + PITCH);
+      const float2 x2 = *reinterpret_cast<const float2*>(at + 2 * PITCH), x3 = *reinterpret_cast<const float2*>(at + 3 * PITCH);
 #pragma unroll
       for (int i = 0; i < RI; ++i) {
         part[i][c] = fmaf(a[i].w, x3.x, fmaf(a[i].z, x2.x, fmaf(a[i].y, x1.x, fmaf(a[i].x, x0.x, part[i][c]))));
@@ -159,7 +163,7 @@ __device__ __forceinline__ int64_t v_at(const TrainParams& p, const HeadInfo& hd
 }
 
 template <int NC>
-__global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const TrainParams p) {
+__global__ void __launch_bounds__(kThreads, 2) train_simt_forward_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
   __shared__ float bias_of[2][kOwn + kWalk];
   const Unit u = query_unit(p, blockIdx.x);
@@ -169,34 +173,34 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
   const int rk = hd.rp_k, rv = hd.rp_v, n = tokens_of(p, u.b), rows = max(0, min(kOwn, n - i0)), end = rows > 0 ? i0 + rows : 0;
   if (blockIdx.x == 0 && blockIdx.y == 0)
     for (int b = tid; b < p.B; b += kThreads) p.lens[b] = tokens_of(p, b);
-  const int k_tile = kWalk * (rk + 4), v_tile = kWalk * (rv + 4);
+  constexpr int kTile = kWalk * kPitch<NC>, kOwnTile = kOwn * kPitch<NC>;
   float* Qs = sm;
-  float* Ks = Qs + kOwn * (rk + 4);
-  float* Vs = Ks + 2 * k_tile;
-  float* Ps = Vs + 2 * v_tile;
+  float* Ks = Qs + kOwnTile;
+  float* Vs = Ks + 2 * kTile;
+  float* Ps = Vs + 2 * kTile;
   const int64_t q_stride = static_cast<int64_t>(p.group) * p.lr_k_width;
   const float *q = static_cast<const float*>(p.q), *k = static_cast<const float*>(p.k), *v = static_cast<const float*>(p.v);
   const bool wide_k = on16(k), wide_v = on16(v);
   auto fetch = [&](int j0) {
     const int buf = (j0 / kWalk) & 1;
-    fetch_rows<kWalk>(Ks + buf * k_tile, k + k_at(p, hd, u.b, j0), p.lr_k_width, n - j0, rk, hd.r_k, wide_k, tid);
-    fetch_rows<kWalk>(Vs + buf * v_tile, v + v_at(p, hd, u.b, j0), p.lr_v_width, n - j0, rv, hd.r_v, wide_v, tid);
+    fetch_rows<kWalk, kPitch<NC>>(Ks + buf * kTile, k + k_at(p, hd, u.b, j0), p.lr_k_width, n - j0, rk, hd.r_k, wide_k, tid);
+    fetch_rows<kWalk, kPitch<NC>>(Vs + buf * kTile, v + v_at(p, hd, u.b, j0), p.lr_v_width, n - j0, rv, hd.r_v, wide_v, tid);
     fetch_bias(bias_of[buf], p, hd, u.h, i0 - j0 - (kWalk - 1), tid);
   };
   if (rows > 0) {
-    fetch_rows<kOwn>(Qs, q + q_at(p, hd, u, i0), q_stride, rows, rk, hd.r_k, on16(q), tid);
+    fetch_rows<kOwn, kPitch<NC>>(Qs, q + q_at(p, hd, u, i0), q_stride, rows, rk, hd.r_k, on16(q), tid);
     if (u.i == 0) {                                          // one query head of the group keeps the keys and values
-      fetch_rows<kOwn>(Ks + k_tile, k + k_at(p, hd, u.b, i0), p.lr_k_width, rows, rk, hd.r_k, wide_k, tid);
-      fetch_rows<kOwn>(Vs + v_tile, v + v_at(p, hd, u.b, i0), p.lr_v_width, rows, rv, hd.r_v, wide_v, tid);
+      fetch_rows<kOwn, kPitch<NC>>(Ks + kTile, k + k_at(p, hd, u.b, i0), p.lr_k_width, rows, rk, hd.r_k, wide_k, tid);
+      fetch_rows<kOwn, kPitch<NC>>(Vs + kTile, v + v_at(p, hd, u.b, i0), p.lr_v_width, rows, rv, hd.r_v, wide_v, tid);
     }
     fetch(0);
     tc::cp_async_commit();
     tc::cp_async_wait<0>();
     __syncthreads();
-    keep_rows(p.q_copy + q_at(p, hd, u, i0), Qs, q_stride, rows, rk, tid);
+    keep_rows<kPitch<NC>>(p.q_copy + q_at(p, hd, u, i0), Qs, q_stride, rows, rk, tid);
     if (u.i == 0) {
-      keep_rows(p.k_copy + k_at(p, hd, u.b, i0), Ks + k_tile, p.lr_k_width, rows, rk, tid);
-      keep_rows(p.v_copy + v_at(p, hd, u.b, i0), Vs + v_tile, p.lr_v_width, rows, rv, tid);
+      keep_rows<kPitch<NC>>(p.k_copy + k_at(p, hd, u.b, i0), Ks + kTile, p.lr_k_width, rows, rk, tid);
+      keep_rows<kPitch<NC>>(p.v_copy + v_at(p, hd, u.b, i0), Vs + kTile, p.lr_v_width, rows, rv, tid);
     }
   }
   float m[RI], l[RI], o[RI][NC];
@@ -214,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
     if (j0 + kWalk < end) fetch(j0 + kWalk);
     tc::cp_async_commit();
     float s[RI][4];
-    product_nt(s, Qs, Ks + buf * k_tile, rk, ty, tx);
+    product_nt<kPitch<NC>>(s, Qs, Ks + buf * kTile, rk, ty, tx);
 #pragma unroll
     for (int i = 0; i < RI; ++i) {
       float top = m[i], bias[4];
@@ -242,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_forward_kernel(const Trai
       for (int c = 0; c < NC; ++c) o[i][c] *= keep;
     }
     __syncwarp();                                            // (a warp reads the rows that it wrote)
-    product_nn<NC>(o, Ps, Vs + buf * v_tile, rv, ty, tx);
+    product_nn<NC, kPitch<NC>>(o, Ps, Vs + buf * kTile, ty, tx);
   }
   float* out = static_cast<float*>(p.out);
   const int64_t stat = static_cast<int64_t>(blockIdx.x) * p.pad, all = static_cast<int64_t>(gridDim.x) * p.pad;
@@ -273,7 +277,7 @@ __device__ __forceinline__ float probability(float s, float scale, float bias, f
 
 // dq' of a tile of query rows; also their delta, and this tile's share of the bias gradient.
 template <int NC>
-__global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainParams p) {
+__global__ void __launch_bounds__(kThreads, 1) train_simt_dq_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
   __shared__ float stats[3][kOwn];                           // maximum, reciprocal sum, delta
   __shared__ float bias_of[2][kOwn + kWalk], diagonal[kOwn + kWalk];
@@ -283,22 +287,22 @@ __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainPara
   const int tile = gridDim.y - 1 - blockIdx.y, i0 = tile * kOwn;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int rk = hd.rp_k, rv = hd.rp_v, n = __ldg(p.lens + u.b), rows = max(0, min(kOwn, n - i0)), end = rows > 0 ? i0 + rows : 0;
-  const int k_tile = kWalk * (rk + 4), v_tile = kWalk * (rv + 4);
+  constexpr int kTile = kWalk * kPitch<NC>, kOwnTile = kOwn * kPitch<NC>;
   float* Qs = sm;
-  float* Gs = Qs + kOwn * (rk + 4);
-  float* Ks = Gs + kOwn * (rv + 4);
-  float* Vs = Ks + 2 * k_tile;
-  float* Ps = Vs + 2 * v_tile;
+  float* Gs = Qs + kOwnTile;
+  float* Ks = Gs + kOwnTile;
+  float* Vs = Ks + 2 * kTile;
+  float* Ps = Vs + 2 * kTile;
   const int64_t stat = static_cast<int64_t>(blockIdx.x) * p.pad, all = static_cast<int64_t>(gridDim.x) * p.pad;
   auto fetch = [&](int j0) {
     const int buf = (j0 / kWalk) & 1;
-    fetch_rows<kWalk>(Ks + buf * k_tile, p.k_copy + k_at(p, hd, u.b, j0), p.lr_k_width, n - j0, rk, hd.r_k, true, tid);
-    fetch_rows<kWalk>(Vs + buf * v_tile, p.v_copy + v_at(p, hd, u.b, j0), p.lr_v_width, n - j0, rv, hd.r_v, true, tid);
+    fetch_rows<kWalk, kPitch<NC>>(Ks + buf * kTile, p.k_copy + k_at(p, hd, u.b, j0), p.lr_k_width, n - j0, rk, hd.r_k, true, tid);
+    fetch_rows<kWalk, kPitch<NC>>(Vs + buf * kTile, p.v_copy + v_at(p, hd, u.b, j0), p.lr_v_width, n - j0, rv, hd.r_v, true, tid);
     fetch_bias(bias_of[buf], p, hd, u.h, i0 - j0 - (kWalk - 1), tid);
   };
   if (rows > 0) {
-    fetch_rows<kOwn>(Qs, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, rows, rk, hd.r_k, true, tid);
-    fetch_rows<kOwn>(Gs, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v,
+    fetch_rows<kOwn, kPitch<NC>>(Qs, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, rows, rk, hd.r_k, true, tid);
+    fetch_rows<kOwn, kPitch<NC>>(Gs, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, rows, rv, hd.r_v,
                      on16(p.d_out), tid);
     fetch(0);
     tc::cp_async_commit();
@@ -311,7 +315,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainPara
     float sum = 0.f;
     if (r < rows) {
       const float* o = p.o + (static_cast<int64_t>(blockIdx.x) * p.T + i0 + r) * p.o_stride;
-      for (int c = tid & 7; c < hd.r_v; c += 8) sum = fmaf(Gs[r * (rv + 4) + c], o[c], sum);
+      for (int c = tid & 7; c < hd.r_v; c += 8) sum = fmaf(Gs[r * kPitch<NC> + c], o[c], sum);
     }
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
@@ -335,8 +339,8 @@ __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainPara
     if (j0 + kWalk < end) fetch(j0 + kWalk);
     tc::cp_async_commit();
     float s[RI][4], g[RI][4];
-    product_nt(s, Qs, Ks + buf * k_tile, rk, ty, tx);
-    product_nt(g, Gs, Vs + buf * v_tile, rv, ty, tx);
+    product_nt<kPitch<NC>>(s, Qs, Ks + buf * kTile, rk, ty, tx);
+    product_nt<kPitch<NC>>(g, Gs, Vs + buf * kTile, rv, ty, tx);
 #pragma unroll
     for (int i = 0; i < RI; ++i) {
       const int r = ty + 16 * i;
@@ -347,7 +351,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainPara
       }
     }
     __syncwarp();                                            // (a warp reads the rows that it wrote)
-    product_nn<NC>(dq, Ps, Ks + buf * k_tile, rk, ty, tx);
+    product_nn<NC, kPitch<NC>>(dq, Ps, Ks + buf * kTile, ty, tx);
     if (p.dtable != nullptr) {
       // sums along the diagonals, i.e. over equal distances; then each bucket's distances by a warp, in a fixed order
       __syncthreads();
@@ -388,7 +392,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_dq_kernel(const TrainPara
 
 // dk', dv' of a tile of keys: the query rows of every query head of the group.
 template <int NC>
-__global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainParams p) {
+__global__ void __launch_bounds__(kThreads, 1) train_simt_dkv_kernel(const TrainParams p) {
   extern __shared__ __align__(16) float sm[];
   __shared__ float stats[2][3][kWalk], bias_of[2][kOwn + kWalk];
   const int h = blockIdx.x / p.B, b = blockIdx.x - h * p.B;
@@ -396,12 +400,12 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
   const int j0 = blockIdx.y * kOwn;                          // the first keys have the most queries
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int rk = hd.rp_k, rv = hd.rp_v, n = __ldg(p.lens + b), rows = max(0, min(kOwn, n - j0));
-  const int k_tile = kWalk * (rk + 4), v_tile = kWalk * (rv + 4);
+  constexpr int kTile = kWalk * kPitch<NC>, kOwnTile = kOwn * kPitch<NC>;
   float* Ks = sm;
-  float* Vs = Ks + kOwn * (rk + 4);
-  float* Qs = Vs + kOwn * (rv + 4);
-  float* Gs = Qs + 2 * k_tile;
-  float* Ps = Gs + 2 * v_tile;
+  float* Vs = Ks + kOwnTile;
+  float* Qs = Vs + kOwnTile;
+  float* Gs = Qs + 2 * kTile;
+  float* Ps = Gs + 2 * kTile;
   const int64_t all = static_cast<int64_t>(p.H) * p.group * p.B * p.pad;
   const int per_head = (n - j0 + kWalk - 1) / kWalk, total = rows > 0 ? p.group * per_head : 0;
   const bool wide_g = on16(p.d_out);
@@ -409,8 +413,8 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
     const int buf = t & 1, i = t / per_head, i0 = j0 + (t - i * per_head) * kWalk;
     const Unit u = {h, i, b};
     const int64_t stat = (static_cast<int64_t>(h * p.group + i) * p.B + b) * p.pad;
-    fetch_rows<kWalk>(Qs + buf * k_tile, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, n - i0, rk, hd.r_k, true, tid);
-    fetch_rows<kWalk>(Gs + buf * v_tile, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, n - i0, rv,
+    fetch_rows<kWalk, kPitch<NC>>(Qs + buf * kTile, p.q_copy + q_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_k_width, n - i0, rk, hd.r_k, true, tid);
+    fetch_rows<kWalk, kPitch<NC>>(Gs + buf * kTile, static_cast<const float*>(p.d_out) + o_at(p, hd, u, i0), static_cast<int64_t>(p.group) * p.lr_v_width, n - i0, rv,
                       hd.r_v, wide_g, tid);
     if (tid < kWalk) {
       const bool there = i0 + tid < n;
@@ -426,8 +430,8 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
 #pragma unroll
     for (int c = 0; c < NC; ++c) dk[i][c] = dv[i][c] = 0.f;
   if (total > 0) {
-    fetch_rows<kOwn>(Ks, p.k_copy + k_at(p, hd, b, j0), p.lr_k_width, rows, rk, hd.r_k, true, tid);
-    fetch_rows<kOwn>(Vs, p.v_copy + v_at(p, hd, b, j0), p.lr_v_width, rows, rv, hd.r_v, true, tid);
+    fetch_rows<kOwn, kPitch<NC>>(Ks, p.k_copy + k_at(p, hd, b, j0), p.lr_k_width, rows, rk, hd.r_k, true, tid);
+    fetch_rows<kOwn, kPitch<NC>>(Vs, p.v_copy + v_at(p, hd, b, j0), p.lr_v_width, rows, rv, hd.r_v, true, tid);
     fetch(0);
     tc::cp_async_commit();
   }
@@ -438,7 +442,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
     if (t + 1 < total) fetch(t + 1);
     tc::cp_async_commit();
     float s[RI][4], g[RI][4];
-    product_nt(s, Ks, Qs + buf * k_tile, rk, ty, tx);
+    product_nt<kPitch<NC>>(s, Ks, Qs + buf * kTile, rk, ty, tx);
 #pragma unroll
     for (int a = 0; a < RI; ++a)
 #pragma unroll
@@ -447,9 +451,9 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
         s[a][c] = probability(s[a][c], p.scale_log2, bias_of[buf][r - key + kOwn - 1], stats[buf][0][r], stats[buf][1][r]);
         Ps[key * kPitchP + r] = s[a][c];
       }
-    product_nt(g, Vs, Gs + buf * v_tile, rv, ty, tx);
+    product_nt<kPitch<NC>>(g, Vs, Gs + buf * kTile, rv, ty, tx);
     __syncwarp();                                            // (a warp reads the rows that it wrote)
-    product_nn<NC>(dv, Ps, Gs + buf * v_tile, rv, ty, tx);
+    product_nn<NC, kPitch<NC>>(dv, Ps, Gs + buf * kTile, ty, tx);
     __syncwarp();
 #pragma unroll
     for (int a = 0; a < RI; ++a)
@@ -457,7 +461,7 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
       for (int c = 0; c < 4; ++c)
         Ps[(ty + 16 * a) * kPitchP + tx + 16 * c] = s[a][c] * (g[a][c] - stats[buf][2][tx + 16 * c]);
     __syncwarp();
-    product_nn<NC>(dk, Ps, Qs + buf * k_tile, rk, ty, tx);
+    product_nn<NC, kPitch<NC>>(dk, Ps, Qs + buf * kTile, ty, tx);
   }
   float *out_k = static_cast<float*>(p.dk), *out_v = static_cast<float*>(p.dv);
 #pragma unroll
@@ -473,15 +477,14 @@ __global__ void __launch_bounds__(kThreads) train_simt_dkv_kernel(const TrainPar
   }
 }
 
-size_t smem_bytes(const TrainParams& p, bool both) {
-  const size_t k = p.max_rp_k + 4, v = p.max_rp_v + 4;
-  return (kOwn * (k + (both ? v : 0)) + 2 * kWalk * (k + v) + kOwn * kPitchP) * sizeof(float);
+constexpr size_t smem_bytes(int pitch, int own) {
+  return (static_cast<size_t>(pitch) * (own * kOwn + 4 * kWalk) + kOwn * kPitchP) * sizeof(float);
 }
 
 template <int NC>
 cudaError_t forward_t(const TrainParams& p, cudaStream_t s) {
   static size_t done[kMaxDevices] = {};
-  const size_t smem = smem_bytes(p, false);
+  const size_t smem = smem_bytes(kPitch<NC>, 1);
   const cudaError_t e = ensure_dynamic_smem(train_simt_forward_kernel<NC>, smem, done);
   if (e != cudaSuccess) return e;
   train_simt_forward_kernel<NC><<<dim3(p.H * p.group * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
@@ -490,7 +493,7 @@ cudaError_t forward_t(const TrainParams& p, cudaStream_t s) {
 template <int NC>
 cudaError_t backward_t(const TrainParams& p, cudaStream_t s) {
   static size_t done_q[kMaxDevices] = {}, done_kv[kMaxDevices] = {};
-  const size_t smem = smem_bytes(p, true);
+  const size_t smem = smem_bytes(kPitch<NC>, 2);
   cudaError_t e = ensure_dynamic_smem(train_simt_dq_kernel<NC>, smem, done_q);
   if (e == cudaSuccess) e = ensure_dynamic_smem(train_simt_dkv_kernel<NC>, smem, done_kv);
   if (e != cudaSuccess) return e;
@@ -503,17 +506,17 @@ cudaError_t backward_t(const TrainParams& p, cudaStream_t s) {
 
 int train_simt_tiles(int T) { return (T + kOwn - 1) / kOwn; }
 
-// Columns of a thread by the widest rank: 32, 64 or 128 columns over 16 threads (a rank of 40 in the widest instance would
-// spend three quarters of its multiply-adds on columns that are not there).
+// Columns of a thread by the widest rank: 32, 64, 96 or 128 columns over 16 threads (a rank of 40 in the widest instance would
+// spend two thirds of its multiply-adds on columns that are not there).
 cudaError_t launch_train_simt_forward(const TrainParams& p, cudaStream_t s, uint64_t* launches) {
   ++*launches;
   const int widest = p.max_rp_k > p.max_rp_v ? p.max_rp_k : p.max_rp_v;
-  return widest <= 32 ? forward_t<2>(p, s) : widest <= 64 ? forward_t<4>(p, s) : forward_t<8>(p, s);
+  return widest <= 32 ? forward_t<2>(p, s) : widest <= 64 ? forward_t<4>(p, s) : widest <= 96 ? forward_t<6>(p, s) : forward_t<8>(p, s);
 }
 cudaError_t launch_train_simt_backward(const TrainParams& p, cudaStream_t s, uint64_t* launches) {
   *launches += 2;
   const int widest = p.max_rp_k > p.max_rp_v ? p.max_rp_k : p.max_rp_v;
-  return widest <= 32 ? backward_t<2>(p, s) : widest <= 64 ? backward_t<4>(p, s) : backward_t<8>(p, s);
+  return widest <= 32 ? backward_t<2>(p, s) : widest <= 64 ? backward_t<4>(p, s) : widest <= 96 ? backward_t<6>(p, s) : backward_t<8>(p, s);
 }
 
 }  // namespace ea
