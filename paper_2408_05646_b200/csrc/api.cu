@@ -239,7 +239,7 @@ struct SparseLayout {
 
 // The caller's buffer of eigen_attn_train_attach.
 struct TrainLayout {
-  size_t lens = 0, o = 0, lse = 0, delta = 0, q = 0, k = 0, v = 0, g = 0, q_exp = 0, k_exp = 0, v_exp = 0, g_exp = 0, bias = 0, bytes = 0;
+  size_t lens = 0, o = 0, lse = 0, delta = 0, q = 0, k = 0, v = 0, g = 0, q_exp = 0, k_exp = 0, v_exp = 0, g_exp = 0, next = 0, bias = 0, bytes = 0;
 };
 
 }  // namespace
@@ -2075,6 +2075,7 @@ void make_train_layout(const eigen_attn* h, int tokens, int group, TrainLayout* 
     t->k_exp = area(units * tiles * sizeof(int32_t));
     t->v_exp = area(units * tiles * sizeof(int32_t));
     t->g_exp = area(q_units * tiles * sizeof(int32_t));
+    t->next = area(2 * sizeof(int32_t));
   } else {
     t->q = area(rows * group * h->L.sum_rp_k * sizeof(float));
     t->k = area(rows * h->L.sum_rp_k * sizeof(float));
@@ -2107,6 +2108,7 @@ void fill_train(eigen_attn_t h, int T, int group, ea::TrainParams* p) {
   } else {
     p->q_tiles = buf + t.q; p->k_tiles = buf + t.k; p->v_tiles = buf + t.v; p->g_tiles = buf + t.g;
     p->q_exp = reinterpret_cast<int32_t*>(buf + t.q_exp);
+    p->next = reinterpret_cast<int32_t*>(buf + t.next);
     p->k_exp = reinterpret_cast<int32_t*>(buf + t.k_exp);
     p->v_exp = reinterpret_cast<int32_t*>(buf + t.v_exp);
     p->g_exp = reinterpret_cast<int32_t*>(buf + t.g_exp);

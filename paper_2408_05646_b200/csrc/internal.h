@@ -517,6 +517,7 @@ struct TrainParams {
   // 16-bit layers: tiles of 128 rows in the order of the products' operands, fp16 numbers times a power of two per tile
   char *q_tiles, *k_tiles, *v_tiles, *g_tiles;     // [unit][tiles][tile bytes]
   int32_t *q_exp, *k_exp, *v_exp, *g_exp;          // [unit][tiles]: exponent of that power
+  int32_t* next;            // [2] entries of the list of items that are taken: forward, backward
   int32_t tile_k, tile_v;   // bytes of a tile: 256 times the widest rank, padded to 16
   int32_t o_stride;         // rp_v of the widest head
   int32_t B, T, H, group, pad, tiles;

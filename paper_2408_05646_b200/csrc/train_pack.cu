@@ -39,6 +39,7 @@ __global__ void __launch_bounds__(kPackThreads) train_pack_kernel(const TrainPar
   __shared__ uint32_t tops[kPackThreads / 32];
   chain_go();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (blockIdx.x == 0 && tid == 0) p.next[GRAD ? 1 : 0] = 0;
   const int tile = blockIdx.x % p.tiles;
   int unit = blockIdx.x / p.tiles;
   const int q_units = p.H * p.group * p.B, units = p.H * p.B;

@@ -158,9 +158,13 @@ __device__ __forceinline__ void item_of(const Plan& plan, int index, int& unit, 
   slot = rest / width;
   unit = first + rest - slot * width;
 }
-// Items of a CTA: every gridDim.x-th, there and back, so that no CTA has the longer one every time.
-__device__ __forceinline__ int64_t list_index(int it, int cta) {
-  return static_cast<int64_t>(it) * gridDim.x + (it & 1 ? gridDim.x - 1 - cta : cta);
+// The next entry for this CTA: lists are worked through in their order, by whichever CTA is free (texts of unequal lengths, dealt
+// out beforehand, left the last CTA with 1.2 to 1.9 times the average work).  The first entries go by the CTA's number; the
+// counter is zeroed by the packing in front.  Which CTA has an item does not change the item's result.
+__device__ __forceinline__ int next_entry(int32_t* counter, int lane) {
+  int x = 0;
+  if (lane == 0) x = atomicAdd(counter, 1);
+  return gridDim.x + __shfl_sync(0xffffffffu, x, 0);
 }
 // Set of own tiles of a CTA's item and the phase of its barriers.
 __device__ __forceinline__ int set_of(const Plan& plan, int it) { return plan.sets == 2 ? it & 1 : 0; }
@@ -287,13 +291,13 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
     const uint64_t keep = policy_evict_normal();
     bool ok = true;
     Place at;
-    int issued = 0, it = 0;
+    int issued = 0, it = 0, index = blockIdx.x;
     for (;; ++it) {
       const int set = set_of(plan, it);
       if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
       if (!ok) break;
       Item* item = &hdr->item[set];
-      const int64_t index = list_index(it, blockIdx.x);
+      if (it > 0) index = next_entry(p.next, lane);
       if (index >= plan.items) {
         if (lane == 0) {
           item->tiles[0] = -1;
@@ -302,7 +306,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
         break;
       }
       int unit, slot;
-      item_of(plan, static_cast<int>(index), unit, slot);
+      item_of(plan, index, unit, slot);
       const int hq = unit / p.B, b = unit - hq * p.B, h = hq / p.group, key_unit = h * p.B + b;
       const int tile = 2 * (plan.per_unit - 1 - slot);
       const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
@@ -575,7 +579,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
 // them (their sum at most 192, each in steps of 32): the next S^T then starts when this one has been read.  Otherwise it takes
 // S^T's place.
 template <int BIAS>
-__device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan, TrHeader* hdr, unsigned char* smem, uint32_t tmem, int warp, int lane, int cta) {
+__device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan, TrHeader* hdr, unsigned char* smem, uint32_t tmem, int warp, int lane, int& index) {
   unsigned char* own = smem;                                 // sets of a tile of k' and one of v'
   unsigned char* ring = own + plan.sets * (p.tile_k + p.tile_v);
   const int rows_at = p.tile_k + p.tile_v, stage_bytes = rows_at + 1024 + kScaleBytes;      // q', do', then L and delta
@@ -594,7 +598,7 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
       if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
       if (!ok) break;
       Item* item = &hdr->item[set];
-      const int64_t index = list_index(it, cta);
+      if (it > 0) index = next_entry(p.next + 1, lane);
       if (index >= plan.items) {
         if (lane == 0) {
           item->tiles[0] = -1;
@@ -603,7 +607,7 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
         break;
       }
       int unit, tile;                                        // (the first keys have the most queries)
-      item_of(plan, static_cast<int>(index), unit, tile);
+      item_of(plan, index, unit, tile);
       const int h = unit / p.B, b = unit - h * p.B;
       const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
       const int k_bytes = kTile * ((rp_k + 15) & ~15) * 2, v_bytes = kTile * ((rp_v + 15) & ~15) * 2;
@@ -668,6 +672,7 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) { ++it; break; }
     }
+    if (!ok) index = 0x7fffffff;                             // (and none of the other kind)
     if (!ok && lane == 0) drain_copies(hdr, plan, it, issued, p.status);
   } else if (warp >= kIssueWarp) {
     const int role = warp - kIssueWarp;                      // S^T; dv'; G^T and dk'
@@ -908,7 +913,7 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
 // bucket, are added up whole; in the others a sum moves one lane up with every column, so that it follows its diagonal, and
 // leaves the warp complete.  All of it in a fixed order, without atomics.
 template <int BIAS>
-__device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan, TrHeader* hdr, unsigned char* smem, uint32_t tmem, int warp, int lane, int cta) {
+__device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan, TrHeader* hdr, unsigned char* smem, uint32_t tmem, int warp, int lane, int index, int first) {
   unsigned char* own = smem;                                 // sets of a tile of q' and one of do'
   unsigned char* ring = own + plan.sets * (p.tile_k + p.tile_v);
   const int scales_at = p.tile_k + p.tile_v, stage_bytes = scales_at + kScaleBytes;
@@ -924,7 +929,7 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
       if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
       if (!ok) break;
       Item* item = &hdr->item[set];
-      const int64_t index = list_index(it, cta);
+      if (it > 0) index = next_entry(p.next + 1, lane) - first;
       if (index >= plan.items) {
         if (lane == 0) {
           item->tiles[0] = -1;
@@ -933,7 +938,7 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
         break;
       }
       int unit, slot;
-      item_of(plan, static_cast<int>(index), unit, slot);
+      item_of(plan, index, unit, slot);
       const int tile = p.tiles - 1 - slot;
       const int hq = unit / p.B, b = unit - hq * p.B, h = hq / p.group, key_unit = h * p.B + b;
       const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
@@ -1199,26 +1204,26 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
 
 // ---------------------------------------------------------------- both in one launch
 
-// A CTA has its share of the tiles of keys, then its share of the tiles of queries; the list of the latter begins at the CTA
-// behind the last one with a tile of keys more, so that a small call has all its items running at a time (a text of 129 tokens
-// through 32 heads: 64 and 64 items).
+// One list: the tiles of keys, then the tiles of queries.  A CTA goes over to the latter when the former are all taken, so that
+// a small call has all its items running at a time (a text of 129 tokens through 32 heads: 64 and 64 items) and a large one
+// does not wait for the last of the first kind.
 template <int BIAS>
 __global__ void __launch_bounds__(kTrThreads, 1) train_backward_kernel(const __grid_constant__ TrainParams p, const __grid_constant__ Plan plan_kv, const __grid_constant__ Plan plan_q) {
   extern __shared__ __align__(1024) unsigned char smem[];
-  TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);         // one for each list
+  TrHeader* hdr = reinterpret_cast<TrHeader*>(smem);         // one for each kind of items
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   if (tid == 0) {
     set_up(hdr, 2, 3 + kSoftmaxWarps, kSoftmaxWarps / 2, 2, kSoftmaxWarps);
     set_up(hdr + 1, 2, 3 + kSoftmaxWarps, kSoftmaxWarps / 2, 1, kSoftmaxWarps);
   }
   const uint32_t tmem = begin(hdr, warp, tid);
-  const int cta = blockIdx.x, behind = cta - plan_kv.items % static_cast<int>(gridDim.x);
-  dkv_items<BIAS>(p, plan_kv, hdr, smem + kHeaderBytes, tmem, warp, lane, cta);
+  int index = blockIdx.x;                                    // (the copying warp's)
+  dkv_items<BIAS>(p, plan_kv, hdr, smem + kHeaderBytes, tmem, warp, lane, index);
   fence_async_smem();                                        // (copies follow on plain writes)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  dq_items<BIAS>(p, plan_q, hdr + 1, smem + kHeaderBytes, tmem, warp, lane, behind < 0 ? behind + gridDim.x : behind);
+  dq_items<BIAS>(p, plan_q, hdr + 1, smem + kHeaderBytes, tmem, warp, lane, index - plan_kv.items, plan_kv.items);
   end(tmem, warp);
 }
 
