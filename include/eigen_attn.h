@@ -336,8 +336,8 @@ ea_status eigen_attn_decode_sparse(eigen_attn_t h, const void* d_q, int64_t stri
  * bias_set:    d_table: DEVICE [n_heads][n_buckets] in the layer's dtype, finite numbers; asynchronous (calls on other streams
  *              are ordered behind it by the caller), can be captured, the table may be changed once the launch has run.
  * bias_starts: first distance of every bucket: HOST [n_buckets], not descending (an empty bucket starts where the next does).
- * In effect for eigen_attn_append_kv's counterparts that attend: decode, decode_static, decode_step(_host) and prefill (unequal
- * lengths, page tables), train_forward and train_backward.  decode_gqa, decode_quant, decode_tree and decode_sparse return
+ * In effect for decode, decode_static, decode_step(_host) and prefill (with unequal lengths and page tables as without) and for
+ * train_forward and train_backward.  decode_gqa, decode_quant, decode_tree and decode_sparse return
  * EA_ERR_UNSUPPORTED while a bias is attached. */
 ea_status eigen_attn_bias_bytes(eigen_attn_t h, int32_t n_buckets, int32_t max_distance, size_t* bytes);
 ea_status eigen_attn_bias_attach(eigen_attn_t h, int32_t n_buckets, int32_t max_distance, void* d_buf, size_t bytes,
@@ -357,6 +357,10 @@ ea_status eigen_attn_bias_starts(eigen_attn_t h, int32_t* starts);
  * whose gradients are summed over them in a fixed order.  Results do not depend on the order in which blocks run.
  * d_lens: DEVICE int32 [B] or NULL (all T): sequence b has its first d_lens[b] tokens (taken into 0..T); rows behind are not
  * read, and their outputs and gradients are zero.  The lengths are read by the launch, so a captured call follows them.
+ * The tokens' numbers are finite (one that is not reaches results of its own head and sequence, those of earlier tokens
+ * among them).  In 16-bit layers a number that is below 2^-22 of the largest of its head within 128 tokens (0 to 127, 128 to
+ * 255, ...) is off by up to 2^-33 of that one, and a result by up to 2^-29 for every term of the product of the largest
+ * numbers that it is made of (of its head and sequence).
  * A position bias (ALiBi or learned) is per K/V head: only with group 1 (EA_ERR_UNSUPPORTED).  Not with a rotary embedding.
  *
  * train_bytes:    size of the scratch for up to max_tokens (1..2^20) tokens and `group` query heads per K/V head.

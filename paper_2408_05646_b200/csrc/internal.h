@@ -424,7 +424,9 @@ inline cudaError_t launch_chained(bool chained, void (*kernel)(Params...), dim3 
   attribute.val.programmaticStreamSerializationAllowed = chained ? 1 : 0;
   config.attrs = &attribute;
   config.numAttrs = 1;
-  return cudaLaunchKernelEx(&config, kernel, static_cast<Params>(args)...);
+  const cudaError_t e = cudaLaunchKernelEx(&config, kernel, static_cast<Params>(args)...);
+  if (e != cudaSuccess) cudaGetLastError();                  // (returned here: the next plain launch does not find it again)
+  return e;
 }
 #endif
 
@@ -535,6 +537,8 @@ struct TrainParams {
   int32_t sm_count;
   int* status;
 };
+// Tokens of sequence b, as the forward pass left them.  (Its launch may have been captured and not replayed yet.)
+__device__ __forceinline__ int kept_tokens(const TrainParams& p, int b) { return min(max(__ldg(p.lens + b), 0), p.T); }
 cudaError_t launch_train_simt_forward(const TrainParams& p, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_train_simt_backward(const TrainParams& p, cudaStream_t s, uint64_t* launches);
 cudaError_t launch_train_pack(const TrainParams& p, bool gradient, cudaStream_t s, uint64_t* launches);

@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kPackThreads) train_pack_kernel(const TrainPar
                              static_cast<int64_t>(b) * p.T * width + group * (key_side ? hd.lr_k_off : hd.lr_v_off) + i * rp;
   int n;
   if (GRAD) {
-    n = __ldg(p.lens + b);
+    n = kept_tokens(p, b);
   } else {
     n = p.lens_in != nullptr ? min(max(__ldg(p.lens_in + b), 0), p.T) : p.T;
     if (blockIdx.x == 0)                                     // the lengths, kept for the launches behind

@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_simt_dq_kernel(const TrainP
   const HeadInfo hd = p.heads[u.h];
   const int tile = gridDim.y - 1 - blockIdx.y, i0 = tile * kOwn;
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  const int rk = hd.rp_k, rv = hd.rp_v, n = __ldg(p.lens + u.b), rows = max(0, min(kOwn, n - i0)), end = rows > 0 ? i0 + rows : 0;
+  const int rk = hd.rp_k, rv = hd.rp_v, n = kept_tokens(p, u.b), rows = max(0, min(kOwn, n - i0)), end = rows > 0 ? i0 + rows : 0;
   constexpr int kTile = kWalk * kPitch<NC>, kOwnTile = kOwn * kPitch<NC>;
   float* Qs = sm;
   float* Gs = Qs + kOwnTile;
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_simt_dkv_kernel(const Train
   const HeadInfo hd = p.heads[h];
   const int j0 = blockIdx.y * kOwn;                          // the first keys have the most queries
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  const int rk = hd.rp_k, rv = hd.rp_v, n = __ldg(p.lens + b), rows = max(0, min(kOwn, n - j0));
+  const int rk = hd.rp_k, rv = hd.rp_v, n = kept_tokens(p, b), rows = max(0, min(kOwn, n - j0));
   constexpr int kTile = kWalk * kPitch<NC>, kOwnTile = kOwn * kPitch<NC>;
   float* Ks = sm;
   float* Vs = Ks + kOwnTile;
@@ -498,6 +498,8 @@ cudaError_t backward_t(const TrainParams& p, cudaStream_t s) {
   if (e == cudaSuccess) e = ensure_dynamic_smem(train_simt_dkv_kernel<NC>, smem, done_kv);
   if (e != cudaSuccess) return e;
   train_simt_dq_kernel<NC><<<dim3(p.H * p.group * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
   train_simt_dkv_kernel<NC><<<dim3(p.H * p.B, train_simt_tiles(p.T)), kThreads, smem, s>>>(p);
   return cudaGetLastError();
 }

@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
       item_of(plan, index, unit, slot);
       const int hq = unit / p.B, b = unit - hq * p.B, h = hq / p.group, key_unit = h * p.B + b;
       const int tile = 2 * (plan.per_unit - 1 - slot);
-      const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
+      const int n = kept_tokens(p, b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
       const int q_bytes = kTile * ((rp_k + 15) & ~15) * 2, v_bytes = kTile * ((rp_v + 15) & ~15) * 2;
       const int nt0 = tile * kTile < n ? tile + 1 : 0, nt1 = (tile + 1) * kTile < n ? tile + 2 : 0, most = max(nt0, nt1);
       const int32_t *k_exp = p.k_exp + static_cast<int64_t>(key_unit) * p.tiles, *v_exp = p.v_exp + static_cast<int64_t>(key_unit) * p.tiles;
@@ -609,7 +609,7 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
       int unit, tile;                                        // (the first keys have the most queries)
       item_of(plan, index, unit, tile);
       const int h = unit / p.B, b = unit - h * p.B;
-      const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
+      const int n = kept_tokens(p, b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
       const int k_bytes = kTile * ((rp_k + 15) & ~15) * 2, v_bytes = kTile * ((rp_v + 15) & ~15) * 2;
       const int per_head = max((n + kTile - 1) / kTile - tile, 0);                          // tiles of queries of one head
       const int64_t own_at = static_cast<int64_t>(unit) * p.tiles + tile;
@@ -941,7 +941,7 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
       item_of(plan, index, unit, slot);
       const int tile = p.tiles - 1 - slot;
       const int hq = unit / p.B, b = unit - hq * p.B, h = hq / p.group, key_unit = h * p.B + b;
-      const int n = __ldg(p.lens + b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
+      const int n = kept_tokens(p, b), rp_k = __ldg(&p.heads[h].rp_k), rp_v = __ldg(&p.heads[h].rp_v);
       const int k_bytes = kTile * ((rp_k + 15) & ~15) * 2, v_bytes = kTile * ((rp_v + 15) & ~15) * 2;
       const int nt = tile * kTile < n ? tile + 1 : 0;
       const int64_t own_at = static_cast<int64_t>(unit) * p.tiles + tile, keys = static_cast<int64_t>(key_unit) * p.tiles;
