@@ -24,7 +24,8 @@
 //     log2 domain; only then do the halves exchange maxima through shared memory and rescale O'),
 //     computes 32 exponentials and writes P (bf16) IN PLACE over the first 32 columns of the S buffer,
 //     from where it is the A operand of the PV product: P never touches shared memory.
-//     The ALiBi bias (per-head slope) is added to the scaled scores in a second instantiation.
+//     The ALiBi bias (per-head slope) is added to the scaled scores in a second instantiation, the learned bias in a third:
+//     entry by entry where a half tile has distances of its own, as one number where all of them share the last bucket.
 // TMEM (512 columns): S_A[2], S_B[2] (64 columns each, P aliased), O'_A, O'_B (up to 128 each).
 // Every wait is bounded.
 #include <cuda_bf16.h>
@@ -116,8 +117,10 @@ __device__ __forceinline__ void issue_s_steps(int ks, uint32_t d_tmem, uint64_t 
   }
 }
 
+constexpr int kNone = 0, kAlibi = 1, kTable = 2;            // position bias
+
 // TAIL: a sequence of the call can end inside a key tile.
-template <bool ALIBI, bool TAIL>
+template <int BIAS, bool TAIL>
 __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const PrefillParams p, int stages) {
   extern __shared__ __align__(1024) unsigned char smem[];
   WsHeader* hdr = reinterpret_cast<WsHeader*>(smem);
@@ -371,7 +374,9 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
     float m_run = -INFINITY, l_run = 0.f;
     bool ok = true;
     const int nt = n_tiles[x];
-    const float slope2 = ALIBI ? hd.alibi_slope2 : 0.f;
+    const float slope2 = BIAS == kAlibi ? hd.alibi_slope2 : 0.f;
+    const float* table = BIAS == kTable ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;   // by distance; the last for all behind
+    const float far_bias = BIAS == kTable ? __ldg(table + p.bias_len - 1) : 0.f;
 
     // The 256 threads of a query tile meet at named barriers, which have no time limit: every decision to leave
     // the loop is therefore taken through a reducing barrier, so that all of them leave after the same tile.
@@ -383,12 +388,14 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
       const bool diag = j * kKeys + kKeys - 1 > len0 + tx; // some (row, key) pair of the tile is masked
       uint32_t r[kHalfKeys];
       float cand = -INFINITY;                                // this half-row's largest score, scaled (log2 domain)
+      const bool near = BIAS == kTable && len0 + tx - key0 - (kHalfKeys - 1) < p.bias_len - 1;
+      const float scale = near ? 1.f : p.scale_log2, base = near ? 0.f : far_bias;               // (learned bias)
       if (waited) {
         tc_fence_after();
         tmem_ld16(tSb + hf * kHalfKeys, *reinterpret_cast<uint32_t(*)[16]>(&r[0]));
         tmem_ld16(tSb + hf * kHalfKeys + 16, *reinterpret_cast<uint32_t(*)[16]>(&r[16]));
         tmem_wait_ld();
-        if (ALIBI) {
+        if (BIAS == kAlibi) {
           // scaled score plus the bias slope * (key - position), kept in place of the raw score
           float off = slope2 * static_cast<float>(key0 - my_pos);
 #pragma unroll
@@ -396,6 +403,12 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
             r[c] = __float_as_uint(fmaf(__uint_as_float(r[c]), p.scale_log2, off));
             off += slope2;
           }
+        }
+        if (near) {
+          const int first = my_pos - key0;
+#pragma unroll
+          for (int c = 0; c < kHalfKeys; ++c)
+            r[c] = __float_as_uint(fmaf(__uint_as_float(r[c]), p.scale_log2, __ldg(table + min(max(first - c, 0), p.bias_len - 1))));
         }
         if (diag) {
 #pragma unroll
@@ -410,7 +423,8 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
           }
           cand = fmaxf(mx0, mx1);
         }
-        if (!ALIBI) cand *= p.scale_log2;                    // the scale is positive: max and scale commute
+        if (BIAS == kNone) cand *= p.scale_log2;             // the scale is positive: max and scale commute
+        if (BIAS == kTable) cand = fmaf(cand, scale, base);
       }
       // Lazy reference: it follows the row maximum only when that has grown by more than 8 (a factor 256 that
       // fp32 sums and bf16 P absorb).  One reducing barrier tells whether any row of the tile needs it; it also
@@ -449,16 +463,16 @@ __global__ void __launch_bounds__(kWsThreads, 1) prefill_tc_ws_kernel(const Pref
       // exponentials against the reference, their sum, P as bf16 pairs
       uint32_t pk[kHalfKeys / 2];
       float sum0 = 0.f, sum1 = 0.f;
-      const float neg_m = -m_run;
+      const float neg_m = BIAS == kTable ? base - m_run : -m_run;
 #pragma unroll
       for (int i = 0; i < kHalfKeys / 2; ++i) {
         const int c = 2 * i;
         float y0, y1;
-        if (ALIBI) {
+        if (BIAS == kAlibi) {
           y0 = __uint_as_float(r[c]) + neg_m;
           y1 = __uint_as_float(r[c + 1]) + neg_m;
         } else {
-          fma2(y0, y1, __uint_as_float(r[c]), __uint_as_float(r[c + 1]), p.scale_log2, neg_m);
+          fma2(y0, y1, __uint_as_float(r[c]), __uint_as_float(r[c + 1]), BIAS == kTable ? scale : p.scale_log2, neg_m);
         }
         float e0 = ex2(y0), e1 = ex2(y1);
         if (diag) {
@@ -580,15 +594,17 @@ cudaError_t launch_prefill_tc_ws(const PrefillParams& p, int stages, size_t smem
                                  uint64_t* launches) {
   // (with unequal lengths some sequence ends inside a tile)
   const bool tail = p.deficit != nullptr || (p.len0 + p.T) % kKeys != 0;
-  static size_t configured[4][kMaxDevices] = {};
+  static size_t configured[6][kMaxDevices] = {};
   auto run = [&](auto kernel, size_t (&done)[kMaxDevices]) -> cudaError_t {
     const cudaError_t e = ensure_dynamic_smem(kernel, smem, done);
     if (e != cudaSuccess) return e;
     kernel<<<dim3(p.B * p.H, (p.T + 2 * kTile - 1) / (2 * kTile)), kWsThreads, smem, s>>>(p, stages);
     return cudaSuccess;
   };
-  const cudaError_t ec = alibi ? (tail ? run(prefill_tc_ws_kernel<true, true>, configured[3]) : run(prefill_tc_ws_kernel<true, false>, configured[2]))
-                               : (tail ? run(prefill_tc_ws_kernel<false, true>, configured[1]) : run(prefill_tc_ws_kernel<false, false>, configured[0]));
+  cudaError_t ec;
+  if (p.bias != nullptr) ec = tail ? run(prefill_tc_ws_kernel<kTable, true>, configured[5]) : run(prefill_tc_ws_kernel<kTable, false>, configured[4]);
+  else if (alibi) ec = tail ? run(prefill_tc_ws_kernel<kAlibi, true>, configured[3]) : run(prefill_tc_ws_kernel<kAlibi, false>, configured[2]);
+  else ec = tail ? run(prefill_tc_ws_kernel<kNone, true>, configured[1]) : run(prefill_tc_ws_kernel<kNone, false>, configured[0]);
   if (ec != cudaSuccess) return ec;
   ++*launches;
   return cudaGetLastError();

@@ -92,6 +92,31 @@ def test_prefill(dtype, impl, T, first):
     helpers.assert_close(got, want, dtype, "prefill")
 
 
+@pytest.mark.parametrize("buckets", [(32, 128), (2, 2), (64, 1024)])
+@pytest.mark.parametrize("impl", [0, 3])
+@pytest.mark.parametrize("T,lens", [(640, [0, 64]), (530, [130, 77])])
+def test_long_prompts_behind_unequal_lengths(T, lens, impl, buckets):
+    """Tiles near the diagonal, and tiles whose distances all share the last bucket."""
+    from paper_2408_05646_b200 import binding
+    d, r_k, r_v = 64, [32, 64], [40, 24]
+    lay, U_k, U_v, bias, rng = make(2, r_k, r_v, d, BF, 768, max_prefill=T, buckets=buckets, seed=T)
+    lay.set_option(binding.EA_OPT_PREFILL_IMPL, impl)
+    k0, v0 = draw(rng, BF, 2, 130, 2, d), draw(rng, BF, 2, 130, 2, d)
+    lay.append_kv(k0.cuda(), v0.cuda())
+    lay.set_lens(lens)
+    q, k, v = (draw(rng, BF, 2, T, 2, d) for _ in range(3))
+    got = lay.prefill(q.cuda(), k.cuda(), v.cuda())
+    want = np.zeros((2, T, 2, d))
+    for b, n in enumerate(lens):
+        for h in range(2):
+            K = np.concatenate([project(k0[b, :n, h], U_k[h], BF), project(k[b, :, h], U_k[h], BF)])
+            V = np.concatenate([project(v0[b, :n, h], U_v[h], BF), project(v[b, :, h], U_v[h], BF)])
+            for t in range(T):
+                want[b, t, h] = attend(q[b, t, h].double().numpy(), K, V, U_k[h], U_v[h], d, bias[h], n + t)
+    helpers.assert_close(got, want, BF, "prefill")
+    lay.poll_status()
+
+
 def test_a_bias_can_be_changed_and_taken_away():
     B, d, r = 1, 64, [32]
     lay, U_k, U_v, bias, rng = make(B, r, r, d, F32, 256)
