@@ -355,6 +355,7 @@ ea_status eigen_attn_bias_starts(eigen_attn_t h, int32_t* starts);
  * [B][T][group * sum rp_v] as in eigen_attn_decode_tree, d_k, d_dk [B][T][sum rp_k], d_v, d_dv [B][T][sum rp_v]; what an
  * input holds in a rank's padding columns is ignored, an output has zeros there.  group query heads (1..16) share a K/V head,
  * whose gradients are summed over them in a fixed order.  Results do not depend on the order in which blocks run.
+ * Outputs overlap neither inputs nor one another.
  * d_lens: DEVICE int32 [B] or NULL (all T): sequence b has its first d_lens[b] tokens (taken into 0..T); rows behind are not
  * read, and their outputs and gradients are zero.  The lengths are read by the launch, so a captured call follows them.
  * The tokens' numbers are finite (one that is not reaches results of its own head and sequence, those of earlier tokens

@@ -261,7 +261,9 @@ __device__ __forceinline__ Piece locate(const DecodeParams& p, const int* pre, l
 
 // ---------------------------------------------------------------- one (CTA, unit) piece
 
-// BIAS: a learned bias of relative positions; `bias` is the head's, one number per distance.
+// BIAS: a learned bias of relative positions; `bias` is the head's, one number per distance.  Every row reads its
+// entry, the last one behind the last bucket's first distance: from L1, in the shadow of the row's own products (16 x 32768 rows:
+// 782 us with 1024 distances of their own, 756 without a bias).
 template <typename T, int NCH, bool BIAS>
 __device__ __forceinline__ void run_segment(const DecodeParams& p, DecodeSmemFixed* fx, const float* bias,
                                             unsigned char* ring, const HeadInfo& hd, int i0, int i1,

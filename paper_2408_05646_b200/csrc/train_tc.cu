@@ -9,15 +9,21 @@
 // A tile is 128 rows.  A persistent CTA per SM (it takes the SM's 512 TMEM columns) works through items: a tile (or two) of one
 // axis, which it keeps in shared memory, against the tiles of the other axis, which stream through a ring in halves of 64 rows
 // with score buffers of their own: while the softmax works on one half, the products of the other run.  Roles:
-//   * a copying warp: one bulk copy per tile.  It alone reads the item list, lengths and exponents; what the others need to know
+//   * a copying warp: a bulk copy per operand tile.  It alone reads the item list, lengths and exponents; what the others need to know
 //     of an item goes with the item's own tiles, of which there are two sets where they fit, so that an item starts with its
 //     tiles at hand (a CTA per item spent some 7000 clocks on its start and end: a fifth of the time at 4096 tokens);
 //   * issuing warps, two or three.  (With one, the products were late: it shares its scheduler with softmax warps, which leave
 //     it an instruction every 10 to 20 clocks.)  Products of one accumulator have one issuer, so that their order is fixed;
 //   * eight softmax warps.  P and dS go back to TMEM as the A operand of the next product and never touch shared memory.
-// The backward pass is two kernels, one that owns tiles of keys (dk', dv': four products per pair of tiles) and one that owns
-// tiles of queries (dq': three, S and do' v' a second time): the alternative, dq' added up in memory by every tile of keys,
+// The backward pass has two kinds of items, one that owns a tile of keys (dk', dv': four products per pair of tiles) and one that
+// owns a tile of queries (dq': three, S and do' v' a second time): the alternative, dq' added up in memory by every tile of keys,
 // moves 512 r bytes of fp32 additions per pair of tiles through L2 and leaves sums whose order changes from run to run.
+// 4 x 4096 tokens, 32 heads, rank 80: forward 514 us, a backward call 1378, 74 of them packing (624 TFLOP/s of the five products
+// that the formulas need); tensor pipe busy 34 and 43 % of the time, exponentials 55 and 40 %, an instruction issued in 0.40 and
+// 0.36 of the clocks.  What is left is the chain of a half tile, product, load, exponentials, store, product, of which two
+// run at a time (some 2970 clocks for a pair of tiles of a key item, 2180 of a query item, against 1600 and 1040 of their
+// products).  Tried and slower: three chains (a third fewer registers for each), sixteen softmax warps with half the columns,
+// turns between the halves' exponentials, a part of the exponentials as polynomials on the multiply-add units.
 //
 // Tiles carry a power of two each (2^e).  What is accumulated over tiles needs one scale: the tile's deviation from the
 // smallest exponent of all goes into the factors that P and dS are formed with, where it costs nothing.
@@ -151,7 +157,7 @@ __device__ __forceinline__ unsigned long long pair_at(const uint32_t (&r)[32], i
 
 // Entry `index` of the list of items.  The items of `chunk` units follow one another, the longest (slot 0) first: those that run
 // at a time then stream tiles of a few units, which stay in L2 (all units at once are 168 MB for 4 x 4096 tokens of 32 heads),
-// and the longest of many units together leave short ones for the end.
+// and the longest of many units together leave short ones for the end.  (Chunks of 32, 48, 80, 110 MB: 1398, 1378, 1380, 1390 us.)
 __device__ __forceinline__ void item_of(const Plan& plan, int index, int& unit, int& slot) {
   const int per_chunk = plan.chunk * plan.per_unit, first = index / per_chunk * plan.chunk, rest = index % per_chunk;
   const int width = min(plan.chunk, plan.units - first);
@@ -275,7 +281,7 @@ __device__ __forceinline__ void drain_copies(TrHeader* hdr, const Plan& plan, in
 // keys: S, the row's maximum, 2^(S - reference) and their sum, P in the place of S, o' += P v'.  The reference is a lazy one:
 // it moves, and o' is rescaled, only when a score exceeds it by 8.  TMEM: two halves of S for both tiles (64 columns each, P in
 // the first 32 of them), o' of both.
-// Bound by the exponentials (16 a clock: 2048 clocks for two pairs of tiles; their products take 1630 at rank 80).
+// Least clocks for two pairs of tiles at rank 80: exponentials 2048 (16 a clock), products 1630.
 template <int BIAS>
 __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __grid_constant__ TrainParams p, const __grid_constant__ Plan plan) {
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -1205,8 +1211,8 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
 // ---------------------------------------------------------------- both in one launch
 
 // One list: the tiles of keys, then the tiles of queries.  A CTA goes over to the latter when the former are all taken, so that
-// a small call has all its items running at a time (a text of 129 tokens through 32 heads: 64 and 64 items) and a large one
-// does not wait for the last of the first kind.
+// a small call has all its items running at a time (a text of 129 tokens through 32 heads: 64 and 64 items; two launches
+// 30.7 us, one 24.0) and a large one does not wait for the last of the first kind.
 template <int BIAS>
 __global__ void __launch_bounds__(kTrThreads, 1) train_backward_kernel(const __grid_constant__ TrainParams p, const __grid_constant__ Plan plan_kv, const __grid_constant__ Plan plan_q) {
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -1227,7 +1233,8 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_backward_kernel(const __g
   end(tmem, warp);
 }
 
-// Sets of own tiles and ring stages: two sets where three stages fit beside them, else one.
+// Sets of own tiles and ring stages: two sets where three stages fit beside them, else one.  (4 x 4096 tokens, rank 80: two sets
+// and three stages 1510 us, one set and four 1612.)
 Plan plan_of(const TrainParams& p, int units, int per_unit, size_t own, size_t stage, size_t behind, size_t* smem) {
   Plan plan{};
   const size_t room = 227 * 1024 - kHeaderBytes - behind;
