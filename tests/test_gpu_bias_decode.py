@@ -117,6 +117,23 @@ def test_long_prompts_behind_unequal_lengths(T, lens, impl, buckets):
     lay.poll_status()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_prompt_in_pages(dtype):
+    """A page table changes addresses and nothing else."""
+    from paper_2408_05646_b200 import binding
+    d, r_k, r_v, T = 64, [32, 40], [24, 64], 300
+    outs = []
+    for paged in (False, True):
+        lay, _, _, _, rng = make(2, r_k, r_v, d, dtype, 512, max_prefill=T)
+        lay.set_option(binding.EA_OPT_PREFILL_IMPL, 1)
+        if paged:
+            lay.set_page_table([[5, 0, 3, 6], [1, 7, 2, 4]], 128)
+        q, k, v = (draw(rng, dtype, 2, T, 2, d).cuda() for _ in range(3))
+        outs.append((lay.prefill(q, k, v), lay.decode(q[:, -1:].contiguous())))
+    assert torch.equal(outs[0][0], outs[1][0])
+    helpers.assert_close(outs[1][1], outs[0][1].double().cpu().numpy(), dtype, "decode")
+
+
 def test_a_bias_can_be_changed_and_taken_away():
     B, d, r = 1, 64, [32]
     lay, U_k, U_v, bias, rng = make(B, r, r, d, F32, 256)

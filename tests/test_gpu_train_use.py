@@ -139,6 +139,72 @@ def test_captured_and_replayed(dtype, group, bias):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_whole_captured_step_with_its_table(dtype):
+    """bias_set, both passes and the table's update in one graph: every replay is an uncaptured step."""
+    s, ref = (Step(2, 150, [32, 24], [24, 40], 64, dtype, bias=True, seed=3) for _ in range(2))
+
+    def step(s, stream=None):
+        s.lay.set_bias(s.table, stream=stream)
+        got = s.run(stream=stream)
+        s.table.sub_(got[4], alpha=0.5)
+        return got
+
+    step(s)
+    step(ref)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(s, torch.cuda.current_stream())
+    for _ in range(3):
+        graph.replay()
+        assert same(captured, step(ref)) and torch.equal(s.table, ref.table)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_long_text(dtype):
+    """20000 tokens, two heads, the formulas in 64 bits on the device, 1000 queries at a time.  Tolerances as in close, with
+    sqrt(20000 / 64) - sqrt(300 / 64) = 15 half steps more for the longer sums of fp32 layers."""
+    T, r, d, chunk = 20000, [16, 24], 32, 1000
+    s = Step(1, T, r, r, d, dtype, bias=True, seed=11)
+    out, dq, dk, dv, dtable = s.run()
+    s.lay.poll_status()
+    starts = torch.tensor(s.lay.bias_starts(), device="cuda")
+    half = torch.finfo(dtype).eps / 2
+    cols, _ = oracle.packed_columns(r)
+    at = torch.arange(T, device="cuda")
+    by, by_size = torch.zeros(2, BUCKETS[0], dtype=torch.float64, device="cuda"), torch.zeros(2, BUCKETS[0], dtype=torch.float64, device="cuda")
+    for h, c in enumerate(cols):
+        c = torch.as_tensor(c, device="cuda")
+        q, k, v, g = (x[0][:, c].double() for x in s.x)
+        table = s.table[h].double()
+        want = {n: torch.zeros_like(q) for n in ("out", "dq", "dk", "dv")}
+        size = {n: torch.zeros_like(q) for n in want}
+        for i in range(0, T, chunk):
+            n = i + chunk
+            dist = at[i:n, None] - at[None, :n]
+            bucket = torch.bucketize(dist.clamp(min=0), starts, right=True) - 1
+            S = q[i:n] @ k[:n].T / np.sqrt(d) + table[bucket]
+            P = torch.softmax(S.masked_fill(dist < 0, float("-inf")), dim=1)
+            o = P @ v[:n]
+            delta = (o * g[i:n]).sum(1, keepdim=True)
+            dS = P * (g[i:n] @ v[:n].T - delta)
+            A = P * (g[i:n].abs() @ v[:n].abs().T + (o * g[i:n]).abs().sum(1, keepdim=True))
+            want["out"][i:n], size["out"][i:n] = o, P @ v[:n].abs()
+            want["dq"][i:n], size["dq"][i:n] = dS @ k[:n] / np.sqrt(d), A @ k[:n].abs() / np.sqrt(d)
+            want["dk"][:n] += dS.T @ q[i:n] / np.sqrt(d)
+            size["dk"][:n] += A.T @ q[i:n].abs() / np.sqrt(d)
+            want["dv"][:n] += P.T @ g[i:n]
+            size["dv"][:n] += P.T @ g[i:n].abs()
+            by[h] += torch.bincount(bucket.flatten(), dS.flatten(), BUCKETS[0])
+            by_size[h] += torch.bincount(bucket.flatten(), A.flatten(), BUCKETS[0])
+        for name, x in zip(want, (out, dq, dk, dv)):
+            over = (x[0][:, c].double() - want[name]).abs() - half * want[name].abs() - (2.0 ** -11 if dtype == BF else 60 * half) * size[name]
+            assert over.max() <= 0, (h, name, over.max().item())
+    over = (dtable.double() - by).abs() - half * by.abs() - (2.0 ** -12 if dtype == BF else 60 * half) * by_size
+    assert over.max() <= 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_a_backward_pass_before_the_captured_forward_pass_has_run(dtype):
     """Its results are of no use, but it reads and writes nothing outside."""
     s = Step(2, 200, [32, 24], [24, 40], 64, dtype)
