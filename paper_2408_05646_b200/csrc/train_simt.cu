@@ -8,9 +8,10 @@
 // of 64, fetched one ahead; a thread has 2 x 4 scores and 2 rows x 2 to 8 columns of the sums.  dq' and dk', dv' are two
 // kernels, so that nothing is added up by atomics.  A tile's products are summed apart and then added, which keeps the rounding
 // errors of long sums down.  Bound by the latency of the shared-memory reads in front of the multiply-adds (2 x 500 tokens,
-// 8 heads of rank 40: forward 49, dq' 60, dk' and dv' 57 us; own tiles of 64 rows, half as many CTAs, took 95, 128 and 136).
+// 8 heads of rank 40: forward 45, dq' 56, dk' and dv' 53 us; own tiles of 64 rows, half as many CTAs, took 95, 128 and 136).
 // The loops are unrolled for registers, not for CTAs: with the compiler's own choice, 128 registers and two CTAs per SM, the
-// three took 188 us, with one CTA and its loads four steps ahead 159.
+// three took 188 us, with one CTA and its loads four steps ahead 159.  Every thread fetches pieces of one row, without a division:
+// 159 to 151.
 #include "internal.h"
 #include "tc_common.cuh"
 
@@ -34,21 +35,20 @@ __device__ __forceinline__ float ex2(float x) {
 // padding: zeros, whatever the caller left there.  wide: the rows lie on 16-byte boundaries.
 template <int COUNT, int PITCH>
 __device__ __forceinline__ void fetch_rows(float* dst, const float* src, int64_t stride, int rows, int width, int live, bool wide, int tid) {
-  const uint32_t to = tc::smem_u32(dst);
+  constexpr int kLanes = kThreads / COUNT;                   // threads of a row
+  const int r = tid / kLanes, first = tid % kLanes;
+  const uint32_t to = tc::smem_u32(dst + r * PITCH);
+  const float* from = r < rows ? src + r * stride : src;
+  const int have = r < rows ? live : 0;                      // numbers of the row
   if (wide) {
-    const int quads = width >> 2;
-    for (int idx = tid; idx < COUNT * quads; idx += kThreads) {
-      const int r = idx / quads, c = 4 * (idx - r * quads);
-      const int bytes = r < rows ? 4 * min(max(live - c, 0), 4) : 0;
-      const float* from = bytes > 0 ? src + r * stride + c : src;
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 4 * (r * PITCH + c)), "l"(from), "r"(bytes) : "memory");
+    for (int c = 4 * first; c < width; c += 4 * kLanes) {
+      const int bytes = 4 * min(max(have - c, 0), 4);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 4 * c), "l"(bytes > 0 ? from + c : src), "r"(bytes) : "memory");
     }
   } else {
-    for (int idx = tid; idx < COUNT * width; idx += kThreads) {
-      const int r = idx / width, c = idx - r * width;
-      const int bytes = r < rows && c < live ? 4 : 0;
-      const float* from = bytes > 0 ? src + r * stride + c : src;
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * (r * PITCH + c)), "l"(from), "r"(bytes) : "memory");
+    for (int c = first; c < width; c += kLanes) {
+      const int bytes = c < have ? 4 : 0;
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * c), "l"(bytes > 0 ? from + c : src), "r"(bytes) : "memory");
     }
   }
 }
@@ -282,6 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_simt_dq_kernel(const TrainP
   __shared__ float stats[3][kOwn];                           // maximum, reciprocal sum, delta
   __shared__ float bias_of[2][kOwn + kWalk], diagonal[kOwn + kWalk];
   __shared__ double by_bucket[kMaxBuckets];
+  __shared__ int starts[kMaxBuckets + 1];
   const Unit u = query_unit(p, blockIdx.x);
   const HeadInfo hd = p.heads[u.h];
   const int tile = gridDim.y - 1 - blockIdx.y, i0 = tile * kOwn;
@@ -308,7 +309,10 @@ __global__ void __launch_bounds__(kThreads, 1) train_simt_dq_kernel(const TrainP
     tc::cp_async_commit();
     tc::cp_async_wait<0>();
   }
-  if (p.dtable != nullptr && tid < p.buckets) by_bucket[tid] = 0;
+  if (p.dtable != nullptr) {
+    if (tid < p.buckets) by_bucket[tid] = 0;
+    for (int b = tid; b <= p.buckets; b += kThreads) starts[b] = __ldg(p.starts + b);
+  }
   __syncthreads();
   {
     const int r = tid >> 3;                                  // eight threads for a row of do' o'
@@ -365,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) train_simt_dq_kernel(const TrainP
       __syncthreads();
       const int shift = i0 - j0 - (kWalk - 1), lane = tid & 31;          // distance of diagonal[0]
       for (int b = tid >> 5; b < p.buckets; b += kThreads / 32) {
-        const int first = __ldg(p.starts + b), behind = __ldg(p.starts + b + 1);
+        const int first = starts[b], behind = starts[b + 1];
         if (first > shift + kOwn + kWalk - 2 || behind <= shift) continue;
         const int from = max(first - shift, 0), to = behind > shift + kOwn + kWalk - 1 ? kOwn + kWalk - 1 : behind - shift;
         double sum = 0;
