@@ -44,7 +44,7 @@ constexpr int kSoftmaxWarps = 8, kCopyWarp = 8, kIssueWarp = 9;
 constexpr int kTrThreads = 12 * 32;       // softmax, copies, up to three issuing warps
 constexpr int kHalf = 64;                 // rows of the walked axis that share a score buffer
 constexpr int kMaxRing = 8;
-constexpr int kHeaderBytes = 1024;
+constexpr int kHeaderBytes = 960;
 constexpr int kScaleBytes = 16;           // behind a stage's tiles: the scales of the pair of tiles, worked out by the copying warp
 constexpr int kForwardShift = 7;          // P of the forward pass times 2^7: its reference lags behind the maximum by up to 2^8
 constexpr int kBackwardShift = 14;        // P of the backward pass, at most 1, times 2^14: fp16 keeps all bits down to 2^-28
@@ -1233,13 +1233,15 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_backward_kernel(const __g
   end(tmem, warp);
 }
 
-// Sets of own tiles and ring stages: two sets where three stages fit beside them, else one.  (4 x 4096 tokens, rank 80: two sets
-// and three stages 1510 us, one set and four 1612.)
+// Sets of own tiles and ring stages: two sets where two stages fit beside them (ranks up to 112), else one.  Rank 80, 4 x 4096
+// tokens: two sets and three stages 1510 us, one set and four 1612; rank 96, 4 x 2048: two and two 512, one and three 567; a step
+// of 2 x 1111 tokens with ranks 48 to 112 161 and 182.
 Plan plan_of(const TrainParams& p, int units, int per_unit, size_t own, size_t stage, size_t behind, size_t* smem) {
   Plan plan{};
   const size_t room = 227 * 1024 - kHeaderBytes - behind;
-  plan.sets = 2 * own + 3 * stage <= room ? 2 : 1;
-  plan.stages = static_cast<int>((room - plan.sets * own) / stage);
+  const size_t one = (room - own) / stage, two = room > 2 * own ? (room - 2 * own) / stage : 0;
+  plan.sets = two >= 2 ? 2 : 1;
+  plan.stages = static_cast<int>(plan.sets == 2 ? two : one);
   if (plan.stages > kMaxRing) plan.stages = kMaxRing;
   *smem = kHeaderBytes + behind + plan.sets * own + plan.stages * stage;
   if (*smem < 120 * 1024) *smem = 120 * 1024;                // one CTA per SM: it takes all of the SM's TMEM
