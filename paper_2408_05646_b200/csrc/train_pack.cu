@@ -67,6 +67,12 @@ __global__ void __launch_bounds__(kPackThreads) train_pack_kernel(const TrainPar
       for (int x = tid; x < p.B; x += kPackThreads)
         p.lens[x] = p.lens_in != nullptr ? min(max(__ldg(p.lens_in + x), 0), p.T) : p.T;
   }
+  const int64_t at = static_cast<int64_t>(unit) * p.tiles + tile;
+  int32_t* e_of = which == 0 ? p.q_exp : which == 1 ? p.k_exp : which == 2 ? p.v_exp : p.g_exp;
+  if (tile * kTile >= n) {                                   // behind the text: nobody takes the tile
+    if (tid == 0) e_of[at] = kTrainNoNumber;
+    return;
+  }
   const bool wide = (aligned >> which) & 1;                  // rows start on 16-byte boundaries
 
   // A warp has the row groups `warp` and `warp + 8`; an instruction takes 8 rows x 4 chunks, so that both the rows' reads and
@@ -111,8 +117,7 @@ __global__ void __launch_bounds__(kPackThreads) train_pack_kernel(const TrainPar
   top = __reduce_max_sync(0xffffffffu, tops[lane & (kPackThreads / 32 - 1)]);
   const int e = top == 0 ? kTrainNoNumber : min(7 - (max(static_cast<int>(top >> 7), 1) - 127), kTrainNoNumber - 1);
   const float scale = __int_as_float((e + 127) << 23);
-  const int64_t at = static_cast<int64_t>(unit) * p.tiles + tile;
-  if (tid == 0) (which == 0 ? p.q_exp : which == 1 ? p.k_exp : which == 2 ? p.v_exp : p.g_exp)[at] = e;
+  if (tid == 0) e_of[at] = e;
   char* dst = (which == 0 ? p.q_tiles : which == 1 ? p.k_tiles : which == 2 ? p.v_tiles : p.g_tiles) + at * (key_side ? p.tile_k : p.tile_v);
 #pragma unroll
   for (int g = 0; g < 2; ++g) {

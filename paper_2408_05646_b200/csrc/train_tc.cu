@@ -1158,10 +1158,13 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
             if (lane < 31) my_diagonals[lane] = s;
             __syncwarp();
             const int first = i0 + (warp & 3) * 32 - j0 - 63;                              // distance of slot 0
+            float last = 0.f;                                // the last bucket's, which can be most of them
+            for (int x = max(p.bias_len - 1 - first, 0) + lane; x < 95; x += 32) last += my_diagonals[x];
+            far_sum = fmaf(last, back, far_sum);
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
               const int bucket = lane + 32 * u;
-              if (bucket < p.buckets) {
+              if (bucket < p.buckets - 1) {
                 const int from = max(__ldg(p.starts + bucket) - first, 0);
                 const int next = __ldg(p.starts + bucket + 1), to = next > first + 95 ? 95 : next - first;
                 float sum = 0.f;
