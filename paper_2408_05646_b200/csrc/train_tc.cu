@@ -84,8 +84,29 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
   return p != 0;
 }
-__device__ __noinline__ bool wait_long(unsigned long long* bar, uint32_t parity, int* status) { return mbar_wait(bar, parity, status); }
+// A wait of a whole warp, in one short loop.  (Waits that leave the loop lane by lane, in a function of their own, cost the softmax
+// warps issue slots and registers: 4 x 4096 tokens 1376 us, so 1258.)
 __device__ __forceinline__ bool wait_all(unsigned long long* bar, uint32_t parity, int* status) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  uint64_t t0 = 0;
+  for (uint32_t i = 1;; ++i) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if ((i & 255u) == 0) {                                   // (as mbar_wait: a bound, and an end when another wait gave up)
+      const uint64_t now = global_ns();
+      if (t0 == 0) t0 = now;
+      bool over = *reinterpret_cast<volatile int*>(status) == kStatusTimeout;
+      if (now - t0 > kWaitBoundNs) {
+        atomicExch(status, kStatusTimeout);
+        over = true;
+      }
+      if (__any_sync(0xffffffffu, over)) return false;
+    }
+  }
+}
+// The same with the loop in a function of its own, lane by lane: the forward pass, whose softmax is longer, is better off with it
+// (514 us, so 538).
+__device__ __noinline__ bool wait_long(unsigned long long* bar, uint32_t parity, int* status) { return mbar_wait(bar, parity, status); }
+__device__ __forceinline__ bool wait_called(unsigned long long* bar, uint32_t parity, int* status) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   return __all_sync(0xffffffffu, wait_long(bar, parity, status)) != 0;
 }
@@ -300,7 +321,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
     int issued = 0, it = 0, index = blockIdx.x;
     for (;; ++it) {
       const int set = set_of(plan, it);
-      if (it >= plan.sets) ok = wait_all(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
+      if (it >= plan.sets) ok = wait_called(&hdr->own_empty[set], set_phase(plan, it) ^ 1u, p.status);
       if (!ok) break;
       Item* item = &hdr->item[set];
       if (it > 0) index = next_entry(p.next, lane);
@@ -365,18 +386,18 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
     Place at, next;                                          // of P v' and of S
     for (int it = 0; ok; ++it) {
       const int set = set_of(plan, it);
-      ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
+      ok = wait_called(&hdr->own_full[set], set_phase(plan, it), p.status);
       if (!ok || hdr->item[set].tiles[0] < 0) break;
       const int nt = hdr->item[set].tiles[x], most = max(hdr->item[set].tiles[0], hdr->item[set].tiles[1]);
       const int rk16 = (hdr->item[set].rp_k + 15) & ~15, rv16 = (hdr->item[set].rp_v + 15) & ~15;
       const uint32_t idesc_o = instr_desc_f16(rv16) | kMnMajorB;
       const uint64_t dq = smem_desc(smem_u32(own) + (set * 2 + x) * p.tile_k, 128, rk16 << 4);
       const uint64_t dk = smem_desc(smem_u32(ring), 128, rk16 << 4), dv = smem_desc(smem_u32(ring) + p.tile_k, rv16 << 4, 128);
-      if (nt > 0 && sums > 0) ok = wait_all(&hdr->acc_free[x], (sums - 1) & 1u, p.status);
+      if (nt > 0 && sums > 0) ok = wait_called(&hdr->acc_free[x], (sums - 1) & 1u, p.status);
       for (int j = 0; nt > 0 && j < 2 * nt + 2 && ok; ++j) { // S of half j, two halves ahead of P
         const int half = j & 1;
         if (j >= 2) {
-          ok = wait_all(&hdr->p_full[x][half], (done + ((j - 2) >> 1)) & 1u, p.status);
+          ok = wait_called(&hdr->p_full[x][half], (done + ((j - 2) >> 1)) & 1u, p.status);
           if (!ok) break;
           tc_fence_after();
           if (lead) {
@@ -388,7 +409,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
           if (half) at.next(plan.stages);
         }
         if (j < 2 * nt) {                                    // (in P's place: behind the product that takes it)
-          if (!half) ok = wait_all(&hdr->full[next.stage], next.phase, p.status);
+          if (!half) ok = wait_called(&hdr->full[next.stage], next.phase, p.status);
           if (!ok) break;
           tc_fence_after();
           if (lead) {
@@ -407,7 +428,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
       done += nt;
       sums += nt > 0;
       for (int j = nt; j < most && ok; ++j) {                // tiles that only the other tile of queries sees
-        ok = wait_all(&hdr->full[at.stage], at.phase, p.status);
+        ok = wait_called(&hdr->full[at.stage], at.phase, p.status);
         if (ok && lead) mbar_arrive(&hdr->empty[at.stage]);
         at.next(plan.stages);
         next.next(plan.stages);
@@ -423,7 +444,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
     Place at;
     for (int it = 0; ok; ++it) {
       const int set = set_of(plan, it);
-      ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
+      ok = wait_called(&hdr->own_full[set], set_phase(plan, it), p.status);
       if (!ok) break;
       const Item item = hdr->item[set];
       if (item.tiles[0] < 0) break;
@@ -438,7 +459,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
         const bool diag = j >= 2 * nt - 2, near = BIAS == kTable && near_tile(p, i0, j0);
         float base = BIAS == kTable && !near ? far_bias : BIAS == kAlibi ? slope2 * static_cast<float>(j0 - i) : 0.f;
         const uint32_t tSh = tS + half * kHalf;
-        ok = (half || wait_all(&hdr->full[at.stage], at.phase, p.status)) && wait_all(&hdr->s_full[x][half], (done + (j >> 1)) & 1u, p.status);
+        ok = (half || wait_called(&hdr->full[at.stage], at.phase, p.status)) && wait_called(&hdr->s_full[x][half], (done + (j >> 1)) & 1u, p.status);
         if (!ok) break;
         tc_fence_after();
         const float4 scales = *reinterpret_cast<const float4*>(ring + at.stage * stage_bytes + p.tile_k + p.tile_v);
@@ -491,7 +512,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
           const float alpha = raise ? ex2(m - now) : 1.f;    // (0 at the first keys)
           l *= alpha;
           if (j > 0) {                                       // the half before has been added to o'
-            ok = wait_all(&hdr->p_used[x][half ^ 1], (done + ((j - 1) >> 1)) & 1u, p.status);
+            ok = wait_called(&hdr->p_used[x][half ^ 1], (done + ((j - 1) >> 1)) & 1u, p.status);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
@@ -531,7 +552,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
       if (!ok) break;
       for (int j = nt; j < most; ++j) at.next(plan.stages);
       done += nt;
-      if (nt > 0) ok = wait_all(&hdr->acc_full[x], sums & 1u, p.status);
+      if (nt > 0) ok = wait_called(&hdr->acc_full[x], sums & 1u, p.status);
       if (!ok) break;
       tc_fence_after();
       if (tile < p.tiles) {
