@@ -18,12 +18,13 @@
 // The backward pass has two kinds of items, one that owns a tile of keys (dk', dv': four products per pair of tiles) and one that
 // owns a tile of queries (dq': three, S and do' v' a second time): the alternative, dq' added up in memory by every tile of keys,
 // moves 512 r bytes of fp32 additions per pair of tiles through L2 and leaves sums whose order changes from run to run.
-// 4 x 4096 tokens, 32 heads, rank 80: forward 514 us, a backward call 1378, 74 of them packing (624 TFLOP/s of the five products
-// that the formulas need); tensor pipe busy 34 and 43 % of the time, exponentials 55 and 40 %, an instruction issued in 0.40 and
-// 0.36 of the clocks.  What is left is the chain of a half tile, product, load, exponentials, store, product, of which two
-// run at a time (some 2970 clocks for a pair of tiles of a key item, 2180 of a query item, against 1600 and 1040 of their
-// products).  Tried and slower: three chains (a third fewer registers for each), sixteen softmax warps with half the columns,
-// turns between the halves' exponentials, a part of the exponentials as polynomials on the multiply-add units.
+// 4 x 4096 tokens, 32 heads, rank 80: forward 514 us, a backward call 1252, 74 of them packing (690 TFLOP/s of the five products
+// that the formulas need); tensor pipe busy 34 and 48 % of the time, exponentials 55 and 44 %, an instruction issued in 0.40 and
+// 0.37 of the clocks.  What is left is the chain of a half tile, product, load, exponentials, store, product, of which two
+// run at a time (some 4700 clocks for a pair of tiles, its key item and its query item together, against 2640 of their products).
+// Tried and slower: three chains (a third fewer registers for each), sixteen softmax warps with half the columns, turns between
+// the halves' exponentials, a part of the exponentials as polynomials on the multiply-add units.  No difference: 216 registers
+// for the softmax warps and 56 for the others, loads of do' v' in front of the exponentials or beside the store of P.
 //
 // Tiles carry a power of two each (2^e).  What is accumulated over tiles needs one scale: the tile's deviation from the
 // smallest exponent of all goes into the factors that P and dS are formed with, where it costs nothing.

@@ -386,3 +386,31 @@ def test_refusals_that_need_a_device():
     s.lay.train_detach()
     with pytest.raises(binding.EigenAttnError):
         s.lay.train_backward(s.x[3])
+
+
+def test_tensors_that_the_binding_refuses():
+    s = Step(2, 64, [32, 16], [16, 32], 64, BF, bias=True)
+    q, k, v, g = s.x
+    wide = torch.zeros(2, 64, 2 * q.shape[2], dtype=BF, device="cuda")
+    lens = torch.tensor([64, 3], dtype=torch.int32, device="cuda")
+    for bad in (q.float(), q.cpu(), q[:, :, :-8].contiguous(), wide[:, :, ::2], wide, q[:1]):
+        with pytest.raises(AssertionError):
+            s.lay.train_forward(bad, k, v)
+        with pytest.raises(AssertionError):
+            s.lay.train_forward(q, bad, v)
+    for bad in (lens.cpu(), lens.long(), lens[:1], torch.zeros(4, dtype=torch.int32, device="cuda")[::2]):
+        with pytest.raises(AssertionError):
+            s.lay.train_forward(q, k, v, lens=bad)
+    with pytest.raises(AssertionError):
+        s.lay.train_forward(q, k, v, group=2)
+    with pytest.raises(AssertionError):
+        s.lay.train_forward(q[:, :63].contiguous(), k, v)
+    want = Step(2, 64, [32, 16], [16, 32], 64, BF, bias=True).run()
+    out = s.lay.train_forward(q, k, v)
+    for bad in (g.float(), g.cpu(), g[:, :63].contiguous()):
+        with pytest.raises(AssertionError):
+            s.lay.train_backward(bad)
+    for bad in (s.table.float(), s.table.cpu(), s.table[:, :-1].contiguous(), s.table[:1]):
+        with pytest.raises(AssertionError):
+            s.lay.set_bias(bad)
+    assert same((out,) + tuple(s.lay.train_backward(g, bias_grad=True)), want)       # none of them changed anything
