@@ -24,7 +24,7 @@
 // run at a time (some 4700 clocks for a pair of tiles, its key item and its query item together, against 2640 of their products).
 // Tried and slower: three chains (a third fewer registers for each), sixteen softmax warps with half the columns, turns between
 // the halves' exponentials, a part of the exponentials as polynomials on the multiply-add units.  No difference: 216 registers
-// for the softmax warps and 56 for the others, loads of do' v' in front of the exponentials or beside the store of P.
+// for the softmax warps and 56 for the others.
 //
 // Tiles carry a power of two each (2^e).  What is accumulated over tiles needs one scale: the tile's deviation from the
 // smallest exponent of all goes into the factors that P and dS are formed with, where it costs nothing.
@@ -871,14 +871,14 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
         }
         tmem_st16(tP, w[0]);
         tmem_st16(tP + 16, w[1]);
-        tmem_wait_st();
-        tc_fence_before();
-        arrive_warp(&hdr->p_full[0][half], lane);
         ok = wait_all(&hdr->g_full[half], phase, p.status);
         if (!ok) break;
         tc_fence_after();
         tmem_ld32(tG, r[0]);
         tmem_ld32(tG + 32, r[1]);
+        tmem_wait_st();
+        tc_fence_before();
+        arrive_warp(&hdr->p_full[0][half], lane);
         tmem_wait_ld_of(r[0]);
         tmem_wait_ld_of(r[1]);
         const unsigned long long a = both(scales.y);
@@ -1126,6 +1126,12 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
         tmem_ld32(tS + 32, r[1]);
         tmem_wait_ld_of(r[0]);
         tmem_wait_ld_of(r[1]);
+        uint32_t gr[2][32];                                  // G, on its way beside the exponentials (it is there before S as a rule)
+        ok = wait_all(&hdr->g_full[half], behind & 1u, p.status);
+        if (!ok) break;
+        tc_fence_after();
+        tmem_ld32(tG, gr[0]);
+        tmem_ld32(tG + 32, gr[1]);
         unsigned long long e[32];                            // pairs of keys
         const unsigned long long c_2 = both(c), add_2 = both(add);
 #pragma unroll
@@ -1134,20 +1140,15 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
           unpack2(fma2p(pair_at(r[k >> 4], k & 15), c_2, BIAS == kAlibi ? fma2p(both(slope2), pack2(2 * k, 2 * k + 1), add_2) : add_2), x, y);
           e[k] = pack2(ex2(x), ex2(y));
         }
-        ok = wait_all(&hdr->g_full[half], behind & 1u, p.status);
-        if (!ok) break;
-        tc_fence_after();
-        tmem_ld32(tG, r[0]);
-        tmem_ld32(tG + 32, r[1]);
-        tmem_wait_ld_of(r[0]);
-        tmem_wait_ld_of(r[1]);
+        tmem_wait_ld_of(gr[0]);
+        tmem_wait_ld_of(gr[1]);
         tc_fence_before();
         arrive_warp(&hdr->g_read[half], lane);
         const unsigned long long a_2 = both(scales.z), d_2 = both(-scales.y * delta);
         uint32_t w[2][16];
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
-          e[k] = mul2p(e[k], fma2p(pair_at(r[k >> 4], k & 15), a_2, d_2));
+          e[k] = mul2p(e[k], fma2p(pair_at(gr[k >> 4], k & 15), a_2, d_2));
           float x, y;
           unpack2(e[k], x, y);
           w[k >> 4][k & 15] = pack_f16(x, y);
