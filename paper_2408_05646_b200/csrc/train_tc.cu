@@ -18,7 +18,7 @@
 // The backward pass has two kinds of items, one that owns a tile of keys (dk', dv': four products per pair of tiles) and one that
 // owns a tile of queries (dq': three, S and do' v' a second time): the alternative, dq' added up in memory by every tile of keys,
 // moves 512 r bytes of fp32 additions per pair of tiles through L2 and leaves sums whose order changes from run to run.
-// 4 x 4096 tokens, 32 heads, rank 80: forward 514 us, a backward call 1252, 74 of them packing (690 TFLOP/s of the five products
+// 4 x 4096 tokens, 32 heads, rank 80: forward 514 us, a backward call 1249, 74 of them packing (690 TFLOP/s of the five products
 // that the formulas need); tensor pipe busy 34 and 48 % of the time, exponentials 55 and 44 %, an instruction issued in 0.40 and
 // 0.37 of the clocks.  What is left is the chain of a half tile, product, load, exponentials, store, product, of which two
 // run at a time (some 4700 clocks for a pair of tiles, its key item and its query item together, against 2640 of their products).
