@@ -2081,7 +2081,8 @@ void make_train_layout(const eigen_attn* h, int tokens, int group, TrainLayout* 
     t->k = area(rows * h->L.sum_rp_k * sizeof(float));
     t->v = area(rows * h->L.sum_rp_v * sizeof(float));
   }
-  t->bias = area(group == 1 ? units * train_bias_parts(h, tokens) * ea::kMaxBuckets * sizeof(float) : 0);
+  // (a pass may have fewer query heads than the scratch: with one, and a learned bias, it leaves sums here)
+  t->bias = area(units * train_bias_parts(h, tokens) * ea::kMaxBuckets * sizeof(float));
   t->bytes = off;
 }
 
