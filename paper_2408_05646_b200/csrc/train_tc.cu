@@ -49,6 +49,8 @@ constexpr int kHeaderBytes = 960;
 constexpr int kScaleBytes = 16;           // behind a stage's tiles: the scales of the pair of tiles, worked out by the copying warp
 constexpr int kForwardShift = 7;          // P of the forward pass times 2^7: its reference lags behind the maximum by up to 2^8
 constexpr int kBackwardShift = 14;        // P of the backward pass, at most 1, times 2^14: fp16 keeps all bits down to 2^-28
+constexpr int kLeastDeviation = -60;      // of a tile from the smallest exponent: with it P and dS are zero in fp16 (a tile of zeros has
+                                          //   any), and what is summed in 32 bits, the rows' sums and dS of a learned bias, stays in range
 
 // What a launch decides for all its CTAs.
 struct Plan {
@@ -361,8 +363,8 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
         const char* k = p.k_tiles + static_cast<int64_t>(key_unit) * p.tiles * p.tile_k;
         const char* v = p.v_tiles + static_cast<int64_t>(key_unit) * p.tiles * p.tile_v;
         for (int j = 0; j < most; ++j, ++issued, at.next(plan.stages)) {
-          // the tile's deviation from the largest v'; at 2^-60 of it P is zero in fp16, and the sum of the row still exact
-          const int k_e = __ldg(k_exp + j), f = max(g_v - __ldg(v_exp + j), -60);
+          // the tile's deviation from the largest v'
+          const int k_e = __ldg(k_exp + j), f = max(g_v - __ldg(v_exp + j), kLeastDeviation);
           unsigned long long* full = &hdr->full[at.stage];
           if (issued >= plan.stages && !(ok = mbar_wait(&hdr->empty[at.stage], at.phase ^ 1u, p.status))) break;
           unsigned char* st = ring + at.stage * stage_bytes;
@@ -989,8 +991,10 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
           mbar_arrive(&hdr->own_full[set]);
         }
         for (int j = 0; j < nt; ++j, ++issued, at.next(plan.stages)) {
-          // P = 2^(S c - L);  dS = P (G a - delta d), at most 2^15 (as above), times the tile's share of the scale of k'
-          const int k_e = __ldg(p.k_exp + keys + j), v_e = __ldg(p.v_exp + keys + j), d_e = -9 + g_e + g_v + g_k - k_e;
+          // P = 2^(S c - L);  dS = P (G a - delta d), at most 2^15 (as above), times the tile's share of the scale of k'.  The
+          // gradient of a learned bias takes dS back to its own size, so a, d and 1 / d are powers of one exponent in range.
+          const int k_e = __ldg(p.k_exp + keys + j), v_e = __ldg(p.v_exp + keys + j);
+          const int d_e = max(-9 + g_e + g_v + max(g_k - k_e, kLeastDeviation), -126);
           unsigned long long* full = &hdr->full[at.stage];
           if (issued >= plan.stages && !(ok = mbar_wait(&hdr->empty[at.stage], at.phase ^ 1u, p.status))) break;
           unsigned char* st = ring + at.stage * stage_bytes;
