@@ -115,6 +115,11 @@ __device__ __forceinline__ bool wait_called(unsigned long long* bar, uint32_t pa
 }
 // 2^e; exponents that no pair of ordinary tiles has end at the ends of the range
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((min(max(e, -126), 127) + 127) << 23); }
+// 2^e in two factors, for results: their exponents are sums of three tiles' and reach over both ends of the range
+__device__ __forceinline__ float2 halves_of(int e) { return make_float2(pow2(e >> 1), pow2(e - (e >> 1))); }
+// Exponent of dS for the smallest exponents of do' and v': |do' v'| and |delta| are below r 2^(16 - g_e - v_e), and with it dS at
+// most 2^15, the end of fp16.  (Gradients too small for that get as much of it as there is.)
+__device__ __forceinline__ int gradient_exponent(int g_e, int v_e) { return min(g_e + v_e - 9, 126); }
 __device__ __forceinline__ void arrive_warp(unsigned long long* bar, int lane) {
   __syncwarp();
   if (lane == 0) mbar_arrive(bar);
@@ -216,9 +221,11 @@ __device__ __forceinline__ void store8(__nv_bfloat16* dst, const float* x, bool 
     }
   }
 }
-// Columns [lo, hi) (multiples of 16) of this thread's accumulator row times `scale` into a packed row; zeros where `live` is false.
-__device__ __forceinline__ void store_row(uint32_t acc, int lo, int hi, int rp, float scale, __nv_bfloat16* dst, bool in_range,
+// Columns [lo, hi) (multiples of 16) of this thread's accumulator row times `scale` 2^e into a packed row; zeros where `live` is false.
+__device__ __forceinline__ void store_row(uint32_t acc, int lo, int hi, int rp, float scale, int e, __nv_bfloat16* dst, bool in_range,
                                           bool live, bool aligned) {
+  const float2 power = halves_of(e);
+  scale *= power.x;
 #pragma unroll 1
   for (int c = lo; c < hi; c += 16) {
     uint32_t r[16];
@@ -226,7 +233,7 @@ __device__ __forceinline__ void store_row(uint32_t acc, int lo, int hi, int rp, 
     tmem_wait_ld_of(r);
     float x[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = live ? __uint_as_float(r[j]) * scale : 0.f;
+    for (int j = 0; j < 16; ++j) x[j] = live ? __uint_as_float(r[j]) * scale * power.y : 0.f;
     if (in_range) {
       store8(dst + c, x, aligned);
       if (c + 8 < rp) store8(dst + c + 8, x + 8, aligned);
@@ -671,13 +678,13 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
       for (int i = 0; i < p.group && ok; ++i) {
         const int64_t q_unit = static_cast<int64_t>(h * p.group + i) * p.B + b;
         for (int t = 0; t < per_head; ++t, ++issued, at.next(plan.stages)) {
-          // P^T = 2^(S c + lift - L), times 2^14 and the tile's share of do''s scale;  dS^T = P^T (G^T a - delta d), at most
-          // 2^15: |do' v'| and |delta| are below r 2^(16 - e - e'), e and e' the smallest exponents of do' and v'.  The rows'
-          // own numbers, lift - L and delta d, are worked out here, four a lane.
+          // P^T = 2^(S c + lift - L), times 2^14 and the tile's share of do''s scale;  dS^T = P^T (G^T a - delta d), with the
+          // tile's share of q''s.  The rows' own numbers, lift - L and delta d, are worked out here, four a lane.
           const int64_t from = q_unit * p.tiles + tile + t, row_at = q_unit * p.pad + (tile + t) * kTile + 4 * lane;
           const int q_e = __ldg(p.q_exp + from), g_e = __ldg(p.g_exp + from);
           float4 l = __ldg(reinterpret_cast<const float4*>(p.lse + row_at)), dl = __ldg(reinterpret_cast<const float4*>(p.delta + row_at));
-          const int lift = kBackwardShift + g_g - g_e, d_e = -9 + g_g + g_v + g_q - q_e - lift;
+          const int lift = kBackwardShift + g_g - g_e;
+          const int d_e = max(gradient_exponent(g_g, g_v) + max(g_q - q_e, kLeastDeviation) - lift, -126);
           float add = static_cast<float>(lift);
           if (BIAS == kTable && !near_tile(p, t * kTile, 0)) add += far_bias;
           if (BIAS == kAlibi) add -= slope2 * static_cast<float>(t * kTile + 4 * lane);
@@ -921,8 +928,8 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
             zero_row(v_lo, v_hi, item.rp_v, to_v, plan.aligned & 2);
           }
         } else {
-          store_row(tmem + lanes + cK, k_lo, k_hi, item.rp_k, p.scale * pow2(9 - item.small[3] - item.small[2] - item.small[0]), to_k, there, live, plan.aligned & 1);
-          store_row(tmem + lanes + cV, v_lo, v_hi, item.rp_v, pow2(-kBackwardShift - item.small[3]), to_v, there, live, plan.aligned & 2);
+          store_row(tmem + lanes + cK, k_lo, k_hi, item.rp_k, p.scale, -gradient_exponent(item.small[3], item.small[2]) - item.small[0], to_k, there, live, plan.aligned & 1);
+          store_row(tmem + lanes + cV, v_lo, v_hi, item.rp_v, 1.f, -kBackwardShift - item.small[3], to_v, there, live, plan.aligned & 2);
           tc_fence_before();
           arrive_warp(&hdr->acc_free[0], lane);
           ++sums;
@@ -991,10 +998,10 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
           mbar_arrive(&hdr->own_full[set]);
         }
         for (int j = 0; j < nt; ++j, ++issued, at.next(plan.stages)) {
-          // P = 2^(S c - L);  dS = P (G a - delta d), at most 2^15 (as above), times the tile's share of the scale of k'.  The
+          // P = 2^(S c - L);  dS = P (G a - delta d), with the tile's share of the scale of k'.  The
           // gradient of a learned bias takes dS back to its own size, so a, d and 1 / d are powers of one exponent in range.
           const int k_e = __ldg(p.k_exp + keys + j), v_e = __ldg(p.v_exp + keys + j);
-          const int d_e = max(-9 + g_e + g_v + max(g_k - k_e, kLeastDeviation), -126);
+          const int d_e = max(gradient_exponent(g_e, g_v) + max(g_k - k_e, kLeastDeviation), -126);
           unsigned long long* full = &hdr->full[at.stage];
           if (issued >= plan.stages && !(ok = mbar_wait(&hdr->empty[at.stage], at.phase ^ 1u, p.status))) break;
           unsigned char* st = ring + at.stage * stage_bytes;
@@ -1227,7 +1234,7 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
         if (nt == 0) {
           if (i < p.T) zero_row(lo, hi, item.rp_k, to, plan.aligned & 1);
         } else {
-          store_row(tmem + lanes + cQ, lo, hi, item.rp_k, p.scale * pow2(9 - item.small[3] - item.small[2] - item.small[1]), to, i < p.T, i < item.n, plan.aligned & 1);
+          store_row(tmem + lanes + cQ, lo, hi, item.rp_k, p.scale, -gradient_exponent(item.small[3], item.small[2]) - item.small[1], to, i < p.T, i < item.n, plan.aligned & 1);
           tc_fence_before();
           arrive_warp(&hdr->acc_free[0], lane);
           ++sums;

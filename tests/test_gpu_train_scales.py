@@ -33,12 +33,13 @@ def step(q, k, v, g, r, d_head, buckets=None, table=None):
     return got, want
 
 
-def within(got, want, names, dtype, part):
-    """Half a step of the type (below the smallest normal number: half of its last bit), and `part` of the terms' sizes."""
+def within(got, want, names, dtype, part, floor={}):
+    """Half a step of the type (below the smallest normal number: half of its last bit), `part` of the terms' sizes, and an
+    absolute `floor` where one is given."""
     half, least = torch.finfo(dtype).eps / 2, torch.finfo(dtype).tiny * torch.finfo(dtype).eps / 2
     for name in names:
         assert np.isfinite(got[name]).all(), name
-        over = np.abs(got[name] - want[name]) - half * np.abs(want[name]) - least - part * want[name + "_size"]
+        over = np.abs(got[name] - want[name]) - half * np.abs(want[name]) - least - part * want[name + "_size"] - floor.get(name, 0)
         worst = np.argmax(over)
         assert over.max() <= 0, (name, got[name].flat[worst], want[name].flat[worst], want[name + "_size"].flat[worst])
 
@@ -56,3 +57,34 @@ def test_the_table_gradient_counts_blocks_of_tiny_keys(key_scale, grad_scale):
     got, want = step(q, k, v, g, r, 64, buckets, table)
     within(got, want, ["table"], BF, 2.0 ** -12)
     within(got, want, ["out", "dq", "dk", "dv"], BF, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("q_e,k_e,v_e,g_e", [(0, 0, 0, -110), (-24, -24, -8, -90), (40, -40, -64, -64), (-40, 40, -64, -64), (30, -30, 20, 60)])
+def test_results_near_the_ends_of_the_range(q_e, k_e, v_e, g_e):
+    """Tensors of very small or large numbers: the powers of two of three tiles add up to more than one factor can hold.  Least
+    products that count: delta = do' o' of 2^-128 in the third and fourth case, kept to 2^-149 or 2^-21 of it."""
+    T, r = 140, [32, 24]
+    gen = torch.Generator().manual_seed(6)
+    x = [rows(gen, 1, T, r, 1, BF, s * 2.0 ** e, 0.0) for s, e in zip((1.5, 1.0, 1.0, 1.0), (q_e, k_e, v_e, g_e))]
+    got, want = step(*x, r, 64)
+    within(got, want, ["out", "dq", "dk", "dv"], BF, 2.0 ** -11)
+
+
+def test_large_results_of_which_the_largest_numbers_are_no_part():
+    """A column of v' (2^42) that do' (2^66) does not ask for sets the exponents; dk' is of the others' (2^26), times q' (2^32).
+    dS is then small in fp16: 2^24 2^(-e-e') becomes 2^15 there (e, e' the smallest exponents of do' and v'; 2^-e <= 2^-7
+    max|do'|, 2^-e' <= 2^-7 max|v'|), so that the smallest half step, 2^-25, is 2^-30 max|do'| max|v'| of dS, and with the tile's deviation, at
+    most a factor of two more, dk' is off by up to 2^-29 max|do'| max|v'| max|q'| scale for every query, dq' by the same with k' for
+    every key (scale 1 / 8).  Here that is 2^121.6 in the sum of all 140; the largest dk' is 2^125.5, and a power of two left out of the
+    results takes nearly all of it away."""
+    T, r = 140, [32, 24]
+    gen = torch.Generator().manual_seed(7)
+    q, k, v, g = (rows(gen, 1, T, r, 1, BF, s, 0.0) for s in (1.5 * 2.0 ** 32, 2.0 ** -32, 2.0 ** 26, 2.0 ** 66))
+    for first in (0, 32):
+        v[:, :, first] *= 2.0 ** 16
+        g[:, :, first] = 0
+    got, want = step(q, k, v, g, r, 64)
+    assert np.abs(want["dk"]).max() > 2.0 ** 118
+    mq, mk, mv, mg = (x.abs().max().item() for x in (q, k, v, g))
+    floor = {"dk": T * 2.0 ** -29 * mg * mv * mq / 8, "dq": T * 2.0 ** -29 * mg * mv * mk / 8}
+    within(got, want, ["out", "dq", "dk", "dv"], BF, 2.0 ** -11, floor)
