@@ -360,8 +360,8 @@ ea_status eigen_attn_bias_starts(eigen_attn_t h, int32_t* starts);
  * read, and their outputs and gradients are zero.  The lengths are read by the launch, so a captured call follows them.
  * The tokens' numbers are finite (one that is not reaches results of its own head and sequence, those of earlier tokens
  * among them).  In 16-bit layers a number that is below 2^-22 of the largest of its head within 128 tokens (0 to 127, 128 to
- * 255, ...) is off by up to 2^-33 of that one, and a result by up to 2^-29 for every term of the product of the largest
- * numbers that it is made of (of its head and sequence).
+ * 255, ...) is off by up to 2^-32 of that one (by 2^-144 where that one is below 2^-112), and a result by up to 2^-29 for every
+ * term of the product of the largest numbers that it is made of (of its head and sequence).
  * A position bias (ALiBi or learned) is per K/V head: only with group 1 (EA_ERR_UNSUPPORTED).  Not with a rotary embedding.
  *
  * train_bytes:    size of the scratch for up to max_tokens (1..2^20) tokens and `group` query heads per K/V head.

@@ -5,8 +5,9 @@
 // registers, keep 11 significant bits instead of bf16's 8 that way (both operands of a product have one type; with bf16 their
 // rounding alone would be as large as that of the output).  bf16 values have 8 bits and fit; what fp16 lacks is range.  Every
 // tile is therefore multiplied by the power of two that brings its largest number into [2^7, 2^8): a number keeps all its
-// bits down to 2^-22 of the tile's largest, and what is below is off by at most 2^-33 of it.  The consumers take the powers out of
-// the scales that they multiply by anyway.  (Numbers that are not finite take no part in the choice and stay what they are.)
+// bits down to 2^-22 of the tile's largest, and what is below is off by at most 2^-32 of it (half of fp16's last step is 2^-25, the
+// largest at least 2^7; powers end at 2^119).  The consumers take the powers out of the scales that they multiply by anyway.
+// (Numbers that are not finite take no part in the choice and stay what they are.)
 // The gradient's tiles also get delta = do' o' here, the dot product of a row with the o' that the forward pass kept in 32 bits
 // (from the rounded output it would be off by a rounding of o', once per row and the same for all its keys).
 // Bound by bytes: rows in, tiles out (4 x 4096 tokens, 32 heads, rank 80: q', k', v' 503 MB in 109 us, do' and o' 336 MB in 74,

@@ -88,3 +88,29 @@ def test_large_results_of_which_the_largest_numbers_are_no_part():
     mq, mk, mv, mg = (x.abs().max().item() for x in (q, k, v, g))
     floor = {"dk": T * 2.0 ** -29 * mg * mv * mq / 8, "dq": T * 2.0 ** -29 * mg * mv * mk / 8}
     within(got, want, ["out", "dq", "dk", "dv"], BF, 2.0 ** -11, floor)
+
+
+@pytest.mark.parametrize("largest", [1.0, 1.9921875, -1.5])
+@pytest.mark.parametrize("side", [1.0, -1.0])
+def test_numbers_far_below_the_largest_of_their_block(largest, side):
+    """One token, whose o' is its v' and whose dv' is its do': what an operand's conversion leaves is seen as it is.  From 2^-22 of the
+    largest on a number is kept; below, it is off by up to 2^-32 of the largest (half of fp16's last step, 2^-25, where the largest
+    is at least 2^7), and one of 2^-32 can be off by just that."""
+    r = 64
+    x = torch.zeros(1, 1, 2 * r, dtype=BF)
+    x[0, 0, 0] = x[0, 0, r] = largest
+    e = torch.arange(1, r)
+    x[0, 0, 1:r] = (side * 1.6953125 * 2.0 ** -(e.double() * 0.75).floor()).to(BF)          # eight bits each
+    x[0, 0, r + 1:] = (side * 2.0 ** -e.double()).to(BF)
+    one = torch.ones(1, 1, 2 * r, dtype=BF)
+    lay = layer(1, [r, r], [r, r], r, BF)
+    lay.train_attach(1)
+    out = lay.train_forward(one.cuda(), one.cuda(), x.cuda())
+    _, _, dv = lay.train_backward(x.cuda())
+    top = abs(largest)
+    for got in (out, dv):
+        err = (got.cpu().double() - x.double()).abs()
+        assert (err[x.double().abs() >= top * 2.0 ** -22] == 0).all()
+        assert err.max() <= top * 2.0 ** -32
+    if largest == 1.0:                                       # the bound is reached: 2^-32 lies between 0 and fp16's 2^-24 / 2^7
+        assert (out.cpu().double() - x.double())[0, 0, r + 32].abs() == 2.0 ** -32
