@@ -655,7 +655,8 @@ class EigenAttnLayer:
 
     # -- a learned bias of relative positions
     def bias_attach(self, n_buckets: int, max_distance: int, stream=None) -> torch.Tensor:
-        """Allocates the buffer of a learned position bias (kept on the layer) and attaches it; the table is zero until set_bias."""
+        """Allocates the buffer of a learned position bias (kept on the layer) and attaches it; the table is zero until set_bias.
+        Work of other streams with an earlier buffer has to be over (here and in bias_detach): its memory goes back to `stream`."""
         n = _sz(0)
         self._check(lib.eigen_attn_bias_bytes(self.handle, int(n_buckets), int(max_distance), ctypes.byref(n)), "eigen_attn_bias_bytes")
         with torch.cuda.stream(stream):
@@ -682,19 +683,35 @@ class EigenAttnLayer:
         return list(arr)
 
     # -- training: attention over rank-space rows with its backward pass
-    def train_attach(self, max_tokens: int, group: int = 1) -> torch.Tensor:
-        """Allocates the scratch of the training calls for up to `max_tokens` tokens (kept on the layer) and attaches it."""
+    def train_attach(self, max_tokens: int, group: int = 1, stream=None) -> torch.Tensor:
+        """Allocates the scratch of the training calls for up to `max_tokens` tokens (kept on the layer) and attaches it.  Passes
+        that other streams still have to run keep the memory of one that is replaced or detached; a captured graph that is to be
+        replayed needs it kept by the caller."""
         n = _sz(0)
         self._check(lib.eigen_attn_train_bytes(self.handle, int(max_tokens), int(group), ctypes.byref(n)), "eigen_attn_train_bytes")
-        buf = device_alloc(n.value, self.device)           # (the layer keeps the one it had if the call refuses)
+        with torch.cuda.stream(stream):
+            buf = device_alloc(n.value, self.device)       # (the layer keeps the one it had if the call refuses)
         self._check(lib.eigen_attn_train_attach(self.handle, int(max_tokens), int(group), buf.data_ptr(), n.value),
                     "eigen_attn_train_attach")
-        self.train_buf, self._trained = buf, None
+        self.train_buf, self._trained, self._train_streams = buf, None, set()
         return buf
 
     def train_detach(self) -> None:
         self._check(lib.eigen_attn_train_attach(self.handle, 0, 0, None, 0), "eigen_attn_train_attach")
         self.train_buf = self._trained = None
+
+    def _train_on(self, stream) -> None:
+        """Tells the allocator, once for each stream, that the scratch is used there."""
+        if getattr(self, "train_buf", None) is None:       # (the call refuses)
+            return
+        if stream is None:
+            index = torch._C._cuda_getDevice() if self.device.index is None else self.device.index
+            ptr = torch._C._cuda_getCurrentRawStream(index)
+        else:
+            ptr = stream.cuda_stream
+        if ptr not in self._train_streams:
+            self.train_buf.record_stream(stream or torch.cuda.current_stream(self.device))
+            self._train_streams.add(ptr)
 
     def train_forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: Optional[torch.Tensor] = None,
                       group: int = 1, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -708,6 +725,7 @@ class EigenAttnLayer:
         if out is None:
             out = self._new_out(self.B, T, group * self.offs_v[-1], stream=stream)
         po = self._packed(out, T, group * self.offs_v[-1])
+        self._train_on(stream)
         self._check(_call_on(self.device, stream, lib.eigen_attn_train_forward, self.handle, pq, pk, pv, T, int(group),
                              None if lens is None else lens.data_ptr(), po), "eigen_attn_train_forward")
         self._trained = (T, int(group))
@@ -728,6 +746,7 @@ class EigenAttnLayer:
         table = None
         if bias_grad:
             table = self._new_out(self.H, max(1, getattr(self, "bias_buckets", 0)), stream=stream)   # (refused without a bias)
+        self._train_on(stream)
         self._check(_call_on(self.device, stream, lib.eigen_attn_train_backward, self.handle, pg,
                              self._packed(dq, T, group * self.offs_k[-1]), self._packed(dk, T, self.offs_k[-1]),
                              self._packed(dv, T, self.offs_v[-1]), None if table is None else table.data_ptr()),

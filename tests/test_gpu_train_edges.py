@@ -17,3 +17,31 @@ def test_scratch_for_more_query_heads_than_the_pass_has(dtype, attached):
     b.lay.train_attach(300, attached)
     assert same(a.run(), b.run())
     b.lay.poll_status()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("how", ["replaced", "detached"])
+def test_scratch_that_is_replaced_while_another_stream_has_a_pass_to_run(dtype, how, monkeypatch):
+    """Its memory is not handed out before that pass is over."""
+    from paper_2408_05646_b200 import binding
+    monkeypatch.setattr(binding, "device_alloc", binding._default_alloc)     # (the guards' keeps every buffer alive)
+    want = Step(2, 300, [32, 40], [40, 32], 64, dtype, seed=8).run()
+    a = Step(2, 300, [32, 40], [40, 32], 64, dtype, seed=8, attach=8000)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(400_000_000)                       # some 0.2 s in front of the passes
+    got = a.run(stream=s)
+    at, n = a.lay.train_buf.data_ptr(), a.lay.train_buf.numel()
+    if how == "replaced":
+        a.lay.train_attach(16)
+    else:
+        a.lay.train_detach()
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    assert not s.query()                                     # it has not begun
+    assert all(x.data_ptr() + n <= at or at + n <= x.data_ptr() for x in others)
+    for x in others:
+        x.fill_(0xff)
+    s.synchronize()
+    assert same(got, want)
+    a.lay.poll_status()
