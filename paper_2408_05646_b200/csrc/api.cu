@@ -1286,13 +1286,15 @@ ea_status eigen_attn_set_alibi(eigen_attn_t h, const float* slopes, void* cuda_s
   bool any = false;
   for (int i = 0; i < H && slopes && h->bias_buf; ++i)
     if (slopes[i] != 0.f) return fail(h, EA_ERR_INVALID_ARG, "set_alibi: the layer has a learned bias (eigen_attn_bias_attach)");
-  ++h->position_writes;
+  for (int i = 0; i < H && slopes; ++i) {
+    if (!(slopes[i] >= 0.f) || !isfinite(slopes[i])) return fail(h, EA_ERR_INVALID_ARG, "set_alibi: slope[%d] = %g", i, slopes[i]);
+    any = any || slopes[i] != 0.f;
+  }
+  if (any || h->alibi) ++h->position_writes;               // (none to none changes nothing that a training pass goes by)
   for (int i = 0; i < H; ++i) {
     const float sl = slopes ? slopes[i] : 0.f;
-    if (!(sl >= 0.f) || !isfinite(sl)) return fail(h, EA_ERR_INVALID_ARG, "set_alibi: slope[%d] = %g", i, sl);
     h->L.heads[i].alibi_slope2 = static_cast<float>(static_cast<double>(sl) * 1.4426950408889634);
     h->L.heads[i].alibi_slope = sl;
-    any = any || sl != 0.f;
   }
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaMemcpyAsync(h->ws + h->L.off_heads, h->L.heads.data(), sizeof(HeadInfo) * H, cudaMemcpyHostToDevice, s);
@@ -1996,8 +1998,8 @@ ea_status eigen_attn_bias_attach(eigen_attn_t h, int32_t n_buckets, int32_t max_
                                  void* cuda_stream) {
   if (!h) return EA_ERR_INVALID_ARG;
   if (!d_buf) {              // detach
+    if (h->bias_buf) ++h->position_writes;
     h->bias_buf = nullptr;
-    ++h->position_writes;
     return EA_OK;
   }
   if (h->rope) return fail(h, EA_ERR_INVALID_ARG, "bias_attach: the layer has a rotary embedding");
