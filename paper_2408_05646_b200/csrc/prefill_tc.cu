@@ -22,6 +22,10 @@ using namespace tc;
 
 // ---------------------------------------------------------------- the kernel
 
+// BIAS: a learned bias of relative positions, in an instance of its own (decided at run time, it cost layers without one 56
+// registers for 40: 2 x 2048 tokens, 32 heads of rank 80 271 us, so 314, of rank 128 625 and 652; with one, 32 buckets up to 128
+// tokens apart, 270 and 567).
+template <bool BIAS>
 __global__ void __launch_bounds__(kThreads) prefill_tc_kernel(const PrefillParams p) {
   extern __shared__ __align__(1024) unsigned char smem[];
   TcSmemHeader* hdr = reinterpret_cast<TcSmemHeader*>(smem);
@@ -70,9 +74,18 @@ __global__ void __launch_bounds__(kThreads) prefill_tc_kernel(const PrefillParam
 
   const int my_pos = len0 + t0 + tid;                      // last key this thread's query sees
   const float slope2 = hd.alibi_slope2;                      // ALiBi: slope * (key - query position), log2 domain
-  const float* bias = p.bias != nullptr ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;   // or a learned bias
-  auto position = [&](int key) {
-    return bias != nullptr ? __ldg(bias + min(max(my_pos - key, 0), p.bias_len - 1)) : slope2 * static_cast<float>(key - my_pos);
+  const float* bias = BIAS ? p.bias + static_cast<int64_t>(h) * p.bias_len : nullptr;
+  const float far_bias = BIAS ? __ldg(bias + p.bias_len - 1) : 0.f;
+  // biases of the keys key0 .. key0 + 15, on their way beside the scores' load; one number where all of the block's queries have
+  // them in the last bucket
+  auto fetch_bias = [&](float (&at)[16], int key0) {
+    if (len0 + t0 - key0 - 15 >= p.bias_len - 1) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) at[i] = far_bias;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) at[i] = __ldg(bias + min(max(my_pos - key0 - i, 0), p.bias_len - 1));
+    }
   };
   const int n_keys = len0 + min(p.T, t0 + kTile);          // keys the block needs
   const int n_tiles = (n_keys + kTile - 1) / kTile;
@@ -107,11 +120,13 @@ __global__ void __launch_bounds__(kThreads) prefill_tc_kernel(const PrefillParam
 #pragma unroll 1
     for (int c0 = 0; c0 < kTile; c0 += 16) {
       uint32_t r[16];
+      float at[16];
       tmem_ld16(tS + c0, r);
+      if (BIAS) fetch_bias(at, key0 + c0);
       tmem_wait_ld();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float s = fmaf(__uint_as_float(r[i]), p.scale_log2, position(key0 + c0 + i));
+        float s = fmaf(__uint_as_float(r[i]), p.scale_log2, BIAS ? at[i] : slope2 * static_cast<float>(key0 + c0 + i - my_pos));
         if (diag && key0 + c0 + i > my_pos) s = -INFINITY;
         row_max = fmaxf(row_max, s);
       }
@@ -122,12 +137,14 @@ __global__ void __launch_bounds__(kThreads) prefill_tc_kernel(const PrefillParam
 #pragma unroll 1
     for (int c0 = 0; c0 < kTile; c0 += 16) {
       uint32_t r[16];
+      float at[16];
       tmem_ld16(tS + c0, r);
+      if (BIAS) fetch_bias(at, key0 + c0);
       tmem_wait_ld();
       float pr[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float s = fmaf(__uint_as_float(r[i]), p.scale_log2, position(key0 + c0 + i)) - m_new;
+        float s = fmaf(__uint_as_float(r[i]), p.scale_log2, BIAS ? at[i] : slope2 * static_cast<float>(key0 + c0 + i - my_pos)) - m_new;
         if (diag && key0 + c0 + i > my_pos) s = -INFINITY;
         pr[i] = ex2(s);
         row_sum += pr[i];
@@ -290,11 +307,15 @@ size_t prefill_tc_smem_bytes(int max_rp_k, int max_rp_v) {
 cudaError_t launch_prefill_tc(const PrefillParams& p, int max_rp_k, int max_rp_v, cudaStream_t s,
                               uint64_t* launches) {
   const size_t smem = prefill_tc_smem_bytes(max_rp_k, max_rp_v);
-  static size_t configured[kMaxDevices] = {};
-  const cudaError_t ec = ensure_dynamic_smem(prefill_tc_kernel, smem, configured);
+  static size_t configured[2][kMaxDevices] = {};
+  auto run = [&](auto kernel, size_t (&done)[kMaxDevices]) -> cudaError_t {
+    const cudaError_t e = ensure_dynamic_smem(kernel, smem, done);
+    if (e != cudaSuccess) return e;
+    kernel<<<dim3(p.B * p.H, (p.T + kTile - 1) / kTile), kThreads, smem, s>>>(p);
+    return cudaSuccess;
+  };
+  const cudaError_t ec = p.bias != nullptr ? run(prefill_tc_kernel<true>, configured[1]) : run(prefill_tc_kernel<false>, configured[0]);
   if (ec != cudaSuccess) return ec;
-  dim3 grid(p.B * p.H, (p.T + kTile - 1) / kTile);
-  prefill_tc_kernel<<<grid, kThreads, smem, s>>>(p);
   ++*launches;
   return cudaGetLastError();
 }
