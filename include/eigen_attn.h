@@ -466,7 +466,9 @@ typedef enum {
                                  rows per K/V head on, unless an ALiBi bias is set or pages do not divide n_max; warp-level
                                  products otherwise), 1 = always the warp-level products                     */
   EA_OPT_TEST_WAIT_GIVES_UP = 7 /* failure-path test hook.  1 arms it for the NEXT eigen_attn_decode /
-                                 _decode_step / _decode_static launch only: one warp of one CTA treats its
+                                 _decode_step / _decode_static launch, or 16-bit layer's train_forward or
+                                 train_backward, only: one warp of one CTA (of train_backward: of the first CTA in
+                                 its items of keys, of the last in its items of queries) treats its
                                  first wait for a tile as having exceeded the bound.  The launch then ends the
                                  way a real timeout ends it (the CTA stops computing, the producer waits for
                                  its copies in flight, the kernel returns), the call's output is undefined and

@@ -264,7 +264,7 @@ struct eigen_attn {
   int page_shift = 0, page_width = 0;
   std::vector<int32_t> page_cap;      // [B]: rows sequence b can hold = leading mapped pages * page_rows
   int64_t opt_min_copy = -1;  // EA_OPT_DECODE_MIN_COPY_BYTES; < 0 = the built-in default
-  int64_t opt_give_up = 0;   // EA_OPT_TEST_WAIT_GIVES_UP: armed for the next split-KV decode launch
+  int64_t opt_give_up = 0;   // EA_OPT_TEST_WAIT_GIVES_UP: armed for the next split-KV decode or 16-bit training launch
   int64_t opt_gqa_impl = 0;  // EA_OPT_GQA_IMPL
   int64_t opt_tree_impl = 0; // EA_OPT_TREE_IMPL
   uint64_t launches = 0;
@@ -2189,6 +2189,8 @@ ea_status eigen_attn_train_forward(eigen_attn_t h, const void* d_q, const void* 
   if (h->desc.dtype == EA_FP32) {
     e = ea::launch_train_simt_forward(p, s, &h->launches);
   } else {
+    p.give_up_once = h->opt_give_up ? 1 : 0;
+    h->opt_give_up = 0;                // one launch only
     e = ea::launch_train_pack(p, false, s, &h->launches);
     if (e == cudaSuccess) e = ea::launch_train_tc_forward(p, s, &h->launches);
   }
@@ -2216,6 +2218,8 @@ ea_status eigen_attn_train_backward(eigen_attn_t h, const void* d_dout, void* d_
   if (h->desc.dtype == EA_FP32) {
     e = ea::launch_train_simt_backward(p, s, &h->launches);
   } else {
+    p.give_up_once = h->opt_give_up ? 1 : 0;
+    h->opt_give_up = 0;                // one launch only
     e = ea::launch_train_pack(p, true, s, &h->launches);
     if (e == cudaSuccess) e = ea::launch_train_tc_backward(p, s, &h->launches);
   }

@@ -535,6 +535,7 @@ struct TrainParams {
   void* dtable;             // [H][buckets] gradient of the table, or NULL
   int32_t alibi;
   int32_t sm_count;
+  int32_t give_up_once;     // test hook of the tensor-core kernels: one warp reports its first wait as run out
   int* status;
 };
 // Tokens of sequence b, as the forward pass left them.  (Its launch may have been captured and not replayed yet.)

@@ -292,18 +292,35 @@ __device__ __forceinline__ void end(uint32_t tmem, int warp) {
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, 512);
 }
+// A wait for products or copies under way, which come to an end by themselves.  It has the bound of every wait, but does not end
+// when another one gave up: that is when it is needed.
+__device__ __noinline__ void wait_landed(unsigned long long* bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity)) return;
+  const uint64_t t0 = global_ns();
+  while (!mbar_try_wait(bar, parity))
+    if (global_ns() - t0 > kWaitBoundNs) return;
+}
 // The end of an issuing warp: nothing of it is under way when the CTA leaves.
-__device__ __forceinline__ void drain(TrHeader* hdr, int which, bool lead, int* status) {
+__device__ __forceinline__ void drain(TrHeader* hdr, int which, bool lead) {
   if (lead) mma_commit(&hdr->drain[which]);
   __syncwarp();
-  wait_all(&hdr->drain[which], 0, status);
+  wait_landed(&hdr->drain[which], 0);
+  __syncwarp();
 }
-// The end of a copying warp that gave up: copies in flight must land before the CTA leaves.  (Otherwise their consumers have
-// waited for all of them.)
-__device__ __forceinline__ void drain_copies(TrHeader* hdr, const Plan& plan, int items, int issued, int* status) {
-  for (int s = 0; s < plan.sets && s < items; ++s)
-    mbar_wait(&hdr->own_full[s], set_phase(plan, items - 1 - ((items - 1 - s) % plan.sets)), status);
-  for (int s = 0; s < plan.stages && s < issued; ++s) mbar_wait(&hdr->full[s], ((issued - 1 - s) / plan.stages) & 1u, status);
+// The end of a copying warp: all of its copies have landed before the CTA leaves, or goes over to the other kind of items.  (Their
+// consumers wait for them too, but not those that gave up.)  `items`: phases of own_full that were begun.
+__device__ __forceinline__ void drain_copies(TrHeader* hdr, const Plan& plan, int items, int issued, int lane) {
+  if (lane == 0) {
+    for (int s = 0; s < plan.sets && s < items; ++s) wait_landed(&hdr->own_full[s], set_phase(plan, items - 1 - ((items - 1 - s) % plan.sets)));
+    for (int s = 0; s < plan.stages && s < issued; ++s) wait_landed(&hdr->full[s], ((issued - 1 - s) / plan.stages) & 1u);
+  }
+  __syncwarp();
+}
+// Test hook: a softmax warp gives up at its first item, as if that wait had run out.
+__device__ __forceinline__ bool gives_up(const TrainParams& p, bool here, int it, int lane) {
+  if (p.give_up_once == 0 || !here || it > 0) return false;
+  if (lane == 0) atomicExch(p.status, kStatusTimeout);
+  return true;
 }
 
 // ---------------------------------------------------------------- forward
@@ -385,7 +402,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) { ++it; break; }
     }
-    if (!ok && lane == 0) drain_copies(hdr, plan, it, issued, p.status);
+    drain_copies(hdr, plan, ok ? it + 1 : it, issued, lane);  // (the last phase ended the list)
   } else if (warp >= kIssueWarp && warp < kIssueWarp + 2) {
     const int x = warp - kIssueWarp;                         // the products of one tile of queries
     const bool lead = elect_one();
@@ -444,7 +461,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
         next.next(plan.stages);
       }
     }
-    drain(hdr, x, lead, p.status);
+    drain(hdr, x, lead);
   } else if (warp < kSoftmaxWarps) {
     const int x = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -455,6 +472,7 @@ __global__ void __launch_bounds__(kTrThreads, 1) train_forward_kernel(const __gr
     for (int it = 0; ok; ++it) {
       const int set = set_of(plan, it);
       ok = wait_called(&hdr->own_full[set], set_phase(plan, it), p.status);
+      if (gives_up(p, blockIdx.x == 0 && warp == 0, it, lane)) ok = false;
       if (!ok) break;
       const Item item = hdr->item[set];
       if (item.tiles[0] < 0) break;
@@ -710,7 +728,7 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
       if (!ok) { ++it; break; }
     }
     if (!ok) index = 0x7fffffff;                             // (and none of the other kind)
-    if (!ok && lane == 0) drain_copies(hdr, plan, it, issued, p.status);
+    drain_copies(hdr, plan, ok ? it + 1 : it, issued, lane);  // (the last phase ended the list)
   } else if (warp >= kIssueWarp) {
     const int role = warp - kIssueWarp;                      // S^T; dv'; G^T and dk'
     const bool lead = elect_one();
@@ -799,7 +817,7 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
       done += total;
       sums += total > 0;
     }
-    drain(hdr, role, lead, p.status);
+    drain(hdr, role, lead);
   } else {
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -810,6 +828,7 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
     for (int it = 0; ok; ++it) {
       const int set = set_of(plan, it);
       ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
+      if (gives_up(p, blockIdx.x == 0 && warp == 0, it, lane)) ok = false;
       if (!ok) break;
       const int total = hdr->item[set].tiles[0], per_head = hdr->item[set].tiles[1], h = hdr->item[set].h;
       if (total < 0) break;
@@ -881,7 +900,10 @@ __device__ __forceinline__ void dkv_items(const TrainParams& p, const Plan& plan
         tmem_st16(tP, w[0]);
         tmem_st16(tP + 16, w[1]);
         ok = wait_all(&hdr->g_full[half], phase, p.status);
-        if (!ok) break;
+        if (!ok) {
+          tmem_wait_st();
+          break;
+        }
         tc_fence_after();
         tmem_ld32(tG, r[0]);
         tmem_ld32(tG + 32, r[1]);
@@ -1015,7 +1037,7 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) { ++it; break; }
     }
-    if (!ok && lane == 0) drain_copies(hdr, plan, it, issued, p.status);
+    drain_copies(hdr, plan, ok ? it + 1 : it, issued, lane);  // (the last phase ended the list)
   } else if (warp >= kIssueWarp) {
     const int role = warp - kIssueWarp;                      // S; dq'; G
     const bool lead = elect_one();
@@ -1077,7 +1099,7 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
       done += nt;
       sums += nt > 0;
     }
-    drain(hdr, role, lead, p.status);
+    drain(hdr, role, lead);
   } else {
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -1090,6 +1112,7 @@ __device__ __forceinline__ void dq_items(const TrainParams& p, const Plan& plan,
     for (int it = 0; ok; ++it) {
       const int set = set_of(plan, it);
       ok = wait_all(&hdr->own_full[set], set_phase(plan, it), p.status);
+      if (gives_up(p, blockIdx.x == gridDim.x - 1 && warp == 0, it, lane)) ok = false;
       if (!ok) break;
       const int nt = hdr->item[set].tiles[0], h = hdr->item[set].h, unit = hdr->item[set].unit, tile = hdr->item[set].tile;
       if (nt < 0) break;

@@ -45,3 +45,28 @@ def test_scratch_that_is_replaced_while_another_stream_has_a_pass_to_run(dtype, 
     s.synchronize()
     assert same(got, want)
     a.lay.poll_status()
+
+
+@pytest.mark.parametrize("group,bias", [(1, True), (4, False)])
+@pytest.mark.parametrize("r", [40, 112])
+@pytest.mark.parametrize("call", ["forward", "backward", "both"])
+def test_a_wait_that_runs_out_is_reported_once_and_the_layer_recovers(call, r, group, bias):
+    """One softmax warp reports its first wait as run out (the library's own hook): every other wait of its CTA then gives up, with
+    products and copies of other warps under way.  The launch ends, the timeout is reported once, and the next step is right."""
+    from paper_2408_05646_b200 import binding
+    s = Step(4, 1200, [r] * 4, [r] * 4, 128, BF, group, bias, seed=6, lens=[1200, 700, 1, 1199])
+    want = s.run()
+    s.lay.poll_status()
+    for _ in range(3):
+        if call != "backward":
+            s.lay.set_option(binding.EA_OPT_TEST_WAIT_GIVES_UP, 1)
+        s.lay.train_forward(*s.x[:3], lens=s.lens, group=group)
+        if call != "forward":
+            s.lay.set_option(binding.EA_OPT_TEST_WAIT_GIVES_UP, 1)
+            s.lay.train_backward(s.x[3], bias_grad=bias)
+        with pytest.raises(binding.EigenAttnError) as e:
+            s.lay.poll_status()
+        assert e.value.status == binding.EA_ERR_TIMEOUT
+        s.lay.poll_status()
+        assert same(s.run(), want)                           # the hook was armed for one launch
+        s.lay.poll_status()
