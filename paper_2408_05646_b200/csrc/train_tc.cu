@@ -17,9 +17,11 @@
 //   * eight softmax warps.  P and dS go back to TMEM as the A operand of the next product and never touch shared memory.
 // The backward pass has two kinds of items, one that owns a tile of keys (dk', dv': four products per pair of tiles) and one that
 // owns a tile of queries (dq': three, S and do' v' a second time): the alternative, dq' added up in memory by every tile of keys,
-// moves 512 r bytes of fp32 additions per pair of tiles through L2 and leaves sums whose order changes from run to run.
-// 4 x 4096 tokens, 32 heads, rank 80: forward 514 us, a backward call 1249, 74 of them packing (690 TFLOP/s of the five products
-// that the formulas need); tensor pipe busy 34 and 48 % of the time, exponentials 55 and 44 %, an instruction issued in 0.40 and
+// moves 512 r bytes of fp32 additions per pair of tiles through L2 and needs turns for sums whose order does not change from run to run (not
+// built).
+// 4 x 4096 tokens, 32 heads, rank 80: forward 514 us, a backward call 1257 in a burst and 1425 under the power limit, 74 of them
+// packing (684 and 603 TFLOP/s of the five products that the formulas need); tensor pipe busy 34 and 48 % of the time, exponentials
+// 55 and 44 %, an instruction issued in 0.40 and
 // 0.37 of the clocks.  What is left is the chain of a half tile, product, load, exponentials, store, product, of which two
 // run at a time (some 4700 clocks for a pair of tiles, its key item and its query item together, against 2640 of their products).
 // Tried and slower: three chains (a third fewer registers for each), sixteen softmax warps with half the columns, turns between
@@ -28,7 +30,8 @@
 //
 // Tiles carry a power of two each (2^e).  What is accumulated over tiles needs one scale: the tile's deviation from the
 // smallest exponent of all goes into the factors that P and dS are formed with, where it costs nothing.
-// Every wait is bounded; one that runs out ends every other one of the launch through the status word.
+// Every wait is bounded; one that runs out ends every other one of the launch through the status word, but for those that see
+// products and copies under way to their end.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
