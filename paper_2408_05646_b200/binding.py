@@ -684,9 +684,10 @@ class EigenAttnLayer:
 
     # -- training: attention over rank-space rows with its backward pass
     def train_attach(self, max_tokens: int, group: int = 1, stream=None) -> torch.Tensor:
-        """Allocates the scratch of the training calls for up to `max_tokens` tokens (kept on the layer) and attaches it.  Passes
-        that other streams still have to run keep the memory of one that is replaced or detached; a captured graph that is to be
-        replayed needs it kept by the caller."""
+        """Allocates the scratch of the training calls for up to `max_tokens` tokens (kept on the layer) and attaches it.  It
+        belongs to `stream`, as results do: another stream that runs passes waits for it first.  Passes that streams still have to
+        run keep the memory of a scratch that is replaced or detached; a captured graph that is to be replayed needs it kept by
+        the caller."""
         n = _sz(0)
         self._check(lib.eigen_attn_train_bytes(self.handle, int(max_tokens), int(group), ctypes.byref(n)), "eigen_attn_train_bytes")
         with torch.cuda.stream(stream):

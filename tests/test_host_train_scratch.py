@@ -27,7 +27,7 @@ def lib(tmp_path_factory):
 
 
 def launches(lib):
-    """Words of the first argument of every launch since the last question."""
+    """Words of the first argument of every training kernel's launch since the last question."""
     out = []
     for i in range(lib.fake_launches()):
         words = (ctypes.c_size_t * WORDS)()
